@@ -7,7 +7,9 @@
  * most recent queries - and keeping the best keys together with the recent
  * window (Sections 4.1-4.3, Appendix D.2).  This library implements the two
  * data-parallel parts of that step for a whole model (all layers, batch rows
- * and KV heads at once):
+ * and KV heads at once), and the attention of a decode loop over the caches
+ * that it compacts, with eviction by accumulated attention weight as a second
+ * rule (bkv_attend, bkv_attend_shared, bkv_evict):
  *
  *   beacon maintenance  - FPS seeding from prompt queries (Appendix D.1,
  *                         Algorithm 1) and, per decode query, nearest-beacon
@@ -258,6 +260,95 @@ int bkv_compress_ragged(bkv_ctx* ctx, void* K, void* V, const int32_t* L, int32_
                         const void* q_recent, const int64_t* recent_pos, int32_t* kept_idx_out, float* scores_out);
 
 /*
+ * Decode-time attention over the caches that this library compacts.  One call
+ * is one layer: each sequence of the batch brings the queries of its n_q
+ * newest tokens (n_q = 1 in plain decoding, a few draft tokens, or a whole
+ * prompt), whose own K and V rows are already the last rows of its caches.
+ *   z(i, j)    = scale * q_i . k_j over the rows j < len - n_q + 1 + i that
+ *                query i sees (causal among the new tokens);
+ *   lse_i      = log sum_j exp z(i, j);     o_i = sum_j exp(z(i, j) - lse_i) v_j;
+ *   weights[j] += sum over the group's G query heads and the n_q queries of
+ *                exp(z(i, j) - lse_i), the accumulated attention weight that
+ *                bkv_evict goes by.
+ * A query that sees no row gets o = 0 and lse = -infinity and adds nothing.
+ *   q            bf16 [batch][n_q_heads][n_q][head_dim], rotated as the keys are.
+ *   K, V         bf16 [batch][n_kv_heads][capacity][head_dim], one layer's slice
+ *                of the caches.  Rows at or past a cache's length are never
+ *                used, whatever they hold; the rows below it must be finite.
+ *   len          DEVICE int32 [batch][n_kv_heads]: rows of each cache, 0 ..
+ *                capacity.  A length outside that range counts as 0 and the
+ *                next bkv_sync returns BKV_EINVAL.
+ *   scale        finite, > 0; 0 stands for 1 / sqrt(head_dim).
+ *   o            bf16 [batch][n_q_heads][n_q][head_dim].
+ *   lse_out      fp32 [batch][n_q_heads][n_q] or NULL (natural logarithm).
+ *   weights      fp32 [batch][n_kv_heads][capacity] or NULL; rows at or past a
+ *                cache's length are not touched.
+ * The logits, softmax statistics, output sums and weights are kept in fp32;
+ * the attention weights are rounded to bf16 where they multiply V.  Results do
+ * not depend on the order in which the GPU runs its blocks.
+ * The softmax here is over the queries' own causal rows; the beacon state and
+ * the context's n_beacons, window, n_prefix and rope_theta play no part.
+ * BKV_ESTATE when the workspace that bkv_attend_reserve made is too small.
+ */
+int bkv_attend(bkv_ctx* ctx, const void* q, int32_t n_q, const void* K, const void* V, const int32_t* len, double scale,
+               void* o, float* lse_out, float* weights);
+
+/*
+ * bkv_attend for sequences that continue a common prefix (several samples of
+ * one prompt): batch rows [g * batch / n_groups, (g + 1) * batch / n_groups)
+ * share prefix g, whose K and V exist once and are read once for all of them.
+ * Every query sees all prefix_len[g] prefix rows, then its own rows as in
+ * bkv_attend; the softmax runs over both.  Only own rows accumulate weights
+ * (a shared row cannot be evicted for one sequence alone).
+ *   Kp, Vp       bf16 [n_groups][n_kv_heads][prefix_capacity][head_dim], with
+ *                the same rules as K and V.
+ *   prefix_len   DEVICE int32 [n_groups], 0 .. prefix_capacity, checked as len is.
+ *   n_groups     >= 1, divides the context's batch.
+ */
+int bkv_attend_shared(bkv_ctx* ctx, const void* q, int32_t n_q, const void* Kp, const void* Vp, const int32_t* prefix_len,
+                      int32_t n_groups, int32_t prefix_capacity, const void* K, const void* V, const int32_t* len,
+                      double scale, void* o, float* lse_out, float* weights);
+
+/*
+ * Makes the workspace of bkv_attend (n_groups = 0) or bkv_attend_shared for
+ * calls with n_q queries per head, with or without weights.  The workspace only
+ * grows, so a reservation for the largest call serves the smaller ones of the
+ * same kind.  Waits for the context's stream when it has to reallocate; call it
+ * before capturing a graph.  BKV_ENOMEM leaves the previous workspace in place.
+ */
+int bkv_attend_reserve(bkv_ctx* ctx, int32_t n_q, int32_t n_groups, int weights);
+
+/*
+ * Eviction by accumulated attention weight, for every instance's cache of all
+ * layers: of the L rows, the first n_prefix, the last `window` and the (budget
+ * - n_prefix - window) others with the largest weight stay, in ascending order
+ * (ties to the lower index, -0 equal to 0, a NaN weight counted as the
+ * largest).  Row i of K_out, V_out and weights_out then holds what row kept[i]
+ * of K, V and weights held.  An instance with L <= budget keeps all its rows.
+ *   K, V          bf16 [n_layers][batch][n_kv_heads][capacity][head_dim].
+ *   weights       fp32 [n_layers][batch][n_kv_heads][capacity].
+ *   L             DEVICE int32 [n_layers][batch][n_kv_heads]: rows of each
+ *                 instance, 0 .. capacity.  A length outside that range leaves
+ *                 the instance's outputs untouched except kept_idx_out, all -1,
+ *                 and len_out, 0; the next bkv_sync returns BKV_EINVAL.
+ *   budget        >= max(1, n_prefix + window).
+ *   K_out, V_out, weights_out  the compacted caches, [n_layers][batch]
+ *                 [n_kv_heads][capacity_out] rows, with capacity_out >=
+ *                 min(budget, capacity).  Either all three are K, V and weights
+ *                 themselves (in place; capacity_out = capacity) or none of
+ *                 them overlaps an input or another output.  Rows of K_out and
+ *                 V_out past the kept ones keep what they held; those of
+ *                 weights_out become 0, ready for the tokens to come.
+ *   kept_idx_out  int32 [n_layers][batch][n_kv_heads][budget]: kept rows, then -1.
+ *   len_out       int32 [n_layers][batch][n_kv_heads] or NULL: min(L, budget).
+ *                 It may be L itself.
+ * The beacon state plays no part.
+ */
+int bkv_evict(bkv_ctx* ctx, const void* K, const void* V, const float* weights, const int32_t* L, int32_t budget,
+              void* K_out, void* V_out, float* weights_out, int32_t capacity_out, int32_t* kept_idx_out,
+              int32_t* len_out);
+
+/*
  * Copies the beacon state to / from caller buffers (checkpoint / resume):
  *   centroids fp32 [n_inst][n_beacons][head_dim]
  *   sums      fp64 [n_inst][n_beacons][head_dim]
@@ -290,7 +381,8 @@ int bkv_set_cfps_state(bkv_ctx* ctx, const void* buffers, const int32_t* sizes);
  * Waits for the context's stream, then reads and clears the device error
  * word.  Returns BKV_OK, BKV_ETIMEOUT (a kernel gave up a bounded wait and
  * its outputs are invalid), BKV_EINVAL (a per-instance length of
- * bkv_compress_ragged outside 1..capacity), BKV_EBOUNDS (a library built with
+ * bkv_compress_ragged outside 1..capacity, or of bkv_attend, bkv_attend_shared
+ * or bkv_evict outside 0..capacity), BKV_EBOUNDS (a library built with
  * BKV_CHECKED found an index from device data out of range, skipped that
  * access, and the outputs are invalid) or BKV_ECUDA.
  */
@@ -332,10 +424,11 @@ int bkv_selftest_bounds(bkv_ctx* ctx);
 
 /*
  * Allocation-failure hook (test diagnostic).  With nth > 0, the nth device
- * or pinned host allocation that later bkv_create calls attempt (counted
- * from this call, across contexts) fails as if memory ran out, without
- * allocating: that bkv_create releases what it had allocated, leaves *out
- * NULL and returns BKV_ENOMEM.  The hook disarms itself after that one
+ * or pinned host allocation that later bkv_create and bkv_attend_reserve calls
+ * attempt (counted from this call, across contexts) fails as if memory ran
+ * out, without allocating: that bkv_create releases what it had allocated,
+ * leaves *out NULL and returns BKV_ENOMEM; that bkv_attend_reserve returns
+ * BKV_ENOMEM and leaves the workspace as it was.  The hook disarms itself after that one
  * failure; nth = 0 disarms it.  Not thread-safe with concurrent bkv_create
  * calls.  Returns BKV_OK, or BKV_EINVAL for nth < 0.
  */
@@ -357,7 +450,11 @@ int bkv_debug_fail_alloc(int32_t nth);
 #define BKV_K_KEEP_ALL 5
 #define BKV_K_CFPS 6 /* Continual FPS buffer update, beacon selection and merge */
 #define BKV_K_ROPE 7 /* rotary table of a compress, copied from pinned host memory */
-#define BKV_NUM_KERNELS 8
+#define BKV_K_ATTEND 8
+#define BKV_K_ATTEND_MERGE 9
+#define BKV_K_ATTEND_WEIGHTS 10
+#define BKV_K_EVICT 11
+#define BKV_NUM_KERNELS 12
 int bkv_profile_enable(bkv_ctx* ctx, int on);
 int bkv_profile_read(bkv_ctx* ctx, double* ms, int64_t* launches, int32_t n_kernels);
 

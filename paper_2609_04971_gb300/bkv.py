@@ -24,7 +24,8 @@ BKV_ETIMEOUT = -4
 BKV_ESTATE = -5
 BKV_EBOUNDS = -6
 
-KERNEL_NAMES = ("fps_init", "update", "qobs", "score", "select_gather", "keep_all", "cfps", "rope_stage")
+KERNEL_NAMES = ("fps_init", "update", "qobs", "score", "select_gather", "keep_all", "cfps", "rope_stage",
+                "attend", "attend_merge", "attend_weights", "evict")
 
 
 # bkv_config.flags options (include/bkv.h)
@@ -52,6 +53,7 @@ class BkvError(RuntimeError):
 _lib = None
 _lock = threading.Lock()
 _P = ctypes.c_void_p
+_streams: dict = {}  # stream handle of every live context, for outputs allocated on its behalf
 
 
 def load_library(path: str | None = None, build: bool = True):
@@ -77,6 +79,11 @@ def load_library(path: str | None = None, build: bool = True):
             "bkv_compress": (ctypes.c_int, [_P, _P, _P, ctypes.c_int32, ctypes.c_int32, ctypes.c_int64, _P, _P,
                                             _P, _P]),
             "bkv_compress_ragged": (ctypes.c_int, [_P, _P, _P, _P, ctypes.c_int32, _P, _P, _P, _P, _P]),
+            "bkv_attend": (ctypes.c_int, [_P, _P, ctypes.c_int32, _P, _P, _P, ctypes.c_double, _P, _P, _P]),
+            "bkv_attend_shared": (ctypes.c_int, [_P, _P, ctypes.c_int32, _P, _P, _P, ctypes.c_int32, ctypes.c_int32,
+                                                 _P, _P, _P, ctypes.c_double, _P, _P, _P]),
+            "bkv_attend_reserve": (ctypes.c_int, [_P, ctypes.c_int32, ctypes.c_int32, ctypes.c_int]),
+            "bkv_evict": (ctypes.c_int, [_P, _P, _P, _P, _P, ctypes.c_int32, _P, _P, _P, ctypes.c_int32, _P, _P]),
             "bkv_get_state": (ctypes.c_int, [_P, _P, _P, _P]),
             "bkv_set_state": (ctypes.c_int, [_P, _P, _P, _P]),
             "bkv_get_cfps_state": (ctypes.c_int, [_P, _P, _P]),
@@ -168,17 +175,22 @@ def bkv_last_error(ctx) -> str:
 
 def bkv_create(cfg: BkvConfig, stream=None) -> ctypes.c_void_p:
     out = ctypes.c_void_p()
-    _check(_l().bkv_create(ctypes.byref(cfg), _stream(stream), ctypes.byref(out)), "bkv_create")
+    handle = _stream(stream)
+    _check(_l().bkv_create(ctypes.byref(cfg), handle, ctypes.byref(out)), "bkv_create")
+    _streams[out.value] = handle.value or 0
     return out
 
 
 def bkv_destroy(ctx) -> None:
     if ctx:
+        _streams.pop(ctx.value, None)
         _l().bkv_destroy(ctx)
 
 
 def bkv_set_stream(ctx, stream=None) -> None:
-    _check(_l().bkv_set_stream(ctx, _stream(stream)), "bkv_set_stream", ctx)
+    handle = _stream(stream)
+    _check(_l().bkv_set_stream(ctx, handle), "bkv_set_stream", ctx)
+    _streams[ctx.value] = handle.value or 0
 
 
 def bkv_init_beacons(ctx, q_init: torch.Tensor, n_init: int) -> None:
@@ -217,6 +229,40 @@ def bkv_compress_ragged(ctx, K: torch.Tensor, V: torch.Tensor, L: torch.Tensor, 
                                     _ptr(q_recent, torch.bfloat16, "q_recent"), ctypes.cast(rp, _P),
                                     _ptr(kept_idx_out, torch.int32, "kept_idx_out"),
                                     _ptr(scores_out, torch.float32, "scores_out")), "bkv_compress_ragged", ctx)
+
+
+def bkv_attend_reserve(ctx, n_q: int, n_groups: int = 0, weights: bool = False) -> None:
+    _check(_l().bkv_attend_reserve(ctx, int(n_q), int(n_groups), int(bool(weights))), "bkv_attend_reserve", ctx)
+
+
+def bkv_attend(ctx, q: torch.Tensor, n_q: int, K: torch.Tensor, V: torch.Tensor, length: torch.Tensor, scale: float,
+               o: torch.Tensor, lse_out: torch.Tensor | None = None, weights: torch.Tensor | None = None) -> None:
+    bf16, f32 = torch.bfloat16, torch.float32
+    _check(_l().bkv_attend(ctx, _ptr(q, bf16, "q"), int(n_q), _ptr(K, bf16, "K"), _ptr(V, bf16, "V"),
+                           _ptr(length, torch.int32, "length"), float(scale), _ptr(o, bf16, "o"),
+                           _ptr(lse_out, f32, "lse_out"), _ptr(weights, f32, "weights")), "bkv_attend", ctx)
+
+
+def bkv_attend_shared(ctx, q: torch.Tensor, n_q: int, Kp: torch.Tensor, Vp: torch.Tensor, prefix_len: torch.Tensor,
+                      n_groups: int, prefix_capacity: int, K: torch.Tensor, V: torch.Tensor, length: torch.Tensor,
+                      scale: float, o: torch.Tensor, lse_out: torch.Tensor | None = None,
+                      weights: torch.Tensor | None = None) -> None:
+    bf16, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    _check(_l().bkv_attend_shared(ctx, _ptr(q, bf16, "q"), int(n_q), _ptr(Kp, bf16, "Kp"), _ptr(Vp, bf16, "Vp"),
+                                  _ptr(prefix_len, i32, "prefix_len"), int(n_groups), int(prefix_capacity),
+                                  _ptr(K, bf16, "K"), _ptr(V, bf16, "V"), _ptr(length, i32, "length"), float(scale),
+                                  _ptr(o, bf16, "o"), _ptr(lse_out, f32, "lse_out"), _ptr(weights, f32, "weights")),
+           "bkv_attend_shared", ctx)
+
+
+def bkv_evict(ctx, K: torch.Tensor, V: torch.Tensor, weights: torch.Tensor, L: torch.Tensor, budget: int,
+              K_out: torch.Tensor, V_out: torch.Tensor, weights_out: torch.Tensor, capacity_out: int,
+              kept_idx_out: torch.Tensor, len_out: torch.Tensor | None = None) -> None:
+    bf16, f32, i32 = torch.bfloat16, torch.float32, torch.int32
+    _check(_l().bkv_evict(ctx, _ptr(K, bf16, "K"), _ptr(V, bf16, "V"), _ptr(weights, f32, "weights"),
+                          _ptr(L, i32, "L"), int(budget), _ptr(K_out, bf16, "K_out"), _ptr(V_out, bf16, "V_out"),
+                          _ptr(weights_out, f32, "weights_out"), int(capacity_out), _ptr(kept_idx_out, i32, "kept"),
+                          _ptr(len_out, i32, "len_out")), "bkv_evict", ctx)
 
 
 def bkv_get_state(ctx, centroids=None, sums=None, counts=None) -> None:
@@ -431,6 +477,97 @@ class BeaconKV:
             kept_out = torch.empty(c.n_layers, c.batch, c.n_kv_heads, budget, dtype=torch.int32, device=K.device)
         bkv_compress_ragged(self.ctx, K, V, L, budget, t_pos, q_recent, recent_pos, kept_out, scores_out)
         return kept_out
+
+    # ------------------------------------------------------------ attention over the caches
+    def _empty(self, *shape, dtype, like: torch.Tensor) -> torch.Tensor:
+        """A new output, from the allocator pool of the context's stream (its memory may have been freed
+        by work that is only ordered on that stream)."""
+        stream = _streams[self.ctx.value]
+        if torch.cuda.current_stream(like.device).cuda_stream == stream:
+            return torch.empty(shape, dtype=dtype, device=like.device)
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=like.device)):
+            return torch.empty(shape, dtype=dtype, device=like.device)
+
+    def reserve_attend(self, *, n_q: int = 1, n_groups: int = 0, weights: bool = False):
+        """Workspace for attend (n_groups = 0) or attend_shared with n_q queries per head; needed once
+        before the first call of that size (bkv_attend_reserve)."""
+        bkv_attend_reserve(self.ctx, n_q, n_groups, weights)
+
+    def _attend_args(self, q, K, V, length, weights, o_out, lse_out):
+        c = self.cfg
+        if q.dim() != 4 or q.shape[0] != c.batch or q.shape[1] != c.n_q_heads or q.shape[3] != c.head_dim:
+            raise ValueError(f"q must be [batch = {c.batch}, n_q_heads = {c.n_q_heads}, n_q, head_dim = "
+                             f"{c.head_dim}], got {tuple(q.shape)}")
+        n_q = q.shape[2]
+        inst, rows = c.batch * c.n_kv_heads, c.batch * c.n_q_heads * n_q
+        self._expect(K, inst * c.capacity * c.head_dim, "K")
+        self._expect(V, inst * c.capacity * c.head_dim, "V")
+        self._expect(length, inst, "length")
+        self._expect(weights, inst * c.capacity, "weights")
+        self._expect(o_out, rows * c.head_dim, "o_out")
+        self._expect(lse_out, rows, "lse_out")
+        if not q.is_cuda:
+            raise TypeError("q must be a CUDA tensor")
+        if o_out is None:
+            o_out = self._empty(c.batch, c.n_q_heads, n_q, c.head_dim, dtype=torch.bfloat16, like=q)
+        if lse_out is None:
+            lse_out = self._empty(c.batch, c.n_q_heads, n_q, dtype=torch.float32, like=q)
+        return n_q, o_out, lse_out
+
+    def attend(self, q, K, V, *, length, scale=None, weights=None, o_out=None, lse_out=None):
+        """Attention of one layer's newest queries over its caches (bkv_attend): q [batch, n_q_heads, n_q,
+        head_dim], K and V [batch, n_kv_heads, capacity, head_dim], length int32 [batch, n_kv_heads];
+        weights fp32 [batch, n_kv_heads, capacity] is added to.  Returns (o, lse)."""
+        n_q, o, lse = self._attend_args(q, K, V, length, weights, o_out, lse_out)
+        bkv_attend(self.ctx, q, n_q, K, V, length, scale or 0.0, o, lse, weights)
+        return o, lse
+
+    def attend_shared(self, q, Kp, Vp, K, V, *, prefix_len, length, scale=None, weights=None, o_out=None,
+                      lse_out=None):
+        """attend for sequences that continue a shared prefix (bkv_attend_shared): Kp and Vp [n_groups,
+        n_kv_heads, prefix_capacity, head_dim], prefix_len int32 [n_groups].  Returns (o, lse)."""
+        c = self.cfg
+        n_q, o, lse = self._attend_args(q, K, V, length, weights, o_out, lse_out)
+        if Kp.dim() != 4 or Kp.shape[1] != c.n_kv_heads or Kp.shape[3] != c.head_dim:
+            raise ValueError(f"Kp must be [n_groups, n_kv_heads = {c.n_kv_heads}, prefix_capacity, head_dim = "
+                             f"{c.head_dim}], got {tuple(Kp.shape)}")
+        groups, pcap = Kp.shape[0], Kp.shape[2]
+        self._expect(Vp, Kp.numel(), "Vp")
+        self._expect(prefix_len, groups, "prefix_len")
+        bkv_attend_shared(self.ctx, q, n_q, Kp, Vp, prefix_len, groups, pcap, K, V, length, scale or 0.0, o, lse,
+                          weights)
+        return o, lse
+
+    def evict(self, K, V, weights, *, L, budget, K_out=None, V_out=None, weights_out=None, kept_out=None,
+              len_out=None):
+        """Eviction by accumulated weight (bkv_evict), in place or, with K_out, V_out and weights_out of
+        [n_layers, batch, n_kv_heads, capacity_out] rows, into another cache.  L: int32 CUDA tensor
+        [n_layers, batch, n_kv_heads].  Returns (kept rows, new lengths)."""
+        c = self.cfg
+        outs = (K_out, V_out, weights_out)
+        if any(t is None for t in outs) and any(t is not None for t in outs):
+            raise ValueError("K_out, V_out and weights_out come together or not at all")
+        if K_out is None:
+            K_out, V_out, weights_out = K, V, weights
+        rows = self.n_inst * c.capacity
+        self._expect(K, rows * c.head_dim, "K")
+        self._expect(V, rows * c.head_dim, "V")
+        self._expect(weights, rows, "weights")
+        self._expect(L, self.n_inst, "L")
+        cap_out = weights_out.numel() // self.n_inst
+        self._expect(weights_out, self.n_inst * cap_out, "weights_out")
+        self._expect(K_out, self.n_inst * cap_out * c.head_dim, "K_out")
+        self._expect(V_out, self.n_inst * cap_out * c.head_dim, "V_out")
+        self._expect(kept_out, self.n_inst * budget, "kept_out")
+        self._expect(len_out, self.n_inst, "len_out")
+        if not K.is_cuda:
+            raise TypeError("K must be a CUDA tensor")
+        if kept_out is None:
+            kept_out = self._empty(c.n_layers, c.batch, c.n_kv_heads, max(0, budget), dtype=torch.int32, like=K)
+        if len_out is None:
+            len_out = self._empty(c.n_layers, c.batch, c.n_kv_heads, dtype=torch.int32, like=K)
+        bkv_evict(self.ctx, K, V, weights, L, budget, K_out, V_out, weights_out, cap_out, kept_out, len_out)
+        return kept_out, len_out
 
     def state(self):
         c = self.cfg

@@ -5,7 +5,6 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
-#include <cstdarg>
 #include <cstdio>
 #include <cstring>
 #include <mutex>
@@ -13,114 +12,17 @@
 #include <vector>
 
 #include "bkv.h"
+#include "bkv_ctx.h"
 #include "bkv_device.cuh"
 #include "bkv_internal.h"
 
+using bkv::aligned16;
+using bkv::cuda_fail;
+using bkv::fail;
+using bkv::ProfScope;
 using bkv::Shape;
 
-struct bkv_ctx {
-  bkv_config cfg{};
-  Shape shape{};
-  cudaStream_t stream = nullptr;
-  int device = 0;
-  // beacon state
-  float* cent = nullptr;
-  double* sums = nullptr;
-  long long* counts = nullptr;
-  bool state_ready = false;
-  // Continual FPS (BKV_F_CONTINUAL_FPS): per-query-head buffers; cent / counts then hold each
-  // compress's beacons ([n_inst][G * n_beacons] rows, count 1 or 0) for the scoring-query build
-  bool cfps = false;
-  int b_min = 0, b_max = 0, n_heads = 0;
-  __nv_bfloat16* cbuf = nullptr;  // [n_heads][b_max][d]
-  int* csize = nullptr;           // [n_heads]
-  // scratch
-  __nv_bfloat16* qobs = nullptr;  // [n_inst][n_obs_pad][d]
-  uint32_t* valid = nullptr;      // [n_inst][4]
-  float* rscore = nullptr;        // [n_inst][cap]
-  double2* rope = nullptr;        // [W + 1][d / 2] fp64 (cos, sin), then the same table in fp32
-  int* err = nullptr;             // device error word
-  // pinned host staging of the rotary table, a ring of kRopeSlots: a compress fills the next slot,
-  // a kernel on the stream copies it to `rope` through the slot's device mapping, and the slot is
-  // refilled only after that copy's event completed
-  static constexpr int kRopeSlots = 4;
-  double2* rope_pinned[kRopeSlots] = {};
-  void* rope_mapped[kRopeSlots] = {};  // device address of rope_pinned[i]
-  cudaEvent_t rope_ev[kRopeSlots] = {};
-  bool rope_used[kRopeSlots] = {};
-  int rope_next = 0;
-  // per-instance lengths (bkv_compress_ragged): the instances a compress evicts from, and a rotary
-  // table per batch row followed by the causal gaps [batch][W] (int32), staged like `rope`
-  int* work = nullptr;            // [n_inst]
-  int* n_work = nullptr;          // [1]
-  unsigned char* rag = nullptr;   // device copy of the per-row tables and gaps
-  size_t rag_bytes = 0, rag_row = 0, rag_gaps_off = 0;  // total bytes; one row's table (double2 units); gaps offset
-  void* rag_pinned[kRopeSlots] = {};
-  void* rag_mapped[kRopeSlots] = {};
-  cudaEvent_t rag_ev[kRopeSlots] = {};
-  bool rag_used[kRopeSlots] = {};
-  int rag_next = 0;
-  cudaEvent_t switch_ev = nullptr;  // orders a new stream after the previous one (bkv_set_stream)
-  std::string last_error;
-  // per-kernel timing
-  struct Rec {
-    cudaEvent_t start, stop;
-    int kernel;
-  };
-  bool prof = false;
-  std::vector<Rec> pending;
-  std::vector<cudaEvent_t> spare;
-  double prof_ms[BKV_NUM_KERNELS] = {};
-  long long prof_n[BKV_NUM_KERNELS] = {};
-};
-
 namespace {
-
-int fail(bkv_ctx* c, int code, const char* fmt, ...) {
-  if (c) {
-    char buf[512];
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(buf, sizeof buf, fmt, ap);
-    va_end(ap);
-    c->last_error = buf;
-  }
-  return code;
-}
-
-int cuda_fail(bkv_ctx* c, cudaError_t e, const char* what) {
-  return fail(c, BKV_ECUDA, "%s: %s", what, cudaGetErrorString(e));
-}
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-cudaEvent_t take_event(bkv_ctx* c) {
-  if (!c->spare.empty()) {
-    cudaEvent_t ev = c->spare.back();
-    c->spare.pop_back();
-    return ev;
-  }
-  cudaEvent_t ev = nullptr;
-  cudaEventCreate(&ev);
-  return ev;
-}
-
-// Brackets one kernel launch with events when timing is enabled.
-struct ProfScope {
-  bkv_ctx* c;
-  int kernel;
-  cudaEvent_t start = nullptr;
-  ProfScope(bkv_ctx* ctx, int k) : c(ctx), kernel(k) {
-    if (c->prof && (start = take_event(c))) cudaEventRecord(start, c->stream);
-  }
-  ~ProfScope() {
-    if (!start) return;
-    cudaEvent_t stop = take_event(c);
-    if (!stop) return;
-    cudaEventRecord(stop, c->stream);
-    c->pending.push_back({start, stop, kernel});
-  }
-};
 
 void fold_profile(bkv_ctx* c) {
   for (auto& r : c->pending) {
@@ -178,27 +80,31 @@ int validate_config(const bkv_config* cfg, std::string& why) {
 }
 
 // Allocation-failure hook (bkv_debug_fail_alloc): once armed with n > 0, the n-th device or pinned
-// host allocation that bkv_create attempts reports cudaErrorMemoryAllocation without allocating,
-// and the hook disarms itself.
+// host allocation that bkv_create or bkv_attend_reserve attempts reports cudaErrorMemoryAllocation
+// without allocating, and the hook disarms itself.
 std::atomic<int> g_fail_nth{0};
 std::atomic<int> g_alloc_seen{0};
 
-bool fail_this_alloc() {
+}  // namespace
+
+bool bkv::fail_this_alloc() {
   const int nth = g_fail_nth.load();
   if (nth <= 0 || g_alloc_seen.fetch_add(1) + 1 != nth) return false;
   g_fail_nth.store(0);
   return true;
 }
 
+namespace {
+
 template <typename T>
 cudaError_t dmalloc(T** p, size_t n) {
-  if (fail_this_alloc()) return cudaErrorMemoryAllocation;
+  if (bkv::fail_this_alloc()) return cudaErrorMemoryAllocation;
   return cudaMalloc(reinterpret_cast<void**>(p), sizeof(T) * (n ? n : 1));
 }
 
 template <typename T>
 cudaError_t hmalloc(T** p, size_t bytes) {
-  if (fail_this_alloc()) return cudaErrorMemoryAllocation;
+  if (bkv::fail_this_alloc()) return cudaErrorMemoryAllocation;
   return cudaMallocHost(reinterpret_cast<void**>(p), bytes);
 }
 
@@ -229,6 +135,7 @@ void free_all(bkv_ctx* c) {
   cudaFree(c->work);
   cudaFree(c->n_work);
   cudaFree(c->rag);
+  cudaFree(c->attend_ws);
   if (c->switch_ev) cudaEventDestroy(c->switch_ev);
 }
 
@@ -252,7 +159,7 @@ const char* bkv_strerror(int code) {
     case BKV_ENOMEM: return "device allocation failed";
     case BKV_ECUDA: return "CUDA error";
     case BKV_ETIMEOUT: return "device wait timed out; outputs are invalid";
-    case BKV_ESTATE: return "beacon state not initialised";
+    case BKV_ESTATE: return "beacon state or workspace not initialised";
     case BKV_EBOUNDS: return "device-side bounds check failed (checked build); outputs are invalid";
     default: return "unknown error";
   }
@@ -887,7 +794,8 @@ int bkv_sync(bkv_ctx* ctx) {
   if (h != 0) {
     cudaMemset(ctx->err, 0, sizeof(int));
     if (h == bkv::kDevBadLength)
-      return fail(ctx, BKV_EINVAL, "a per-instance cache length was outside 1..capacity; that instance was left untouched");
+      return fail(ctx, BKV_EINVAL, "a per-instance cache length was out of range; that instance was left untouched (compress, evict) or "
+                  "taken as empty (attend)");
     if (h == bkv::kDevBounds)
       return fail(ctx, BKV_EBOUNDS, "a device-side bounds check failed; the access was skipped and the outputs are invalid");
     return fail(ctx, BKV_ETIMEOUT, "device wait expired (code %d)", h);

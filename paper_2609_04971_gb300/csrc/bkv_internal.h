@@ -164,6 +164,41 @@ cudaError_t launch_select_gather_ragged(const Shape& s, const float* r, const in
 
 cudaError_t launch_keep_all(const Shape& s, int L, int budget, int* kept, cudaStream_t st);
 
+// ---- attention over the caches (k_attend.cu, k_attend_weights.cu); rows are (query head, query) pairs
+struct AttendArgs {
+  const __nv_bfloat16* q = nullptr;              // [batch][n_kv * G][n_q][d]
+  const __nv_bfloat16 *K = nullptr, *V = nullptr;    // [batch][n_kv][cap][d]
+  const __nv_bfloat16 *Kp = nullptr, *Vp = nullptr;  // [groups][n_kv][pcap][d]
+  const int* len = nullptr;   // [batch][n_kv]
+  const int* plen = nullptr;  // [groups]
+  int n_q = 0;
+  int groups = 0, pcap = 0;  // 0 groups: no shared prefix
+  float sc = 0.f;            // log2(e) * scale
+  __nv_bfloat16* o = nullptr;
+  float* lse = nullptr;      // [batch][n_kv * G][n_q] or nullptr
+  float* weights = nullptr;  // [batch][n_kv][cap] or nullptr
+  unsigned char* ws = nullptr;
+  int* err = nullptr;
+};
+// Workspace bytes of one call (0 when the shape overflows the kernels' 32-bit item counts).
+size_t attend_workspace(const Shape& s, int n_q, int groups, bool weights);
+cudaError_t launch_attend(const Shape& s, const AttendArgs& a, cudaStream_t st);
+cudaError_t launch_attend_weights(const Shape& s, const AttendArgs& a, cudaStream_t st);
+
+// ---- eviction by accumulated weight (k_evict.cu)
+struct EvictArgs {
+  const __nv_bfloat16 *K = nullptr, *V = nullptr;
+  const float* weights = nullptr;
+  const int* L = nullptr;
+  int budget = 0, cap_out = 0;
+  __nv_bfloat16 *K_out = nullptr, *V_out = nullptr;
+  float* weights_out = nullptr;
+  int* kept = nullptr;
+  int* len_out = nullptr;
+  int* err = nullptr;
+};
+cudaError_t launch_evict(const Shape& s, const EvictArgs& a, cudaStream_t st);
+
 // ---- diagnostics (k_selftest.cu): a bounded wait that expires after limit_ns
 cudaError_t launch_selftest_wait(int* err, unsigned long long limit_ns, cudaStream_t st);
 // One checked access at an index one past the logical end of a buffer that is twice that long, so
