@@ -60,7 +60,12 @@ int attend(bkv_ctx* ctx, bkv::AttendArgs& a, double scale) {
     e = bkv::launch_attend(s, a, ctx->stream);
   }
   if (e != cudaSuccess) return cuda_fail(ctx, e, "attend launch");
-  if (a.weights) {
+  {
+    ProfScope ps(ctx, BKV_K_ATTEND_MERGE);
+    e = bkv::launch_attend_merge(s, a, ctx->stream);
+  }
+  if (e != cudaSuccess) return cuda_fail(ctx, e, "attend merge launch");
+  if (a.weights && bkv::attend_recomputes_weights(s, a.n_q)) {
     ProfScope ps(ctx, BKV_K_ATTEND_WEIGHTS);
     e = bkv::launch_attend_weights(s, a, ctx->stream);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "attend weights launch");

@@ -140,6 +140,11 @@ inline void set_causal(ScoreArgs& a, int L, int W, long long t_pos, const int64_
 // 128-byte swizzle; CUDA_ERROR_NOT_FOUND when the driver has no cuTensorMapEncodeTiled.
 CUresult encode_rows_bf16(CUtensorMap* map, const void* base, uint64_t rows, int d, uint32_t box_rows);
 
+// Tensor map of queries [batch][n_kv][rows][d] in boxes of [box_batch][1][box_rows][64], laid out and swizzled
+// like the boxes of encode_rows_bf16.
+CUresult encode_queries_bf16(CUtensorMap* map, const void* base, uint64_t batch, uint64_t n_kv, uint64_t rows, int d,
+                             uint32_t box_batch, uint32_t box_rows);
+
 constexpr int kScoreMaxCols = 64;  // scoring queries per score launch (column split beyond)
 // kmap / kmap32: K as [n_inst * cap][d] in 128-row and 32-row boxes of [64]
 // columns (128-byte swizzle); qmap: Qobs as [n_inst * n_obs_pad][d] in boxes
@@ -182,7 +187,11 @@ struct AttendArgs {
 };
 // Workspace bytes of one call (0 when the shape overflows the kernels' 32-bit item counts).
 size_t attend_workspace(const Shape& s, int n_q, int groups, bool weights);
+// In this order on one stream: tiles, merge (with the weights where the logits were kept), and the
+// weights recomputed from the keys where they were not.
 cudaError_t launch_attend(const Shape& s, const AttendArgs& a, cudaStream_t st);
+cudaError_t launch_attend_merge(const Shape& s, const AttendArgs& a, cudaStream_t st);
+bool attend_recomputes_weights(const Shape& s, int n_q);
 cudaError_t launch_attend_weights(const Shape& s, const AttendArgs& a, cudaStream_t st);
 
 // ---- eviction by accumulated weight (k_evict.cu)

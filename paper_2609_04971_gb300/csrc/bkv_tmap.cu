@@ -38,4 +38,18 @@ CUresult encode_rows_bf16(CUtensorMap* map, const void* base, uint64_t rows, int
              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
+CUresult encode_queries_bf16(CUtensorMap* map, const void* base, uint64_t batch, uint64_t n_kv, uint64_t rows, int d,
+                             uint32_t box_batch, uint32_t box_rows) {
+  auto enc = encoder();
+  if (!enc) return CUDA_ERROR_NOT_FOUND;
+  const cuuint64_t row = static_cast<cuuint64_t>(d) * 2;
+  cuuint64_t dims[4] = {static_cast<cuuint64_t>(d), rows, n_kv, batch};
+  cuuint64_t strides[3] = {row, row * rows, row * rows * n_kv};
+  cuuint32_t box[4] = {64, box_rows, 1, box_batch};
+  cuuint32_t estr[4] = {1, 1, 1, 1};
+  return enc(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, estr,
+             CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+             CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+
 }  // namespace bkv

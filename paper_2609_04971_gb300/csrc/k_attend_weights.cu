@@ -1,7 +1,6 @@
 // Accumulated attention weights (include/bkv.h, bkv_attend): one warp per
 // cached key adds the weights of the queries of its group, in row order.
-#include "bkv_device.cuh"
-#include "bkv_internal.h"
+#include "k_attend.cuh"
 
 namespace bkv {
 namespace {
@@ -36,12 +35,13 @@ __global__ void __launch_bounds__(kThreads) weights_kernel(Shape s, AttendArgs a
 }  // namespace
 
 cudaError_t launch_attend_weights(const Shape& s, const AttendArgs& a, cudaStream_t st) {
+  const float* lse2 = reinterpret_cast<const float*>(a.ws + attend_layout(s, a.n_q, a.groups, a.pcap, true).off_lse2);
   const long long keys = 1LL * s.batch * s.n_kv * s.cap;
   const unsigned blocks = static_cast<unsigned>((keys * 32 + kThreads - 1) / kThreads);
   if (s.d == 128)
-    weights_kernel<128><<<blocks, kThreads, 0, st>>>(s, a, reinterpret_cast<float*>(a.ws));
+    weights_kernel<128><<<blocks, kThreads, 0, st>>>(s, a, lse2);
   else
-    weights_kernel<64><<<blocks, kThreads, 0, st>>>(s, a, reinterpret_cast<float*>(a.ws));
+    weights_kernel<64><<<blocks, kThreads, 0, st>>>(s, a, lse2);
   return cudaGetLastError();
 }
 
