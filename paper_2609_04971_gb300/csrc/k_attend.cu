@@ -20,7 +20,9 @@ constexpr int kLogitRows = 16;      // rows per instance up to which logits are 
 
 size_t align_up(size_t n) { return (n + 255) / 256 * 256; }
 
-int sm_count() {
+}  // namespace
+
+int attend_sms() {
   int dev = 0, n = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
       n < 1) {
@@ -29,6 +31,8 @@ int sm_count() {
   }
   return n;
 }
+
+namespace {
 
 // Row blocks of m sequences x R rows with at most 128 rows each, as even as 16-row steps allow.
 AtPlan make_plan(const Shape& s, int I, int m, int R, int n_q, bool causal, int cap, int len_div, int sms) {
@@ -201,7 +205,7 @@ __global__ void __launch_bounds__(kMergeThreads) merge_kernel(MergeArgs a) {
 
 AtLayout attend_layout(const Shape& s, int n_q, int groups, int pcap, bool weights) {
   AtLayout l;
-  const int sms = sm_count();
+  const int sms = attend_sms();
   const int R = s.G * n_q;
   l.own = make_plan(s, s.batch * s.n_kv, 1, R, n_q, true, s.cap, 1, sms);
   size_t at = place_parts(l.own, s.d, sms, 0);
@@ -216,6 +220,12 @@ AtLayout attend_layout(const Shape& s, int n_q, int groups, int pcap, bool weigh
   l.logits = weights && R <= kLogitRows;
   l.off_logits = at;
   if (l.logits) at = align_up(at + rows * s.cap * sizeof(float));
+  if (weights && !l.logits) {
+    l.off_wpart = at;
+    at = align_up(at + static_cast<size_t>(2 * sms) * kAtTile * sizeof(float));
+    l.off_wu0 = at;
+    at = align_up(at + static_cast<size_t>(weights_items(s) + 1) * sizeof(long long));
+  }
   l.bytes = at;
   return l;
 }

@@ -77,6 +77,58 @@ __device__ __forceinline__ long long at_row(const AtGeo& g, int e, AtBlock blk, 
   return (seq * g.n_kv + e % g.n_kv) * g.R + r;
 }
 
+// ---------------------------------------------------------------- an even split of a run of units
+// Units of all items in order, cut into equal shares: where this CTA's share starts.  `inst(e)` is the
+// number of units of instance e, `item(e, k)` that of its k-th item.  Called by the whole block; ends
+// with a barrier.
+struct AtShare {
+  int e, k, t;        // instance, item of it, unit of that
+  long long left, u;  // units of this CTA; number of the first one
+  long long per;      // units of a full share
+};
+
+template <int THREADS, typename Inst, typename Item>
+__device__ __forceinline__ void at_split(int I, Inst&& inst, Item&& item, long long* scan, AtShare* out) {
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int chunk = (I + THREADS - 1) / THREADS;
+  const int e0 = min(I, tid * chunk), e1 = min(I, e0 + chunk);
+  long long mine = 0;
+  for (int e = e0; e < e1; ++e) mine += inst(e);
+  long long incl = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const long long n = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += n;
+  }
+  if (lane == 31) scan[warp] = incl;
+  __syncthreads();
+  long long before = incl - mine, total = 0;
+  for (int w = 0; w < THREADS / 32; ++w) {
+    before += w < warp ? scan[w] : 0;
+    total += scan[w];
+  }
+  const long long per = max(1ll, (total + gridDim.x - 1) / gridDim.x);
+  const long long u0 = blockIdx.x * per;
+  if (u0 >= total) {
+    if (tid == 0) *out = {0, 0, 0, 0, u0, per};
+  } else if (u0 >= before && u0 < before + mine) {  // the start lies in this thread's instances
+    long long u = before;
+    int e = e0, k = 0;
+    for (;; ++e) {
+      const long long n = inst(e);
+      if (u0 < u + n) break;
+      u += n;
+    }
+    for (;; ++k) {
+      const int n = item(e, k);
+      if (u0 < u + n) break;
+      u += n;
+    }
+    *out = {e, k, static_cast<int>(u0 - u), min(per, total - u0), u0, per};
+  }
+  __syncthreads();
+}
+
 // Where one source's kernel leaves what the merge needs.  Segment `cta + item` is the part of an
 // item that a CTA worked on: both rise along the run of all segments, one of them by at least 1 from
 // each segment to the next, so the numbers differ.
@@ -122,9 +174,17 @@ struct AtLayout {
   bool logits = false;     // the own kernel stores its logits for the weights
   size_t off_lse2 = 0;     // fp32 [rows]: log2 normalisers
   size_t off_logits = 0;   // fp32 [rows][cap]
+  size_t off_wpart = 0, off_wu0 = 0;  // weights recomputed from the keys: see k_attend_weights.cu
   size_t bytes = 0;
 };
+// SMs of the current device (one CTA of the attention kernels each).
+int attend_sms();
 AtLayout attend_layout(const Shape& s, int n_q, int groups, int pcap, bool weights);
+
+// Workspace of the recomputed weights: [2 grid][128] partial sums, then [items + 1] unit numbers.
+inline long long weights_items(const Shape& s) {
+  return 1ll * s.batch * s.n_kv * ((s.cap + kAtTile - 1) / kAtTile);
+}
 
 // Arguments of the attention kernel.
 struct AtKernelArgs {

@@ -140,8 +140,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
   __shared__ uint32_t tmem_base_sh;
   __shared__ int abort_sh;
   __shared__ long long scan_sh[kAtThreads / 32];
-  __shared__ long long start_left_sh, start_u_sh;
-  __shared__ int start_e_sh, start_rb_sh, start_t_sh;
+  __shared__ AtShare share_sh;
   __shared__ __align__(16) float ref_sh[2][N];   // minus the reference of a column, by segment parity
   __shared__ __align__(16) int lim_sh[2][N];
   __shared__ int row_sh[2][N];  // row of q, o and lse (below 2^27), or -1
@@ -173,8 +172,6 @@ __global__ void __launch_bounds__(kAtThreads, 1)
     }
     mbar_init(&drain_bar, 1);
     abort_sh = 0;
-    start_left_sh = start_u_sh = 0;
-    start_e_sh = start_rb_sh = start_t_sh = 0;
     fence_mbar_init();
   }
   if (warp == 1) {
@@ -187,62 +184,21 @@ __global__ void __launch_bounds__(kAtThreads, 1)
     *reinterpret_cast<uint4*>(q_smem + i) = make_uint4(0, 0, 0, 0);
   fence_async_smem();
 
-  // ---------------------------------------------------------------- this CTA's share of all tiles
-  {
-    const int chunk = (g.I + kAtThreads - 1) / kAtThreads;
-    const int e0 = min(g.I, tid * chunk), e1 = min(g.I, e0 + chunk);
-    long long mine = 0;
-    for (int e = e0; e < e1; ++e) {
-      mine += at_inst_tiles(g, e);
-      if (blockIdx.x == 0) {
-        const int n = __ldg(g.len + e / g.len_div);
-        if (n < 0 || n > g.cap) record_error(a.err, kDevBadLength);
-      }
-    }
-    long long incl = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long n = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += n;
-    }
-    if (lane == 31) scan_sh[warp] = incl;
-    __syncthreads();
-    long long before = incl - mine, total = 0;
-    for (int w = 0; w < kAtThreads / 32; ++w) {
-      before += w < warp ? scan_sh[w] : 0;
-      total += scan_sh[w];
-    }
-    const long long per = max(1ll, (total + gridDim.x - 1) / gridDim.x);
-    const long long u0 = blockIdx.x * per;
-    if (blockIdx.x == 0 && tid == 0) *a.parts.per = per;
-    if (u0 < total && u0 >= before && u0 < before + mine) {  // the start lies in this thread's instances
-      long long u = before;
-      int e = e0;
-      for (;; ++e) {
-        const long long n = at_inst_tiles(g, e);
-        if (u0 < u + n) break;
-        u += n;
-      }
-      const int len = at_len(g, e);
-      int rb = 0;
-      for (;; ++rb) {
-        const int n = at_tiles(at_limit_max(g, len, at_block(g, rb).r0));
-        if (u0 < u + n) break;
-        u += n;
-      }
-      start_e_sh = e;
-      start_rb_sh = rb;
-      start_t_sh = static_cast<int>(u0 - u);
-      start_left_sh = min(per, total - u0);
-      start_u_sh = u0;
+  if (blockIdx.x == 0) {
+    for (int e = tid; e < g.I; e += kAtThreads) {
+      const int n = __ldg(g.len + e / g.len_div);
+      if (n < 0 || n > g.cap) record_error(a.err, kDevBadLength);
     }
   }
   tc_fence_before();
-  __syncthreads();
+  at_split<kAtThreads>(
+      g.I, [&](int e) { return at_inst_tiles(g, e); },
+      [&](int e, int rb) { return at_tiles(at_limit_max(g, at_len(g, e), at_block(g, rb).r0)); }, scan_sh, &share_sh);
   tc_fence_after();
+  if (blockIdx.x == 0 && tid == 0) *a.parts.per = share_sh.per;
   const uint32_t tmem = tmem_base_sh;
-  Walk walk{start_e_sh, start_rb_sh, start_t_sh, start_left_sh, start_u_sh};
-  const int n_tiles = static_cast<int>(start_left_sh);  // tiles of this CTA (below 2^31)
+  Walk walk{share_sh.e, share_sh.k, share_sh.t, share_sh.left, share_sh.u};
+  const int n_tiles = static_cast<int>(share_sh.left);  // tiles of this CTA (below 2^31)
 
   // Ring positions.  Tile i of the CTA: K(0); then for each i: K(i + 1), V(i), but V(i) first where
   // K(i + 1) needs a Q buffer that is still in use (one buffer, next segment) and at the end.

@@ -1,48 +1,398 @@
-// Accumulated attention weights (include/bkv.h, bkv_attend): one warp per
-// cached key adds the weights of the queries of its group, in row order.
+// Accumulated attention weights (include/bkv.h, bkv_attend) of many query rows:
+// the logits are computed again from the keys, and
+//   weights[j] += sum over rows of 2^(scale2 q.k_j - lse2_row)
+// is a sum along the rows of S^T = K_tile Q^T, whose lanes are the keys: every
+// thread owns a key and adds its columns, no reduction over lanes is needed.
+//
+// Persistent, one CTA per SM.  An item is one tile of 128 keys of an instance, a
+// unit is one block of up to 128 query rows that sees some of its keys; with
+// more than 64 queries per head a block lies in one head and starts at the first
+// query that sees the tile, so what the causal mask hides is not computed.  All
+// units in item order are split evenly over the grid.  An item that one CTA
+// finished is added to the weights there; the parts of a split one go to the
+// workspace (a CTA has two at most: its first and its last) and a second launch
+// adds them in order.
+//
+// Warp roles as in k_attend_tiles.cu.  Bound by the exponentials: 128 x 128 of
+// them per unit at 16 per clock and SM, twice what the matrix product takes.
 #include "k_attend.cuh"
 
 namespace bkv {
 namespace {
 
-constexpr int kThreads = 128;
+constexpr int kSmWarps = 8;
+constexpr int kThreads = 32 * (2 + kSmWarps);
+constexpr uint32_t kBox = 128 * 128;
+constexpr int kCols = 128, kNC = kCols / 2;
+constexpr uint32_t kTmem = 2 * kCols;
+
+struct WArgs {
+  int I, n_kv, G, R, n_q, cap;
+  int hp, brow;     // heads per block (1: blocks within a head); rows of a Q box
+  const int* len;
+  float sc;
+  const float* lse2;
+  float* weights;
+  float* parts;     // [2 grid][128]
+  long long* u0;    // [I * tiles]: number of an item's first unit; [I * tiles]: units per CTA
+  int tiles;        // tiles of the capacity
+  int* err;
+};
+
+__device__ __forceinline__ int w_len(const WArgs& a, int e) {
+  const int n = __ldg(a.len + e);
+  return n >= 0 && n <= a.cap ? n : 0;
+}
+
+// First query that sees a key of tile t, and units of the item.
+__device__ __forceinline__ int w_first(const WArgs& a, int len, int t) { return max(0, t * kAtTile - len + a.n_q); }
+__device__ __forceinline__ int w_units(const WArgs& a, int len, int t) {
+  if (t * kAtTile >= len) return 0;
+  if (a.hp > 1) return (a.G + a.hp - 1) / a.hp;
+  return a.G * ((a.n_q - w_first(a, len, t) + kCols - 1) / kCols);
+}
+
+struct Unit {
+  int e, t, k, n, len;  // unit k of the n of item (e, t)
+  int r0, i0, cols;     // its rows r0 .. r0 + cols - 1; the query of the first
+  __device__ __forceinline__ void place(const WArgs& a) {
+    if (a.hp > 1) {
+      r0 = k * a.hp * a.n_q;
+      i0 = 0;
+      cols = min(a.hp, a.G - k * a.hp) * a.n_q;
+    } else {
+      const int per_head = n / a.G, first = w_first(a, len, t);
+      i0 = first + k % per_head * kCols;
+      r0 = k / per_head * a.n_q + i0;
+      cols = min(kCols, a.n_q - i0);
+    }
+  }
+  __device__ __forceinline__ void start(const WArgs& a, const AtShare& s) {
+    e = s.e;
+    t = s.k;
+    k = s.t;
+    len = w_len(a, e);
+    n = w_units(a, len, t);
+    place(a);
+  }
+  // The next unit; call it only while there is one.
+  __device__ __forceinline__ void next(const WArgs& a) {
+    if (++k == n) {
+      k = 0;
+      do {
+        if (++t >= a.tiles || t * kAtTile >= len) {
+          t = 0;
+          ++e;
+          len = w_len(a, e);
+        }
+        n = w_units(a, len, t);
+      } while (n == 0);
+    }
+    place(a);
+  }
+};
 
 template <int D>
-__global__ void __launch_bounds__(kThreads) weights_kernel(Shape s, AttendArgs a, const float* lse2) {
-  const int lane = threadIdx.x & 31;
-  const long long key = (blockIdx.x * static_cast<long long>(kThreads) + threadIdx.x) / 32;
-  const int j = static_cast<int>(key % s.cap), e = static_cast<int>(key / s.cap);
-  if (e >= s.batch * s.n_kv) return;
-  const int len = a.len[e];
-  if (len < 0 || len > s.cap || j >= len) return;
-  float k[D / 32];
-#pragma unroll
-  for (int x = 0; x < D / 32; ++x) k[x] = __bfloat162float(a.K[key * D + x * 32 + lane]);
-  float sum = 0.f;
-  for (int r = 0; r < s.G * a.n_q; ++r) {
-    const long long row = static_cast<long long>(e) * s.G * a.n_q + r;
-    if (j >= len - a.n_q + 1 + r % a.n_q) continue;
-    float dot = 0.f;
-#pragma unroll
-    for (int x = 0; x < D / 32; ++x) dot = fmaf(k[x], __bfloat162float(a.q[row * D + x * 32 + lane]), dot);
-#pragma unroll
-    for (int x = 16; x; x >>= 1) dot += __shfl_xor_sync(0xffffffffu, dot, x);
-    sum += exp2f(dot * a.sc - lse2[row]);
+struct WCfg {
+  static constexpr int kBoxes = D / 64;
+  static constexpr uint32_t kTileBytes = kBoxes * kBox;
+  static constexpr int kStages = D == 128 ? 4 : 8;
+  static constexpr size_t kSmem = 1024 + (2 + kStages) * static_cast<size_t>(kTileBytes);
+};
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+    weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap, WArgs a) {
+  using C = WCfg<D>;
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ __align__(8) uint64_t full_bar[C::kStages], empty_bar[C::kStages];
+  __shared__ __align__(8) uint64_t kfull_bar[2], kempty_bar[2], sfull_bar[2], sfree_bar[2], drain_bar;
+  __shared__ uint32_t tmem_base_sh;
+  __shared__ int abort_sh;
+  __shared__ long long scan_sh[kThreads / 32];
+  __shared__ AtShare share_sh;
+  __shared__ __align__(16) float lse_sh[2][kCols];
+  __shared__ __align__(16) int lim_sh[2][kCols];
+  __shared__ float sum_sh[kAtTile];
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  unsigned char* base = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  unsigned char* k_smem = base;
+  unsigned char* q_smem = base + 2 * C::kTileBytes;
+  volatile int* abort_flag = &abort_sh;
+
+  if (tid == 0) {
+    for (int i = 0; i < C::kStages; ++i) {
+      mbar_init(&full_bar[i], 1);
+      mbar_init(&empty_bar[i], 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&kfull_bar[i], 1);
+      mbar_init(&kempty_bar[i], 1);
+      mbar_init(&sfull_bar[i], 1);
+      mbar_init(&sfree_bar[i], kSmWarps);
+    }
+    mbar_init(&drain_bar, 1);
+    abort_sh = 0;
+    fence_mbar_init();
   }
-  if (lane == 0) a.weights[key] += sum;
+  if (warp == 1) {
+    tmem_alloc(&tmem_base_sh, kTmem);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  at_split<kThreads>(
+      a.I,
+      [&](int e) {
+        const int len = w_len(a, e), n_t = (len + kAtTile - 1) / kAtTile;
+        if (a.hp > 1) return static_cast<long long>(n_t) * w_units(a, len, 0);
+        long long n = 0;
+        for (int t = 0; t < n_t; ++t) n += w_units(a, len, t);
+        return n;
+      },
+      [&](int e, int t) { return w_units(a, w_len(a, e), t); }, scan_sh, &share_sh);
+  tc_fence_after();
+  const uint32_t tmem = tmem_base_sh;
+  const AtShare share = share_sh;
+  const int n_units = static_cast<int>(share.left);
+  if (blockIdx.x == 0 && tid == 0) a.u0[static_cast<size_t>(a.I) * a.tiles] = share.per;
+
+  if (warp == 0) {
+    // ---------------------------------------------------------------- producer
+    if (lane == 0 && n_units > 0) {
+      const uint64_t pol = l2_policy_evict_last();
+      prefetch_tmap(&qmap);
+      prefetch_tmap(&kmap);
+      Unit u;
+      u.start(a, share);
+      bool ok = true;
+      int n_k = 0, i = 0;
+      for (; ok && i < n_units; ++i) {
+        if (i > 0) u.next(a);
+        if (i == 0 || u.k == 0) {  // a new tile of keys
+          const int kb = n_k & 1;
+          if (n_k >= 2 && !mbar_wait(&kempty_bar[kb], ((n_k >> 1) - 1) & 1, abort_flag, a.err, kDevTimeoutProducer)) break;
+          mbar_arrive_expect_tx(&kfull_bar[kb], C::kTileBytes);
+          for (int b = 0; b < C::kBoxes; ++b)
+            tma_load_2d(k_smem + kb * C::kTileBytes + b * kBox, &kmap, &kfull_bar[kb], b * 64, u.e * a.cap + u.t * kAtTile,
+                        pol);
+          ++n_k;
+        }
+        const int st = i % C::kStages;
+        if (i >= C::kStages &&
+            !mbar_wait(&empty_bar[st], ((i / C::kStages) - 1) & 1, abort_flag, a.err, kDevTimeoutProducer)) {
+          ok = false;
+          break;
+        }
+        mbar_arrive_expect_tx(&full_bar[st], static_cast<uint32_t>(a.brow) * D * 2);
+        for (int b = 0; b < C::kBoxes; ++b)
+          tma_load_4d(q_smem + st * C::kTileBytes + b * kBox, &qmap, &full_bar[st], b * 64, u.r0, u.e % a.n_kv,
+                      u.e / a.n_kv, pol);
+      }
+      if (i < n_units || *abort_flag) {  // let every copy already issued land before the CTA exits
+        int never = 0;
+        for (int p = max(0, n_k - 2); p < n_k; ++p)
+          mbar_wait(&kfull_bar[p & 1], (p >> 1) & 1, &never, a.err, kDevTimeoutDrain);
+        for (int p = max(0, i - C::kStages); p < i; ++p)
+          mbar_wait(&full_bar[p % C::kStages], (p / C::kStages) & 1, &never, a.err, kDevTimeoutDrain);
+      }
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    // ---------------------------------------------------------------- MMA issuer
+    if (lane == 0) {
+      if (n_units > 0) {
+        Unit u;
+        u.start(a, share);
+        int n_k = 0;
+        for (int i = 0; i < n_units; ++i) {
+          if (i > 0) {
+            u.next(a);
+            if (u.k == 0) {
+              mma_commit(&kempty_bar[n_k & 1]);  // the products with the tile before are issued
+              ++n_k;
+            }
+          }
+          const int st = i % C::kStages, buf = i & 1, kb = n_k & 1;
+          if ((i == 0 || u.k == 0) &&
+              !mbar_wait(&kfull_bar[kb], (n_k >> 1) & 1, abort_flag, a.err, kDevTimeoutMma))
+            break;
+          if (!mbar_wait(&full_bar[st], (i / C::kStages) & 1, abort_flag, a.err, kDevTimeoutMma) ||
+              (i >= 2 && !mbar_wait(&sfree_bar[buf], ((i >> 1) - 1) & 1, abort_flag, a.err, kDevTimeoutMma)))
+            break;
+          tc_fence_after();
+          const uint32_t idesc = idesc_bf16_f32(128, (u.cols + 15) / 16 * 16);
+          const uint32_t k_addr = smem_u32(k_smem + kb * C::kTileBytes), q_addr = smem_u32(q_smem + st * C::kTileBytes);
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk)
+            mma_bf16_ss(tmem + buf * kCols, sdesc_kmajor_sw128(k_addr + (kk >> 2) * kBox + (kk & 3) * 32),
+                        sdesc_kmajor_sw128(q_addr + (kk >> 2) * kBox + (kk & 3) * 32), idesc, kk > 0);
+          mma_commit(&empty_bar[st]);
+          mma_commit(&sfull_bar[buf]);
+        }
+      }
+      mma_commit(&drain_bar);
+      int never = 0;
+      mbar_wait(&drain_bar, 0, &never, a.err, kDevTimeoutDrain);
+    }
+    __syncwarp();
+  } else if (n_units > 0) {
+    // ---------------------------------------------------------------- weights
+    const int grp = (warp - 2) >> 2, wt = (tid - 64) & 127;
+    const int quarter = warp & 3, key_lane = quarter * 32 + lane;
+    const uint32_t lane_addr = static_cast<uint32_t>(quarter * 32) << 16;
+    const uint32_t bar_id = 1 + grp;
+    const int c0 = grp * kNC;
+    const float sc = a.sc;
+    Unit u;
+    u.start(a, share);
+    // normaliser and limit of column c of a unit; columns without a row see nothing
+    auto column = [&](const Unit& v, int c, float& lse, int& lim) {
+      lse = 0.f;
+      lim = 0;
+      if (c < v.cols) {
+        lse = a.lse2[static_cast<size_t>(v.e) * a.R + v.r0 + c];
+        lim = v.len - a.n_q + 1 + (a.hp > 1 ? c % a.n_q : v.i0 + c);
+      }
+    };
+    if (wt < kNC) column(u, c0 + wt, lse_sh[0][c0 + wt], lim_sh[0][c0 + wt]);
+    named_barrier(bar_id, 128);
+    float acc = 0.f;
+    bool from_start = u.k == 0;  // this CTA has the item's units from its first one on
+    if (from_start && wt == 0 && grp == 0) a.u0[static_cast<size_t>(u.e) * a.tiles + u.t] = share.u;
+    for (int i = 0; i < n_units; ++i) {
+      const int buf = i & 1;
+      Unit v = u;
+      float lse_n = 0.f;
+      int lim_n = 0;
+      const bool more = i + 1 < n_units;
+      if (more) {
+        v.next(a);
+        if (wt < kNC) column(v, c0 + wt, lse_n, lim_n);
+      }
+      if (!*abort_flag) mbar_wait(&sfull_bar[buf], (i >> 1) & 1, abort_flag, a.err, kDevTimeoutEpilogue);
+      __syncwarp();
+      tc_fence_after();
+      const int ncw = max(0, min(kNC, u.cols - c0));
+      float y[kNC];
+#pragma unroll
+      for (int x = 0; x < kNC / 8; ++x)
+        if (x * 8 < ncw) tmem_ld8(tmem + buf * kCols + c0 + x * 8 + lane_addr, y + x * 8);
+      tmem_wait_ld();
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&sfree_bar[buf]);
+      const int j = u.t * kAtTile + key_lane;
+      const int lim_min = u.len - a.n_q + 1 + u.i0;
+      const bool masked = (u.t + 1) * kAtTile > lim_min || (u.cols & 7) != 0;
+      float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+#pragma unroll
+      for (int c = 0; c < kNC; c += 4) {
+        if (c / 8 * 8 < ncw) {
+          const float4 l = *reinterpret_cast<const float4*>(&lse_sh[buf][c0 + c]);
+          float p0 = ex2_approx(fmaf(y[c], sc, -l.x)), p1 = ex2_approx(fmaf(y[c + 1], sc, -l.y));
+          float p2 = ex2_approx(fmaf(y[c + 2], sc, -l.z)), p3 = ex2_approx(fmaf(y[c + 3], sc, -l.w));
+          if (masked) {
+            const int4 m = *reinterpret_cast<const int4*>(&lim_sh[buf][c0 + c]);
+            p0 = j < m.x ? p0 : 0.f;
+            p1 = j < m.y ? p1 : 0.f;
+            p2 = j < m.z ? p2 : 0.f;
+            p3 = j < m.w ? p3 : 0.f;
+          }
+          s0 += p0;
+          s1 += p1;
+          s2 += p2;
+          s3 += p3;
+        }
+      }
+      acc += (s0 + s1) + (s2 + s3);
+      if (!more || v.k == 0) {  // the item's last unit here
+        if (grp == 1) sum_sh[key_lane] = acc;
+        named_barrier(3, 256);
+        if (grp == 0) {
+          const float sum = acc + sum_sh[key_lane];
+          if (from_start && u.k + 1 == u.n) {
+            if (j < u.len) a.weights[static_cast<size_t>(u.e) * a.cap + j] += sum;
+          } else {
+            // the item began in this CTA after its first unit: part 1; else it is the CTA's first item
+            const bool second = from_start && i != u.k;
+            a.parts[(static_cast<size_t>(blockIdx.x) * 2 + second) * kAtTile + key_lane] = sum;
+          }
+        }
+        named_barrier(3, 256);
+        acc = 0.f;
+        from_start = true;
+        if (more && wt == 0 && grp == 0) a.u0[static_cast<size_t>(v.e) * a.tiles + v.t] = share.u + i + 1;
+      }
+      if (more) {
+        if (wt < kNC) {
+          lse_sh[buf ^ 1][c0 + wt] = lse_n;
+          lim_sh[buf ^ 1][c0 + wt] = lim_n;
+        }
+        named_barrier(bar_id, 128);
+        u = v;
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc(tmem, kTmem);
+}
+
+// Parts of split items, in order: one thread per key.
+__global__ void __launch_bounds__(kAtTile) weights_merge_kernel(WArgs a) {
+  const int t = blockIdx.x % a.tiles, e = blockIdx.x / a.tiles;
+  const int len = w_len(a, e), n = w_units(a, len, t);
+  if (n == 0) return;
+  const long long per = a.u0[static_cast<size_t>(a.I) * a.tiles], u = a.u0[static_cast<size_t>(e) * a.tiles + t];
+  const int first = static_cast<int>(u / per), last = static_cast<int>((u + n - 1) / per);
+  const int j = t * kAtTile + threadIdx.x;
+  if (first == last || j >= len) return;
+  float sum = 0.f;
+  for (int c = first; c <= last; ++c)
+    sum += a.parts[(static_cast<size_t>(c) * 2 + (c == first && u != c * per)) * kAtTile + threadIdx.x];
+  a.weights[static_cast<size_t>(e) * a.cap + j] += sum;
+}
+
+template <int D>
+cudaError_t launch(const CUtensorMap& qmap, const CUtensorMap& kmap, const WArgs& a, int grid, cudaStream_t st) {
+  const cudaError_t e = cudaFuncSetAttribute(weights_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             static_cast<int>(WCfg<D>::kSmem));
+  if (e != cudaSuccess) return e;
+  weights_kernel<D><<<grid, kThreads, WCfg<D>::kSmem, st>>>(qmap, kmap, a);
+  weights_merge_kernel<<<static_cast<unsigned>(a.I) * a.tiles, kAtTile, 0, st>>>(a);
+  return cudaGetLastError();
 }
 
 }  // namespace
 
 cudaError_t launch_attend_weights(const Shape& s, const AttendArgs& a, cudaStream_t st) {
-  const float* lse2 = reinterpret_cast<const float*>(a.ws + attend_layout(s, a.n_q, a.groups, a.pcap, true).off_lse2);
-  const long long keys = 1LL * s.batch * s.n_kv * s.cap;
-  const unsigned blocks = static_cast<unsigned>((keys * 32 + kThreads - 1) / kThreads);
-  if (s.d == 128)
-    weights_kernel<128><<<blocks, kThreads, 0, st>>>(s, a, lse2);
-  else
-    weights_kernel<64><<<blocks, kThreads, 0, st>>>(s, a, lse2);
-  return cudaGetLastError();
+  const AtLayout l = attend_layout(s, a.n_q, a.groups, a.pcap, true);
+  WArgs w{};
+  w.I = s.batch * s.n_kv;
+  w.n_kv = s.n_kv;
+  w.G = s.G;
+  w.R = s.G * a.n_q;
+  w.n_q = a.n_q;
+  w.cap = s.cap;
+  // several whole heads to a block while that halves the number of blocks at least
+  w.hp = a.n_q <= kCols / 2 ? kCols / a.n_q : 1;
+  if (w.hp > s.G) w.hp = s.G;
+  w.brow = w.hp > 1 ? w.hp * a.n_q : (a.n_q < kCols ? a.n_q : kCols);
+  w.len = a.len;
+  w.sc = a.sc;
+  w.lse2 = reinterpret_cast<const float*>(a.ws + l.off_lse2);
+  w.weights = a.weights;
+  w.parts = reinterpret_cast<float*>(a.ws + l.off_wpart);
+  w.u0 = reinterpret_cast<long long*>(a.ws + l.off_wu0);
+  w.tiles = (s.cap + kAtTile - 1) / kAtTile;
+  w.err = a.err;
+  CUtensorMap qmap, kmap;
+  if (encode_queries_bf16(&qmap, a.q, s.batch, s.n_kv, w.R, s.d, 1, w.brow) != CUDA_SUCCESS ||
+      encode_rows_bf16(&kmap, a.K, static_cast<uint64_t>(w.I) * s.cap, s.d, kAtTile) != CUDA_SUCCESS)
+    return cudaErrorInvalidValue;
+  return s.d == 128 ? launch<128>(qmap, kmap, w, attend_sms(), st) : launch<64>(qmap, kmap, w, attend_sms(), st);
 }
 
 }  // namespace bkv
