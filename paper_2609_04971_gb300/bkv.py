@@ -479,14 +479,14 @@ class BeaconKV:
         return kept_out
 
     # ------------------------------------------------------------ attention over the caches
-    def _empty(self, *shape, dtype, like: torch.Tensor) -> torch.Tensor:
-        """A new output, from the allocator pool of the context's stream (its memory may have been freed
-        by work that is only ordered on that stream)."""
+    def _new(self, device: torch.device, *specs) -> list:
+        """New outputs, one per (shape, dtype), from the allocator pool of the context's stream (their memory
+        may have been freed by work that is only ordered on that stream)."""
         stream = _streams[self.ctx.value]
-        if torch.cuda.current_stream(like.device).cuda_stream == stream:
-            return torch.empty(shape, dtype=dtype, device=like.device)
-        with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=like.device)):
-            return torch.empty(shape, dtype=dtype, device=like.device)
+        if torch._C._cuda_getCurrentRawStream(device.index) == stream:
+            return [torch.empty(shape, dtype=dtype, device=device) for shape, dtype in specs]
+        with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)):
+            return [torch.empty(shape, dtype=dtype, device=device) for shape, dtype in specs]
 
     def reserve_attend(self, *, n_q: int = 1, n_groups: int = 0, weights: bool = False):
         """Workspace for attend (n_groups = 0) or attend_shared with n_q queries per head; needed once
@@ -495,24 +495,26 @@ class BeaconKV:
 
     def _attend_args(self, q, K, V, length, weights, o_out, lse_out):
         c = self.cfg
-        if q.dim() != 4 or q.shape[0] != c.batch or q.shape[1] != c.n_q_heads or q.shape[3] != c.head_dim:
-            raise ValueError(f"q must be [batch = {c.batch}, n_q_heads = {c.n_q_heads}, n_q, head_dim = "
-                             f"{c.head_dim}], got {tuple(q.shape)}")
-        n_q = q.shape[2]
-        inst, rows = c.batch * c.n_kv_heads, c.batch * c.n_q_heads * n_q
-        self._expect(K, inst * c.capacity * c.head_dim, "K")
-        self._expect(V, inst * c.capacity * c.head_dim, "V")
-        self._expect(length, inst, "length")
-        self._expect(weights, inst * c.capacity, "weights")
-        self._expect(o_out, rows * c.head_dim, "o_out")
-        self._expect(lse_out, rows, "lse_out")
+        batch, heads, d = c.batch, c.n_q_heads, c.head_dim
+        shape = tuple(q.shape)
+        if len(shape) != 4 or shape[0] != batch or shape[1] != heads or shape[3] != d:
+            raise ValueError(f"q must be [batch = {batch}, n_q_heads = {heads}, n_q, head_dim = {d}], got {shape}")
+        rows_kv = batch * c.n_kv_heads * c.capacity
+        self._expect(K, rows_kv * d, "K")
+        self._expect(V, rows_kv * d, "V")
+        self._expect(length, batch * c.n_kv_heads, "length")
+        self._expect(weights, rows_kv, "weights")
         if not q.is_cuda:
             raise TypeError("q must be a CUDA tensor")
-        if o_out is None:
-            o_out = self._empty(c.batch, c.n_q_heads, n_q, c.head_dim, dtype=torch.bfloat16, like=q)
-        if lse_out is None:
-            lse_out = self._empty(c.batch, c.n_q_heads, n_q, dtype=torch.float32, like=q)
-        return n_q, o_out, lse_out
+        if o_out is None and lse_out is None:
+            o_out, lse_out = self._new(q.device, (shape, torch.bfloat16), (shape[:3], torch.float32))
+        elif o_out is None:
+            o_out, = self._new(q.device, (shape, torch.bfloat16))
+        elif lse_out is None:
+            lse_out, = self._new(q.device, (shape[:3], torch.float32))
+        self._expect(o_out, q.numel(), "o_out")
+        self._expect(lse_out, q.numel() // d, "lse_out")
+        return shape[2], o_out, lse_out
 
     def attend(self, q, K, V, *, length, scale=None, weights=None, o_out=None, lse_out=None):
         """Attention of one layer's newest queries over its caches (bkv_attend): q [batch, n_q_heads, n_q,
@@ -562,10 +564,11 @@ class BeaconKV:
         self._expect(len_out, self.n_inst, "len_out")
         if not K.is_cuda:
             raise TypeError("K must be a CUDA tensor")
+        inst = (c.n_layers, c.batch, c.n_kv_heads)
         if kept_out is None:
-            kept_out = self._empty(c.n_layers, c.batch, c.n_kv_heads, max(0, budget), dtype=torch.int32, like=K)
+            kept_out, = self._new(K.device, ((*inst, max(0, budget)), torch.int32))
         if len_out is None:
-            len_out = self._empty(c.n_layers, c.batch, c.n_kv_heads, dtype=torch.int32, like=K)
+            len_out, = self._new(K.device, (inst, torch.int32))
         bkv_evict(self.ctx, K, V, weights, L, budget, K_out, V_out, weights_out, cap_out, kept_out, len_out)
         return kept_out, len_out
 

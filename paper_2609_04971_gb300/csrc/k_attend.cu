@@ -6,7 +6,7 @@
 // sums O_p = sum p v and l_p = sum p of each row against a reference m_p (p = 2^(y -
 // m_p), y the base-2 logits).  A row's result over all its parts is
 //   lse2 = log2 sum_p l_p 2^(m_p),   o = sum_p O_p 2^(m_p - lse2),
-// taken in the parts' order, one warp per row.  A row that one CTA finished is
+// taken in the parts' order, a warp to a row.  A row that one CTA finished is
 // already written.  The same launch adds the attention weights where the logits
 // were kept: weights[j] += sum over rows of 2^(y - lse2).
 #include "k_attend.cuh"
@@ -15,7 +15,8 @@ namespace bkv {
 namespace {
 
 constexpr int kMergeThreads = 256;
-constexpr int kMergeKeys = 1024;    // keys per block of the weights' part
+constexpr int kMergeRows = 32;      // rows per block: four per warp
+constexpr int kMergeKeys = 512;    // keys per block of the weights' part
 constexpr int kLogitRows = 16;      // rows per instance up to which logits are kept for the weights
 
 size_t align_up(size_t n) { return (n + 255) / 256 * 256; }
@@ -58,8 +59,6 @@ AtPlan make_plan(const Shape& s, int I, int m, int R, int n_q, bool causal, int 
     g.nr = (R + g.rr - 1) / g.rr;
   }
   g.nrb = (m + g.mb - 1) / g.mb * g.nr;
-  const int rows = g.mb * g.rr;
-  p.n_cols = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
   p.items = static_cast<long long>(I) * g.nrb;
   const long long most = p.items * ((cap + kAtTile - 1) / kAtTile);
   p.grid = static_cast<int>(most < sms ? most : sms);
@@ -82,7 +81,6 @@ struct MergeArgs {
   AtGeo own, pre;
   AtParts own_parts, pre_parts;
   int has_prefix;
-  long long rows;
   int row_blocks;
   float sc;
   __nv_bfloat16* o;
@@ -122,57 +120,110 @@ __device__ __forceinline__ RowParts row_parts(const MergeArgs& a, int e, int r) 
   return p;
 }
 
-// f(reference, sum of p, partial o or its place) over the parts of a row, in order.
-template <typename F>
-__device__ __forceinline__ void each_part(const MergeArgs& a, const RowParts& p, F&& f) {
-  for (int c = p.pre.first; c <= p.pre.last; ++c) {
-    const long long at = (c + p.pre_item) * a.pre_parts.rows + p.pre_c;
-    f(a.pre_parts.ml[at], a.pre_parts.o, at);
-  }
-  for (int c = p.own.first; c <= p.own.last; ++c) {
-    const long long at = (c + p.own_item) * a.own_parts.rows + p.own_c;
-    f(a.own_parts.ml[at], a.own_parts.o, at);
-  }
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+  return v;
+}
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
 }
 
-// log2 of the sum of the parts' l 2^m; -inf when no part saw a key.
-__device__ __forceinline__ float merged_lse2(const MergeArgs& a, const RowParts& p) {
-  float top = -INFINITY;
-  each_part(a, p, [&](float2 ml, const float*, long long) {
-    if (ml.y != 0.f) top = fmaxf(top, ml.x);
-  });
+// The parts of a row, a warp at a time: lane x holds part base + x.
+struct WarpParts {
+  int n_pre, n;
+  __device__ __forceinline__ explicit WarpParts(const RowParts& p)
+      : n_pre(p.pre.last - p.pre.first + 1), n(n_pre + p.own.last - p.own.first + 1) {}
+  // Index of part i in ml, and whether it is the prefix's.
+  __device__ __forceinline__ long long at(const MergeArgs& a, const RowParts& p, int i, bool& pre) const {
+    pre = i < n_pre;
+    return pre ? (p.pre.first + i + p.pre_item) * a.pre_parts.rows + p.pre_c
+               : (p.own.first + i - n_pre + p.own_item) * a.own_parts.rows + p.own_c;
+  }
+  __device__ __forceinline__ float2 ml(const MergeArgs& a, const RowParts& p, int i) const {
+    if (i >= n) return make_float2(0.f, 0.f);
+    bool pre;
+    const long long x = at(a, p, i, pre);
+    return pre ? a.pre_parts.ml[x] : a.own_parts.ml[x];
+  }
+};
+
+// log2 of the sum of the parts' l 2^m; -inf when no part saw a key.  The whole warp.
+__device__ __forceinline__ float merged_lse2(const MergeArgs& a, const RowParts& p, const WarpParts& wp, int lane) {
+  const float2 mine = wp.ml(a, p, lane);
+  float top = mine.y != 0.f ? mine.x : -INFINITY;
+  for (int i = 32 + lane; i - lane < wp.n; i += 32) {
+    const float2 v = wp.ml(a, p, i);
+    if (v.y != 0.f) top = fmaxf(top, v.x);
+  }
+  top = warp_max(top);
   if (top == -INFINITY) top = 0.f;
-  float sum = 0.f;
-  each_part(a, p, [&](float2 ml, const float*, long long) {
-    if (ml.y != 0.f) sum += ml.y * exp2f(ml.x - top);
-  });
+  float sum = mine.y != 0.f ? mine.y * exp2f(mine.x - top) : 0.f;
+  for (int i = 32 + lane; i - lane < wp.n; i += 32) {
+    const float2 v = wp.ml(a, p, i);
+    if (v.y != 0.f) sum += v.y * exp2f(v.x - top);
+  }
+  sum = warp_sum(sum);
   return sum == 0.f ? -INFINITY : top + log2f(sum);
 }
 
 template <int D>
-__global__ void __launch_bounds__(kMergeThreads) merge_kernel(MergeArgs a) {
+__global__ void __launch_bounds__(kMergeThreads, 5) merge_kernel(MergeArgs a) {
   constexpr int kPer = D / 32;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  grid_dependents_go();
+  grid_dependency_wait();
   if (static_cast<int>(blockIdx.x) < a.row_blocks) {
-    const long long row = static_cast<long long>(blockIdx.x) * (kMergeThreads / 32) + warp;
-    if (row >= a.rows) return;
-    const RowParts p = row_parts(a, static_cast<int>(row / a.own.R), static_cast<int>(row % a.own.R));
-    if (!p.split) return;
-    const float lse2 = merged_lse2(a, p);
-    float o[kPer] = {};
-    if (lse2 != -INFINITY) {
-      each_part(a, p, [&](float2 ml, const float* src, long long at) {
-        if (ml.y == 0.f) return;
-        const float w = exp2f(ml.x - lse2);
+    // kMergeRows rows of one item of the own caches to a block
+    const AtGeo& g = a.own;
+    const int per_item = (g.rr + kMergeRows - 1) / kMergeRows;
+    const int item = blockIdx.x / per_item;
+    const int e = item / g.nrb, r0 = item % g.nrb * g.rr, c1 = min(g.rr, g.R - r0);
+    for (int c = blockIdx.x % per_item * kMergeRows + warp, n = 0; c < c1 && n < kMergeRows / 8; c += 8, ++n) {
+      const int r = r0 + c;
+      const long long row = static_cast<long long>(e) * g.R + r;
+      const RowParts p = row_parts(a, e, r);
+      if (!p.split) return;  // the same for the whole item
+      const WarpParts wp(p);
+      const float lse2 = merged_lse2(a, p, wp, lane);
+      float o[kPer] = {};
+      // parts in runs of consecutive places, four loads of O under way at a time
+      auto run = [&](const AtParts& parts, long long item, int c, int first, int n) {
+        const float2* ml = parts.ml + (first + item) * parts.rows + c;
+        const float* src = parts.o + ((first + item) * parts.rows + c) * D + lane;
+        const size_t step = static_cast<size_t>(parts.rows) * D;
+        for (int base = 0; base < n; base += 32) {
+          float w = 0.f;
+          if (base + lane < n) {
+            const float2 v = ml[static_cast<size_t>(base + lane) * parts.rows];
+            w = v.y == 0.f || lse2 == -INFINITY ? 0.f : exp2f(v.x - lse2);
+          }
+          const int here = min(32, n - base);
+          for (int i = 0; i < here; i += 4) {
+            float v[4][kPer];
 #pragma unroll
-        for (int x = 0; x < kPer; ++x) o[x] = fmaf(src[at * D + x * 32 + lane], w, o[x]);
-      });
-    }
+            for (int y = 0; y < 4; ++y)
 #pragma unroll
-    for (int x = 0; x < kPer; ++x) a.o[row * D + x * 32 + lane] = __float2bfloat16(o[x]);
-    if (lane == 0) {
-      a.lse2[row] = lse2;
-      if (a.lse) a.lse[row] = lse2 * 0.69314718055994531f;
+              for (int x = 0; x < kPer; ++x) v[y][x] = i + y < here ? src[(base + i + y) * step + x * 32] : 0.f;
+#pragma unroll
+            for (int y = 0; y < 4; ++y) {
+              const float wi = __shfl_sync(0xffffffffu, w, (i + y) & 31);
+#pragma unroll
+              for (int x = 0; x < kPer; ++x) o[x] = i + y < here && wi != 0.f ? fmaf(v[y][x], wi, o[x]) : o[x];
+            }
+          }
+        }
+      };
+      if (a.has_prefix) run(a.pre_parts, p.pre_item, p.pre_c, p.pre.first, p.pre.last - p.pre.first + 1);
+      run(a.own_parts, p.own_item, p.own_c, p.own.first, p.own.last - p.own.first + 1);
+#pragma unroll
+      for (int x = 0; x < kPer; ++x) a.o[row * D + x * 32 + lane] = __float2bfloat16(o[x]);
+      if (lane == 0) {
+        a.lse2[row] = lse2;
+        if (a.lse) a.lse[row] = lse2 * 0.69314718055994531f;
+      }
     }
     return;
   }
@@ -183,21 +234,46 @@ __global__ void __launch_bounds__(kMergeThreads) merge_kernel(MergeArgs a) {
   const AtGeo& g = a.own;
   const int len = at_len(g, e);
   if (j0 >= len) return;
+  constexpr int kKeys = kMergeKeys / kMergeThreads, kAhead = 4;
+  const float* y = a.logits + static_cast<size_t>(e) * g.R * g.cap;
+  float sum[kKeys], ahead[kAhead][kKeys];  // loads that need no normaliser, under way while it is computed
+#pragma unroll
+  for (int x = 0; x < kKeys; ++x) {
+    const int j = j0 + x * kMergeThreads + tid;
+    sum[x] = j < len ? a.weights[static_cast<size_t>(e) * g.cap + j] : 0.f;
+#pragma unroll
+    for (int r = 0; r < kAhead; ++r)
+      ahead[r][x] = j < len && r < g.R ? __ldcg(y + static_cast<size_t>(r) * g.cap + j) : 0.f;
+  }
   for (int r = warp; r < g.R; r += kMergeThreads / 32) {
     const RowParts p = row_parts(a, e, r);
-    const float v = p.split ? merged_lse2(a, p) : a.lse2[static_cast<long long>(e) * g.R + r];
+    const float v = p.split ? merged_lse2(a, p, WarpParts(p), lane) : a.lse2[static_cast<long long>(e) * g.R + r];
     if (lane == 0) lse2_sh[r] = v;
   }
   __syncthreads();
-  const float* y = a.logits + static_cast<size_t>(e) * g.R * g.cap;
-#pragma unroll
-  for (int x = 0; x < kMergeKeys / kMergeThreads; ++x) {
+  float add[kKeys] = {};
+  auto term = [&](int x, int r, float logit) {
     const int j = j0 + x * kMergeThreads + tid;
-    if (j >= len) break;
-    float sum = 0.f;
-    for (int r = 0; r < g.R; ++r)
-      if (j < len - g.n_q + 1 + r % g.n_q) sum += exp2f(fmaf(__ldcg(y + static_cast<size_t>(r) * g.cap + j), a.sc, -lse2_sh[r]));
-    a.weights[static_cast<size_t>(e) * g.cap + j] += sum;
+    if (j < min(len, len - g.n_q + 1 + r % g.n_q)) add[x] += exp2f(fmaf(logit, a.sc, -lse2_sh[r]));
+  };
+#pragma unroll
+  for (int r = 0; r < kAhead; ++r) {
+    if (r < g.R) {
+#pragma unroll
+      for (int x = 0; x < kKeys; ++x) term(x, r, ahead[r][x]);
+    }
+  }
+  for (int r = kAhead; r < g.R; ++r) {
+#pragma unroll
+    for (int x = 0; x < kKeys; ++x) {
+      const int j = j0 + x * kMergeThreads + tid;
+      if (j < len) term(x, r, __ldcg(y + static_cast<size_t>(r) * g.cap + j));
+    }
+  }
+#pragma unroll
+  for (int x = 0; x < kKeys; ++x) {
+    const int j = j0 + x * kMergeThreads + tid;
+    if (j < len) a.weights[static_cast<size_t>(e) * g.cap + j] = sum[x] + add[x];
   }
 }
 
@@ -260,7 +336,9 @@ cudaError_t launch_attend(const Shape& s, const AttendArgs& a, cudaStream_t st) 
     k.lse2 = lse2;
     k.logits = own ? logits : nullptr;
     k.err = a.err;
-    return launch_attend_tiles(s.d, p, qmap, kmap, vmap, k, st);
+    k.after_prefix = own && l.has_prefix;
+    return s.d == 128 ? launch_attend_tiles_128(p, qmap, kmap, vmap, k, st)
+                      : launch_attend_tiles_64(p, qmap, kmap, vmap, k, st);
   };
   cudaError_t e = cudaSuccess;
   if (l.has_prefix && (e = tiles(l.prefix, a.Kp, a.Vp, a.plen, false)) != cudaSuccess) return e;
@@ -280,8 +358,7 @@ cudaError_t launch_attend_merge(const Shape& s, const AttendArgs& a, cudaStream_
     m.pre.len = a.plen;
     m.pre_parts = l.prefix.parts(a.ws);
   }
-  m.rows = static_cast<long long>(l.own.geo.I) * l.own.geo.R;
-  m.row_blocks = static_cast<int>((m.rows + kMergeThreads / 32 - 1) / (kMergeThreads / 32));
+  m.row_blocks = static_cast<int>(l.own.items * ((l.own.geo.rr + kMergeRows - 1) / kMergeRows));
   m.sc = a.sc;
   m.o = a.o;
   m.lse = a.lse;
@@ -293,11 +370,8 @@ cudaError_t launch_attend_merge(const Shape& s, const AttendArgs& a, cudaStream_
     m.key_blocks = (s.cap + kMergeKeys - 1) / kMergeKeys;
     blocks += static_cast<unsigned>(l.own.geo.I) * m.key_blocks;
   }
-  if (s.d == 128)
-    merge_kernel<128><<<blocks, kMergeThreads, 0, st>>>(m);
-  else
-    merge_kernel<64><<<blocks, kMergeThreads, 0, st>>>(m);
-  return cudaGetLastError();
+  return s.d == 128 ? launch_after(merge_kernel<128>, blocks, kMergeThreads, 0, st, m)
+                    : launch_after(merge_kernel<64>, blocks, kMergeThreads, 0, st, m);
 }
 
 }  // namespace bkv

@@ -61,70 +61,65 @@ __device__ __forceinline__ int at_limit_min(const AtGeo& g, int len, int r0) {
 // Tiles of an item: an item without keys still has one, all masked, that writes its empty rows.
 __device__ __forceinline__ int at_tiles(int limit) { return max(1, (limit + kAtTile - 1) / kAtTile); }
 
-__device__ __forceinline__ long long at_inst_tiles(const AtGeo& g, int e) {
-  const int len = at_len(g, e);
-  if (!g.causal || g.n_q == 1) return static_cast<long long>(g.nrb) * at_tiles(len);
-  long long n = 0;  // m == 1 here: every row block starts at another row
-  for (int rb = 0; rb < g.nrb; ++rb) n += at_tiles(at_limit_max(g, len, at_block(g, rb).r0));
-  return n;
-}
-
-// Row of q, o and lse that column c of a row block stands for, or -1.
-__device__ __forceinline__ long long at_row(const AtGeo& g, int e, AtBlock blk, int c) {
+// Row of q, o and lse (there are fewer than 2^27) that column c of a row block stands for, or -1.
+__device__ __forceinline__ int at_row(const AtGeo& g, int e, AtBlock blk, int c) {
   const int bi = c / g.rr, r = blk.r0 + c % g.rr;
   if (bi >= g.mb || blk.b0 + bi >= g.m || r >= g.R) return -1;
-  const long long seq = static_cast<long long>(e / g.n_kv) * g.m + blk.b0 + bi;
+  const int seq = e / g.n_kv * g.m + blk.b0 + bi;
   return (seq * g.n_kv + e % g.n_kv) * g.R + r;
 }
 
 // ---------------------------------------------------------------- an even split of a run of units
-// Units of all items in order, cut into equal shares: where this CTA's share starts.  `inst(e)` is the
-// number of units of instance e, `item(e, k)` that of its k-th item.  Called by the whole block; ends
-// with a barrier.
+// Units of all items in order, cut into equal shares: where this CTA's share starts.  There are n groups
+// of items; `count(x)` is the number of units of group x, and `find(x, u)` turns unit u of group x into
+// the unit's place.  Called by the whole block; ends with a barrier.
+struct AtPlace {
+  int e, k, t;  // instance, item of it, unit of that
+};
 struct AtShare {
-  int e, k, t;        // instance, item of it, unit of that
+  AtPlace at;
   long long left, u;  // units of this CTA; number of the first one
   long long per;      // units of a full share
 };
 
-template <int THREADS, typename Inst, typename Item>
-__device__ __forceinline__ void at_split(int I, Inst&& inst, Item&& item, long long* scan, AtShare* out) {
+template <int THREADS, typename Count, typename Find>
+__device__ __forceinline__ void at_split(int n, Count&& count, Find&& find, long long* scan, AtShare* out) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int chunk = (I + THREADS - 1) / THREADS;
-  const int e0 = min(I, tid * chunk), e1 = min(I, e0 + chunk);
+  const int chunk = (n + THREADS - 1) / THREADS;
+  const int x0 = min(n, tid * chunk), x1 = min(n, x0 + chunk);
   long long mine = 0;
-  for (int e = e0; e < e1; ++e) mine += inst(e);
+  for (int x = x0; x < x1; ++x) mine += count(x);
   long long incl = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long n = __shfl_up_sync(0xffffffffu, incl, o);
-    if (lane >= o) incl += n;
+    const long long v = __shfl_up_sync(0xffffffffu, incl, o);
+    if (lane >= o) incl += v;
   }
   if (lane == 31) scan[warp] = incl;
   __syncthreads();
   long long before = incl - mine, total = 0;
+#pragma unroll
   for (int w = 0; w < THREADS / 32; ++w) {
-    before += w < warp ? scan[w] : 0;
-    total += scan[w];
+    const long long v = scan[w];
+    before += w < warp ? v : 0;
+    total += v;
   }
-  const long long per = max(1ll, (total + gridDim.x - 1) / gridDim.x);
+  // 32-bit division where it will do: it is on every CTA's way to its first load
+  const long long per = total + gridDim.x < (1ll << 32)
+                            ? max(1u, (static_cast<uint32_t>(total) + gridDim.x - 1) / gridDim.x)
+                            : (total + gridDim.x - 1) / gridDim.x;
   const long long u0 = blockIdx.x * per;
   if (u0 >= total) {
-    if (tid == 0) *out = {0, 0, 0, 0, u0, per};
-  } else if (u0 >= before && u0 < before + mine) {  // the start lies in this thread's instances
+    if (tid == 0) *out = {{0, 0, 0}, 0, u0, per};
+  } else if (u0 >= before && u0 < before + mine) {  // the start lies in this thread's groups
     long long u = before;
-    int e = e0, k = 0;
-    for (;; ++e) {
-      const long long n = inst(e);
-      if (u0 < u + n) break;
-      u += n;
+    int x = x0;
+    for (;; ++x) {
+      const long long c = count(x);
+      if (u0 < u + c) break;
+      u += c;
     }
-    for (;; ++k) {
-      const int n = item(e, k);
-      if (u0 < u + n) break;
-      u += n;
-    }
-    *out = {e, k, static_cast<int>(u0 - u), min(per, total - u0), u0, per};
+    *out = {find(x, u0 - u), min(per, total - u0), u0, per};
   }
   __syncthreads();
 }
@@ -152,7 +147,6 @@ __device__ __forceinline__ AtSpan at_span(const AtParts& p, long long item, int 
 // One source's launch plan, made on the host.
 struct AtPlan {
   AtGeo geo;
-  int n_cols;   // template columns: 16, 32, 64 or 128
   int grid;
   long long items;
   size_t off_o, off_ml, off_u0, off_per;  // byte offsets in the workspace
@@ -191,6 +185,7 @@ struct AtKernelArgs {
   AtGeo geo;
   AtParts parts;
   int whole_is_final;  // an item that one CTA finished writes o and lse itself (no other source)
+  int after_prefix;    // launched to overlap the prefix's kernel, which its own work does not need
   int reuse;           // several row blocks read the same keys: let them stay in L2
   float sc;
   __nv_bfloat16* o;
@@ -199,7 +194,34 @@ struct AtKernelArgs {
   float* logits;       // [rows][cap] or nullptr
   int* err;
 };
-cudaError_t launch_attend_tiles(int d, const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap,
-                                const CUtensorMap& vmap, const AtKernelArgs& a, cudaStream_t st);
+// Overlapping launches on one stream.  A kernel launched by launch_after starts while the one before it
+// on the stream still runs, as soon as all of that one's blocks have called grid_dependents_go() (or
+// ended); grid_dependency_wait() then returns once the kernel before has ended and its writes are
+// visible.  A kernel whose work needs nothing of the one before waits at its end instead: what follows
+// it may rely on both.
+__device__ __forceinline__ void grid_dependents_go() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+template <typename... P, typename... A>
+cudaError_t launch_after(void (*kernel)(P...), unsigned blocks, unsigned threads, size_t smem, cudaStream_t st,
+                         const A&... args) {
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(blocks);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+// One translation unit per head_dim.
+cudaError_t launch_attend_tiles_64(const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap,
+                                   const CUtensorMap& vmap, const AtKernelArgs& a, cudaStream_t st);
+cudaError_t launch_attend_tiles_128(const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap,
+                                    const CUtensorMap& vmap, const AtKernelArgs& a, cudaStream_t st);
 
 }  // namespace bkv

@@ -52,8 +52,19 @@ __device__ __forceinline__ int w_units(const WArgs& a, int len, int t) {
   return a.G * ((a.n_q - w_first(a, len, t) + kCols - 1) / kCols);
 }
 
+// Units of the tiles before tile t (at most the tiles in use): whole runs of query blocks for the tiles
+// that every query sees, then one block less from tile to tile.
+__device__ __forceinline__ long long w_units_before(const WArgs& a, int len, int t) {
+  if (a.hp > 1) return static_cast<long long>(t) * ((a.G + a.hp - 1) / a.hp);
+  const int tiles = (len + kAtTile - 1) / kAtTile;
+  const int t1 = len >= a.n_q ? (len - a.n_q) / kAtTile + 1 : 0;
+  const long long full = min(t, t1), m = max(0, t - t1), last = tiles - t1;  // m tiles of last, last - 1, ... blocks
+  return a.G * (full * ((a.n_q + kCols - 1) / kCols) + m * last - m * (m - 1) / 2);
+}
+
 struct Unit {
   int e, t, k, n, len;  // unit k of the n of item (e, t)
+  int head, blk, per_head, first;  // hp == 1: its head, block of the head's rows from query `first` on
   int r0, i0, cols;     // its rows r0 .. r0 + cols - 1; the query of the first
   __device__ __forceinline__ void place(const WArgs& a) {
     if (a.hp > 1) {
@@ -61,22 +72,35 @@ struct Unit {
       i0 = 0;
       cols = min(a.hp, a.G - k * a.hp) * a.n_q;
     } else {
-      const int per_head = n / a.G, first = w_first(a, len, t);
-      i0 = first + k % per_head * kCols;
-      r0 = k / per_head * a.n_q + i0;
+      i0 = first + blk * kCols;
+      r0 = head * a.n_q + i0;
       cols = min(kCols, a.n_q - i0);
     }
   }
-  __device__ __forceinline__ void start(const WArgs& a, const AtShare& s) {
-    e = s.e;
-    t = s.k;
-    k = s.t;
-    len = w_len(a, e);
+  __device__ __forceinline__ void item(const WArgs& a) {
     n = w_units(a, len, t);
+    first = w_first(a, len, t);
+    per_head = (a.n_q - first + kCols - 1) / kCols;
+    head = blk = 0;
+  }
+  __device__ __forceinline__ void start(const WArgs& a, const AtShare& s) {
+    e = s.at.e;
+    t = s.at.k;
+    k = s.at.t;
+    len = w_len(a, e);
+    item(a);
+    if (a.hp == 1) {
+      head = k / per_head;
+      blk = k % per_head;
+    }
     place(a);
   }
   // The next unit; call it only while there is one.
   __device__ __forceinline__ void next(const WArgs& a) {
+    if (++blk == per_head) {
+      blk = 0;
+      ++head;
+    }
     if (++k == n) {
       k = 0;
       do {
@@ -85,7 +109,7 @@ struct Unit {
           ++e;
           len = w_len(a, e);
         }
-        n = w_units(a, len, t);
+        item(a);
       } while (n == 0);
     }
     place(a);
@@ -136,6 +160,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     abort_sh = 0;
     fence_mbar_init();
   }
+  grid_dependents_go();
   if (warp == 1) {
     tmem_alloc(&tmem_base_sh, kTmem);
     tmem_relinquish();
@@ -144,14 +169,22 @@ __global__ void __launch_bounds__(kThreads, 1)
   at_split<kThreads>(
       a.I,
       [&](int e) {
-        const int len = w_len(a, e), n_t = (len + kAtTile - 1) / kAtTile;
-        if (a.hp > 1) return static_cast<long long>(n_t) * w_units(a, len, 0);
-        long long n = 0;
-        for (int t = 0; t < n_t; ++t) n += w_units(a, len, t);
-        return n;
+        const int len = w_len(a, e);
+        return w_units_before(a, len, (len + kAtTile - 1) / kAtTile);
       },
-      [&](int e, int t) { return w_units(a, w_len(a, e), t); }, scan_sh, &share_sh);
+      [&](int e, long long u) {
+        const int len = w_len(a, e);
+        int lo = 0, hi = (len + kAtTile - 1) / kAtTile - 1;  // the last tile that begins at or before unit u
+        while (lo < hi) {
+          const int mid = (lo + hi + 1) / 2;
+          if (w_units_before(a, len, mid) <= u) lo = mid;
+          else hi = mid - 1;
+        }
+        return AtPlace{e, lo, static_cast<int>(u - w_units_before(a, len, lo))};
+      },
+      scan_sh, &share_sh);
   tc_fence_after();
+  grid_dependency_wait();  // the normalisers; what came before reads len, q and K only
   const uint32_t tmem = tmem_base_sh;
   const AtShare share = share_sh;
   const int n_units = static_cast<int>(share.left);
@@ -248,10 +281,11 @@ __global__ void __launch_bounds__(kThreads, 1)
     u.start(a, share);
     // normaliser and limit of column c of a unit; columns without a row see nothing
     auto column = [&](const Unit& v, int c, float& lse, int& lim) {
-      lse = 0.f;
+      lse = 0.f;  // never an infinity: a row that sees nothing has one, and its columns are masked
       lim = 0;
       if (c < v.cols) {
-        lse = a.lse2[static_cast<size_t>(v.e) * a.R + v.r0 + c];
+        const float x = a.lse2[static_cast<size_t>(v.e) * a.R + v.r0 + c];
+        lse = x == -INFINITY ? 0.f : x;
         lim = v.len - a.n_q + 1 + (a.hp > 1 ? c % a.n_q : v.i0 + c);
       }
     };
@@ -273,37 +307,48 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!*abort_flag) mbar_wait(&sfull_bar[buf], (i >> 1) & 1, abort_flag, a.err, kDevTimeoutEpilogue);
       __syncwarp();
       tc_fence_after();
-      const int ncw = max(0, min(kNC, u.cols - c0));
-      float y[kNC];
-#pragma unroll
-      for (int x = 0; x < kNC / 8; ++x)
-        if (x * 8 < ncw) tmem_ld8(tmem + buf * kCols + c0 + x * 8 + lane_addr, y + x * 8);
-      tmem_wait_ld();
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&sfree_bar[buf]);
       const int j = u.t * kAtTile + key_lane;
       const int lim_min = u.len - a.n_q + 1 + u.i0;
-      const bool masked = (u.t + 1) * kAtTile > lim_min || (u.cols & 7) != 0;
       float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+      auto add4 = [&](const float* y, int c) {
+        const float4 l = *reinterpret_cast<const float4*>(&lse_sh[buf][c0 + c]);
+        s0 += ex2_approx(fmaf(y[0], sc, -l.x));
+        s1 += ex2_approx(fmaf(y[1], sc, -l.y));
+        s2 += ex2_approx(fmaf(y[2], sc, -l.z));
+        s3 += ex2_approx(fmaf(y[3], sc, -l.w));
+      };
+      const uint32_t at = tmem + buf * kCols + c0 + lane_addr;
+      auto release = [&] {
+        tmem_wait_ld();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sfree_bar[buf]);
+      };
+      if (u.cols == kCols && (u.t + 1) * kAtTile <= lim_min) {
+        float y[kNC];
 #pragma unroll
-      for (int c = 0; c < kNC; c += 4) {
-        if (c / 8 * 8 < ncw) {
-          const float4 l = *reinterpret_cast<const float4*>(&lse_sh[buf][c0 + c]);
-          float p0 = ex2_approx(fmaf(y[c], sc, -l.x)), p1 = ex2_approx(fmaf(y[c + 1], sc, -l.y));
-          float p2 = ex2_approx(fmaf(y[c + 2], sc, -l.z)), p3 = ex2_approx(fmaf(y[c + 3], sc, -l.w));
-          if (masked) {
-            const int4 m = *reinterpret_cast<const int4*>(&lim_sh[buf][c0 + c]);
-            p0 = j < m.x ? p0 : 0.f;
-            p1 = j < m.y ? p1 : 0.f;
-            p2 = j < m.z ? p2 : 0.f;
-            p3 = j < m.w ? p3 : 0.f;
+        for (int c = 0; c < kNC; c += 32) tmem_ld32(at + c, *reinterpret_cast<float(*)[32]>(y + c));
+        release();
+#pragma unroll
+        for (int c = 0; c < kNC; c += 4) add4(y + c, c);
+      } else {  // a masked or an incomplete block: what a key's lane does not see, or no row, adds nothing
+        const int ncw = min(kNC, u.cols - c0);
+#pragma unroll 1
+        for (int c = 0; c < ncw; c += 8) {
+          float y[8];
+          tmem_ld8(at + c, y);
+          tmem_wait_ld();
+#pragma unroll
+          for (int x = 0; x < 8; x += 4) {
+            const int4 m = *reinterpret_cast<const int4*>(&lim_sh[buf][c0 + c + x]);
+            y[x] = j < m.x ? y[x] : -INFINITY;
+            y[x + 1] = j < m.y ? y[x + 1] : -INFINITY;
+            y[x + 2] = j < m.z ? y[x + 2] : -INFINITY;
+            y[x + 3] = j < m.w ? y[x + 3] : -INFINITY;
+            add4(y + x, c + x);
           }
-          s0 += p0;
-          s1 += p1;
-          s2 += p2;
-          s3 += p3;
         }
+        release();
       }
       acc += (s0 + s1) + (s2 + s3);
       if (!more || v.k == 0) {  // the item's last unit here
@@ -342,6 +387,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // Parts of split items, in order: one thread per key.
 __global__ void __launch_bounds__(kAtTile) weights_merge_kernel(WArgs a) {
+  grid_dependency_wait();
   const int t = blockIdx.x % a.tiles, e = blockIdx.x / a.tiles;
   const int len = w_len(a, e), n = w_units(a, len, t);
   if (n == 0) return;
@@ -360,9 +406,9 @@ cudaError_t launch(const CUtensorMap& qmap, const CUtensorMap& kmap, const WArgs
   const cudaError_t e = cudaFuncSetAttribute(weights_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                              static_cast<int>(WCfg<D>::kSmem));
   if (e != cudaSuccess) return e;
-  weights_kernel<D><<<grid, kThreads, WCfg<D>::kSmem, st>>>(qmap, kmap, a);
-  weights_merge_kernel<<<static_cast<unsigned>(a.I) * a.tiles, kAtTile, 0, st>>>(a);
-  return cudaGetLastError();
+  const cudaError_t w = launch_after(weights_kernel<D>, grid, kThreads, WCfg<D>::kSmem, st, qmap, kmap, a);
+  if (w != cudaSuccess) return w;
+  return launch_after(weights_merge_kernel, static_cast<unsigned>(a.I) * a.tiles, kAtTile, 0, st, a);
 }
 
 }  // namespace

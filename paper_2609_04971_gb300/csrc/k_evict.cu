@@ -2,7 +2,9 @@
 // compaction of K, V and the weights, one CTA per instance.
 //
 // Selection.  Each warp owns a contiguous run of rows, 32 at a time across its
-// lanes, and holds their weights in registers, so the weights are read once.
+// lanes.  Up to a capacity of 10240 their keys stay in registers; longer caches
+// are read again in each of the five passes, from L1 and L2, which leaves room for
+// four CTAs per SM.
 // A three-pass radix select (digits of 12, 10 and 10 bits from the top, one
 // shared histogram) finds the key T of the last row that is kept by weight and
 // how many rows equal to T are needed.  A 12-bit first digit splits an octave
@@ -15,7 +17,11 @@
 // independent.  In place they are taken in ascending chunks: all loads of a
 // chunk are issued before the barrier that precedes its stores, and they touch
 // only rows that no earlier chunk writes; rows before the first evicted one
-// already stand where they belong.
+// already stand where they belong.  The weights move with the rows.
+//
+// Into other buffers an instance may be worked on by several CTAs, each of which
+// repeats the selection and moves its share of the rows.  That fills the GPU when
+// there are few instances, and evens out what a last wave of CTAs leaves idle.
 //
 // Bound by HBM: the kept rows are read and written once (8 d bytes a row), the
 // weights read (4 bytes a cached row) and written.
@@ -57,24 +63,59 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* wsum, uint3
   return before + incl - v;
 }
 
-// One digit of the radix select: among the candidates that match `prefix` under `mask`, finds the
-// digit that holds the k-th largest (k >= 1, at most the number of matches) and what is left of k
-// inside it.  Called by the whole block; the result is the same in every thread.
+// The rows of one warp: row0 + 32 i + lane for i < n, with their keys in registers (KPT > 0) or read
+// again on every use (KPT = 0).
+template <int KPT>
+struct WarpRows {
+  uint32_t key[KPT > 0 ? KPT : 1];
+  const float* w;
+  int row0, n, L, lane;
+  __device__ __forceinline__ int row(int i) const { return row0 + i * 32 + lane; }
+  __device__ __forceinline__ void init() {
+    if constexpr (KPT > 0) {
+#pragma unroll
+      for (int i = 0; i < KPT; ++i) key[i] = i < n && row(i) < L ? weight_key(w[row(i)]) : 0;
+    }
+  }
+  // f(row, key) for every i, also where the row is not below L (every lane takes part).
+  template <typename F>
+  __device__ __forceinline__ void each(F&& f) const {
+    if constexpr (KPT > 0) {
+#pragma unroll
+      for (int i = 0; i < KPT; ++i)
+        if (i < n) f(row(i), key[i]);
+    } else {
+      constexpr int kBatch = 8;  // loads in flight
+      for (int i0 = 0; i0 < n; i0 += kBatch) {
+        uint32_t k[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          const int j = row(i0 + u);
+          k[u] = i0 + u < n && j < L ? weight_key(w[j]) : 0;
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u)
+          if (i0 + u < n) f(row(i0 + u), k[u]);
+      }
+    }
+  }
+};
+
+// One digit of the radix select: among the candidates [c_lo, c_hi) that match `prefix` under `mask`,
+// finds the digit that holds the k-th largest (k >= 1, at most the number of matches) and what is left
+// of k inside it.  Called by the whole block; the result is the same in every thread.
 template <int THREADS, int KPT, int BITS>
-__device__ __forceinline__ void select_digit(const uint32_t (&key)[KPT], int c_lo, int c_hi, int row0, int rpw, int shift,
-                                             uint32_t& prefix, uint32_t& mask, uint32_t& k, uint32_t* hist,
-                                             uint32_t* wsum, uint32_t* found) {
+__device__ __forceinline__ void select_digit(const WarpRows<KPT>& rows, int c_lo, int c_hi, int shift, uint32_t& prefix,
+                                             uint32_t& mask, uint32_t& k, uint32_t* hist, uint32_t* wsum,
+                                             uint32_t* found) {
   constexpr int kBins = 1 << BITS;
   constexpr int kPer = (kBins + THREADS - 1) / THREADS;
-  const int tid = threadIdx.x, lane = tid & 31;
+  const int tid = threadIdx.x;
   for (int i = tid; i < kBins; i += THREADS) hist[i] = 0;
   __syncthreads();
-#pragma unroll
-  for (int i = 0; i < KPT; ++i) {
-    const int j = row0 + i * 32 + lane;
-    if (i * 32 < rpw && j >= c_lo && j < c_hi && (key[i] & mask) == prefix)
-      atomicAdd(&hist[(key[i] >> shift) & (kBins - 1)], 1u);
-  }
+  rows.each([&](int j, uint32_t key) {
+    if (j >= c_lo && j < c_hi && (key & mask) == prefix) atomicAdd(&hist[(key >> shift) & (kBins - 1)], 1u);
+  });
   __syncthreads();
   uint32_t loc[kPer], sum = 0;
 #pragma unroll
@@ -102,9 +143,9 @@ __device__ __forceinline__ void select_digit(const uint32_t (&key)[KPT], int c_l
   __syncthreads();
 }
 
-// KPT * THREADS rows at most per instance.
-template <int D, int THREADS, int KPT>
-__global__ void __launch_bounds__(THREADS) evict_kernel(Shape s, EvictArgs a) {
+// KPT > 0: at most KPT * THREADS rows per instance.
+template <int D, int THREADS, int KPT, int MINB>
+__global__ void __launch_bounds__(THREADS, MINB) evict_kernel(Shape s, EvictArgs a, int shares) {
   constexpr int kWarps = THREADS / 32;
   extern __shared__ __align__(16) uint16_t kept_s[];  // [min(budget, cap)] kept rows (cap <= 32768)
   __shared__ uint32_t hist[kEvBins];
@@ -112,14 +153,15 @@ __global__ void __launch_bounds__(THREADS) evict_kernel(Shape s, EvictArgs a) {
   __shared__ uint32_t w_tie[kWarps], w_keep[kWarps];
   __shared__ int first_sh;
 
-  const int e = blockIdx.x;
+  const int e = blockIdx.x / shares, share = blockIdx.x % shares;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  int L = a.L[e];
+  const int L = a.L[e];  // len_out may be L itself, but then the instance has one CTA
   int* kept_e = a.kept + static_cast<size_t>(e) * a.budget;
   if (L < 0 || L > s.cap) {  // the whole block
-    for (int i = tid; i < a.budget; i += THREADS) kept_e[i] = -1;
-    __syncthreads();  // len_out may be L itself
-    if (tid == 0) {
+    if (share == 0)
+      for (int i = tid; i < a.budget; i += THREADS) kept_e[i] = -1;
+    __syncthreads();
+    if (tid == 0 && share == 0) {
       record_error(a.err, kDevBadLength);
       if (a.len_out) a.len_out[e] = 0;
     }
@@ -130,17 +172,13 @@ __global__ void __launch_bounds__(THREADS) evict_kernel(Shape s, EvictArgs a) {
   float* w_out = a.weights_out + static_cast<size_t>(e) * a.cap_out;
   const int n_keep = min(L, a.budget);
 
-  // this warp's rows: row0 + 32 i + lane, rpw of them (a multiple of 32)
-  const int rpw = (L + kWarps * 32 - 1) / (kWarps * 32) * 32;
-  const int row0 = warp * rpw;
-  float w[KPT];
-  uint32_t key[KPT];
-#pragma unroll
-  for (int i = 0; i < KPT; ++i) {
-    const int j = row0 + i * 32 + lane;
-    w[i] = i * 32 < rpw && j < L ? w_in[j] : 0.f;
-    key[i] = weight_key(w[i]);
-  }
+  WarpRows<KPT> rows;
+  rows.n = (L + kWarps * 32 - 1) / (kWarps * 32);
+  rows.row0 = warp * rows.n * 32;
+  rows.w = w_in;
+  rows.L = L;
+  rows.lane = lane;
+  rows.init();
   if (tid == 0) first_sh = n_keep;
   uint32_t T = 0, ties = 0;
   const int c_lo = s.n_prefix, c_hi = L - s.W;
@@ -148,32 +186,30 @@ __global__ void __launch_bounds__(THREADS) evict_kernel(Shape s, EvictArgs a) {
   const int k_sel = a.budget - s.n_prefix - s.W;
   if (!all && k_sel > 0) {
     uint32_t prefix = 0, mask = 0, k = static_cast<uint32_t>(k_sel);
-    select_digit<THREADS, KPT, 12>(key, c_lo, c_hi, row0, rpw, 20, prefix, mask, k, hist, wsum, found);
-    select_digit<THREADS, KPT, 10>(key, c_lo, c_hi, row0, rpw, 10, prefix, mask, k, hist, wsum, found);
-    select_digit<THREADS, KPT, 10>(key, c_lo, c_hi, row0, rpw, 0, prefix, mask, k, hist, wsum, found);
+    select_digit<THREADS, KPT, 12>(rows, c_lo, c_hi, 20, prefix, mask, k, hist, wsum, found);
+    select_digit<THREADS, KPT, 10>(rows, c_lo, c_hi, 10, prefix, mask, k, hist, wsum, found);
+    select_digit<THREADS, KPT, 10>(rows, c_lo, c_hi, 0, prefix, mask, k, hist, wsum, found);
     T = prefix;
     ties = k;
   }
   // 0: not kept, 1: kept, 2: kept if it is among the first `ties` rows equal to T
-  auto kind = [&](int i) -> int {
-    const int j = row0 + i * 32 + lane;
-    if (i * 32 >= rpw || j >= L) return 0;
+  auto kind = [&](int j, uint32_t key) -> int {
+    if (j >= L) return 0;
     if (all || j < c_lo || j >= c_hi) return 1;
     if (k_sel <= 0) return 0;
-    return key[i] > T ? 1 : (key[i] == T ? 2 : 0);
+    return key > T ? 1 : (key == T ? 2 : 0);
   };
   uint32_t n_tie = 0, n_sure = 0;
-#pragma unroll
-  for (int i = 0; i < KPT; ++i) {
-    const int c = kind(i);
+  rows.each([&](int j, uint32_t key) {
+    const int c = kind(j, key);
     n_tie += __popc(__ballot_sync(0xffffffffu, c == 2));
     n_sure += __popc(__ballot_sync(0xffffffffu, c == 1));
-  }
+  });
   if (lane == 0) {
     w_tie[warp] = n_tie;
     w_keep[warp] = n_sure;
   }
-  __syncthreads();  // every weight has been read: the outputs may be the inputs
+  __syncthreads();
   uint32_t tie_at = 0, at = 0;
   for (int v = 0; v < warp; ++v) {
     const uint32_t t = w_tie[v];
@@ -181,83 +217,101 @@ __global__ void __launch_bounds__(THREADS) evict_kernel(Shape s, EvictArgs a) {
     tie_at += t;
   }
   const uint32_t below = (1u << lane) - 1u;
-#pragma unroll
-  for (int i = 0; i < KPT; ++i) {
-    const int c = kind(i);
+  rows.each([&](int j, uint32_t key) {
+    const int c = kind(j, key);
     const uint32_t tie_mask = __ballot_sync(0xffffffffu, c == 2);
     const bool keep = c == 1 || (c == 2 && tie_at + __popc(tie_mask & below) < ties);
     const uint32_t keep_mask = __ballot_sync(0xffffffffu, keep);
-    const int j = row0 + i * 32 + lane;
     const int pos = static_cast<int>(at + __popc(keep_mask & below));
     if (keep && in_bounds(pos, n_keep, a.err)) {
       kept_s[pos] = static_cast<uint16_t>(j);
-      kept_e[pos] = j;
-      w_out[pos] = w[i];
+      if (share == 0) kept_e[pos] = j;
       if (pos != j) atomicMin(&first_sh, pos);  // rows before it stand where they belong
     }
     tie_at += __popc(tie_mask);
     at += __popc(keep_mask);
-  }
-  for (int i = n_keep + tid; i < a.budget; i += THREADS) kept_e[i] = -1;
-  for (int i = n_keep + tid; i < a.cap_out; i += THREADS) w_out[i] = 0.f;
+  });
+  if (share == 0)
+    for (int i = n_keep + tid; i < a.budget; i += THREADS) kept_e[i] = -1;
   __syncthreads();
-  if (tid == 0 && a.len_out) a.len_out[e] = n_keep;
+  if (tid == 0 && share == 0 && a.len_out) a.len_out[e] = n_keep;
 
   // ---------------------------------------------------------------- gather
   constexpr int kVpr = D * 2 / 16;    // 16-byte vectors per row of one tensor
   constexpr int kRowVec = 2 * kVpr;   // K row, then V row
-  constexpr int kPer = 8;             // vectors per thread and chunk
+  constexpr int kPer = MINB > 1 ? 4 : 8;  // vectors per thread and chunk
   constexpr int kRowsPerPass = THREADS / kRowVec;
   constexpr int kChunkRows = kRowsPerPass * kPer;
+  static_assert(kChunkRows <= THREADS, "one weight per thread and chunk");
   const int col = tid % kRowVec, r0 = tid / kRowVec;
   const int vcol = col < kVpr ? col : col - kVpr;
   const uint4* src = reinterpret_cast<const uint4*>((col < kVpr ? a.K : a.V) + static_cast<size_t>(e) * s.cap * D) + vcol;
   uint4* dst = reinterpret_cast<uint4*>((col < kVpr ? a.K_out : a.V_out) + static_cast<size_t>(e) * a.cap_out * D) + vcol;
-  const int first = in_place ? first_sh : 0;
+  const int first = in_place ? first_sh : static_cast<int>(static_cast<long long>(n_keep) * share / shares);
+  const int end = in_place ? n_keep : static_cast<int>(static_cast<long long>(n_keep) * (share + 1) / shares);
 
   uint4 cur[kPer], nxt[kPer];
-  auto load_chunk = [&](int i0, uint4 (&R)[kPer]) {
+  float w_cur = 0.f, w_nxt = 0.f;
+  auto load_chunk = [&](int i0, uint4 (&R)[kPer], float& w) {
 #pragma unroll
     for (int u = 0; u < kPer; ++u) {
       const int row = i0 + r0 + kRowsPerPass * u;
-      if (row < n_keep) {
+      if (row < end) {
         int from = kept_s[row];
         if (!in_bounds(from - row, L - row, a.err)) from = row;  // row <= kept[row] < L
         R[u] = __ldcg(src + static_cast<size_t>(from) * kVpr);
       }
     }
+    if (tid < kChunkRows && i0 + tid < end) {
+      int from = kept_s[i0 + tid];
+      if (!in_bounds(from, L, a.err)) from = i0 + tid;
+      w = __ldcg(w_in + from);
+    }
   };
-  if (first < n_keep) load_chunk(first, cur);
-  for (int i0 = first; i0 < n_keep; i0 += kChunkRows) {
+  if (first < end) load_chunk(first, cur, w_cur);
+  for (int i0 = first; i0 < end; i0 += kChunkRows) {
     if (in_place) __syncthreads();  // every load of this chunk was issued before any of its stores
     const int i1 = i0 + kChunkRows;
-    if (i1 < n_keep) load_chunk(i1, nxt);
+    if (i1 < end) load_chunk(i1, nxt, w_nxt);
 #pragma unroll
     for (int u = 0; u < kPer; ++u) {
       const int row = i0 + r0 + kRowsPerPass * u;
-      if (row < n_keep) dst[static_cast<size_t>(row) * kVpr] = cur[u];
+      if (row < end) dst[static_cast<size_t>(row) * kVpr] = cur[u];
     }
+    if (tid < kChunkRows && i0 + tid < end) w_out[i0 + tid] = w_cur;
 #pragma unroll
     for (int u = 0; u < kPer; ++u) cur[u] = nxt[u];
+    w_cur = w_nxt;
   }
+  if (in_place) __syncthreads();  // the last kept weights have been read
+  for (int i = n_keep + share * THREADS + tid; i < a.cap_out; i += shares * THREADS) w_out[i] = 0.f;
 }
 
-template <int D, int THREADS, int KPT>
+template <int D, int THREADS, int KPT, int MINB>
 cudaError_t launch(const Shape& s, const EvictArgs& a, cudaStream_t st) {
-  const int smem = (a.budget < s.cap ? a.budget : s.cap) * static_cast<int>(sizeof(uint16_t));
-  const cudaError_t e = cudaFuncSetAttribute(evict_kernel<D, THREADS, KPT>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  const int kept = a.budget < s.cap ? a.budget : s.cap;
+  const int smem = kept * static_cast<int>(sizeof(uint16_t));
+  const cudaError_t e = cudaFuncSetAttribute(evict_kernel<D, THREADS, KPT, MINB>,
+                                             cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   if (e != cudaSuccess) return e;
-  evict_kernel<D, THREADS, KPT><<<s.n_inst, THREADS, smem, st>>>(s, a);
+  // Shares of an instance into other buffers: as many as bring the grid to kShareGrid CTAs, with rows
+  // enough for each (a selection costs what a few hundred rows do).
+  int shares = 1;
+  if (a.K_out != a.K && a.len_out != a.L) {
+    constexpr int kShareGrid = 304, kShareRows = 64;
+    shares = (kShareGrid + s.n_inst - 1) / s.n_inst;
+    if (shares > (kept + kShareRows - 1) / kShareRows) shares = (kept + kShareRows - 1) / kShareRows;
+  }
+  evict_kernel<D, THREADS, KPT, MINB><<<s.n_inst * shares, THREADS, smem, st>>>(s, a, shares);
   return cudaGetLastError();
 }
 
-// The capacity decides how many rows a CTA must be able to hold in registers.
+// The capacity decides whether a CTA can hold an instance's keys in registers.
 template <int D>
 cudaError_t launch_d(const Shape& s, const EvictArgs& a, cudaStream_t st) {
-  if (s.cap <= 256 * 8) return launch<D, 256, 8>(s, a, st);
-  if (s.cap <= 512 * 20) return launch<D, 512, 20>(s, a, st);
-  static_assert(kMaxCapacity <= 1024 * 32, "rows of the largest capacity in registers");
-  return launch<D, 1024, 32>(s, a, st);
+  if (s.cap <= 256 * 8) return launch<D, 256, 8, 1>(s, a, st);
+  if (s.cap <= 512 * 20) return launch<D, 512, 20, 1>(s, a, st);
+  return launch<D, 512, 0, 2>(s, a, st);
 }
 
 }  // namespace
