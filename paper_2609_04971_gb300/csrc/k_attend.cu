@@ -35,7 +35,8 @@ int attend_sms() {
 
 namespace {
 
-// Row blocks of m sequences x R rows with at most 128 rows each, as even as 16-row steps allow.
+// Row blocks of m sequences x R rows: all rows of an instance in one block while there are at most 128
+// of them, else blocks of at most 256, as even as 16-row steps allow.
 AtPlan make_plan(const Shape& s, int I, int m, int R, int n_q, bool causal, int cap, int len_div, int sms) {
   AtPlan p{};
   AtGeo& g = p.geo;
@@ -47,13 +48,14 @@ AtPlan make_plan(const Shape& s, int I, int m, int R, int n_q, bool causal, int 
   g.causal = causal;
   g.cap = cap;
   g.len_div = len_div;
-  if (R <= 128) {
-    const int most = 128 / R, nb = (m + most - 1) / most;
+  const int most_rows = 1ll * R * m <= 128 ? 128 : 256;
+  if (R <= most_rows) {
+    const int most = most_rows / R, nb = (m + most - 1) / most;
     g.rr = R;
     g.mb = (m + nb - 1) / nb;
     g.nr = 1;
   } else {
-    const int nr = (R + 127) / 128;
+    const int nr = (R + 255) / 256;
     g.rr = ((R + nr - 1) / nr + 15) / 16 * 16;
     g.mb = 1;
     g.nr = (R + g.rr - 1) / g.rr;
@@ -337,6 +339,7 @@ cudaError_t launch_attend(const Shape& s, const AttendArgs& a, cudaStream_t st) 
     k.logits = own ? logits : nullptr;
     k.err = a.err;
     k.after_prefix = own && l.has_prefix;
+    if (g.mb * g.rr > 128) return launch_attend_rows(s.d, p, qmap, kmap, vmap, k, st);
     return s.d == 128 ? launch_attend_tiles_128(p, qmap, kmap, vmap, k, st)
                       : launch_attend_tiles_64(p, qmap, kmap, vmap, k, st);
   };

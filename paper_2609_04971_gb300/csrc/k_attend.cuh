@@ -16,7 +16,10 @@
 
 namespace bkv {
 
-constexpr int kAtTile = 128;  // keys per tile
+constexpr int kAtTile = 128;             // keys per tile
+constexpr uint32_t kAtBox = 128 * 128;   // [128 rows][64 bf16] swizzled box
+constexpr float kMaxAbove = 32.f;        // log2 of how far p may exceed 1 before its reference moves
+constexpr float kRefFloor = -1e30f;
 
 struct AtGeo {
   int I;          // instances
@@ -124,6 +127,79 @@ __device__ __forceinline__ void at_split(int n, Count&& count, Find&& find, long
   __syncthreads();
 }
 
+// The split of a source's tiles.
+template <int THREADS>
+__device__ __forceinline__ void at_split_tiles(const AtGeo& g, long long* scan, AtShare* out) {
+  if (!g.causal || g.n_q == 1) {  // all row blocks of an instance have the same tiles
+    at_split<THREADS>(
+        g.I, [&](int e) { return static_cast<long long>(g.nrb) * at_tiles(at_len(g, e)); },
+        [&](int e, long long u) {
+          const int n = at_tiles(at_len(g, e));
+          return AtPlace{e, static_cast<int>(u / n), static_cast<int>(u % n)};
+        },
+        scan, out);
+  } else {
+    at_split<THREADS>(
+        g.I * g.nrb,
+        [&](int x) {
+          return static_cast<long long>(at_tiles(at_limit_max(g, at_len(g, x / g.nrb), at_block(g, x % g.nrb).r0)));
+        },
+        [&](int x, long long u) { return AtPlace{x / g.nrb, x % g.nrb, static_cast<int>(u)}; }, scan, out);
+  }
+}
+
+// Reports lengths out of range; by the threads of one CTA.
+template <int THREADS>
+__device__ __forceinline__ void at_check_lengths(const AtGeo& g, int* err) {
+  for (int e = threadIdx.x; e < g.I; e += THREADS) {
+    const int n = __ldg(g.len + e / g.len_div);
+    if (n < 0 || n > g.cap) record_error(err, kDevBadLength);
+  }
+}
+
+// One segment of a CTA's run.
+struct AtSeg {
+  int e, rb, t0, t1, T, len, r0, b0;
+  long long item, u;  // u: number of tile t0 in the run of all tiles
+};
+
+// Walks the CTA's segments; every role has its own.
+struct AtWalk {
+  int e, rb, t;
+  long long left, u;
+  __device__ __forceinline__ bool next(const AtGeo& g, AtSeg& s) {
+    if (left <= 0 || e >= g.I) return false;
+    const AtBlock blk = at_block(g, rb);
+    s.e = e;
+    s.rb = rb;
+    s.b0 = blk.b0;
+    s.r0 = blk.r0;
+    s.len = at_len(g, e);
+    s.T = at_tiles(at_limit_max(g, s.len, blk.r0));
+    s.t0 = t;
+    s.t1 = static_cast<int>(min(static_cast<long long>(s.T), t + left));
+    s.item = static_cast<long long>(e) * g.nrb + rb;
+    s.u = u;
+    u += s.t1 - s.t0;
+    left -= s.t1 - s.t0;
+    t = s.t1;
+    if (t == s.T) {
+      t = 0;
+      if (++rb == g.nrb) {
+        rb = 0;
+        ++e;
+      }
+    }
+    return true;
+  }
+};
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
 // Where one source's kernel leaves what the merge needs.  Segment `cta + item` is the part of an
 // item that a CTA worked on: both rise along the run of all segments, one of them by at least 1 from
 // each segment to the next, so the numbers differ.
@@ -218,7 +294,10 @@ cudaError_t launch_after(void (*kernel)(P...), unsigned blocks, unsigned threads
   return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-// One translation unit per head_dim.
+// Row blocks of up to 128 rows (k_attend_tiles.cuh, one translation unit per head_dim), and of up to
+// 256 (k_attend_rows.cu).
+cudaError_t launch_attend_rows(int d, const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap,
+                               const CUtensorMap& vmap, const AtKernelArgs& a, cudaStream_t st);
 cudaError_t launch_attend_tiles_64(const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap,
                                    const CUtensorMap& vmap, const AtKernelArgs& a, cudaStream_t st);
 cudaError_t launch_attend_tiles_128(const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap,

@@ -1,0 +1,415 @@
+// The attention kernel for row blocks of more than 128 query rows (whole prompts,
+// prefixes that many sequences share): compute bound, so the query rows are the
+// lanes.
+//
+// Persistent, one CTA per SM, the work split into segments as in k_attend.cuh.  A
+// row block is two row tiles of 128 that share every tile of keys and values:
+//   S_w [128 rows x 128 keys] = Q_w K_tile^T     (both from shared memory, K-major)
+//   P_w = 2^(scale S_w - ref)                    (registers; bf16, into tensor memory
+//                                                 in place of S_w)
+//   O_w [128 rows x D] += P_w V_tile             (P from tensor memory, V MN-major)
+// Each softmax group (four warps, one thread per row) has one of the row tiles to
+// itself: sum and reference are one register each, nothing is reduced across
+// lanes, and P takes no shared-memory traffic.  While one group computes
+// exponentials the tensor cores work for the other.
+//
+// The reference of a row is the logit of the segment's first key; only when a
+// logit of a tile exceeds it by more than 2^32 the warp moves its references to
+// the tile's maxima and scales its sums and its lanes of O (fp32 sums and bf16 P
+// have the exponent range for that).  S_w stays in tensor memory until the tile's P is
+// known to stand, so the exponentials need not wait for a maximum.
+//
+// Bound by the exponentials (16 per clock and SM: 1024 clocks for 128 x 128) and by
+// the tensor cores (1024 clocks for both products of 128 x 128 x 128) alike.
+#include "k_attend.cuh"
+
+namespace bkv {
+namespace {
+
+constexpr int kThreads = 384;  // producer, MMA, two idle warps; two groups of four
+constexpr int kRegsFew = 80, kRegsMany = 208;  // 80 + 2 x 208 of the 3 x 168 per scheduler at launch
+constexpr int kRows = 128;     // rows of a row tile
+
+template <int D>
+struct RowsCfg {
+  static constexpr int kBoxes = D / 64;
+  static constexpr uint32_t kTileBytes = kBoxes * kAtBox;
+  static constexpr uint32_t kQBox = 2 * kAtBox;  // 256 rows of 64 columns
+  static constexpr uint32_t kQBytes = kBoxes * kQBox;
+  static constexpr int kStages = D == 128 ? 5 : 10;
+  static constexpr size_t kSmem = 1024 + kQBytes + static_cast<size_t>(kStages) * kTileBytes;
+  // tensor memory: S_0, S_1 (P in their first 64 columns), O_0, O_1
+  static constexpr uint32_t kO = 2 * kAtTile;
+  static constexpr uint32_t kTmem = 512;
+};
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+    rows_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
+                const __grid_constant__ CUtensorMap vmap, AtKernelArgs a) {
+  using C = RowsCfg<D>;
+  extern __shared__ unsigned char smem_raw[];
+  __shared__ __align__(8) uint64_t full_bar[C::kStages], empty_bar[C::kStages];
+  __shared__ __align__(8) uint64_t qfull_bar, qempty_bar, sfull_bar[2], pfull_bar[2], ofull_bar[2], ofree_bar[2], drain_bar;
+  __shared__ uint32_t tmem_base_sh;
+  __shared__ int abort_sh;
+  __shared__ long long scan_sh[kThreads / 32];
+  __shared__ AtShare share_sh;
+
+  const AtGeo& g = a.geo;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  unsigned char* base = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+  unsigned char* q_smem = base;
+  unsigned char* kv_smem = base + C::kQBytes;
+  volatile int* abort_flag = &abort_sh;
+
+  if (tid == 32) {
+    prefetch_tmap(&qmap);
+    prefetch_tmap(&kmap);
+    prefetch_tmap(&vmap);
+  }
+  if (tid == 0) {
+    for (int i = 0; i < C::kStages; ++i) {
+      mbar_init(&full_bar[i], 1);
+      mbar_init(&empty_bar[i], 1);
+    }
+    mbar_init(&qfull_bar, 1);
+    mbar_init(&qempty_bar, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sfull_bar[i], 1);
+      mbar_init(&pfull_bar[i], 4);
+      mbar_init(&ofull_bar[i], 1);
+      mbar_init(&ofree_bar[i], 4);
+    }
+    mbar_init(&drain_bar, 1);
+    abort_sh = 0;
+    fence_mbar_init();
+  }
+  if (warp == 1) {
+    tmem_alloc(&tmem_base_sh, C::kTmem);
+    tmem_relinquish();
+  }
+  // rows of the Q buffer that no load fills are rows whose results are not used
+  for (uint32_t i = tid * 16; i < C::kQBytes; i += kThreads * 16)
+    *reinterpret_cast<uint4*>(q_smem + i) = make_uint4(0, 0, 0, 0);
+  fence_async_smem();
+
+  if (!a.after_prefix) grid_dependency_wait();  // whatever came before may have written the inputs
+  grid_dependents_go();
+  if (blockIdx.x == 0) at_check_lengths<kThreads>(g, a.err);
+  tc_fence_before();
+  at_split_tiles<kThreads>(g, scan_sh, &share_sh);
+  tc_fence_after();
+  if (blockIdx.x == 0 && tid == 0) *a.parts.per = share_sh.per;
+  const uint32_t tmem = tmem_base_sh;
+  AtWalk walk{share_sh.at.e, share_sh.at.k, share_sh.at.t, share_sh.left, share_sh.u};
+  const int n_tiles = static_cast<int>(share_sh.left);  // key tiles of this CTA
+
+  // Ring of stages: K(0), then for each tile i: V(i), K(i + 1).
+  if (warp < 4) {
+    set_max_regs_dec<kRegsFew>();
+    if (warp == 0) {
+      // -------------------------------------------------------------- producer
+      if (lane == 0 && n_tiles > 0) {
+        const uint64_t pol = l2_policy_evict_last();
+        int pos = 0, n_seg = 0;
+        bool ok = true;
+        auto load = [&](const CUtensorMap* map, int row) {
+          const int st = pos % C::kStages;
+          if (pos >= C::kStages &&
+              !mbar_wait(&empty_bar[st], ((pos / C::kStages) - 1) & 1, abort_flag, a.err, kDevTimeoutProducer)) {
+            ok = false;
+            return;
+          }
+          mbar_arrive_expect_tx(&full_bar[st], C::kTileBytes);
+          for (int b = 0; b < C::kBoxes; ++b)
+            tma_load_2d(kv_smem + st * C::kTileBytes + b * kAtBox, map, &full_bar[st], b * 64, row, pol);
+          ++pos;
+        };
+        auto load_q = [&](const AtSeg& s) {
+          if (n_seg >= 1 && !mbar_wait(&qempty_bar, (n_seg - 1) & 1, abort_flag, a.err, kDevTimeoutProducer)) {
+            ok = false;
+            return;
+          }
+          mbar_arrive_expect_tx(&qfull_bar, static_cast<uint32_t>(g.mb * g.rr) * D * 2);
+          for (int b = 0; b < C::kBoxes; ++b)
+            tma_load_4d(q_smem + b * C::kQBox, &qmap, &qfull_bar, b * 64, s.r0, s.e % g.n_kv, s.e / g.n_kv * g.m + s.b0,
+                        pol);
+          ++n_seg;
+        };
+        AtSeg s;
+        walk.next(g, s);
+        load_q(s);
+        if (ok) load(&kmap, s.e * g.cap + s.t0 * kAtTile);
+        int t = s.t0;
+        for (int i = 0; ok && i < n_tiles; ++i) {
+          load(&vmap, s.e * g.cap + t * kAtTile);
+          if (ok && i + 1 < n_tiles) {
+            if (++t == s.t1) {
+              walk.next(g, s);
+              t = s.t0;
+              load(&kmap, s.e * g.cap + t * kAtTile);
+              if (ok) load_q(s);
+            } else {
+              load(&kmap, s.e * g.cap + t * kAtTile);
+            }
+          }
+        }
+        if (!ok || *abort_flag) {  // let every copy already issued land before the CTA exits
+          int never = 0;
+          if (n_seg > 0) mbar_wait(&qfull_bar, (n_seg - 1) & 1, &never, a.err, kDevTimeoutDrain);
+          for (int p = max(0, pos - C::kStages); p < pos; ++p)
+            mbar_wait(&full_bar[p % C::kStages], (p / C::kStages) & 1, &never, a.err, kDevTimeoutDrain);
+        }
+      }
+      __syncwarp();
+    } else if (warp == 1) {
+      // -------------------------------------------------------------- MMA issuer
+      // Products run in the order in which they are issued, so S_w of the next tile may follow O_w of
+      // this one at once although it overwrites its P.
+      if (lane == 0) {
+        const uint32_t idesc_s = idesc_bf16_f32(kRows, kAtTile), idesc_o = idesc_bf16_f32(kRows, D) | kIdescMnMajorB;
+        bool ok = true;
+        auto ready = [&](int pos) {
+          ok = ok && mbar_wait(&full_bar[pos % C::kStages], (pos / C::kStages) & 1, abort_flag, a.err, kDevTimeoutMma);
+        };
+        auto issue_s = [&](int w, int pos) {
+          if (!ok) return;
+          tc_fence_after();
+          const uint32_t k_addr = smem_u32(kv_smem + pos % C::kStages * C::kTileBytes);
+          const uint32_t q_addr = smem_u32(q_smem + w * kAtBox);
+#pragma unroll
+          for (int kk = 0; kk < D / 16; ++kk)
+            mma_bf16_ss(tmem + w * kAtTile, sdesc_kmajor_sw128(q_addr + (kk >> 2) * C::kQBox + (kk & 3) * 32),
+                        sdesc_kmajor_sw128(k_addr + (kk >> 2) * kAtBox + (kk & 3) * 32), idesc_s, kk > 0);
+          mma_commit(&sfull_bar[w]);
+        };
+        auto issue_o = [&](int w, int i, int pos, int seg, bool first, bool last_of_seg) {
+          ok = ok && mbar_wait(&pfull_bar[w], i & 1, abort_flag, a.err, kDevTimeoutMma);
+          if (first && seg >= 1) ok = ok && mbar_wait(&ofree_bar[w], (seg - 1) & 1, abort_flag, a.err, kDevTimeoutMma);
+          if (!ok) return;
+          tc_fence_after();
+          const uint32_t v_addr = smem_u32(kv_smem + pos % C::kStages * C::kTileBytes);
+#pragma unroll
+          for (int kk = 0; kk < kAtTile / 16; ++kk)
+            mma_bf16_ts(tmem + C::kO + w * D, tmem + w * kAtTile + kk * 8, sdesc_mnmajor_sw128(v_addr + kk * 2048, kAtBox),
+                        idesc_o, !first || kk > 0);
+          if (last_of_seg) mma_commit(&ofull_bar[w]);
+        };
+        if (n_tiles > 0) {
+          AtSeg s;
+          walk.next(g, s);
+          int t = s.t0, seg = 0;
+          ok = ok && mbar_wait(&qfull_bar, 0, abort_flag, a.err, kDevTimeoutMma);
+          ready(0);
+          issue_s(0, 0);
+          issue_s(1, 0);
+          if (ok) mma_commit(&empty_bar[0]);
+          if (ok && s.t1 - s.t0 == 1) mma_commit(&qempty_bar);
+          for (int i = 0; ok && i < n_tiles; ++i) {
+            const int v_pos = 2 * i + 1, k_pos = 2 * i + 2;
+            const bool last = i + 1 == n_tiles, first = t == s.t0, turn = t + 1 == s.t1;
+            const int seg_o = seg;
+            ready(v_pos);
+            issue_o(0, i, v_pos, seg_o, first, turn);
+            if (!last) {
+              ++t;
+              if (turn) {
+                walk.next(g, s);
+                t = s.t0;
+                ++seg;
+                ok = ok && mbar_wait(&qfull_bar, seg & 1, abort_flag, a.err, kDevTimeoutMma);
+              }
+              ready(k_pos);
+              issue_s(0, k_pos);
+            }
+            issue_o(1, i, v_pos, seg_o, first, turn);
+            if (ok) mma_commit(&empty_bar[v_pos % C::kStages]);
+            if (!last) {
+              issue_s(1, k_pos);
+              if (ok) mma_commit(&empty_bar[k_pos % C::kStages]);
+              if (ok && t + 1 == s.t1) mma_commit(&qempty_bar);
+            }
+          }
+        }
+        mma_commit(&drain_bar);  // every MMA issued above has finished once this arrives
+        int never = 0;
+        mbar_wait(&drain_bar, 0, &never, a.err, kDevTimeoutDrain);
+      }
+      __syncwarp();
+    }
+  } else {
+    set_max_regs_inc<kRegsMany>();
+    // ---------------------------------------------------------------- softmax
+    const int w = (warp - 4) >> 2;                       // row tile of the group
+    const int lane_row = (warp & 3) * 32 + lane;         // row of it (tensor-memory lane)
+    const uint32_t lane_addr = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t s_addr = tmem + w * kAtTile + lane_addr, o_addr = tmem + C::kO + w * D + lane_addr;
+    const int c = w * kRows + lane_row, cols = g.mb * g.rr;  // row of the block
+    const float sc = a.sc;
+    auto wait = [&](uint64_t* bar, uint32_t parity) {  // after an abort every wait returns at once
+      if (!mbar_try_wait(bar, parity) && !*abort_flag) mbar_wait(bar, parity, abort_flag, a.err, kDevTimeoutEpilogue);
+      __syncwarp();
+    };
+    AtSeg s, next;
+    int i = 0;  // tile of the CTA
+    bool more = walk.next(g, next);
+    for (int seg = 0; more; ++seg) {
+      s = next;
+      more = walk.next(g, next);
+      const int row = c < cols ? at_row(g, s.e, {s.b0, s.r0}, c) : -1;
+      const int lim = row < 0 ? 0 : g.causal ? max(0, s.len - g.n_q + 1 + (s.r0 + c % g.rr) % g.n_q) : s.len;
+      const int lim_min = __reduce_min_sync(0xffffffffu, row < 0 ? 0x7fffffff : lim);  // of the warp's rows
+      const int limit_max = at_limit_max(g, s.len, s.r0);
+      if (tid == 128 && s.t0 == 0) a.parts.u0[s.item] = s.u;
+      float ref = 0.f, l = 0.f;  // ref: minus the reference
+      for (int t = s.t0; t < s.t1; ++t, ++i) {
+        const int k0 = t * kAtTile, seen = lim - k0;  // keys of the tile that the row sees
+        const bool masked = k0 + kAtTile > lim_min;
+        wait(&sfull_bar[w], i & 1);
+        tc_fence_after();
+        uint32_t p[kAtTile / 2];
+        float top = -INFINITY, sum = 0.f;
+        // the tile's weights against the present reference; the largest exponent in `top`
+        auto weigh = [&](bool first) {
+          sum = 0.f;
+          top = -INFINITY;
+          float y[2][32];
+          tmem_ld32(s_addr, y[0]);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            float(&v)[32] = y[q & 1];
+            tmem_wait_ld();
+            if (q < 3) tmem_ld32(s_addr + (q + 1) * 32, y[(q + 1) & 1]);
+            if (q == 0 && first) ref = seen > 0 ? -fmaxf(v[0] * sc, kRefFloor) : 0.f;
+#pragma unroll
+            for (int x = 0; x < 32; ++x) v[x] = fmaf(v[x], sc, ref);
+            if (masked) {
+#pragma unroll
+              for (int x = 0; x < 32; ++x) v[x] = q * 32 + x < seen ? v[x] : -INFINITY;
+            }
+            float m0 = v[0], m1 = v[1], s0 = 0.f, s1 = 0.f;
+#pragma unroll
+            for (int x = 2; x < 32; x += 2) {
+              m0 = fmaxf(m0, v[x]);
+              m1 = fmaxf(m1, v[x + 1]);
+            }
+            top = fmaxf(top, fmaxf(m0, m1));
+#pragma unroll
+            for (int x = 0; x < 32; x += 2) {
+              const float e0 = ex2_approx(v[x]), e1 = ex2_approx(v[x + 1]);
+              s0 += e0;
+              s1 += e1;
+              p[q * 16 + x / 2] = pack_bf16(e0, e1);
+            }
+            sum += s0 + s1;
+          }
+        };
+        weigh(t == s.t0);
+        if (__any_sync(0xffffffffu, top > kMaxAbove)) {
+          // Move the references up to the tile's maxima.  The products of the tiles before are complete:
+          // the barrier of this tile's S was waited for, and they were issued before it.
+          const float up = fmaxf(top, 0.f), f = ex2_approx(-up);
+          ref -= up;
+          l *= f;
+          if (t > s.t0) {
+#pragma unroll 1
+            for (int x = 0; x < D; x += 8) {
+              float o8[8];
+              tmem_ld8(o_addr + x, o8);
+              tmem_wait_ld();
+#pragma unroll
+              for (int z = 0; z < 8; ++z) o8[z] *= f;
+              tmem_st8(o_addr + x, o8);
+            }
+            tmem_wait_st();
+          }
+          weigh(false);
+        }
+        l += sum;
+        tmem_st32(s_addr, p);
+        tmem_st32(s_addr + 32, p + 32);
+        tmem_wait_st();
+        if (w == 0 && k0 + kAtTile > limit_max && k0 + lane_row >= limit_max) {
+          // rows of V that no row of the item sees must not hold what 0 times it is not 0
+          const int v_pos = 2 * i + 1, st = v_pos % C::kStages;
+          if (!*abort_flag) mbar_wait(&full_bar[st], (v_pos / C::kStages) & 1, abort_flag, a.err, kDevTimeoutEpilogue);
+#pragma unroll
+          for (int b = 0; b < C::kBoxes; ++b)
+#pragma unroll
+            for (int x = 0; x < 8; ++x)
+              *reinterpret_cast<uint4*>(kv_smem + st * C::kTileBytes + b * kAtBox + lane_row * 128 + x * 16) =
+                  make_uint4(0, 0, 0, 0);
+          fence_async_smem();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&pfull_bar[w]);
+      }
+      // ---- the segment's result
+      const bool final_rows = a.whole_is_final && s.t0 == 0 && s.t1 == s.T;
+      const long long part = blockIdx.x + s.item;
+      const bool some = l != 0.f;  // a NaN stays one
+      if (row >= 0) {
+        if (final_rows) {
+          const float y2 = some ? log2f(l) - ref : -INFINITY;
+          a.lse2[row] = y2;
+          if (a.lse) a.lse[row] = y2 * 0.69314718055994531f;
+        } else {
+          a.parts.ml[part * a.parts.rows + c] = make_float2(-ref, l);
+        }
+      }
+      const float inv = some ? 1.f / l : 0.f;
+      wait(&ofull_bar[w], seg & 1);
+      tc_fence_after();
+      float* dst = a.parts.o + (part * a.parts.rows + c) * D;
+#pragma unroll 1
+      for (int x = 0; x < D; x += 32) {
+        float o[32];
+        tmem_ld32(o_addr + x, o);
+        tmem_wait_ld();
+        if (row >= 0) {
+          if (final_rows) {
+#pragma unroll
+            for (int z = 0; z < 32; z += 8) {
+              const uint4 v = make_uint4(pack_bf16(o[z] * inv, o[z + 1] * inv), pack_bf16(o[z + 2] * inv, o[z + 3] * inv),
+                                         pack_bf16(o[z + 4] * inv, o[z + 5] * inv), pack_bf16(o[z + 6] * inv, o[z + 7] * inv));
+              *reinterpret_cast<uint4*>(a.o + static_cast<size_t>(row) * D + x + z) = v;
+            }
+          } else {
+#pragma unroll
+            for (int z = 0; z < 32; z += 4)
+              *reinterpret_cast<float4*>(dst + x + z) = make_float4(o[z], o[z + 1], o[z + 2], o[z + 3]);
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&ofree_bar[w]);
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (warp == 1) tmem_dealloc(tmem, C::kTmem);
+  if (a.after_prefix) grid_dependency_wait();  // what follows this kernel needs the prefix's results too
+}
+
+template <int D>
+cudaError_t launch(const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap, const CUtensorMap& vmap,
+                   const AtKernelArgs& a, cudaStream_t st) {
+  using C = RowsCfg<D>;
+  const cudaError_t e =
+      cudaFuncSetAttribute(rows_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(C::kSmem));
+  if (e != cudaSuccess) return e;
+  return launch_after(rows_kernel<D>, p.grid, kThreads, C::kSmem, st, qmap, kmap, vmap, a);
+}
+
+}  // namespace
+
+cudaError_t launch_attend_rows(int d, const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap,
+                               const CUtensorMap& vmap, const AtKernelArgs& a, cudaStream_t st) {
+  return d == 128 ? launch<128>(p, qmap, kmap, vmap, a, st) : launch<64>(p, qmap, kmap, vmap, a, st);
+}
+
+}  // namespace bkv

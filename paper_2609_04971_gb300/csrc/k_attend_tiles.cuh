@@ -39,11 +39,8 @@ constexpr int kAtThreads = 32 * (4 + kSmWarps);
 // Registers: 168 a thread at launch; the first four warps give back what the softmax warps take, 80 + 2 x 208
 // of 3 x 168 per scheduler.
 constexpr int kRegsFew = 80, kRegsMany = 208;
-constexpr uint32_t kAtBox = 128 * 128;       // [128 rows][64 bf16]
 constexpr int kAtMaxStages = 12;
 constexpr size_t kAtSmem = 218 * 1024;       // dynamic shared memory, next to up to 8 KB of static
-constexpr float kMaxAbove = 32.f;            // log2 of how far p may exceed 1
-constexpr float kRefFloor = -1e30f;
 
 // U: 8-column units per softmax group; N = 16 U columns.
 template <int D, int U>
@@ -63,42 +60,6 @@ struct AtCfg {
   static constexpr int kNC = N / 2;  // columns of a softmax group
   static constexpr uint32_t kTmem = U <= 1 ? 64 : U <= 2 ? 128 : U <= 4 ? 256 : 512;  // S, S, O, O of N columns
   static_assert(kStages >= 3, "K of the next tile, V of this one, and one in flight");
-};
-
-struct Seg {
-  int e, rb, t0, t1, T, len, r0, b0;
-  long long item, u;  // u: number of tile t0 in the run of all tiles
-};
-
-// Walks the CTA's segments; every role has its own.
-struct Walk {
-  int e, rb, t;
-  long long left, u;
-  __device__ __forceinline__ bool next(const AtGeo& g, Seg& s) {
-    if (left <= 0 || e >= g.I) return false;
-    const AtBlock blk = at_block(g, rb);
-    s.e = e;
-    s.rb = rb;
-    s.b0 = blk.b0;
-    s.r0 = blk.r0;
-    s.len = at_len(g, e);
-    s.T = at_tiles(at_limit_max(g, s.len, blk.r0));
-    s.t0 = t;
-    s.t1 = static_cast<int>(min(static_cast<long long>(s.T), t + left));
-    s.item = static_cast<long long>(e) * g.nrb + rb;
-    s.u = u;
-    u += s.t1 - s.t0;
-    left -= s.t1 - s.t0;
-    t = s.t1;
-    if (t == s.T) {
-      t = 0;
-      if (++rb == g.nrb) {
-        rb = 0;
-        ++e;
-      }
-    }
-    return true;
-  }
 };
 
 // NC column sums of each lane, summed over the warp: the totals of columns first .. first + n - 1 end up
@@ -147,12 +108,6 @@ __device__ __forceinline__ void tmem_ld_units(uint32_t taddr, float (&v)[8 * U])
   for (int c = 0; c < n32; c += 32) tmem_ld32(taddr + c, *reinterpret_cast<float(*)[32]>(v + c));
   if constexpr (U & 2) tmem_ld16(taddr + n32, v + n32);
   if constexpr (U & 1) tmem_ld8(taddr + 8 * U - 8, v + 8 * U - 8);
-}
-
-__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
-  uint32_t r;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-  return r;
 }
 
 // What is left of (lo, hi) beside the bf16 pair `p` that they were rounded to.
@@ -228,33 +183,13 @@ __global__ void __launch_bounds__(kAtThreads, 1)
 
   if (!a.after_prefix) grid_dependency_wait();  // whatever came before may have written the inputs
   grid_dependents_go();
-  if (blockIdx.x == 0) {
-    for (int e = tid; e < g.I; e += kAtThreads) {
-      const int n = __ldg(g.len + e / g.len_div);
-      if (n < 0 || n > g.cap) record_error(a.err, kDevBadLength);
-    }
-  }
+  if (blockIdx.x == 0) at_check_lengths<kAtThreads>(g, a.err);
   tc_fence_before();
-  if (!g.causal || g.n_q == 1) {  // all row blocks of an instance have the same tiles
-    at_split<kAtThreads>(
-        g.I, [&](int e) { return static_cast<long long>(g.nrb) * at_tiles(at_len(g, e)); },
-        [&](int e, long long u) {
-          const int n = at_tiles(at_len(g, e));
-          return AtPlace{e, static_cast<int>(u / n), static_cast<int>(u % n)};
-        },
-        scan_sh, &share_sh);
-  } else {
-    at_split<kAtThreads>(
-        g.I * g.nrb,
-        [&](int x) {
-          return static_cast<long long>(at_tiles(at_limit_max(g, at_len(g, x / g.nrb), at_block(g, x % g.nrb).r0)));
-        },
-        [&](int x, long long u) { return AtPlace{x / g.nrb, x % g.nrb, static_cast<int>(u)}; }, scan_sh, &share_sh);
-  }
+  at_split_tiles<kAtThreads>(g, scan_sh, &share_sh);
   tc_fence_after();
   if (blockIdx.x == 0 && tid == 0) *a.parts.per = share_sh.per;
   const uint32_t tmem = tmem_base_sh;
-  Walk walk{share_sh.at.e, share_sh.at.k, share_sh.at.t, share_sh.left, share_sh.u};
+  AtWalk walk{share_sh.at.e, share_sh.at.k, share_sh.at.t, share_sh.left, share_sh.u};
   const int n_tiles = static_cast<int>(share_sh.left);  // tiles of this CTA (below 2^31)
 
   // Ring positions.  Tile i of the CTA: K(0); then for each i: K(i + 1), V(i), but V(i) first where
@@ -280,7 +215,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
             tma_load_2d(kv_smem + st * C::kTileBytes + b * kAtBox, map, &full_bar[st], b * 64, row, pol);
           ++pos;
         };
-        auto load_q = [&](const Seg& s) {
+        auto load_q = [&](const AtSeg& s) {
           const int qb = n_seg % C::kQBufs;
           if (n_seg >= C::kQBufs &&
               !mbar_wait(&qempty_bar[qb], (n_seg / C::kQBufs - 1) & 1, abort_flag, a.err, kDevTimeoutProducer)) {
@@ -293,7 +228,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
                         s.e / g.n_kv * g.m + s.b0, pol_q);
           ++n_seg;
         };
-        Seg s;
+        AtSeg s;
         walk.next(g, s);
         load_q(s);
         if (ok) load(&kmap, s.e * g.cap + s.t0 * kAtTile);
@@ -368,7 +303,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
           ++pos;
         };
         if (n_tiles > 0) {
-          Seg s;
+          AtSeg s;
           walk.next(g, s);
           int t = s.t0, seg = 0;
           issue_s(0, 0, true, s.t1 - s.t0 == 1);
@@ -456,7 +391,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
       __syncwarp();
       if (lane == 0) mbar_arrive(&ofree_bar[out_seg & 1]);
     };
-    Seg s, next;
+    AtSeg s, next;
     int i = 0;  // tile of the CTA
     bool more = walk.next(g, next);
     for (int seg = 0; more; ++seg) {

@@ -13,17 +13,18 @@
 // workspace (a CTA has two at most: its first and its last) and a second launch
 // adds them in order.
 //
-// Warp roles as in k_attend_tiles.cu.  Bound by the exponentials: 128 x 128 of
+// Warp roles: warp 0 TMA producer, warp 1 MMA issue, sixteen warps of exponentials in
+// four groups, a quarter of the columns each.  Bound by the exponentials: 128 x 128 of
 // them per unit at 16 per clock and SM, twice what the matrix product takes.
 #include "k_attend.cuh"
 
 namespace bkv {
 namespace {
 
-constexpr int kSmWarps = 8;
+constexpr int kSmWarps = 16, kGroups = kSmWarps / 4;  // groups of four warps share the columns
 constexpr int kThreads = 32 * (2 + kSmWarps);
 constexpr uint32_t kBox = 128 * 128;
-constexpr int kCols = 128, kNC = kCols / 2;
+constexpr int kCols = 128, kNC = kCols / kGroups;
 constexpr uint32_t kTmem = 2 * kCols;
 
 struct WArgs {
@@ -137,7 +138,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __shared__ AtShare share_sh;
   __shared__ __align__(16) float lse_sh[2][kCols];
   __shared__ __align__(16) int lim_sh[2][kCols];
-  __shared__ float sum_sh[kAtTile];
+  __shared__ float sum_sh[kGroups][kAtTile];
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   unsigned char* base = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -352,10 +353,11 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       acc += (s0 + s1) + (s2 + s3);
       if (!more || v.k == 0) {  // the item's last unit here
-        if (grp == 1) sum_sh[key_lane] = acc;
-        named_barrier(3, 256);
+        sum_sh[grp][key_lane] = acc;
+        named_barrier(1 + kGroups, 32 * kSmWarps);
         if (grp == 0) {
-          const float sum = acc + sum_sh[key_lane];
+          float sum = acc;
+          for (int x = 1; x < kGroups; ++x) sum += sum_sh[x][key_lane];
           if (from_start && u.k + 1 == u.n) {
             if (j < u.len) a.weights[static_cast<size_t>(u.e) * a.cap + j] += sum;
           } else {
@@ -364,7 +366,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             a.parts[(static_cast<size_t>(blockIdx.x) * 2 + second) * kAtTile + key_lane] = sum;
           }
         }
-        named_barrier(3, 256);
+        named_barrier(1 + kGroups, 32 * kSmWarps);
         acc = 0.f;
         from_start = true;
         if (more && wt == 0 && grp == 0) a.u0[static_cast<size_t>(v.e) * a.tiles + v.t] = share.u + i + 1;
