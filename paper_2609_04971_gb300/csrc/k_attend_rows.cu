@@ -167,75 +167,86 @@ __global__ void __launch_bounds__(kThreads, 1)
       // -------------------------------------------------------------- MMA issuer
       // Products run in the order in which they are issued, so S_w of the next tile may follow O_w of
       // this one at once although it overwrites its P.
-      if (lane == 0) {
-        const uint32_t idesc_s = idesc_bf16_f32(kRows, kAtTile), idesc_o = idesc_bf16_f32(kRows, D) | kIdescMnMajorB;
-        bool ok = true;
-        auto ready = [&](int pos) {
-          ok = ok && mbar_wait(&full_bar[pos % C::kStages], (pos / C::kStages) & 1, abort_flag, a.err, kDevTimeoutMma);
-        };
-        auto issue_s = [&](int w, int pos) {
-          if (!ok) return;
-          tc_fence_after();
-          const uint32_t k_addr = smem_u32(kv_smem + pos % C::kStages * C::kTileBytes);
-          const uint32_t q_addr = smem_u32(q_smem + w * kAtBox);
+      // The whole warp walks along and one lane issues, so that descriptors stay in uniform registers.
+      const uint32_t idesc_s = idesc_bf16_f32(kRows, kAtTile), idesc_o = idesc_bf16_f32(kRows, D) | kIdescMnMajorB;
+      const uint32_t kv_addr = smem_u32(kv_smem), q_addr = smem_u32(q_smem);
+      const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+      bool ok = true;
+      auto await = [&](uint64_t* bar, uint32_t parity) {
+        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, a.err, kDevTimeoutMma));
+      };
+      auto issue_s = [&](int w, int st) {
+        if (!ok) return;
+        tc_fence_after();
+        const uint64_t q = sdesc_kmajor_sw128(q_addr + w * kAtBox), k = sdesc_kmajor_sw128(kv_addr + st * C::kTileBytes);
+        if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk)
-            mma_bf16_ss(tmem + w * kAtTile, sdesc_kmajor_sw128(q_addr + (kk >> 2) * C::kQBox + (kk & 3) * 32),
-                        sdesc_kmajor_sw128(k_addr + (kk >> 2) * kAtBox + (kk & 3) * 32), idesc_s, kk > 0);
+            mma_bf16_ss(tm + w * kAtTile, q + (((kk >> 2) * C::kQBox + (kk & 3) * 32) >> 4),
+                        k + (((kk >> 2) * kAtBox + (kk & 3) * 32) >> 4), idesc_s, kk > 0);
           mma_commit(&sfull_bar[w]);
-        };
-        auto issue_o = [&](int w, int i, int pos, int seg, bool first, bool last_of_seg) {
-          ok = ok && mbar_wait(&pfull_bar[w], i & 1, abort_flag, a.err, kDevTimeoutMma);
-          if (first && seg >= 1) ok = ok && mbar_wait(&ofree_bar[w], (seg - 1) & 1, abort_flag, a.err, kDevTimeoutMma);
-          if (!ok) return;
-          tc_fence_after();
-          const uint32_t v_addr = smem_u32(kv_smem + pos % C::kStages * C::kTileBytes);
+        }
+        __syncwarp();
+      };
+      auto issue_o = [&](int w, int i, int st, int seg, bool first, bool last_of_seg) {
+        await(&pfull_bar[w], i & 1);
+        if (first && seg >= 1) await(&ofree_bar[w], (seg - 1) & 1);
+        if (!ok) return;
+        tc_fence_after();
+        const uint64_t v = sdesc_mnmajor_sw128(kv_addr + st * C::kTileBytes, kAtBox);
+        if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < kAtTile / 16; ++kk)
-            mma_bf16_ts(tmem + C::kO + w * D, tmem + w * kAtTile + kk * 8, sdesc_mnmajor_sw128(v_addr + kk * 2048, kAtBox),
-                        idesc_o, !first || kk > 0);
+            mma_bf16_ts(tm + C::kO + w * D, tm + w * kAtTile + kk * 8, v + kk * (2048 >> 4), idesc_o, !first || kk > 0);
           if (last_of_seg) mma_commit(&ofull_bar[w]);
-        };
-        if (n_tiles > 0) {
-          AtSeg s;
-          walk.next(g, s);
-          int t = s.t0, seg = 0;
-          ok = ok && mbar_wait(&qfull_bar, 0, abort_flag, a.err, kDevTimeoutMma);
-          ready(0);
-          issue_s(0, 0);
-          issue_s(1, 0);
-          if (ok) mma_commit(&empty_bar[0]);
-          if (ok && s.t1 - s.t0 == 1) mma_commit(&qempty_bar);
-          for (int i = 0; ok && i < n_tiles; ++i) {
-            const int v_pos = 2 * i + 1, k_pos = 2 * i + 2;
-            const bool last = i + 1 == n_tiles, first = t == s.t0, turn = t + 1 == s.t1;
-            const int seg_o = seg;
-            ready(v_pos);
-            issue_o(0, i, v_pos, seg_o, first, turn);
-            if (!last) {
-              ++t;
-              if (turn) {
-                walk.next(g, s);
-                t = s.t0;
-                ++seg;
-                ok = ok && mbar_wait(&qfull_bar, seg & 1, abort_flag, a.err, kDevTimeoutMma);
-              }
-              ready(k_pos);
-              issue_s(0, k_pos);
+        }
+        __syncwarp();
+      };
+      auto commit = [&](uint64_t* bar) {
+        if (ok && elect_one()) mma_commit(bar);
+        __syncwarp();
+      };
+      if (n_tiles > 0) {
+        AtSeg s;
+        walk.next(g, s);
+        int t = s.t0, seg = 0;
+        await(&qfull_bar, 0);
+        await(&full_bar[0], 0);
+        issue_s(0, 0);
+        issue_s(1, 0);
+        commit(&empty_bar[0]);
+        if (s.t1 - s.t0 == 1) commit(&qempty_bar);
+        int pos = 1;  // ring position of V(i)
+        for (int i = 0; ok && i < n_tiles; ++i, pos += 2) {
+          const int v_st = pos % C::kStages, k_st = (pos + 1) % C::kStages;
+          const bool last = i + 1 == n_tiles, first = t == s.t0, turn = t + 1 == s.t1;
+          const int seg_o = seg;
+          await(&full_bar[v_st], (pos / C::kStages) & 1);
+          issue_o(0, i, v_st, seg_o, first, turn);
+          if (!last) {
+            ++t;
+            if (turn) {
+              walk.next(g, s);
+              t = s.t0;
+              ++seg;
+              await(&qfull_bar, seg & 1);
             }
-            issue_o(1, i, v_pos, seg_o, first, turn);
-            if (ok) mma_commit(&empty_bar[v_pos % C::kStages]);
-            if (!last) {
-              issue_s(1, k_pos);
-              if (ok) mma_commit(&empty_bar[k_pos % C::kStages]);
-              if (ok && t + 1 == s.t1) mma_commit(&qempty_bar);
-            }
+            await(&full_bar[k_st], ((pos + 1) / C::kStages) & 1);
+            issue_s(0, k_st);
+          }
+          issue_o(1, i, v_st, seg_o, first, turn);
+          commit(&empty_bar[v_st]);
+          if (!last) {
+            issue_s(1, k_st);
+            commit(&empty_bar[k_st]);
+            if (t + 1 == s.t1) commit(&qempty_bar);
           }
         }
-        mma_commit(&drain_bar);  // every MMA issued above has finished once this arrives
-        int never = 0;
-        mbar_wait(&drain_bar, 0, &never, a.err, kDevTimeoutDrain);
       }
+      if (elect_one()) mma_commit(&drain_bar);  // every MMA issued above has finished once this arrives
+      __syncwarp();
+      int never = 0;
+      mbar_wait(&drain_bar, 0, &never, a.err, kDevTimeoutDrain);
       __syncwarp();
     }
   } else {

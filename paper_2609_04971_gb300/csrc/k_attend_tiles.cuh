@@ -260,74 +260,83 @@ __global__ void __launch_bounds__(kAtThreads, 1)
       __syncwarp();
     } else if (warp == 1) {
       // ---------------------------------------------------------------- MMA issuer
-      if (lane == 0) {
-        const int cols = (g.mb * g.rr + 15) / 16 * 16;
-        const uint32_t idesc_s = idesc_bf16_f32(128, cols);
-        const uint32_t idesc_o = idesc_s | kIdescMnMajorA | kIdescMnMajorB;
-        const uint32_t v_box = C::kBoxes > 1 ? kAtBox : 0;  // head_dim 64: lanes 64 .. 127 repeat 0 .. 63
-        int pos = 0;
-        bool ok = true;
-        auto issue_s = [&](int i, int seg, bool first, bool last_of_seg) {
-          const int st = pos % C::kStages, buf = i & 1, qb = seg % C::kQBufs;
-          if (first) ok = ok && mbar_wait(&qfull_bar[qb], (seg / C::kQBufs) & 1, abort_flag, a.err, kDevTimeoutMma);
-          ok = ok && mbar_wait(&full_bar[st], (pos / C::kStages) & 1, abort_flag, a.err, kDevTimeoutMma);
-          if (i >= 2) ok = ok && mbar_wait(&sfree_bar[buf], ((i >> 1) - 1) & 1, abort_flag, a.err, kDevTimeoutMma);
-          if (!ok) return;
-          tc_fence_after();
-          const uint32_t k_addr = smem_u32(kv_smem + st * C::kTileBytes), q_addr = smem_u32(q_smem + qb * C::kQBytes);
+      // The whole warp walks along and one lane issues, so that descriptors stay in uniform registers.
+      const uint32_t idesc_s = idesc_bf16_f32(128, N);
+      const uint32_t idesc_o = idesc_s | kIdescMnMajorA | kIdescMnMajorB;
+      const uint32_t v_box = C::kBoxes > 1 ? kAtBox : 0;  // head_dim 64: lanes 64 .. 127 repeat 0 .. 63
+      const uint32_t kv_addr = smem_u32(kv_smem), q_addr = smem_u32(q_smem), p_addr = smem_u32(p_smem);
+      const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+      int pos = 0;
+      bool ok = true;
+      auto await = [&](uint64_t* bar, uint32_t parity) {
+        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, a.err, kDevTimeoutMma));
+      };
+      auto issue_s = [&](int i, int seg, bool first, bool last_of_seg) {
+        const int st = pos % C::kStages, buf = i & 1, qb = seg % C::kQBufs;
+        if (first) await(&qfull_bar[qb], (seg / C::kQBufs) & 1);
+        await(&full_bar[st], (pos / C::kStages) & 1);
+        if (i >= 2) await(&sfree_bar[buf], ((i >> 1) - 1) & 1);
+        if (!ok) return;
+        tc_fence_after();
+        const uint64_t k = sdesc_kmajor_sw128(kv_addr + st * C::kTileBytes), q = sdesc_kmajor_sw128(q_addr + qb * C::kQBytes);
+        if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk)
-            mma_bf16_ss(tmem + buf * N, sdesc_kmajor_sw128(k_addr + (kk >> 2) * kAtBox + (kk & 3) * 32),
-                        sdesc_kmajor_sw128(q_addr + (kk >> 2) * C::kQBox + (kk & 3) * 32), idesc_s, kk > 0);
+            mma_bf16_ss(tm + buf * N, k + (((kk >> 2) * kAtBox + (kk & 3) * 32) >> 4),
+                        q + (((kk >> 2) * C::kQBox + (kk & 3) * 32) >> 4), idesc_s, kk > 0);
           mma_commit(&empty_bar[st]);
           mma_commit(&sfull_bar[buf]);
           if (last_of_seg) mma_commit(&qempty_bar[qb]);
-          ++pos;
-        };
-        auto issue_o = [&](int i, int seg, bool first, bool last_of_seg) {
-          const int st = pos % C::kStages, pb = i % C::kPBufs, ob = seg & 1;
-          ok = ok && mbar_wait(&full_bar[st], (pos / C::kStages) & 1, abort_flag, a.err, kDevTimeoutMma);
-          ok = ok && mbar_wait(&pfull_bar[pb], (i / C::kPBufs) & 1, abort_flag, a.err, kDevTimeoutMma);
-          if (first && seg >= 2)
-            ok = ok && mbar_wait(&ofree_bar[ob], ((seg >> 1) - 1) & 1, abort_flag, a.err, kDevTimeoutMma);
-          if (!ok) return;
-          tc_fence_after();
-          const uint32_t v_addr = smem_u32(kv_smem + st * C::kTileBytes), p_addr = smem_u32(p_smem + pb * C::kPBytes);
+        }
+        __syncwarp();
+        ++pos;
+      };
+      auto issue_o = [&](int i, int seg, bool first, bool last_of_seg) {
+        const int st = pos % C::kStages, pb = i % C::kPBufs, ob = seg & 1;
+        await(&full_bar[st], (pos / C::kStages) & 1);
+        await(&pfull_bar[pb], (i / C::kPBufs) & 1);
+        if (first && seg >= 2) await(&ofree_bar[ob], ((seg >> 1) - 1) & 1);
+        if (!ok) return;
+        tc_fence_after();
+        const uint64_t v = sdesc_mnmajor_sw128(kv_addr + st * C::kTileBytes, v_box);
+        const uint64_t p = sdesc_mnmajor_sw128(p_addr + pb * C::kPBytes, kAtBox);
+        if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < kAtTile / 16; ++kk)
-            mma_bf16_ss(tmem + (2 + ob) * N, sdesc_mnmajor_sw128(v_addr + kk * 2048, v_box),
-                        sdesc_mnmajor_sw128(p_addr + kk * 2048, kAtBox), idesc_o, !first || kk > 0);
+            mma_bf16_ss(tm + (2 + ob) * N, v + kk * (2048 >> 4), p + kk * (2048 >> 4), idesc_o, !first || kk > 0);
           mma_commit(&empty_bar[st]);
           mma_commit(&pfree_bar[pb]);
           if (last_of_seg) mma_commit(&ofull_bar[ob]);
-          ++pos;
-        };
-        if (n_tiles > 0) {
-          AtSeg s;
-          walk.next(g, s);
-          int t = s.t0, seg = 0;
-          issue_s(0, 0, true, s.t1 - s.t0 == 1);
-          for (int i = 0; ok && i < n_tiles; ++i) {
-            const bool last = i + 1 == n_tiles, first = t == s.t0, turn = t + 1 == s.t1;
-            const int seg_o = seg;
-            const bool v_first = last || (turn && C::kQBufs == 1);
-            if (v_first) issue_o(i, seg_o, first, turn);
-            if (!last && ok) {
-              ++t;
-              if (turn) {
-                walk.next(g, s);
-                t = s.t0;
-                ++seg;
-              }
-              issue_s(i + 1, seg, t == s.t0, t + 1 == s.t1);
-            }
-            if (!v_first && ok) issue_o(i, seg_o, first, turn);
-          }
         }
-        mma_commit(&drain_bar);  // every MMA issued above has finished once this arrives
-        int never = 0;
-        mbar_wait(&drain_bar, 0, &never, a.err, kDevTimeoutDrain);
+        __syncwarp();
+        ++pos;
+      };
+      if (n_tiles > 0) {
+        AtSeg s;
+        walk.next(g, s);
+        int t = s.t0, seg = 0;
+        issue_s(0, 0, true, s.t1 - s.t0 == 1);
+        for (int i = 0; ok && i < n_tiles; ++i) {
+          const bool last = i + 1 == n_tiles, first = t == s.t0, turn = t + 1 == s.t1;
+          const int seg_o = seg;
+          const bool v_first = last || (turn && C::kQBufs == 1);
+          if (v_first) issue_o(i, seg_o, first, turn);
+          if (!last && ok) {
+            ++t;
+            if (turn) {
+              walk.next(g, s);
+              t = s.t0;
+              ++seg;
+            }
+            issue_s(i + 1, seg, t == s.t0, t + 1 == s.t1);
+          }
+          if (!v_first && ok) issue_o(i, seg_o, first, turn);
+        }
       }
+      if (elect_one()) mma_commit(&drain_bar);  // every MMA issued above has finished once this arrives
+      __syncwarp();
+      int never = 0;
+      mbar_wait(&drain_bar, 0, &never, a.err, kDevTimeoutDrain);
       __syncwarp();
     }
   } else {

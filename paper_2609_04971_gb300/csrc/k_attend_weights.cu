@@ -234,41 +234,51 @@ __global__ void __launch_bounds__(kThreads, 1)
     __syncwarp();
   } else if (warp == 1) {
     // ---------------------------------------------------------------- MMA issuer
-    if (lane == 0) {
-      if (n_units > 0) {
-        Unit u;
-        u.start(a, share);
-        int n_k = 0;
-        for (int i = 0; i < n_units; ++i) {
-          if (i > 0) {
-            u.next(a);
-            if (u.k == 0) {
-              mma_commit(&kempty_bar[n_k & 1]);  // the products with the tile before are issued
-              ++n_k;
-            }
-          }
-          const int st = i % C::kStages, buf = i & 1, kb = n_k & 1;
-          if ((i == 0 || u.k == 0) &&
-              !mbar_wait(&kfull_bar[kb], (n_k >> 1) & 1, abort_flag, a.err, kDevTimeoutMma))
-            break;
-          if (!mbar_wait(&full_bar[st], (i / C::kStages) & 1, abort_flag, a.err, kDevTimeoutMma) ||
-              (i >= 2 && !mbar_wait(&sfree_bar[buf], ((i >> 1) - 1) & 1, abort_flag, a.err, kDevTimeoutMma)))
-            break;
-          tc_fence_after();
-          const uint32_t idesc = idesc_bf16_f32(128, (u.cols + 15) / 16 * 16);
-          const uint32_t k_addr = smem_u32(k_smem + kb * C::kTileBytes), q_addr = smem_u32(q_smem + st * C::kTileBytes);
+    // The whole warp walks along and one lane issues, so that descriptors stay in uniform registers.
+    const uint32_t k_addr = smem_u32(k_smem), q_addr = smem_u32(q_smem);
+    const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
+    bool ok = true;
+    auto await = [&](uint64_t* bar, uint32_t parity) {
+      if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, a.err, kDevTimeoutMma));
+    };
+    if (n_units > 0) {
+      Unit u;
+      u.start(a, share);
+      int n_k = 0;
+      await(&kfull_bar[0], 0);
+      for (int i = 0; ok && i < n_units; ++i) {
+        const int st = i % C::kStages, buf = i & 1;
+        await(&full_bar[st], (i / C::kStages) & 1);
+        if (i >= 2) await(&sfree_bar[buf], ((i >> 1) - 1) & 1);
+        if (!ok) break;
+        tc_fence_after();
+        const uint32_t idesc = idesc_bf16_f32(128, (u.cols + 15) / 16 * 16);
+        const uint64_t k = sdesc_kmajor_sw128(k_addr + (n_k & 1) * C::kTileBytes);
+        const uint64_t q = sdesc_kmajor_sw128(q_addr + st * C::kTileBytes);
+        if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk)
-            mma_bf16_ss(tmem + buf * kCols, sdesc_kmajor_sw128(k_addr + (kk >> 2) * kBox + (kk & 3) * 32),
-                        sdesc_kmajor_sw128(q_addr + (kk >> 2) * kBox + (kk & 3) * 32), idesc, kk > 0);
+            mma_bf16_ss(tm + buf * kCols, k + (((kk >> 2) * kBox + (kk & 3) * 32) >> 4),
+                        q + (((kk >> 2) * kBox + (kk & 3) * 32) >> 4), idesc, kk > 0);
           mma_commit(&empty_bar[st]);
           mma_commit(&sfull_bar[buf]);
         }
+        __syncwarp();
+        if (i + 1 < n_units) {
+          u.next(a);
+          if (u.k == 0) {
+            if (elect_one()) mma_commit(&kempty_bar[n_k & 1]);  // the products with the tile before are issued
+            __syncwarp();
+            ++n_k;
+            await(&kfull_bar[n_k & 1], (n_k >> 1) & 1);
+          }
+        }
       }
-      mma_commit(&drain_bar);
-      int never = 0;
-      mbar_wait(&drain_bar, 0, &never, a.err, kDevTimeoutDrain);
     }
+    if (elect_one()) mma_commit(&drain_bar);
+    __syncwarp();
+    int never = 0;
+    mbar_wait(&drain_bar, 0, &never, a.err, kDevTimeoutDrain);
     __syncwarp();
   } else if (n_units > 0) {
     // ---------------------------------------------------------------- weights
