@@ -13,8 +13,10 @@
 // workspace (a CTA has two at most: its first and its last) and a second launch
 // adds them in order.
 //
-// Warp roles: warp 0 TMA producer, warp 1 MMA issue, sixteen warps of exponentials in
-// four groups, a quarter of the columns each.  Bound by the exponentials: 128 x 128 of
+// Warp roles: warp 0 TMA producer, warp 1 MMA issue, warp 2 describes the units (the
+// columns' normalisers and limits, what is masked, where an item ends) in a ring in
+// shared memory, warps 4..19 exponentials, in four groups with a quarter of the
+// columns each.  Bound by the exponentials: 128 x 128 of
 // them per unit at 16 per clock and SM, twice what the matrix product takes.
 #include "k_attend.cuh"
 
@@ -22,7 +24,8 @@ namespace bkv {
 namespace {
 
 constexpr int kSmWarps = 16, kGroups = kSmWarps / 4;  // groups of four warps share the columns
-constexpr int kThreads = 32 * (2 + kSmWarps);
+constexpr int kThreads = 32 * (4 + kSmWarps);
+constexpr int kDescs = 4;  // units described ahead
 constexpr uint32_t kBox = 128 * 128;
 constexpr int kCols = 128, kNC = kCols / kGroups;
 constexpr uint32_t kTmem = 2 * kCols;
@@ -117,6 +120,14 @@ struct Unit {
   }
 };
 
+// What the exponentials need to know of a unit.
+struct Desc {
+  int e, j0, len, cols;
+  int plain;  // every column is a row that sees every key of the tile
+  int ends;   // the item's last unit in this CTA: 1: all its units were here, 2: a part of them
+  int part;   // slot of the part
+};
+
 template <int D>
 struct WCfg {
   static constexpr int kBoxes = D / 64;
@@ -136,8 +147,10 @@ __global__ void __launch_bounds__(kThreads, 1)
   __shared__ int abort_sh;
   __shared__ long long scan_sh[kThreads / 32];
   __shared__ AtShare share_sh;
-  __shared__ __align__(16) float lse_sh[2][kCols];
-  __shared__ __align__(16) int lim_sh[2][kCols];
+  __shared__ __align__(16) float lse_sh[kDescs][kCols];
+  __shared__ __align__(16) int lim_sh[kDescs][kCols];
+  __shared__ Desc desc_sh[kDescs];
+  __shared__ __align__(8) uint64_t dfull_bar[kDescs], dempty_bar[kDescs];
   __shared__ float sum_sh[kGroups][kAtTile];
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -156,6 +169,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(&kempty_bar[i], 1);
       mbar_init(&sfull_bar[i], 1);
       mbar_init(&sfree_bar[i], kSmWarps);
+    }
+    for (int i = 0; i < kDescs; ++i) {
+      mbar_init(&dfull_bar[i], 1);
+      mbar_init(&dempty_bar[i], kSmWarps);
     }
     mbar_init(&drain_bar, 1);
     abort_sh = 0;
@@ -242,17 +259,19 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, a.err, kDevTimeoutMma));
     };
     if (n_units > 0) {
-      Unit u;
-      u.start(a, share);
       int n_k = 0;
       await(&kfull_bar[0], 0);
       for (int i = 0; ok && i < n_units; ++i) {
-        const int st = i % C::kStages, buf = i & 1;
+        const int st = i % C::kStages, buf = i & 1, x = i % kDescs;
+        await(&dfull_bar[x], (i / kDescs) & 1);
         await(&full_bar[st], (i / C::kStages) & 1);
+        if (!ok) break;
+        // read before S is issued: the description stays until the exponentials of this S are done
+        const int cols = __shfl_sync(0xffffffffu, desc_sh[x].cols, 0), ends = __shfl_sync(0xffffffffu, desc_sh[x].ends, 0);
         if (i >= 2) await(&sfree_bar[buf], ((i >> 1) - 1) & 1);
         if (!ok) break;
         tc_fence_after();
-        const uint32_t idesc = idesc_bf16_f32(128, (u.cols + 15) / 16 * 16);
+        const uint32_t idesc = idesc_bf16_f32(128, (cols + 15) / 16 * 16);
         const uint64_t k = sdesc_kmajor_sw128(k_addr + (n_k & 1) * C::kTileBytes);
         const uint64_t q = sdesc_kmajor_sw128(q_addr + st * C::kTileBytes);
         if (elect_one()) {
@@ -262,16 +281,12 @@ __global__ void __launch_bounds__(kThreads, 1)
                         q + (((kk >> 2) * kBox + (kk & 3) * 32) >> 4), idesc, kk > 0);
           mma_commit(&empty_bar[st]);
           mma_commit(&sfull_bar[buf]);
+          if (ends) mma_commit(&kempty_bar[n_k & 1]);
         }
         __syncwarp();
-        if (i + 1 < n_units) {
-          u.next(a);
-          if (u.k == 0) {
-            if (elect_one()) mma_commit(&kempty_bar[n_k & 1]);  // the products with the tile before are issued
-            __syncwarp();
-            ++n_k;
-            await(&kfull_bar[n_k & 1], (n_k >> 1) & 1);
-          }
+        if (ends && i + 1 < n_units) {
+          ++n_k;
+          await(&kfull_bar[n_k & 1], (n_k >> 1) & 1);
         }
       }
     }
@@ -280,49 +295,78 @@ __global__ void __launch_bounds__(kThreads, 1)
     int never = 0;
     mbar_wait(&drain_bar, 0, &never, a.err, kDevTimeoutDrain);
     __syncwarp();
-  } else if (n_units > 0) {
+  } else if (warp == 2) {
+    // ---------------------------------------------------------------- descriptions
+    if (n_units > 0) {
+      Unit u;
+      u.start(a, share);
+      bool from_start = u.k == 0;  // this CTA has the item's units from its first one on
+      int began = 0;               // unit of the CTA at which the item began
+      for (int i = 0; i < n_units; ++i) {
+        const int x = i % kDescs;
+        if (i > 0) {
+          u.next(a);
+          if (u.k == 0) {
+            from_start = true;
+            began = i;
+          }
+        }
+        if (from_start && u.k == 0 && lane == 0) a.u0[static_cast<size_t>(u.e) * a.tiles + u.t] = share.u + i;
+        float lse[kCols / 32];
+        int lim[kCols / 32];
+#pragma unroll
+        for (int y = 0; y < kCols / 32; ++y) {  // columns without a row see nothing
+          const int c = y * 32 + lane;
+          lse[y] = 0.f;
+          lim[y] = 0;
+          if (c < u.cols) {
+            lse[y] = a.lse2[static_cast<size_t>(u.e) * a.R + u.r0 + c];
+            lim[y] = u.len - a.n_q + 1 + (a.hp > 1 ? c % a.n_q : u.i0 + c);
+          }
+        }
+        if (i >= kDescs &&
+            !__all_sync(0xffffffffu,
+                        mbar_wait(&dempty_bar[x], ((i / kDescs) - 1) & 1, abort_flag, a.err, kDevTimeoutProducer)))
+          break;
+#pragma unroll
+        for (int y = 0; y < kCols / 32; ++y) {
+          // a row that sees nothing has -inf, and its columns are masked: any finite number will do
+          lse_sh[x][y * 32 + lane] = lse[y] == -INFINITY ? 0.f : lse[y];
+          lim_sh[x][y * 32 + lane] = lim[y];
+        }
+        if (lane == 0) {
+          const bool ends = i + 1 == n_units || u.k + 1 == u.n, whole = from_start && u.k + 1 == u.n;
+          desc_sh[x] = {u.e, u.t * kAtTile, u.len, u.cols,
+                        u.cols == kCols && (u.t + 1) * kAtTile <= u.len - a.n_q + 1 + u.i0, ends ? (whole ? 1 : 2) : 0,
+                        // an item that began here after the CTA's first unit leaves part 1; else part 0
+                        static_cast<int>(blockIdx.x) * 2 + (from_start && began > 0)};
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&dfull_bar[x]);
+      }
+    }
+  } else if (warp >= 4) {
     // ---------------------------------------------------------------- weights
-    const int grp = (warp - 2) >> 2, wt = (tid - 64) & 127;
+    const int grp = (warp - 4) >> 2;
     const int quarter = warp & 3, key_lane = quarter * 32 + lane;
     const uint32_t lane_addr = static_cast<uint32_t>(quarter * 32) << 16;
-    const uint32_t bar_id = 1 + grp;
     const int c0 = grp * kNC;
     const float sc = a.sc;
-    Unit u;
-    u.start(a, share);
-    // normaliser and limit of column c of a unit; columns without a row see nothing
-    auto column = [&](const Unit& v, int c, float& lse, int& lim) {
-      lse = 0.f;  // never an infinity: a row that sees nothing has one, and its columns are masked
-      lim = 0;
-      if (c < v.cols) {
-        const float x = a.lse2[static_cast<size_t>(v.e) * a.R + v.r0 + c];
-        lse = x == -INFINITY ? 0.f : x;
-        lim = v.len - a.n_q + 1 + (a.hp > 1 ? c % a.n_q : v.i0 + c);
-      }
-    };
-    if (wt < kNC) column(u, c0 + wt, lse_sh[0][c0 + wt], lim_sh[0][c0 + wt]);
-    named_barrier(bar_id, 128);
-    float acc = 0.f;
-    bool from_start = u.k == 0;  // this CTA has the item's units from its first one on
-    if (from_start && wt == 0 && grp == 0) a.u0[static_cast<size_t>(u.e) * a.tiles + u.t] = share.u;
-    for (int i = 0; i < n_units; ++i) {
-      const int buf = i & 1;
-      Unit v = u;
-      float lse_n = 0.f;
-      int lim_n = 0;
-      const bool more = i + 1 < n_units;
-      if (more) {
-        v.next(a);
-        if (wt < kNC) column(v, c0 + wt, lse_n, lim_n);
-      }
-      if (!*abort_flag) mbar_wait(&sfull_bar[buf], (i >> 1) & 1, abort_flag, a.err, kDevTimeoutEpilogue);
+    auto wait = [&](uint64_t* bar, uint32_t parity) {  // after an abort every wait returns at once
+      if (!mbar_try_wait(bar, parity) && !*abort_flag) mbar_wait(bar, parity, abort_flag, a.err, kDevTimeoutEpilogue);
       __syncwarp();
+    };
+    float acc = 0.f;
+    for (int i = 0; i < n_units; ++i) {
+      const int buf = i & 1, x = i % kDescs;
+      wait(&dfull_bar[x], (i / kDescs) & 1);
+      const Desc u = desc_sh[x];
+      wait(&sfull_bar[buf], (i >> 1) & 1);
       tc_fence_after();
-      const int j = u.t * kAtTile + key_lane;
-      const int lim_min = u.len - a.n_q + 1 + u.i0;
+      const int j = u.j0 + key_lane;
       float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
       auto add4 = [&](const float* y, int c) {
-        const float4 l = *reinterpret_cast<const float4*>(&lse_sh[buf][c0 + c]);
+        const float4 l = *reinterpret_cast<const float4*>(&lse_sh[x][c0 + c]);
         s0 += ex2_approx(fmaf(y[0], sc, -l.x));
         s1 += ex2_approx(fmaf(y[1], sc, -l.y));
         s2 += ex2_approx(fmaf(y[2], sc, -l.z));
@@ -335,10 +379,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive(&sfree_bar[buf]);
       };
-      if (u.cols == kCols && (u.t + 1) * kAtTile <= lim_min) {
+      if (u.plain) {
         float y[kNC];
-#pragma unroll
-        for (int c = 0; c < kNC; c += 32) tmem_ld32(at + c, *reinterpret_cast<float(*)[32]>(y + c));
+        tmem_ld32(at, y);
         release();
 #pragma unroll
         for (int c = 0; c < kNC; c += 4) add4(y + c, c);
@@ -350,44 +393,31 @@ __global__ void __launch_bounds__(kThreads, 1)
           tmem_ld8(at + c, y);
           tmem_wait_ld();
 #pragma unroll
-          for (int x = 0; x < 8; x += 4) {
-            const int4 m = *reinterpret_cast<const int4*>(&lim_sh[buf][c0 + c + x]);
-            y[x] = j < m.x ? y[x] : -INFINITY;
-            y[x + 1] = j < m.y ? y[x + 1] : -INFINITY;
-            y[x + 2] = j < m.z ? y[x + 2] : -INFINITY;
-            y[x + 3] = j < m.w ? y[x + 3] : -INFINITY;
-            add4(y + x, c + x);
+          for (int z = 0; z < 8; z += 4) {
+            const int4 m = *reinterpret_cast<const int4*>(&lim_sh[x][c0 + c + z]);
+            y[z] = j < m.x ? y[z] : -INFINITY;
+            y[z + 1] = j < m.y ? y[z + 1] : -INFINITY;
+            y[z + 2] = j < m.z ? y[z + 2] : -INFINITY;
+            y[z + 3] = j < m.w ? y[z + 3] : -INFINITY;
+            add4(y + z, c + z);
           }
         }
         release();
       }
       acc += (s0 + s1) + (s2 + s3);
-      if (!more || v.k == 0) {  // the item's last unit here
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&dempty_bar[x]);
+      if (u.ends) {
         sum_sh[grp][key_lane] = acc;
-        named_barrier(1 + kGroups, 32 * kSmWarps);
+        named_barrier(1, 32 * kSmWarps);
         if (grp == 0) {
           float sum = acc;
-          for (int x = 1; x < kGroups; ++x) sum += sum_sh[x][key_lane];
-          if (from_start && u.k + 1 == u.n) {
-            if (j < u.len) a.weights[static_cast<size_t>(u.e) * a.cap + j] += sum;
-          } else {
-            // the item began in this CTA after its first unit: part 1; else it is the CTA's first item
-            const bool second = from_start && i != u.k;
-            a.parts[(static_cast<size_t>(blockIdx.x) * 2 + second) * kAtTile + key_lane] = sum;
-          }
+          for (int y = 1; y < kGroups; ++y) sum += sum_sh[y][key_lane];
+          if (u.ends == 2) a.parts[static_cast<size_t>(u.part) * kAtTile + key_lane] = sum;
+          else if (j < u.len) a.weights[static_cast<size_t>(u.e) * a.cap + j] += sum;
         }
-        named_barrier(1 + kGroups, 32 * kSmWarps);
+        named_barrier(1, 32 * kSmWarps);
         acc = 0.f;
-        from_start = true;
-        if (more && wt == 0 && grp == 0) a.u0[static_cast<size_t>(v.e) * a.tiles + v.t] = share.u + i + 1;
-      }
-      if (more) {
-        if (wt < kNC) {
-          lse_sh[buf ^ 1][c0 + wt] = lse_n;
-          lim_sh[buf ^ 1][c0 + wt] = lim_n;
-        }
-        named_barrier(bar_id, 128);
-        u = v;
       }
     }
   }
