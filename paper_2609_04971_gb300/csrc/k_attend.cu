@@ -76,7 +76,9 @@ size_t place_parts(AtPlan& p, int d, int sms, size_t at) {
   p.off_u0 = at;
   at = align_up(at + static_cast<size_t>(p.items) * sizeof(long long));
   p.off_per = at;
-  return align_up(at + sizeof(long long));
+  at = align_up(at + sizeof(long long));
+  p.off_cut = at;
+  return align_up(at + static_cast<size_t>(sms) * sizeof(long long));
 }
 
 struct MergeArgs {
@@ -172,22 +174,23 @@ __device__ __forceinline__ float merged_lse2(const MergeArgs& a, const RowParts&
 }
 
 template <int D>
-__global__ void __launch_bounds__(kMergeThreads, 5) merge_kernel(MergeArgs a) {
+__global__ void __launch_bounds__(kMergeThreads, 4) merge_kernel(MergeArgs a) {
   constexpr int kPer = D / 32;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   grid_dependents_go();
   grid_dependency_wait();
   if (static_cast<int>(blockIdx.x) < a.row_blocks) {
-    // kMergeRows rows of one item of the own caches to a block
+    // kMergeRows rows of an item of the own caches to a block: of every item where there is a prefix, else
+    // of those that a CTA began and did not finish
     const AtGeo& g = a.own;
     const int per_item = (g.rr + kMergeRows - 1) / kMergeRows;
-    const int item = blockIdx.x / per_item;
-    const int e = item / g.nrb, r0 = item % g.nrb * g.rr, c1 = min(g.rr, g.R - r0);
+    const long long x = blockIdx.x / per_item, item = a.has_prefix ? x : a.own_parts.cut[x];
+    if (item < 0) return;
+    const int e = static_cast<int>(item / g.nrb), r0 = static_cast<int>(item % g.nrb) * g.rr, c1 = min(g.rr, g.R - r0);
     for (int c = blockIdx.x % per_item * kMergeRows + warp, n = 0; c < c1 && n < kMergeRows / 8; c += 8, ++n) {
       const int r = r0 + c;
       const long long row = static_cast<long long>(e) * g.R + r;
       const RowParts p = row_parts(a, e, r);
-      if (!p.split) return;  // the same for the whole item
       const WarpParts wp(p);
       const float lse2 = merged_lse2(a, p, wp, lane);
       float o[kPer] = {};
@@ -361,7 +364,8 @@ cudaError_t launch_attend_merge(const Shape& s, const AttendArgs& a, cudaStream_
     m.pre.len = a.plen;
     m.pre_parts = l.prefix.parts(a.ws);
   }
-  m.row_blocks = static_cast<int>(l.own.items * ((l.own.geo.rr + kMergeRows - 1) / kMergeRows));
+  m.row_blocks = static_cast<int>((l.has_prefix ? l.own.items : l.own.grid) *
+                                  ((l.own.geo.rr + kMergeRows - 1) / kMergeRows));
   m.sc = a.sc;
   m.o = a.o;
   m.lse = a.lse;

@@ -208,8 +208,12 @@ struct AtParts {
   float2* ml = nullptr;         // [segment][N rows] (reference, sum of p), base 2
   long long* u0 = nullptr;      // [item] number of its first tile in the run of all tiles
   long long* per = nullptr;     // [1] tiles per CTA
+  long long* cut = nullptr;     // [CTA] the item that the CTA began and left to others to finish, or -1
   int rows = 0;                 // rows per segment in o and ml
 };
+
+// What a CTA leaves in `cut` after its last segment.
+__device__ __forceinline__ long long at_cut(const AtSeg& s) { return s.t0 == 0 && s.t1 < s.T ? s.item : -1; }
 
 // Parts of an item: CTAs first .. last worked on it.
 struct AtSpan {
@@ -225,13 +229,14 @@ struct AtPlan {
   AtGeo geo;
   int grid;
   long long items;
-  size_t off_o, off_ml, off_u0, off_per;  // byte offsets in the workspace
+  size_t off_o, off_ml, off_u0, off_per, off_cut;  // byte offsets in the workspace
   AtParts parts(unsigned char* ws) const {
     AtParts p;
     p.o = reinterpret_cast<float*>(ws + off_o);
     p.ml = reinterpret_cast<float2*>(ws + off_ml);
     p.u0 = reinterpret_cast<long long*>(ws + off_u0);
     p.per = reinterpret_cast<long long*>(ws + off_per);
+    p.cut = reinterpret_cast<long long*>(ws + off_cut);
     p.rows = geo.mb * geo.rr;
     return p;
   }

@@ -14,7 +14,7 @@
 // exponentials the tensor cores work for the other.
 //
 // The reference of a row is the logit of the segment's first key; only when a
-// logit of a tile exceeds it by more than 2^32 the warp moves its references to
+// logit of a tile exceeds it by more than 2^32, or their sum does, the warp moves its references to
 // the tile's maxima and scales its sums and its lanes of O (fp32 sums and bf16 P
 // have the exponent range for that).  S_w stays in tensor memory until the tile's P is
 // known to stand, so the exponentials need not wait for a maximum.
@@ -27,8 +27,9 @@ namespace bkv {
 namespace {
 
 constexpr int kThreads = 384;  // producer, MMA, two idle warps; two groups of four
-constexpr int kRegsFew = 80, kRegsMany = 208;  // 80 + 2 x 208 of the 3 x 168 per scheduler at launch
+constexpr int kRegsFew = 72, kRegsMany = 216;  // 72 + 2 x 216 of the 3 x 168 per scheduler at launch
 constexpr int kRows = 128;     // rows of a row tile
+constexpr float kSumAbove = 4294967296.f;  // 2^kMaxAbove
 
 template <int D>
 struct RowsCfg {
@@ -101,6 +102,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   at_split_tiles<kThreads>(g, scan_sh, &share_sh);
   tc_fence_after();
   if (blockIdx.x == 0 && tid == 0) *a.parts.per = share_sh.per;
+  if (tid == 0 && share_sh.left == 0) a.parts.cut[blockIdx.x] = -1;
   const uint32_t tmem = tmem_base_sh;
   AtWalk walk{share_sh.at.e, share_sh.at.k, share_sh.at.t, share_sh.left, share_sh.u};
   const int n_tiles = static_cast<int>(share_sh.left);  // key tiles of this CTA
@@ -272,7 +274,10 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int lim = row < 0 ? 0 : g.causal ? max(0, s.len - g.n_q + 1 + (s.r0 + c % g.rr) % g.n_q) : s.len;
       const int lim_min = __reduce_min_sync(0xffffffffu, row < 0 ? 0x7fffffff : lim);  // of the warp's rows
       const int limit_max = at_limit_max(g, s.len, s.r0);
-      if (tid == 128 && s.t0 == 0) a.parts.u0[s.item] = s.u;
+      if (tid == 128) {
+        if (s.t0 == 0) a.parts.u0[s.item] = s.u;
+        if (!more) a.parts.cut[blockIdx.x] = at_cut(s);
+      }
       float ref = 0.f, l = 0.f;  // ref: minus the reference
       for (int t = s.t0; t < s.t1; ++t, ++i) {
         const int k0 = t * kAtTile, seen = lim - k0;  // keys of the tile that the row sees
@@ -280,11 +285,24 @@ __global__ void __launch_bounds__(kThreads, 1)
         wait(&sfull_bar[w], i & 1);
         tc_fence_after();
         uint32_t p[kAtTile / 2];
-        float top = -INFINITY, sum = 0.f;
-        // the tile's weights against the present reference; the largest exponent in `top`
+        float sum = 0.f;
+        // a quarter of the tile's logits, as exponents against the reference
+        auto shift = [&](float(&v)[32], int q) {
+          const float2 sc2 = make_float2(sc, sc), ref2 = make_float2(ref, ref);
+#pragma unroll
+          for (int x = 0; x < 32; x += 2) {
+            const float2 y = fma2(make_float2(v[x], v[x + 1]), sc2, ref2);
+            v[x] = y.x;
+            v[x + 1] = y.y;
+          }
+          if (masked) {
+#pragma unroll
+            for (int x = 0; x < 32; ++x) v[x] = q * 32 + x < seen ? v[x] : -INFINITY;
+          }
+        };
+        // the tile's weights against the present reference, and their sum
         auto weigh = [&](bool first) {
-          sum = 0.f;
-          top = -INFINITY;
+          float2 s0 = make_float2(0.f, 0.f), s1 = s0;
           float y[2][32];
           tmem_ld32(s_addr, y[0]);
 #pragma unroll
@@ -293,34 +311,36 @@ __global__ void __launch_bounds__(kThreads, 1)
             tmem_wait_ld();
             if (q < 3) tmem_ld32(s_addr + (q + 1) * 32, y[(q + 1) & 1]);
             if (q == 0 && first) ref = seen > 0 ? -fmaxf(v[0] * sc, kRefFloor) : 0.f;
+            shift(v, q);
 #pragma unroll
-            for (int x = 0; x < 32; ++x) v[x] = fmaf(v[x], sc, ref);
-            if (masked) {
-#pragma unroll
-              for (int x = 0; x < 32; ++x) v[x] = q * 32 + x < seen ? v[x] : -INFINITY;
+            for (int x = 0; x < 32; x += 4) {
+              const float2 e0 = make_float2(ex2_approx(v[x]), ex2_approx(v[x + 1]));
+              const float2 e1 = make_float2(ex2_approx(v[x + 2]), ex2_approx(v[x + 3]));
+              s0 = add2(s0, e0);
+              s1 = add2(s1, e1);
+              p[q * 16 + x / 2] = pack_bf16(e0.x, e0.y);
+              p[q * 16 + x / 2 + 1] = pack_bf16(e1.x, e1.y);
             }
-            float m0 = v[0], m1 = v[1], s0 = 0.f, s1 = 0.f;
-#pragma unroll
-            for (int x = 2; x < 32; x += 2) {
-              m0 = fmaxf(m0, v[x]);
-              m1 = fmaxf(m1, v[x + 1]);
-            }
-            top = fmaxf(top, fmaxf(m0, m1));
-#pragma unroll
-            for (int x = 0; x < 32; x += 2) {
-              const float e0 = ex2_approx(v[x]), e1 = ex2_approx(v[x + 1]);
-              s0 += e0;
-              s1 += e1;
-              p[q * 16 + x / 2] = pack_bf16(e0, e1);
-            }
-            sum += s0 + s1;
           }
+          s0 = add2(s0, s1);
+          sum = s0.x + s0.y;
         };
         weigh(t == s.t0);
-        if (__any_sync(0xffffffffu, top > kMaxAbove)) {
+        // a weight above 2^32 shows in the sum, so no maximum is kept
+        if (__any_sync(0xffffffffu, sum > kSumAbove)) {
           // Move the references up to the tile's maxima.  The products of the tiles before are complete:
           // the barrier of this tile's S was waited for, and they were issued before it.
-          const float up = fmaxf(top, 0.f), f = ex2_approx(-up);
+          float up = 0.f;
+#pragma unroll 1
+          for (int q = 0; q < 4; ++q) {
+            float v[32];
+            tmem_ld32(s_addr + q * 32, v);
+            tmem_wait_ld();
+            shift(v, 0);
+#pragma unroll
+            for (int x = 0; x < 32; ++x) up = fmaxf(up, q * 32 + x < seen ? v[x] : 0.f);
+          }
+          const float f = ex2_approx(-up);
           ref -= up;
           l *= f;
           if (t > s.t0) {

@@ -36,9 +36,9 @@ namespace {
 
 constexpr int kSmWarps = 8;
 constexpr int kAtThreads = 32 * (4 + kSmWarps);
-// Registers: 168 a thread at launch; the first four warps give back what the softmax warps take, 80 + 2 x 208
+// Registers: 168 a thread at launch; the first four warps give back what the softmax warps take, 72 + 2 x 216
 // of 3 x 168 per scheduler.
-constexpr int kRegsFew = 80, kRegsMany = 208;
+constexpr int kRegsFew = 72, kRegsMany = 216;
 constexpr int kAtMaxStages = 12;
 constexpr size_t kAtSmem = 218 * 1024;       // dynamic shared memory, next to up to 8 KB of static
 
@@ -188,6 +188,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
   at_split_tiles<kAtThreads>(g, scan_sh, &share_sh);
   tc_fence_after();
   if (blockIdx.x == 0 && tid == 0) *a.parts.per = share_sh.per;
+  if (tid == 0 && share_sh.left == 0) a.parts.cut[blockIdx.x] = -1;
   const uint32_t tmem = tmem_base_sh;
   AtWalk walk{share_sh.at.e, share_sh.at.k, share_sh.at.t, share_sh.left, share_sh.u};
   const int n_tiles = static_cast<int>(share_sh.left);  // tiles of this CTA (below 2^31)
@@ -415,7 +416,10 @@ __global__ void __launch_bounds__(kAtThreads, 1)
         rows[wt] = c < cols ? at_row(g, s.e, {s.b0, s.r0}, c) : -1;
         lim[wt] = g.causal ? max(0, s.len - g.n_q + 1 + (s.r0 + c % g.rr) % g.n_q) : s.len;
       }
-      if (wt == 0 && grp == 0 && s.t0 == 0) a.parts.u0[s.item] = s.u;
+      if (wt == 0 && grp == 0) {
+        if (s.t0 == 0) a.parts.u0[s.item] = s.u;
+        if (!more) a.parts.cut[blockIdx.x] = at_cut(s);
+      }
       named_barrier(bar_id, 128);
       float l[NC];
 #pragma unroll
@@ -436,10 +440,13 @@ __global__ void __launch_bounds__(kAtThreads, 1)
 #pragma unroll
             for (int c = 0; c < NC; c += 4) {
               const float4 r = *reinterpret_cast<const float4*>(ref + c);
-              y[c] = fmaf(y[c], sc, r.x);
-              y[c + 1] = fmaf(y[c + 1], sc, r.y);
-              y[c + 2] = fmaf(y[c + 2], sc, r.z);
-              y[c + 3] = fmaf(y[c + 3], sc, r.w);
+              const float2 sc2 = make_float2(sc, sc);
+              const float2 a0 = fma2(make_float2(y[c], y[c + 1]), sc2, make_float2(r.x, r.y));
+              const float2 a1 = fma2(make_float2(y[c + 2], y[c + 3]), sc2, make_float2(r.z, r.w));
+              y[c] = a0.x;
+              y[c + 1] = a0.y;
+              y[c + 2] = a1.x;
+              y[c + 3] = a1.y;
             }
             if (k0 + kAtTile > limit_min) {  // some row does not see all keys of the tile
 #pragma unroll
@@ -544,7 +551,11 @@ __global__ void __launch_bounds__(kAtThreads, 1)
           for (int u = 0; u < U; ++u) {
             const float* p = y + u * 8;
 #pragma unroll
-            for (int c = 0; c < 8; ++c) l[u * 8 + c] += p[c];
+            for (int c = 0; c < 8; c += 2) {
+              const float2 v = add2(make_float2(l[u * 8 + c], l[u * 8 + c + 1]), make_float2(p[c], p[c + 1]));
+              l[u * 8 + c] = v.x;
+              l[u * 8 + c + 1] = v.y;
+            }
             packed[u] = make_uint4(pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]),
                                    pack_bf16(p[6], p[7]));
           }

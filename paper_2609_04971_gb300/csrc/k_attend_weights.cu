@@ -302,37 +302,34 @@ __global__ void __launch_bounds__(kThreads, 1)
       u.start(a, share);
       bool from_start = u.k == 0;  // this CTA has the item's units from its first one on
       int began = 0;               // unit of the CTA at which the item began
+      float lse[kCols / 32], lse_next[kCols / 32];
+      auto fetch = [&](const Unit& v, float(&out)[kCols / 32]) {
+#pragma unroll
+        for (int y = 0; y < kCols / 32; ++y) {
+          const int c = y * 32 + lane;
+          out[y] = c < v.cols ? a.lse2[static_cast<size_t>(v.e) * a.R + v.r0 + c] : 0.f;
+        }
+      };
+      fetch(u, lse);
       for (int i = 0; i < n_units; ++i) {
         const int x = i % kDescs;
-        if (i > 0) {
-          u.next(a);
-          if (u.k == 0) {
-            from_start = true;
-            began = i;
-          }
+        Unit v = u;
+        if (i + 1 < n_units) {  // the next unit's normalisers are under way while this one is described
+          v.next(a);
+          fetch(v, lse_next);
         }
         if (from_start && u.k == 0 && lane == 0) a.u0[static_cast<size_t>(u.e) * a.tiles + u.t] = share.u + i;
-        float lse[kCols / 32];
-        int lim[kCols / 32];
-#pragma unroll
-        for (int y = 0; y < kCols / 32; ++y) {  // columns without a row see nothing
-          const int c = y * 32 + lane;
-          lse[y] = 0.f;
-          lim[y] = 0;
-          if (c < u.cols) {
-            lse[y] = a.lse2[static_cast<size_t>(u.e) * a.R + u.r0 + c];
-            lim[y] = u.len - a.n_q + 1 + (a.hp > 1 ? c % a.n_q : u.i0 + c);
-          }
-        }
         if (i >= kDescs &&
             !__all_sync(0xffffffffu,
                         mbar_wait(&dempty_bar[x], ((i / kDescs) - 1) & 1, abort_flag, a.err, kDevTimeoutProducer)))
           break;
 #pragma unroll
         for (int y = 0; y < kCols / 32; ++y) {
+          const int c = y * 32 + lane;
           // a row that sees nothing has -inf, and its columns are masked: any finite number will do
-          lse_sh[x][y * 32 + lane] = lse[y] == -INFINITY ? 0.f : lse[y];
-          lim_sh[x][y * 32 + lane] = lim[y];
+          lse_sh[x][c] = lse[y] == -INFINITY ? 0.f : -lse[y];
+          // columns without a row see nothing
+          lim_sh[x][c] = c < u.cols ? u.len - a.n_q + 1 + (a.hp > 1 ? c % a.n_q : u.i0 + c) : 0;
         }
         if (lane == 0) {
           const bool ends = i + 1 == n_units || u.k + 1 == u.n, whole = from_start && u.k + 1 == u.n;
@@ -343,6 +340,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(&dfull_bar[x]);
+        if (v.k == 0) {
+          from_start = true;
+          began = i + 1;
+        }
+        u = v;
+#pragma unroll
+        for (int y = 0; y < kCols / 32; ++y) lse[y] = lse_next[y];
       }
     }
   } else if (warp >= 4) {
@@ -364,13 +368,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       wait(&sfull_bar[buf], (i >> 1) & 1);
       tc_fence_after();
       const int j = u.j0 + key_lane;
-      float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f;
+      float2 s0 = make_float2(0.f, 0.f), s1 = s0;
       auto add4 = [&](const float* y, int c) {
-        const float4 l = *reinterpret_cast<const float4*>(&lse_sh[x][c0 + c]);
-        s0 += ex2_approx(fmaf(y[0], sc, -l.x));
-        s1 += ex2_approx(fmaf(y[1], sc, -l.y));
-        s2 += ex2_approx(fmaf(y[2], sc, -l.z));
-        s3 += ex2_approx(fmaf(y[3], sc, -l.w));
+        const float4 l = *reinterpret_cast<const float4*>(&lse_sh[x][c0 + c]);  // minus the normalisers
+        const float2 sc2 = make_float2(sc, sc);
+        const float2 a0 = fma2(make_float2(y[0], y[1]), sc2, make_float2(l.x, l.y));
+        const float2 a1 = fma2(make_float2(y[2], y[3]), sc2, make_float2(l.z, l.w));
+        s0 = add2(s0, make_float2(ex2_approx(a0.x), ex2_approx(a0.y)));
+        s1 = add2(s1, make_float2(ex2_approx(a1.x), ex2_approx(a1.y)));
       };
       const uint32_t at = tmem + buf * kCols + c0 + lane_addr;
       auto release = [&] {
@@ -404,7 +409,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         release();
       }
-      acc += (s0 + s1) + (s2 + s3);
+      s0 = add2(s0, s1);
+      acc += s0.x + s0.y;
       __syncwarp();
       if (lane == 0) mbar_arrive(&dempty_bar[x]);
       if (u.ends) {
