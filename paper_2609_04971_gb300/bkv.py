@@ -124,7 +124,7 @@ def _ptr(t: torch.Tensor | None, dtype: torch.dtype, name: str, device=None):
         raise TypeError(f"{name} must be a CUDA tensor")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    return ctypes.c_void_p(t.data_ptr())
+    return t.data_ptr()
 
 
 def _ptr_any(t: torch.Tensor | None, dtype: torch.dtype, name: str):
@@ -551,24 +551,26 @@ class BeaconKV:
             raise ValueError("K_out, V_out and weights_out come together or not at all")
         if K_out is None:
             K_out, V_out, weights_out = K, V, weights
-        rows = self.n_inst * c.capacity
-        self._expect(K, rows * c.head_dim, "K")
-        self._expect(V, rows * c.head_dim, "V")
-        self._expect(weights, rows, "weights")
-        self._expect(L, self.n_inst, "L")
-        cap_out = weights_out.numel() // self.n_inst
-        self._expect(weights_out, self.n_inst * cap_out, "weights_out")
-        self._expect(K_out, self.n_inst * cap_out * c.head_dim, "K_out")
-        self._expect(V_out, self.n_inst * cap_out * c.head_dim, "V_out")
-        self._expect(kept_out, self.n_inst * budget, "kept_out")
-        self._expect(len_out, self.n_inst, "len_out")
+        n_inst, d = self.n_inst, c.head_dim
+        rows = n_inst * c.capacity
+        cap_out = weights_out.numel() // n_inst
+        rows_out = n_inst * cap_out
+        for t, n, name in ((K, rows * d, "K"), (V, rows * d, "V"), (weights, rows, "weights"), (L, n_inst, "L"),
+                           (weights_out, rows_out, "weights_out"), (K_out, rows_out * d, "K_out"),
+                           (V_out, rows_out * d, "V_out"), (kept_out, n_inst * budget, "kept_out"),
+                           (len_out, n_inst, "len_out")):
+            if t is not None and t.numel() != n:
+                self._expect(t, n, name)
         if not K.is_cuda:
             raise TypeError("K must be a CUDA tensor")
-        inst = (c.n_layers, c.batch, c.n_kv_heads)
-        if kept_out is None:
-            kept_out, = self._new(K.device, ((*inst, max(0, budget)), torch.int32))
-        if len_out is None:
-            len_out, = self._new(K.device, (inst, torch.int32))
+        if kept_out is None or len_out is None:
+            inst = (c.n_layers, c.batch, c.n_kv_heads)
+            new = self._new(K.device, *([((*inst, max(0, budget)), torch.int32)] if kept_out is None else []),
+                            *([(inst, torch.int32)] if len_out is None else []))
+            if kept_out is None:
+                kept_out = new.pop(0)
+            if len_out is None:
+                len_out = new.pop(0)
         bkv_evict(self.ctx, K, V, weights, L, budget, K_out, V_out, weights_out, cap_out, kept_out, len_out)
         return kept_out, len_out
 

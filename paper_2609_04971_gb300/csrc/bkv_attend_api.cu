@@ -199,6 +199,7 @@ int bkv_evict(bkv_ctx* ctx, const void* K, const void* V, const float* weights, 
   a.weights_out = weights_out;
   a.kept = kept_idx_out;
   a.len_out = len_out;
+  a.plan = reinterpret_cast<int2*>(ctx->valid);  // scratch of a compress, 16 bytes per instance
   a.err = ctx->err;
   ProfScope ps(ctx, BKV_K_EVICT);
   const cudaError_t e = bkv::launch_evict(s, a, ctx->stream);

@@ -204,6 +204,7 @@ struct EvictArgs {
   float* weights_out = nullptr;
   int* kept = nullptr;
   int* len_out = nullptr;
+  int2* plan = nullptr;  // [n_inst] scratch
   int* err = nullptr;
 };
 cudaError_t launch_evict(const Shape& s, const EvictArgs& a, cudaStream_t st);

@@ -15,8 +15,7 @@ namespace bkv {
 namespace {
 
 constexpr int kMergeThreads = 256;
-constexpr int kMergeRows = 32;      // rows per block: four per warp
-constexpr int kMergeKeys = 512;    // keys per block of the weights' part
+constexpr int kMergeKeys = 1536;   // keys per block of the weights' part
 constexpr int kLogitRows = 16;      // rows per instance up to which logits are kept for the weights
 
 size_t align_up(size_t n) { return (n + 255) / 256 * 256; }
@@ -73,10 +72,8 @@ size_t place_parts(AtPlan& p, int d, int sms, size_t at) {
   at = align_up(at + parts * rows * d * sizeof(float));
   p.off_ml = at;
   at = align_up(at + parts * rows * sizeof(float2));
-  p.off_u0 = at;
-  at = align_up(at + static_cast<size_t>(p.items) * sizeof(long long));
-  p.off_per = at;
-  at = align_up(at + sizeof(long long));
+  p.off_span = at;
+  at = align_up(at + static_cast<size_t>(p.items) * sizeof(int2));
   p.off_cut = at;
   return align_up(at + static_cast<size_t>(sms) * sizeof(long long));
 }
@@ -95,33 +92,28 @@ struct MergeArgs {
   int key_blocks;  // blocks of kMergeKeys keys per instance
 };
 
-// The parts of one row: own instance e, row r of R.
-struct RowParts {
-  AtSpan own, pre;
-  long long own_item, pre_item;
-  int own_c, pre_c;
-  bool split;  // more than one part
+// The run of a row's parts in one source: n of them, `step` segments' rows apart in ml and o.
+struct Run {
+  const float2* ml;
+  const float* o;
+  int n, rows;
 };
 
-__device__ __forceinline__ RowParts row_parts(const MergeArgs& a, int e, int r) {
-  RowParts p;
-  const AtGeo& g = a.own;
-  const int rb = r / g.rr;
-  p.own_item = static_cast<long long>(e) * g.nrb + rb;
-  p.own_c = r % g.rr;
-  p.own = at_span(a.own_parts, p.own_item, at_tiles(at_limit_max(g, at_len(g, e), rb * g.rr)));
-  p.pre = {0, -1};
-  p.pre_item = 0;
-  p.pre_c = 0;
-  if (a.has_prefix) {
-    const AtGeo& q = a.pre;
-    const int b = e / g.n_kv, bb = b % q.m, pe = b / q.m * g.n_kv + e % g.n_kv;
-    p.pre_item = static_cast<long long>(pe) * q.nrb + bb / q.mb * q.nr + r / q.rr;
-    p.pre_c = bb % q.mb * q.rr + r % q.rr;
-    p.pre = at_span(a.pre_parts, p.pre_item, at_tiles(at_len(q, pe)));
-  }
-  p.split = a.has_prefix || p.own.first != p.own.last;
-  return p;
+__device__ __forceinline__ Run make_run(const AtParts& p, int2 span, long long item, int c, int d) {
+  const long long at = (span.x + item) * p.rows + c;
+  return {p.ml + at, p.o + at * d, span.y - span.x + 1, p.rows};
+}
+
+// Row r of own instance e in the own caches, and in the prefix.
+__device__ __forceinline__ Run own_run(const MergeArgs& a, int e, int r, int d) {
+  const long long item = static_cast<long long>(e) * a.own.nrb + r / a.own.rr;
+  return make_run(a.own_parts, a.own_parts.span[item], item, r % a.own.rr, d);
+}
+__device__ __forceinline__ Run prefix_run(const MergeArgs& a, int e, int r, int d) {
+  const AtGeo& q = a.pre;
+  const int b = e / q.n_kv, bb = b % q.m, pe = b / q.m * q.n_kv + e % q.n_kv;
+  const long long item = static_cast<long long>(pe) * q.nrb + bb / q.mb * q.nr + r / q.rr;
+  return make_run(a.pre_parts, a.pre_parts.span[item], item, bb % q.mb * q.rr + r % q.rr, d);
 }
 
 __device__ __forceinline__ float warp_max(float v) {
@@ -135,99 +127,108 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-// The parts of a row, a warp at a time: lane x holds part base + x.
-struct WarpParts {
-  int n_pre, n;
-  __device__ __forceinline__ explicit WarpParts(const RowParts& p)
-      : n_pre(p.pre.last - p.pre.first + 1), n(n_pre + p.own.last - p.own.first + 1) {}
-  // Index of part i in ml, and whether it is the prefix's.
-  __device__ __forceinline__ long long at(const MergeArgs& a, const RowParts& p, int i, bool& pre) const {
-    pre = i < n_pre;
-    return pre ? (p.pre.first + i + p.pre_item) * a.pre_parts.rows + p.pre_c
-               : (p.own.first + i - n_pre + p.own_item) * a.own_parts.rows + p.own_c;
-  }
-  __device__ __forceinline__ float2 ml(const MergeArgs& a, const RowParts& p, int i) const {
-    if (i >= n) return make_float2(0.f, 0.f);
-    bool pre;
-    const long long x = at(a, p, i, pre);
-    return pre ? a.pre_parts.ml[x] : a.own_parts.ml[x];
-  }
-};
+__device__ __forceinline__ float2 part_ml(const Run& u, int i) {
+  return i < u.n ? __ldcg(u.ml + static_cast<size_t>(i) * u.rows) : make_float2(0.f, 0.f);
+}
 
-// log2 of the sum of the parts' l 2^m; -inf when no part saw a key.  The whole warp.
-__device__ __forceinline__ float merged_lse2(const MergeArgs& a, const RowParts& p, const WarpParts& wp, int lane) {
-  const float2 mine = wp.ml(a, p, lane);
-  float top = mine.y != 0.f ? mine.x : -INFINITY;
-  for (int i = 32 + lane; i - lane < wp.n; i += 32) {
-    const float2 v = wp.ml(a, p, i);
-    if (v.y != 0.f) top = fmaxf(top, v.x);
-  }
+// Parts of a row that a lane holds: part `lane` of its run in each source; l = 0 stands for none.
+struct Held {
+  float2 own, pre;
+};
+__device__ __forceinline__ float held_top(float2 v) { return v.y != 0.f ? v.x : -INFINITY; }
+__device__ __forceinline__ float held_sum(float2 v, float top) { return v.y != 0.f ? v.y * exp2f(v.x - top) : 0.f; }
+
+// log2 of the sum of the parts' l 2^m; -inf when no part saw a key.  The whole warp, a part to a lane;
+// `h` holds the first 32 parts of each run, and `pre` has no parts where there is no prefix.
+__device__ __forceinline__ float merged_lse2(const Held& h, const Run& own, const Run& pre, int lane) {
+  const int n = max(own.n, pre.n);
+  float top = fmaxf(held_top(h.own), held_top(h.pre));
+  for (int i = 32 + lane; i - lane < n; i += 32) top = fmaxf(top, fmaxf(held_top(part_ml(own, i)), held_top(part_ml(pre, i))));
   top = warp_max(top);
   if (top == -INFINITY) top = 0.f;
-  float sum = mine.y != 0.f ? mine.y * exp2f(mine.x - top) : 0.f;
-  for (int i = 32 + lane; i - lane < wp.n; i += 32) {
-    const float2 v = wp.ml(a, p, i);
-    if (v.y != 0.f) sum += v.y * exp2f(v.x - top);
-  }
+  float sum = held_sum(h.own, top) + held_sum(h.pre, top);
+  for (int i = 32 + lane; i - lane < n; i += 32) sum += held_sum(part_ml(own, i), top) + held_sum(part_ml(pre, i), top);
   sum = warp_sum(sum);
   return sum == 0.f ? -INFINITY : top + log2f(sum);
 }
 
-template <int D>
+// RPW rows to a warp, U parts of each under way at a time.
+template <int D, int RPW, int U>
 __global__ void __launch_bounds__(kMergeThreads, 4) merge_kernel(MergeArgs a) {
-  constexpr int kPer = D / 32;
+  constexpr int kPer = D / 32, kRowsPerWarp = RPW, kMergeRows = kMergeThreads / 32 * RPW;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const AtGeo& g = a.own;
   grid_dependents_go();
   grid_dependency_wait();
   if (static_cast<int>(blockIdx.x) < a.row_blocks) {
-    // kMergeRows rows of an item of the own caches to a block: of every item where there is a prefix, else
-    // of those that a CTA began and did not finish
-    const AtGeo& g = a.own;
+    // kMergeRows rows of an item of the own caches to a block, kRowsPerWarp to a warp: of every item where
+    // there is a prefix, else of those that a CTA began and did not finish
     const int per_item = (g.rr + kMergeRows - 1) / kMergeRows;
-    const long long x = blockIdx.x / per_item, item = a.has_prefix ? x : a.own_parts.cut[x];
+    const int x = blockIdx.x / per_item, c0 = blockIdx.x % per_item * kMergeRows + warp;
+    const long long item = a.has_prefix ? x : a.own_parts.cut[x];
     if (item < 0) return;
-    const int e = static_cast<int>(item / g.nrb), r0 = static_cast<int>(item % g.nrb) * g.rr, c1 = min(g.rr, g.R - r0);
-    for (int c = blockIdx.x % per_item * kMergeRows + warp, n = 0; c < c1 && n < kMergeRows / 8; c += 8, ++n) {
-      const int r = r0 + c;
-      const long long row = static_cast<long long>(e) * g.R + r;
-      const RowParts p = row_parts(a, e, r);
-      const WarpParts wp(p);
-      const float lse2 = merged_lse2(a, p, wp, lane);
-      float o[kPer] = {};
-      // parts in runs of consecutive places, four loads of O under way at a time
-      auto run = [&](const AtParts& parts, long long item, int c, int first, int n) {
-        const float2* ml = parts.ml + (first + item) * parts.rows + c;
-        const float* src = parts.o + ((first + item) * parts.rows + c) * D + lane;
-        const size_t step = static_cast<size_t>(parts.rows) * D;
-        for (int base = 0; base < n; base += 32) {
-          float w = 0.f;
-          if (base + lane < n) {
-            const float2 v = ml[static_cast<size_t>(base + lane) * parts.rows];
-            w = v.y == 0.f || lse2 == -INFINITY ? 0.f : exp2f(v.x - lse2);
-          }
-          const int here = min(32, n - base);
-          for (int i = 0; i < here; i += 4) {
-            float v[4][kPer];
+    const int e = static_cast<int>(item / g.nrb), r0 = static_cast<int>(item % g.nrb) * g.rr;
+    Run own[kRowsPerWarp], pre[kRowsPerWarp];
+    Held held[kRowsPerWarp];
+    float lse2[kRowsPerWarp], o[kRowsPerWarp][kPer] = {};
+    int row[kRowsPerWarp], n_own = 0, n_pre = 0;
 #pragma unroll
-            for (int y = 0; y < 4; ++y)
+    for (int y = 0; y < kRowsPerWarp; ++y) {  // the rows' loads are under way together
+      const int c = c0 + y * (kMergeThreads / 32), r = r0 + c;
+      const bool there = c < g.rr && r < g.R;
+      row[y] = there ? e * g.R + r : -1;
+      own[y] = own_run(a, e, there ? r : r0, D);
+      if (a.has_prefix) pre[y] = prefix_run(a, e, there ? r : r0, D);
+      else pre[y] = Run{own[y].ml, own[y].o, 0, 0};
+      held[y] = {part_ml(own[y], lane), part_ml(pre[y], lane)};
+      n_own = max(n_own, own[y].n);
+      n_pre = max(n_pre, pre[y].n);
+    }
 #pragma unroll
-              for (int x = 0; x < kPer; ++x) v[y][x] = i + y < here ? src[(base + i + y) * step + x * 32] : 0.f;
+    for (int y = 0; y < kRowsPerWarp; ++y) lse2[y] = merged_lse2(held[y], own[y], pre[y], lane);
+    // O of the parts, in order: the prefix's, then the own ones
+    auto add = [&](const Run(&u)[kRowsPerWarp], int n, bool is_own) {
+      for (int base = 0; base < n; base += 32) {
+        float w[kRowsPerWarp];
 #pragma unroll
-            for (int y = 0; y < 4; ++y) {
-              const float wi = __shfl_sync(0xffffffffu, w, (i + y) & 31);
-#pragma unroll
-              for (int x = 0; x < kPer; ++x) o[x] = i + y < here && wi != 0.f ? fmaf(v[y][x], wi, o[x]) : o[x];
-            }
-          }
+        for (int y = 0; y < kRowsPerWarp; ++y) {
+          const float2 v = base == 0 ? (is_own ? held[y].own : held[y].pre) : part_ml(u[y], base + lane);
+          w[y] = v.y == 0.f || lse2[y] == -INFINITY ? 0.f : exp2f(v.x - lse2[y]);
         }
-      };
-      if (a.has_prefix) run(a.pre_parts, p.pre_item, p.pre_c, p.pre.first, p.pre.last - p.pre.first + 1);
-      run(a.own_parts, p.own_item, p.own_c, p.own.first, p.own.last - p.own.first + 1);
+        const int here = min(32, n - base);
+        for (int i = 0; i < here; i += U) {
+          float f[U][kRowsPerWarp][kPer];
 #pragma unroll
-      for (int x = 0; x < kPer; ++x) a.o[row * D + x * 32 + lane] = __float2bfloat16(o[x]);
+          for (int v = 0; v < U; ++v)
+#pragma unroll
+            for (int y = 0; y < kRowsPerWarp; ++y) {
+              const bool some = i + v < here && base + i + v < u[y].n;
+              const float* src = u[y].o + static_cast<size_t>(base + i + v) * u[y].rows * D + lane;
+#pragma unroll
+              for (int z = 0; z < kPer; ++z) f[v][y][z] = some ? __ldcg(src + z * 32) : 0.f;
+            }
+#pragma unroll
+          for (int v = 0; v < U; ++v)
+#pragma unroll
+            for (int y = 0; y < kRowsPerWarp; ++y) {
+              const float wi = __shfl_sync(0xffffffffu, w[y], (i + v) & 31);
+#pragma unroll
+              for (int z = 0; z < kPer; ++z)
+                o[y][z] = i + v < here && wi != 0.f ? fmaf(f[v][y][z], wi, o[y][z]) : o[y][z];
+            }
+        }
+      }
+    };
+    add(pre, n_pre, false);
+    add(own, n_own, true);
+#pragma unroll
+    for (int y = 0; y < kRowsPerWarp; ++y) {
+      if (row[y] < 0) continue;
+#pragma unroll
+      for (int z = 0; z < kPer; ++z) a.o[static_cast<size_t>(row[y]) * D + z * 32 + lane] = __float2bfloat16(o[y][z]);
       if (lane == 0) {
-        a.lse2[row] = lse2;
-        if (a.lse) a.lse[row] = lse2 * 0.69314718055994531f;
+        a.lse2[row[y]] = lse2[y];
+        if (a.lse) a.lse[row[y]] = lse2[y] * 0.69314718055994531f;
       }
     }
     return;
@@ -236,23 +237,25 @@ __global__ void __launch_bounds__(kMergeThreads, 4) merge_kernel(MergeArgs a) {
   __shared__ float lse2_sh[kLogitRows];
   const int w = blockIdx.x - a.row_blocks;
   const int e = w / a.key_blocks, j0 = w % a.key_blocks * kMergeKeys;
-  const AtGeo& g = a.own;
   const int len = at_len(g, e);
-  if (j0 >= len) return;
+  // loads that need no normaliser, under way while it is computed
   constexpr int kKeys = kMergeKeys / kMergeThreads, kAhead = 4;
   const float* y = a.logits + static_cast<size_t>(e) * g.R * g.cap;
-  float sum[kKeys], ahead[kAhead][kKeys];  // loads that need no normaliser, under way while it is computed
+  float sum[kKeys], ahead[kAhead][kKeys];
 #pragma unroll
   for (int x = 0; x < kKeys; ++x) {
     const int j = j0 + x * kMergeThreads + tid;
-    sum[x] = j < len ? a.weights[static_cast<size_t>(e) * g.cap + j] : 0.f;
+    sum[x] = j < g.cap ? a.weights[static_cast<size_t>(e) * g.cap + j] : 0.f;
 #pragma unroll
     for (int r = 0; r < kAhead; ++r)
-      ahead[r][x] = j < len && r < g.R ? __ldcg(y + static_cast<size_t>(r) * g.cap + j) : 0.f;
+      ahead[r][x] = j < g.cap && r < g.R ? __ldcg(y + static_cast<size_t>(r) * g.cap + j) : 0.f;
   }
+  if (j0 >= len) return;
   for (int r = warp; r < g.R; r += kMergeThreads / 32) {
-    const RowParts p = row_parts(a, e, r);
-    const float v = p.split ? merged_lse2(a, p, WarpParts(p), lane) : a.lse2[static_cast<long long>(e) * g.R + r];
+    const Run own = own_run(a, e, r, D);
+    const Run pre = a.has_prefix ? prefix_run(a, e, r, D) : Run{own.ml, own.o, 0, 0};
+    const float v = a.has_prefix || own.n > 1 ? merged_lse2({part_ml(own, lane), part_ml(pre, lane)}, own, pre, lane)
+                                              : a.lse2[static_cast<size_t>(e) * g.R + r];
     if (lane == 0) lse2_sh[r] = v;
   }
   __syncthreads();
@@ -364,8 +367,10 @@ cudaError_t launch_attend_merge(const Shape& s, const AttendArgs& a, cudaStream_
     m.pre.len = a.plen;
     m.pre_parts = l.prefix.parts(a.ws);
   }
-  m.row_blocks = static_cast<int>((l.has_prefix ? l.own.items : l.own.grid) *
-                                  ((l.own.geo.rr + kMergeRows - 1) / kMergeRows));
+  // Few items are cut into many parts each, of few rows; many items into two or three parts, of many rows.
+  const bool many_rows = !l.has_prefix && l.own.items >= l.own.grid;
+  const int rows = kMergeThreads / 32 * (many_rows ? 2 : 1);
+  m.row_blocks = static_cast<int>((l.has_prefix ? l.own.items : l.own.grid) * ((l.own.geo.rr + rows - 1) / rows));
   m.sc = a.sc;
   m.o = a.o;
   m.lse = a.lse;
@@ -377,8 +382,9 @@ cudaError_t launch_attend_merge(const Shape& s, const AttendArgs& a, cudaStream_
     m.key_blocks = (s.cap + kMergeKeys - 1) / kMergeKeys;
     blocks += static_cast<unsigned>(l.own.geo.I) * m.key_blocks;
   }
-  return s.d == 128 ? launch_after(merge_kernel<128>, blocks, kMergeThreads, 0, st, m)
-                    : launch_after(merge_kernel<64>, blocks, kMergeThreads, 0, st, m);
+  const auto kernel = s.d == 128 ? (many_rows ? merge_kernel<128, 2, 2> : merge_kernel<128, 1, 4>)
+                                 : (many_rows ? merge_kernel<64, 2, 2> : merge_kernel<64, 1, 4>);
+  return launch_after(kernel, blocks, kMergeThreads, 0, st, m);
 }
 
 }  // namespace bkv

@@ -13,6 +13,7 @@
 
 #include "bkv_device.cuh"
 #include "bkv_internal.h"
+#include "k_launch.cuh"
 
 namespace bkv {
 
@@ -206,22 +207,21 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
 struct AtParts {
   float* o = nullptr;           // [segment][N rows][D] sums of p v
   float2* ml = nullptr;         // [segment][N rows] (reference, sum of p), base 2
-  long long* u0 = nullptr;      // [item] number of its first tile in the run of all tiles
-  long long* per = nullptr;     // [1] tiles per CTA
+  int2* span = nullptr;         // [item] first and last CTA that worked on it
   long long* cut = nullptr;     // [CTA] the item that the CTA began and left to others to finish, or -1
   int rows = 0;                 // rows per segment in o and ml
 };
 
-// What a CTA leaves in `cut` after its last segment.
-__device__ __forceinline__ long long at_cut(const AtSeg& s) { return s.t0 == 0 && s.t1 < s.T ? s.item : -1; }
-
-// Parts of an item: CTAs first .. last worked on it.
-struct AtSpan {
-  int first, last;
-};
-__device__ __forceinline__ AtSpan at_span(const AtParts& p, long long item, int tiles) {
-  const long long u = p.u0[item], per = *p.per;
-  return {static_cast<int>(u / per), static_cast<int>((u + tiles - 1) / per)};
+// What a CTA notes of its segments for the merge; `per` is the number of tiles of a full share.
+__device__ __forceinline__ void at_note(const AtParts& p, const AtSeg& s, bool last_segment, long long per) {
+  if (s.t0 == 0) {
+    // the division is by 32-bit numbers unless there are more than 2^32 tiles
+    const long long u = s.u + s.T - 1;
+    const int last = u < (1ll << 32) ? static_cast<int>(static_cast<uint32_t>(u) / static_cast<uint32_t>(per))
+                                     : static_cast<int>(u / per);
+    p.span[s.item] = make_int2(blockIdx.x, last);
+  }
+  if (last_segment) p.cut[blockIdx.x] = s.t0 == 0 && s.t1 < s.T ? s.item : -1;
 }
 
 // One source's launch plan, made on the host.
@@ -229,13 +229,12 @@ struct AtPlan {
   AtGeo geo;
   int grid;
   long long items;
-  size_t off_o, off_ml, off_u0, off_per, off_cut;  // byte offsets in the workspace
+  size_t off_o, off_ml, off_span, off_cut;  // byte offsets in the workspace
   AtParts parts(unsigned char* ws) const {
     AtParts p;
     p.o = reinterpret_cast<float*>(ws + off_o);
     p.ml = reinterpret_cast<float2*>(ws + off_ml);
-    p.u0 = reinterpret_cast<long long*>(ws + off_u0);
-    p.per = reinterpret_cast<long long*>(ws + off_per);
+    p.span = reinterpret_cast<int2*>(ws + off_span);
     p.cut = reinterpret_cast<long long*>(ws + off_cut);
     p.rows = geo.mb * geo.rr;
     return p;
@@ -275,30 +274,6 @@ struct AtKernelArgs {
   float* logits;       // [rows][cap] or nullptr
   int* err;
 };
-// Overlapping launches on one stream.  A kernel launched by launch_after starts while the one before it
-// on the stream still runs, as soon as all of that one's blocks have called grid_dependents_go() (or
-// ended); grid_dependency_wait() then returns once the kernel before has ended and its writes are
-// visible.  A kernel whose work needs nothing of the one before waits at its end instead: what follows
-// it may rely on both.
-__device__ __forceinline__ void grid_dependents_go() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-__device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
-
-template <typename... P, typename... A>
-cudaError_t launch_after(void (*kernel)(P...), unsigned blocks, unsigned threads, size_t smem, cudaStream_t st,
-                         const A&... args) {
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr.val.programmaticStreamSerializationAllowed = 1;
-  cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(blocks);
-  cfg.blockDim = dim3(threads);
-  cfg.dynamicSmemBytes = smem;
-  cfg.stream = st;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, kernel, args...);
-}
-
 // Row blocks of up to 128 rows (k_attend_tiles.cuh, one translation unit per head_dim), and of up to
 // 256 (k_attend_rows.cu).
 cudaError_t launch_attend_rows(int d, const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap,

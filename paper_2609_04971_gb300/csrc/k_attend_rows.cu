@@ -101,7 +101,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_before();
   at_split_tiles<kThreads>(g, scan_sh, &share_sh);
   tc_fence_after();
-  if (blockIdx.x == 0 && tid == 0) *a.parts.per = share_sh.per;
   if (tid == 0 && share_sh.left == 0) a.parts.cut[blockIdx.x] = -1;
   const uint32_t tmem = tmem_base_sh;
   AtWalk walk{share_sh.at.e, share_sh.at.k, share_sh.at.t, share_sh.left, share_sh.u};
@@ -274,10 +273,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int lim = row < 0 ? 0 : g.causal ? max(0, s.len - g.n_q + 1 + (s.r0 + c % g.rr) % g.n_q) : s.len;
       const int lim_min = __reduce_min_sync(0xffffffffu, row < 0 ? 0x7fffffff : lim);  // of the warp's rows
       const int limit_max = at_limit_max(g, s.len, s.r0);
-      if (tid == 128) {
-        if (s.t0 == 0) a.parts.u0[s.item] = s.u;
-        if (!more) a.parts.cut[blockIdx.x] = at_cut(s);
-      }
+      if (tid == 128) at_note(a.parts, s, !more, share_sh.per);
       float ref = 0.f, l = 0.f;  // ref: minus the reference
       for (int t = s.t0; t < s.t1; ++t, ++i) {
         const int k0 = t * kAtTile, seen = lim - k0;  // keys of the tile that the row sees

@@ -187,7 +187,6 @@ __global__ void __launch_bounds__(kAtThreads, 1)
   tc_fence_before();
   at_split_tiles<kAtThreads>(g, scan_sh, &share_sh);
   tc_fence_after();
-  if (blockIdx.x == 0 && tid == 0) *a.parts.per = share_sh.per;
   if (tid == 0 && share_sh.left == 0) a.parts.cut[blockIdx.x] = -1;
   const uint32_t tmem = tmem_base_sh;
   AtWalk walk{share_sh.at.e, share_sh.at.k, share_sh.at.t, share_sh.left, share_sh.u};
@@ -416,10 +415,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
         rows[wt] = c < cols ? at_row(g, s.e, {s.b0, s.r0}, c) : -1;
         lim[wt] = g.causal ? max(0, s.len - g.n_q + 1 + (s.r0 + c % g.rr) % g.n_q) : s.len;
       }
-      if (wt == 0 && grp == 0) {
-        if (s.t0 == 0) a.parts.u0[s.item] = s.u;
-        if (!more) a.parts.cut[blockIdx.x] = at_cut(s);
-      }
+      if (tid == 128) at_note(a.parts, s, !more, share_sh.per);
       named_barrier(bar_id, 128);
       float l[NC];
 #pragma unroll

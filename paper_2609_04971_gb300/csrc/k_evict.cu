@@ -1,32 +1,27 @@
 // Eviction by accumulated attention weight: selection of the kept rows and
-// compaction of K, V and the weights, one CTA per instance.
+// compaction of K, V and the weights.
 //
-// Selection.  Each warp owns a contiguous run of rows, 32 at a time across its
-// lanes.  Up to a capacity of 10240 their keys stay in registers; longer caches
-// are read again in each of the five passes, from L1 and L2, which leaves room for
-// four CTAs per SM.
-// A three-pass radix select (digits of 12, 10 and 10 bits from the top, one
-// shared histogram) finds the key T of the last row that is kept by weight and
-// how many rows equal to T are needed.  A 12-bit first digit splits an octave
-// into 8 bins: weights that span a few octaves, as softmax sums do, then spread
-// over enough bins that the histogram's atomics seldom meet.  Kept rows are
-// numbered in index order by ballots inside each warp and one scan of the warps'
-// totals; rows equal to T are taken in index order.
+// Selection, one CTA per instance.  Each warp owns a contiguous run of rows, 32 at
+// a time across its lanes, and holds their keys in registers.  A three-pass radix
+// select (digits of 12, 10 and 10 bits from the top, one shared histogram) finds the
+// key T of the last row that is kept by weight and how many rows equal to T are needed.
+// A 12-bit first digit splits an octave into 8 bins: weights that span a few octaves,
+// as softmax sums do, then spread over enough bins that the histogram's atomics seldom
+// meet.  Kept rows are numbered in index order by ballots inside each warp and one scan
+// of the warps' totals; rows equal to T are taken in index order.
 //
-// Compaction.  Row i receives row kept[i] >= i.  Into other buffers the rows are
-// independent.  In place they are taken in ascending chunks: all loads of a
-// chunk are issued before the barrier that precedes its stores, and they touch
-// only rows that no earlier chunk writes; rows before the first evicted one
-// already stand where they belong.  The weights move with the rows.
-//
-// Into other buffers an instance may be worked on by several CTAs, each of which
-// repeats the selection and moves its share of the rows.  That fills the GPU when
-// there are few instances, and evens out what a last wave of CTAs leaves idle.
+// Compaction, a launch of its own.  Row i receives row kept[i] >= i.  Into other
+// buffers the rows are independent and move in small blocks spread over all SMs.  In
+// place an instance has one CTA, which takes its rows in ascending chunks: all loads of
+// a chunk are issued before the barrier that precedes its stores, and they touch only
+// rows that no earlier chunk writes; rows before the first evicted one already stand
+// where they belong.  The weights move with the rows.
 //
 // Bound by HBM: the kept rows are read and written once (8 d bytes a row), the
 // weights read (4 bytes a cached row) and written.
 #include "bkv_device.cuh"
 #include "bkv_internal.h"
+#include "k_launch.cuh"
 
 namespace bkv {
 namespace {
@@ -63,41 +58,41 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* wsum, uint3
   return before + incl - v;
 }
 
-// The rows of one warp: row0 + 32 i + lane for i < n, with their keys in registers (KPT > 0) or read
-// again on every use (KPT = 0).
+// A load that a false predicate skips, without the branch that would keep the next load from starting.
+__device__ __forceinline__ float load_if(const float* p, bool yes) {
+  float v;
+  asm volatile(
+      "{\n\t.reg .pred q;\n\t"
+      "setp.ne.u32 q, %2, 0;\n\t"
+      "mov.f32 %0, 0f00000000;\n\t"
+      "@q ld.global.f32 %0, [%1];\n\t}"
+      : "=f"(v)
+      : "l"(p), "r"(static_cast<uint32_t>(yes))
+      : "memory");
+  return v;
+}
+
+// The rows of one warp: row0 + 32 i + lane for i < n, and their keys.
 template <int KPT>
 struct WarpRows {
-  uint32_t key[KPT > 0 ? KPT : 1];
-  const float* w;
-  int row0, n, L, lane;
-  __device__ __forceinline__ int row(int i) const { return row0 + i * 32 + lane; }
-  __device__ __forceinline__ void init() {
-    if constexpr (KPT > 0) {
+  uint32_t key[KPT];
+  int row0, n, lane;
+  __device__ __forceinline__ void init(const float* w, int L) {
+    float v[KPT];
 #pragma unroll
-      for (int i = 0; i < KPT; ++i) key[i] = i < n && row(i) < L ? weight_key(w[row(i)]) : 0;
+    for (int i = 0; i < KPT; ++i) {
+      const int j = row0 + i * 32 + lane;
+      v[i] = load_if(w + j, i < n && j < L);
     }
+#pragma unroll
+    for (int i = 0; i < KPT; ++i) key[i] = weight_key(v[i]);
   }
   // f(row, key) for every i, also where the row is not below L (every lane takes part).
   template <typename F>
   __device__ __forceinline__ void each(F&& f) const {
-    if constexpr (KPT > 0) {
 #pragma unroll
-      for (int i = 0; i < KPT; ++i)
-        if (i < n) f(row(i), key[i]);
-    } else {
-      constexpr int kBatch = 8;  // loads in flight
-      for (int i0 = 0; i0 < n; i0 += kBatch) {
-        uint32_t k[kBatch];
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u) {
-          const int j = row(i0 + u);
-          k[u] = i0 + u < n && j < L ? weight_key(w[j]) : 0;
-        }
-#pragma unroll
-        for (int u = 0; u < kBatch; ++u)
-          if (i0 + u < n) f(row(i0 + u), k[u]);
-      }
-    }
+    for (int i = 0; i < KPT; ++i)
+      if (i < n) f(row0 + i * 32 + lane, key[i]);
   }
 };
 
@@ -109,7 +104,7 @@ __device__ __forceinline__ void select_digit(const WarpRows<KPT>& rows, int c_lo
                                              uint32_t& mask, uint32_t& k, uint32_t* hist, uint32_t* wsum,
                                              uint32_t* found) {
   constexpr int kBins = 1 << BITS;
-  constexpr int kPer = (kBins + THREADS - 1) / THREADS;
+  constexpr int kPer = kBins / THREADS >= 4 ? kBins / THREADS : 4;  // bins per thread, from the top
   const int tid = threadIdx.x;
   for (int i = tid; i < kBins; i += THREADS) hist[i] = 0;
   __syncthreads();
@@ -119,10 +114,14 @@ __device__ __forceinline__ void select_digit(const WarpRows<KPT>& rows, int c_lo
   __syncthreads();
   uint32_t loc[kPer], sum = 0;
 #pragma unroll
-  for (int i = 0; i < kPer; ++i) {
-    const int b = kBins - 1 - (tid * kPer + i);  // descending digits
-    loc[i] = b >= 0 ? hist[b] : 0;
-    sum += loc[i];
+  for (int i = 0; i < kPer; i += 4) {
+    const int b = kBins - 4 - (tid * kPer + i);  // descending digits, four at a time
+    const uint4 v = b >= 0 ? *reinterpret_cast<const uint4*>(hist + b) : make_uint4(0, 0, 0, 0);
+    loc[i] = v.w;
+    loc[i + 1] = v.z;
+    loc[i + 2] = v.y;
+    loc[i + 3] = v.x;
+    sum += v.x + v.y + v.z + v.w;
   }
   uint32_t total;
   uint32_t above = block_scan<THREADS>(sum, wsum, total);
@@ -143,27 +142,27 @@ __device__ __forceinline__ void select_digit(const WarpRows<KPT>& rows, int c_lo
   __syncthreads();
 }
 
-// KPT > 0: at most KPT * THREADS rows per instance.
-template <int D, int THREADS, int KPT, int MINB>
-__global__ void __launch_bounds__(THREADS, MINB) evict_kernel(Shape s, EvictArgs a, int shares) {
+// Selection: kept, len_out, into other buffers the zeros of weights_out, and in `plan` the number of kept rows (-1 for
+// a length out of range) and the first of them that has to move.  At most KPT * THREADS rows.
+template <int THREADS, int KPT, int MINB>
+__global__ void __launch_bounds__(THREADS, MINB) evict_select_kernel(Shape s, EvictArgs a) {
   constexpr int kWarps = THREADS / 32;
-  extern __shared__ __align__(16) uint16_t kept_s[];  // [min(budget, cap)] kept rows (cap <= 32768)
-  __shared__ uint32_t hist[kEvBins];
+  __shared__ __align__(16) uint32_t hist[kEvBins];
   __shared__ uint32_t wsum[kWarps], found[2];
   __shared__ uint32_t w_tie[kWarps], w_keep[kWarps];
   __shared__ int first_sh;
-
-  const int e = blockIdx.x / shares, share = blockIdx.x % shares;
+  const int e = blockIdx.x;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int L = a.L[e];  // len_out may be L itself, but then the instance has one CTA
+  grid_dependents_go();
+  const int L = a.L[e];
   int* kept_e = a.kept + static_cast<size_t>(e) * a.budget;
   if (L < 0 || L > s.cap) {  // the whole block
-    if (share == 0)
-      for (int i = tid; i < a.budget; i += THREADS) kept_e[i] = -1;
-    __syncthreads();
-    if (tid == 0 && share == 0) {
+    for (int i = tid; i < a.budget; i += THREADS) kept_e[i] = -1;
+    __syncthreads();  // len_out may be L itself
+    if (tid == 0) {
       record_error(a.err, kDevBadLength);
       if (a.len_out) a.len_out[e] = 0;
+      a.plan[e] = make_int2(-1, 0);
     }
     return;
   }
@@ -175,10 +174,8 @@ __global__ void __launch_bounds__(THREADS, MINB) evict_kernel(Shape s, EvictArgs
   WarpRows<KPT> rows;
   rows.n = (L + kWarps * 32 - 1) / (kWarps * 32);
   rows.row0 = warp * rows.n * 32;
-  rows.w = w_in;
-  rows.L = L;
   rows.lane = lane;
-  rows.init();
+  rows.init(w_in, L);
   if (tid == 0) first_sh = n_keep;
   uint32_t T = 0, ties = 0;
   const int c_lo = s.n_prefix, c_hi = L - s.W;
@@ -202,9 +199,11 @@ __global__ void __launch_bounds__(THREADS, MINB) evict_kernel(Shape s, EvictArgs
   uint32_t n_tie = 0, n_sure = 0;
   rows.each([&](int j, uint32_t key) {
     const int c = kind(j, key);
-    n_tie += __popc(__ballot_sync(0xffffffffu, c == 2));
-    n_sure += __popc(__ballot_sync(0xffffffffu, c == 1));
+    n_tie += c == 2;
+    n_sure += c == 1;
   });
+  n_tie = __reduce_add_sync(0xffffffffu, n_tie);
+  n_sure = __reduce_add_sync(0xffffffffu, n_sure);
   if (lane == 0) {
     w_tie[warp] = n_tie;
     w_keep[warp] = n_sure;
@@ -217,38 +216,56 @@ __global__ void __launch_bounds__(THREADS, MINB) evict_kernel(Shape s, EvictArgs
     tie_at += t;
   }
   const uint32_t below = (1u << lane) - 1u;
+  bool moves = false;  // a row of this warp that has to move was seen
   rows.each([&](int j, uint32_t key) {
     const int c = kind(j, key);
-    const uint32_t tie_mask = __ballot_sync(0xffffffffu, c == 2);
+    const uint32_t tie_mask = n_tie ? __ballot_sync(0xffffffffu, c == 2) : 0;
     const bool keep = c == 1 || (c == 2 && tie_at + __popc(tie_mask & below) < ties);
     const uint32_t keep_mask = __ballot_sync(0xffffffffu, keep);
     const int pos = static_cast<int>(at + __popc(keep_mask & below));
     if (keep && in_bounds(pos, n_keep, a.err)) {
-      kept_s[pos] = static_cast<uint16_t>(j);
-      if (share == 0) kept_e[pos] = j;
-      if (pos != j) atomicMin(&first_sh, pos);  // rows before it stand where they belong
+      kept_e[pos] = j;
+    }
+    if (!moves) {  // rows before the first one that moves stand where they belong
+      const uint32_t m = __ballot_sync(0xffffffffu, keep && pos != j);
+      if (m) {
+        moves = true;
+        if (lane == __ffs(m) - 1) atomicMin(&first_sh, pos);
+      }
     }
     tie_at += __popc(tie_mask);
     at += __popc(keep_mask);
   });
-  if (share == 0)
-    for (int i = n_keep + tid; i < a.budget; i += THREADS) kept_e[i] = -1;
+  for (int i = n_keep + tid; i < a.budget; i += THREADS) kept_e[i] = -1;
+  if (!in_place)
+    for (int i = n_keep + tid; i < a.cap_out; i += THREADS) w_out[i] = 0.f;
   __syncthreads();
-  if (tid == 0 && share == 0 && a.len_out) a.len_out[e] = n_keep;
+  if (tid == 0) {
+    if (a.len_out) a.len_out[e] = n_keep;
+    a.plan[e] = make_int2(n_keep, first_sh);
+  }
+}
 
-  // ---------------------------------------------------------------- gather
+// Compaction in place: one CTA per instance.
+template <int D>
+__global__ void __launch_bounds__(512, 2) evict_move_in_place_kernel(Shape s, EvictArgs a) {
+  constexpr int kThreads = 512;
   constexpr int kVpr = D * 2 / 16;    // 16-byte vectors per row of one tensor
   constexpr int kRowVec = 2 * kVpr;   // K row, then V row
-  constexpr int kPer = MINB > 1 ? 4 : 8;  // vectors per thread and chunk
-  constexpr int kRowsPerPass = THREADS / kRowVec;
+  constexpr int kPer = 4;             // vectors per thread and chunk, one chunk ahead
+  constexpr int kRowsPerPass = kThreads / kRowVec;
   constexpr int kChunkRows = kRowsPerPass * kPer;
-  static_assert(kChunkRows <= THREADS, "one weight per thread and chunk");
+  static_assert(kChunkRows <= kThreads, "one weight per thread and chunk");
+  const int e = blockIdx.x, tid = threadIdx.x;
+  grid_dependency_wait();
+  const int2 plan = a.plan[e];
+  if (plan.x < 0) return;
+  const int first = plan.y, end = plan.x;
+  const int* kept = a.kept + static_cast<size_t>(e) * a.budget;
   const int col = tid % kRowVec, r0 = tid / kRowVec;
   const int vcol = col < kVpr ? col : col - kVpr;
-  const uint4* src = reinterpret_cast<const uint4*>((col < kVpr ? a.K : a.V) + static_cast<size_t>(e) * s.cap * D) + vcol;
-  uint4* dst = reinterpret_cast<uint4*>((col < kVpr ? a.K_out : a.V_out) + static_cast<size_t>(e) * a.cap_out * D) + vcol;
-  const int first = in_place ? first_sh : static_cast<int>(static_cast<long long>(n_keep) * share / shares);
-  const int end = in_place ? n_keep : static_cast<int>(static_cast<long long>(n_keep) * (share + 1) / shares);
+  uint4* base = reinterpret_cast<uint4*>((col < kVpr ? a.K_out : a.V_out) + static_cast<size_t>(e) * s.cap * D) + vcol;
+  float* weights = a.weights_out + static_cast<size_t>(e) * s.cap;
 
   uint4 cur[kPer], nxt[kPer];
   float w_cur = 0.f, w_nxt = 0.f;
@@ -257,61 +274,94 @@ __global__ void __launch_bounds__(THREADS, MINB) evict_kernel(Shape s, EvictArgs
     for (int u = 0; u < kPer; ++u) {
       const int row = i0 + r0 + kRowsPerPass * u;
       if (row < end) {
-        int from = kept_s[row];
-        if (!in_bounds(from - row, L - row, a.err)) from = row;  // row <= kept[row] < L
-        R[u] = __ldcg(src + static_cast<size_t>(from) * kVpr);
+        int j = __ldcg(kept + row);
+        if (!in_bounds(j - row, s.cap - row, a.err)) j = row;  // row <= kept[row] < cap
+        R[u] = __ldcg(base + static_cast<size_t>(j) * kVpr);
       }
     }
     if (tid < kChunkRows && i0 + tid < end) {
-      int from = kept_s[i0 + tid];
-      if (!in_bounds(from, L, a.err)) from = i0 + tid;
-      w = __ldcg(w_in + from);
+      int j = __ldcg(kept + i0 + tid);
+      if (!in_bounds(j, s.cap, a.err)) j = i0 + tid;
+      w = __ldcg(weights + j);
     }
   };
   if (first < end) load_chunk(first, cur, w_cur);
   for (int i0 = first; i0 < end; i0 += kChunkRows) {
-    if (in_place) __syncthreads();  // every load of this chunk was issued before any of its stores
+    __syncthreads();  // every load of this chunk was issued before any of its stores
     const int i1 = i0 + kChunkRows;
     if (i1 < end) load_chunk(i1, nxt, w_nxt);
 #pragma unroll
     for (int u = 0; u < kPer; ++u) {
       const int row = i0 + r0 + kRowsPerPass * u;
-      if (row < end) dst[static_cast<size_t>(row) * kVpr] = cur[u];
+      if (row < end) base[static_cast<size_t>(row) * kVpr] = cur[u];
     }
-    if (tid < kChunkRows && i0 + tid < end) w_out[i0 + tid] = w_cur;
+    if (tid < kChunkRows && i0 + tid < end) weights[i0 + tid] = w_cur;
 #pragma unroll
     for (int u = 0; u < kPer; ++u) cur[u] = nxt[u];
     w_cur = w_nxt;
   }
-  if (in_place) __syncthreads();  // the last kept weights have been read
-  for (int i = n_keep + share * THREADS + tid; i < a.cap_out; i += shares * THREADS) w_out[i] = 0.f;
+  __syncthreads();  // the last kept weights have been read
+  for (int i = end + tid; i < s.cap; i += kThreads) weights[i] = 0.f;
 }
 
-template <int D, int THREADS, int KPT, int MINB>
-cudaError_t launch(const Shape& s, const EvictArgs& a, cudaStream_t st) {
-  const int kept = a.budget < s.cap ? a.budget : s.cap;
-  const int smem = kept * static_cast<int>(sizeof(uint16_t));
-  const cudaError_t e = cudaFuncSetAttribute(evict_kernel<D, THREADS, KPT, MINB>,
-                                             cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e != cudaSuccess) return e;
-  // Shares of an instance into other buffers: as many as bring the grid to kShareGrid CTAs, with rows
-  // enough for each (a selection costs what a few hundred rows do).
-  int shares = 1;
-  if (a.K_out != a.K && a.len_out != a.L) {
-    constexpr int kShareGrid = 304, kShareRows = 64;
-    shares = (kShareGrid + s.n_inst - 1) / s.n_inst;
-    if (shares > (kept + kShareRows - 1) / kShareRows) shares = (kept + kShareRows - 1) / kShareRows;
+// Compaction into other buffers: kMoveRows rows of an instance to a block.
+constexpr int kMoveRows = 64, kMoveThreads = 256;
+template <int D>
+__global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(Shape s, EvictArgs a, int chunks) {
+  constexpr int kVpr = D * 2 / 16, kRowVec = 2 * kVpr, kPer = kMoveRows * kRowVec / kMoveThreads;
+  __shared__ int rows[kMoveRows];
+  const int e = blockIdx.x / chunks, i0 = blockIdx.x % chunks * kMoveRows;
+  const int tid = threadIdx.x;
+  grid_dependency_wait();
+  const int n = min(kMoveRows, a.plan[e].x - i0);
+  if (tid < kMoveRows) rows[tid] = tid < n ? __ldcg(a.kept + static_cast<size_t>(e) * a.budget + i0 + tid) : 0;
+  if (n <= 0) return;
+  __syncthreads();
+  const int col = tid % kRowVec, r0 = tid / kRowVec;
+  const int vcol = col < kVpr ? col : col - kVpr;
+  const uint4* src = reinterpret_cast<const uint4*>((col < kVpr ? a.K : a.V) + static_cast<size_t>(e) * s.cap * D) + vcol;
+  uint4* dst = reinterpret_cast<uint4*>((col < kVpr ? a.K_out : a.V_out) +
+                                        (static_cast<size_t>(e) * a.cap_out + i0) * D) + vcol;
+  const bool mine = tid < n;  // one weight per thread
+  float w = 0.f;
+  if (mine) {
+    int j = rows[tid];
+    if (!in_bounds(j, s.cap, a.err)) j = i0 + tid;
+    w = a.weights[static_cast<size_t>(e) * s.cap + j];
   }
-  evict_kernel<D, THREADS, KPT, MINB><<<s.n_inst * shares, THREADS, smem, st>>>(s, a, shares);
-  return cudaGetLastError();
+  uint4 R[kPer];
+#pragma unroll
+  for (int u = 0; u < kPer; ++u) {
+    const int r = r0 + u * (kMoveThreads / kRowVec);
+    if (r < n) {
+      int j = rows[r];
+      if (!in_bounds(j, s.cap, a.err)) j = i0 + r;
+      R[u] = __ldcg(src + static_cast<size_t>(j) * kVpr);
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kPer; ++u) {
+    const int r = r0 + u * (kMoveThreads / kRowVec);
+    if (r < n) dst[static_cast<size_t>(r) * kVpr] = R[u];
+  }
+  if (mine) a.weights_out[static_cast<size_t>(e) * a.cap_out + i0 + tid] = w;
 }
 
-// The capacity decides whether a CTA can hold an instance's keys in registers.
 template <int D>
 cudaError_t launch_d(const Shape& s, const EvictArgs& a, cudaStream_t st) {
-  if (s.cap <= 256 * 8) return launch<D, 256, 8, 1>(s, a, st);
-  if (s.cap <= 512 * 20) return launch<D, 512, 20, 1>(s, a, st);
-  return launch<D, 512, 0, 2>(s, a, st);
+  // threads by the rows that the registers of a CTA have to hold
+  if (s.cap <= 256 * 8)
+    evict_select_kernel<256, 8, 5><<<s.n_inst, 256, 0, st>>>(s, a);
+  else if (s.cap <= 512 * 20)
+    evict_select_kernel<512, 20, 2><<<s.n_inst, 512, 0, st>>>(s, a);
+  else
+    evict_select_kernel<1024, 32, 1><<<s.n_inst, 1024, 0, st>>>(s, a);
+  static_assert(kMaxCapacity <= 1024 * 32, "rows of the largest capacity in registers");
+  const cudaError_t e = cudaGetLastError();
+  if (e != cudaSuccess) return e;
+  if (a.K_out == a.K) return launch_after(evict_move_in_place_kernel<D>, s.n_inst, 512, 0, st, s, a);
+  const int kept = a.budget < s.cap ? a.budget : s.cap, chunks = (kept + kMoveRows - 1) / kMoveRows;
+  return launch_after(evict_move_kernel<D>, static_cast<unsigned>(s.n_inst) * chunks, kMoveThreads, 0, st, s, a, chunks);
 }
 
 }  // namespace

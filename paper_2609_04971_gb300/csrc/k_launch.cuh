@@ -1,0 +1,32 @@
+// Launches that overlap the kernel before them on the stream.
+#pragma once
+
+#include <cuda_runtime.h>
+
+namespace bkv {
+
+// A kernel launched by launch_after starts while the one before it
+// on the stream still runs, as soon as all of that one's blocks have called grid_dependents_go() (or
+// ended); grid_dependency_wait() then returns once the kernel before has ended and its writes are
+// visible.  A kernel whose work needs nothing of the one before waits at its end instead: what follows
+// it may rely on both.
+__device__ __forceinline__ void grid_dependents_go() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void grid_dependency_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+template <typename... P, typename... A>
+cudaError_t launch_after(void (*kernel)(P...), unsigned blocks, unsigned threads, size_t smem, cudaStream_t st,
+                         const A&... args) {
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(blocks);
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+}  // namespace bkv
