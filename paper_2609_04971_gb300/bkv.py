@@ -479,14 +479,15 @@ class BeaconKV:
         return kept_out
 
     # ------------------------------------------------------------ attention over the caches
-    def _new(self, device: torch.device, *specs) -> list:
-        """New outputs, one per (shape, dtype), from the allocator pool of the context's stream (their memory
-        may have been freed by work that is only ordered on that stream)."""
+    def _new(self, like: torch.Tensor, shape, dtype) -> torch.Tensor:
+        """A new output, from the allocator pool of the context's stream (its memory may have been freed by
+        work that is only ordered on that stream)."""
+        device = like.device
         stream = _streams[self.ctx.value]
         if torch._C._cuda_getCurrentRawStream(device.index) == stream:
-            return [torch.empty(shape, dtype=dtype, device=device) for shape, dtype in specs]
+            return torch.empty(shape, dtype=dtype, device=device)
         with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)):
-            return [torch.empty(shape, dtype=dtype, device=device) for shape, dtype in specs]
+            return torch.empty(shape, dtype=dtype, device=device)
 
     def reserve_attend(self, *, n_q: int = 1, n_groups: int = 0, weights: bool = False):
         """Workspace for attend (n_groups = 0) or attend_shared with n_q queries per head; needed once
@@ -506,14 +507,14 @@ class BeaconKV:
         self._expect(weights, rows_kv, "weights")
         if not q.is_cuda:
             raise TypeError("q must be a CUDA tensor")
-        if o_out is None and lse_out is None:
-            o_out, lse_out = self._new(q.device, (shape, torch.bfloat16), (shape[:3], torch.float32))
-        elif o_out is None:
-            o_out, = self._new(q.device, (shape, torch.bfloat16))
-        elif lse_out is None:
-            lse_out, = self._new(q.device, (shape[:3], torch.float32))
-        self._expect(o_out, q.numel(), "o_out")
-        self._expect(lse_out, q.numel() // d, "lse_out")
+        if o_out is None:
+            o_out = self._new(q, shape, torch.bfloat16)
+        else:
+            self._expect(o_out, q.numel(), "o_out")
+        if lse_out is None:
+            lse_out = self._new(q, shape[:3], torch.float32)
+        else:
+            self._expect(lse_out, q.numel() // d, "lse_out")
         return shape[2], o_out, lse_out
 
     def attend(self, q, K, V, *, length, scale=None, weights=None, o_out=None, lse_out=None):
@@ -563,14 +564,11 @@ class BeaconKV:
                 self._expect(t, n, name)
         if not K.is_cuda:
             raise TypeError("K must be a CUDA tensor")
-        if kept_out is None or len_out is None:
-            inst = (c.n_layers, c.batch, c.n_kv_heads)
-            new = self._new(K.device, *([((*inst, max(0, budget)), torch.int32)] if kept_out is None else []),
-                            *([(inst, torch.int32)] if len_out is None else []))
-            if kept_out is None:
-                kept_out = new.pop(0)
-            if len_out is None:
-                len_out = new.pop(0)
+        inst = (c.n_layers, c.batch, c.n_kv_heads)
+        if kept_out is None:
+            kept_out = self._new(K, (*inst, max(0, budget)), torch.int32)
+        if len_out is None:
+            len_out = self._new(K, inst, torch.int32)
         bkv_evict(self.ctx, K, V, weights, L, budget, K_out, V_out, weights_out, cap_out, kept_out, len_out)
         return kept_out, len_out
 

@@ -9,6 +9,7 @@
 #include "bkv_ctx.h"
 #include "bkv_device.cuh"
 #include "bkv_internal.h"
+#include "k_attend.cuh"
 
 using bkv::aligned16;
 using bkv::cuda_fail;
@@ -48,26 +49,26 @@ int attend(bkv_ctx* ctx, bkv::AttendArgs& a, double scale) {
   a.sc = static_cast<float>(1.4426950408889634 * (scale == 0.0 ? 1.0 / std::sqrt(static_cast<double>(s.d)) : scale));
   if (!std::isfinite(a.sc) || a.sc < 1.17549435e-38f)
     return fail(ctx, BKV_EINVAL, "scale is out of the range of fp32");
-  const size_t need = bkv::attend_workspace(s, a.n_q, a.groups, a.weights != nullptr);
-  if (need > ctx->attend_ws_bytes)
-    return fail(ctx, BKV_ESTATE, "this call needs %zu bytes of workspace, bkv_attend_reserve made %zu", need,
+  const bkv::AtLayout l = bkv::attend_layout(s, a.n_q, a.groups, a.pcap, a.weights != nullptr);
+  if (l.bytes > ctx->attend_ws_bytes)
+    return fail(ctx, BKV_ESTATE, "this call needs %zu bytes of workspace, bkv_attend_reserve made %zu", l.bytes,
                 ctx->attend_ws_bytes);
   a.ws = ctx->attend_ws;
   a.err = ctx->err;
   cudaError_t e;
   {
     ProfScope ps(ctx, BKV_K_ATTEND);
-    e = bkv::launch_attend(s, a, ctx->stream);
+    e = bkv::launch_attend(s, a, l, ctx->stream);
   }
   if (e != cudaSuccess) return cuda_fail(ctx, e, "attend launch");
   {
     ProfScope ps(ctx, BKV_K_ATTEND_MERGE);
-    e = bkv::launch_attend_merge(s, a, ctx->stream);
+    e = bkv::launch_attend_merge(s, a, l, ctx->stream);
   }
   if (e != cudaSuccess) return cuda_fail(ctx, e, "attend merge launch");
-  if (a.weights && bkv::attend_recomputes_weights(s, a.n_q)) {
+  if (a.weights && !l.logits) {
     ProfScope ps(ctx, BKV_K_ATTEND_WEIGHTS);
-    e = bkv::launch_attend_weights(s, a, ctx->stream);
+    e = bkv::launch_attend_weights(s, a, l, ctx->stream);
     if (e != cudaSuccess) return cuda_fail(ctx, e, "attend weights launch");
   }
   return BKV_OK;
@@ -81,7 +82,7 @@ int bkv_attend_reserve(bkv_ctx* ctx, int32_t n_q, int32_t n_groups, int weights)
   if (!ctx) return BKV_EINVAL;
   const int rc = check_attend_shape(ctx, n_q, n_groups);
   if (rc != BKV_OK) return rc;
-  const size_t need = bkv::attend_workspace(ctx->shape, n_q, n_groups, weights != 0);
+  const size_t need = n_q == 0 ? 0 : bkv::attend_layout(ctx->shape, n_q, n_groups, 1, weights != 0).bytes;
   if (need <= ctx->attend_ws_bytes) return BKV_OK;
   // the new workspace exists before the old one goes, so that a failure changes nothing
   unsigned char* ws = nullptr;

@@ -169,7 +169,7 @@ cudaError_t launch_select_gather_ragged(const Shape& s, const float* r, const in
 
 cudaError_t launch_keep_all(const Shape& s, int L, int budget, int* kept, cudaStream_t st);
 
-// ---- attention over the caches (k_attend.cu, k_attend_weights.cu); rows are (query head, query) pairs
+// ---- attention over the caches (k_attend.cuh); rows are (query head, query) pairs
 struct AttendArgs {
   const __nv_bfloat16* q = nullptr;              // [batch][n_kv * G][n_q][d]
   const __nv_bfloat16 *K = nullptr, *V = nullptr;    // [batch][n_kv][cap][d]
@@ -185,15 +185,6 @@ struct AttendArgs {
   unsigned char* ws = nullptr;
   int* err = nullptr;
 };
-// Workspace bytes of one call (0 when the shape overflows the kernels' 32-bit item counts).
-size_t attend_workspace(const Shape& s, int n_q, int groups, bool weights);
-// In this order on one stream: tiles, merge (with the weights where the logits were kept), and the
-// weights recomputed from the keys where they were not.
-cudaError_t launch_attend(const Shape& s, const AttendArgs& a, cudaStream_t st);
-cudaError_t launch_attend_merge(const Shape& s, const AttendArgs& a, cudaStream_t st);
-bool attend_recomputes_weights(const Shape& s, int n_q);
-cudaError_t launch_attend_weights(const Shape& s, const AttendArgs& a, cudaStream_t st);
-
 // ---- eviction by accumulated weight (k_evict.cu)
 struct EvictArgs {
   const __nv_bfloat16 *K = nullptr, *V = nullptr;

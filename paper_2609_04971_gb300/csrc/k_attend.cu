@@ -22,7 +22,7 @@ size_t align_up(size_t n) { return (n + 255) / 256 * 256; }
 
 }  // namespace
 
-int attend_sms() {
+static int attend_sms() {
   int dev = 0, n = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
       n < 1) {
@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(kMergeThreads, 4) merge_kernel(MergeArgs a) {
 
 AtLayout attend_layout(const Shape& s, int n_q, int groups, int pcap, bool weights) {
   AtLayout l;
-  const int sms = attend_sms();
+  const int sms = l.sms = attend_sms();
   const int R = s.G * n_q;
   l.own = make_plan(s, s.batch * s.n_kv, 1, R, n_q, true, s.cap, 1, sms);
   size_t at = place_parts(l.own, s.d, sms, 0);
@@ -314,14 +314,7 @@ AtLayout attend_layout(const Shape& s, int n_q, int groups, int pcap, bool weigh
   return l;
 }
 
-bool attend_recomputes_weights(const Shape& s, int n_q) { return s.G * n_q > kLogitRows; }
-
-size_t attend_workspace(const Shape& s, int n_q, int groups, bool weights) {
-  return n_q < 1 ? 0 : attend_layout(s, n_q, groups, 1, weights).bytes;
-}
-
-cudaError_t launch_attend(const Shape& s, const AttendArgs& a, cudaStream_t st) {
-  const AtLayout l = attend_layout(s, a.n_q, a.groups, a.pcap, a.weights != nullptr);
+cudaError_t launch_attend(const Shape& s, const AttendArgs& a, const AtLayout& l, cudaStream_t st) {
   float* lse2 = reinterpret_cast<float*>(a.ws + l.off_lse2);
   float* logits = l.logits ? reinterpret_cast<float*>(a.ws + l.off_logits) : nullptr;
   auto tiles = [&](const AtPlan& p, const __nv_bfloat16* K, const __nv_bfloat16* V, const int* len, bool own) {
@@ -355,8 +348,7 @@ cudaError_t launch_attend(const Shape& s, const AttendArgs& a, cudaStream_t st) 
   return cudaSuccess;
 }
 
-cudaError_t launch_attend_merge(const Shape& s, const AttendArgs& a, cudaStream_t st) {
-  const AtLayout l = attend_layout(s, a.n_q, a.groups, a.pcap, a.weights != nullptr);
+cudaError_t launch_attend_merge(const Shape& s, const AttendArgs& a, const AtLayout& l, cudaStream_t st) {
   MergeArgs m{};
   m.own = l.own.geo;
   m.own.len = a.len;

@@ -250,15 +250,21 @@ struct AtLayout {
   size_t off_logits = 0;   // fp32 [rows][cap]
   size_t off_wpart = 0, off_wu0 = 0;  // weights recomputed from the keys: see k_attend_weights.cu
   size_t bytes = 0;
+  int sms = 0;             // of the current device: one CTA of the attention kernels each
 };
-// SMs of the current device (one CTA of the attention kernels each).
-int attend_sms();
+// The workspace does not depend on pcap.
 AtLayout attend_layout(const Shape& s, int n_q, int groups, int pcap, bool weights);
 
 // Workspace of the recomputed weights: [2 grid][128] partial sums, then [items + 1] unit numbers.
 inline long long weights_items(const Shape& s) {
   return 1ll * s.batch * s.n_kv * ((s.cap + kAtTile - 1) / kAtTile);
 }
+
+// In this order on one stream: tiles, merge (with the weights where the logits were kept), and with
+// weights but no logits the weights, recomputed from the keys.
+cudaError_t launch_attend(const Shape& s, const AttendArgs& a, const AtLayout& l, cudaStream_t st);
+cudaError_t launch_attend_merge(const Shape& s, const AttendArgs& a, const AtLayout& l, cudaStream_t st);
+cudaError_t launch_attend_weights(const Shape& s, const AttendArgs& a, const AtLayout& l, cudaStream_t st);
 
 // Arguments of the attention kernel.
 struct AtKernelArgs {

@@ -426,8 +426,7 @@ template <int D>
 cudaError_t launch(const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap, const CUtensorMap& vmap,
                    const AtKernelArgs& a, cudaStream_t st) {
   using C = RowsCfg<D>;
-  const cudaError_t e =
-      cudaFuncSetAttribute(rows_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(C::kSmem));
+  const cudaError_t e = allow_smem<rows_kernel<D>>(C::kSmem);
   if (e != cudaSuccess) return e;
   return launch_after(rows_kernel<D>, p.grid, kThreads, C::kSmem, st, qmap, kmap, vmap, a);
 }

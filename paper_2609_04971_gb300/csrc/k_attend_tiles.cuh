@@ -629,8 +629,7 @@ template <int D, int U>
 cudaError_t launch(const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap, const CUtensorMap& vmap,
                    const AtKernelArgs& a, cudaStream_t st) {
   using C = AtCfg<D, U>;
-  const cudaError_t e = cudaFuncSetAttribute(attend_kernel<D, U>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             static_cast<int>(C::kSmem));
+  const cudaError_t e = allow_smem<attend_kernel<D, U>>(C::kSmem);
   if (e != cudaSuccess) return e;
   return launch_after(attend_kernel<D, U>, p.grid, kAtThreads, C::kSmem, st, qmap, kmap, vmap, a);
 }

@@ -451,8 +451,7 @@ __global__ void __launch_bounds__(kAtTile) weights_merge_kernel(WArgs a) {
 
 template <int D>
 cudaError_t launch(const CUtensorMap& qmap, const CUtensorMap& kmap, const WArgs& a, int grid, cudaStream_t st) {
-  const cudaError_t e = cudaFuncSetAttribute(weights_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             static_cast<int>(WCfg<D>::kSmem));
+  const cudaError_t e = allow_smem<weights_kernel<D>>(WCfg<D>::kSmem);
   if (e != cudaSuccess) return e;
   const cudaError_t w = launch_after(weights_kernel<D>, grid, kThreads, WCfg<D>::kSmem, st, qmap, kmap, a);
   if (w != cudaSuccess) return w;
@@ -461,8 +460,7 @@ cudaError_t launch(const CUtensorMap& qmap, const CUtensorMap& kmap, const WArgs
 
 }  // namespace
 
-cudaError_t launch_attend_weights(const Shape& s, const AttendArgs& a, cudaStream_t st) {
-  const AtLayout l = attend_layout(s, a.n_q, a.groups, a.pcap, true);
+cudaError_t launch_attend_weights(const Shape& s, const AttendArgs& a, const AtLayout& l, cudaStream_t st) {
   WArgs w{};
   w.I = s.batch * s.n_kv;
   w.n_kv = s.n_kv;
@@ -486,7 +484,7 @@ cudaError_t launch_attend_weights(const Shape& s, const AttendArgs& a, cudaStrea
   if (encode_queries_bf16(&qmap, a.q, s.batch, s.n_kv, w.R, s.d, 1, w.brow) != CUDA_SUCCESS ||
       encode_rows_bf16(&kmap, a.K, static_cast<uint64_t>(w.I) * s.cap, s.d, kAtTile) != CUDA_SUCCESS)
     return cudaErrorInvalidValue;
-  return s.d == 128 ? launch<128>(qmap, kmap, w, attend_sms(), st) : launch<64>(qmap, kmap, w, attend_sms(), st);
+  return s.d == 128 ? launch<128>(qmap, kmap, w, l.sms, st) : launch<64>(qmap, kmap, w, l.sms, st);
 }
 
 }  // namespace bkv

@@ -1,9 +1,26 @@
 // Launches that overlap the kernel before them on the stream.
 #pragma once
 
+#include <atomic>
+
 #include <cuda_runtime.h>
 
 namespace bkv {
+
+// Lets `kernel` use `bytes` of dynamic shared memory, always the same number for one kernel: told to the
+// runtime once per device and kernel (KERNEL makes the note a kernel's own).
+template <auto KERNEL>
+cudaError_t allow_smem(size_t bytes) {
+  static std::atomic<unsigned long long> done{0};
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const unsigned long long bit = dev < 64 ? 1ull << dev : 0;
+  if (bit && (done.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+  e = cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
+  if (e == cudaSuccess) done.fetch_or(bit, std::memory_order_relaxed);
+  return e;
+}
 
 // A kernel launched by launch_after starts while the one before it
 // on the stream still runs, as soon as all of that one's blocks have called grid_dependents_go() (or
