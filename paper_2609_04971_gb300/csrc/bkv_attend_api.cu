@@ -50,6 +50,7 @@ int attend(bkv_ctx* ctx, bkv::AttendArgs& a, double scale) {
   if (!std::isfinite(a.sc) || a.sc < 1.17549435e-38f)
     return fail(ctx, BKV_EINVAL, "scale is out of the range of fp32");
   const bkv::AtLayout l = bkv::attend_layout(s, a.n_q, a.groups, a.pcap, a.weights != nullptr);
+  if (l.too_large) return fail(ctx, BKV_EINVAL, "row blocks times key tiles must be below 2^31");
   if (l.bytes > ctx->attend_ws_bytes)
     return fail(ctx, BKV_ESTATE, "this call needs %zu bytes of workspace, bkv_attend_reserve made %zu", l.bytes,
                 ctx->attend_ws_bytes);

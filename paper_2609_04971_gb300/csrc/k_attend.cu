@@ -15,7 +15,7 @@ namespace bkv {
 namespace {
 
 constexpr int kMergeThreads = 256;
-constexpr int kMergeKeys = 1536;   // keys per block of the weights' part
+constexpr int kMergeKeys = 1024;   // keys per block of the weights' part
 constexpr int kLogitRows = 16;      // rows per instance up to which logits are kept for the weights
 
 size_t align_up(size_t n) { return (n + 255) / 256 * 256; }
@@ -36,7 +36,8 @@ namespace {
 
 // Row blocks of m sequences x R rows: all rows of an instance in one block while there are at most 128
 // of them, else blocks of at most 256, as even as 16-row steps allow.
-AtPlan make_plan(const Shape& s, int I, int m, int R, int n_q, bool causal, int cap, int len_div, int sms) {
+AtPlan make_plan(const Shape& s, int I, int m, int R, int n_q, bool causal, int cap, int len_div, int sms,
+                 bool& too_large) {
   AtPlan p{};
   AtGeo& g = p.geo;
   g.I = I;
@@ -60,8 +61,17 @@ AtPlan make_plan(const Shape& s, int I, int m, int R, int n_q, bool causal, int 
     g.nr = (R + g.rr - 1) / g.rr;
   }
   g.nrb = (m + g.mb - 1) / g.mb * g.nr;
+  g.by_n_kv = FastDiv(g.n_kv);
+  g.by_m = FastDiv(m);
+  g.by_rr = FastDiv(g.rr);
+  g.by_mb = FastDiv(g.mb);
+  g.by_nr = FastDiv(g.nr);
+  g.by_nrb = FastDiv(g.nrb);
+  g.by_n_q = FastDiv(n_q);
+  g.by_len_div = FastDiv(len_div);
   p.items = static_cast<long long>(I) * g.nrb;
   const long long most = p.items * ((cap + kAtTile - 1) / kAtTile);
+  too_large |= most >= (1ll << 31) - sms;
   p.grid = static_cast<int>(most < sms ? most : sms);
   return p;
 }
@@ -75,7 +85,7 @@ size_t place_parts(AtPlan& p, int d, int sms, size_t at) {
   p.off_span = at;
   at = align_up(at + static_cast<size_t>(p.items) * sizeof(int2));
   p.off_cut = at;
-  return align_up(at + static_cast<size_t>(sms) * sizeof(long long));
+  return align_up(at + static_cast<size_t>(sms) * sizeof(int));
 }
 
 struct MergeArgs {
@@ -89,7 +99,7 @@ struct MergeArgs {
   float* lse2;
   const float* logits;
   float* weights;
-  int key_blocks;  // blocks of kMergeKeys keys per instance
+  FastDiv by_row_blocks, by_key_blocks;  // blocks per item, and blocks of kMergeKeys keys per instance
 };
 
 // The run of a row's parts in one source: n of them, `step` segments' rows apart in ml and o.
@@ -99,21 +109,23 @@ struct Run {
   int n, rows;
 };
 
-__device__ __forceinline__ Run make_run(const AtParts& p, int2 span, long long item, int c, int d) {
-  const long long at = (span.x + item) * p.rows + c;
+__device__ __forceinline__ Run make_run(const AtParts& p, int2 span, int item, int c, int d) {
+  const size_t at = static_cast<size_t>(span.x + item) * p.rows + c;
   return {p.ml + at, p.o + at * d, span.y - span.x + 1, p.rows};
 }
 
 // Row r of own instance e in the own caches, and in the prefix.
 __device__ __forceinline__ Run own_run(const MergeArgs& a, int e, int r, int d) {
-  const long long item = static_cast<long long>(e) * a.own.nrb + r / a.own.rr;
-  return make_run(a.own_parts, a.own_parts.span[item], item, r % a.own.rr, d);
+  int rb;
+  const int c = a.own.by_rr.mod(r, rb), item = e * a.own.nrb + rb;
+  return make_run(a.own_parts, a.own_parts.span[item], item, c, d);
 }
 __device__ __forceinline__ Run prefix_run(const MergeArgs& a, int e, int r, int d) {
   const AtGeo& q = a.pre;
-  const int b = e / q.n_kv, bb = b % q.m, pe = b / q.m * q.n_kv + e % q.n_kv;
-  const long long item = static_cast<long long>(pe) * q.nrb + bb / q.mb * q.nr + r / q.rr;
-  return make_run(a.pre_parts, a.pre_parts.span[item], item, bb % q.mb * q.rr + r % q.rr, d);
+  int b, group, bq, rb;
+  const int kv = q.by_n_kv.mod(e, b), bb = q.by_m.mod(b, group), pe = group * q.n_kv + kv;
+  const int bi = q.by_mb.mod(bb, bq), c = q.by_rr.mod(r, rb), item = pe * q.nrb + bq * q.nr + rb;
+  return make_run(a.pre_parts, a.pre_parts.span[item], item, bi * q.rr + c, d);
 }
 
 __device__ __forceinline__ float warp_max(float v) {
@@ -136,17 +148,19 @@ struct Held {
   float2 own, pre;
 };
 __device__ __forceinline__ float held_top(float2 v) { return v.y != 0.f ? v.x : -INFINITY; }
-__device__ __forceinline__ float held_sum(float2 v, float top) { return v.y != 0.f ? v.y * exp2f(v.x - top) : 0.f; }
+__device__ __forceinline__ float held_sum(float2 v, float top) { return v.y != 0.f ? v.y * ex2_approx(v.x - top) : 0.f; }
 
 // log2 of the sum of the parts' l 2^m; -inf when no part saw a key.  The whole warp, a part to a lane;
 // `h` holds the first 32 parts of each run, and `pre` has no parts where there is no prefix.
 __device__ __forceinline__ float merged_lse2(const Held& h, const Run& own, const Run& pre, int lane) {
   const int n = max(own.n, pre.n);
   float top = fmaxf(held_top(h.own), held_top(h.pre));
+#pragma unroll 1
   for (int i = 32 + lane; i - lane < n; i += 32) top = fmaxf(top, fmaxf(held_top(part_ml(own, i)), held_top(part_ml(pre, i))));
   top = warp_max(top);
   if (top == -INFINITY) top = 0.f;
   float sum = held_sum(h.own, top) + held_sum(h.pre, top);
+#pragma unroll 1
   for (int i = 32 + lane; i - lane < n; i += 32) sum += held_sum(part_ml(own, i), top) + held_sum(part_ml(pre, i), top);
   sum = warp_sum(sum);
   return sum == 0.f ? -INFINITY : top + log2f(sum);
@@ -163,11 +177,12 @@ __global__ void __launch_bounds__(kMergeThreads, 4) merge_kernel(MergeArgs a) {
   if (static_cast<int>(blockIdx.x) < a.row_blocks) {
     // kMergeRows rows of an item of the own caches to a block, kRowsPerWarp to a warp: of every item where
     // there is a prefix, else of those that a CTA began and did not finish
-    const int per_item = (g.rr + kMergeRows - 1) / kMergeRows;
-    const int x = blockIdx.x / per_item, c0 = blockIdx.x % per_item * kMergeRows + warp;
-    const long long item = a.has_prefix ? x : a.own_parts.cut[x];
+    int x;
+    const int c0 = a.by_row_blocks.mod(blockIdx.x, x) * kMergeRows + warp;
+    const int item = a.has_prefix ? x : a.own_parts.cut[x];
     if (item < 0) return;
-    const int e = static_cast<int>(item / g.nrb), r0 = static_cast<int>(item % g.nrb) * g.rr;
+    int e;
+    const int r0 = g.by_nrb.mod(item, e) * g.rr;
     Run own[kRowsPerWarp], pre[kRowsPerWarp];
     Held held[kRowsPerWarp];
     float lse2[kRowsPerWarp], o[kRowsPerWarp][kPer] = {};
@@ -188,14 +203,16 @@ __global__ void __launch_bounds__(kMergeThreads, 4) merge_kernel(MergeArgs a) {
     for (int y = 0; y < kRowsPerWarp; ++y) lse2[y] = merged_lse2(held[y], own[y], pre[y], lane);
     // O of the parts, in order: the prefix's, then the own ones
     auto add = [&](const Run(&u)[kRowsPerWarp], int n, bool is_own) {
+#pragma unroll 1
       for (int base = 0; base < n; base += 32) {
         float w[kRowsPerWarp];
 #pragma unroll
         for (int y = 0; y < kRowsPerWarp; ++y) {
           const float2 v = base == 0 ? (is_own ? held[y].own : held[y].pre) : part_ml(u[y], base + lane);
-          w[y] = v.y == 0.f || lse2[y] == -INFINITY ? 0.f : exp2f(v.x - lse2[y]);
+          w[y] = v.y == 0.f || lse2[y] == -INFINITY ? 0.f : ex2_approx(v.x - lse2[y]);
         }
         const int here = min(32, n - base);
+#pragma unroll 1
         for (int i = 0; i < here; i += U) {
           float f[U][kRowsPerWarp][kPer];
 #pragma unroll
@@ -235,8 +252,9 @@ __global__ void __launch_bounds__(kMergeThreads, 4) merge_kernel(MergeArgs a) {
   }
   // ---- weights from the kept logits: one block per instance and run of keys
   __shared__ float lse2_sh[kLogitRows];
-  const int w = blockIdx.x - a.row_blocks;
-  const int e = w / a.key_blocks, j0 = w % a.key_blocks * kMergeKeys;
+  __shared__ int seen_sh[kLogitRows];
+  int e;
+  const int j0 = a.by_key_blocks.mod(blockIdx.x - a.row_blocks, e) * kMergeKeys;
   const int len = at_len(g, e);
   // loads that need no normaliser, under way while it is computed
   constexpr int kKeys = kMergeKeys / kMergeThreads, kAhead = 4;
@@ -251,31 +269,37 @@ __global__ void __launch_bounds__(kMergeThreads, 4) merge_kernel(MergeArgs a) {
       ahead[r][x] = j < g.cap && r < g.R ? __ldcg(y + static_cast<size_t>(r) * g.cap + j) : 0.f;
   }
   if (j0 >= len) return;
+#pragma unroll 1
   for (int r = warp; r < g.R; r += kMergeThreads / 32) {
     const Run own = own_run(a, e, r, D);
     const Run pre = a.has_prefix ? prefix_run(a, e, r, D) : Run{own.ml, own.o, 0, 0};
     const float v = a.has_prefix || own.n > 1 ? merged_lse2({part_ml(own, lane), part_ml(pre, lane)}, own, pre, lane)
                                               : a.lse2[static_cast<size_t>(e) * g.R + r];
-    if (lane == 0) lse2_sh[r] = v;
+    if (lane == 0) {
+      lse2_sh[r] = v;
+      seen_sh[r] = min(len, len - g.n_q + 1 + g.by_n_q.mod(r));
+    }
   }
   __syncthreads();
   float add[kKeys] = {};
-  auto term = [&](int x, int r, float logit) {
-    const int j = j0 + x * kMergeThreads + tid;
-    if (j < min(len, len - g.n_q + 1 + r % g.n_q)) add[x] += exp2f(fmaf(logit, a.sc, -lse2_sh[r]));
-  };
 #pragma unroll
   for (int r = 0; r < kAhead; ++r) {
     if (r < g.R) {
+      const float lse2 = lse2_sh[r];
+      const int seen = seen_sh[r];
 #pragma unroll
-      for (int x = 0; x < kKeys; ++x) term(x, r, ahead[r][x]);
+      for (int x = 0; x < kKeys; ++x)
+        if (j0 + x * kMergeThreads + tid < seen) add[x] += ex2_approx(fmaf(ahead[r][x], a.sc, -lse2));
     }
   }
+#pragma unroll 1
   for (int r = kAhead; r < g.R; ++r) {
+    const float lse2 = lse2_sh[r];
+    const int seen = seen_sh[r];
 #pragma unroll
     for (int x = 0; x < kKeys; ++x) {
       const int j = j0 + x * kMergeThreads + tid;
-      if (j < len) term(x, r, __ldcg(y + static_cast<size_t>(r) * g.cap + j));
+      if (j < seen) add[x] += ex2_approx(fmaf(__ldcg(y + static_cast<size_t>(r) * g.cap + j), a.sc, -lse2));
     }
   }
 #pragma unroll
@@ -291,11 +315,12 @@ AtLayout attend_layout(const Shape& s, int n_q, int groups, int pcap, bool weigh
   AtLayout l;
   const int sms = l.sms = attend_sms();
   const int R = s.G * n_q;
-  l.own = make_plan(s, s.batch * s.n_kv, 1, R, n_q, true, s.cap, 1, sms);
+  l.own = make_plan(s, s.batch * s.n_kv, 1, R, n_q, true, s.cap, 1, sms, l.too_large);
   size_t at = place_parts(l.own, s.d, sms, 0);
   l.has_prefix = groups > 0;
   if (l.has_prefix) {
-    l.prefix = make_plan(s, groups * s.n_kv, s.batch / groups, R, n_q, false, pcap, s.n_kv, sms);
+    l.prefix = make_plan(s, groups * s.n_kv, s.batch / groups, R, n_q, false, pcap, s.n_kv, sms,
+                         l.too_large);
     at = place_parts(l.prefix, s.d, sms, at);
   }
   const size_t rows = static_cast<size_t>(s.batch) * s.n_kv * R;
@@ -308,7 +333,7 @@ AtLayout attend_layout(const Shape& s, int n_q, int groups, int pcap, bool weigh
     l.off_wpart = at;
     at = align_up(at + static_cast<size_t>(2 * sms) * kAtTile * sizeof(float));
     l.off_wu0 = at;
-    at = align_up(at + static_cast<size_t>(weights_items(s) + 1) * sizeof(long long));
+    at = align_up(at + static_cast<size_t>(weights_items(s) + 1) * sizeof(int));
   }
   l.bytes = at;
   return l;
@@ -362,7 +387,9 @@ cudaError_t launch_attend_merge(const Shape& s, const AttendArgs& a, const AtLay
   // Few items are cut into many parts each, of few rows; many items into two or three parts, of many rows.
   const bool many_rows = !l.has_prefix && l.own.items >= l.own.grid;
   const int rows = kMergeThreads / 32 * (many_rows ? 2 : 1);
-  m.row_blocks = static_cast<int>((l.has_prefix ? l.own.items : l.own.grid) * ((l.own.geo.rr + rows - 1) / rows));
+  const int per_item = (l.own.geo.rr + rows - 1) / rows;
+  m.by_row_blocks = FastDiv(per_item);
+  m.row_blocks = static_cast<int>((l.has_prefix ? l.own.items : l.own.grid) * per_item);
   m.sc = a.sc;
   m.o = a.o;
   m.lse = a.lse;
@@ -371,8 +398,9 @@ cudaError_t launch_attend_merge(const Shape& s, const AttendArgs& a, const AtLay
   if (l.logits) {
     m.logits = reinterpret_cast<const float*>(a.ws + l.off_logits);
     m.weights = a.weights;
-    m.key_blocks = (s.cap + kMergeKeys - 1) / kMergeKeys;
-    blocks += static_cast<unsigned>(l.own.geo.I) * m.key_blocks;
+    const int key_blocks = (s.cap + kMergeKeys - 1) / kMergeKeys;
+    m.by_key_blocks = FastDiv(key_blocks);
+    blocks += static_cast<unsigned>(l.own.geo.I) * key_blocks;
   }
   const auto kernel = s.d == 128 ? (many_rows ? merge_kernel<128, 2, 2> : merge_kernel<128, 1, 4>)
                                  : (many_rows ? merge_kernel<64, 2, 2> : merge_kernel<64, 1, 4>);

@@ -22,6 +22,59 @@ constexpr uint32_t kAtBox = 128 * 128;   // [128 rows][64 bf16] swizzled box
 constexpr float kMaxAbove = 32.f;        // log2 of how far p may exceed 1 before its reference moves
 constexpr float kRefFloor = -1e30f;
 
+// mbar_wait in few instructions: the attention kernels wait in many places, and a short kernel pays for
+// the instructions it has to fetch.  Gives up after limit_ns (below 2^32), or once *abort is set.
+__device__ __forceinline__ uint32_t globaltimer_lo() {
+  uint32_t t;
+  asm volatile("mov.u32 %0, %%globaltimer_lo;" : "=r"(t));
+  return t;
+}
+__device__ __forceinline__ bool at_wait_for(uint64_t* bar, uint32_t parity, volatile int* abort, int* err, int code,
+                                            uint32_t limit_ns) {
+  if (mbar_try_wait(bar, parity)) return true;
+  const uint32_t t0 = globaltimer_lo();
+#pragma unroll 1
+  while (!mbar_try_wait_sleep(bar, parity)) {
+    if (abort && *abort) return false;
+    if (globaltimer_lo() - t0 > limit_ns) {
+      if (abort) *abort = 1;
+      record_error(err, code);
+      return false;
+    }
+  }
+  return true;
+}
+constexpr uint32_t kAtWaitNs = static_cast<uint32_t>(kWaitLimitNs);
+__device__ __forceinline__ bool at_wait(uint64_t* bar, uint32_t parity, volatile int* abort, int* err, int code) {
+  return at_wait_for(bar, parity, abort, err, code, kAtWaitNs);
+}
+// The same for a barrier that arrives whatever the abort flag says.
+__device__ __forceinline__ void at_wait_always(uint64_t* bar, uint32_t parity, int* err, int code, int limit_s) {
+  at_wait_for(bar, parity, nullptr, err, code, limit_s * kAtWaitNs);
+}
+
+// Division of numbers below 2^31 by a number fixed on the host.
+struct FastDiv {
+  uint32_t d, mul, shift;
+  FastDiv() = default;
+  explicit FastDiv(uint32_t n) : d(n), mul(0), shift(0) {
+    while ((1ull << shift) < n) ++shift;
+    mul = static_cast<uint32_t>(((1ull << 32) * ((1ull << shift) - n)) / n + 1);
+  }
+  // x / d and x % d
+  __device__ __forceinline__ int div(int x) const {
+    return static_cast<int>((__umulhi(static_cast<uint32_t>(x), mul) + static_cast<uint32_t>(x)) >> shift);
+  }
+  __device__ __forceinline__ int mod(int x, int& quotient) const {
+    quotient = div(x);
+    return x - quotient * static_cast<int>(d);
+  }
+  __device__ __forceinline__ int mod(int x) const {
+    int q;
+    return mod(x, q);
+  }
+};
+
 struct AtGeo {
   int I;          // instances
   int n_kv;       // KV heads: instance e is KV head e % n_kv of sequence group e / n_kv
@@ -33,6 +86,7 @@ struct AtGeo {
   int cap;        // rows allocated per instance
   const int* len; // own: one per instance; prefix: one per sequence group
   int len_div;    // instance e has length len[e / len_div]
+  FastDiv by_n_kv, by_m, by_rr, by_mb, by_nr, by_nrb, by_n_q, by_len_div;
 };
 
 // Rows of a row block and the row it starts at.
@@ -40,11 +94,15 @@ struct AtBlock {
   int b0, r0;
 };
 
-__host__ __device__ inline AtBlock at_block(const AtGeo& g, int rb) { return {rb / g.nr * g.mb, rb % g.nr * g.rr}; }
+__device__ __forceinline__ AtBlock at_block(const AtGeo& g, int rb) {
+  int q;
+  const int r = g.by_nr.mod(rb, q);
+  return {q * g.mb, r * g.rr};
+}
 
 // Instance length; out of range counts as 0 (the caller reports it).
 __device__ __forceinline__ int at_len(const AtGeo& g, int e) {
-  const int n = __ldg(g.len + e / g.len_div);
+  const int n = __ldg(g.len + g.by_len_div.div(e));
   return n >= 0 && n <= g.cap ? n : 0;
 }
 
@@ -52,14 +110,21 @@ __device__ __forceinline__ int at_len(const AtGeo& g, int e) {
 __device__ __forceinline__ int at_limit_max(const AtGeo& g, int len, int r0) {
   if (!g.causal) return len;
   const int r1 = min(g.R, r0 + g.rr) - 1;
-  const int i = r1 / g.n_q > r0 / g.n_q ? g.n_q - 1 : r1 % g.n_q;
+  int h1;
+  const int i1 = g.by_n_q.mod(r1, h1), i = h1 > g.by_n_q.div(r0) ? g.n_q - 1 : i1;
   return max(0, len - g.n_q + 1 + i);
 }
 __device__ __forceinline__ int at_limit_min(const AtGeo& g, int len, int r0) {
   if (!g.causal) return len;
   const int r1 = min(g.R, r0 + g.rr) - 1;
-  const int i = r1 / g.n_q > r0 / g.n_q ? 0 : r0 % g.n_q;
+  int h0;
+  const int i0 = g.by_n_q.mod(r0, h0), i = g.by_n_q.div(r1) > h0 ? 0 : i0;
   return max(0, len - g.n_q + 1 + i);
+}
+
+// Keys that column c of a row block sees.
+__device__ __forceinline__ int at_limit(const AtGeo& g, int len, int r0, int c) {
+  return g.causal ? max(0, len - g.n_q + 1 + g.by_n_q.mod(r0 + g.by_rr.mod(c))) : len;
 }
 
 // Tiles of an item: an item without keys still has one, all masked, that writes its empty rows.
@@ -67,10 +132,11 @@ __device__ __forceinline__ int at_tiles(int limit) { return max(1, (limit + kAtT
 
 // Row of q, o and lse (there are fewer than 2^27) that column c of a row block stands for, or -1.
 __device__ __forceinline__ int at_row(const AtGeo& g, int e, AtBlock blk, int c) {
-  const int bi = c / g.rr, r = blk.r0 + c % g.rr;
+  int bi, group;
+  const int r = blk.r0 + g.by_rr.mod(c, bi), kv = g.by_n_kv.mod(e, group);
   if (bi >= g.mb || blk.b0 + bi >= g.m || r >= g.R) return -1;
-  const int seq = e / g.n_kv * g.m + blk.b0 + bi;
-  return (seq * g.n_kv + e % g.n_kv) * g.R + r;
+  const int seq = group * g.m + blk.b0 + bi;
+  return (seq * g.n_kv + kv) * g.R + r;
 }
 
 // ---------------------------------------------------------------- an even split of a run of units
@@ -82,44 +148,42 @@ struct AtPlace {
 };
 struct AtShare {
   AtPlace at;
-  long long left, u;  // units of this CTA; number of the first one
-  long long per;      // units of a full share
+  int left, u;  // units of this CTA; number of the first one (there are fewer than 2^31 of them)
+  int per;      // units of a full share
 };
 
 template <int THREADS, typename Count, typename Find>
-__device__ __forceinline__ void at_split(int n, Count&& count, Find&& find, long long* scan, AtShare* out) {
+__device__ __forceinline__ void at_split(int n, Count&& count, Find&& find, int* scan, AtShare* out) {
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int chunk = (n + THREADS - 1) / THREADS;
   const int x0 = min(n, tid * chunk), x1 = min(n, x0 + chunk);
-  long long mine = 0;
+  int mine = 0;
+#pragma unroll 1
   for (int x = x0; x < x1; ++x) mine += count(x);
-  long long incl = mine;
+  int incl = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const long long v = __shfl_up_sync(0xffffffffu, incl, o);
+    const int v = __shfl_up_sync(0xffffffffu, incl, o);
     if (lane >= o) incl += v;
   }
   if (lane == 31) scan[warp] = incl;
   __syncthreads();
-  long long before = incl - mine, total = 0;
+  int before = incl - mine, total = 0;
 #pragma unroll
   for (int w = 0; w < THREADS / 32; ++w) {
-    const long long v = scan[w];
+    const int v = scan[w];
     before += w < warp ? v : 0;
     total += v;
   }
-  // 32-bit division where it will do: it is on every CTA's way to its first load
-  const long long per = total + gridDim.x < (1ll << 32)
-                            ? max(1u, (static_cast<uint32_t>(total) + gridDim.x - 1) / gridDim.x)
-                            : (total + gridDim.x - 1) / gridDim.x;
-  const long long u0 = blockIdx.x * per;
-  if (u0 >= total) {
+  const int per = max(1u, (static_cast<uint32_t>(total) + gridDim.x - 1) / gridDim.x);
+  const int u0 = static_cast<int>(min(static_cast<uint32_t>(total), blockIdx.x * static_cast<uint32_t>(per)));
+  if (u0 == total) {
     if (tid == 0) *out = {{0, 0, 0}, 0, u0, per};
   } else if (u0 >= before && u0 < before + mine) {  // the start lies in this thread's groups
-    long long u = before;
-    int x = x0;
+    int u = before, x = x0;
+#pragma unroll 1
     for (;; ++x) {
-      const long long c = count(x);
+      const int c = count(x);
       if (u0 < u + c) break;
       u += c;
     }
@@ -128,32 +192,32 @@ __device__ __forceinline__ void at_split(int n, Count&& count, Find&& find, long
   __syncthreads();
 }
 
-// The split of a source's tiles.
+// The split of a source's tiles: by instances where all row blocks of one have the same tiles, else by
+// row blocks.
 template <int THREADS>
-__device__ __forceinline__ void at_split_tiles(const AtGeo& g, long long* scan, AtShare* out) {
-  if (!g.causal || g.n_q == 1) {  // all row blocks of an instance have the same tiles
-    at_split<THREADS>(
-        g.I, [&](int e) { return static_cast<long long>(g.nrb) * at_tiles(at_len(g, e)); },
-        [&](int e, long long u) {
-          const int n = at_tiles(at_len(g, e));
-          return AtPlace{e, static_cast<int>(u / n), static_cast<int>(u % n)};
-        },
-        scan, out);
-  } else {
-    at_split<THREADS>(
-        g.I * g.nrb,
-        [&](int x) {
-          return static_cast<long long>(at_tiles(at_limit_max(g, at_len(g, x / g.nrb), at_block(g, x % g.nrb).r0)));
-        },
-        [&](int x, long long u) { return AtPlace{x / g.nrb, x % g.nrb, static_cast<int>(u)}; }, scan, out);
-  }
+__device__ __forceinline__ void at_split_tiles(const AtGeo& g, int* scan, AtShare* out) {
+  const bool even = !g.causal || g.n_q == 1;
+  auto tiles = [&](int x) {
+    const int e = even ? x : g.by_nrb.div(x), len = at_len(g, e);
+    return at_tiles(even ? len : at_limit_max(g, len, at_block(g, x - e * g.nrb).r0));
+  };
+  at_split<THREADS>(
+      even ? g.I : g.I * g.nrb, [&](int x) { return tiles(x) * (even ? g.nrb : 1); },
+      [&](int x, int u) {
+        const int n = tiles(x);
+        if (even) return AtPlace{x, u / n, u % n};
+        int e;
+        const int rb = g.by_nrb.mod(x, e);
+        return AtPlace{e, rb, u};
+      },
+      scan, out);
 }
 
 // Reports lengths out of range; by the threads of one CTA.
 template <int THREADS>
 __device__ __forceinline__ void at_check_lengths(const AtGeo& g, int* err) {
   for (int e = threadIdx.x; e < g.I; e += THREADS) {
-    const int n = __ldg(g.len + e / g.len_div);
+    const int n = __ldg(g.len + g.by_len_div.div(e));
     if (n < 0 || n > g.cap) record_error(err, kDevBadLength);
   }
 }
@@ -161,13 +225,12 @@ __device__ __forceinline__ void at_check_lengths(const AtGeo& g, int* err) {
 // One segment of a CTA's run.
 struct AtSeg {
   int e, rb, t0, t1, T, len, r0, b0;
-  long long item, u;  // u: number of tile t0 in the run of all tiles
+  int item, u;  // u: number of tile t0 in the run of all tiles
 };
 
 // Walks the CTA's segments; every role has its own.
 struct AtWalk {
-  int e, rb, t;
-  long long left, u;
+  int e, rb, t, left, u;
   __device__ __forceinline__ bool next(const AtGeo& g, AtSeg& s) {
     if (left <= 0 || e >= g.I) return false;
     const AtBlock blk = at_block(g, rb);
@@ -178,8 +241,8 @@ struct AtWalk {
     s.len = at_len(g, e);
     s.T = at_tiles(at_limit_max(g, s.len, blk.r0));
     s.t0 = t;
-    s.t1 = static_cast<int>(min(static_cast<long long>(s.T), t + left));
-    s.item = static_cast<long long>(e) * g.nrb + rb;
+    s.t1 = min(s.T, t + left);
+    s.item = e * g.nrb + rb;
     s.u = u;
     u += s.t1 - s.t0;
     left -= s.t1 - s.t0;
@@ -208,19 +271,13 @@ struct AtParts {
   float* o = nullptr;           // [segment][N rows][D] sums of p v
   float2* ml = nullptr;         // [segment][N rows] (reference, sum of p), base 2
   int2* span = nullptr;         // [item] first and last CTA that worked on it
-  long long* cut = nullptr;     // [CTA] the item that the CTA began and left to others to finish, or -1
+  int* cut = nullptr;           // [CTA] the item that the CTA began and left to others to finish, or -1
   int rows = 0;                 // rows per segment in o and ml
 };
 
 // What a CTA notes of its segments for the merge; `per` is the number of tiles of a full share.
-__device__ __forceinline__ void at_note(const AtParts& p, const AtSeg& s, bool last_segment, long long per) {
-  if (s.t0 == 0) {
-    // the division is by 32-bit numbers unless there are more than 2^32 tiles
-    const long long u = s.u + s.T - 1;
-    const int last = u < (1ll << 32) ? static_cast<int>(static_cast<uint32_t>(u) / static_cast<uint32_t>(per))
-                                     : static_cast<int>(u / per);
-    p.span[s.item] = make_int2(blockIdx.x, last);
-  }
+__device__ __forceinline__ void at_note(const AtParts& p, const AtSeg& s, bool last_segment, int per) {
+  if (s.t0 == 0) p.span[s.item] = make_int2(blockIdx.x, static_cast<uint32_t>(s.u + s.T - 1) / static_cast<uint32_t>(per));
   if (last_segment) p.cut[blockIdx.x] = s.t0 == 0 && s.t1 < s.T ? s.item : -1;
 }
 
@@ -235,7 +292,7 @@ struct AtPlan {
     p.o = reinterpret_cast<float*>(ws + off_o);
     p.ml = reinterpret_cast<float2*>(ws + off_ml);
     p.span = reinterpret_cast<int2*>(ws + off_span);
-    p.cut = reinterpret_cast<long long*>(ws + off_cut);
+    p.cut = reinterpret_cast<int*>(ws + off_cut);
     p.rows = geo.mb * geo.rr;
     return p;
   }
@@ -250,6 +307,7 @@ struct AtLayout {
   size_t off_logits = 0;   // fp32 [rows][cap]
   size_t off_wpart = 0, off_wu0 = 0;  // weights recomputed from the keys: see k_attend_weights.cu
   size_t bytes = 0;
+  bool too_large = false;  // 2^31 tiles or more
   int sms = 0;             // of the current device: one CTA of the attention kernels each
 };
 // The workspace does not depend on pcap.

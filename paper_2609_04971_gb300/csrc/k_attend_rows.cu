@@ -54,7 +54,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __shared__ __align__(8) uint64_t qfull_bar, qempty_bar, sfull_bar[2], pfull_bar[2], ofull_bar[2], ofree_bar[2], drain_bar;
   __shared__ uint32_t tmem_base_sh;
   __shared__ int abort_sh;
-  __shared__ long long scan_sh[kThreads / 32];
+  __shared__ int scan_sh[kThreads / 32];
   __shared__ AtShare share_sh;
 
   const AtGeo& g = a.geo;
@@ -104,7 +104,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (tid == 0 && share_sh.left == 0) a.parts.cut[blockIdx.x] = -1;
   const uint32_t tmem = tmem_base_sh;
   AtWalk walk{share_sh.at.e, share_sh.at.k, share_sh.at.t, share_sh.left, share_sh.u};
-  const int n_tiles = static_cast<int>(share_sh.left);  // key tiles of this CTA
+  const int n_tiles = share_sh.left;  // key tiles of this CTA
 
   // Ring of stages: K(0), then for each tile i: V(i), K(i + 1).
   if (warp < 4) {
@@ -118,7 +118,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         auto load = [&](const CUtensorMap* map, int row) {
           const int st = pos % C::kStages;
           if (pos >= C::kStages &&
-              !mbar_wait(&empty_bar[st], ((pos / C::kStages) - 1) & 1, abort_flag, a.err, kDevTimeoutProducer)) {
+              !at_wait(&empty_bar[st], ((pos / C::kStages) - 1) & 1, abort_flag, a.err, kDevTimeoutProducer)) {
             ok = false;
             return;
           }
@@ -128,39 +128,42 @@ __global__ void __launch_bounds__(kThreads, 1)
           ++pos;
         };
         auto load_q = [&](const AtSeg& s) {
-          if (n_seg >= 1 && !mbar_wait(&qempty_bar, (n_seg - 1) & 1, abort_flag, a.err, kDevTimeoutProducer)) {
+          if (n_seg >= 1 && !at_wait(&qempty_bar, (n_seg - 1) & 1, abort_flag, a.err, kDevTimeoutProducer)) {
             ok = false;
             return;
           }
           mbar_arrive_expect_tx(&qfull_bar, static_cast<uint32_t>(g.mb * g.rr) * D * 2);
+          int group;
+          const int kv = g.by_n_kv.mod(s.e, group);
           for (int b = 0; b < C::kBoxes; ++b)
-            tma_load_4d(q_smem + b * C::kQBox, &qmap, &qfull_bar, b * 64, s.r0, s.e % g.n_kv, s.e / g.n_kv * g.m + s.b0,
+            tma_load_4d(q_smem + b * C::kQBox, &qmap, &qfull_bar, b * 64, s.r0, kv, group * g.m + s.b0,
                         pol);
           ++n_seg;
         };
         AtSeg s;
-        walk.next(g, s);
-        load_q(s);
-        if (ok) load(&kmap, s.e * g.cap + s.t0 * kAtTile);
-        int t = s.t0;
-        for (int i = 0; ok && i < n_tiles; ++i) {
-          load(&vmap, s.e * g.cap + t * kAtTile);
-          if (ok && i + 1 < n_tiles) {
-            if (++t == s.t1) {
+        int t = 0, v_row = 0;
+        s.t1 = 0;
+        for (int i = 0; ok && i <= n_tiles; ++i) {  // V(i - 1), then K(i) and with a new segment its Q
+          const bool turn = t == s.t1;
+          int k_row = 0;
+          if (i < n_tiles) {
+            if (turn) {
               walk.next(g, s);
               t = s.t0;
-              load(&kmap, s.e * g.cap + t * kAtTile);
-              if (ok) load_q(s);
-            } else {
-              load(&kmap, s.e * g.cap + t * kAtTile);
             }
+            k_row = s.e * g.cap + t * kAtTile;
+            ++t;
           }
+#pragma unroll 1
+          for (int h = 0; ok && h < 2; ++h)
+            if (h == 0 ? i > 0 : i < n_tiles) load(h == 0 ? &vmap : &kmap, h == 0 ? v_row : k_row);
+          if (ok && turn && i < n_tiles) load_q(s);
+          v_row = k_row;
         }
         if (!ok || *abort_flag) {  // let every copy already issued land before the CTA exits
-          int never = 0;
-          if (n_seg > 0) mbar_wait(&qfull_bar, (n_seg - 1) & 1, &never, a.err, kDevTimeoutDrain);
+          if (n_seg > 0) at_wait_always(&qfull_bar, (n_seg - 1) & 1, a.err, kDevTimeoutDrain, 1);
           for (int p = max(0, pos - C::kStages); p < pos; ++p)
-            mbar_wait(&full_bar[p % C::kStages], (p / C::kStages) & 1, &never, a.err, kDevTimeoutDrain);
+            at_wait_always(&full_bar[p % C::kStages], (p / C::kStages) & 1, a.err, kDevTimeoutDrain, 1);
         }
       }
       __syncwarp();
@@ -174,9 +177,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
       bool ok = true;
       auto await = [&](uint64_t* bar, uint32_t parity) {
-        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, a.err, kDevTimeoutMma));
+        if (ok) ok = __all_sync(0xffffffffu, at_wait(bar, parity, abort_flag, a.err, kDevTimeoutMma));
       };
-      auto issue_s = [&](int w, int st) {
+      auto issue_s = [&](int w, int st, bool done, bool last_of_seg) {
         if (!ok) return;
         tc_fence_after();
         const uint64_t q = sdesc_kmajor_sw128(q_addr + w * kAtBox), k = sdesc_kmajor_sw128(kv_addr + st * C::kTileBytes);
@@ -186,10 +189,12 @@ __global__ void __launch_bounds__(kThreads, 1)
             mma_bf16_ss(tm + w * kAtTile, q + (((kk >> 2) * C::kQBox + (kk & 3) * 32) >> 4),
                         k + (((kk >> 2) * kAtBox + (kk & 3) * 32) >> 4), idesc_s, kk > 0);
           mma_commit(&sfull_bar[w]);
+          if (done) mma_commit(&empty_bar[st]);
+          if (done && last_of_seg) mma_commit(&qempty_bar);
         }
         __syncwarp();
       };
-      auto issue_o = [&](int w, int i, int st, int seg, bool first, bool last_of_seg) {
+      auto issue_o = [&](int w, int i, int st, int seg, bool first, bool last_of_seg, bool done) {
         await(&pfull_bar[w], i & 1);
         if (first && seg >= 1) await(&ofree_bar[w], (seg - 1) & 1);
         if (!ok) return;
@@ -200,54 +205,45 @@ __global__ void __launch_bounds__(kThreads, 1)
           for (int kk = 0; kk < kAtTile / 16; ++kk)
             mma_bf16_ts(tm + C::kO + w * D, tm + w * kAtTile + kk * 8, v + kk * (2048 >> 4), idesc_o, !first || kk > 0);
           if (last_of_seg) mma_commit(&ofull_bar[w]);
+          if (done) mma_commit(&empty_bar[st]);
         }
         __syncwarp();
       };
-      auto commit = [&](uint64_t* bar) {
-        if (ok && elect_one()) mma_commit(bar);
-        __syncwarp();
-      };
-      if (n_tiles > 0) {
-        AtSeg s;
-        walk.next(g, s);
-        int t = s.t0, seg = 0;
-        await(&qfull_bar, 0);
-        await(&full_bar[0], 0);
-        issue_s(0, 0);
-        issue_s(1, 0);
-        commit(&empty_bar[0]);
-        if (s.t1 - s.t0 == 1) commit(&qempty_bar);
-        int pos = 1;  // ring position of V(i)
-        for (int i = 0; ok && i < n_tiles; ++i, pos += 2) {
-          const int v_st = pos % C::kStages, k_st = (pos + 1) % C::kStages;
-          const bool last = i + 1 == n_tiles, first = t == s.t0, turn = t + 1 == s.t1;
-          const int seg_o = seg;
-          await(&full_bar[v_st], (pos / C::kStages) & 1);
-          issue_o(0, i, v_st, seg_o, first, turn);
-          if (!last) {
-            ++t;
-            if (turn) {
-              walk.next(g, s);
-              t = s.t0;
-              ++seg;
-              await(&qfull_bar, seg & 1);
-            }
-            await(&full_bar[k_st], ((pos + 1) / C::kStages) & 1);
-            issue_s(0, k_st);
+      AtSeg s;
+      int t = 0, seg = -1;
+      bool o_first = false, o_last = false;  // tile i - 1 begins, ends its segment
+      s.t1 = 0;
+      for (int i = 0; ok && i <= n_tiles; ++i) {  // for each row tile O(i - 1), then S(i)
+        const bool turn = t == s.t1, more = i < n_tiles;
+        const int seg_o = seg, v_pos = 2 * i - 1, k_pos = 2 * i;
+        const int v_st = i > 0 ? v_pos % C::kStages : 0, k_st = k_pos % C::kStages;
+        if (more) {
+          if (turn) {
+            walk.next(g, s);
+            t = s.t0;
+            ++seg;
           }
-          issue_o(1, i, v_st, seg_o, first, turn);
-          commit(&empty_bar[v_st]);
-          if (!last) {
-            issue_s(1, k_st);
-            commit(&empty_bar[k_st]);
-            if (t + 1 == s.t1) commit(&qempty_bar);
+          ++t;
+        }
+        const bool first = o_first, last = o_last, last_s = t == s.t1;
+        o_first = turn;
+        o_last = last_s;
+#pragma unroll 1
+        for (int w = 0; ok && w < 2; ++w) {
+          if (i > 0) {
+            if (w == 0) await(&full_bar[v_st], (v_pos / C::kStages) & 1);
+            issue_o(w, i - 1, v_st, seg_o, first, last, w == 1);
+          }
+          if (more) {
+            if (w == 0 && turn) await(&qfull_bar, seg & 1);
+            if (w == 0) await(&full_bar[k_st], (k_pos / C::kStages) & 1);
+            issue_s(w, k_st, w == 1, last_s);
           }
         }
       }
       if (elect_one()) mma_commit(&drain_bar);  // every MMA issued above has finished once this arrives
       __syncwarp();
-      int never = 0;
-      mbar_wait(&drain_bar, 0, &never, a.err, kDevTimeoutDrain);
+      at_wait_always(&drain_bar, 0, a.err, kDevTimeoutDrain, 1);
       __syncwarp();
     }
   } else {
@@ -260,17 +256,20 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int c = w * kRows + lane_row, cols = g.mb * g.rr;  // row of the block
     const float sc = a.sc;
     auto wait = [&](uint64_t* bar, uint32_t parity) {  // after an abort every wait returns at once
-      if (!mbar_try_wait(bar, parity) && !*abort_flag) mbar_wait(bar, parity, abort_flag, a.err, kDevTimeoutEpilogue);
+      at_wait(bar, parity, abort_flag, a.err, kDevTimeoutEpilogue);
       __syncwarp();
     };
     AtSeg s, next;
     int i = 0;  // tile of the CTA
-    bool more = walk.next(g, next);
-    for (int seg = 0; more; ++seg) {
+    bool more = false;
+    for (int seg = -1;; ++seg) {  // each segment is looked up one ahead
+      const bool have = more;
       s = next;
       more = walk.next(g, next);
+      if (seg < 0) continue;
+      if (!have) break;
       const int row = c < cols ? at_row(g, s.e, {s.b0, s.r0}, c) : -1;
-      const int lim = row < 0 ? 0 : g.causal ? max(0, s.len - g.n_q + 1 + (s.r0 + c % g.rr) % g.n_q) : s.len;
+      const int lim = row < 0 ? 0 : at_limit(g, s.len, s.r0, c);
       const int lim_min = __reduce_min_sync(0xffffffffu, row < 0 ? 0x7fffffff : lim);  // of the warp's rows
       const int limit_max = at_limit_max(g, s.len, s.r0);
       if (tid == 128) at_note(a.parts, s, !more, share_sh.per);
@@ -321,9 +320,11 @@ __global__ void __launch_bounds__(kThreads, 1)
           s0 = add2(s0, s1);
           sum = s0.x + s0.y;
         };
-        weigh(t == s.t0);
-        // a weight above 2^32 shows in the sum, so no maximum is kept
-        if (__any_sync(0xffffffffu, sum > kSumAbove)) {
+#pragma unroll 1
+        for (int pass = 0;; ++pass) {
+          weigh(pass == 0 && t == s.t0);
+          // a weight above 2^32 shows in the sum, so no maximum is kept
+          if (pass > 0 || !__any_sync(0xffffffffu, sum > kSumAbove)) break;
           // Move the references up to the tile's maxima.  The products of the tiles before are complete:
           // the barrier of this tile's S was waited for, and they were issued before it.
           float up = 0.f;
@@ -351,7 +352,6 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
             tmem_wait_st();
           }
-          weigh(false);
         }
         l += sum;
         tmem_st32(s_addr, p);
@@ -360,7 +360,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (w == 0 && k0 + kAtTile > limit_max && k0 + lane_row >= limit_max) {
           // rows of V that no row of the item sees must not hold what 0 times it is not 0
           const int v_pos = 2 * i + 1, st = v_pos % C::kStages;
-          if (!*abort_flag) mbar_wait(&full_bar[st], (v_pos / C::kStages) & 1, abort_flag, a.err, kDevTimeoutEpilogue);
+          at_wait(&full_bar[st], (v_pos / C::kStages) & 1, abort_flag, a.err, kDevTimeoutEpilogue);
 #pragma unroll
           for (int b = 0; b < C::kBoxes; ++b)
 #pragma unroll
@@ -375,7 +375,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       // ---- the segment's result
       const bool final_rows = a.whole_is_final && s.t0 == 0 && s.t1 == s.T;
-      const long long part = blockIdx.x + s.item;
+      const size_t part = blockIdx.x + s.item;
       const bool some = l != 0.f;  // a NaN stays one
       if (row >= 0) {
         if (final_rows) {

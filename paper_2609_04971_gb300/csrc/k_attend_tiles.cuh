@@ -127,7 +127,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
   __shared__ __align__(8) uint64_t ofull_bar[2], ofree_bar[2], vote_bar[2], drain_bar;
   __shared__ uint32_t tmem_base_sh;
   __shared__ int abort_sh;
-  __shared__ long long scan_sh[kAtThreads / 32];
+  __shared__ int scan_sh[kAtThreads / 32];
   __shared__ AtShare share_sh;
   __shared__ __align__(16) float ref_sh[2][N];   // minus the reference of a column, by segment parity
   __shared__ __align__(16) int lim_sh[2][N];
@@ -190,7 +190,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
   if (tid == 0 && share_sh.left == 0) a.parts.cut[blockIdx.x] = -1;
   const uint32_t tmem = tmem_base_sh;
   AtWalk walk{share_sh.at.e, share_sh.at.k, share_sh.at.t, share_sh.left, share_sh.u};
-  const int n_tiles = static_cast<int>(share_sh.left);  // tiles of this CTA (below 2^31)
+  const int n_tiles = share_sh.left;  // tiles of this CTA (below 2^31)
 
   // Ring positions.  Tile i of the CTA: K(0); then for each i: K(i + 1), V(i), but V(i) first where
   // K(i + 1) needs a Q buffer that is still in use (one buffer, next segment) and at the end.
@@ -206,7 +206,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
         auto load = [&](const CUtensorMap* map, int row) {
           const int st = pos % C::kStages;
           if (pos >= C::kStages &&
-              !mbar_wait(&empty_bar[st], ((pos / C::kStages) - 1) & 1, abort_flag, a.err, kDevTimeoutProducer)) {
+              !at_wait(&empty_bar[st], ((pos / C::kStages) - 1) & 1, abort_flag, a.err, kDevTimeoutProducer)) {
             ok = false;
             return;
           }
@@ -218,43 +218,45 @@ __global__ void __launch_bounds__(kAtThreads, 1)
         auto load_q = [&](const AtSeg& s) {
           const int qb = n_seg % C::kQBufs;
           if (n_seg >= C::kQBufs &&
-              !mbar_wait(&qempty_bar[qb], (n_seg / C::kQBufs - 1) & 1, abort_flag, a.err, kDevTimeoutProducer)) {
+              !at_wait(&qempty_bar[qb], (n_seg / C::kQBufs - 1) & 1, abort_flag, a.err, kDevTimeoutProducer)) {
             ok = false;
             return;
           }
           mbar_arrive_expect_tx(&qfull_bar[qb], static_cast<uint32_t>(g.mb * g.rr) * D * 2);
+        int group;
+        const int kv = g.by_n_kv.mod(s.e, group);
           for (int b = 0; b < C::kBoxes; ++b)
-            tma_load_4d(q_smem + qb * C::kQBytes + b * C::kQBox, &qmap, &qfull_bar[qb], b * 64, s.r0, s.e % g.n_kv,
-                        s.e / g.n_kv * g.m + s.b0, pol_q);
+            tma_load_4d(q_smem + qb * C::kQBytes + b * C::kQBox, &qmap, &qfull_bar[qb], b * 64, s.r0, kv, group * g.m + s.b0, pol_q);
           ++n_seg;
         };
         AtSeg s;
-        walk.next(g, s);
-        load_q(s);
-        if (ok) load(&kmap, s.e * g.cap + s.t0 * kAtTile);
-        int t = s.t0;
-        for (int i = 0; ok && i < n_tiles; ++i) {
-          const int v_row = s.e * g.cap + t * kAtTile;
-          const bool last = i + 1 == n_tiles, turn = t + 1 == s.t1;
-          const bool v_first = last || (turn && C::kQBufs == 1);
-          if (v_first) load(&vmap, v_row);
-          if (!last && ok) {
-            ++t;
+        int t = 0, k_row = 0, v_row = 0;
+        s.t1 = 0;
+        for (int i = 0; ok && i <= n_tiles; ++i) {  // K(i) and V(i - 1)
+          const bool turn = t == s.t1;              // tile i begins a segment
+          const bool v_first = turn && C::kQBufs == 1;
+          if (i < n_tiles) {
             if (turn) {
               walk.next(g, s);
               t = s.t0;
-              load_q(s);
             }
-            if (ok) load(&kmap, s.e * g.cap + t * kAtTile);
+            k_row = s.e * g.cap + t * kAtTile;
+            ++t;
           }
-          if (!v_first && ok) load(&vmap, v_row);
+#pragma unroll 1
+          for (int h = 0; ok && h < 2; ++h) {
+            const bool is_k = (h == 0) != v_first;
+            if (is_k ? i == n_tiles : i == 0) continue;
+            if (is_k && turn) load_q(s);
+            if (ok) load(is_k ? &kmap : &vmap, is_k ? k_row : v_row);
+          }
+          v_row = k_row;
         }
         if (!ok || *abort_flag) {  // let every copy already issued land before the CTA exits
-          int never = 0;
           for (int p = max(0, n_seg - C::kQBufs); p < n_seg; ++p)
-            mbar_wait(&qfull_bar[p % C::kQBufs], (p / C::kQBufs) & 1, &never, a.err, kDevTimeoutDrain);
+            at_wait_always(&qfull_bar[p % C::kQBufs], (p / C::kQBufs) & 1, a.err, kDevTimeoutDrain, 1);
           for (int p = max(0, pos - C::kStages); p < pos; ++p)
-            mbar_wait(&full_bar[p % C::kStages], (p / C::kStages) & 1, &never, a.err, kDevTimeoutDrain);
+            at_wait_always(&full_bar[p % C::kStages], (p / C::kStages) & 1, a.err, kDevTimeoutDrain, 1);
         }
       }
       __syncwarp();
@@ -269,7 +271,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
       int pos = 0;
       bool ok = true;
       auto await = [&](uint64_t* bar, uint32_t parity) {
-        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, a.err, kDevTimeoutMma));
+        if (ok) ok = __all_sync(0xffffffffu, at_wait(bar, parity, abort_flag, a.err, kDevTimeoutMma));
       };
       auto issue_s = [&](int i, int seg, bool first, bool last_of_seg) {
         const int st = pos % C::kStages, buf = i & 1, qb = seg % C::kQBufs;
@@ -311,32 +313,37 @@ __global__ void __launch_bounds__(kAtThreads, 1)
         __syncwarp();
         ++pos;
       };
-      if (n_tiles > 0) {
-        AtSeg s;
-        walk.next(g, s);
-        int t = s.t0, seg = 0;
-        issue_s(0, 0, true, s.t1 - s.t0 == 1);
-        for (int i = 0; ok && i < n_tiles; ++i) {
-          const bool last = i + 1 == n_tiles, first = t == s.t0, turn = t + 1 == s.t1;
-          const int seg_o = seg;
-          const bool v_first = last || (turn && C::kQBufs == 1);
-          if (v_first) issue_o(i, seg_o, first, turn);
-          if (!last && ok) {
-            ++t;
-            if (turn) {
-              walk.next(g, s);
-              t = s.t0;
-              ++seg;
-            }
-            issue_s(i + 1, seg, t == s.t0, t + 1 == s.t1);
+      AtSeg s;
+      int t = 0, seg = -1;
+      bool o_first = false, o_last = false;  // tile i - 1 begins, ends its segment
+      s.t1 = 0;
+      for (int i = 0; ok && i <= n_tiles; ++i) {  // S(i) and O(i - 1)
+        const bool turn = t == s.t1;
+        const bool o_before = turn && C::kQBufs == 1;
+        const int seg_o = seg;
+        if (i < n_tiles) {
+          if (turn) {
+            walk.next(g, s);
+            t = s.t0;
+            ++seg;
           }
-          if (!v_first && ok) issue_o(i, seg_o, first, turn);
+          ++t;
+        }
+        const bool first = o_first, last = o_last;
+        o_first = turn;
+        o_last = t == s.t1;
+#pragma unroll 1
+        for (int h = 0; ok && h < 2; ++h) {
+          if ((h == 0) != o_before) {
+            if (i < n_tiles) issue_s(i, seg, turn, t == s.t1);
+          } else if (i > 0) {
+            issue_o(i - 1, seg_o, first, last);
+          }
         }
       }
       if (elect_one()) mma_commit(&drain_bar);  // every MMA issued above has finished once this arrives
       __syncwarp();
-      int never = 0;
-      mbar_wait(&drain_bar, 0, &never, a.err, kDevTimeoutDrain);
+      at_wait_always(&drain_bar, 0, a.err, kDevTimeoutDrain, 1);
       __syncwarp();
     }
   } else {
@@ -354,13 +361,13 @@ __global__ void __launch_bounds__(kAtThreads, 1)
     const bool two_term = U == 1 && cols <= 8;
     const float sc = a.sc;
     auto wait = [&](uint64_t* bar, uint32_t parity) {  // after an abort every wait returns at once
-      if (!mbar_try_wait(bar, parity) && !*abort_flag) mbar_wait(bar, parity, abort_flag, a.err, kDevTimeoutEpilogue);
+      at_wait(bar, parity, abort_flag, a.err, kDevTimeoutEpilogue);
       __syncwarp();
     };
     // A finished segment's O^T is read out after the next segment's first tile: by then its last
     // product is complete.
     int out_seg = -1;
-    long long out_part = 0;
+    size_t out_part = 0;
     bool out_final = false;
     auto read_out = [&] {
       wait(&ofull_bar[out_seg & 1], (out_seg >> 1) & 1);
@@ -402,191 +409,203 @@ __global__ void __launch_bounds__(kAtThreads, 1)
     };
     AtSeg s, next;
     int i = 0;  // tile of the CTA
-    bool more = walk.next(g, next);
-    for (int seg = 0; more; ++seg) {
+    bool more = false;
+    for (int seg = -1;; ++seg) {  // each segment is looked up one ahead
+      const bool have = more;     // after the last one there is only its result to read out
       s = next;
       more = walk.next(g, next);
+      if (seg < 0) continue;
+      if (!have && out_seg < 0) break;
       float* ref = ref_sh[seg & 1] + c0;
       int* lim = lim_sh[seg & 1] + c0;
       int* rows = row_sh[seg & 1] + c0;
-      const int limit_min = at_limit_min(g, s.len, s.r0), limit_max = at_limit_max(g, s.len, s.r0);
-      if (wt < NC) {
+      int limit_min = 0, limit_max = 0, t = 0, t_end = 1;
+      if (have) {
+        limit_min = at_limit_min(g, s.len, s.r0);
+        limit_max = at_limit_max(g, s.len, s.r0);
+        t = s.t0;
+        t_end = s.t1;
+        if (tid == 128) at_note(a.parts, s, !more, share_sh.per);
+      }
+      if (have && wt < NC) {
         const int c = c0 + wt;
         rows[wt] = c < cols ? at_row(g, s.e, {s.b0, s.r0}, c) : -1;
-        lim[wt] = g.causal ? max(0, s.len - g.n_q + 1 + (s.r0 + c % g.rr) % g.n_q) : s.len;
+        lim[wt] = at_limit(g, s.len, s.r0, c);
       }
-      if (tid == 128) at_note(a.parts, s, !more, share_sh.per);
       named_barrier(bar_id, 128);
       float l[NC];
 #pragma unroll
       for (int c = 0; c < NC; ++c) l[c] = 0.f;
-      for (int t = s.t0; t < s.t1; ++t, ++i) {
-        const int buf = i & 1, k0 = t * kAtTile, j = k0 + key_lane;
-        wait(&sfull_bar[buf], (i >> 1) & 1);
-        tc_fence_after();
-        const int pb = i % C::kPBufs;
-        if (active) {
-          float y[NC];
-          // logits to base 2, less the references; masked ones to -inf
-          auto load = [&] {
-            tmem_ld_units<U>(tmem + buf * N + c0 + lane_addr, y);
-            tmem_wait_ld();
-          };
-          auto shift = [&] {
-#pragma unroll
-            for (int c = 0; c < NC; c += 4) {
-              const float4 r = *reinterpret_cast<const float4*>(ref + c);
-              const float2 sc2 = make_float2(sc, sc);
-              const float2 a0 = fma2(make_float2(y[c], y[c + 1]), sc2, make_float2(r.x, r.y));
-              const float2 a1 = fma2(make_float2(y[c + 2], y[c + 3]), sc2, make_float2(r.z, r.w));
-              y[c] = a0.x;
-              y[c + 1] = a0.y;
-              y[c + 2] = a1.x;
-              y[c + 3] = a1.y;
-            }
-            if (k0 + kAtTile > limit_min) {  // some row does not see all keys of the tile
+      for (bool first = true; t < t_end; ++t, first = false) {
+        if (have) {
+          const int buf = i & 1, k0 = t * kAtTile, j = k0 + key_lane;
+          wait(&sfull_bar[buf], (i >> 1) & 1);
+          tc_fence_after();
+          const int pb = i % C::kPBufs;
+          if (active) {
+            float y[NC];
+            // logits to base 2, less the references; masked ones to -inf
+            auto load = [&] {
+              tmem_ld_units<U>(tmem + buf * N + c0 + lane_addr, y);
+              tmem_wait_ld();
+            };
+            auto shift = [&] {
 #pragma unroll
               for (int c = 0; c < NC; c += 4) {
-                const int4 m = *reinterpret_cast<const int4*>(lim + c);
-                y[c] = j < m.x ? y[c] : -INFINITY;
-                y[c + 1] = j < m.y ? y[c + 1] : -INFINITY;
-                y[c + 2] = j < m.z ? y[c + 2] : -INFINITY;
-                y[c + 3] = j < m.w ? y[c + 3] : -INFINITY;
+                const float4 r = *reinterpret_cast<const float4*>(ref + c);
+                const float2 sc2 = make_float2(sc, sc);
+                const float2 a0 = fma2(make_float2(y[c], y[c + 1]), sc2, make_float2(r.x, r.y));
+                const float2 a1 = fma2(make_float2(y[c + 2], y[c + 3]), sc2, make_float2(r.z, r.w));
+                y[c] = a0.x;
+                y[c + 1] = a0.y;
+                y[c + 2] = a1.x;
+                y[c + 3] = a1.y;
               }
-            }
-          };
-          load();
-          if constexpr (U == 1) {
-            // rows of an instance with at most 16 of them are one block: consecutive
-            if (a.logits && j < s.len) {
-              float* dst = a.logits + (static_cast<size_t>(s.e) * g.R + c0) * g.cap + j;
+              if (k0 + kAtTile > limit_min) {  // some row does not see all keys of the tile
 #pragma unroll
-              for (int c = 0; c < NC; ++c)
-                if (c0 + c < cols) dst[static_cast<size_t>(c) * g.cap] = y[c];
-            }
-          }
-          if (t == s.t0) {
-            if (key_lane == 0) {
-#pragma unroll
-              for (int c = 0; c < NC; ++c) ref[c] = k0 < lim[c] ? -fmaxf(y[c] * sc, kRefFloor) : 0.f;
-            }
-            named_barrier(bar_id, 128);
-          }
-          shift();
-          float top0 = y[0], top1 = y[1], top2 = y[2], top3 = y[3];
-#pragma unroll
-          for (int c = 4; c < NC; c += 4) {
-            top0 = fmaxf(top0, y[c]);
-            top1 = fmaxf(top1, y[c + 1]);
-            top2 = fmaxf(top2, y[c + 2]);
-            top3 = fmaxf(top3, y[c + 3]);
-          }
-          // the group's vote is under way while the exponentials are computed
-          const bool high = __any_sync(0xffffffffu, fmaxf(fmaxf(top0, top1), fmaxf(top2, top3)) > kMaxAbove);
-          if (lane == 0) {
-            if (high) *reinterpret_cast<volatile int*>(&high_sh[grp]) = i + 1;
-            mbar_arrive(&vote_bar[grp]);
-          }
-#pragma unroll
-          for (int c = 0; c < NC; ++c) y[c] = ex2_approx(y[c]);
-          // Not given up after an abort: the four warps must agree on the path below, which has barriers,
-          // and each of them arrives after waits that are bounded.
-          if (!mbar_try_wait(&vote_bar[grp], i & 1)) {
-            int never = 0;
-            mbar_wait_for(&vote_bar[grp], i & 1, &never, a.err, kDevTimeoutEpilogue, 10 * kWaitLimitNs);
-          }
-          __syncwarp();
-          if (*reinterpret_cast<volatile int*>(&high_sh[grp]) == i + 1) {
-            // move the references up to the tile's maxima; the logits are still in tensor memory
+                for (int c = 0; c < NC; c += 4) {
+                  const int4 m = *reinterpret_cast<const int4*>(lim + c);
+                  y[c] = j < m.x ? y[c] : -INFINITY;
+                  y[c + 1] = j < m.y ? y[c + 1] : -INFINITY;
+                  y[c + 2] = j < m.z ? y[c + 2] : -INFINITY;
+                  y[c + 3] = j < m.w ? y[c + 3] : -INFINITY;
+                }
+              }
+            };
             load();
-            shift();
+            if constexpr (U == 1) {
+              // rows of an instance with at most 16 of them are one block: consecutive
+              if (a.logits && j < s.len) {
+                float* dst = a.logits + (static_cast<size_t>(s.e) * g.R + c0) * g.cap + j;
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-              float v = y[c];
-#pragma unroll
-              for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
-              if (lane == 0) red_sh[warp - 4][c] = v;
-            }
-            named_barrier(bar_id, 128);
-            if (wt < NC) {
-              float v = 0.f;
-              for (int w = 0; w < 4; ++w) v = fmaxf(v, red_sh[grp * 4 + w][wt]);
-              ref[wt] -= v;
-              fac_sh[c0 + wt] = v;
-            }
-            named_barrier(bar_id, 128);
-#pragma unroll
-            for (int c = 0; c < NC; ++c) {
-              const float v = fac_sh[c0 + c];
-              y[c] = ex2_approx(y[c] - v);
-              l[c] *= ex2_approx(-v);
-            }
-            if (t > s.t0) {  // O^T of the tiles before this one, complete once the last of them is
-              wait(&pfree_bar[(i - 1) % C::kPBufs], ((i - 1) / C::kPBufs) & 1);
-              tc_fence_after();
-              const int units = two_term ? 2 : U;
-#pragma unroll 1
-              for (int u = 0; u < units; ++u) {
-                float o8[8];
-                const uint32_t at = tmem + (2 + (seg & 1)) * N + c0 + u * 8 + lane_addr;
-                tmem_ld8(at, o8);
-                tmem_wait_ld();
-#pragma unroll
-                for (int c = 0; c < 8; ++c) o8[c] *= ex2_approx(-fac_sh[c0 + (two_term ? 0 : u * 8) + c]);
-                tmem_st8(at, o8);
+                for (int c = 0; c < NC; ++c)
+                  if (c0 + c < cols) dst[static_cast<size_t>(c) * g.cap] = y[c];
               }
-              tmem_wait_st();
             }
-            named_barrier(bar_id, 128);  // fac_sh and red_sh may be written again
-          }
-          tc_fence_before();
-          if (lane == 0) mbar_arrive(&sfree_bar[buf]);
-          uint4 packed[U];
-          uint4 low = make_uint4(0, 0, 0, 0);
+            if (t == s.t0) {
+              if (key_lane == 0) {
 #pragma unroll
-          for (int u = 0; u < U; ++u) {
-            const float* p = y + u * 8;
-#pragma unroll
-            for (int c = 0; c < 8; c += 2) {
-              const float2 v = add2(make_float2(l[u * 8 + c], l[u * 8 + c + 1]), make_float2(p[c], p[c + 1]));
-              l[u * 8 + c] = v.x;
-              l[u * 8 + c + 1] = v.y;
+                for (int c = 0; c < NC; ++c) ref[c] = k0 < lim[c] ? -fmaxf(y[c] * sc, kRefFloor) : 0.f;
+              }
+              named_barrier(bar_id, 128);
             }
-            packed[u] = make_uint4(pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]),
-                                   pack_bf16(p[6], p[7]));
+            shift();
+            float top0 = y[0], top1 = y[1], top2 = y[2], top3 = y[3];
+#pragma unroll
+            for (int c = 4; c < NC; c += 4) {
+              top0 = fmaxf(top0, y[c]);
+              top1 = fmaxf(top1, y[c + 1]);
+              top2 = fmaxf(top2, y[c + 2]);
+              top3 = fmaxf(top3, y[c + 3]);
+            }
+            // the group's vote is under way while the exponentials are computed
+            const bool high = __any_sync(0xffffffffu, fmaxf(fmaxf(top0, top1), fmaxf(top2, top3)) > kMaxAbove);
+            if (lane == 0) {
+              if (high) *reinterpret_cast<volatile int*>(&high_sh[grp]) = i + 1;
+              mbar_arrive(&vote_bar[grp]);
+            }
+#pragma unroll
+            for (int c = 0; c < NC; ++c) y[c] = ex2_approx(y[c]);
+            // Not given up after an abort: the four warps must agree on the path below, which has barriers,
+            // and each of them arrives after waits that are bounded.
+            if (!mbar_try_wait(&vote_bar[grp], i & 1)) {
+              at_wait_always(&vote_bar[grp], i & 1, a.err, kDevTimeoutEpilogue, 10);
+            }
+            __syncwarp();
+            if (*reinterpret_cast<volatile int*>(&high_sh[grp]) == i + 1) {
+              // move the references up to the tile's maxima; the logits are still in tensor memory
+              load();
+              shift();
+#pragma unroll
+              for (int c = 0; c < NC; ++c) {
+                float v = y[c];
+#pragma unroll
+                for (int o = 16; o; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+                if (lane == 0) red_sh[warp - 4][c] = v;
+              }
+              named_barrier(bar_id, 128);
+              if (wt < NC) {
+                float v = 0.f;
+                for (int w = 0; w < 4; ++w) v = fmaxf(v, red_sh[grp * 4 + w][wt]);
+                ref[wt] -= v;
+                fac_sh[c0 + wt] = v;
+              }
+              named_barrier(bar_id, 128);
+#pragma unroll
+              for (int c = 0; c < NC; ++c) {
+                const float v = fac_sh[c0 + c];
+                y[c] = ex2_approx(y[c] - v);
+                l[c] *= ex2_approx(-v);
+              }
+              if (t > s.t0) {  // O^T of the tiles before this one, complete once the last of them is
+                wait(&pfree_bar[(i - 1) % C::kPBufs], ((i - 1) / C::kPBufs) & 1);
+                tc_fence_after();
+                const int units = two_term ? 2 : U;
+#pragma unroll 1
+                for (int u = 0; u < units; ++u) {
+                  float o8[8];
+                  const uint32_t at = tmem + (2 + (seg & 1)) * N + c0 + u * 8 + lane_addr;
+                  tmem_ld8(at, o8);
+                  tmem_wait_ld();
+#pragma unroll
+                  for (int c = 0; c < 8; ++c) o8[c] *= ex2_approx(-fac_sh[c0 + (two_term ? 0 : u * 8) + c]);
+                  tmem_st8(at, o8);
+                }
+                tmem_wait_st();
+              }
+              named_barrier(bar_id, 128);  // fac_sh and red_sh may be written again
+            }
+            tc_fence_before();
+            if (lane == 0) mbar_arrive(&sfree_bar[buf]);
+            uint4 packed[U];
+            uint4 low = make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              const float* p = y + u * 8;
+#pragma unroll
+              for (int c = 0; c < 8; c += 2) {
+                const float2 v = add2(make_float2(l[u * 8 + c], l[u * 8 + c + 1]), make_float2(p[c], p[c + 1]));
+                l[u * 8 + c] = v.x;
+                l[u * 8 + c + 1] = v.y;
+              }
+              packed[u] = make_uint4(pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]),
+                                     pack_bf16(p[6], p[7]));
+            }
+            if (two_term)
+              low = make_uint4(pack_rest(packed[0].x, y[0], y[1]), pack_rest(packed[0].y, y[2], y[3]),
+                               pack_rest(packed[0].z, y[4], y[5]), pack_rest(packed[0].w, y[6], y[7]));
+            if (i >= C::kPBufs) wait(&pfree_bar[pb], (i / C::kPBufs - 1) & 1);
+            unsigned char* p_row = p_smem + pb * C::kPBytes + key_lane * 128;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              const int unit = grp * U + u;  // 16-byte unit of the key's row; 8 units to a box
+              *reinterpret_cast<uint4*>(p_row + (unit >> 3) * kAtBox + (((unit ^ key_lane) & 7) * 16)) = packed[u];
+            }
+            if (two_term) *reinterpret_cast<uint4*>(p_row + ((1 ^ key_lane) & 7) * 16) = low;
+          } else if (lane == 0) {
+            mbar_arrive(&sfree_bar[buf]);
           }
-          if (two_term)
-            low = make_uint4(pack_rest(packed[0].x, y[0], y[1]), pack_rest(packed[0].y, y[2], y[3]),
-                             pack_rest(packed[0].z, y[4], y[5]), pack_rest(packed[0].w, y[6], y[7]));
-          if (i >= C::kPBufs) wait(&pfree_bar[pb], (i / C::kPBufs - 1) & 1);
-          unsigned char* p_row = p_smem + pb * C::kPBytes + key_lane * 128;
+          if (grp == 0 && k0 + kAtTile > limit_max && j >= limit_max) {
+            // rows of V that no row of the item sees
+            const bool last = i + 1 == n_tiles, turn = t + 1 == s.t1;
+            const int vpos = 2 * i + (last || (turn && C::kQBufs == 1) ? 1 : 2);
+            const int st = vpos % C::kStages;
+            at_wait(&full_bar[st], (vpos / C::kStages) & 1, abort_flag, a.err, kDevTimeoutEpilogue);
 #pragma unroll
-          for (int u = 0; u < U; ++u) {
-            const int unit = grp * U + u;  // 16-byte unit of the key's row; 8 units to a box
-            *reinterpret_cast<uint4*>(p_row + (unit >> 3) * kAtBox + (((unit ^ key_lane) & 7) * 16)) = packed[u];
+            for (int b = 0; b < C::kBoxes; ++b)
+#pragma unroll
+              for (int x = 0; x < 8; ++x)
+                *reinterpret_cast<uint4*>(kv_smem + st * C::kTileBytes + b * kAtBox + key_lane * 128 + x * 16) =
+                    make_uint4(0, 0, 0, 0);
           }
-          if (two_term) *reinterpret_cast<uint4*>(p_row + ((1 ^ key_lane) & 7) * 16) = low;
-        } else if (lane == 0) {
-          mbar_arrive(&sfree_bar[buf]);
+          fence_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&pfull_bar[pb]);
+          ++i;
         }
-        if (grp == 0 && k0 + kAtTile > limit_max && j >= limit_max) {
-          // rows of V that no row of the item sees
-          const bool last = i + 1 == n_tiles, turn = t + 1 == s.t1;
-          const int vpos = 2 * i + (last || (turn && C::kQBufs == 1) ? 1 : 2);
-          const int st = vpos % C::kStages;
-          if (!*abort_flag) mbar_wait(&full_bar[st], (vpos / C::kStages) & 1, abort_flag, a.err, kDevTimeoutEpilogue);
-#pragma unroll
-          for (int b = 0; b < C::kBoxes; ++b)
-#pragma unroll
-            for (int x = 0; x < 8; ++x)
-              *reinterpret_cast<uint4*>(kv_smem + st * C::kTileBytes + b * kAtBox + key_lane * 128 + x * 16) =
-                  make_uint4(0, 0, 0, 0);
-        }
-        fence_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&pfull_bar[pb]);
-        if (t == s.t0 && out_seg >= 0) read_out();
+        if (first && out_seg >= 0) read_out();
       }
+      if (!have) break;
       // ---- the segment's sums
       out_seg = seg;
       out_final = a.whole_is_final && s.t0 == 0 && s.t1 == s.T;
@@ -612,10 +631,6 @@ __global__ void __launch_bounds__(kAtThreads, 1)
           }
         }
       }
-    }
-    if (out_seg >= 0) {
-      named_barrier(bar_id, 128);
-      read_out();
     }
   }
   tc_fence_before();

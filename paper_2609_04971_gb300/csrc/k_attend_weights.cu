@@ -32,13 +32,14 @@ constexpr uint32_t kTmem = 2 * kCols;
 
 struct WArgs {
   int I, n_kv, G, R, n_q, cap;
+  FastDiv by_n_kv, by_n_q, by_tiles;
   int hp, brow;     // heads per block (1: blocks within a head); rows of a Q box
   const int* len;
   float sc;
   const float* lse2;
   float* weights;
   float* parts;     // [2 grid][128]
-  long long* u0;    // [I * tiles]: number of an item's first unit; [I * tiles]: units per CTA
+  int* u0;          // [I * tiles]: number of an item's first unit; [I * tiles]: units per CTA
   int tiles;        // tiles of the capacity
   int* err;
 };
@@ -58,11 +59,11 @@ __device__ __forceinline__ int w_units(const WArgs& a, int len, int t) {
 
 // Units of the tiles before tile t (at most the tiles in use): whole runs of query blocks for the tiles
 // that every query sees, then one block less from tile to tile.
-__device__ __forceinline__ long long w_units_before(const WArgs& a, int len, int t) {
-  if (a.hp > 1) return static_cast<long long>(t) * ((a.G + a.hp - 1) / a.hp);
+__device__ __forceinline__ int w_units_before(const WArgs& a, int len, int t) {
+  if (a.hp > 1) return t * ((a.G + a.hp - 1) / a.hp);
   const int tiles = (len + kAtTile - 1) / kAtTile;
   const int t1 = len >= a.n_q ? (len - a.n_q) / kAtTile + 1 : 0;
-  const long long full = min(t, t1), m = max(0, t - t1), last = tiles - t1;  // m tiles of last, last - 1, ... blocks
+  const int full = min(t, t1), m = max(0, t - t1), last = tiles - t1;  // m tiles of last, last - 1, ... blocks
   return a.G * (full * ((a.n_q + kCols - 1) / kCols) + m * last - m * (m - 1) / 2);
 }
 
@@ -145,7 +146,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __shared__ __align__(8) uint64_t kfull_bar[2], kempty_bar[2], sfull_bar[2], sfree_bar[2], drain_bar;
   __shared__ uint32_t tmem_base_sh;
   __shared__ int abort_sh;
-  __shared__ long long scan_sh[kThreads / 32];
+  __shared__ int scan_sh[kThreads / 32];
   __shared__ AtShare share_sh;
   __shared__ __align__(16) float lse_sh[kDescs][kCols];
   __shared__ __align__(16) int lim_sh[kDescs][kCols];
@@ -190,7 +191,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int len = w_len(a, e);
         return w_units_before(a, len, (len + kAtTile - 1) / kAtTile);
       },
-      [&](int e, long long u) {
+      [&](int e, int u) {
         const int len = w_len(a, e);
         int lo = 0, hi = (len + kAtTile - 1) / kAtTile - 1;  // the last tile that begins at or before unit u
         while (lo < hi) {
@@ -205,7 +206,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   grid_dependency_wait();  // the normalisers; what came before reads len, q and K only
   const uint32_t tmem = tmem_base_sh;
   const AtShare share = share_sh;
-  const int n_units = static_cast<int>(share.left);
+  const int n_units = share.left;
   if (blockIdx.x == 0 && tid == 0) a.u0[static_cast<size_t>(a.I) * a.tiles] = share.per;
 
   if (warp == 0) {
@@ -222,7 +223,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (i > 0) u.next(a);
         if (i == 0 || u.k == 0) {  // a new tile of keys
           const int kb = n_k & 1;
-          if (n_k >= 2 && !mbar_wait(&kempty_bar[kb], ((n_k >> 1) - 1) & 1, abort_flag, a.err, kDevTimeoutProducer)) break;
+          if (n_k >= 2 && !at_wait(&kempty_bar[kb], ((n_k >> 1) - 1) & 1, abort_flag, a.err, kDevTimeoutProducer)) break;
           mbar_arrive_expect_tx(&kfull_bar[kb], C::kTileBytes);
           for (int b = 0; b < C::kBoxes; ++b)
             tma_load_2d(k_smem + kb * C::kTileBytes + b * kBox, &kmap, &kfull_bar[kb], b * 64, u.e * a.cap + u.t * kAtTile,
@@ -231,21 +232,21 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         const int st = i % C::kStages;
         if (i >= C::kStages &&
-            !mbar_wait(&empty_bar[st], ((i / C::kStages) - 1) & 1, abort_flag, a.err, kDevTimeoutProducer)) {
+            !at_wait(&empty_bar[st], ((i / C::kStages) - 1) & 1, abort_flag, a.err, kDevTimeoutProducer)) {
           ok = false;
           break;
         }
         mbar_arrive_expect_tx(&full_bar[st], static_cast<uint32_t>(a.brow) * D * 2);
+        int b_kv;
+        const int kv = a.by_n_kv.mod(u.e, b_kv);
         for (int b = 0; b < C::kBoxes; ++b)
-          tma_load_4d(q_smem + st * C::kTileBytes + b * kBox, &qmap, &full_bar[st], b * 64, u.r0, u.e % a.n_kv,
-                      u.e / a.n_kv, pol);
+          tma_load_4d(q_smem + st * C::kTileBytes + b * kBox, &qmap, &full_bar[st], b * 64, u.r0, kv, b_kv, pol);
       }
       if (i < n_units || *abort_flag) {  // let every copy already issued land before the CTA exits
-        int never = 0;
         for (int p = max(0, n_k - 2); p < n_k; ++p)
-          mbar_wait(&kfull_bar[p & 1], (p >> 1) & 1, &never, a.err, kDevTimeoutDrain);
+          at_wait_always(&kfull_bar[p & 1], (p >> 1) & 1, a.err, kDevTimeoutDrain, 1);
         for (int p = max(0, i - C::kStages); p < i; ++p)
-          mbar_wait(&full_bar[p % C::kStages], (p / C::kStages) & 1, &never, a.err, kDevTimeoutDrain);
+          at_wait_always(&full_bar[p % C::kStages], (p / C::kStages) & 1, a.err, kDevTimeoutDrain, 1);
       }
     }
     __syncwarp();
@@ -256,7 +257,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
     bool ok = true;
     auto await = [&](uint64_t* bar, uint32_t parity) {
-      if (ok) ok = __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, a.err, kDevTimeoutMma));
+      if (ok) ok = __all_sync(0xffffffffu, at_wait(bar, parity, abort_flag, a.err, kDevTimeoutMma));
     };
     if (n_units > 0) {
       int n_k = 0;
@@ -292,8 +293,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     if (elect_one()) mma_commit(&drain_bar);
     __syncwarp();
-    int never = 0;
-    mbar_wait(&drain_bar, 0, &never, a.err, kDevTimeoutDrain);
+    at_wait_always(&drain_bar, 0, a.err, kDevTimeoutDrain, 1);
     __syncwarp();
   } else if (warp == 2) {
     // ---------------------------------------------------------------- descriptions
@@ -321,7 +321,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (from_start && u.k == 0 && lane == 0) a.u0[static_cast<size_t>(u.e) * a.tiles + u.t] = share.u + i;
         if (i >= kDescs &&
             !__all_sync(0xffffffffu,
-                        mbar_wait(&dempty_bar[x], ((i / kDescs) - 1) & 1, abort_flag, a.err, kDevTimeoutProducer)))
+                        at_wait(&dempty_bar[x], ((i / kDescs) - 1) & 1, abort_flag, a.err, kDevTimeoutProducer)))
           break;
 #pragma unroll
         for (int y = 0; y < kCols / 32; ++y) {
@@ -329,7 +329,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           // a row that sees nothing has -inf, and its columns are masked: any finite number will do
           lse_sh[x][c] = lse[y] == -INFINITY ? 0.f : -lse[y];
           // columns without a row see nothing
-          lim_sh[x][c] = c < u.cols ? u.len - a.n_q + 1 + (a.hp > 1 ? c % a.n_q : u.i0 + c) : 0;
+          lim_sh[x][c] = c < u.cols ? u.len - a.n_q + 1 + (a.hp > 1 ? a.by_n_q.mod(c) : u.i0 + c) : 0;
         }
         if (lane == 0) {
           const bool ends = i + 1 == n_units || u.k + 1 == u.n, whole = from_start && u.k + 1 == u.n;
@@ -357,7 +357,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int c0 = grp * kNC;
     const float sc = a.sc;
     auto wait = [&](uint64_t* bar, uint32_t parity) {  // after an abort every wait returns at once
-      if (!mbar_try_wait(bar, parity) && !*abort_flag) mbar_wait(bar, parity, abort_flag, a.err, kDevTimeoutEpilogue);
+      at_wait(bar, parity, abort_flag, a.err, kDevTimeoutEpilogue);
       __syncwarp();
     };
     float acc = 0.f;
@@ -436,11 +436,12 @@ __global__ void __launch_bounds__(kThreads, 1)
 // Parts of split items, in order: one thread per key.
 __global__ void __launch_bounds__(kAtTile) weights_merge_kernel(WArgs a) {
   grid_dependency_wait();
-  const int t = blockIdx.x % a.tiles, e = blockIdx.x / a.tiles;
+  int e;
+  const int t = a.by_tiles.mod(blockIdx.x, e);
   const int len = w_len(a, e), n = w_units(a, len, t);
   if (n == 0) return;
-  const long long per = a.u0[static_cast<size_t>(a.I) * a.tiles], u = a.u0[static_cast<size_t>(e) * a.tiles + t];
-  const int first = static_cast<int>(u / per), last = static_cast<int>((u + n - 1) / per);
+  const uint32_t per = a.u0[static_cast<size_t>(a.I) * a.tiles], u = a.u0[static_cast<size_t>(e) * a.tiles + t];
+  const int first = u / per, last = (u + n - 1) / per;
   const int j = t * kAtTile + threadIdx.x;
   if (first == last || j >= len) return;
   float sum = 0.f;
@@ -477,9 +478,12 @@ cudaError_t launch_attend_weights(const Shape& s, const AttendArgs& a, const AtL
   w.lse2 = reinterpret_cast<const float*>(a.ws + l.off_lse2);
   w.weights = a.weights;
   w.parts = reinterpret_cast<float*>(a.ws + l.off_wpart);
-  w.u0 = reinterpret_cast<long long*>(a.ws + l.off_wu0);
+  w.u0 = reinterpret_cast<int*>(a.ws + l.off_wu0);
   w.tiles = (s.cap + kAtTile - 1) / kAtTile;
   w.err = a.err;
+  w.by_n_kv = FastDiv(w.n_kv);
+  w.by_n_q = FastDiv(w.n_q);
+  w.by_tiles = FastDiv(w.tiles);
   CUtensorMap qmap, kmap;
   if (encode_queries_bf16(&qmap, a.q, s.batch, s.n_kv, w.R, s.d, 1, w.brow) != CUDA_SUCCESS ||
       encode_rows_bf16(&kmap, a.K, static_cast<uint64_t>(w.I) * s.cap, s.d, kAtTile) != CUDA_SUCCESS)
