@@ -168,13 +168,15 @@ __device__ __forceinline__ void at_split(int n, Count&& count, Find&& find, int*
   }
   if (lane == 31) scan[warp] = incl;
   __syncthreads();
-  int before = incl - mine, total = 0;
+  constexpr int kWarps = THREADS / 32;
+  int w = lane < kWarps ? scan[lane] : 0;  // every warp scans the warps' totals
 #pragma unroll
-  for (int w = 0; w < THREADS / 32; ++w) {
-    const int v = scan[w];
-    before += w < warp ? v : 0;
-    total += v;
+  for (int o = 1; o < kWarps; o <<= 1) {
+    const int v = __shfl_up_sync(0xffffffffu, w, o);
+    if (lane >= o) w += v;
   }
+  const int total = __shfl_sync(0xffffffffu, w, kWarps - 1);
+  const int before = __shfl_sync(0xffffffffu, w, warp) - __shfl_sync(0xffffffffu, incl, 31) + incl - mine;
   const int per = max(1u, (static_cast<uint32_t>(total) + gridDim.x - 1) / gridDim.x);
   const int u0 = static_cast<int>(min(static_cast<uint32_t>(total), blockIdx.x * static_cast<uint32_t>(per)));
   if (u0 == total) {

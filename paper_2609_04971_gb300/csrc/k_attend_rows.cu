@@ -27,7 +27,7 @@ namespace bkv {
 namespace {
 
 constexpr int kThreads = 384;  // producer, MMA, two idle warps; two groups of four
-constexpr int kRegsFew = 72, kRegsMany = 216;  // 72 + 2 x 216 of the 3 x 168 per scheduler at launch
+constexpr int kRegsFew = 88, kRegsMany = 208;  // 88 + 2 x 208 of the 3 x 168 per scheduler at launch
 constexpr int kRows = 128;     // rows of a row tile
 constexpr float kSumAbove = 4294967296.f;  // 2^kMaxAbove
 
@@ -228,8 +228,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         const bool first = o_first, last = o_last, last_s = t == s.t1;
         o_first = turn;
         o_last = last_s;
-#pragma unroll 1
-        for (int w = 0; ok && w < 2; ++w) {
+#pragma unroll
+        for (int w = 0; w < 2; ++w) {
           if (i > 0) {
             if (w == 0) await(&full_bar[v_st], (v_pos / C::kStages) & 1);
             issue_o(w, i - 1, v_st, seg_o, first, last, w == 1);

@@ -36,9 +36,9 @@ namespace {
 
 constexpr int kSmWarps = 8;
 constexpr int kAtThreads = 32 * (4 + kSmWarps);
-// Registers: 168 a thread at launch; the first four warps give back what the softmax warps take, 72 + 2 x 216
+// Registers: 168 a thread at launch; the first four warps give back what the softmax warps take, 88 + 2 x 208
 // of 3 x 168 per scheduler.
-constexpr int kRegsFew = 72, kRegsMany = 216;
+constexpr int kRegsFew = 88, kRegsMany = 208;
 constexpr int kAtMaxStages = 12;
 constexpr size_t kAtSmem = 218 * 1024;       // dynamic shared memory, next to up to 8 KB of static
 

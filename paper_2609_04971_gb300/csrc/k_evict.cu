@@ -2,8 +2,9 @@
 // compaction of K, V and the weights.
 //
 // Selection, one CTA per instance.  Each warp owns a contiguous run of rows, 32 at
-// a time across its lanes, and holds their keys in registers.  A three-pass radix
-// select (digits of 12, 10 and 10 bits from the top, one shared histogram) finds the
+// a time across its lanes; the keys stay in shared memory (in registers the passes
+// would have to be unrolled, and a short kernel pays for every instruction that it
+// fetches).  A three-pass radix select (digits of 12, 10 and 10 bits from the top, one shared histogram) finds the
 // key T of the last row that is kept by weight and how many rows equal to T are needed.
 // A 12-bit first digit splits an octave into 8 bins: weights that span a few octaves,
 // as softmax sums do, then spread over enough bins that the histogram's atomics seldom
@@ -46,61 +47,57 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* wsum, uint3
   }
   if (lane == 31) wsum[warp] = incl;
   __syncthreads();
-  uint32_t before = 0, all = 0;
+  uint32_t w = lane < kWarps ? wsum[lane] : 0;  // every warp scans the warps' totals
 #pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
-    const uint32_t c = wsum[w];
-    before += w < warp ? c : 0;
-    all += c;
+  for (int o = 1; o < kWarps; o <<= 1) {
+    const uint32_t n = __shfl_up_sync(0xffffffffu, w, o);
+    if (lane >= o) w += n;
   }
-  total = all;
+  total = __shfl_sync(0xffffffffu, w, kWarps - 1);
+  const uint32_t upto = __shfl_sync(0xffffffffu, w, warp);  // this warp's total among them
+  const uint32_t before = upto - __shfl_sync(0xffffffffu, incl, 31);
   __syncthreads();  // wsum may be written again
   return before + incl - v;
 }
 
-// A load that a false predicate skips, without the branch that would keep the next load from starting.
-__device__ __forceinline__ float load_if(const float* p, bool yes) {
-  float v;
-  asm volatile(
-      "{\n\t.reg .pred q;\n\t"
-      "setp.ne.u32 q, %2, 0;\n\t"
-      "mov.f32 %0, 0f00000000;\n\t"
-      "@q ld.global.f32 %0, [%1];\n\t}"
-      : "=f"(v)
-      : "l"(p), "r"(static_cast<uint32_t>(yes))
-      : "memory");
-  return v;
-}
-
-// The rows of one warp: row0 + 32 i + lane for i < n, and their keys.
-template <int KPT>
+// The rows of one warp: row0 + 32 i + lane for i < n, and their keys in shared memory.
 struct WarpRows {
-  uint32_t key[KPT];
-  int row0, n, lane;
-  __device__ __forceinline__ void init(const float* w, int L) {
-    float v[KPT];
+  uint32_t* key;
+  int row0, n, lane, L;
+  __device__ __forceinline__ void init(const float* w) {
+    constexpr int kBatch = 8;  // loads under way
+#pragma unroll 1
+    for (int i0 = 0; i0 < n; i0 += kBatch) {
+      float v[kBatch];
 #pragma unroll
-    for (int i = 0; i < KPT; ++i) {
-      const int j = row0 + i * 32 + lane;
-      v[i] = load_if(w + j, i < n && j < L);
+      for (int u = 0; u < kBatch; ++u) {
+        const int j = row0 + (i0 + u) * 32 + lane;
+        v[u] = j < L ? w[j] : 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        const int j = row0 + (i0 + u) * 32 + lane;
+        if (i0 + u < n && j < L) key[j] = weight_key(v[u]);
+      }
     }
-#pragma unroll
-    for (int i = 0; i < KPT; ++i) key[i] = weight_key(v[i]);
+    __syncwarp();
   }
   // f(row, key) for every i, also where the row is not below L (every lane takes part).
   template <typename F>
   __device__ __forceinline__ void each(F&& f) const {
-#pragma unroll
-    for (int i = 0; i < KPT; ++i)
-      if (i < n) f(row0 + i * 32 + lane, key[i]);
+#pragma unroll 2
+    for (int i = 0; i < n; ++i) {
+      const int j = row0 + i * 32 + lane;
+      f(j, j < L ? key[j] : 0u);
+    }
   }
 };
 
 // One digit of the radix select: among the candidates [c_lo, c_hi) that match `prefix` under `mask`,
 // finds the digit that holds the k-th largest (k >= 1, at most the number of matches) and what is left
 // of k inside it.  Called by the whole block; the result is the same in every thread.
-template <int THREADS, int KPT, int BITS>
-__device__ __forceinline__ void select_digit(const WarpRows<KPT>& rows, int c_lo, int c_hi, int shift, uint32_t& prefix,
+template <int THREADS, int BITS>
+__device__ __forceinline__ void select_digit(const WarpRows& rows, int c_lo, int c_hi, int shift, uint32_t& prefix,
                                              uint32_t& mask, uint32_t& k, uint32_t* hist, uint32_t* wsum,
                                              uint32_t* found) {
   constexpr int kBins = 1 << BITS;
@@ -142,10 +139,11 @@ __device__ __forceinline__ void select_digit(const WarpRows<KPT>& rows, int c_lo
   __syncthreads();
 }
 
-// Selection: kept, len_out, into other buffers the zeros of weights_out, and in `plan` the number of kept rows (-1 for
-// a length out of range) and the first of them that has to move.  At most KPT * THREADS rows.
-template <int THREADS, int KPT, int MINB>
-__global__ void __launch_bounds__(THREADS, MINB) evict_select_kernel(Shape s, EvictArgs a) {
+// Selection: kept, len_out, into other buffers the zeros of weights_out, and in `plan` the number of kept
+// rows (-1 for a length out of range) and the first of them that has to move.
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS, 2048 / THREADS) evict_select_kernel(Shape s, EvictArgs a) {
+  extern __shared__ uint32_t keys[];  // [cap]
   constexpr int kWarps = THREADS / 32;
   __shared__ __align__(16) uint32_t hist[kEvBins];
   __shared__ uint32_t wsum[kWarps], found[2];
@@ -171,11 +169,13 @@ __global__ void __launch_bounds__(THREADS, MINB) evict_select_kernel(Shape s, Ev
   float* w_out = a.weights_out + static_cast<size_t>(e) * a.cap_out;
   const int n_keep = min(L, a.budget);
 
-  WarpRows<KPT> rows;
+  WarpRows rows;
+  rows.key = keys;
+  rows.L = L;
   rows.n = (L + kWarps * 32 - 1) / (kWarps * 32);
   rows.row0 = warp * rows.n * 32;
   rows.lane = lane;
-  rows.init(w_in, L);
+  rows.init(w_in);
   if (tid == 0) first_sh = n_keep;
   uint32_t T = 0, ties = 0;
   const int c_lo = s.n_prefix, c_hi = L - s.W;
@@ -183,9 +183,9 @@ __global__ void __launch_bounds__(THREADS, MINB) evict_select_kernel(Shape s, Ev
   const int k_sel = a.budget - s.n_prefix - s.W;
   if (!all && k_sel > 0) {
     uint32_t prefix = 0, mask = 0, k = static_cast<uint32_t>(k_sel);
-    select_digit<THREADS, KPT, 12>(rows, c_lo, c_hi, 20, prefix, mask, k, hist, wsum, found);
-    select_digit<THREADS, KPT, 10>(rows, c_lo, c_hi, 10, prefix, mask, k, hist, wsum, found);
-    select_digit<THREADS, KPT, 10>(rows, c_lo, c_hi, 0, prefix, mask, k, hist, wsum, found);
+    select_digit<THREADS, 12>(rows, c_lo, c_hi, 20, prefix, mask, k, hist, wsum, found);
+    select_digit<THREADS, 10>(rows, c_lo, c_hi, 10, prefix, mask, k, hist, wsum, found);
+    select_digit<THREADS, 10>(rows, c_lo, c_hi, 0, prefix, mask, k, hist, wsum, found);
     T = prefix;
     ties = k;
   }
@@ -210,6 +210,7 @@ __global__ void __launch_bounds__(THREADS, MINB) evict_select_kernel(Shape s, Ev
   }
   __syncthreads();
   uint32_t tie_at = 0, at = 0;
+#pragma unroll 1
   for (int v = 0; v < warp; ++v) {
     const uint32_t t = w_tie[v];
     at += w_keep[v] + min(t, ties > tie_at ? ties - tie_at : 0u);
@@ -347,17 +348,21 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(Shape s, Evict
   if (mine) a.weights_out[static_cast<size_t>(e) * a.cap_out + i0 + tid] = w;
 }
 
+// More threads for more rows: 8 to 32 rows to a thread at the ends of each range.
+template <int THREADS>
+cudaError_t select(const Shape& s, const EvictArgs& a, cudaStream_t st) {
+  const size_t smem = sizeof(uint32_t) * s.cap;
+  if (smem > 40 * 1024) {  // with the static 17 KB past what needs no opt-in
+    const cudaError_t e = allow_smem<evict_select_kernel<THREADS>>(sizeof(uint32_t) * kMaxCapacity);
+    if (e != cudaSuccess) return e;
+  }
+  evict_select_kernel<THREADS><<<s.n_inst, THREADS, smem, st>>>(s, a);
+  return cudaGetLastError();
+}
+
 template <int D>
 cudaError_t launch_d(const Shape& s, const EvictArgs& a, cudaStream_t st) {
-  // threads by the rows that the registers of a CTA have to hold
-  if (s.cap <= 256 * 8)
-    evict_select_kernel<256, 8, 5><<<s.n_inst, 256, 0, st>>>(s, a);
-  else if (s.cap <= 512 * 20)
-    evict_select_kernel<512, 20, 2><<<s.n_inst, 512, 0, st>>>(s, a);
-  else
-    evict_select_kernel<1024, 32, 1><<<s.n_inst, 1024, 0, st>>>(s, a);
-  static_assert(kMaxCapacity <= 1024 * 32, "rows of the largest capacity in registers");
-  const cudaError_t e = cudaGetLastError();
+  const cudaError_t e = s.cap <= 2048 ? select<256>(s, a, st) : s.cap <= 10240 ? select<512>(s, a, st) : select<1024>(s, a, st);
   if (e != cudaSuccess) return e;
   if (a.K_out == a.K) return launch_after(evict_move_in_place_kernel<D>, s.n_inst, 512, 0, st, s, a);
   const int kept = a.budget < s.cap ? a.budget : s.cap, chunks = (kept + kMoveRows - 1) / kMoveRows;
