@@ -14,7 +14,7 @@
 namespace bkv {
 namespace {
 
-constexpr int kMergeThreads = 256;
+constexpr int kMergeThreads = 256, kMergeRows = kMergeThreads / 32;  // rows per block
 constexpr int kMergeKeys = 1024;   // keys per block of the weights' part
 constexpr int kLogitRows = 16;      // rows per instance up to which logits are kept for the weights
 
@@ -85,7 +85,7 @@ size_t place_parts(AtPlan& p, int d, int sms, size_t at) {
   p.off_span = at;
   at = align_up(at + static_cast<size_t>(p.items) * sizeof(int2));
   p.off_cut = at;
-  return align_up(at + static_cast<size_t>(sms) * sizeof(int));
+  return align_up(at + static_cast<size_t>(sms) * sizeof(int2));
 }
 
 struct MergeArgs {
@@ -114,13 +114,9 @@ __device__ __forceinline__ Run make_run(const AtParts& p, int2 span, int item, i
   return {p.ml + at, p.o + at * d, span.y - span.x + 1, p.rows};
 }
 
-// Row r of own instance e in the own caches, and in the prefix.
-__device__ __forceinline__ Run own_run(const MergeArgs& a, int e, int r, int d) {
-  int rb;
-  const int c = a.own.by_rr.mod(r, rb), item = e * a.own.nrb + rb;
-  return make_run(a.own_parts, a.own_parts.span[item], item, c, d);
-}
+// Row r of own instance e in the prefix; no parts where there is none.
 __device__ __forceinline__ Run prefix_run(const MergeArgs& a, int e, int r, int d) {
+  if (!a.has_prefix) return {nullptr, nullptr, 0, 0};
   const AtGeo& q = a.pre;
   int b, group, bq, rb;
   const int kv = q.by_n_kv.mod(e, b), bb = q.by_m.mod(b, group), pe = group * q.n_kv + kv;
@@ -139,114 +135,87 @@ __device__ __forceinline__ float warp_sum(float v) {
   return v;
 }
 
-__device__ __forceinline__ float2 part_ml(const Run& u, int i) {
-  return i < u.n ? __ldcg(u.ml + static_cast<size_t>(i) * u.rows) : make_float2(0.f, 0.f);
+// Part i of a row, counting the prefix's parts first: its (reference, sum of p); l = 0 past the last.
+__device__ __forceinline__ float2 part_ml(const Run& pre, const Run& own, int i) {
+  const float2* at = i < pre.n ? pre.ml + static_cast<size_t>(i) * pre.rows : own.ml + static_cast<size_t>(i - pre.n) * own.rows;
+  return i < pre.n + own.n ? __ldcg(at) : make_float2(0.f, 0.f);
 }
 
-// Parts of a row that a lane holds: part `lane` of its run in each source; l = 0 stands for none.
-struct Held {
-  float2 own, pre;
-};
-__device__ __forceinline__ float held_top(float2 v) { return v.y != 0.f ? v.x : -INFINITY; }
-__device__ __forceinline__ float held_sum(float2 v, float top) { return v.y != 0.f ? v.y * ex2_approx(v.x - top) : 0.f; }
-
-// log2 of the sum of the parts' l 2^m; -inf when no part saw a key.  The whole warp, a part to a lane;
-// `h` holds the first 32 parts of each run, and `pre` has no parts where there is no prefix.
-__device__ __forceinline__ float merged_lse2(const Held& h, const Run& own, const Run& pre, int lane) {
-  const int n = max(own.n, pre.n);
-  float top = fmaxf(held_top(h.own), held_top(h.pre));
+// log2 of the sum of the parts' l 2^m; -inf when no part saw a key.  The whole warp; `mine` is part
+// `lane`, the parts past the 32nd are read here.
+__device__ __noinline__ float merged_lse2(Run pre, Run own, float2 mine, int lane) {
+  const int n = pre.n + own.n;
+  float top = mine.y != 0.f ? mine.x : -INFINITY;
 #pragma unroll 1
-  for (int i = 32 + lane; i - lane < n; i += 32) top = fmaxf(top, fmaxf(held_top(part_ml(own, i)), held_top(part_ml(pre, i))));
+  for (int i = 32 + lane; i - lane < n; i += 32) {
+    const float2 v = part_ml(pre, own, i);
+    if (v.y != 0.f) top = fmaxf(top, v.x);
+  }
   top = warp_max(top);
   if (top == -INFINITY) top = 0.f;
-  float sum = held_sum(h.own, top) + held_sum(h.pre, top);
+  float sum = mine.y != 0.f ? mine.y * ex2_approx(mine.x - top) : 0.f;
 #pragma unroll 1
-  for (int i = 32 + lane; i - lane < n; i += 32) sum += held_sum(part_ml(own, i), top) + held_sum(part_ml(pre, i), top);
+  for (int i = 32 + lane; i - lane < n; i += 32) {
+    const float2 v = part_ml(pre, own, i);
+    if (v.y != 0.f) sum += v.y * ex2_approx(v.x - top);
+  }
   sum = warp_sum(sum);
   return sum == 0.f ? -INFINITY : top + log2f(sum);
 }
 
-// RPW rows to a warp, U parts of each under way at a time.
-template <int D, int RPW, int U>
-__global__ void __launch_bounds__(kMergeThreads, 4) merge_kernel(MergeArgs a) {
-  constexpr int kPer = D / 32, kRowsPerWarp = RPW, kMergeRows = kMergeThreads / 32 * RPW;
+// U parts of O under way at a time, MINB blocks to an SM.
+template <int D, int U, int MINB>
+__global__ void __launch_bounds__(kMergeThreads, MINB) merge_kernel(MergeArgs a) {
+  constexpr int kPer = D / 32;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const AtGeo& g = a.own;
   grid_dependents_go();
   grid_dependency_wait();
   if (static_cast<int>(blockIdx.x) < a.row_blocks) {
-    // kMergeRows rows of an item of the own caches to a block, kRowsPerWarp to a warp: of every item where
-    // there is a prefix, else of those that a CTA began and did not finish
+    // kMergeRows rows of an item of the own caches to a block, one to a warp: of every item where there is a
+    // prefix, else of those that a CTA began and did not finish
     int x;
-    const int c0 = a.by_row_blocks.mod(blockIdx.x, x) * kMergeRows + warp;
-    const int item = a.has_prefix ? x : a.own_parts.cut[x];
-    if (item < 0) return;
+    const int c = a.by_row_blocks.mod(blockIdx.x, x) * kMergeRows + warp;
+    const int2 cut = a.has_prefix ? make_int2(x, 0) : a.own_parts.cut[x];
+    if (cut.x < 0) return;
     int e;
-    const int r0 = g.by_nrb.mod(item, e) * g.rr;
-    Run own[kRowsPerWarp], pre[kRowsPerWarp];
-    Held held[kRowsPerWarp];
-    float lse2[kRowsPerWarp], o[kRowsPerWarp][kPer] = {};
-    int row[kRowsPerWarp], n_own = 0, n_pre = 0;
+    const int r = g.by_nrb.mod(cut.x, e) * g.rr + c;
+    if (c >= g.rr || r >= g.R) return;
+    const Run own = make_run(a.own_parts, a.has_prefix ? a.own_parts.span[x] : make_int2(x, cut.y), cut.x, c, D);
+    const Run pre = prefix_run(a, e, r, D);
+    const int n = pre.n + own.n;
+    float2 mine = part_ml(pre, own, lane);
+    const float lse2 = merged_lse2(pre, own, mine, lane);
+    float o[kPer] = {};
+#pragma unroll 1
+    for (int base = 0; base < n; base += 32) {
+      if (base > 0) mine = part_ml(pre, own, base + lane);
+      const float w = mine.y == 0.f || lse2 == -INFINITY ? 0.f : ex2_approx(mine.x - lse2);
+#pragma unroll 1
+      for (int i = base; i < min(n, base + 32); i += U) {
+        float f[U][kPer];
 #pragma unroll
-    for (int y = 0; y < kRowsPerWarp; ++y) {  // the rows' loads are under way together
-      const int c = c0 + y * (kMergeThreads / 32), r = r0 + c;
-      const bool there = c < g.rr && r < g.R;
-      row[y] = there ? e * g.R + r : -1;
-      own[y] = own_run(a, e, there ? r : r0, D);
-      if (a.has_prefix) pre[y] = prefix_run(a, e, there ? r : r0, D);
-      else pre[y] = Run{own[y].ml, own[y].o, 0, 0};
-      held[y] = {part_ml(own[y], lane), part_ml(pre[y], lane)};
-      n_own = max(n_own, own[y].n);
-      n_pre = max(n_pre, pre[y].n);
+        for (int y = 0; y < U; ++y) {
+          const int j = i + y;
+          const float* src = lane + (j < pre.n ? pre.o + static_cast<size_t>(j) * pre.rows * D
+                                               : own.o + static_cast<size_t>(j - pre.n) * own.rows * D);
+#pragma unroll
+          for (int z = 0; z < kPer; ++z) f[y][z] = j < n ? __ldcg(src + z * 32) : 0.f;
+        }
+#pragma unroll
+        for (int y = 0; y < U; ++y) {
+          const float wi = __shfl_sync(0xffffffffu, w, (i + y) & 31);
+#pragma unroll
+          for (int z = 0; z < kPer; ++z) o[z] = i + y < n && wi != 0.f ? fmaf(f[y][z], wi, o[z]) : o[z];
+        }
+      }
     }
+    const size_t row = static_cast<size_t>(e) * g.R + r;
 #pragma unroll
-    for (int y = 0; y < kRowsPerWarp; ++y) lse2[y] = merged_lse2(held[y], own[y], pre[y], lane);
-    // O of the parts, in order: the prefix's, then the own ones
-    auto add = [&](const Run(&u)[kRowsPerWarp], int n, bool is_own) {
-#pragma unroll 1
-      for (int base = 0; base < n; base += 32) {
-        float w[kRowsPerWarp];
-#pragma unroll
-        for (int y = 0; y < kRowsPerWarp; ++y) {
-          const float2 v = base == 0 ? (is_own ? held[y].own : held[y].pre) : part_ml(u[y], base + lane);
-          w[y] = v.y == 0.f || lse2[y] == -INFINITY ? 0.f : ex2_approx(v.x - lse2[y]);
-        }
-        const int here = min(32, n - base);
-#pragma unroll 1
-        for (int i = 0; i < here; i += U) {
-          float f[U][kRowsPerWarp][kPer];
-#pragma unroll
-          for (int v = 0; v < U; ++v)
-#pragma unroll
-            for (int y = 0; y < kRowsPerWarp; ++y) {
-              const bool some = i + v < here && base + i + v < u[y].n;
-              const float* src = u[y].o + static_cast<size_t>(base + i + v) * u[y].rows * D + lane;
-#pragma unroll
-              for (int z = 0; z < kPer; ++z) f[v][y][z] = some ? __ldcg(src + z * 32) : 0.f;
-            }
-#pragma unroll
-          for (int v = 0; v < U; ++v)
-#pragma unroll
-            for (int y = 0; y < kRowsPerWarp; ++y) {
-              const float wi = __shfl_sync(0xffffffffu, w[y], (i + v) & 31);
-#pragma unroll
-              for (int z = 0; z < kPer; ++z)
-                o[y][z] = i + v < here && wi != 0.f ? fmaf(f[v][y][z], wi, o[y][z]) : o[y][z];
-            }
-        }
-      }
-    };
-    add(pre, n_pre, false);
-    add(own, n_own, true);
-#pragma unroll
-    for (int y = 0; y < kRowsPerWarp; ++y) {
-      if (row[y] < 0) continue;
-#pragma unroll
-      for (int z = 0; z < kPer; ++z) a.o[static_cast<size_t>(row[y]) * D + z * 32 + lane] = __float2bfloat16(o[y][z]);
-      if (lane == 0) {
-        a.lse2[row[y]] = lse2[y];
-        if (a.lse) a.lse[row[y]] = lse2[y] * 0.69314718055994531f;
-      }
+    for (int z = 0; z < kPer; ++z) a.o[row * D + z * 32 + lane] = __float2bfloat16(o[z]);
+    if (lane == 0) {
+      a.lse2[row] = lse2;
+      if (a.lse) a.lse[row] = lse2 * 0.69314718055994531f;
     }
     return;
   }
@@ -254,27 +223,27 @@ __global__ void __launch_bounds__(kMergeThreads, 4) merge_kernel(MergeArgs a) {
   __shared__ float lse2_sh[kLogitRows];
   __shared__ int seen_sh[kLogitRows];
   int e;
-  const int j0 = a.by_key_blocks.mod(blockIdx.x - a.row_blocks, e) * kMergeKeys;
-  const int len = at_len(g, e);
-  // loads that need no normaliser, under way while it is computed
+  const int j0 = a.by_key_blocks.mod(blockIdx.x - a.row_blocks, e) * kMergeKeys + tid;
+  // loads that need no normaliser, under way while it is computed: the first kAhead rows
   constexpr int kKeys = kMergeKeys / kMergeThreads, kAhead = 4;
   const float* y = a.logits + static_cast<size_t>(e) * g.R * g.cap;
+  float* weights = a.weights + static_cast<size_t>(e) * g.cap;
   float sum[kKeys], ahead[kAhead][kKeys];
 #pragma unroll
   for (int x = 0; x < kKeys; ++x) {
-    const int j = j0 + x * kMergeThreads + tid;
-    sum[x] = j < g.cap ? a.weights[static_cast<size_t>(e) * g.cap + j] : 0.f;
+    const int j = j0 + x * kMergeThreads;
+    sum[x] = j < g.cap ? weights[j] : 0.f;
 #pragma unroll
-    for (int r = 0; r < kAhead; ++r)
-      ahead[r][x] = j < g.cap && r < g.R ? __ldcg(y + static_cast<size_t>(r) * g.cap + j) : 0.f;
+    for (int r = 0; r < kAhead; ++r) ahead[r][x] = j < g.cap && r < g.R ? __ldcg(y + static_cast<size_t>(r) * g.cap + j) : 0.f;
   }
-  if (j0 >= len) return;
+  const int len = at_len(g, e);
+  if (j0 - tid >= len) return;
 #pragma unroll 1
   for (int r = warp; r < g.R; r += kMergeThreads / 32) {
-    const Run own = own_run(a, e, r, D);
-    const Run pre = a.has_prefix ? prefix_run(a, e, r, D) : Run{own.ml, own.o, 0, 0};
-    const float v = a.has_prefix || own.n > 1 ? merged_lse2({part_ml(own, lane), part_ml(pre, lane)}, own, pre, lane)
-                                              : a.lse2[static_cast<size_t>(e) * g.R + r];
+    const int2 span = a.own_parts.span[e];  // the rows are one block: item e
+    const Run own = make_run(a.own_parts, span, e, r, D), pre = prefix_run(a, e, r, D);
+    const float v = pre.n + own.n > 1 || a.has_prefix ? merged_lse2(pre, own, part_ml(pre, own, lane), lane)
+                                                      : a.lse2[static_cast<size_t>(e) * g.R + r];
     if (lane == 0) {
       lse2_sh[r] = v;
       seen_sh[r] = min(len, len - g.n_q + 1 + g.by_n_q.mod(r));
@@ -289,7 +258,7 @@ __global__ void __launch_bounds__(kMergeThreads, 4) merge_kernel(MergeArgs a) {
       const int seen = seen_sh[r];
 #pragma unroll
       for (int x = 0; x < kKeys; ++x)
-        if (j0 + x * kMergeThreads + tid < seen) add[x] += ex2_approx(fmaf(ahead[r][x], a.sc, -lse2));
+        if (j0 + x * kMergeThreads < seen) add[x] += ex2_approx(fmaf(ahead[r][x], a.sc, -lse2));
     }
   }
 #pragma unroll 1
@@ -298,14 +267,14 @@ __global__ void __launch_bounds__(kMergeThreads, 4) merge_kernel(MergeArgs a) {
     const int seen = seen_sh[r];
 #pragma unroll
     for (int x = 0; x < kKeys; ++x) {
-      const int j = j0 + x * kMergeThreads + tid;
+      const int j = j0 + x * kMergeThreads;
       if (j < seen) add[x] += ex2_approx(fmaf(__ldcg(y + static_cast<size_t>(r) * g.cap + j), a.sc, -lse2));
     }
   }
 #pragma unroll
   for (int x = 0; x < kKeys; ++x) {
-    const int j = j0 + x * kMergeThreads + tid;
-    if (j < len) a.weights[static_cast<size_t>(e) * g.cap + j] = sum[x] + add[x];
+    const int j = j0 + x * kMergeThreads;
+    if (j < len) weights[j] = sum[x] + add[x];
   }
 }
 
@@ -385,9 +354,8 @@ cudaError_t launch_attend_merge(const Shape& s, const AttendArgs& a, const AtLay
     m.pre_parts = l.prefix.parts(a.ws);
   }
   // Few items are cut into many parts each, of few rows; many items into two or three parts, of many rows.
-  const bool many_rows = !l.has_prefix && l.own.items >= l.own.grid;
-  const int rows = kMergeThreads / 32 * (many_rows ? 2 : 1);
-  const int per_item = (l.own.geo.rr + rows - 1) / rows;
+  const bool many_rows = !l.has_prefix && l.own.items >= l.own.grid && l.own.geo.rr > 16;
+  const int per_item = (l.own.geo.rr + kMergeRows - 1) / kMergeRows;
   m.by_row_blocks = FastDiv(per_item);
   m.row_blocks = static_cast<int>((l.has_prefix ? l.own.items : l.own.grid) * per_item);
   m.sc = a.sc;
@@ -402,8 +370,8 @@ cudaError_t launch_attend_merge(const Shape& s, const AttendArgs& a, const AtLay
     m.by_key_blocks = FastDiv(key_blocks);
     blocks += static_cast<unsigned>(l.own.geo.I) * key_blocks;
   }
-  const auto kernel = s.d == 128 ? (many_rows ? merge_kernel<128, 2, 2> : merge_kernel<128, 1, 4>)
-                                 : (many_rows ? merge_kernel<64, 2, 2> : merge_kernel<64, 1, 4>);
+  const auto kernel = s.d == 128 ? (many_rows ? merge_kernel<128, 2, 6> : merge_kernel<128, 4, 4>)
+                                 : (many_rows ? merge_kernel<64, 2, 6> : merge_kernel<64, 4, 4>);
   return launch_after(kernel, blocks, kMergeThreads, 0, st, m);
 }
 

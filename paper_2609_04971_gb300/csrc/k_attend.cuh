@@ -101,10 +101,9 @@ __device__ __forceinline__ AtBlock at_block(const AtGeo& g, int rb) {
 }
 
 // Instance length; out of range counts as 0 (the caller reports it).
-__device__ __forceinline__ int at_len(const AtGeo& g, int e) {
-  const int n = __ldg(g.len + g.by_len_div.div(e));
-  return n >= 0 && n <= g.cap ? n : 0;
-}
+__device__ __forceinline__ int at_raw_len(const AtGeo& g, int e) { return __ldg(g.len + g.by_len_div.div(e)); }
+__device__ __forceinline__ int at_valid_len(const AtGeo& g, int n) { return n >= 0 && n <= g.cap ? n : 0; }
+__device__ __forceinline__ int at_len(const AtGeo& g, int e) { return at_valid_len(g, at_raw_len(g, e)); }
 
 // Keys that the last and the first row (in causal order) of rows [r0, r0 + rr) see.
 __device__ __forceinline__ int at_limit_max(const AtGeo& g, int len, int r0) {
@@ -233,6 +232,12 @@ struct AtSeg {
 // Walks the CTA's segments; every role has its own.
 struct AtWalk {
   int e, rb, t, left, u;
+  int raw, raw_ahead;  // lengths of instances e and e + 1; the latter is under way until it is needed
+  __device__ __forceinline__ void look(const AtGeo& g) { raw_ahead = at_raw_len(g, min(e + 1, g.I - 1)); }
+  __device__ __forceinline__ AtWalk(const AtGeo& g, const AtShare& s)
+      : e(s.at.e), rb(s.at.k), t(s.at.t), left(s.left), u(s.u), raw(at_raw_len(g, s.at.e)) {
+    look(g);
+  }
   __device__ __forceinline__ bool next(const AtGeo& g, AtSeg& s) {
     if (left <= 0 || e >= g.I) return false;
     const AtBlock blk = at_block(g, rb);
@@ -240,7 +245,7 @@ struct AtWalk {
     s.rb = rb;
     s.b0 = blk.b0;
     s.r0 = blk.r0;
-    s.len = at_len(g, e);
+    s.len = at_valid_len(g, raw);
     s.T = at_tiles(at_limit_max(g, s.len, blk.r0));
     s.t0 = t;
     s.t1 = min(s.T, t + left);
@@ -254,6 +259,8 @@ struct AtWalk {
       if (++rb == g.nrb) {
         rb = 0;
         ++e;
+        raw = raw_ahead;
+        look(g);
       }
     }
     return true;
@@ -273,14 +280,16 @@ struct AtParts {
   float* o = nullptr;           // [segment][N rows][D] sums of p v
   float2* ml = nullptr;         // [segment][N rows] (reference, sum of p), base 2
   int2* span = nullptr;         // [item] first and last CTA that worked on it
-  int* cut = nullptr;           // [CTA] the item that the CTA began and left to others to finish, or -1
+  int2* cut = nullptr;          // [CTA] the item that the CTA began and left to others to finish (or -1), and
+                                // the last CTA that worked on it
   int rows = 0;                 // rows per segment in o and ml
 };
 
 // What a CTA notes of its segments for the merge; `per` is the number of tiles of a full share.
 __device__ __forceinline__ void at_note(const AtParts& p, const AtSeg& s, bool last_segment, int per) {
-  if (s.t0 == 0) p.span[s.item] = make_int2(blockIdx.x, static_cast<uint32_t>(s.u + s.T - 1) / static_cast<uint32_t>(per));
-  if (last_segment) p.cut[blockIdx.x] = s.t0 == 0 && s.t1 < s.T ? s.item : -1;
+  const int last = static_cast<uint32_t>(s.u - s.t0 + s.T - 1) / static_cast<uint32_t>(per);
+  if (s.t0 == 0) p.span[s.item] = make_int2(blockIdx.x, last);
+  if (last_segment) p.cut[blockIdx.x] = make_int2(s.t0 == 0 && s.t1 < s.T ? s.item : -1, last);
 }
 
 // One source's launch plan, made on the host.
@@ -294,7 +303,7 @@ struct AtPlan {
     p.o = reinterpret_cast<float*>(ws + off_o);
     p.ml = reinterpret_cast<float2*>(ws + off_ml);
     p.span = reinterpret_cast<int2*>(ws + off_span);
-    p.cut = reinterpret_cast<int*>(ws + off_cut);
+    p.cut = reinterpret_cast<int2*>(ws + off_cut);
     p.rows = geo.mb * geo.rr;
     return p;
   }

@@ -101,9 +101,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_before();
   at_split_tiles<kThreads>(g, scan_sh, &share_sh);
   tc_fence_after();
-  if (tid == 0 && share_sh.left == 0) a.parts.cut[blockIdx.x] = -1;
+  if (tid == 0 && share_sh.left == 0) a.parts.cut[blockIdx.x] = make_int2(-1, -1);
   const uint32_t tmem = tmem_base_sh;
-  AtWalk walk{share_sh.at.e, share_sh.at.k, share_sh.at.t, share_sh.left, share_sh.u};
+  AtWalk walk(g, share_sh);
   const int n_tiles = share_sh.left;  // key tiles of this CTA
 
   // Ring of stages: K(0), then for each tile i: V(i), K(i + 1).

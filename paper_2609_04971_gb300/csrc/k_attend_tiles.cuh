@@ -39,6 +39,9 @@ constexpr int kAtThreads = 32 * (4 + kSmWarps);
 // Registers: 168 a thread at launch; the first four warps give back what the softmax warps take, 88 + 2 x 208
 // of 3 x 168 per scheduler.
 constexpr int kRegsFew = 88, kRegsMany = 208;
+// With 16 columns 128 registers do for all warps (the limit that this block size stands for): blocks of the
+// merge that follows then fit beside, and start without waiting for room.
+constexpr int kAtFewRegsThreads = 512;
 constexpr int kAtMaxStages = 12;
 constexpr size_t kAtSmem = 218 * 1024;       // dynamic shared memory, next to up to 8 KB of static
 
@@ -116,7 +119,7 @@ __device__ __forceinline__ uint32_t pack_rest(uint32_t p, float lo, float hi) {
 }
 
 template <int D, int U>
-__global__ void __launch_bounds__(kAtThreads, 1)
+__global__ void __launch_bounds__(U == 1 ? kAtFewRegsThreads : kAtThreads, 1)
     attend_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
                   const __grid_constant__ CUtensorMap vmap, AtKernelArgs a) {
   using C = AtCfg<D, U>;
@@ -187,15 +190,15 @@ __global__ void __launch_bounds__(kAtThreads, 1)
   tc_fence_before();
   at_split_tiles<kAtThreads>(g, scan_sh, &share_sh);
   tc_fence_after();
-  if (tid == 0 && share_sh.left == 0) a.parts.cut[blockIdx.x] = -1;
+  if (tid == 0 && share_sh.left == 0) a.parts.cut[blockIdx.x] = make_int2(-1, -1);
   const uint32_t tmem = tmem_base_sh;
-  AtWalk walk{share_sh.at.e, share_sh.at.k, share_sh.at.t, share_sh.left, share_sh.u};
+  AtWalk walk(g, share_sh);
   const int n_tiles = share_sh.left;  // tiles of this CTA (below 2^31)
 
   // Ring positions.  Tile i of the CTA: K(0); then for each i: K(i + 1), V(i), but V(i) first where
   // K(i + 1) needs a Q buffer that is still in use (one buffer, next segment) and at the end.
   if (warp < 4) {
-    set_max_regs_dec<kRegsFew>();
+    if constexpr (U > 1) set_max_regs_dec<kRegsFew>();
     if (warp == 0) {
       // ---------------------------------------------------------------- producer
       if (lane == 0 && n_tiles > 0) {
@@ -347,7 +350,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
       __syncwarp();
     }
   } else {
-    set_max_regs_inc<kRegsMany>();
+    if constexpr (U > 1) set_max_regs_inc<kRegsMany>();
     // ---------------------------------------------------------------- softmax
     const int grp = (warp - 4) >> 2, wt = tid & 127;  // column group; thread of the group
     const int quarter = warp & 3, key_lane = quarter * 32 + lane;

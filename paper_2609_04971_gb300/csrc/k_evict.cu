@@ -82,13 +82,15 @@ struct WarpRows {
     }
     __syncwarp();
   }
-  // f(row, key) for every i, also where the row is not below L (every lane takes part).
-  template <typename F>
-  __device__ __forceinline__ void each(F&& f) const {
+  // inner(row, key) for 32 rows that are all candidates, [c_lo, c_hi); edge(row, key) for the others, also
+  // where a row is not below L (every lane takes part).
+  template <typename F, typename G>
+  __device__ __forceinline__ void each(int c_lo, int c_hi, F&& inner, G&& edge) const {
 #pragma unroll 2
     for (int i = 0; i < n; ++i) {
-      const int j = row0 + i * 32 + lane;
-      f(j, j < L ? key[j] : 0u);
+      const int j = row0 + i * 32;
+      if (j >= c_lo && j + 32 <= c_hi) inner(j + lane, key[j + lane]);
+      else edge(j + lane, j + lane < L ? key[j + lane] : 0u);
     }
   }
 };
@@ -105,9 +107,13 @@ __device__ __forceinline__ void select_digit(const WarpRows& rows, int c_lo, int
   const int tid = threadIdx.x;
   for (int i = tid; i < kBins; i += THREADS) hist[i] = 0;
   __syncthreads();
-  rows.each([&](int j, uint32_t key) {
-    if (j >= c_lo && j < c_hi && (key & mask) == prefix) atomicAdd(&hist[(key >> shift) & (kBins - 1)], 1u);
-  });
+  auto count = [&](uint32_t key) {
+    if ((key & mask) == prefix) atomicAdd(&hist[(key >> shift) & (kBins - 1)], 1u);
+  };
+  rows.each(c_lo, c_hi, [&](int, uint32_t key) { count(key); },
+            [&](int j, uint32_t key) {
+              if (j >= c_lo && j < c_hi) count(key);
+            });
   __syncthreads();
   uint32_t loc[kPer], sum = 0;
 #pragma unroll
@@ -197,11 +203,17 @@ __global__ void __launch_bounds__(THREADS, 2048 / THREADS) evict_select_kernel(S
     return key > T ? 1 : (key == T ? 2 : 0);
   };
   uint32_t n_tie = 0, n_sure = 0;
-  rows.each([&](int j, uint32_t key) {
-    const int c = kind(j, key);
-    n_tie += c == 2;
-    n_sure += c == 1;
-  });
+  const int in_lo = all || k_sel <= 0 ? L : c_lo;  // no inner rows where nothing is selected by weight
+  rows.each(in_lo, c_hi,
+            [&](int, uint32_t key) {
+              n_tie += key == T;
+              n_sure += key > T;
+            },
+            [&](int j, uint32_t key) {
+              const int c = kind(j, key);
+              n_tie += c == 2;
+              n_sure += c == 1;
+            });
   n_tie = __reduce_add_sync(0xffffffffu, n_tie);
   n_sure = __reduce_add_sync(0xffffffffu, n_sure);
   if (lane == 0) {
@@ -218,15 +230,16 @@ __global__ void __launch_bounds__(THREADS, 2048 / THREADS) evict_select_kernel(S
   }
   const uint32_t below = (1u << lane) - 1u;
   bool moves = false;  // a row of this warp that has to move was seen
-  rows.each([&](int j, uint32_t key) {
-    const int c = kind(j, key);
-    const uint32_t tie_mask = n_tie ? __ballot_sync(0xffffffffu, c == 2) : 0;
-    const bool keep = c == 1 || (c == 2 && tie_at + __popc(tie_mask & below) < ties);
+  auto put = [&](int j, bool sure, bool tie) {
+    bool keep = sure;
+    if (n_tie) {
+      const uint32_t tie_mask = __ballot_sync(0xffffffffu, tie);
+      keep = sure || (tie && tie_at + __popc(tie_mask & below) < ties);
+      tie_at += __popc(tie_mask);
+    }
     const uint32_t keep_mask = __ballot_sync(0xffffffffu, keep);
     const int pos = static_cast<int>(at + __popc(keep_mask & below));
-    if (keep && in_bounds(pos, n_keep, a.err)) {
-      kept_e[pos] = j;
-    }
+    if (keep && in_bounds(pos, n_keep, a.err)) kept_e[pos] = j;
     if (!moves) {  // rows before the first one that moves stand where they belong
       const uint32_t m = __ballot_sync(0xffffffffu, keep && pos != j);
       if (m) {
@@ -234,9 +247,13 @@ __global__ void __launch_bounds__(THREADS, 2048 / THREADS) evict_select_kernel(S
         if (lane == __ffs(m) - 1) atomicMin(&first_sh, pos);
       }
     }
-    tie_at += __popc(tie_mask);
     at += __popc(keep_mask);
-  });
+  };
+  rows.each(in_lo, c_hi, [&](int j, uint32_t key) { put(j, key > T, key == T); },
+            [&](int j, uint32_t key) {
+              const int c = kind(j, key);
+              put(j, c == 1, c == 2);
+            });
   for (int i = n_keep + tid; i < a.budget; i += THREADS) kept_e[i] = -1;
   if (!in_place)
     for (int i = n_keep + tid; i < a.cap_out; i += THREADS) w_out[i] = 0.f;
