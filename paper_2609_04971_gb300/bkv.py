@@ -118,13 +118,13 @@ def _l():
 def _ptr(t: torch.Tensor | None, dtype: torch.dtype, name: str, device=None):
     if t is None:
         return None
+    if t.dtype is dtype and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
     if t.dtype != dtype:
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
     if not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    return t.data_ptr()
+    raise ValueError(f"{name} must be contiguous")
 
 
 def _ptr_any(t: torch.Tensor | None, dtype: torch.dtype, name: str):

@@ -15,20 +15,24 @@
 //
 // Warp roles: warp 0 TMA producer, warp 1 MMA issue, warp 2 describes the units (the
 // columns' normalisers and limits, what is masked, where an item ends) in a ring in
-// shared memory, warps 4..19 exponentials, in four groups with a quarter of the
-// columns each.  Bound by the exponentials: 128 x 128 of
-// them per unit at 16 per clock and SM, twice what the matrix product takes.
+// shared memory, warps 4..11 exponentials: two groups take the units in turn, so that
+// one computes while the other waits for its next unit (with both on every unit, half
+// of the columns each, they waited and computed together).
+//
+// Per unit the matrix product takes 512 clocks and the exponentials, 32 per clock and
+// SM, as long.
 #include "k_attend.cuh"
 
 namespace bkv {
 namespace {
 
-constexpr int kSmWarps = 16, kGroups = kSmWarps / 4;  // groups of four warps share the columns
+constexpr int kSmWarps = 8, kGroups = kSmWarps / 4;  // two groups of four warps take the units in turn
 constexpr int kThreads = 32 * (4 + kSmWarps);
-constexpr int kDescs = 4;  // units described ahead
+constexpr int kDescs = 8;  // units described ahead
 constexpr uint32_t kBox = 128 * 128;
-constexpr int kCols = 128, kNC = kCols / kGroups;
-constexpr uint32_t kTmem = 2 * kCols;
+constexpr int kCols = 128, kHalf = 64;
+constexpr int kBufs = 4;  // of S in tensor memory
+constexpr uint32_t kTmem = kBufs * kCols;
 
 struct WArgs {
   int I, n_kv, G, R, n_q, cap;
@@ -127,6 +131,7 @@ struct Desc {
   int plain;  // every column is a row that sees every key of the tile
   int ends;   // the item's last unit in this CTA: 1: all its units were here, 2: a part of them
   int part;   // slot of the part
+  int prev_e, prev_j0, prev_len, prev_ends, prev_part;  // the same of the unit before, which the other group had
 };
 
 template <int D>
@@ -143,7 +148,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   using C = WCfg<D>;
   extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(8) uint64_t full_bar[C::kStages], empty_bar[C::kStages];
-  __shared__ __align__(8) uint64_t kfull_bar[2], kempty_bar[2], sfull_bar[2], sfree_bar[2], drain_bar;
+  __shared__ __align__(8) uint64_t kfull_bar[2], kempty_bar[2], sfull_bar[kBufs], sfree_bar[kBufs], meet_bar, drain_bar;
   __shared__ uint32_t tmem_base_sh;
   __shared__ int abort_sh;
   __shared__ int scan_sh[kThreads / 32];
@@ -168,14 +173,17 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int i = 0; i < 2; ++i) {
       mbar_init(&kfull_bar[i], 1);
       mbar_init(&kempty_bar[i], 1);
+    }
+    for (int i = 0; i < kBufs; ++i) {
       mbar_init(&sfull_bar[i], 1);
-      mbar_init(&sfree_bar[i], kSmWarps);
+      mbar_init(&sfree_bar[i], 4);
     }
     for (int i = 0; i < kDescs; ++i) {
       mbar_init(&dfull_bar[i], 1);
-      mbar_init(&dempty_bar[i], kSmWarps);
+      mbar_init(&dempty_bar[i], 4);
     }
     mbar_init(&drain_bar, 1);
+    mbar_init(&meet_bar, kSmWarps);
     abort_sh = 0;
     fence_mbar_init();
   }
@@ -263,13 +271,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       int n_k = 0;
       await(&kfull_bar[0], 0);
       for (int i = 0; ok && i < n_units; ++i) {
-        const int st = i % C::kStages, buf = i & 1, x = i % kDescs;
+        const int st = i % C::kStages, buf = i % kBufs, x = i % kDescs;
         await(&dfull_bar[x], (i / kDescs) & 1);
         await(&full_bar[st], (i / C::kStages) & 1);
         if (!ok) break;
         // read before S is issued: the description stays until the exponentials of this S are done
         const int cols = __shfl_sync(0xffffffffu, desc_sh[x].cols, 0), ends = __shfl_sync(0xffffffffu, desc_sh[x].ends, 0);
-        if (i >= 2) await(&sfree_bar[buf], ((i >> 1) - 1) & 1);
+        if (i >= kBufs) await(&sfree_bar[buf], (i / kBufs - 1) & 1);
         if (!ok) break;
         tc_fence_after();
         const uint32_t idesc = idesc_bf16_f32(128, (cols + 15) / 16 * 16);
@@ -302,6 +310,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       u.start(a, share);
       bool from_start = u.k == 0;  // this CTA has the item's units from its first one on
       int began = 0;               // unit of the CTA at which the item began
+      Desc d;
+      d.e = d.j0 = d.len = d.ends = d.part = 0;
       float lse[kCols / 32], lse_next[kCols / 32];
       auto fetch = [&](const Unit& v, float(&out)[kCols / 32]) {
 #pragma unroll
@@ -331,13 +341,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           // columns without a row see nothing
           lim_sh[x][c] = c < u.cols ? u.len - a.n_q + 1 + (a.hp > 1 ? a.by_n_q.mod(c) : u.i0 + c) : 0;
         }
-        if (lane == 0) {
-          const bool ends = i + 1 == n_units || u.k + 1 == u.n, whole = from_start && u.k + 1 == u.n;
-          desc_sh[x] = {u.e, u.t * kAtTile, u.len, u.cols,
-                        u.cols == kCols && (u.t + 1) * kAtTile <= u.len - a.n_q + 1 + u.i0, ends ? (whole ? 1 : 2) : 0,
-                        // an item that began here after the CTA's first unit leaves part 1; else part 0
-                        static_cast<int>(blockIdx.x) * 2 + (from_start && began > 0)};
-        }
+        const bool ends = i + 1 == n_units || u.k + 1 == u.n, whole = from_start && u.k + 1 == u.n;
+        d = {u.e, u.t * kAtTile, u.len, u.cols,
+             u.cols == kCols && (u.t + 1) * kAtTile <= u.len - a.n_q + 1 + u.i0, ends ? (whole ? 1 : 2) : 0,
+             // an item that began here after the CTA's first unit leaves part 1; else part 0
+             static_cast<int>(blockIdx.x) * 2 + (from_start && began > 0), d.e, d.j0, d.len, d.ends, d.part};
+        if (lane == 0) desc_sh[x] = d;
         __syncwarp();
         if (lane == 0) mbar_arrive(&dfull_bar[x]);
         if (v.k == 0) {
@@ -354,77 +363,91 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int grp = (warp - 4) >> 2;
     const int quarter = warp & 3, key_lane = quarter * 32 + lane;
     const uint32_t lane_addr = static_cast<uint32_t>(quarter * 32) << 16;
-    const int c0 = grp * kNC;
     const float sc = a.sc;
-    auto wait = [&](uint64_t* bar, uint32_t parity) {  // after an abort every wait returns at once
-      at_wait(bar, parity, abort_flag, a.err, kDevTimeoutEpilogue);
+    bool ok = true;  // after an expired wait the warp leaves: its descriptions cannot be trusted
+    auto wait = [&](uint64_t* bar, uint32_t parity) {
+      if (ok) ok = __all_sync(0xffffffffu, at_wait(bar, parity, abort_flag, a.err, kDevTimeoutEpilogue));
+    };
+    uint32_t meetings = 0;
+    auto meet = [&] {  // all eight warps; a barrier whose wait is bounded
       __syncwarp();
+      if (lane == 0) mbar_arrive(&meet_bar);
+      wait(&meet_bar, meetings++ & 1);
     };
     float acc = 0.f;
-    for (int i = 0; i < n_units; ++i) {
-      const int buf = i & 1, x = i % kDescs;
-      wait(&dfull_bar[x], (i / kDescs) & 1);
+    // An item's sums, by both groups after their last unit of it: the one that had its last unit then, the
+    // other before its next unit.
+    auto finish = [&](int e, int j0, int len, int ends, int part) {
+      sum_sh[grp][key_lane] = acc;
+      acc = 0.f;
+      meet();
+      if (grp == 0 && ok) {
+        const int j = j0 + key_lane;
+        const float sum = sum_sh[0][key_lane] + sum_sh[1][key_lane];
+        if (ends == 2) a.parts[static_cast<size_t>(part) * kAtTile + key_lane] = sum;
+        else if (j < len) a.weights[static_cast<size_t>(e) * a.cap + j] += sum;
+      }
+      meet();
+    };
+#pragma unroll 1
+    for (int i = grp; ok && i < n_units + 1; i += kGroups) {
+      // past the last unit only its item is left to finish, by the group that did not have it
+      const bool have = i < n_units;
+      const int buf = i % kBufs, x = (have ? i : n_units - 1) % kDescs;
+      if (!have && n_units == 0) break;
+      wait(&dfull_bar[x], ((have ? i : n_units - 1) / kDescs) & 1);
+      if (!ok) break;
       const Desc u = desc_sh[x];
-      wait(&sfull_bar[buf], (i >> 1) & 1);
+      if (have ? u.prev_ends : u.ends) {
+        if (have) finish(u.prev_e, u.prev_j0, u.prev_len, u.prev_ends, u.prev_part);
+        else finish(u.e, u.j0, u.len, u.ends, u.part);
+      }
+      if (!have) break;
+      wait(&sfull_bar[buf], (i / kBufs) & 1);
+      if (!ok) break;
       tc_fence_after();
       const int j = u.j0 + key_lane;
       float2 s0 = make_float2(0.f, 0.f), s1 = s0;
       auto add4 = [&](const float* y, int c) {
-        const float4 l = *reinterpret_cast<const float4*>(&lse_sh[x][c0 + c]);  // minus the normalisers
+        const float4 l = *reinterpret_cast<const float4*>(&lse_sh[x][c]);  // minus the normalisers
         const float2 sc2 = make_float2(sc, sc);
         const float2 a0 = fma2(make_float2(y[0], y[1]), sc2, make_float2(l.x, l.y));
         const float2 a1 = fma2(make_float2(y[2], y[3]), sc2, make_float2(l.z, l.w));
         s0 = add2(s0, make_float2(ex2_approx(a0.x), ex2_approx(a0.y)));
         s1 = add2(s1, make_float2(ex2_approx(a1.x), ex2_approx(a1.y)));
       };
-      const uint32_t at = tmem + buf * kCols + c0 + lane_addr;
+      const uint32_t at = tmem + buf * kCols + lane_addr;
       auto release = [&] {
-        tmem_wait_ld();
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(&sfree_bar[buf]);
       };
-      if (u.plain) {
-        float y[kNC];
-        tmem_ld32(at, y);
-        release();
-#pragma unroll
-        for (int c = 0; c < kNC; c += 4) add4(y + c, c);
-      } else {  // a masked or an incomplete block: what a key's lane does not see, or no row, adds nothing
-        const int ncw = min(kNC, u.cols - c0);
+      const int end = (u.cols + kHalf - 1) & ~(kHalf - 1);
 #pragma unroll 1
-        for (int c = 0; c < ncw; c += 8) {
-          float y[8];
-          tmem_ld8(at + c, y);
-          tmem_wait_ld();
+      for (int h = 0; h < end; h += kHalf) {
+        float y[kHalf];
 #pragma unroll
-          for (int z = 0; z < 8; z += 4) {
-            const int4 m = *reinterpret_cast<const int4*>(&lim_sh[x][c0 + c + z]);
-            y[z] = j < m.x ? y[z] : -INFINITY;
-            y[z + 1] = j < m.y ? y[z + 1] : -INFINITY;
-            y[z + 2] = j < m.z ? y[z + 2] : -INFINITY;
-            y[z + 3] = j < m.w ? y[z + 3] : -INFINITY;
-            add4(y + z, c + z);
+        for (int c = 0; c < kHalf; c += 32) tmem_ld32(at + h + c, *reinterpret_cast<float(*)[32]>(y + c));
+        tmem_wait_ld();
+        if (h + kHalf == end) release();
+        if (!u.plain) {  // what a key's lane does not see, or no row, adds nothing
+#pragma unroll
+          for (int c = 0; c < kHalf; c += 4) {
+            const int4 m = *reinterpret_cast<const int4*>(&lim_sh[x][h + c]);
+            y[c] = j < m.x ? y[c] : -INFINITY;
+            y[c + 1] = j < m.y ? y[c + 1] : -INFINITY;
+            y[c + 2] = j < m.z ? y[c + 2] : -INFINITY;
+            y[c + 3] = j < m.w ? y[c + 3] : -INFINITY;
           }
         }
-        release();
+#pragma unroll
+        for (int c = 0; c < kHalf; c += 4) add4(y + c, h + c);
       }
       s0 = add2(s0, s1);
       acc += s0.x + s0.y;
       __syncwarp();
       if (lane == 0) mbar_arrive(&dempty_bar[x]);
-      if (u.ends) {
-        sum_sh[grp][key_lane] = acc;
-        named_barrier(1, 32 * kSmWarps);
-        if (grp == 0) {
-          float sum = acc;
-          for (int y = 1; y < kGroups; ++y) sum += sum_sh[y][key_lane];
-          if (u.ends == 2) a.parts[static_cast<size_t>(u.part) * kAtTile + key_lane] = sum;
-          else if (j < u.len) a.weights[static_cast<size_t>(u.e) * a.cap + j] += sum;
-        }
-        named_barrier(1, 32 * kSmWarps);
-        acc = 0.f;
-      }
+      if (u.ends) finish(u.e, u.j0, u.len, u.ends, u.part);
     }
   }
   tc_fence_before();
