@@ -547,28 +547,30 @@ class BeaconKV:
         [n_layers, batch, n_kv_heads, capacity_out] rows, into another cache.  L: int32 CUDA tensor
         [n_layers, batch, n_kv_heads].  Returns (kept rows, new lengths)."""
         c = self.cfg
-        outs = (K_out, V_out, weights_out)
-        if any(t is None for t in outs) and any(t is not None for t in outs):
-            raise ValueError("K_out, V_out and weights_out come together or not at all")
-        if K_out is None:
+        given = (K_out is not None) + (V_out is not None) + (weights_out is not None)
+        if given == 0:
             K_out, V_out, weights_out = K, V, weights
+        elif given != 3:
+            raise ValueError("K_out, V_out and weights_out come together or not at all")
         n_inst, d = self.n_inst, c.head_dim
         rows = n_inst * c.capacity
         cap_out = weights_out.numel() // n_inst
         rows_out = n_inst * cap_out
-        for t, n, name in ((K, rows * d, "K"), (V, rows * d, "V"), (weights, rows, "weights"), (L, n_inst, "L"),
-                           (weights_out, rows_out, "weights_out"), (K_out, rows_out * d, "K_out"),
-                           (V_out, rows_out * d, "V_out"), (kept_out, n_inst * budget, "kept_out"),
-                           (len_out, n_inst, "len_out")):
-            if t is not None and t.numel() != n:
-                self._expect(t, n, name)
+        self._expect(K, rows * d, "K")
+        self._expect(V, rows * d, "V")
+        self._expect(weights, rows, "weights")
+        self._expect(L, n_inst, "L")
+        self._expect(weights_out, rows_out, "weights_out")
+        self._expect(K_out, rows_out * d, "K_out")
+        self._expect(V_out, rows_out * d, "V_out")
+        self._expect(kept_out, n_inst * budget, "kept_out")
+        self._expect(len_out, n_inst, "len_out")
         if not K.is_cuda:
             raise TypeError("K must be a CUDA tensor")
-        inst = (c.n_layers, c.batch, c.n_kv_heads)
         if kept_out is None:
-            kept_out = self._new(K, (*inst, max(0, budget)), torch.int32)
+            kept_out = self._new(K, (c.n_layers, c.batch, c.n_kv_heads, max(0, budget)), torch.int32)
         if len_out is None:
-            len_out = self._new(K, inst, torch.int32)
+            len_out = self._new(K, (c.n_layers, c.batch, c.n_kv_heads), torch.int32)
         bkv_evict(self.ctx, K, V, weights, L, budget, K_out, V_out, weights_out, cap_out, kept_out, len_out)
         return kept_out, len_out
 

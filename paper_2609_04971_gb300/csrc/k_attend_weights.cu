@@ -28,10 +28,10 @@ namespace {
 
 constexpr int kSmWarps = 8, kGroups = kSmWarps / 4;  // two groups of four warps take the units in turn
 constexpr int kThreads = 32 * (4 + kSmWarps);
-constexpr int kDescs = 8;  // units described ahead
+constexpr int kDescs = 4;  // units described ahead
 constexpr uint32_t kBox = 128 * 128;
 constexpr int kCols = 128, kHalf = 64;
-constexpr int kBufs = 4;  // of S in tensor memory
+constexpr int kBufs = kDescs;  // of S in tensor memory: a unit described is a unit whose buffer is free
 constexpr uint32_t kTmem = kBufs * kCols;
 
 struct WArgs {
@@ -131,6 +131,7 @@ struct Desc {
   int plain;  // every column is a row that sees every key of the tile
   int ends;   // the item's last unit in this CTA: 1: all its units were here, 2: a part of them
   int part;   // slot of the part
+  int ends_cols;  // ends << 16 | cols
   int prev_e, prev_j0, prev_len, prev_ends, prev_part;  // the same of the unit before, which the other group had
 };
 
@@ -148,7 +149,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   using C = WCfg<D>;
   extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(8) uint64_t full_bar[C::kStages], empty_bar[C::kStages];
-  __shared__ __align__(8) uint64_t kfull_bar[2], kempty_bar[2], sfull_bar[kBufs], sfree_bar[kBufs], meet_bar, drain_bar;
+  __shared__ __align__(8) uint64_t kfull_bar[2], kempty_bar[2], sfull_bar[kBufs], meet_bar, drain_bar;
   __shared__ uint32_t tmem_base_sh;
   __shared__ int abort_sh;
   __shared__ int scan_sh[kThreads / 32];
@@ -176,7 +177,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     for (int i = 0; i < kBufs; ++i) {
       mbar_init(&sfull_bar[i], 1);
-      mbar_init(&sfree_bar[i], 4);
     }
     for (int i = 0; i < kDescs; ++i) {
       mbar_init(&dfull_bar[i], 1);
@@ -275,12 +275,11 @@ __global__ void __launch_bounds__(kThreads, 1)
         await(&dfull_bar[x], (i / kDescs) & 1);
         await(&full_bar[st], (i / C::kStages) & 1);
         if (!ok) break;
-        // read before S is issued: the description stays until the exponentials of this S are done
-        const int cols = __shfl_sync(0xffffffffu, desc_sh[x].cols, 0), ends = __shfl_sync(0xffffffffu, desc_sh[x].ends, 0);
-        if (i >= kBufs) await(&sfree_bar[buf], (i / kBufs - 1) & 1);
-        if (!ok) break;
+        // The description's slot was free, so the exponentials of the unit that had it, and with it this
+        // buffer of S, are done.  It stays until those of this unit are.
+        const int cols = __shfl_sync(0xffffffffu, desc_sh[x].ends_cols, 0), ends = cols >> 16;
         tc_fence_after();
-        const uint32_t idesc = idesc_bf16_f32(128, (cols + 15) / 16 * 16);
+        const uint32_t idesc = idesc_bf16_f32(128, ((cols & 0xFFFF) + 15) / 16 * 16);
         const uint64_t k = sdesc_kmajor_sw128(k_addr + (n_k & 1) * C::kTileBytes);
         const uint64_t q = sdesc_kmajor_sw128(q_addr + st * C::kTileBytes);
         if (elect_one()) {
@@ -342,10 +341,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           lim_sh[x][c] = c < u.cols ? u.len - a.n_q + 1 + (a.hp > 1 ? a.by_n_q.mod(c) : u.i0 + c) : 0;
         }
         const bool ends = i + 1 == n_units || u.k + 1 == u.n, whole = from_start && u.k + 1 == u.n;
+        const int how = ends ? (whole ? 1 : 2) : 0;
         d = {u.e, u.t * kAtTile, u.len, u.cols,
-             u.cols == kCols && (u.t + 1) * kAtTile <= u.len - a.n_q + 1 + u.i0, ends ? (whole ? 1 : 2) : 0,
+             u.cols == kCols && (u.t + 1) * kAtTile <= u.len - a.n_q + 1 + u.i0, how,
              // an item that began here after the CTA's first unit leaves part 1; else part 0
-             static_cast<int>(blockIdx.x) * 2 + (from_start && began > 0), d.e, d.j0, d.len, d.ends, d.part};
+             static_cast<int>(blockIdx.x) * 2 + (from_start && began > 0), how << 16 | u.cols, d.e, d.j0, d.len,
+             d.ends, d.part};
         if (lane == 0) desc_sh[x] = d;
         __syncwarp();
         if (lane == 0) mbar_arrive(&dfull_bar[x]);
@@ -417,11 +418,6 @@ __global__ void __launch_bounds__(kThreads, 1)
         s1 = add2(s1, make_float2(ex2_approx(a1.x), ex2_approx(a1.y)));
       };
       const uint32_t at = tmem + buf * kCols + lane_addr;
-      auto release = [&] {
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(&sfree_bar[buf]);
-      };
       const int end = (u.cols + kHalf - 1) & ~(kHalf - 1);
 #pragma unroll 1
       for (int h = 0; h < end; h += kHalf) {
@@ -429,7 +425,6 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
         for (int c = 0; c < kHalf; c += 32) tmem_ld32(at + h + c, *reinterpret_cast<float(*)[32]>(y + c));
         tmem_wait_ld();
-        if (h + kHalf == end) release();
         if (!u.plain) {  // what a key's lane does not see, or no row, adds nothing
 #pragma unroll
           for (int c = 0; c < kHalf; c += 4) {
@@ -445,6 +440,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       }
       s0 = add2(s0, s1);
       acc += s0.x + s0.y;
+      tc_fence_before();  // also gives back the buffer of S
       __syncwarp();
       if (lane == 0) mbar_arrive(&dempty_bar[x]);
       if (u.ends) finish(u.e, u.j0, u.len, u.ends, u.part);
