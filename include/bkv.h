@@ -369,7 +369,8 @@ int bkv_set_state(bkv_ctx* ctx, const float* centroids, const double* sums, cons
  * Continual FPS contexts: copies the buffers to / from caller memory (device
  * or host, as for bkv_get_state).
  *   buffers  bf16 [n_layers][batch][n_q_heads][n_beacons + window][head_dim];
- *            rows [0, size) of each head are in use, in buffer order.
+ *            rows [0, size) of each head are in use, in buffer order; the others
+ *            hold zeros or what was in use there before.
  *   sizes    int32 [n_layers][batch][n_q_heads], each in 0..n_beacons + window - 1.
  * bkv_set_cfps_state needs both and marks the state as initialised.
  * BKV_EINVAL on a context without BKV_F_CONTINUAL_FPS.

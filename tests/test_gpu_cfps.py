@@ -185,3 +185,28 @@ def test_continual_fps_state_round_trip():
     finally:
         a.close()
         b.close()
+
+
+def test_continual_fps_fresh_buffers_are_zero():
+    """bkv_get_cfps_state copies whole buffers, so a new context's are defined, whatever memory it was given
+    (here that of a context whose buffers were full of ones); after the seeding the rows past it are still zero."""
+    wl = TINY.scaled(name="cfps_fresh", n_layers=2, batch=2)
+    kw = dict(n_layers=2, batch=2, n_q_heads=wl.n_q_heads, n_kv_heads=wl.n_kv_heads, head_dim=wl.head_dim,
+              n_beacons=8, window=wl.window, capacity=wl.capacity, rope_theta=wl.rope_theta, continual_fps=True)
+    inp = synth.step_inputs(wl, 41, torch.device("cuda"))
+    a = BeaconKV(**kw)
+    buf, sizes = a.cfps_state()
+    a.set_cfps_state(torch.ones_like(buf), sizes)
+    a.sync()
+    a.close()
+    b = BeaconKV(**kw)
+    try:
+        buf, sizes = b.cfps_state()
+        b.sync()
+        assert (buf == 0).all() and (sizes == 0).all()
+        b.init_beacons(inp["q_init"])
+        buf, sizes = b.cfps_state()
+        b.sync()
+        assert (sizes == 8).all() and (buf[..., :8, :] != 0).any() and (buf[..., 8:, :] == 0).all()
+    finally:
+        b.close()
