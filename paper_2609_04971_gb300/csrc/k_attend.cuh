@@ -48,7 +48,7 @@ constexpr uint32_t kAtWaitNs = static_cast<uint32_t>(kWaitLimitNs);
 __device__ __forceinline__ bool at_wait(uint64_t* bar, uint32_t parity, volatile int* abort, int* err, int code) {
   return at_wait_for(bar, parity, abort, err, code, kAtWaitNs);
 }
-// The same for a barrier that arrives whatever the abort flag says.
+// The same for a barrier that arrives whatever the abort flag says (limit_s: at most 4).
 __device__ __forceinline__ void at_wait_always(uint64_t* bar, uint32_t parity, int* err, int code, int limit_s) {
   at_wait_for(bar, parity, nullptr, err, code, limit_s * kAtWaitNs);
 }

@@ -512,7 +512,7 @@ __global__ void __launch_bounds__(U == 1 ? kAtFewRegsThreads : kAtThreads, 1)
             // Not given up after an abort: the four warps must agree on the path below, which has barriers,
             // and each of them arrives after waits that are bounded.
             if (!mbar_try_wait(&vote_bar[grp], i & 1)) {
-              at_wait_always(&vote_bar[grp], i & 1, a.err, kDevTimeoutEpilogue, 10);
+              at_wait_always(&vote_bar[grp], i & 1, a.err, kDevTimeoutEpilogue, 4);
             }
             __syncwarp();
             if (*reinterpret_cast<volatile int*>(&high_sh[grp]) == i + 1) {

@@ -369,7 +369,7 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(Shape s, Evict
 template <int THREADS>
 cudaError_t select(const Shape& s, const EvictArgs& a, cudaStream_t st) {
   const size_t smem = sizeof(uint32_t) * s.cap;
-  if (smem > 40 * 1024) {  // with the static 17 KB past what needs no opt-in
+  if (smem > 30 * 1024) {  // with the static 17 KB past the 48 KB that need no opt-in
     const cudaError_t e = allow_smem<evict_select_kernel<THREADS>>(sizeof(uint32_t) * kMaxCapacity);
     if (e != cudaSuccess) return e;
   }

@@ -141,7 +141,12 @@ def test_single_tokens(d, G):
 @pytest.mark.parametrize("n_q,G,values", [
     (2, 4, [1, 2, 3, 200, 0, 130]), (7, 1, [6, 7, 8, 135, 128, 3]), (16, 1, [16, 15, 17, 400, 1, 144]),
     (33, 4, [33, 32, 0, 399, 160, 34]), (33, 2, [400, 5, 129, 256, 31, 66]), (130, 3, [130, 129, 131, 400, 7, 258]),
-    (257, 1, [400, 257, 128, 1, 384, 300]), (400, 2, [400, 399, 130, 0, 256, 1])])
+    (257, 1, [400, 257, 128, 1, 384, 300]), (400, 2, [400, 399, 130, 0, 256, 1]),
+    # 24, 44, 64, 92, 112 and 128 rows to a block: every column count of the narrow kernel
+    (6, 4, [6, 5, 0, 400, 129, 140]), (11, 4, [11, 10, 139, 266, 1, 400]), (16, 4, [16, 1, 128, 143, 400, 0]),
+    (23, 4, [23, 150, 400, 0, 22, 257]), (28, 4, [28, 400, 128, 1, 155, 300]), (32, 4, [32, 31, 160, 400, 0, 287]),
+    # 256 and 260 rows: the widest block, and one that needs two
+    (64, 4, [64, 63, 400, 0, 128, 191]), (65, 4, [65, 400, 2, 128, 192, 0])])
 def test_several_tokens(d, n_q, G, values):
     """Causal queries at the end of caches that may be shorter than their number (empty rows)."""
     b, hkv, cap = 3, 2, 400
@@ -169,7 +174,7 @@ def test_smallest_capacities(cap):
 
 
 @pytest.mark.parametrize("order", ["rising", "falling", "spike", "equal", "far"])
-@pytest.mark.parametrize("n_q", [1, 20])
+@pytest.mark.parametrize("n_q", [1, 4, 12, 20, 32, 60])
 def test_running_maximum(order, n_q):
     """Logits that force the running reference to move, by far more than a float's exponent range can bridge
     in one step: rising and falling through +-150, one spike late in the cache, all equal, all far below 0."""
@@ -198,6 +203,19 @@ def test_scale_and_accumulation():
     bk = _bk(b, hq, hkv, d, cap)
     try:
         run_and_check(bk, q, K, V, _lens(b, hkv, [300, 17]), scale=0.31, times=2)
+    finally:
+        bk.close()
+
+
+def test_many_short_caches():
+    """More caches than SMs, most of them shorter than a tile: many segments to a block, several to a tile's time."""
+    b, hkv, cap, d = 150, 4, 300, 64
+    lens = _lens(b, hkv, [3, 0, 140, 1, 299, 64, 128, 129, 17])
+    q, K, V = _inputs(b, 2 * hkv, hkv, d, cap, 2, seed=40)
+    _poison(K, V, lens)
+    bk = _bk(b, 2 * hkv, hkv, d, cap)
+    try:
+        run_and_check(bk, q, K, V, lens)
     finally:
         bk.close()
 
@@ -304,7 +322,8 @@ def test_attend_in_a_graph():
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("groups,m,G,n_q,pcap,plens", [
     (1, 4, 4, 1, 300, [300]), (1, 3, 5, 1, 129, [129]), (2, 3, 1, 1, 400, [0, 399]), (1, 40, 4, 1, 257, [200]),
-    (3, 2, 8, 3, 200, [1, 128, 200]), (1, 2, 2, 70, 300, [291]), (2, 1, 3, 1, 64, [64, 5]), (1, 20, 7, 1, 1000, [999])])
+    (3, 2, 8, 3, 200, [1, 128, 200]), (1, 2, 2, 70, 300, [291]), (2, 1, 3, 1, 64, [64, 5]), (1, 20, 7, 1, 1000, [999]),
+    (1, 33, 8, 1, 700, [640]), (2, 3, 4, 80, 300, [300, 1]), (1, 9, 16, 1, 513, [513])])
 def test_shared_prefix(d, groups, m, G, n_q, pcap, plens):
     """Prefixes of odd lengths, an empty one, own caches that are empty or short; row blocks that split the
     sequences' rows unevenly."""
@@ -389,7 +408,8 @@ def _check_evict(bk, K, V, w, L, budget, cap_out=None):
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("cap,budget,n_prefix,window", [
     (40, 1, 0, 0), (40, 13, 4, 9), (300, 200, 0, 8), (700, 699, 3, 1), (700, 350, 0, 0), (2049, 1000, 4, 8),
-    (10241, 5000, 1, 32), (333, 400, 2, 2)])
+    (10241, 5000, 1, 32), (333, 400, 2, 2), (2048, 2047, 0, 1), (8300, 8000, 3, 64), (10240, 77, 0, 8),
+    (32768, 30000, 4, 16)])
 def test_evict(d, cap, budget, n_prefix, window):
     g = torch.Generator(device="cuda").manual_seed(cap)
     shape = (2, 3, 2)
