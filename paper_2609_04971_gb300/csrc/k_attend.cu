@@ -16,7 +16,6 @@ namespace {
 
 constexpr int kMergeThreads = 256, kMergeRows = kMergeThreads / 32;  // rows per block
 constexpr int kMergeKeys = 1024;   // keys per block of the weights' part
-constexpr int kLogitRows = 16;      // rows per instance up to which logits are kept for the weights
 
 size_t align_up(size_t n) { return (n + 255) / 256 * 256; }
 
@@ -163,10 +162,9 @@ __device__ __noinline__ float merged_lse2(Run pre, Run own, float2 mine, int lan
   return sum == 0.f ? -INFINITY : top + log2f(sum);
 }
 
-// U parts of O under way at a time, MINB blocks to an SM.
-template <int D, int U, int MINB>
-__global__ void __launch_bounds__(kMergeThreads, MINB) merge_kernel(MergeArgs a) {
-  constexpr int kPer = D / 32;
+template <int D>
+__global__ void __launch_bounds__(kMergeThreads, 4) merge_kernel(MergeArgs a) {
+  constexpr int kPer = D / 32, U = 4;  // parts of O under way at a time
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const AtGeo& g = a.own;
   grid_dependents_go();
@@ -353,8 +351,6 @@ cudaError_t launch_attend_merge(const Shape& s, const AttendArgs& a, const AtLay
     m.pre.len = a.plen;
     m.pre_parts = l.prefix.parts(a.ws);
   }
-  // Few items are cut into many parts each, of few rows; many items into two or three parts, of many rows.
-  const bool many_rows = !l.has_prefix && l.own.items >= l.own.grid && l.own.geo.rr > 16;
   const int per_item = (l.own.geo.rr + kMergeRows - 1) / kMergeRows;
   m.by_row_blocks = FastDiv(per_item);
   m.row_blocks = static_cast<int>((l.has_prefix ? l.own.items : l.own.grid) * per_item);
@@ -370,9 +366,7 @@ cudaError_t launch_attend_merge(const Shape& s, const AttendArgs& a, const AtLay
     m.by_key_blocks = FastDiv(key_blocks);
     blocks += static_cast<unsigned>(l.own.geo.I) * key_blocks;
   }
-  const auto kernel = s.d == 128 ? (many_rows ? merge_kernel<128, 2, 6> : merge_kernel<128, 4, 4>)
-                                 : (many_rows ? merge_kernel<64, 2, 6> : merge_kernel<64, 4, 4>);
-  return launch_after(kernel, blocks, kMergeThreads, 0, st, m);
+  return launch_after(s.d == 128 ? merge_kernel<128> : merge_kernel<64>, blocks, kMergeThreads, 0, st, m);
 }
 
 }  // namespace bkv

@@ -19,6 +19,7 @@ namespace bkv {
 
 constexpr int kAtTile = 128;             // keys per tile
 constexpr uint32_t kAtBox = 128 * 128;   // [128 rows][64 bf16] swizzled box
+constexpr int kLogitRows = 32;           // query rows per KV head up to which logits are kept for the weights
 constexpr float kMaxAbove = 32.f;        // log2 of how far p may exceed 1 before its reference moves
 constexpr float kRefFloor = -1e30f;
 

@@ -476,8 +476,8 @@ __global__ void __launch_bounds__(U == 1 ? kAtFewRegsThreads : kAtThreads, 1)
               }
             };
             load();
-            if constexpr (U == 1) {
-              // rows of an instance with at most 16 of them are one block: consecutive
+            if constexpr (16 * U <= kLogitRows) {
+              // rows of an instance with so few of them are one block: consecutive
               if (a.logits && j < s.len) {
                 float* dst = a.logits + (static_cast<size_t>(s.e) * g.R + c0) * g.cap + j;
 #pragma unroll

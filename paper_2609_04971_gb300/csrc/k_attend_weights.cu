@@ -129,10 +129,12 @@ struct Unit {
 struct Desc {
   int e, j0, len, cols;
   int plain;  // every column is a row that sees every key of the tile
-  int ends;   // the item's last unit in this CTA: 1: all its units were here, 2: a part of them
+  int ends;   // the item's last unit in this CTA: 1: all its units were here, 2: a part of them; + 4: it had this
+              // one here only, and the other group has nothing to do with it
   int part;   // slot of the part
   int ends_cols;  // ends << 16 | cols
-  int prev_e, prev_j0, prev_len, prev_ends, prev_part;  // the same of the unit before, which the other group had
+  int prev_e, prev_j0, prev_len, prev_ends, prev_part;  // the same of the unit before, which the other group had;
+                                                        // prev_ends = 0 where that group needs no help
 };
 
 template <int D>
@@ -341,12 +343,12 @@ __global__ void __launch_bounds__(kThreads, 1)
           lim_sh[x][c] = c < u.cols ? u.len - a.n_q + 1 + (a.hp > 1 ? a.by_n_q.mod(c) : u.i0 + c) : 0;
         }
         const bool ends = i + 1 == n_units || u.k + 1 == u.n, whole = from_start && u.k + 1 == u.n;
-        const int how = ends ? (whole ? 1 : 2) : 0;
+        const int how = ends ? (whole ? 1 : 2) + (i == began ? 4 : 0) : 0;
         d = {u.e, u.t * kAtTile, u.len, u.cols,
              u.cols == kCols && (u.t + 1) * kAtTile <= u.len - a.n_q + 1 + u.i0, how,
              // an item that began here after the CTA's first unit leaves part 1; else part 0
              static_cast<int>(blockIdx.x) * 2 + (from_start && began > 0), how << 16 | u.cols, d.e, d.j0, d.len,
-             d.ends, d.part};
+             d.ends & 4 ? 0 : d.ends, d.part};
         if (lane == 0) desc_sh[x] = d;
         __syncwarp();
         if (lane == 0) mbar_arrive(&dfull_bar[x]);
@@ -376,18 +378,20 @@ __global__ void __launch_bounds__(kThreads, 1)
       wait(&meet_bar, meetings++ & 1);
     };
     float acc = 0.f;
-    // An item's sums, by both groups after their last unit of it: the one that had its last unit then, the
-    // other before its next unit.
+    // An item's sum.  A weight is added to once in a call, so the order of the additions cannot matter, and
+    // nobody waits for the old value.
+    auto write = [&](int e, int j0, int len, int ends, int part, float sum) {
+      const int j = j0 + key_lane;
+      if (ends & 2) a.parts[static_cast<size_t>(part) * kAtTile + key_lane] = sum;
+      else if (j < len) atomicAdd(a.weights + static_cast<size_t>(e) * a.cap + j, sum);
+    };
+    // The sums of an item that both groups had units of, by both after their last unit of it: the one that
+    // had its last unit then, the other before its next unit.
     auto finish = [&](int e, int j0, int len, int ends, int part) {
       sum_sh[grp][key_lane] = acc;
       acc = 0.f;
       meet();
-      if (grp == 0 && ok) {
-        const int j = j0 + key_lane;
-        const float sum = sum_sh[0][key_lane] + sum_sh[1][key_lane];
-        if (ends == 2) a.parts[static_cast<size_t>(part) * kAtTile + key_lane] = sum;
-        else if (j < len) a.weights[static_cast<size_t>(e) * a.cap + j] += sum;
-      }
+      if (grp == 0 && ok) write(e, j0, len, ends, part, sum_sh[0][key_lane] + sum_sh[1][key_lane]);
       meet();
     };
 #pragma unroll 1
@@ -401,7 +405,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const Desc u = desc_sh[x];
       if (have ? u.prev_ends : u.ends) {
         if (have) finish(u.prev_e, u.prev_j0, u.prev_len, u.prev_ends, u.prev_part);
-        else finish(u.e, u.j0, u.len, u.ends, u.part);
+        else if (!(u.ends & 4)) finish(u.e, u.j0, u.len, u.ends, u.part);
       }
       if (!have) break;
       wait(&sfull_bar[buf], (i / kBufs) & 1);
@@ -443,7 +447,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       tc_fence_before();  // also gives back the buffer of S
       __syncwarp();
       if (lane == 0) mbar_arrive(&dempty_bar[x]);
-      if (u.ends) finish(u.e, u.j0, u.len, u.ends, u.part);
+      if (u.ends & 4) {
+        write(u.e, u.j0, u.len, u.ends, u.part, acc);
+        acc = 0.f;
+      } else if (u.ends) {
+        finish(u.e, u.j0, u.len, u.ends, u.part);
+      }
     }
   }
   tc_fence_before();
