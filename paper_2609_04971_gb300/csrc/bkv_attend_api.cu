@@ -83,7 +83,7 @@ int bkv_attend_reserve(bkv_ctx* ctx, int32_t n_q, int32_t n_groups, int weights)
   if (!ctx) return BKV_EINVAL;
   const int rc = check_attend_shape(ctx, n_q, n_groups);
   if (rc != BKV_OK) return rc;
-  const size_t need = n_q == 0 ? 0 : bkv::attend_layout(ctx->shape, n_q, n_groups, 1, weights != 0).bytes;
+  const size_t need = n_q == 0 ? 0 : bkv::attend_workspace(ctx->shape, n_q, n_groups, weights != 0);
   if (need <= ctx->attend_ws_bytes) return BKV_OK;
   // the new workspace exists before the old one goes, so that a failure changes nothing
   unsigned char* ws = nullptr;

@@ -449,20 +449,6 @@ __device__ __forceinline__ uint32_t float_order_key(float f) {
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-// Named barrier that also tells every thread whether any of them passed true.
-__device__ __forceinline__ bool named_barrier_any(uint32_t id, uint32_t nthreads, bool mine) {
-  uint32_t any;
-  asm volatile(
-      "{\n\t.reg .pred p, q;\n\t"
-      "setp.ne.u32 p, %3, 0;\n\t"
-      "barrier.cta.red.or.pred q, %1, %2, p;\n\t"
-      "selp.u32 %0, 1, 0, q;\n\t}"
-      : "=r"(any)
-      : "r"(id), "r"(nthreads), "r"(static_cast<uint32_t>(mine))
-      : "memory");
-  return any != 0;
-}
-
 // Named barrier among `nthreads` threads (id 1..15; id 0 is __syncthreads).
 __device__ __forceinline__ void named_barrier(uint32_t id, uint32_t nthreads) {
   asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(nthreads) : "memory");

@@ -9,6 +9,8 @@
 // taken in the parts' order, a warp to a row.  A row that one CTA finished is
 // already written.  The same launch adds the attention weights where the logits
 // were kept: weights[j] += sum over rows of 2^(y - lse2).
+#include <algorithm>
+
 #include "k_attend.cuh"
 
 namespace bkv {
@@ -47,14 +49,14 @@ AtPlan make_plan(const Shape& s, int I, int m, int R, int n_q, bool causal, int 
   g.causal = causal;
   g.cap = cap;
   g.len_div = len_div;
-  const int most_rows = 1ll * R * m <= 128 ? 128 : 256;
+  const int most_rows = 1ll * R * m <= kAtTile ? kAtTile : kMaxRows;
   if (R <= most_rows) {
     const int most = most_rows / R, nb = (m + most - 1) / most;
     g.rr = R;
     g.mb = (m + nb - 1) / nb;
     g.nr = 1;
   } else {
-    const int nr = (R + 255) / 256;
+    const int nr = (R + kMaxRows - 1) / kMaxRows;
     g.rr = ((R + nr - 1) / nr + 15) / 16 * 16;
     g.mb = 1;
     g.nr = (R + g.rr - 1) / g.rr;
@@ -76,7 +78,12 @@ AtPlan make_plan(const Shape& s, int I, int m, int R, int n_q, bool causal, int 
 }
 
 size_t place_parts(AtPlan& p, int d, int sms, size_t at) {
-  const size_t parts = static_cast<size_t>(p.items) + sms, rows = static_cast<size_t>(p.geo.mb) * p.geo.rr;
+  const AtGeo& g = p.geo;
+  size_t parts = static_cast<size_t>(p.items) + sms, rows = static_cast<size_t>(g.mb) * g.rr;
+  if (g.R > kMaxRows) {  // room that only grows with the rows, whatever their split rounds to
+    rows = kMaxRows;
+    parts = static_cast<size_t>(g.I) * g.m * ((g.R + kMaxRows - 1) / kMaxRows) + sms;
+  }
   p.off_o = at;
   at = align_up(at + parts * rows * d * sizeof(float));
   p.off_ml = at;
@@ -278,6 +285,12 @@ __global__ void __launch_bounds__(kMergeThreads, 4) merge_kernel(MergeArgs a) {
 
 }  // namespace
 
+size_t attend_workspace(const Shape& s, int n_q, int groups, bool weights) {
+  size_t most = attend_layout(s, n_q, groups, 1, weights).bytes;
+  for (int n = 1; n < n_q && n <= kMaxRows; ++n) most = std::max(most, attend_layout(s, n, groups, 1, weights).bytes);
+  return most;
+}
+
 AtLayout attend_layout(const Shape& s, int n_q, int groups, int pcap, bool weights) {
   AtLayout l;
   const int sms = l.sms = attend_sms();
@@ -330,7 +343,7 @@ cudaError_t launch_attend(const Shape& s, const AttendArgs& a, const AtLayout& l
     k.logits = own ? logits : nullptr;
     k.err = a.err;
     k.after_prefix = own && l.has_prefix;
-    if (g.mb * g.rr > 128) return launch_attend_rows(s.d, p, qmap, kmap, vmap, k, st);
+    if (g.mb * g.rr > kAtTile) return launch_attend_rows(s.d, p, qmap, kmap, vmap, k, st);
     return s.d == 128 ? launch_attend_tiles_128(p, qmap, kmap, vmap, k, st)
                       : launch_attend_tiles_64(p, qmap, kmap, vmap, k, st);
   };

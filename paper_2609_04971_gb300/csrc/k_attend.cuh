@@ -19,6 +19,7 @@ namespace bkv {
 
 constexpr int kAtTile = 128;             // keys per tile
 constexpr uint32_t kAtBox = 128 * 128;   // [128 rows][64 bf16] swizzled box
+constexpr int kMaxRows = 256;            // query rows per row block
 constexpr int kLogitRows = 32;           // query rows per KV head up to which logits are kept for the weights
 constexpr float kMaxAbove = 32.f;        // log2 of how far p may exceed 1 before its reference moves
 constexpr float kRefFloor = -1e30f;
@@ -324,6 +325,9 @@ struct AtLayout {
 };
 // The workspace does not depend on pcap.
 AtLayout attend_layout(const Shape& s, int n_q, int groups, int pcap, bool weights);
+// Bytes that serve every call with at most n_q queries: more queries can need less (beyond kLogitRows rows no
+// logits are kept), but beyond kMaxRows of them the need only grows.
+size_t attend_workspace(const Shape& s, int n_q, int groups, bool weights);
 
 // Workspace of the recomputed weights: [2 grid][128] partial sums, then [items + 1] unit numbers.
 inline long long weights_items(const Shape& s) {

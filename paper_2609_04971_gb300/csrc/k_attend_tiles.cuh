@@ -226,10 +226,11 @@ __global__ void __launch_bounds__(U == 1 ? kAtFewRegsThreads : kAtThreads, 1)
             return;
           }
           mbar_arrive_expect_tx(&qfull_bar[qb], static_cast<uint32_t>(g.mb * g.rr) * D * 2);
-        int group;
-        const int kv = g.by_n_kv.mod(s.e, group);
+          int group;
+          const int kv = g.by_n_kv.mod(s.e, group);
           for (int b = 0; b < C::kBoxes; ++b)
-            tma_load_4d(q_smem + qb * C::kQBytes + b * C::kQBox, &qmap, &qfull_bar[qb], b * 64, s.r0, kv, group * g.m + s.b0, pol_q);
+            tma_load_4d(q_smem + qb * C::kQBytes + b * C::kQBox, &qmap, &qfull_bar[qb], b * 64, s.r0, kv,
+                        group * g.m + s.b0, pol_q);
           ++n_seg;
         };
         AtSeg s;

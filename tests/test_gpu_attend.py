@@ -580,3 +580,50 @@ def test_refusals():
     finally:
         bkv.bkv_debug_fail_alloc(0)
         bk.close()
+
+
+@pytest.mark.parametrize("groups", [0, 2])
+@pytest.mark.parametrize("most", [300, 70, 40])
+def test_a_reservation_serves_every_smaller_call(groups, most):
+    """Fewer queries can need more room (their logits are kept); the reservation covers them all."""
+    b, hq, hkv, d, cap = 4, 8, 2, 64, 12000
+    lens = _lens(b, hkv, [700, 333, 0, 12000])
+    plens = torch.tensor([150, 0], dtype=torch.int32, device="cuda")
+    bk = _bk(b, hq, hkv, d, cap)
+    try:
+        bk.reserve_attend(n_q=most, n_groups=groups, weights=True)
+        for n_q in (1, 2, 4, 7, 8, 9, 16, 17, 31, 32, 33, 39, 40, 63, 64, 65, 70, 100, 128, 129, 255, 256, 257, 299, 300):
+            if n_q > most:
+                continue
+            q, K, V = _inputs(b, hq, hkv, d, cap, n_q, seed=50)
+            w = torch.zeros(b, hkv, cap, device="cuda")
+            if groups:
+                Kp, Vp = _inputs(groups, hq, hkv, d, 150, 1, seed=51)[1:]
+                bk.attend_shared(q, Kp, Vp, K, V, prefix_len=plens, length=lens, weights=w)
+            else:
+                bk.attend(q, K, V, length=lens, weights=w)
+                # every query that sees a row spreads a weight of 1
+                rows = torch.clamp(lens, max=n_q).float() * (hq // hkv)
+                bk.sync()
+                torch.testing.assert_close(w.sum(-1), rows, rtol=2.0 ** -11, atol=1e-6)
+        bk.sync()
+    finally:
+        bk.close()
+
+
+def test_more_tiles_than_fit_31_bits_are_refused():
+    """A prefix as long as the limits allow times as many row blocks: refused before anything is read."""
+    b, cap, n_q = 64, 16, 1 << 20
+    bk = _bk(b, 1, 1, 64, cap)
+    x = torch.zeros(64, dtype=torch.bfloat16, device="cuda")  # the addresses only have to be valid
+    n = torch.zeros(b, dtype=torch.int32, device="cuda")
+    try:
+        with pytest.raises(bkv.BkvError) as ei:
+            bkv.bkv_attend_shared(bk.ctx, x, n_q, x, x, n, 1, 1 << 29, x, x, n, 0.0, x)
+        assert ei.value.code == bkv.BKV_EINVAL
+        with pytest.raises(bkv.BkvError) as ei:  # one prefix of 2^30 rows is past the row limit
+            bkv.bkv_attend_shared(bk.ctx, x, 1, x, x, n, 1, 1 << 30, x, x, n, 0.0, x)
+        assert ei.value.code == bkv.BKV_EINVAL
+        bk.sync()
+    finally:
+        bk.close()
