@@ -2,13 +2,22 @@
 // prefix, over the prefix of its group (include/bkv.h, bkv_attend): the plan of
 // a call, its workspace, and the merge of the partial results.
 //
-// k_attend_tiles.cu leaves, for every part of an item that one CTA worked on, the
-// sums O_p = sum p v and l_p = sum p of each row against a reference m_p (p = 2^(y -
-// m_p), y the base-2 logits).  A row's result over all its parts is
+// The attention kernels (k_attend_tiles.cuh, k_attend_rows.cu) leave, for every part
+// of an item that one CTA worked on, the sums O_p = sum p v and l_p = sum p of each
+// row against a reference m_p (p = 2^(y - m_p), y the base-2 logits), all in fp32.  A
+// row's result over all its parts is
 //   lse2 = log2 sum_p l_p 2^(m_p),   o = sum_p O_p 2^(m_p - lse2),
-// taken in the parts' order, a warp to a row.  A row that one CTA finished is
-// already written.  The same launch adds the attention weights where the logits
-// were kept: weights[j] += sum over rows of 2^(y - lse2).
+// taken in the parts' order, a warp to a row: the order of the GPU's blocks does not
+// show.  A row that one CTA finished is already written, so without a prefix the
+// merge goes by the CTAs: each leaves one unfinished item at most.  The same launch
+// adds the attention weights where the logits were kept, a thread to a key:
+// weights[j] += sum over rows of 2^(y - lse2), rows in order.
+//
+// Bound by latency: it starts while the attention kernel ends (its launch overlaps),
+// and then reads a row's references, its parts and its weights one after the other.
+// Cold: one token, 128 caches of 4224 keys 7.7 us (11 MB of parts and logits); 8 caches
+// of 32768 keys 7.8 us; 16 samples of a prefix of 32768 keys 9.6 us; a prompt of 4096
+// tokens, 32 heads, 22 us for 152 split blocks of 256 rows, 40 MB of parts.
 #include <algorithm>
 
 #include "k_attend.cuh"
@@ -25,8 +34,8 @@ size_t align_up(size_t n) { return (n + 255) / 256 * 256; }
 
 static int attend_sms() {
   int dev = 0, n = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
-      n < 1) {
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) {
     cudaGetLastError();
     return 152;
   }
@@ -36,7 +45,9 @@ static int attend_sms() {
 namespace {
 
 // Row blocks of m sequences x R rows: all rows of an instance in one block while there are at most 128
-// of them, else blocks of at most 256, as even as 16-row steps allow.
+// of them (keys as lanes, k_attend_tiles.cuh), else blocks of at most 256, as even as 16-row steps allow (rows
+// as lanes, k_attend_rows.cu).  Both sides of the 128, head_dim 128, 128 caches of 4224 keys: 80 rows 54 and 64 us,
+// 128 rows 64 and 70 us; 160 rows (two blocks, and one) 102 and 73 us, 256 rows 119 and 85 us.
 AtPlan make_plan(const Shape& s, int I, int m, int R, int n_q, bool causal, int cap, int len_div, int sms,
                  bool& too_large) {
   AtPlan p{};
@@ -143,7 +154,8 @@ __device__ __forceinline__ float warp_sum(float v) {
 
 // Part i of a row, counting the prefix's parts first: its (reference, sum of p); l = 0 past the last.
 __device__ __forceinline__ float2 part_ml(const Run& pre, const Run& own, int i) {
-  const float2* at = i < pre.n ? pre.ml + static_cast<size_t>(i) * pre.rows : own.ml + static_cast<size_t>(i - pre.n) * own.rows;
+  const float2* at = i < pre.n ? pre.ml + static_cast<size_t>(i) * pre.rows
+                               : own.ml + static_cast<size_t>(i - pre.n) * own.rows;
   return i < pre.n + own.n ? __ldcg(at) : make_float2(0.f, 0.f);
 }
 
@@ -239,7 +251,8 @@ __global__ void __launch_bounds__(kMergeThreads, 4) merge_kernel(MergeArgs a) {
     const int j = j0 + x * kMergeThreads;
     sum[x] = j < g.cap ? weights[j] : 0.f;
 #pragma unroll
-    for (int r = 0; r < kAhead; ++r) ahead[r][x] = j < g.cap && r < g.R ? __ldcg(y + static_cast<size_t>(r) * g.cap + j) : 0.f;
+    for (int r = 0; r < kAhead; ++r)
+      ahead[r][x] = j < g.cap && r < g.R ? __ldcg(y + static_cast<size_t>(r) * g.cap + j) : 0.f;
   }
   const int len = at_len(g, e);
   if (j0 - tid >= len) return;
@@ -335,7 +348,6 @@ cudaError_t launch_attend(const Shape& s, const AttendArgs& a, const AtLayout& l
     k.geo.len = len;
     k.parts = p.parts(a.ws);
     k.whole_is_final = !l.has_prefix;
-    k.reuse = g.nrb > 1;
     k.sc = a.sc;
     k.o = a.o;
     k.lse = a.lse;

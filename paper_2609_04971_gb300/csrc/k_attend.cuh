@@ -20,7 +20,10 @@ namespace bkv {
 constexpr int kAtTile = 128;             // keys per tile
 constexpr uint32_t kAtBox = 128 * 128;   // [128 rows][64 bf16] swizzled box
 constexpr int kMaxRows = 256;            // query rows per row block
-constexpr int kLogitRows = 32;           // query rows per KV head up to which logits are kept for the weights
+// Query rows per KV head up to which the logits are kept for the weights, 4 bytes a row and key written and
+// read once more; beyond, the weights are recomputed from the keys.  head_dim 128, kept and recomputed: 128
+// caches of 4224 keys, 24 rows 71 and 84 us, 32 rows 89 and 85; 8 caches of 32768 keys, 32 rows 46 and 53 us.
+constexpr int kLogitRows = 32;
 constexpr float kMaxAbove = 32.f;        // log2 of how far p may exceed 1 before its reference moves
 constexpr float kRefFloor = -1e30f;
 
@@ -318,7 +321,8 @@ struct AtLayout {
   bool logits = false;     // the own kernel stores its logits for the weights
   size_t off_lse2 = 0;     // fp32 [rows]: log2 normalisers
   size_t off_logits = 0;   // fp32 [rows][cap]
-  size_t off_wpart = 0, off_wu0 = 0;  // weights recomputed from the keys: see k_attend_weights.cu
+  size_t off_wpart = 0, off_wu0 = 0;  // weights recomputed from the keys: [2 CTAs][128] partial sums, and the
+                                      // [items + 1] unit numbers of their merge
   size_t bytes = 0;
   bool too_large = false;  // 2^31 tiles or more
   int sms = 0;             // of the current device: one CTA of the attention kernels each
@@ -329,7 +333,7 @@ AtLayout attend_layout(const Shape& s, int n_q, int groups, int pcap, bool weigh
 // logits are kept), but beyond kMaxRows of them the need only grows.
 size_t attend_workspace(const Shape& s, int n_q, int groups, bool weights);
 
-// Workspace of the recomputed weights: [2 grid][128] partial sums, then [items + 1] unit numbers.
+// Tiles of keys that the recomputed weights are made for.
 inline long long weights_items(const Shape& s) {
   return 1ll * s.batch * s.n_kv * ((s.cap + kAtTile - 1) / kAtTile);
 }
@@ -346,7 +350,6 @@ struct AtKernelArgs {
   AtParts parts;
   int whole_is_final;  // an item that one CTA finished writes o and lse itself (no other source)
   int after_prefix;    // launched to overlap the prefix's kernel, which its own work does not need
-  int reuse;           // several row blocks read the same keys: let them stay in L2
   float sc;
   __nv_bfloat16* o;
   float* lse;

@@ -17,10 +17,16 @@
 // logit of a tile exceeds it by more than 2^32, or their sum does, the warp moves its references to
 // the tile's maxima and scales its sums and its lanes of O (fp32 sums and bf16 P
 // have the exponent range for that).  S_w stays in tensor memory until the tile's P is
-// known to stand, so the exponentials need not wait for a maximum.
+// known to stand, so the exponentials need not wait for a maximum.  P is rounded to bf16 for
+// the tensor cores, its sum is taken in fp32 before.
 //
-// Bound by the exponentials (16 per clock and SM: 1024 clocks for 128 x 128) and by
-// the tensor cores (1024 clocks for both products of 128 x 128 x 128) alike.
+// Per 256 x 128 tile with head_dim 128 the products take 2048 clocks, as do the shared
+// memory's reads for them and the copies into it (256 KB), and the exponentials, 32 per
+// clock and SM, 1024; the two groups overlap them to some 3500.  A prompt of 4096
+// tokens, 32 heads, cold: 134 us, 1.03 PFLOP/s of the causal pairs (0.55 of the measured
+// rate of a large product).  Steps of 64 keys, with S of both halves under way, were slower
+// (a call of this prompt 196 us instead of 152): a product of half the columns takes more than
+// half the time, and there are twice as many hand-overs.  So were two issuing warps.
 #include "k_attend.cuh"
 
 namespace bkv {
@@ -51,7 +57,8 @@ __global__ void __launch_bounds__(kThreads, 1)
   using C = RowsCfg<D>;
   extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(8) uint64_t full_bar[C::kStages], empty_bar[C::kStages];
-  __shared__ __align__(8) uint64_t qfull_bar, qempty_bar, sfull_bar[2], pfull_bar[2], ofull_bar[2], ofree_bar[2], drain_bar;
+  __shared__ __align__(8) uint64_t qfull_bar, qempty_bar, sfull_bar[2], pfull_bar[2];
+  __shared__ __align__(8) uint64_t ofull_bar[2], ofree_bar[2], drain_bar;
   __shared__ uint32_t tmem_base_sh;
   __shared__ int abort_sh;
   __shared__ int scan_sh[kThreads / 32];
@@ -399,8 +406,9 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (final_rows) {
 #pragma unroll
             for (int z = 0; z < 32; z += 8) {
-              const uint4 v = make_uint4(pack_bf16(o[z] * inv, o[z + 1] * inv), pack_bf16(o[z + 2] * inv, o[z + 3] * inv),
-                                         pack_bf16(o[z + 4] * inv, o[z + 5] * inv), pack_bf16(o[z + 6] * inv, o[z + 7] * inv));
+              const uint4 v =
+                  make_uint4(pack_bf16(o[z] * inv, o[z + 1] * inv), pack_bf16(o[z + 2] * inv, o[z + 3] * inv),
+                             pack_bf16(o[z + 4] * inv, o[z + 5] * inv), pack_bf16(o[z + 6] * inv, o[z + 7] * inv));
               *reinterpret_cast<uint4*>(a.o + static_cast<size_t>(row) * D + x + z) = v;
             }
           } else {

@@ -7,17 +7,26 @@
 //   P^T [128 keys x N]  = 2^(scale S^T - ref)  (registers, rounded to bf16)
 //   O^T [D x N]        += V_tile^T P           (V and P from shared memory, MN-major)
 // S^T is double buffered in tensor memory, and O^T too, so that a segment's
-// result is read out while the next one accumulates.  A softmax thread owns one
-// key and half of the columns: the sum of p over the keys is a register per
-// column, reduced over lanes once per segment.
+// result is read out while the next one accumulates; up to 64 columns P and Q are
+// double buffered in shared memory.  A softmax thread owns one key and half of the
+// columns: the sum of p over the keys is a register per column, reduced over lanes
+// once per segment.
 //
 // The reference of a column is the logit of the first key of the segment, not
 // the maximum: p and its sum are fp32 and P is bf16, whose exponent range is as
 // wide, so p may be large without losing precision.  Only when a logit exceeds
 // the reference by more than 2^32 the reference moves to the tile's maximum, and
 // the sums and O^T are scaled once.  That takes the reduction of the maximum over
-// the lanes off the path.  With causal rows a column whose first key is masked is
-// masked throughout the segment (rows see a prefix of the keys).
+// the lanes off the path: what is left of it is a vote of a group's four warps,
+// under way on a barrier while they compute their exponentials.  With causal rows a
+// column whose first key is masked is masked throughout the segment (rows see a
+// prefix of the keys).
+//
+// Roundings: P to bf16 for the tensor cores, u = 2^-8 of each weight.  With 8 rows
+// or fewer half of the columns are free and take the rest of each p, rounded to bf16
+// again: the weights then carry 16 bits, the output is as exact as one of fp32
+// weights (error 0.0017 of the output's size, its own rounding, against 0.0022), and
+// the products cost the same (a step of 128 caches 53.4 us either way).
 //
 // Warp roles: warp 0 TMA producer, warp 1 MMA issue, warps 2 and 3 none, warps 4..11
 // softmax (two groups of four warps, each with half of the columns).  K and V tiles share one
@@ -27,6 +36,15 @@
 // Rows of V past the last key of an item are zeroed in shared memory before they
 // are used (0 * NaN would spread); rows of K need nothing, a key only reaches its
 // own lane.
+//
+// Every wait, product and copy has one place in the code: a CTA runs through it 28 to
+// 110 times, and before that the instructions come from memory (the same kernel with
+// its loops peeled was twice as long and 5 us slower on one token).
+//
+// Bound by HBM, and in short calls by start and end.  head_dim 128, cold: 128 caches
+// of 4097..4224 keys, 4 rows: 48 us, 277 MB, 5.8 TB/s (0.85 of the measured copy rate);
+// 8 caches of 32768 keys: 27 us, 134 MB, 5.0 TB/s; 8 prefixes of 32768 keys, 64 rows:
+// 28 us.  About 4.5 us pass until the first tile is there and 2 us after the last.
 #pragma once
 
 #include "k_attend.cuh"
@@ -39,9 +57,6 @@ constexpr int kAtThreads = 32 * (4 + kSmWarps);
 // Registers: 168 a thread at launch; the first four warps give back what the softmax warps take, 88 + 2 x 208
 // of 3 x 168 per scheduler.
 constexpr int kRegsFew = 88, kRegsMany = 208;
-// With 16 columns 128 registers do for all warps (the limit that this block size stands for): blocks of the
-// merge that follows then fit beside, and start without waiting for room.
-constexpr int kAtFewRegsThreads = 512;
 constexpr int kAtMaxStages = 12;
 constexpr size_t kAtSmem = 218 * 1024;       // dynamic shared memory, next to up to 8 KB of static
 
@@ -119,7 +134,7 @@ __device__ __forceinline__ uint32_t pack_rest(uint32_t p, float lo, float hi) {
 }
 
 template <int D, int U>
-__global__ void __launch_bounds__(U == 1 ? kAtFewRegsThreads : kAtThreads, 1)
+__global__ void __launch_bounds__(kAtThreads, 1)
     attend_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
                   const __grid_constant__ CUtensorMap vmap, AtKernelArgs a) {
   using C = AtCfg<D, U>;
@@ -198,11 +213,13 @@ __global__ void __launch_bounds__(U == 1 ? kAtFewRegsThreads : kAtThreads, 1)
   // Ring positions.  Tile i of the CTA: K(0); then for each i: K(i + 1), V(i), but V(i) first where
   // K(i + 1) needs a Q buffer that is still in use (one buffer, next segment) and at the end.
   if (warp < 4) {
-    if constexpr (U > 1) set_max_regs_dec<kRegsFew>();
+    set_max_regs_dec<kRegsFew>();
     if (warp == 0) {
       // ---------------------------------------------------------------- producer
       if (lane == 0 && n_tiles > 0) {
-        const uint64_t pol = a.reuse ? l2_policy_evict_last() : l2_policy_evict_first();
+        // Every key is read once (all rows of an instance are one block); kept in L2 the keys would push the
+        // partial results out: a step of 128 caches 55.3 us, like this 53.4 us.
+        const uint64_t pol = l2_policy_evict_first();
         const uint64_t pol_q = l2_policy_evict_last();
         int pos = 0, n_seg = 0;
         bool ok = true;
@@ -284,7 +301,8 @@ __global__ void __launch_bounds__(U == 1 ? kAtFewRegsThreads : kAtThreads, 1)
         if (i >= 2) await(&sfree_bar[buf], ((i >> 1) - 1) & 1);
         if (!ok) return;
         tc_fence_after();
-        const uint64_t k = sdesc_kmajor_sw128(kv_addr + st * C::kTileBytes), q = sdesc_kmajor_sw128(q_addr + qb * C::kQBytes);
+        const uint64_t k = sdesc_kmajor_sw128(kv_addr + st * C::kTileBytes);
+        const uint64_t q = sdesc_kmajor_sw128(q_addr + qb * C::kQBytes);
         if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk)
@@ -351,7 +369,7 @@ __global__ void __launch_bounds__(U == 1 ? kAtFewRegsThreads : kAtThreads, 1)
       __syncwarp();
     }
   } else {
-    if constexpr (U > 1) set_max_regs_inc<kRegsMany>();
+    set_max_regs_inc<kRegsMany>();
     // ---------------------------------------------------------------- softmax
     const int grp = (warp - 4) >> 2, wt = tid & 127;  // column group; thread of the group
     const int quarter = warp & 3, key_lane = quarter * 32 + lane;
@@ -360,8 +378,7 @@ __global__ void __launch_bounds__(U == 1 ? kAtFewRegsThreads : kAtThreads, 1)
     const int cols = g.mb * g.rr;
     const int c0 = grp * NC;
     const bool active = c0 < cols;  // the group has columns in use
-    // With 8 columns in use at most, the second group's columns of P and O carry what rounding the
-    // first group's P to bf16 leaves: O is then as exact as 16 bits of P make it.
+    // The second group's columns of P and O carry what rounding the first group's P to bf16 leaves.
     const bool two_term = U == 1 && cols <= 8;
     const float sc = a.sc;
     auto wait = [&](uint64_t* bar, uint32_t parity) {  // after an abort every wait returns at once

@@ -19,7 +19,10 @@
 // where they belong.  The weights move with the rows.
 //
 // Bound by HBM: the kept rows are read and written once (8 d bytes a row), the
-// weights read (4 bytes a cached row) and written.
+// weights read (4 bytes a cached row) and written.  head_dim 128, cold: 1024 instances of
+// 4224 rows to 4096, selection 35.5 us, rows 604 us, 4.3 GB at 7.1 TB/s (1.05 of the measured copy
+// rate); 320 instances of 1..32768 rows to 2048, 47.5 and 95.5 us (the selection there
+// is one CTA of 1024 threads to an SM, in 2.1 waves).
 #include "bkv_device.cuh"
 #include "bkv_internal.h"
 #include "k_launch.cuh"
@@ -264,7 +267,7 @@ __global__ void __launch_bounds__(THREADS, 2048 / THREADS) evict_select_kernel(S
   }
 }
 
-// Compaction in place: one CTA per instance.
+// Compaction in place: one CTA per instance, the next chunk under way while one is written.
 template <int D>
 __global__ void __launch_bounds__(512, 2) evict_move_in_place_kernel(Shape s, EvictArgs a) {
   constexpr int kThreads = 512;
@@ -365,7 +368,9 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(Shape s, Evict
   if (mine) a.weights_out[static_cast<size_t>(e) * a.cap_out + i0 + tid] = w;
 }
 
-// More threads for more rows: 8 to 32 rows to a thread at the ends of each range.
+// More threads for more rows.  A call with 256, 512 and 1024 threads, 4.3 M rows in all: instances of 1088 rows
+// 51, 63 and 94 us; of 2048 rows 45, 46 and 60; of 4224 rows 47, 45 and 52; of 10240 rows 50, 44 and 45 us;
+// 2.1 M rows, instances of 16384 rows 58, 46 and 41 us, of 32768 rows 86, 62 and 50 us.
 template <int THREADS>
 cudaError_t select(const Shape& s, const EvictArgs& a, cudaStream_t st) {
   const size_t smem = sizeof(uint32_t) * s.cap;
@@ -379,7 +384,9 @@ cudaError_t select(const Shape& s, const EvictArgs& a, cudaStream_t st) {
 
 template <int D>
 cudaError_t launch_d(const Shape& s, const EvictArgs& a, cudaStream_t st) {
-  const cudaError_t e = s.cap <= 2048 ? select<256>(s, a, st) : s.cap <= 10240 ? select<512>(s, a, st) : select<1024>(s, a, st);
+  const cudaError_t e = s.cap <= 2048    ? select<256>(s, a, st)
+                        : s.cap <= 10240 ? select<512>(s, a, st)
+                                         : select<1024>(s, a, st);
   if (e != cudaSuccess) return e;
   if (a.K_out == a.K) return launch_after(evict_move_in_place_kernel<D>, s.n_inst, 512, 0, st, s, a);
   const int kept = a.budget < s.cap ? a.budget : s.cap, chunks = (kept + kMoveRows - 1) / kMoveRows;

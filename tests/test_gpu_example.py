@@ -67,5 +67,5 @@ def test_evictions_bound_the_caches(ex):
 
 
 def test_command_line(ex, capsys):
-    ex.main(["--samples", "3", "--prompt", "200", "--prefix-budget", "64", "--budget", "32", "--period", "8", "--tokens", "50"])
+    ex.main("--samples 3 --prompt 200 --prefix-budget 64 --budget 32 --period 8 --tokens 50".split())
     assert "shared prefix of 64 rows" in capsys.readouterr().out
