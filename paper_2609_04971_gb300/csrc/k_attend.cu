@@ -16,9 +16,9 @@
 // Bound by latency: it starts while the attention kernel ends (its launch overlaps),
 // and then reads a row's references, its parts and its weights one after the other.
 // Cold: one token, 128 caches of 4224 keys 7.7 us (11 MB of parts and logits); 8 caches
-// of 32768 keys 7.8 us; 16 samples of a prefix of 32768 keys 9.6 us; a prompt of 4096
-// tokens, 32 heads, 22 us for 152 split blocks of 256 rows, 40 MB of parts.
+// of 32768 keys 7.8 us; 16 samples of a prefix of 32768 keys 9.6 us.
 #include <algorithm>
+#include <type_traits>
 
 #include "k_attend.cuh"
 
@@ -26,6 +26,7 @@ namespace bkv {
 namespace {
 
 constexpr int kMergeThreads = 256, kMergeRows = kMergeThreads / 32;  // rows per block
+constexpr int kMergeWarpRows = 4;  // rows per warp of merge_rows_kernel
 constexpr int kMergeKeys = 1024;   // keys per block of the weights' part
 
 size_t align_up(size_t n) { return (n + 255) / 256 * 256; }
@@ -296,6 +297,91 @@ __global__ void __launch_bounds__(kMergeThreads, 4) merge_kernel(MergeArgs a) {
   }
 }
 
+// The same for many rows in few parts, without a prefix or kept logits: four rows of an unfinished item to a
+// warp, eight lanes for the parts of each while the normalisers are computed, all lanes along D for the sums.
+template <int D>
+__global__ void __launch_bounds__(kMergeThreads, 3) merge_rows_kernel(MergeArgs a) {
+  constexpr int RW = kMergeWarpRows, P = 32 / RW, kPer = D / 32, U = 2;
+  using Vec = std::conditional_t<kPer == 4, float4, float2>;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, sub = lane / P, slot = lane % P;
+  const AtGeo& g = a.own;
+  grid_dependents_go();
+  grid_dependency_wait();
+  int x;
+  const int c0 = (a.by_row_blocks.mod(blockIdx.x, x) * (kMergeThreads / 32) + warp) * RW, c = c0 + sub;
+  const int2 cut = a.own_parts.cut[x];
+  if (cut.x < 0) return;
+  int e;
+  const int r0 = g.by_nrb.mod(cut.x, e) * g.rr, rows = min(g.rr, g.R - r0);  // of the row block
+  if (c0 >= rows) return;
+  const Run run = make_run(a.own_parts, make_int2(x, cut.y), cut.x, c0, D);
+  const int n = run.n, part = run.rows;
+  const bool mine = c < rows;
+  auto ml = [&](int i) {
+    return mine && i < n ? __ldcg(run.ml + static_cast<size_t>(i) * part + sub) : make_float2(0.f, 0.f);
+  };
+  const float2 v0 = ml(slot);
+  float top = v0.y != 0.f ? v0.x : -INFINITY;
+#pragma unroll 1
+  for (int i = P + slot; i - slot < n; i += P) {
+    const float2 v = ml(i);
+    if (v.y != 0.f) top = fmaxf(top, v.x);
+  }
+#pragma unroll
+  for (int o = P / 2; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  if (top == -INFINITY) top = 0.f;
+  float sum = v0.y != 0.f ? v0.y * ex2_approx(v0.x - top) : 0.f;
+#pragma unroll 1
+  for (int i = P + slot; i - slot < n; i += P) {
+    const float2 v = ml(i);
+    if (v.y != 0.f) sum += v.y * ex2_approx(v.x - top);
+  }
+#pragma unroll
+  for (int o = P / 2; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  const float lse2 = sum == 0.f ? -INFINITY : top + log2f(sum);
+  const size_t row0 = static_cast<size_t>(e) * g.R + r0 + c0;
+  if (mine && slot == 0) {
+    a.lse2[row0 + sub] = lse2;
+    if (a.lse) a.lse[row0 + sub] = lse2 * 0.69314718055994531f;
+  }
+  float o[RW][kPer] = {};
+  float w = 0.f;
+  const Vec* src = reinterpret_cast<const Vec*>(run.o) + lane;
+#pragma unroll 1
+  for (int i = 0; i < n; i += U) {
+    if (i % P == 0) {
+      const float2 v = i == 0 ? v0 : ml(i + slot);
+      w = v.y == 0.f || lse2 == -INFINITY ? 0.f : ex2_approx(v.x - lse2);
+    }
+    Vec f[U][RW];
+#pragma unroll
+    for (int y = 0; y < U; ++y)
+#pragma unroll
+      for (int k = 0; k < RW; ++k)
+        if (i + y < n && c0 + k < rows) f[y][k] = __ldcg(src + (static_cast<size_t>(i + y) * part + k) * (D / kPer));
+#pragma unroll
+    for (int y = 0; y < U; ++y) {
+#pragma unroll
+      for (int k = 0; k < RW; ++k) {
+        const float wi = __shfl_sync(0xffffffffu, w, k * P + (i + y) % P);
+        if (i + y < n && wi != 0.f) {
+          const float* v = reinterpret_cast<const float*>(&f[y][k]);
+#pragma unroll
+          for (int z = 0; z < kPer; ++z) o[k][z] = fmaf(v[z], wi, o[k][z]);
+        }
+      }
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < RW; ++k) {
+    if (c0 + k < rows) {
+      uint32_t* dst = reinterpret_cast<uint32_t*>(a.o + (row0 + k) * D) + lane * (kPer / 2);
+#pragma unroll
+      for (int z = 0; z < kPer; z += 2) dst[z / 2] = pack_bf16(o[k][z], o[k][z + 1]);
+    }
+  }
+}
+
 }  // namespace
 
 size_t attend_workspace(const Shape& s, int n_q, int groups, bool weights) {
@@ -376,7 +462,12 @@ cudaError_t launch_attend_merge(const Shape& s, const AttendArgs& a, const AtLay
     m.pre.len = a.plen;
     m.pre_parts = l.prefix.parts(a.ws);
   }
-  const int per_item = (l.own.geo.rr + kMergeRows - 1) / kMergeRows;
+  // Many rows in few parts are bound by the instructions of a row, few rows in many parts by the latency of a
+  // part.  A call with merge_rows_kernel and with merge_kernel: a prompt of 4096 tokens, 32 heads 143 and 153 us;
+  // 128 caches of 4224 keys, 256 rows 75 and 85 us; 256 caches of 2176 keys, 128 rows 67 and 73 us.
+  const bool many_rows = !l.has_prefix && !l.logits && 4 * l.own.items >= l.own.grid && l.own.geo.rr > kLogitRows;
+  const int block_rows = many_rows ? kMergeRows * kMergeWarpRows : kMergeRows;
+  const int per_item = (l.own.geo.rr + block_rows - 1) / block_rows;
   m.by_row_blocks = FastDiv(per_item);
   m.row_blocks = static_cast<int>((l.has_prefix ? l.own.items : l.own.grid) * per_item);
   m.sc = a.sc;
@@ -391,7 +482,9 @@ cudaError_t launch_attend_merge(const Shape& s, const AttendArgs& a, const AtLay
     m.by_key_blocks = FastDiv(key_blocks);
     blocks += static_cast<unsigned>(l.own.geo.I) * key_blocks;
   }
-  return launch_after(s.d == 128 ? merge_kernel<128> : merge_kernel<64>, blocks, kMergeThreads, 0, st, m);
+  const auto kernel = many_rows ? (s.d == 128 ? merge_rows_kernel<128> : merge_rows_kernel<64>)
+                                : (s.d == 128 ? merge_kernel<128> : merge_kernel<64>);
+  return launch_after(kernel, blocks, kMergeThreads, 0, st, m);
 }
 
 }  // namespace bkv
