@@ -50,6 +50,13 @@ struct RowsCfg {
   static constexpr uint32_t kTmem = 512;
 };
 
+// 8 floats to a 32-byte aligned address, a whole sector at once.
+__device__ __forceinline__ void store_sector(float* dst, const float* v) {
+  asm volatile("st.global.v8.f32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(dst), "f"(v[0]), "f"(v[1]), "f"(v[2]),
+               "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7])
+               : "memory");
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
     rows_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
@@ -413,8 +420,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           } else {
 #pragma unroll
-            for (int z = 0; z < 32; z += 4)
-              *reinterpret_cast<float4*>(dst + x + z) = make_float4(o[z], o[z + 1], o[z + 2], o[z + 3]);
+            for (int z = 0; z < 32; z += 8) store_sector(dst + x + z, o + z);
           }
         }
       }
