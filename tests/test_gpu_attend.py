@@ -627,3 +627,22 @@ def test_more_tiles_than_fit_31_bits_are_refused():
         bk.sync()
     finally:
         bk.close()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_output_aligned_to_16_bytes_only(d):
+    b, hq, hkv, cap, n_q = 2, 8, 2, 500, 100
+    lens = _lens(b, hkv, [500, 333, 100, 90])
+    q, K, V = _inputs(b, hq, hkv, d, cap, n_q, seed=60)
+    _poison(K, V, lens)
+    bk = _bk(b, hq, hkv, d, cap)
+    try:
+        o, _, _ = run_and_check(bk, q, K, V, lens)
+        room = torch.full((q.numel() + 16,), 7.0, dtype=torch.bfloat16, device="cuda")
+        out = room[8:-8].view(q.shape)
+        assert out.data_ptr() % 32 == 16
+        bk.attend(q, K, V, length=lens, o_out=out)
+        bk.sync()
+        assert torch.equal(out, o) and bool((room[:8] == 7).all()) and bool((room[-8:] == 7).all())
+    finally:
+        bk.close()
