@@ -283,9 +283,14 @@ int bkv_compress_ragged(bkv_ctx* ctx, void* K, void* V, const int32_t* L, int32_
  *   lse_out      fp32 [batch][n_q_heads][n_q] or NULL (natural logarithm).
  *   weights      fp32 [batch][n_kv_heads][capacity] or NULL; rows at or past a
  *                cache's length are not touched.
- * The logits, softmax statistics, output sums and weights are kept in fp32;
- * the attention weights are rounded to bf16 where they multiply V.  Results do
- * not depend on the order in which the GPU runs its blocks.
+ * The logits, softmax statistics, output sums and weights are kept in fp32.
+ * Where the attention weights multiply V they are rounded to bf16, with 8 or
+ * fewer query rows per KV head (G * n_q, times the sequences of a group for a
+ * shared prefix) to the sum of two bf16 numbers.  Results do not depend on the
+ * order in which the GPU runs its blocks.
+ * Limits, BKV_EINVAL beyond them: batch * n_q_heads * n_q below 2^27; n_groups *
+ * n_kv_heads * prefix_capacity below 2^31, prefix_capacity below 2^30; blocks of
+ * 256 query rows times tiles of 128 keys, over all KV heads, below 2^31.
  * The softmax here is over the queries' own causal rows; the beacon state and
  * the context's n_beacons, window, n_prefix and rope_theta play no part.
  * BKV_ESTATE when the workspace that bkv_attend_reserve made is too small.

@@ -16,7 +16,8 @@
 // Bound by latency: it starts while the attention kernel ends (its launch overlaps),
 // and then reads a row's references, its parts and its weights one after the other.
 // Cold: one token, 128 caches of 4224 keys 7.7 us (11 MB of parts and logits); 8 caches
-// of 32768 keys 7.8 us; 16 samples of a prefix of 32768 keys 9.6 us.
+// of 32768 keys 8 us; 16 samples of a prefix of 32768 keys 9.8 us; merge_rows_kernel, a prompt
+// of 4096 tokens, 32 heads, 152 split blocks of 256 rows, 10.8 us for 35 MB of parts.
 #include <algorithm>
 #include <type_traits>
 

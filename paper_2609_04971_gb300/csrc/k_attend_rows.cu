@@ -22,9 +22,10 @@
 //
 // Per 256 x 128 tile with head_dim 128 the products take 2048 clocks, as do the shared
 // memory's reads for them and the copies into it (256 KB), and the exponentials, 32 per
-// clock and SM, 1024; the two groups overlap them to some 3500.  A prompt of 4096
-// tokens, 32 heads, cold: 134 us, 1.03 PFLOP/s of the causal pairs (0.55 of the measured
-// rate of a large product).  Steps of 64 keys, with S of both halves under way, were slower
+// clock and SM, 1024; the two groups overlap them to some 3400.  A prompt of 4096
+// tokens, 32 heads, cold: 128 us, 1.07 PFLOP/s of the causal pairs (0.57 of the measured
+// rate of a large product); some 2 us at the end of each of a CTA's four segments are its
+// results' way out, in which the tensor cores wait.  Steps of 64 keys, with S of both halves under way, were slower
 // (a call of this prompt 196 us instead of 152): a product of half the columns takes more than
 // half the time, and there are twice as many hand-overs.  So were two issuing warps.
 #include "k_attend.cuh"
