@@ -391,6 +391,7 @@ class BeaconKV:
                              capacity, float(rope_theta), flags)
         self.ctx = bkv_create(self.cfg, stream)
         self.n_inst = n_layers * batch * n_kv_heads
+        self._layer = (batch, n_q_heads, head_dim, batch * n_kv_heads, batch * n_kv_heads * capacity)
 
     @classmethod
     def for_workload(cls, wl, stream=None, capacity=None, mean_agg=False, continual_fps=False,
@@ -479,15 +480,15 @@ class BeaconKV:
         return kept_out
 
     # ------------------------------------------------------------ attention over the caches
-    def _new(self, like: torch.Tensor, shape, dtype) -> torch.Tensor:
-        """A new output, from the allocator pool of the context's stream (its memory may have been freed by
-        work that is only ordered on that stream)."""
+    def _new(self, like: torch.Tensor, shape, dtype, shape2, dtype2):
+        """Two new outputs, from the allocator pool of the context's stream (their memory may have been freed
+        by work that is only ordered on that stream)."""
         device = like.device
         stream = _streams[self.ctx.value]
         if torch._C._cuda_getCurrentRawStream(device.index) == stream:
-            return torch.empty(shape, dtype=dtype, device=device)
+            return torch.empty(shape, dtype=dtype, device=device), torch.empty(shape2, dtype=dtype2, device=device)
         with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=device)):
-            return torch.empty(shape, dtype=dtype, device=device)
+            return torch.empty(shape, dtype=dtype, device=device), torch.empty(shape2, dtype=dtype2, device=device)
 
     def reserve_attend(self, *, n_q: int = 1, n_groups: int = 0, weights: bool = False):
         """Workspace for attend (n_groups = 0) or attend_shared with n_q queries per head; needed once
@@ -495,27 +496,31 @@ class BeaconKV:
         bkv_attend_reserve(self.ctx, n_q, n_groups, weights)
 
     def _attend_args(self, q, K, V, length, weights, o_out, lse_out):
-        c = self.cfg
-        batch, heads, d = c.batch, c.n_q_heads, c.head_dim
-        shape = tuple(q.shape)
+        batch, heads, d, lens, rows_kv = self._layer
+        shape = q.shape
         if len(shape) != 4 or shape[0] != batch or shape[1] != heads or shape[3] != d:
-            raise ValueError(f"q must be [batch = {batch}, n_q_heads = {heads}, n_q, head_dim = {d}], got {shape}")
-        rows_kv = batch * c.n_kv_heads * c.capacity
-        self._expect(K, rows_kv * d, "K")
-        self._expect(V, rows_kv * d, "V")
-        self._expect(length, batch * c.n_kv_heads, "length")
-        self._expect(weights, rows_kv, "weights")
+            raise ValueError(f"q must be [batch = {batch}, n_q_heads = {heads}, n_q, head_dim = {d}], got "
+                             f"{tuple(shape)}")
+        expect = self._expect
+        expect(K, rows_kv * d, "K")
+        expect(V, rows_kv * d, "V")
+        expect(length, lens, "length")
+        expect(weights, rows_kv, "weights")
         if not q.is_cuda:
             raise TypeError("q must be a CUDA tensor")
-        if o_out is None:
-            o_out = self._new(q, shape, torch.bfloat16)
+        n_q = shape[2]
+        if o_out is None and lse_out is None:
+            o_out, lse_out = self._new(q, shape, torch.bfloat16, shape[:3], torch.float32)
+        elif o_out is None:
+            expect(lse_out, q.numel() // d, "lse_out")
+            o_out, _ = self._new(q, shape, torch.bfloat16, 0, torch.float32)
         else:
-            self._expect(o_out, q.numel(), "o_out")
-        if lse_out is None:
-            lse_out = self._new(q, shape[:3], torch.float32)
-        else:
-            self._expect(lse_out, q.numel() // d, "lse_out")
-        return shape[2], o_out, lse_out
+            expect(o_out, q.numel(), "o_out")
+            if lse_out is None:
+                lse_out, _ = self._new(q, shape[:3], torch.float32, 0, torch.float32)
+            else:
+                expect(lse_out, q.numel() // d, "lse_out")
+        return n_q, o_out, lse_out
 
     def attend(self, q, K, V, *, length, scale=None, weights=None, o_out=None, lse_out=None):
         """Attention of one layer's newest queries over its caches (bkv_attend): q [batch, n_q_heads, n_q,
@@ -567,10 +572,11 @@ class BeaconKV:
         self._expect(len_out, n_inst, "len_out")
         if not K.is_cuda:
             raise TypeError("K must be a CUDA tensor")
-        if kept_out is None:
-            kept_out = self._new(K, (c.n_layers, c.batch, c.n_kv_heads, max(0, budget)), torch.int32)
-        if len_out is None:
-            len_out = self._new(K, (c.n_layers, c.batch, c.n_kv_heads), torch.int32)
+        if kept_out is None or len_out is None:
+            shape, i32 = (c.n_layers, c.batch, c.n_kv_heads), torch.int32
+            kept, length = self._new(K, shape + (max(0, budget) if kept_out is None else 0,), i32, shape, i32)
+            kept_out = kept if kept_out is None else kept_out
+            len_out = length if len_out is None else len_out
         bkv_evict(self.ctx, K, V, weights, L, budget, K_out, V_out, weights_out, cap_out, kept_out, len_out)
         return kept_out, len_out
 
