@@ -32,20 +32,6 @@ constexpr int kMergeKeys = 1024;   // keys per block of the weights' part
 
 size_t align_up(size_t n) { return (n + 255) / 256 * 256; }
 
-}  // namespace
-
-static int attend_sms() {
-  int dev = 0, n = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess ||
-      cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) {
-    cudaGetLastError();
-    return 152;
-  }
-  return n;
-}
-
-namespace {
-
 // Row blocks of m sequences x R rows: all rows of an instance in one block while there are at most 128
 // of them (keys as lanes, k_attend_tiles.cuh), else blocks of at most 256, as even as 16-row steps allow (rows
 // as lanes, k_attend_rows.cu).  Both sides of the 128, head_dim 128, 128 caches of 4224 keys: 80 rows 54 and 64 us,
@@ -393,7 +379,7 @@ size_t attend_workspace(const Shape& s, int n_q, int groups, bool weights) {
 
 AtLayout attend_layout(const Shape& s, int n_q, int groups, int pcap, bool weights) {
   AtLayout l;
-  const int sms = l.sms = attend_sms();
+  const int sms = l.sms = device_sms();
   const int R = s.G * n_q;
   l.own = make_plan(s, s.batch * s.n_kv, 1, R, n_q, true, s.cap, 1, sms, l.too_large);
   size_t at = place_parts(l.own, s.d, sms, 0);

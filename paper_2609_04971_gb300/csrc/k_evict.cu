@@ -21,7 +21,7 @@
 // Bound by HBM: the kept rows are read and written once (8 d bytes a row), the
 // weights read (4 bytes a cached row) and written.  head_dim 128, cold: 1024 instances of
 // 4224 rows to 4096, selection 35.5 us, rows 604 us, 4.3 GB at 7.1 TB/s (1.05 of the measured copy
-// rate); 320 instances of 1..32768 rows to 2048, 47.5 and 95.5 us (the selection there
+// rate), in place 701 us for the whole call; 320 instances of 1..32768 rows to 2048, 47.5 and 95.5 us (the selection there
 // is one CTA of 1024 threads to an SM, in 2.1 waves).
 #include "bkv_device.cuh"
 #include "bkv_internal.h"
@@ -268,9 +268,8 @@ __global__ void __launch_bounds__(THREADS, 2048 / THREADS) evict_select_kernel(S
 }
 
 // Compaction in place: one CTA per instance, the next chunk under way while one is written.
-template <int D>
-__global__ void __launch_bounds__(512, 2) evict_move_in_place_kernel(Shape s, EvictArgs a) {
-  constexpr int kThreads = 512;
+template <int D, int kThreads>
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads) evict_move_in_place_kernel(Shape s, EvictArgs a) {
   constexpr int kVpr = D * 2 / 16;    // 16-byte vectors per row of one tensor
   constexpr int kRowVec = 2 * kVpr;   // K row, then V row
   constexpr int kPer = 4;             // vectors per thread and chunk, one chunk ahead
@@ -388,7 +387,18 @@ cudaError_t launch_d(const Shape& s, const EvictArgs& a, cudaStream_t st) {
                         : s.cap <= 10240 ? select<512>(s, a, st)
                                          : select<1024>(s, a, st);
   if (e != cudaSuccess) return e;
-  if (a.K_out == a.K) return launch_after(evict_move_in_place_kernel<D>, s.n_inst, 512, 0, st, s, a);
+  if (a.K_out == a.K) {
+    // An instance's rows move in order, so its block has as many threads as still let the blocks of all
+    // instances be on the SMs at once, 1024 threads of 64 registers on each.  A call with blocks of 512 threads,
+    // and of this rule's: 16 instances, 32768 rows to 2048, 73 and 60 us; 4224 rows to 4096, 128 instances 138 and
+    // 110 us, 384 instances 343 and 318, 1024 instances 762 and 701, 4608 instances 3216 and 3095 us.
+    const int sms = device_sms();
+    const auto move = [&](auto kernel, int threads) { return launch_after(kernel, s.n_inst, threads, 0, st, s, a); };
+    return s.n_inst <= sms       ? move(evict_move_in_place_kernel<D, 1024>, 1024)
+           : s.n_inst <= 2 * sms ? move(evict_move_in_place_kernel<D, 512>, 512)
+           : s.n_inst <= 4 * sms ? move(evict_move_in_place_kernel<D, 256>, 256)
+                                 : move(evict_move_in_place_kernel<D, 128>, 128);
+  }
   const int kept = a.budget < s.cap ? a.budget : s.cap, chunks = (kept + kMoveRows - 1) / kMoveRows;
   return launch_after(evict_move_kernel<D>, static_cast<unsigned>(s.n_inst) * chunks, kMoveThreads, 0, st, s, a, chunks);
 }

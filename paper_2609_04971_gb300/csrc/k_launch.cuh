@@ -7,6 +7,17 @@
 
 namespace bkv {
 
+// SMs of the current device.
+inline int device_sms() {
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 1) {
+    cudaGetLastError();
+    return 152;
+  }
+  return n;
+}
+
 // Lets `kernel` use `bytes` of dynamic shared memory, always the same number for one kernel: told to the
 // runtime once per device and kernel (KERNEL makes the note a kernel's own).
 template <auto KERNEL>

@@ -646,3 +646,55 @@ def test_output_aligned_to_16_bytes_only(d):
         assert torch.equal(out, o) and bool((room[:8] == 7).all()) and bool((room[-8:] == 7).all())
     finally:
         bk.close()
+
+
+@pytest.mark.parametrize("kind", ["random", "equal", "rising", "falling"])
+@pytest.mark.parametrize("cap", [10241, 16384, 20480, 20481, 27000, 32768])
+def test_evict_long_instances(cap, kind):
+    """Instances whose rows several blocks share: lengths that leave blocks without rows or with one, ties that
+    run across blocks."""
+    g = torch.Generator(device="cuda").manual_seed(cap)
+    budget = 700
+    shape = (1, 2, 6)
+    K, V = (torch.randn(*shape, cap, 64, generator=g, device="cuda").bfloat16() for _ in "KV")
+    if kind == "random":
+        w = torch.exp(2 * torch.randn(*shape, cap, generator=g, device="cuda"))
+    elif kind == "equal":
+        w = torch.full((*shape, cap), 0.25, device="cuda")
+        w[..., ::7] = 0.5
+    else:
+        w = torch.arange(cap, device="cuda").float().expand(*shape, cap).contiguous()
+        w = w if kind == "rising" else -w
+    L = torch.tensor([cap, cap - 1, 0, 1, 700, 701, 1025, 2049, 4097, cap // 2 + 1, 8193, 10000], dtype=torch.int32,
+                     device="cuda").view(shape)
+    bk = _bk(2, 12, 6, 64, cap, window=16, n_beacons=0, n_prefix=4)
+    try:
+        _check_evict(bk, K, V, w, L, budget)
+        bad = L.clone()
+        bad[0, 0, 0], bad[0, 1, 5] = cap + 1, -3
+        out = [torch.zeros(*shape, budget, 64, dtype=torch.bfloat16, device="cuda") for _ in "KV"]
+        kept, new = bk.evict(K, V, w, L=bad, budget=budget, K_out=out[0], V_out=out[1],
+                             weights_out=torch.zeros(*shape, budget, device="cuda"))
+        with pytest.raises(bkv.BkvError):
+            bk.sync()
+        for e in (0, 11):
+            assert int(new.flatten()[e]) == 0 and bool((kept.view(12, -1)[e] == -1).all())
+    finally:
+        bk.close()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("n_inst", [152, 153, 304, 306, 608, 610, 1300])
+def test_evict_in_place_of_many_instances(n_inst, d):
+    """From more instances on, each has fewer threads."""
+    g = torch.Generator(device="cuda").manual_seed(n_inst)
+    cap, budget, hkv = 90, 61, 1 if n_inst % 2 else 2
+    shape = (1, n_inst // hkv, hkv)
+    K, V = (torch.randn(*shape, cap, d, generator=g, device="cuda").bfloat16() for _ in "KV")
+    w = torch.rand(*shape, cap, generator=g, device="cuda")
+    L = torch.randint(0, cap + 1, shape, generator=g, device="cuda", dtype=torch.int32)
+    bk = _bk(shape[1], hkv, hkv, d, cap, window=4, n_beacons=0, n_prefix=2)
+    try:
+        _check_evict(bk, K, V, w, L, budget)
+    finally:
+        bk.close()
