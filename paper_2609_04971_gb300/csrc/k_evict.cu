@@ -21,8 +21,8 @@
 // Bound by HBM: the kept rows are read and written once (8 d bytes a row), the
 // weights read (4 bytes a cached row) and written.  head_dim 128, cold: 1024 instances of
 // 4224 rows to 4096, selection 35.5 us, rows 604 us, 4.3 GB at 7.1 TB/s (1.05 of the measured copy
-// rate), in place 701 us for the whole call; 320 instances of 1..32768 rows to 2048, 47.5 and 95.5 us (the selection there
-// is one CTA of 1024 threads to an SM, in 2.1 waves).
+// rate), in place 701 us for the whole call; 320 instances of 1..32768 rows to 2048, 47.5 and
+// 95.5 us (the selection there is one CTA of 1024 threads to an SM, in 2.1 waves).
 #include "bkv_device.cuh"
 #include "bkv_internal.h"
 #include "k_launch.cuh"
