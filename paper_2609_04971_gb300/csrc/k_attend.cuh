@@ -228,6 +228,17 @@ __device__ __forceinline__ void at_check_lengths(const AtGeo& g, int* err) {
   }
 }
 
+// CTAs of `ctas` that an item of n >= 1 units was split over, where its first unit has number u and a full share
+// `per` units: first .. last.  False where one CTA had it all, and for numbers that no split makes: a CTA that
+// gave up a wait leaves u of its later items unwritten.
+__host__ __device__ inline bool at_split_over(uint32_t u, uint32_t n, uint32_t per, uint32_t ctas, uint32_t& first,
+                                              uint32_t& last) {
+  if (per == 0) return false;
+  first = u / per;
+  last = (u + n - 1) / per;
+  return first < last && last < ctas;  // a sum that wraps is below u
+}
+
 // One segment of a CTA's run.
 struct AtSeg {
   int e, rb, t0, t1, T, len, r0, b0;

@@ -50,6 +50,7 @@ struct WArgs {
   float* parts;     // [2 grid][128]
   int* u0;          // [I * tiles]: number of an item's first unit; [I * tiles]: units per CTA
   int tiles;        // tiles of the capacity
+  int ctas;         // of weights_kernel
   int* err;
 };
 
@@ -474,20 +475,20 @@ __global__ void __launch_bounds__(kAtTile) weights_merge_kernel(WArgs a) {
   const int len = w_len(a, e), n = w_units(a, len, t);
   if (n == 0) return;
   const uint32_t per = a.u0[static_cast<size_t>(a.I) * a.tiles], u = a.u0[static_cast<size_t>(e) * a.tiles + t];
-  const int first = u / per, last = (u + n - 1) / per;
   const int j = t * kAtTile + threadIdx.x;
-  if (first == last || j >= len) return;
+  uint32_t first, last;
+  if (!at_split_over(u, n, per, a.ctas, first, last) || j >= len) return;
   float sum = 0.f;
-  for (int c = first; c <= last; ++c)
+  for (uint32_t c = first; c <= last; ++c)
     sum += a.parts[(static_cast<size_t>(c) * 2 + (c == first && u != c * per)) * kAtTile + threadIdx.x];
   a.weights[static_cast<size_t>(e) * a.cap + j] += sum;
 }
 
 template <int D>
-cudaError_t launch(const CUtensorMap& qmap, const CUtensorMap& kmap, const WArgs& a, int grid, cudaStream_t st) {
+cudaError_t launch(const CUtensorMap& qmap, const CUtensorMap& kmap, const WArgs& a, cudaStream_t st) {
   const cudaError_t e = allow_smem<weights_kernel<D>>(WCfg<D>::kSmem);
   if (e != cudaSuccess) return e;
-  const cudaError_t w = launch_after(weights_kernel<D>, grid, kThreads, WCfg<D>::kSmem, st, qmap, kmap, a);
+  const cudaError_t w = launch_after(weights_kernel<D>, a.ctas, kThreads, WCfg<D>::kSmem, st, qmap, kmap, a);
   if (w != cudaSuccess) return w;
   return launch_after(weights_merge_kernel, static_cast<unsigned>(a.I) * a.tiles, kAtTile, 0, st, a);
 }
@@ -514,6 +515,7 @@ cudaError_t launch_attend_weights(const Shape& s, const AttendArgs& a, const AtL
   w.parts = reinterpret_cast<float*>(a.ws + l.off_wpart);
   w.u0 = reinterpret_cast<int*>(a.ws + l.off_wu0);
   w.tiles = (s.cap + kAtTile - 1) / kAtTile;
+  w.ctas = l.sms;
   w.err = a.err;
   w.by_n_kv = FastDiv(w.n_kv);
   w.by_n_q = FastDiv(w.n_q);
@@ -522,7 +524,7 @@ cudaError_t launch_attend_weights(const Shape& s, const AttendArgs& a, const AtL
   if (encode_queries_bf16(&qmap, a.q, s.batch, s.n_kv, w.R, s.d, 1, w.brow) != CUDA_SUCCESS ||
       encode_rows_bf16(&kmap, a.K, static_cast<uint64_t>(w.I) * s.cap, s.d, kAtTile) != CUDA_SUCCESS)
     return cudaErrorInvalidValue;
-  return s.d == 128 ? launch<128>(qmap, kmap, w, l.sms, st) : launch<64>(qmap, kmap, w, l.sms, st);
+  return s.d == 128 ? launch<128>(qmap, kmap, w, st) : launch<64>(qmap, kmap, w, st);
 }
 
 }  // namespace bkv
