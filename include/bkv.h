@@ -341,12 +341,13 @@ int bkv_attend_reserve(bkv_ctx* ctx, int32_t n_q, int32_t n_groups, int weights)
  *                 [n_kv_heads][capacity_out] rows, with capacity_out >=
  *                 min(budget, capacity).  Either all three are K, V and weights
  *                 themselves (in place; capacity_out = capacity) or none of
- *                 them overlaps an input or another output.  Rows of K_out and
+ *                 them overlaps an input.  No output, kept_idx_out and len_out
+ *                 among them, overlaps another (BKV_EINVAL).  Rows of K_out and
  *                 V_out past the kept ones keep what they held; those of
  *                 weights_out become 0, ready for the tokens to come.
  *   kept_idx_out  int32 [n_layers][batch][n_kv_heads][budget]: kept rows, then -1.
  *   len_out       int32 [n_layers][batch][n_kv_heads] or NULL: min(L, budget).
- *                 It may be L itself.
+ *                 It may be L itself, but not a part of it.
  * The beacon state plays no part.
  */
 int bkv_evict(bkv_ctx* ctx, const void* K, const void* V, const float* weights, const int32_t* L, int32_t budget,

@@ -21,10 +21,26 @@ namespace {
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
-// Whether [a, a + na) and [b, b + nb) share a byte.
-bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return x < y + nb && y < x + na;
+// Bytes of an argument; none for one that is not given.
+struct Range {
+  const void* p;
+  size_t n;
+  bool overlaps(const Range& o) const {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(p), y = reinterpret_cast<uintptr_t>(o.p);
+    return p && o.p && x < y + o.n && y < x + n;
+  }
+};
+
+// Whether an output shares a byte with an input or with another output.
+template <int IN, int OUT>
+bool overlap(const Range (&in)[IN], const Range (&out)[OUT]) {
+  for (int i = 0; i < OUT; ++i) {
+    for (const Range& r : in)
+      if (out[i].overlaps(r)) return true;
+    for (int j = 0; j < i; ++j)
+      if (out[i].overlaps(out[j])) return true;
+  }
+  return false;
 }
 
 // Limits shared by the calls and the reservation: 32-bit row counts everywhere.
@@ -172,23 +188,22 @@ int bkv_evict(bkv_ctx* ctx, const void* K, const void* V, const float* weights, 
   if (1LL * s.n_inst * capacity_out >= (1LL << 31)) return fail(ctx, BKV_EINVAL, "capacity_out too large");
   const bool in_place = K_out == K && V_out == V && weights_out == weights;
   const size_t rows = static_cast<size_t>(s.n_inst) * s.cap, rows_out = static_cast<size_t>(s.n_inst) * capacity_out;
-  const size_t kv = rows * s.d * 2, kv_out = rows_out * s.d * 2;
-  if (in_place) {
-    if (capacity_out != s.cap)
-      return fail(ctx, BKV_EINVAL, "in place, capacity_out = %d must be the capacity (%d)", capacity_out, s.cap);
-    if (overlap(K, kv, V, kv) || overlap(K, kv, weights, rows * 4) || overlap(V, kv, weights, rows * 4))
-      return fail(ctx, BKV_EINVAL, "K, V and weights overlap");
-  } else {
-    const struct {
-      const void* p;
-      size_t n;
-    } in[3] = {{K, kv}, {V, kv}, {weights, rows * 4}},
-      out[3] = {{K_out, kv_out}, {V_out, kv_out}, {weights_out, rows_out * 4}};
-    for (int i = 0; i < 3; ++i)
-      for (int j = 0; j < 3; ++j)
-        if (overlap(out[i].p, out[i].n, in[j].p, in[j].n) || (j < i && overlap(out[i].p, out[i].n, out[j].p, out[j].n)))
-          return fail(ctx, BKV_EINVAL, "an output overlaps an input or another output, and the call is not in place");
-  }
+  const size_t kv = rows * s.d * 2, kv_out = rows_out * s.d * 2, lens = sizeof(int32_t) * s.n_inst;
+  if (in_place && capacity_out != s.cap)
+    return fail(ctx, BKV_EINVAL, "in place, capacity_out = %d must be the capacity (%d)", capacity_out, s.cap);
+  // The rows are moved by kept_idx_out, so a row number must not be written over either.
+  const Range in[] = {{in_place ? nullptr : K, kv},
+                      {in_place ? nullptr : V, kv},
+                      {in_place ? nullptr : weights, rows * 4},
+                      {len_out == L ? nullptr : L, lens}},
+              out[] = {{K_out, kv_out},
+                       {V_out, kv_out},
+                       {weights_out, rows_out * 4},
+                       {kept_idx_out, sizeof(int32_t) * s.n_inst * budget},
+                       {len_out, lens}};
+  if (overlap(in, out))
+    return fail(ctx, BKV_EINVAL, "an output overlaps an input or another output (K, V and weights may be their own "
+                "outputs, all three, and L may be len_out)");
   bkv::EvictArgs a;
   a.K = static_cast<const __nv_bfloat16*>(K);
   a.V = static_cast<const __nv_bfloat16*>(V);
