@@ -283,6 +283,7 @@ int bkv_compress_ragged(bkv_ctx* ctx, void* K, void* V, const int32_t* L, int32_
  *   lse_out      fp32 [batch][n_q_heads][n_q] or NULL (natural logarithm).
  *   weights      fp32 [batch][n_kv_heads][capacity] or NULL; rows at or past a
  *                cache's length are not touched.
+ * o, lse_out and weights overlap neither an input nor one another (BKV_EINVAL).
  * The logits, softmax statistics, output sums and weights are kept in fp32.
  * Where the attention weights multiply V they are rounded to bf16, with 8 or
  * fewer query rows per KV head (G * n_q, times the sequences of a group for a

@@ -65,6 +65,18 @@ int attend(bkv_ctx* ctx, bkv::AttendArgs& a, double scale) {
   a.sc = static_cast<float>(1.4426950408889634 * (scale == 0.0 ? 1.0 / std::sqrt(static_cast<double>(s.d)) : scale));
   if (!std::isfinite(a.sc) || a.sc < 1.17549435e-38f)
     return fail(ctx, BKV_EINVAL, "scale is out of the range of fp32");
+  // Outputs are written while other blocks and the kernels that follow still read the inputs.
+  const size_t rows = static_cast<size_t>(s.batch) * s.n_kv * s.G * a.n_q, lens = static_cast<size_t>(s.batch) * s.n_kv,
+               kv = lens * s.cap, kvp = static_cast<size_t>(a.groups) * s.n_kv * a.pcap;
+  const Range in[] = {{a.q, rows * s.d * 2},
+                      {a.K, kv * s.d * 2},
+                      {a.V, kv * s.d * 2},
+                      {a.Kp, kvp * s.d * 2},
+                      {a.Vp, kvp * s.d * 2},
+                      {a.len, lens * 4},
+                      {a.plen, static_cast<size_t>(a.groups) * 4}},
+              out[] = {{a.o, rows * s.d * 2}, {a.lse, rows * 4}, {a.weights, kv * 4}};
+  if (overlap(in, out)) return fail(ctx, BKV_EINVAL, "o, lse_out or weights overlaps an input or another output");
   const bkv::AtLayout l = bkv::attend_layout(s, a.n_q, a.groups, a.pcap, a.weights != nullptr);
   if (l.too_large) return fail(ctx, BKV_EINVAL, "row blocks times key tiles must be below 2^31");
   if (l.bytes > ctx->attend_ws_bytes)

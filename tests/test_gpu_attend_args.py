@@ -3,9 +3,72 @@ import pytest
 import torch
 
 from paper_2609_04971_gb300 import bkv
-from tests.test_gpu_attend import _bk
+from tests.test_gpu_attend import _bk, _inputs, _lens
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("n_q", [2, 40])
+def test_overlapping_arguments_are_refused(n_q):
+    """Every output is written while inputs may still be read; none may share a byte with an input or another."""
+    b, hq, hkv, d, cap = 4, 4, 2, 64, 100
+    q, K, V = _inputs(b, hq, hkv, d, cap, n_q, seed=31)
+    lens = _lens(b, hkv, [100])
+    Kp, Vp = K[:2].clone(), V[:2].clone()
+    pl = torch.tensor([10, 20], dtype=torch.int32, device="cuda")
+    o, lse = torch.full_like(q, 3.0), torch.full((b, hq, n_q), 3.0, device="cuda")
+    w = torch.full((b, hkv, cap), 3.0, device="cuda")
+    before = [t.clone() for t in (q, K, V, Kp, Vp, lens, pl, o, lse, w)]
+    bk = _bk(b, hq, hkv, d, cap)
+
+    def refused(shared=False, **kw):
+        a = dict(q=q, K=K, V=V, length=lens, Kp=Kp, Vp=Vp, prefix_len=pl, o=o, lse=lse, w=w)
+        a.update(kw)
+        with pytest.raises(bkv.BkvError) as ei:
+            if shared:
+                bkv.bkv_attend_shared(bk.ctx, a["q"], n_q, a["Kp"], a["Vp"], a["prefix_len"], 2, cap, a["K"], a["V"],
+                                      a["length"], 0.0, a["o"], a["lse"], a["w"])
+            else:
+                bkv.bkv_attend(bk.ctx, a["q"], n_q, a["K"], a["V"], a["length"], 0.0, a["o"], a["lse"], a["w"])
+        assert ei.value.code == bkv.BKV_EINVAL
+
+    def view(t, dtype, at=0):  # another type's view of the last bytes of t, or of those `at` bytes from its start
+        return t.view(-1).view(torch.uint8)[at:].view(dtype)
+
+    try:
+        bk.reserve_attend(n_q=n_q, n_groups=2, weights=True)
+        for shared in (False, True):
+            refused(shared, o=q)
+            refused(shared, o=view(q, torch.bfloat16, 16))   # shifted by 16 bytes
+            refused(shared, o=K)
+            refused(shared, o=V)
+            refused(shared, o=view(w, torch.bfloat16))
+            refused(shared, o=view(lse, torch.bfloat16))
+            refused(shared, lse=view(q, torch.float32))
+            refused(shared, lse=view(K, torch.float32))
+            refused(shared, lse=view(lens, torch.float32))
+            refused(shared, lse=w)
+            refused(shared, w=view(V, torch.float32))
+            refused(shared, w=view(q, torch.float32, q.numel() * 2 - 4))  # one element
+            refused(shared, w=view(lens, torch.float32))
+        refused(True, o=Kp)
+        refused(True, o=Vp)
+        refused(True, lse=view(pl, torch.float32))
+        refused(True, w=view(Kp, torch.float32))
+        bk.sync()
+        for x, y in zip((q, K, V, Kp, Vp, lens, pl, o, lse, w), before):
+            assert torch.equal(x, y)
+        # inputs may share memory with one another, and outputs may lie side by side
+        room = torch.zeros(q.numel() * 2 + 4 * lse.numel() + 4 * w.numel(), dtype=torch.uint8, device="cuda")
+        n1, n2 = q.numel() * 2, q.numel() * 2 + 4 * lse.numel()
+        o2, l2, w2 = (room[:n1].view(torch.bfloat16).view(q.shape), room[n1:n2].view(torch.float32).view(lse.shape),
+                      room[n2:].view(torch.float32).view(w.shape))
+        bkv.bkv_attend(bk.ctx, q, n_q, K, K, lens, 0.0, o2, l2, w2)
+        want, want_l = bk.attend(q, K, K.clone(), length=lens)
+        bk.sync()
+        assert torch.equal(o2, want) and torch.equal(l2, want_l) and bool((w2.sum(-1) > 0).all())
+    finally:
+        bk.close()
 
 
 def test_overlapping_outputs_of_an_eviction_are_refused():
