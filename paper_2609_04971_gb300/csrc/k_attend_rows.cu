@@ -322,7 +322,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             float(&v)[32] = y[q & 1];
             tmem_wait_ld();
             if (q < 3) tmem_ld32(s_addr + (q + 1) * 32, y[(q + 1) & 1]);
-            if (q == 0 && first) ref = seen > 0 ? -fmaxf(v[0] * sc, kRefFloor) : 0.f;
+            // A lane that sees nothing of the segment, or stands for no row but holds one of the next group, has
+            // p = 0 whatever its logits are, so that they cannot ask for a move of the references.
+            if (q == 0 && first) ref = seen > 0 ? -fmaxf(v[0] * sc, kRefFloor) : -INFINITY;
             shift(v, q);
 #pragma unroll
             for (int x = 0; x < 32; x += 4) {
