@@ -414,8 +414,9 @@ int bkv_selftest_wait_timeout(bkv_ctx* ctx, int64_t limit_ns);
  * compiled with BKV_CHECKED defined checks every index that its kernels take
  * from device data before using it: work-list entries and per-instance
  * lengths of a ragged compress, the positions and source rows of the kept
- * set in the selection and gather, and the stored Continual FPS buffer
- * sizes.  A failing check records BKV_EBOUNDS in the device error word (see
+ * set in the selection and gather, the stored Continual FPS buffer sizes,
+ * the rows that an eviction moves, and the blocks whose partial results the
+ * merges of bkv_attend add.  A failing check records BKV_EBOUNDS in the device error word (see
  * bkv_sync) and the access is skipped or redirected in range; nothing traps.
  * The default build compiles the checks out.
  *

@@ -105,6 +105,8 @@ struct MergeArgs {
   const float* logits;
   float* weights;
   FastDiv by_row_blocks, by_key_blocks;  // blocks per item, and blocks of kMergeKeys keys per instance
+  int own_items, own_ctas, pre_ctas;     // what items and CTAs that device data names are checked against
+  int* err;
 };
 
 // The run of a row's parts in one source: n of them, `step` segments' rows apart in ml and o.
@@ -114,7 +116,9 @@ struct Run {
   int n, rows;
 };
 
-__device__ __forceinline__ Run make_run(const AtParts& p, int2 span, int item, int c, int d) {
+__device__ __forceinline__ Run make_run(const AtParts& p, int2 span, int item, int c, int d, int ctas, int* err) {
+  if (!in_bounds(span.x, ctas, err) || !in_bounds(span.y, ctas, err) || !in_bounds(span.y - span.x, ctas, err))
+    return {nullptr, nullptr, 0, 0};
   const size_t at = static_cast<size_t>(span.x + item) * p.rows + c;
   return {p.ml + at, p.o + at * d, span.y - span.x + 1, p.rows};
 }
@@ -126,7 +130,7 @@ __device__ __forceinline__ Run prefix_run(const MergeArgs& a, int e, int r, int 
   int b, group, bq, rb;
   const int kv = q.by_n_kv.mod(e, b), bb = q.by_m.mod(b, group), pe = group * q.n_kv + kv;
   const int bi = q.by_mb.mod(bb, bq), c = q.by_rr.mod(r, rb), item = pe * q.nrb + bq * q.nr + rb;
-  return make_run(a.pre_parts, a.pre_parts.span[item], item, bi * q.rr + c, d);
+  return make_run(a.pre_parts, a.pre_parts.span[item], item, bi * q.rr + c, d, a.pre_ctas, a.err);
 }
 
 __device__ __forceinline__ float warp_max(float v) {
@@ -182,11 +186,12 @@ __global__ void __launch_bounds__(kMergeThreads, 4) merge_kernel(MergeArgs a) {
     int x;
     const int c = a.by_row_blocks.mod(blockIdx.x, x) * kMergeRows + warp;
     const int2 cut = a.has_prefix ? make_int2(x, 0) : a.own_parts.cut[x];
-    if (cut.x < 0) return;
+    if (cut.x < 0 || !in_bounds(cut.x, a.own_items, a.err)) return;
     int e;
     const int r = g.by_nrb.mod(cut.x, e) * g.rr + c;
     if (c >= g.rr || r >= g.R) return;
-    const Run own = make_run(a.own_parts, a.has_prefix ? a.own_parts.span[x] : make_int2(x, cut.y), cut.x, c, D);
+    const Run own = make_run(a.own_parts, a.has_prefix ? a.own_parts.span[x] : make_int2(x, cut.y), cut.x, c, D,
+                             a.own_ctas, a.err);
     const Run pre = prefix_run(a, e, r, D);
     const int n = pre.n + own.n;
     float2 mine = part_ml(pre, own, lane);
@@ -247,7 +252,7 @@ __global__ void __launch_bounds__(kMergeThreads, 4) merge_kernel(MergeArgs a) {
 #pragma unroll 1
   for (int r = warp; r < g.R; r += kMergeThreads / 32) {
     const int2 span = a.own_parts.span[e];  // the rows are one block: item e
-    const Run own = make_run(a.own_parts, span, e, r, D), pre = prefix_run(a, e, r, D);
+    const Run own = make_run(a.own_parts, span, e, r, D, a.own_ctas, a.err), pre = prefix_run(a, e, r, D);
     const float v = pre.n + own.n > 1 || a.has_prefix ? merged_lse2(pre, own, part_ml(pre, own, lane), lane)
                                                       : a.lse2[static_cast<size_t>(e) * g.R + r];
     if (lane == 0) {
@@ -297,11 +302,11 @@ __global__ void __launch_bounds__(kMergeThreads, 3) merge_rows_kernel(MergeArgs 
   int x;
   const int c0 = (a.by_row_blocks.mod(blockIdx.x, x) * (kMergeThreads / 32) + warp) * RW, c = c0 + sub;
   const int2 cut = a.own_parts.cut[x];
-  if (cut.x < 0) return;
+  if (cut.x < 0 || !in_bounds(cut.x, a.own_items, a.err)) return;
   int e;
   const int r0 = g.by_nrb.mod(cut.x, e) * g.rr, rows = min(g.rr, g.R - r0);  // of the row block
   if (c0 >= rows) return;
-  const Run run = make_run(a.own_parts, make_int2(x, cut.y), cut.x, c0, D);
+  const Run run = make_run(a.own_parts, make_int2(x, cut.y), cut.x, c0, D, a.own_ctas, a.err);
   const int n = run.n, part = run.rows;
   const bool mine = c < rows;
   auto ml = [&](int i) {
@@ -448,7 +453,11 @@ cudaError_t launch_attend_merge(const Shape& s, const AttendArgs& a, const AtLay
     m.pre = l.prefix.geo;
     m.pre.len = a.plen;
     m.pre_parts = l.prefix.parts(a.ws);
+    m.pre_ctas = l.prefix.grid;
   }
+  m.own_items = static_cast<int>(l.own.items);
+  m.own_ctas = l.own.grid;
+  m.err = a.err;
   // Many rows in few parts are bound by the instructions of a row, few rows in many parts by the latency of a
   // part.  A call with merge_rows_kernel and with merge_kernel: a prompt of 4096 tokens, 32 heads 143 and 153 us;
   // 128 caches of 4224 keys, 256 rows 75 and 85 us; 256 caches of 2176 keys, 128 rows 67 and 73 us.

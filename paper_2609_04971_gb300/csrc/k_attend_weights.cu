@@ -476,6 +476,7 @@ __global__ void __launch_bounds__(kAtTile) weights_merge_kernel(WArgs a) {
   if (n == 0) return;
   const uint32_t per = a.u0[static_cast<size_t>(a.I) * a.tiles], u = a.u0[static_cast<size_t>(e) * a.tiles + t];
   const int j = t * kAtTile + threadIdx.x;
+  if (!in_bounds(static_cast<long long>(u) + n - 1, static_cast<long long>(per) * a.ctas, a.err)) return;
   uint32_t first, last;
   if (!at_split_over(u, n, per, a.ctas, first, last) || j >= len) return;
   float sum = 0.f;

@@ -279,7 +279,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) evict_move_in_place
   const int e = blockIdx.x, tid = threadIdx.x;
   grid_dependency_wait();
   const int2 plan = a.plan[e];
-  if (plan.x < 0) return;
+  if (plan.x < 0 || !in_bounds(plan.x, min(a.budget, s.cap) + 1, a.err) || !in_bounds(plan.y, plan.x + 1, a.err)) return;
   const int first = plan.y, end = plan.x;
   const int* kept = a.kept + static_cast<size_t>(e) * a.budget;
   const int col = tid % kRowVec, r0 = tid / kRowVec;
@@ -333,7 +333,9 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(Shape s, Evict
   const int e = blockIdx.x / chunks, i0 = blockIdx.x % chunks * kMoveRows;
   const int tid = threadIdx.x;
   grid_dependency_wait();
-  const int n = min(kMoveRows, a.plan[e].x - i0);
+  const int kept = a.plan[e].x;
+  if (kept >= 0 && !in_bounds(kept, min(a.budget, s.cap) + 1, a.err)) return;
+  const int n = min(kMoveRows, kept - i0);
   if (tid < kMoveRows) rows[tid] = tid < n ? __ldcg(a.kept + static_cast<size_t>(e) * a.budget + i0 + tid) : 0;
   if (n <= 0) return;
   __syncthreads();

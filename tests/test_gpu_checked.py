@@ -76,6 +76,16 @@ def test_checked_flavour_parity_suites_run_clean():
     assert r.returncode == 0, r.stdout[-4000:] + r.stderr[-2000:]
 
 
+def test_checked_flavour_attention_and_eviction_run_clean():
+    """Attention, its merges, the accumulated weights and eviction likewise: no check fires (bkv_sync would raise
+    BKV_EBOUNDS) and the results match the 64-bit references."""
+    tests = ["tests/test_gpu_attend.py", "tests/test_gpu_attend_args.py",
+             "tests/test_gpu_attend_tiles.py::test_uneven_row_blocks_of_several_groups"]
+    r = subprocess.run([sys.executable, "-m", "pytest", "-x", "-q", "-p", "no:cacheprovider", *tests], cwd=ROOT,
+                       env=_checked_env(), capture_output=True, text=True, timeout=1500)
+    assert r.returncode == 0, r.stdout[-4000:] + r.stderr[-2000:]
+
+
 def test_allocation_failure_at_each_allocation_of_create():
     # 64 instances x 32768 rows: the score scratch alone is 8 MB, so a buffer left behind by a
     # failed create would show in the device's free memory after a few dozen failures
