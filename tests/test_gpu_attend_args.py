@@ -115,3 +115,41 @@ def test_overlapping_outputs_of_an_eviction_are_refused():
         assert bool((L == budget).all()) and bool((kept >= 0).all())
     finally:
         bk.close()
+
+
+@pytest.mark.parametrize("cap", [300, 5000, 12000])
+def test_refused_instances_are_untouched(cap):
+    """Lengths out of range among good ones: kept rows -1, new length 0, and nothing else of the instance written,
+    in place and into another cache."""
+    shape, d, budget = (1, 2, 3), 64, 120
+    K, V = (torch.randn(*shape, cap, d, device="cuda").bfloat16() for _ in "KV")
+    w = torch.rand(*shape, cap, device="cuda")
+    L = torch.tensor([cap + 1, cap, -1, 121, -2 ** 31, 2 ** 31 - 1], dtype=torch.int32, device="cuda").view(shape)
+    bad = [0, 2, 4, 5]
+    bk = _bk(2, 3, 3, d, cap, window=8, n_beacons=0, n_prefix=2)
+    try:
+        for in_place in (True, False):
+            rows = cap if in_place else budget
+            Ko, Vo, wo = (K.clone(), V.clone(), w.clone()) if in_place else (
+                torch.randn(*shape, rows, d, device="cuda").bfloat16(),
+                torch.randn(*shape, rows, d, device="cuda").bfloat16(), torch.full((*shape, rows), 7.0, device="cuda"))
+            before = [t.clone() for t in (Ko, Vo, wo)]
+            src = (Ko, Vo, wo) if in_place else (K, V, w)
+            kept, new = bk.evict(*src, L=L, budget=budget, K_out=Ko, V_out=Vo, weights_out=wo)
+            with pytest.raises(bkv.BkvError) as ei:
+                bk.sync()
+            assert ei.value.code == bkv.BKV_EINVAL
+            bk.sync()
+            flat = lambda t: t.flatten(0, 2)  # noqa: E731
+            assert new.flatten().tolist() == [0, budget, 0, budget, 0, 0]
+            for e in bad:
+                assert bool((flat(kept)[e] == -1).all())
+                for x, y in zip((Ko, Vo, wo), before):
+                    assert torch.equal(flat(x)[e], flat(y)[e])
+            for e in (1, 3):
+                at = flat(kept)[e].long()
+                assert bool((at[1:] > at[:-1]).all())
+                for x, y in zip((Ko, Vo, wo), (K, V, w)):
+                    assert torch.equal(flat(x)[e, :budget], flat(y)[e, at])
+    finally:
+        bk.close()
