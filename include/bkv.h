@@ -31,8 +31,9 @@
  * Memory.  Every tensor argument is a DEVICE pointer owned by the caller,
  * row-major and contiguous, aligned to 16 bytes, unless the description says
  * "host".  bf16 tensors hold IEEE binary32 values truncated to their top 16
- * bits (bfloat16).  The library owns only what bkv_create allocates (beacon
- * state and scratch) and frees it in bkv_destroy.
+ * bits (bfloat16).  The library owns only what bkv_create (beacon state and
+ * scratch) and bkv_attend_reserve (workspace) allocate and frees it in
+ * bkv_destroy.
  *
  * Streams.  All work is enqueued on the CUDA stream given to bkv_create (or
  * bkv_set_stream); calls return before it completes.  Outputs are valid once
@@ -319,8 +320,12 @@ int bkv_attend_shared(bkv_ctx* ctx, const void* q, int32_t n_q, const void* Kp, 
  * Makes the workspace of bkv_attend (n_groups = 0) or bkv_attend_shared for
  * calls with n_q queries per head, with or without weights.  The workspace only
  * grows, so a reservation for the largest call serves the smaller ones of the
- * same kind.  Waits for the context's stream when it has to reallocate; call it
- * before capturing a graph.  BKV_ENOMEM leaves the previous workspace in place.
+ * same kind.  It takes some 4 bytes for each element of o, 8 for
+ * bkv_attend_shared (up to twice that where G * n_q is a little more than 256),
+ * 40 MB at most beside that, and with weights and up to 32 query rows per KV
+ * head (G * n_q) 4 bytes for each such row and cache row.  Waits for the
+ * context's stream when it has to reallocate; call it before capturing a graph.
+ * BKV_ENOMEM leaves the previous workspace in place.
  */
 int bkv_attend_reserve(bkv_ctx* ctx, int32_t n_q, int32_t n_groups, int weights);
 
@@ -349,7 +354,11 @@ int bkv_attend_reserve(bkv_ctx* ctx, int32_t n_q, int32_t n_groups, int weights)
  *   kept_idx_out  int32 [n_layers][batch][n_kv_heads][budget]: kept rows, then -1.
  *   len_out       int32 [n_layers][batch][n_kv_heads] or NULL: min(L, budget).
  *                 It may be L itself, but not a part of it.
- * The beacon state plays no part.
+ * n_prefix and window are the context's, whose limit on G * window stems from
+ * the scoring queries of bkv_compress.  An eviction does not look at query
+ * heads: a context of its own with n_q_heads = n_kv_heads and n_beacons = 0
+ * serves it with every window of 1 to 64, whatever the group size.  The beacon
+ * state plays no part.
  */
 int bkv_evict(bkv_ctx* ctx, const void* K, const void* V, const float* weights, const int32_t* L, int32_t budget,
               void* K_out, void* V_out, float* weights_out, int32_t capacity_out, int32_t* kept_idx_out,

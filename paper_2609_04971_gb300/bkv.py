@@ -525,7 +525,8 @@ class BeaconKV:
     def attend(self, q, K, V, *, length, scale=None, weights=None, o_out=None, lse_out=None):
         """Attention of one layer's newest queries over its caches (bkv_attend): q [batch, n_q_heads, n_q,
         head_dim], K and V [batch, n_kv_heads, capacity, head_dim], length int32 [batch, n_kv_heads];
-        weights fp32 [batch, n_kv_heads, capacity] is added to.  Returns (o, lse)."""
+        weights fp32 [batch, n_kv_heads, capacity] is added to.  o_out and lse_out share no memory with q or the
+        caches.  Returns (o, lse)."""
         n_q, o, lse = self._attend_args(q, K, V, length, weights, o_out, lse_out)
         bkv_attend(self.ctx, q, n_q, K, V, length, scale or 0.0, o, lse, weights)
         return o, lse
@@ -550,7 +551,8 @@ class BeaconKV:
               len_out=None):
         """Eviction by accumulated weight (bkv_evict), in place or, with K_out, V_out and weights_out of
         [n_layers, batch, n_kv_heads, capacity_out] rows, into another cache.  L: int32 CUDA tensor
-        [n_layers, batch, n_kv_heads].  Returns (kept rows, new lengths)."""
+        [n_layers, batch, n_kv_heads]; len_out may be L.  A window that the context's limit on G * window refuses
+        is taken by a context of its own with n_q_heads = n_kv_heads.  Returns (kept rows, new lengths)."""
         c = self.cfg
         given = (K_out is not None) + (V_out is not None) + (weights_out is not None)
         if given == 0:

@@ -19,7 +19,7 @@ enum DevErr : int {
   kDevTimeoutDrain = 4,
   kDevTimeoutCluster = 5,
   kDevTimeoutSelftest = 6,
-  kDevBadLength = 7,  // a per-instance cache length outside 1..capacity (bkv_compress_ragged)
+  kDevBadLength = 7,  // a cache length outside 1..capacity (bkv_compress_ragged) or 0..capacity (attend, evict)
   kDevBounds = 8,     // a device-side bounds check failed (builds with BKV_CHECKED only)
 };
 

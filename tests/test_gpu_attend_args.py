@@ -153,3 +153,29 @@ def test_refused_instances_are_untouched(cap):
                     assert torch.equal(flat(x)[e, :budget], flat(y)[e, at])
     finally:
         bk.close()
+
+
+@pytest.mark.parametrize("G,window", [(8, 32), (16, 64), (1, 64)])
+def test_windows_past_the_scoring_limit(G, window):
+    """G * window is bounded by a compress's scoring queries.  Eviction does not see query heads: a context with as
+    many query heads as KV heads takes every window up to 64."""
+    with pytest.raises(bkv.BkvError):
+        _bk(2, 2 * 64, 2, 64, 200, window=window, n_beacons=0)  # 64 query heads to a KV head
+    b, hkv, d, cap, budget = 2, 2, 64, 200, 100
+    shape = (1, b, hkv)
+    K, V = (torch.randn(*shape, cap, d, device="cuda").bfloat16() for _ in "KV")
+    w = torch.zeros(*shape, cap, device="cuda")
+    lens = torch.full(shape, cap, dtype=torch.int32, device="cuda")
+    q = torch.randn(b, G * hkv, 1, d, device="cuda").bfloat16()
+    att, ev = _bk(b, G * hkv, hkv, d, cap), _bk(b, hkv, hkv, d, cap, window=window, n_beacons=0)
+    try:
+        att.reserve_attend(weights=True)
+        att.attend(q, K[0], V[0], length=lens[0], weights=w[0])
+        att.sync()
+        kept, new = ev.evict(K, V, w, L=lens, budget=budget)
+        ev.sync()
+        assert bool((new == budget).all())
+        assert bool((kept[..., -window:] == torch.arange(cap - window, cap, device="cuda")).all())
+    finally:
+        att.close()
+        ev.close()
