@@ -325,7 +325,8 @@ int bkv_attend_shared(bkv_ctx* ctx, const void* q, int32_t n_q, const void* Kp, 
  * 40 MB at most beside that, and with weights and up to 32 query rows per KV
  * head (G * n_q) 4 bytes for each such row and cache row.  Waits for the
  * context's stream when it has to reallocate; call it before capturing a graph.
- * BKV_ENOMEM leaves the previous workspace in place.
+ * A graph that was captured before a larger reservation keeps the workspace it
+ * was captured with, until bkv_destroy.  BKV_ENOMEM leaves the previous workspace in place.
  */
 int bkv_attend_reserve(bkv_ctx* ctx, int32_t n_q, int32_t n_groups, int weights);
 

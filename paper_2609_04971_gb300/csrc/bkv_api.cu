@@ -136,6 +136,12 @@ void free_all(bkv_ctx* c) {
   cudaFree(c->n_work);
   cudaFree(c->rag);
   cudaFree(c->attend_ws);
+  while (c->attend_ws_old) {
+    bkv_ctx::Workspace* w = c->attend_ws_old;
+    c->attend_ws_old = w->next;
+    cudaFree(w->p);
+    delete w;
+  }
   if (c->switch_ev) cudaEventDestroy(c->switch_ev);
 }
 

@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <new>
 
 #include "bkv.h"
 #include "bkv_ctx.h"
@@ -83,6 +84,12 @@ int attend(bkv_ctx* ctx, bkv::AttendArgs& a, double scale) {
     return fail(ctx, BKV_ESTATE, "this call needs %zu bytes of workspace, bkv_attend_reserve made %zu", l.bytes,
                 ctx->attend_ws_bytes);
   a.ws = ctx->attend_ws;
+  if (!ctx->attend_ws_captured) {
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    // on an error the launches report what is wrong with the stream
+    if (cudaStreamIsCapturing(ctx->stream, &status) != cudaSuccess) cudaGetLastError();
+    ctx->attend_ws_captured = status != cudaStreamCaptureStatusNone;
+  }
   a.err = ctx->err;
   cudaError_t e;
   {
@@ -126,7 +133,17 @@ int bkv_attend_reserve(bkv_ctx* ctx, int32_t n_q, int32_t n_groups, int weights)
     cudaFree(ws);
     return cuda_fail(ctx, e, "stream synchronize");
   }
-  cudaFree(ctx->attend_ws);
+  if (ctx->attend_ws_captured) {
+    auto* old = new (std::nothrow) bkv_ctx::Workspace{ctx->attend_ws, ctx->attend_ws_old};
+    if (!old) {
+      cudaFree(ws);
+      return fail(ctx, BKV_ENOMEM, "no host memory");
+    }
+    ctx->attend_ws_old = old;
+    ctx->attend_ws_captured = false;
+  } else {
+    cudaFree(ctx->attend_ws);
+  }
   ctx->attend_ws = ws;
   ctx->attend_ws_bytes = need;
   return BKV_OK;

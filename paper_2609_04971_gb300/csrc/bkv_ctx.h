@@ -54,6 +54,13 @@ struct bkv_ctx {
   // attention (bkv_attend_reserve): partial results, logits and normalisers of one call
   unsigned char* attend_ws = nullptr;
   size_t attend_ws_bytes = 0;
+  bool attend_ws_captured = false;  // a graph may hold its address
+  // workspaces that a larger one replaced while a graph may hold their address; freed with the context
+  struct Workspace {
+    unsigned char* p;
+    Workspace* next;
+  };
+  Workspace* attend_ws_old = nullptr;
   cudaEvent_t switch_ev = nullptr;  // orders a new stream after the previous one (bkv_set_stream)
   std::string last_error;
   // per-kernel timing

@@ -1,9 +1,11 @@
-"""Arguments that share memory, and eviction of instances whose length is refused."""
+"""Arguments that share memory, workspaces that graphs hold, and what an eviction refuses."""
+import math
+
 import pytest
 import torch
 
 from paper_2609_04971_gb300 import bkv
-from tests.test_gpu_attend import _bk, _inputs, _lens
+from tests.test_gpu_attend import _bk, _inputs, _lens, check, reference
 
 pytestmark = pytest.mark.gpu
 
@@ -115,6 +117,56 @@ def test_overlapping_outputs_of_an_eviction_are_refused():
         assert bool((L == budget).all()) and bool((kept >= 0).all())
     finally:
         bk.close()
+
+
+def test_a_graph_outlives_a_larger_reservation():
+    """A decode step is captured, then a prompt reserves more: the graph's workspace stays its own, so that neither
+    the allocator's next tensors nor calls in the new workspace reach it."""
+    b, hq, hkv, d, cap = 2, 8, 2, 128, 6000
+    q, K, V = _inputs(b, hq, hkv, d, cap, 1, seed=10)
+    qp, Kp, Vp = _inputs(b, hq, hkv, d, cap, 300, seed=11)
+    lens, lens_p = _lens(b, hkv, [6000, 5, 200, 5128]), _lens(b, hkv, [300, 4000, 900, 301])
+    w = torch.zeros(b, hkv, cap, device="cuda")
+    o = torch.empty(b, hq, 1, d, dtype=torch.bfloat16, device="cuda")
+    lse = torch.empty(b, hq, 1, device="cuda")
+    (o64, l64, w64), (to, tl, tw) = reference(q, K, V, lens)
+    (op64, lp64, _), (top, tlp, _) = reference(qp, Kp, Vp, lens_p)
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    bk = _bk(b, hq, hkv, d, cap, stream=stream)
+    free = lambda: torch.cuda.mem_get_info()[0]  # noqa: E731
+    try:
+        with torch.cuda.stream(stream):
+            bk.reserve_attend(weights=True)
+            bk.attend(q, K, V, length=lens, weights=w, o_out=o, lse_out=lse)
+            bk.sync()
+            graphs = []
+            for n_q in (None, 64, 300):  # each reservation is larger than the one before
+                if n_q:
+                    bk.reserve_attend(n_q=n_q, weights=True)
+                graph = torch.cuda.CUDAGraph()
+                with torch.cuda.graph(graph, stream=stream):
+                    bk.attend(q, K, V, length=lens, weights=w, o_out=o, lse_out=lse)
+                graphs.append(graph)
+            junk = [torch.full((n,), math.nan, device="cuda") for n in [1 << 20] * 8 + [1 << 22] * 4]
+            for graph in graphs:
+                for t in (o, lse, w):
+                    t.fill_(math.nan if t is not w else 0)
+                op, lp = bk.attend(qp, Kp, Vp, length=lens_p)
+                graph.replay()
+                bk.sync()
+                check(o, o64, to, "o")
+                check(lse, l64, tl, "lse")
+                check(w, w64, tw, "weights")
+                check(op, op64, top, "o of the prompt")
+                check(lp, lp64, tlp, "lse of the prompt")
+            assert all(bool(t.isnan().all()) for t in junk)
+            del graphs, graph
+        torch.cuda.synchronize()
+        before = free()
+    finally:
+        bk.close()
+    assert free() > before  # all workspaces, the old ones among them
 
 
 @pytest.mark.parametrize("cap", [300, 5000, 12000])
