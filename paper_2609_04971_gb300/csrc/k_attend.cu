@@ -34,8 +34,9 @@ size_t align_up(size_t n) { return (n + 255) / 256 * 256; }
 
 // Row blocks of m sequences x R rows: all rows of an instance in one block while there are at most 128
 // of them (keys as lanes, k_attend_tiles.cuh), else blocks of at most 256, as even as 16-row steps allow (rows
-// as lanes, k_attend_rows.cu).  Both sides of the 128, head_dim 128, 128 caches of 4224 keys: 80 rows 54 and 64 us,
-// 128 rows 64 and 70 us; 160 rows (two blocks, and one) 102 and 73 us, 256 rows 119 and 85 us.
+// as lanes, k_attend_rows.cu).  Both sides of the 128, head_dim 128, 128 caches of 4224 keys: 80 rows 51 and 59 us,
+// 128 rows 60 and 63 us; 144 rows (two blocks, and one) 90 and 64 us, 256 rows 105 and 72 us; 8 caches of 32768 keys:
+// 80 rows 35 and 40, 128 rows 42.5 and 42.5, 144 rows 52 and 43 us.
 AtPlan make_plan(const Shape& s, int I, int m, int R, int n_q, bool causal, int cap, int len_div, int sms,
                  bool& too_large) {
   AtPlan p{};
@@ -459,9 +460,12 @@ cudaError_t launch_attend_merge(const Shape& s, const AttendArgs& a, const AtLay
   m.own_ctas = l.own.grid;
   m.err = a.err;
   // Many rows in few parts are bound by the instructions of a row, few rows in many parts by the latency of a
-  // part.  A call with merge_rows_kernel and with merge_kernel: a prompt of 4096 tokens, 32 heads 143 and 153 us;
-  // 128 caches of 4224 keys, 256 rows 75 and 85 us; 256 caches of 2176 keys, 128 rows 67 and 73 us.
-  const bool many_rows = !l.has_prefix && !l.logits && 4 * l.own.items >= l.own.grid && l.own.geo.rr > kLogitRows;
+  // part; with merge_rows_kernel an item has 8 parts at most on average.  A call with it and with merge_kernel,
+  // head_dim 128: a prompt of 4096 tokens, 32 heads 143 and 153 us; 128 caches of 4224 keys, 256 rows 72 and 82,
+  // 128 rows 60 and 64, 44 rows 50 and 51 us; 32 caches of 8320 keys, 256 rows 46 and 50, 128 rows 41 and 42 us; 24
+  // of them, 256 rows 40.5 and 43.5, 128 rows 37 and 37 us; 16 caches of 16384 keys, 256 rows 48 and 49, 128 rows 43
+  // and 41 us; 8 caches of 32768 keys, 256 rows 53 and 49, 128 rows 47 and 42, 44 rows 33.5 and 33 us.
+  const bool many_rows = !l.has_prefix && !l.logits && 8 * l.own.items >= l.own.grid && l.own.geo.rr > kLogitRows;
   const int block_rows = many_rows ? kMergeRows * kMergeWarpRows : kMergeRows;
   const int per_item = (l.own.geo.rr + block_rows - 1) / block_rows;
   m.by_row_blocks = FastDiv(per_item);

@@ -21,8 +21,14 @@ constexpr int kAtTile = 128;             // keys per tile
 constexpr uint32_t kAtBox = 128 * 128;   // [128 rows][64 bf16] swizzled box
 constexpr int kMaxRows = 256;            // query rows per row block
 // Query rows per KV head up to which the logits are kept for the weights, 4 bytes a row and key written and
-// read once more; beyond, the weights are recomputed from the keys.  head_dim 128, kept and recomputed: 128
-// caches of 4224 keys, 24 rows 71 and 84 us, 32 rows 89 and 85; 8 caches of 32768 keys, 32 rows 46 and 53 us.
+// read once more, row by row by the merge; beyond, the weights are recomputed from the keys by two more launches.
+// A call in us, kept and recomputed, by the number of caches and their keys:
+//   head_dim 128        4 rows       16 rows      24 rows      32 rows      44 rows       64 rows
+//   56 x 1088       15.0, 22.7   21.0, 23.3   25.9, 24.2   29.1, 24.2   35.9, 25.1   48.2, 26.5
+//   8 x 32768       30.2, 50.0   36.0, 50.7   40.8, 51.9   45.9, 52.5   53.7, 53.5   71.8, 54.5
+//   128 x 4224      52.5, 81.6   62.2, 82.7   73.4, 83.9   89.9, 84.4    111, 85.2    144, 85.9
+// (head_dim 64 crosses at the same rows.)  32 rows gain a seventh where the keys are many and the logits stay in L2
+// and lose a fifth on short caches; 24 rows gain a fifth or an eighth, or lose a twelfth.
 constexpr int kLogitRows = 32;
 constexpr float kMaxAbove = 32.f;        // log2 of how far p may exceed 1 before its reference moves
 constexpr float kRefFloor = -1e30f;
