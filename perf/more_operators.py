@@ -10,8 +10,9 @@ evict4   4-bit caches are cut to their budget by accumulated weight and compacte
 ``run`` is the plain form (elementary torch operations in 32 bits, 64 where a code is chosen) unless ``own`` is
 set, and then the framework's operators.
 
-A row of a 4-bit cache of head_dim d holds d / 8 words of 32 bits; word w holds the codes of elements w, w + d / 8,
-.., w + 7 d / 8, the first in its lowest four bits.  A row's scales are fp16 [2 (K, V)][d / 32][2 (step, low)].
+A row of a 4-bit cache of head_dim d holds d / 8 words of 32 bits with eight codes each, the first in the lowest four
+bits.  Word t d / 32 + g of a row of K (t < 4) holds elements 32 g + 8 t .. 32 g + 8 t + 7; word w of a row of V holds
+elements w, w + d / 8, .., w + 7 d / 8.  A row's scales are fp16 [2 (K, V)][d / 32][2 (step, low)].
 """
 import math
 
@@ -150,16 +151,24 @@ def _quantise(x, dtype):
     return code.flatten(-2), step, low
 
 
-def _words(code):
-    """Codes [.., d] as the bytes of their words, [.., d / 2]."""
-    n = code.to(torch.uint8).unflatten(-1, (8, -1)).transpose(-1, -2)
+def _words(code, which):
+    """Codes [.., d] of rows of K (which: 0) or V (1) as the bytes of their words, [.., d / 2]."""
+    n = code.to(torch.uint8)
+    if which == 0:
+        n = n.unflatten(-1, (-1, 4, 8)).transpose(-2, -3).flatten(-3, -2)
+    else:
+        n = n.unflatten(-1, (8, -1)).transpose(-1, -2)
     return (n[..., 0::2] | (n[..., 1::2] << 4)).flatten(-2).contiguous()
 
 
 def _values(packed, scales, which, dtype):
-    """Rows of a 4-bit cache (which: 0 for K, 1 for V) as numbers."""
+    """Rows of a 4-bit cache as numbers."""
     p = packed.unflatten(-1, (-1, 4))
-    code = torch.stack((p & 15, p >> 4), -1).flatten(-2).transpose(-1, -2).flatten(-2)
+    code = torch.stack((p & 15, p >> 4), -1).flatten(-2)
+    if which == 0:
+        code = code.unflatten(-2, (4, -1)).transpose(-2, -3).flatten(-3)
+    else:
+        code = code.transpose(-1, -2).flatten(-2)
     sc = scales[..., which, :, :].to(dtype)
     g = code.to(dtype).unflatten(-1, (-1, GROUP))
     return (sc[..., 1, None] + sc[..., 0, None] * g).flatten(-2)
@@ -175,7 +184,7 @@ def _cache4(gen, d, *lead):
             if which == 0:
                 x += 0.5 * _randn(gen, lead[-2], 1, d)
             code, step, low = _quantise(x, torch.float32)
-            out[i] = _words(code)
+            out[i] = _words(code, which)
             S4[i, ..., which, :, 0], S4[i, ..., which, :, 1] = step, low
     return K4, V4, S4
 
@@ -287,7 +296,7 @@ def _plain_pack(s):
     at = (torch.arange(b * hkv, device=DEV).view(b, hkv, 1) * cap + row)[there]
     for which, (src, codes, back) in enumerate(((s["K"], s["K4"], s["K_out"]), (s["V"], s["V4"], s["V_out"]))):
         code, step, low = _quantise(src[there], torch.float64)
-        packed = _words(code)
+        packed = _words(code, which)
         codes.view(-1, d // 2)[at] = packed
         flat = s["S4"].view(-1, 2, d // GROUP, 2)
         flat[at, which] = torch.stack((step, low), -1).to(torch.float16)
@@ -439,11 +448,11 @@ def _nearest_half(x):
     return torch.copysign(y, x)
 
 
-def _codes(words, d):
+def _codes(words, d, which):
     """Codes of rows of bytes, element by element of the format's definition."""
     out = torch.empty(*words.shape[:-1], d, dtype=torch.float64, device=DEV)
     for e in range(d):
-        w, x = e % (d // 8), e // (d // 8)
+        w, x = (e % 32 // 8 * (d // 32) + e // 32, e % 8) if which == 0 else (e % (d // 8), e // (d // 8))
         out[..., e] = ((words[..., 4 * w + x // 2] >> (4 * (x % 2))) & 15).double()
     return out
 
@@ -463,8 +472,8 @@ def _exact_attention(s):
                 continue
             if c["op"] == "attend4":
                 sc = s["S4"][x, y, :n].double().repeat_interleave(GROUP, 2)
-                keys = sc[:, 0, :, 1] + sc[:, 0, :, 0] * _codes(s["K4"][x, y, :n], d)
-                vals = sc[:, 1, :, 1] + sc[:, 1, :, 0] * _codes(s["V4"][x, y, :n], d)
+                keys = sc[:, 0, :, 1] + sc[:, 0, :, 0] * _codes(s["K4"][x, y, :n], d, 0)
+                vals = sc[:, 1, :, 1] + sc[:, 1, :, 0] * _codes(s["V4"][x, y, :n], d, 1)
             else:
                 keys, vals = s["K"][x, y, :n].double(), s["V"][x, y, :n].double()
             pos = torch.arange(n, device=DEV)[None, :]
