@@ -331,6 +331,62 @@ int bkv_attend_shared(bkv_ctx* ctx, const void* q, int32_t n_q, const void* Kp, 
 int bkv_attend_reserve(bkv_ctx* ctx, int32_t n_q, int32_t n_groups, int weights);
 
 /*
+ * Caches held in 4 bits.  A group of 32 consecutive elements x of a row keeps
+ *   low = fp16(min x), step = fp16((max x - low) / 15), both limited to 65504,
+ *   codes n = (x - low) / step rounded to the nearest of 0 .. 15 (0 for step 0),
+ * ties of each rounding to even, and stands for low + step * n.  An element must
+ * be finite; beyond +-65504 it counts as that.  One row takes 1.25 d bytes of K
+ * and V together instead of 4 d:
+ *   K4, V4   uint8 [batch][n_kv_heads][capacity][head_dim / 2], words of 32 bits
+ *            with eight codes each, the first in the lowest four bits.  Word
+ *            t d/32 + g of a row of K4 (t < 4) holds elements 32 g + 8 t ..
+ *            32 g + 8 t + 7; word w of a row of V4 holds elements w, w + d/8, ..,
+ *            w + 7 d/8.
+ *   S4       fp16 [batch][n_kv_heads][capacity][2][head_dim / 32][2]: (step, low)
+ *            of K's groups, then of V's.  Steps and lows must be finite, steps
+ *            >= 0.
+ *
+ * bkv_pack4 writes new rows into one layer's 4-bit caches (a prompt's, or a
+ * decode step's one): row i of K and V becomes row first + i of its cache, for
+ * first + i < len.
+ *   K, V      bf16 [batch][n_kv_heads][n_rows][head_dim].
+ *   first     DEVICE int32 [batch][n_kv_heads]: rows that each cache held before,
+ *             0 .. len, or NULL for none.
+ *   len       DEVICE int32 [batch][n_kv_heads]: rows that it holds now, 0 ..
+ *             capacity.  With a first or len outside these ranges nothing of the
+ *             cache is written and the next bkv_sync returns BKV_EINVAL.
+ * bkv_unpack4 is its inverse: row first + i of a cache, where that is below len,
+ * to row i of K and V as bf16 numbers (one rounding); the other rows of K and V
+ * keep what they held.  Outputs overlap neither an input nor one another
+ * (BKV_EINVAL), also where no row of theirs is used.  n_rows >= 0, batch *
+ * n_kv_heads * n_rows below 2^31.
+ */
+int bkv_pack4(bkv_ctx* ctx, const void* K, const void* V, int32_t n_rows, const int32_t* first, const int32_t* len,
+              void* K4, void* V4, void* S4);
+int bkv_unpack4(bkv_ctx* ctx, const void* K4, const void* V4, const void* S4, int32_t n_rows, const int32_t* first,
+                const int32_t* len, void* K, void* V);
+
+/*
+ * bkv_attend over 4-bit caches: the same formulas, arguments and limits, with
+ * K and V the numbers that K4, V4 and S4 stand for.
+ * Up to 96 query rows per KV head (G * n_q), 32 with weights, the codes are
+ * multiplied as they are: the logits are fp32, and only the products of an
+ * attention weight and a step are rounded, to fp16.  More rows read the caches
+ * unpacked to bf16 into the workspace, and then all is as in bkv_attend.
+ * Queries up to 2^100 in magnitude.
+ * BKV_ESTATE when the workspace that bkv_attend4_reserve made is too small.
+ */
+int bkv_attend4(bkv_ctx* ctx, const void* q, int32_t n_q, const void* K4, const void* V4, const void* S4,
+                const int32_t* len, double scale, void* o, float* lse_out, float* weights);
+
+/*
+ * bkv_attend_reserve for bkv_attend4, out of the same workspace.  Past the rows
+ * that are read code by code it holds one layer's caches in bf16 beside what
+ * bkv_attend takes.
+ */
+int bkv_attend4_reserve(bkv_ctx* ctx, int32_t n_q, int weights);
+
+/*
  * Eviction by accumulated attention weight, for every instance's cache of all
  * layers: of the L rows, the first n_prefix, the last `window` and the (budget
  * - n_prefix - window) others with the largest weight stay, in ascending order
@@ -364,6 +420,15 @@ int bkv_attend_reserve(bkv_ctx* ctx, int32_t n_q, int32_t n_groups, int weights)
 int bkv_evict(bkv_ctx* ctx, const void* K, const void* V, const float* weights, const int32_t* L, int32_t budget,
               void* K_out, void* V_out, float* weights_out, int32_t capacity_out, int32_t* kept_idx_out,
               int32_t* len_out);
+
+/*
+ * bkv_evict for 4-bit caches of all layers: K4, V4 and S4 (and their outputs) are
+ * [n_layers] times the caches of bkv_pack4, rows of capacity_out in the outputs.
+ * In place means all four outputs are K4, V4, S4 and weights themselves.
+ */
+int bkv_evict4(bkv_ctx* ctx, const void* K4, const void* V4, const void* S4, const float* weights, const int32_t* L,
+               int32_t budget, void* K4_out, void* V4_out, void* S4_out, float* weights_out, int32_t capacity_out,
+               int32_t* kept_idx_out, int32_t* len_out);
 
 /*
  * Copies the beacon state to / from caller buffers (checkpoint / resume):
@@ -473,7 +538,10 @@ int bkv_debug_fail_alloc(int32_t nth);
 #define BKV_K_ATTEND_MERGE 9
 #define BKV_K_ATTEND_WEIGHTS 10
 #define BKV_K_EVICT 11
-#define BKV_NUM_KERNELS 12
+#define BKV_K_PACK4 12
+#define BKV_K_UNPACK4 13
+#define BKV_K_ATTEND4 14
+#define BKV_NUM_KERNELS 15
 int bkv_profile_enable(bkv_ctx* ctx, int on);
 int bkv_profile_read(bkv_ctx* ctx, double* ms, int64_t* launches, int32_t n_kernels);
 

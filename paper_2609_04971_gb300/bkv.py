@@ -25,7 +25,7 @@ BKV_ESTATE = -5
 BKV_EBOUNDS = -6
 
 KERNEL_NAMES = ("fps_init", "update", "qobs", "score", "select_gather", "keep_all", "cfps", "rope_stage",
-                "attend", "attend_merge", "attend_weights", "evict")
+                "attend", "attend_merge", "attend_weights", "evict", "pack4", "unpack4", "attend4")
 
 
 # bkv_config.flags options (include/bkv.h)
@@ -84,6 +84,12 @@ def load_library(path: str | None = None, build: bool = True):
                                                  _P, _P, _P, ctypes.c_double, _P, _P, _P]),
             "bkv_attend_reserve": (ctypes.c_int, [_P, ctypes.c_int32, ctypes.c_int32, ctypes.c_int]),
             "bkv_evict": (ctypes.c_int, [_P, _P, _P, _P, _P, ctypes.c_int32, _P, _P, _P, ctypes.c_int32, _P, _P]),
+            "bkv_pack4": (ctypes.c_int, [_P, _P, _P, ctypes.c_int32, _P, _P, _P, _P, _P]),
+            "bkv_unpack4": (ctypes.c_int, [_P, _P, _P, _P, ctypes.c_int32, _P, _P, _P, _P]),
+            "bkv_attend4": (ctypes.c_int, [_P, _P, ctypes.c_int32, _P, _P, _P, _P, ctypes.c_double, _P, _P, _P]),
+            "bkv_attend4_reserve": (ctypes.c_int, [_P, ctypes.c_int32, ctypes.c_int]),
+            "bkv_evict4": (ctypes.c_int, [_P, _P, _P, _P, _P, _P, ctypes.c_int32, _P, _P, _P, _P, ctypes.c_int32, _P,
+                                          _P]),
             "bkv_get_state": (ctypes.c_int, [_P, _P, _P, _P]),
             "bkv_set_state": (ctypes.c_int, [_P, _P, _P, _P]),
             "bkv_get_cfps_state": (ctypes.c_int, [_P, _P, _P]),
@@ -263,6 +269,48 @@ def bkv_evict(ctx, K: torch.Tensor, V: torch.Tensor, weights: torch.Tensor, L: t
                           _ptr(L, i32, "L"), int(budget), _ptr(K_out, bf16, "K_out"), _ptr(V_out, bf16, "V_out"),
                           _ptr(weights_out, f32, "weights_out"), int(capacity_out), _ptr(kept_idx_out, i32, "kept"),
                           _ptr(len_out, i32, "len_out")), "bkv_evict", ctx)
+
+
+def bkv_pack4(ctx, K: torch.Tensor, V: torch.Tensor, n_rows: int, first: torch.Tensor | None, length: torch.Tensor,
+              K4: torch.Tensor, V4: torch.Tensor, S4: torch.Tensor) -> None:
+    bf16, u8, i32 = torch.bfloat16, torch.uint8, torch.int32
+    _check(_l().bkv_pack4(ctx, _ptr(K, bf16, "K"), _ptr(V, bf16, "V"), int(n_rows), _ptr(first, i32, "first"),
+                          _ptr(length, i32, "length"), _ptr(K4, u8, "K4"), _ptr(V4, u8, "V4"),
+                          _ptr(S4, torch.float16, "S4")), "bkv_pack4", ctx)
+
+
+def bkv_unpack4(ctx, K4: torch.Tensor, V4: torch.Tensor, S4: torch.Tensor, n_rows: int, first: torch.Tensor | None,
+                length: torch.Tensor, K: torch.Tensor, V: torch.Tensor) -> None:
+    bf16, u8, i32 = torch.bfloat16, torch.uint8, torch.int32
+    _check(_l().bkv_unpack4(ctx, _ptr(K4, u8, "K4"), _ptr(V4, u8, "V4"), _ptr(S4, torch.float16, "S4"), int(n_rows),
+                            _ptr(first, i32, "first"), _ptr(length, i32, "length"), _ptr(K, bf16, "K"),
+                            _ptr(V, bf16, "V")), "bkv_unpack4", ctx)
+
+
+def bkv_attend4(ctx, q: torch.Tensor, n_q: int, K4: torch.Tensor, V4: torch.Tensor, S4: torch.Tensor,
+                length: torch.Tensor, scale: float, o: torch.Tensor, lse_out: torch.Tensor | None = None,
+                weights: torch.Tensor | None = None) -> None:
+    bf16, f32, u8 = torch.bfloat16, torch.float32, torch.uint8
+    _check(_l().bkv_attend4(ctx, _ptr(q, bf16, "q"), int(n_q), _ptr(K4, u8, "K4"), _ptr(V4, u8, "V4"),
+                            _ptr(S4, torch.float16, "S4"), _ptr(length, torch.int32, "length"), float(scale),
+                            _ptr(o, bf16, "o"), _ptr(lse_out, f32, "lse_out"), _ptr(weights, f32, "weights")),
+           "bkv_attend4", ctx)
+
+
+def bkv_attend4_reserve(ctx, n_q: int, weights: bool = False) -> None:
+    _check(_l().bkv_attend4_reserve(ctx, int(n_q), int(bool(weights))), "bkv_attend4_reserve", ctx)
+
+
+def bkv_evict4(ctx, K4: torch.Tensor, V4: torch.Tensor, S4: torch.Tensor, weights: torch.Tensor, L: torch.Tensor,
+               budget: int, K4_out: torch.Tensor, V4_out: torch.Tensor, S4_out: torch.Tensor,
+               weights_out: torch.Tensor, capacity_out: int, kept_idx_out: torch.Tensor,
+               len_out: torch.Tensor | None = None) -> None:
+    u8, f16, f32, i32 = torch.uint8, torch.float16, torch.float32, torch.int32
+    _check(_l().bkv_evict4(ctx, _ptr(K4, u8, "K4"), _ptr(V4, u8, "V4"), _ptr(S4, f16, "S4"),
+                           _ptr(weights, f32, "weights"), _ptr(L, i32, "L"), int(budget), _ptr(K4_out, u8, "K4_out"),
+                           _ptr(V4_out, u8, "V4_out"), _ptr(S4_out, f16, "S4_out"),
+                           _ptr(weights_out, f32, "weights_out"), int(capacity_out), _ptr(kept_idx_out, i32, "kept"),
+                           _ptr(len_out, i32, "len_out")), "bkv_evict4", ctx)
 
 
 def bkv_get_state(ctx, centroids=None, sums=None, counts=None) -> None:
@@ -496,14 +544,18 @@ class BeaconKV:
         bkv_attend_reserve(self.ctx, n_q, n_groups, weights)
 
     def _attend_args(self, q, K, V, length, weights, o_out, lse_out):
+        d, rows_kv = self._layer[2], self._layer[4]
+        self._expect(K, rows_kv * d, "K")
+        self._expect(V, rows_kv * d, "V")
+        return self._query_args(q, length, weights, o_out, lse_out)
+
+    def _query_args(self, q, length, weights, o_out, lse_out):
         batch, heads, d, lens, rows_kv = self._layer
         shape = q.shape
         if len(shape) != 4 or shape[0] != batch or shape[1] != heads or shape[3] != d:
             raise ValueError(f"q must be [batch = {batch}, n_q_heads = {heads}, n_q, head_dim = {d}], got "
                              f"{tuple(shape)}")
         expect = self._expect
-        expect(K, rows_kv * d, "K")
-        expect(V, rows_kv * d, "V")
         expect(length, lens, "length")
         expect(weights, rows_kv, "weights")
         if not q.is_cuda:
@@ -547,6 +599,84 @@ class BeaconKV:
                           weights)
         return o, lse
 
+    # ------------------------------------------------------------ caches in 4 bits
+    def _cache4_args(self, K4, V4, S4, rows, suffix=""):
+        d = self.cfg.head_dim
+        self._expect(K4, rows * (d // 2), "K4" + suffix)
+        self._expect(V4, rows * (d // 2), "V4" + suffix)
+        self._expect(S4, rows * (d // 8), "S4" + suffix)
+
+    def _rows4(self, K, V, K4, V4, S4, first, length):
+        c = self.cfg
+        if K.dim() != 4 or K.shape[0] != c.batch or K.shape[1] != c.n_kv_heads or K.shape[3] != c.head_dim:
+            raise ValueError(f"K must be [batch = {c.batch}, n_kv_heads = {c.n_kv_heads}, n_rows, head_dim = "
+                             f"{c.head_dim}], got {tuple(K.shape)}")
+        lens, rows_kv = self._layer[3], self._layer[4]
+        self._expect(V, K.numel(), "V")
+        self._cache4_args(K4, V4, S4, rows_kv)
+        self._expect(first, lens, "first")
+        self._expect(length, lens, "length")
+        return K.shape[2]
+
+    def pack4(self, K, V, K4, V4, S4, *, length, first=None):
+        """Writes rows of one layer into its 4-bit caches (bkv_pack4): row i of K and V [batch, n_kv_heads, n_rows,
+        head_dim] becomes row first + i of its cache, for first + i < length.  K4 and V4 are uint8 [batch,
+        n_kv_heads, capacity, head_dim / 2], S4 fp16 [batch, n_kv_heads, capacity, 2, head_dim / 32, 2]; first
+        (None: 0) and length int32 [batch, n_kv_heads]."""
+        n = self._rows4(K, V, K4, V4, S4, first, length)
+        bkv_pack4(self.ctx, K, V, n, first, length, K4, V4, S4)
+
+    def unpack4(self, K4, V4, S4, K_out, V_out, *, length, first=None):
+        """The inverse of pack4 (bkv_unpack4): row first + i of each cache, below its length, to row i of K_out and
+        V_out; their other rows keep what they held."""
+        n = self._rows4(K_out, V_out, K4, V4, S4, first, length)
+        bkv_unpack4(self.ctx, K4, V4, S4, n, first, length, K_out, V_out)
+
+    def reserve_attend4(self, *, n_q: int = 1, weights: bool = False):
+        """Workspace for attend4 with n_q queries per head (bkv_attend4_reserve)."""
+        bkv_attend4_reserve(self.ctx, n_q, weights)
+
+    def attend4(self, q, K4, V4, S4, *, length, scale=None, weights=None, o_out=None, lse_out=None):
+        """attend over one layer's 4-bit caches (bkv_attend4), which are those of pack4.  Returns (o, lse)."""
+        self._cache4_args(K4, V4, S4, self._layer[4])
+        n_q, o, lse = self._query_args(q, length, weights, o_out, lse_out)
+        bkv_attend4(self.ctx, q, n_q, K4, V4, S4, length, scale or 0.0, o, lse, weights)
+        return o, lse
+
+    def evict4(self, K4, V4, S4, weights, *, L, budget, K4_out=None, V4_out=None, S4_out=None, weights_out=None,
+               kept_out=None, len_out=None):
+        """evict for 4-bit caches of all layers (bkv_evict4), in place or, with all of K4_out, V4_out, S4_out and
+        weights_out, into other caches.  Returns (kept rows, new lengths)."""
+        given = (K4_out is not None) + (V4_out is not None) + (S4_out is not None) + (weights_out is not None)
+        if given == 0:
+            K4_out, V4_out, S4_out, weights_out = K4, V4, S4, weights
+        elif given != 4:
+            raise ValueError("K4_out, V4_out, S4_out and weights_out come together or not at all")
+        rows = self.n_inst * self.cfg.capacity
+        cap_out = weights_out.numel() // self.n_inst
+        self._cache4_args(K4, V4, S4, rows)
+        self._cache4_args(K4_out, V4_out, S4_out, self.n_inst * cap_out, "_out")
+        kept_out, len_out = self._evict_args(K4, weights, L, budget, weights_out, kept_out, len_out)
+        bkv_evict4(self.ctx, K4, V4, S4, weights, L, budget, K4_out, V4_out, S4_out, weights_out, cap_out, kept_out,
+                   len_out)
+        return kept_out, len_out
+
+    def _evict_args(self, K, weights, L, budget, weights_out, kept_out, len_out):
+        c, n_inst = self.cfg, self.n_inst
+        self._expect(weights, n_inst * c.capacity, "weights")
+        self._expect(L, n_inst, "L")
+        self._expect(weights_out, weights_out.numel() // n_inst * n_inst, "weights_out")
+        self._expect(kept_out, n_inst * budget, "kept_out")
+        self._expect(len_out, n_inst, "len_out")
+        if not K.is_cuda:
+            raise TypeError("the caches must be CUDA tensors")
+        if kept_out is None or len_out is None:
+            shape, i32 = (c.n_layers, c.batch, c.n_kv_heads), torch.int32
+            kept, length = self._new(K, shape + (max(0, budget) if kept_out is None else 0,), i32, shape, i32)
+            kept_out = kept if kept_out is None else kept_out
+            len_out = length if len_out is None else len_out
+        return kept_out, len_out
+
     def evict(self, K, V, weights, *, L, budget, K_out=None, V_out=None, weights_out=None, kept_out=None,
               len_out=None):
         """Eviction by accumulated weight (bkv_evict), in place or, with K_out, V_out and weights_out of
@@ -565,20 +695,9 @@ class BeaconKV:
         rows_out = n_inst * cap_out
         self._expect(K, rows * d, "K")
         self._expect(V, rows * d, "V")
-        self._expect(weights, rows, "weights")
-        self._expect(L, n_inst, "L")
-        self._expect(weights_out, rows_out, "weights_out")
         self._expect(K_out, rows_out * d, "K_out")
         self._expect(V_out, rows_out * d, "V_out")
-        self._expect(kept_out, n_inst * budget, "kept_out")
-        self._expect(len_out, n_inst, "len_out")
-        if not K.is_cuda:
-            raise TypeError("K must be a CUDA tensor")
-        if kept_out is None or len_out is None:
-            shape, i32 = (c.n_layers, c.batch, c.n_kv_heads), torch.int32
-            kept, length = self._new(K, shape + (max(0, budget) if kept_out is None else 0,), i32, shape, i32)
-            kept_out = kept if kept_out is None else kept_out
-            len_out = length if len_out is None else len_out
+        kept_out, len_out = self._evict_args(K, weights, L, budget, weights_out, kept_out, len_out)
         bkv_evict(self.ctx, K, V, weights, L, budget, K_out, V_out, weights_out, cap_out, kept_out, len_out)
         return kept_out, len_out
 

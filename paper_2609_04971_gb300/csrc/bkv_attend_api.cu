@@ -55,6 +55,60 @@ int check_attend_shape(bkv_ctx* c, int32_t n_q, int32_t n_groups) {
   return BKV_OK;
 }
 
+// Bytes of a row of K (and of V), and of the scales of a row of a 4-bit cache.
+size_t row_bytes(const Shape& s, bool four) { return four ? s.d / 2 : 2 * static_cast<size_t>(s.d); }
+size_t scale_bytes(const Shape& s, bool four) { return four ? s.d / 4 : 0; }
+
+// The scale of the logits, to base 2.
+int check_scale(bkv_ctx* ctx, double scale, float& sc) {
+  if (!std::isfinite(scale) || scale < 0.0) return fail(ctx, BKV_EINVAL, "scale must be finite and >= 0");
+  const double by_dim = 1.0 / std::sqrt(static_cast<double>(ctx->shape.d));
+  sc = static_cast<float>(1.4426950408889634 * (scale == 0.0 ? by_dim : scale));
+  if (!std::isfinite(sc) || sc < 1.17549435e-38f)
+    return fail(ctx, BKV_EINVAL, "scale is out of the range of fp32");
+  return BKV_OK;
+}
+
+// The workspace of a call laid out as `l`.
+int take_workspace(bkv_ctx* ctx, const bkv::AtLayout& l, const char* reserve, unsigned char*& ws) {
+  if (l.too_large) return fail(ctx, BKV_EINVAL, "row blocks times key tiles must be below 2^31");
+  if (l.bytes > ctx->attend_ws_bytes)
+    return fail(ctx, BKV_ESTATE, "this call needs %zu bytes of workspace, %s made %zu", l.bytes, reserve,
+                ctx->attend_ws_bytes);
+  ws = ctx->attend_ws;
+  if (!ctx->attend_ws_captured) {
+    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
+    // on an error the launches report what is wrong with the stream
+    if (cudaStreamIsCapturing(ctx->stream, &status) != cudaSuccess) cudaGetLastError();
+    ctx->attend_ws_captured = status != cudaStreamCaptureStatusNone;
+  }
+  return BKV_OK;
+}
+
+int launch_merge(bkv_ctx* ctx, const bkv::AttendArgs& a, const bkv::AtLayout& l) {
+  ProfScope ps(ctx, BKV_K_ATTEND_MERGE);
+  const cudaError_t e = bkv::launch_attend_merge(ctx->shape, a, l, ctx->stream);
+  return e == cudaSuccess ? BKV_OK : cuda_fail(ctx, e, "attend merge launch");
+}
+
+int launch_attend_kernels(bkv_ctx* ctx, const bkv::AttendArgs& a, const bkv::AtLayout& l) {
+  const Shape& s = ctx->shape;
+  cudaError_t e;
+  {
+    ProfScope ps(ctx, BKV_K_ATTEND);
+    e = bkv::launch_attend(s, a, l, ctx->stream);
+  }
+  if (e != cudaSuccess) return cuda_fail(ctx, e, "attend launch");
+  const int rc = launch_merge(ctx, a, l);
+  if (rc != BKV_OK) return rc;
+  if (a.weights && !l.logits) {
+    ProfScope ps(ctx, BKV_K_ATTEND_WEIGHTS);
+    e = bkv::launch_attend_weights(s, a, l, ctx->stream);
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "attend weights launch");
+  }
+  return BKV_OK;
+}
+
 int attend(bkv_ctx* ctx, bkv::AttendArgs& a, double scale) {
   const Shape& s = ctx->shape;
   if (!a.q || !a.K || !a.V || !a.len || !a.o) return fail(ctx, BKV_EINVAL, "q, K, V, len and o must be non-NULL");
@@ -62,10 +116,8 @@ int attend(bkv_ctx* ctx, bkv::AttendArgs& a, double scale) {
     return fail(ctx, BKV_EINVAL, "q, K, V and o must be 16-byte aligned");
   if (!aligned4(a.len) || !aligned4(a.lse) || !aligned4(a.weights))
     return fail(ctx, BKV_EINVAL, "len, lse_out and weights must be 4-byte aligned");
-  if (!std::isfinite(scale) || scale < 0.0) return fail(ctx, BKV_EINVAL, "scale must be finite and >= 0");
-  a.sc = static_cast<float>(1.4426950408889634 * (scale == 0.0 ? 1.0 / std::sqrt(static_cast<double>(s.d)) : scale));
-  if (!std::isfinite(a.sc) || a.sc < 1.17549435e-38f)
-    return fail(ctx, BKV_EINVAL, "scale is out of the range of fp32");
+  int rc = check_scale(ctx, scale, a.sc);
+  if (rc != BKV_OK) return rc;
   // Outputs are written while other blocks and the kernels that follow still read the inputs.
   const size_t rows = static_cast<size_t>(s.batch) * s.n_kv * s.G * a.n_q, lens = static_cast<size_t>(s.batch) * s.n_kv,
                kv = lens * s.cap, kvp = static_cast<size_t>(a.groups) * s.n_kv * a.pcap;
@@ -79,46 +131,14 @@ int attend(bkv_ctx* ctx, bkv::AttendArgs& a, double scale) {
               out[] = {{a.o, rows * s.d * 2}, {a.lse, rows * 4}, {a.weights, kv * 4}};
   if (overlap(in, out)) return fail(ctx, BKV_EINVAL, "o, lse_out or weights overlaps an input or another output");
   const bkv::AtLayout l = bkv::attend_layout(s, a.n_q, a.groups, a.pcap, a.weights != nullptr);
-  if (l.too_large) return fail(ctx, BKV_EINVAL, "row blocks times key tiles must be below 2^31");
-  if (l.bytes > ctx->attend_ws_bytes)
-    return fail(ctx, BKV_ESTATE, "this call needs %zu bytes of workspace, bkv_attend_reserve made %zu", l.bytes,
-                ctx->attend_ws_bytes);
-  a.ws = ctx->attend_ws;
-  if (!ctx->attend_ws_captured) {
-    cudaStreamCaptureStatus status = cudaStreamCaptureStatusNone;
-    // on an error the launches report what is wrong with the stream
-    if (cudaStreamIsCapturing(ctx->stream, &status) != cudaSuccess) cudaGetLastError();
-    ctx->attend_ws_captured = status != cudaStreamCaptureStatusNone;
-  }
+  rc = take_workspace(ctx, l, "bkv_attend_reserve", a.ws);
+  if (rc != BKV_OK) return rc;
   a.err = ctx->err;
-  cudaError_t e;
-  {
-    ProfScope ps(ctx, BKV_K_ATTEND);
-    e = bkv::launch_attend(s, a, l, ctx->stream);
-  }
-  if (e != cudaSuccess) return cuda_fail(ctx, e, "attend launch");
-  {
-    ProfScope ps(ctx, BKV_K_ATTEND_MERGE);
-    e = bkv::launch_attend_merge(s, a, l, ctx->stream);
-  }
-  if (e != cudaSuccess) return cuda_fail(ctx, e, "attend merge launch");
-  if (a.weights && !l.logits) {
-    ProfScope ps(ctx, BKV_K_ATTEND_WEIGHTS);
-    e = bkv::launch_attend_weights(s, a, l, ctx->stream);
-    if (e != cudaSuccess) return cuda_fail(ctx, e, "attend weights launch");
-  }
-  return BKV_OK;
+  return launch_attend_kernels(ctx, a, l);
 }
 
-}  // namespace
-
-extern "C" {
-
-int bkv_attend_reserve(bkv_ctx* ctx, int32_t n_q, int32_t n_groups, int weights) {
-  if (!ctx) return BKV_EINVAL;
-  const int rc = check_attend_shape(ctx, n_q, n_groups);
-  if (rc != BKV_OK) return rc;
-  const size_t need = n_q == 0 ? 0 : bkv::attend_workspace(ctx->shape, n_q, n_groups, weights != 0);
+// Grows the attention workspace to `need` bytes.
+int reserve(bkv_ctx* ctx, size_t need) {
   if (need <= ctx->attend_ws_bytes) return BKV_OK;
   // the new workspace exists before the old one goes, so that a failure changes nothing
   unsigned char* ws = nullptr;
@@ -147,6 +167,163 @@ int bkv_attend_reserve(bkv_ctx* ctx, int32_t n_q, int32_t n_groups, int weights)
   ctx->attend_ws = ws;
   ctx->attend_ws_bytes = need;
   return BKV_OK;
+}
+
+// Rows of K and V into (pack) or out of one layer's 4-bit caches.
+int pack4(bkv_ctx* ctx, bool pack, bkv::Pack4Args& a) {
+  const Shape& s = ctx->shape;
+  if (a.n_rows < 0) return fail(ctx, BKV_EINVAL, "n_rows must be >= 0");
+  a.n_inst = s.batch * s.n_kv;
+  a.cap = s.cap;
+  if (1LL * a.n_inst * a.n_rows >= (1LL << 31)) return fail(ctx, BKV_EINVAL, "batch * n_kv_heads * n_rows must be below 2^31");
+  if (a.n_rows == 0) return BKV_OK;
+  if (!a.K || !a.V || !a.K4 || !a.V4 || !a.S4 || !a.len)
+    return fail(ctx, BKV_EINVAL, "K, V, K4, V4, S4 and len must be non-NULL");
+  if (!aligned16(a.K) || !aligned16(a.V) || !aligned16(a.K4) || !aligned16(a.V4) || !aligned16(a.S4))
+    return fail(ctx, BKV_EINVAL, "K, V, K4, V4 and S4 must be 16-byte aligned");
+  if (!aligned4(a.first) || !aligned4(a.len)) return fail(ctx, BKV_EINVAL, "first and len must be 4-byte aligned");
+  const size_t lens = static_cast<size_t>(a.n_inst) * 4, rows = static_cast<size_t>(a.n_inst) * a.n_rows * s.d * 2,
+               caches = static_cast<size_t>(a.n_inst) * s.cap;
+  const Range K{a.K, rows}, V{a.V, rows}, K4{a.K4, caches * row_bytes(s, true)}, V4{a.V4, caches * row_bytes(s, true)},
+      S4{a.S4, caches * scale_bytes(s, true)}, first{a.first, lens}, len{a.len, lens}, none{nullptr, 0};
+  bool bad;
+  if (pack) {
+    const Range in[] = {K, V, first, len}, out[] = {K4, V4, S4};
+    bad = overlap(in, out);
+  } else {
+    const Range in[] = {K4, V4, S4, first, len}, out[] = {K, V, none};
+    bad = overlap(in, out);
+  }
+  if (bad) return fail(ctx, BKV_EINVAL, "an output overlaps an input or another output");
+  a.err = ctx->err;
+  ProfScope ps(ctx, pack ? BKV_K_PACK4 : BKV_K_UNPACK4);
+  const cudaError_t e = pack ? bkv::launch_pack4(s.d, a, ctx->stream) : bkv::launch_unpack4(s.d, a, ctx->stream);
+  return e == cudaSuccess ? BKV_OK : cuda_fail(ctx, e, pack ? "pack launch" : "unpack launch");
+}
+
+int attend4(bkv_ctx* ctx, bkv::Attend4Args& a, double scale) {
+  const Shape& s = ctx->shape;
+  if (!a.q || !a.K4 || !a.V4 || !a.S4 || !a.len || !a.o)
+    return fail(ctx, BKV_EINVAL, "q, K4, V4, S4, len and o must be non-NULL");
+  if (!aligned16(a.q) || !aligned16(a.K4) || !aligned16(a.V4) || !aligned16(a.S4) || !aligned16(a.o))
+    return fail(ctx, BKV_EINVAL, "q, K4, V4, S4 and o must be 16-byte aligned");
+  if (!aligned4(a.len) || !aligned4(a.lse) || !aligned4(a.weights))
+    return fail(ctx, BKV_EINVAL, "len, lse_out and weights must be 4-byte aligned");
+  int rc = check_scale(ctx, scale, a.sc);
+  if (rc != BKV_OK) return rc;
+  const size_t rows = static_cast<size_t>(s.batch) * s.n_kv * s.G * a.n_q, lens = static_cast<size_t>(s.batch) * s.n_kv,
+               kv = lens * s.cap;
+  const Range in[] = {{a.q, rows * s.d * 2},
+                      {a.K4, kv * row_bytes(s, true)},
+                      {a.V4, kv * row_bytes(s, true)},
+                      {a.S4, kv * scale_bytes(s, true)},
+                      {a.len, lens * 4}},
+              out[] = {{a.o, rows * s.d * 2}, {a.lse, rows * 4}, {a.weights, kv * 4}};
+  if (overlap(in, out)) return fail(ctx, BKV_EINVAL, "o, lse_out or weights overlaps an input or another output");
+  const bkv::AtLayout l = bkv::attend4_layout(s, a.n_q, a.weights != nullptr);
+  rc = take_workspace(ctx, l, "bkv_attend4_reserve", a.ws);
+  if (rc != BKV_OK) return rc;
+  a.err = ctx->err;
+  bkv::AttendArgs b;
+  b.q = a.q;
+  b.len = a.len;
+  b.n_q = a.n_q;
+  b.sc = a.sc;
+  b.o = a.o;
+  b.lse = a.lse;
+  b.weights = a.weights;
+  b.ws = a.ws;
+  b.err = a.err;
+  if (l.unpacked) {
+    bkv::Pack4Args u;
+    u.K = reinterpret_cast<uint4*>(a.ws + l.off_k);
+    u.V = reinterpret_cast<uint4*>(a.ws + l.off_v);
+    u.K4 = const_cast<uint32_t*>(a.K4);
+    u.V4 = const_cast<uint32_t*>(a.V4);
+    u.S4 = const_cast<uint32_t*>(a.S4);
+    u.len = a.len;
+    u.n_inst = s.batch * s.n_kv;
+    u.n_rows = u.cap = s.cap;
+    u.err = a.err;
+    b.K = reinterpret_cast<const __nv_bfloat16*>(u.K);
+    b.V = reinterpret_cast<const __nv_bfloat16*>(u.V);
+    cudaError_t e;
+    {
+      ProfScope ps(ctx, BKV_K_UNPACK4);
+      e = bkv::launch_unpack4(s.d, u, ctx->stream);
+    }
+    if (e != cudaSuccess) return cuda_fail(ctx, e, "unpack launch");
+    return launch_attend_kernels(ctx, b, l);
+  }
+  cudaError_t e;
+  {
+    ProfScope ps(ctx, BKV_K_ATTEND4);
+    e = bkv::launch_attend4(s, a, l, ctx->stream);
+  }
+  if (e != cudaSuccess) return cuda_fail(ctx, e, "attend4 launch");
+  return launch_merge(ctx, b, l);
+}
+
+int evict(bkv_ctx* ctx, bkv::EvictArgs& a) {
+  const Shape& s = ctx->shape;
+  if (!a.K || !a.V || !a.weights || !a.L || !a.K_out || !a.V_out || !a.weights_out || !a.kept ||
+      (a.four && (!a.S || !a.S_out)))
+    return fail(ctx, BKV_EINVAL, "the caches, weights, L, their outputs and kept_idx_out must be non-NULL");
+  if (!aligned16(a.K) || !aligned16(a.V) || !aligned16(a.S) || !aligned16(a.K_out) || !aligned16(a.V_out) ||
+      !aligned16(a.S_out))
+    return fail(ctx, BKV_EINVAL, "the caches and their outputs must be 16-byte aligned");
+  if (!aligned4(a.weights) || !aligned4(a.weights_out) || !aligned4(a.L) || !aligned4(a.kept) || !aligned4(a.len_out))
+    return fail(ctx, BKV_EINVAL, "weights, L and the index outputs must be 4-byte aligned");
+  if (a.budget < 1 || a.budget < s.n_prefix + s.W)
+    return fail(ctx, BKV_EINVAL, "budget = %d must be >= max(1, n_prefix + window = %d)", a.budget, s.n_prefix + s.W);
+  if (1LL * s.n_inst * a.budget >= (1LL << 31)) return fail(ctx, BKV_EINVAL, "budget too large");
+  if (a.cap_out < std::min(a.budget, s.cap))
+    return fail(ctx, BKV_EINVAL, "capacity_out = %d is below min(budget, capacity) = %d", a.cap_out,
+                std::min(a.budget, s.cap));
+  if (1LL * s.n_inst * a.cap_out >= (1LL << 31)) return fail(ctx, BKV_EINVAL, "capacity_out too large");
+  const bool in_place = a.K_out == a.K && a.V_out == a.V && a.S_out == a.S && a.weights_out == a.weights;
+  const size_t rows = static_cast<size_t>(s.n_inst) * s.cap, rows_out = static_cast<size_t>(s.n_inst) * a.cap_out;
+  const size_t kv = row_bytes(s, a.four), sc = scale_bytes(s, a.four), lens = sizeof(int32_t) * s.n_inst;
+  if (in_place && a.cap_out != s.cap)
+    return fail(ctx, BKV_EINVAL, "in place, capacity_out = %d must be the capacity (%d)", a.cap_out, s.cap);
+  // The rows are moved by kept_idx_out, so a row number must not be written over either.
+  const Range in[] = {{in_place ? nullptr : a.K, rows * kv},
+                      {in_place ? nullptr : a.V, rows * kv},
+                      {in_place ? nullptr : a.S, rows * sc},
+                      {in_place ? nullptr : a.weights, rows * 4},
+                      {a.len_out == a.L ? nullptr : a.L, lens}},
+              out[] = {{a.K_out, rows_out * kv},
+                       {a.V_out, rows_out * kv},
+                       {a.S_out, rows_out * sc},
+                       {a.weights_out, rows_out * 4},
+                       {a.kept, sizeof(int32_t) * s.n_inst * a.budget},
+                       {a.len_out, lens}};
+  if (overlap(in, out))
+    return fail(ctx, BKV_EINVAL, "an output overlaps an input or another output (the caches and weights may be their "
+                "own outputs, all of them, and L may be len_out)");
+  a.plan = reinterpret_cast<int2*>(ctx->valid);  // scratch of a compress, 16 bytes per instance
+  a.err = ctx->err;
+  ProfScope ps(ctx, BKV_K_EVICT);
+  const cudaError_t e = bkv::launch_evict(s, a, ctx->stream);
+  return e == cudaSuccess ? BKV_OK : cuda_fail(ctx, e, "evict launch");
+}
+
+}  // namespace
+
+extern "C" {
+
+int bkv_attend_reserve(bkv_ctx* ctx, int32_t n_q, int32_t n_groups, int weights) {
+  if (!ctx) return BKV_EINVAL;
+  const int rc = check_attend_shape(ctx, n_q, n_groups);
+  if (rc != BKV_OK) return rc;
+  return reserve(ctx, n_q == 0 ? 0 : bkv::attend_workspace(ctx->shape, n_q, n_groups, weights != 0));
+}
+
+int bkv_attend4_reserve(bkv_ctx* ctx, int32_t n_q, int weights) {
+  if (!ctx) return BKV_EINVAL;
+  const int rc = check_attend_shape(ctx, n_q, 0);
+  if (rc != BKV_OK) return rc;
+  return reserve(ctx, n_q == 0 ? 0 : bkv::attend4_workspace(ctx->shape, n_q, weights != 0));
 }
 
 int bkv_attend(bkv_ctx* ctx, const void* q, int32_t n_q, const void* K, const void* V, const int32_t* len, double scale,
@@ -197,59 +374,93 @@ int bkv_attend_shared(bkv_ctx* ctx, const void* q, int32_t n_q, const void* Kp, 
   return attend(ctx, a, scale);
 }
 
-int bkv_evict(bkv_ctx* ctx, const void* K, const void* V, const float* weights, const int32_t* L, int32_t budget,
-              void* K_out, void* V_out, float* weights_out, int32_t capacity_out, int32_t* kept_idx_out,
-              int32_t* len_out) {
+int bkv_pack4(bkv_ctx* ctx, const void* K, const void* V, int32_t n_rows, const int32_t* first, const int32_t* len,
+              void* K4, void* V4, void* S4) {
   if (!ctx) return BKV_EINVAL;
-  const Shape& s = ctx->shape;
-  if (!K || !V || !weights || !L || !K_out || !V_out || !weights_out || !kept_idx_out)
-    return fail(ctx, BKV_EINVAL, "K, V, weights, L, their outputs and kept_idx_out must be non-NULL");
-  if (!aligned16(K) || !aligned16(V) || !aligned16(K_out) || !aligned16(V_out))
-    return fail(ctx, BKV_EINVAL, "K, V, K_out and V_out must be 16-byte aligned");
-  if (!aligned4(weights) || !aligned4(weights_out) || !aligned4(L) || !aligned4(kept_idx_out) || !aligned4(len_out))
-    return fail(ctx, BKV_EINVAL, "weights, L and the index outputs must be 4-byte aligned");
-  if (budget < 1 || budget < s.n_prefix + s.W)
-    return fail(ctx, BKV_EINVAL, "budget = %d must be >= max(1, n_prefix + window = %d)", budget, s.n_prefix + s.W);
-  if (1LL * s.n_inst * budget >= (1LL << 31)) return fail(ctx, BKV_EINVAL, "budget too large");
-  if (capacity_out < std::min(budget, s.cap))
-    return fail(ctx, BKV_EINVAL, "capacity_out = %d is below min(budget, capacity) = %d", capacity_out,
-                std::min(budget, s.cap));
-  if (1LL * s.n_inst * capacity_out >= (1LL << 31)) return fail(ctx, BKV_EINVAL, "capacity_out too large");
-  const bool in_place = K_out == K && V_out == V && weights_out == weights;
-  const size_t rows = static_cast<size_t>(s.n_inst) * s.cap, rows_out = static_cast<size_t>(s.n_inst) * capacity_out;
-  const size_t kv = rows * s.d * 2, kv_out = rows_out * s.d * 2, lens = sizeof(int32_t) * s.n_inst;
-  if (in_place && capacity_out != s.cap)
-    return fail(ctx, BKV_EINVAL, "in place, capacity_out = %d must be the capacity (%d)", capacity_out, s.cap);
-  // The rows are moved by kept_idx_out, so a row number must not be written over either.
-  const Range in[] = {{in_place ? nullptr : K, kv},
-                      {in_place ? nullptr : V, kv},
-                      {in_place ? nullptr : weights, rows * 4},
-                      {len_out == L ? nullptr : L, lens}},
-              out[] = {{K_out, kv_out},
-                       {V_out, kv_out},
-                       {weights_out, rows_out * 4},
-                       {kept_idx_out, sizeof(int32_t) * s.n_inst * budget},
-                       {len_out, lens}};
-  if (overlap(in, out))
-    return fail(ctx, BKV_EINVAL, "an output overlaps an input or another output (K, V and weights may be their own "
-                "outputs, all three, and L may be len_out)");
+  bkv::Pack4Args a;
+  a.K = static_cast<uint4*>(const_cast<void*>(K));
+  a.V = static_cast<uint4*>(const_cast<void*>(V));
+  a.K4 = static_cast<uint32_t*>(K4);
+  a.V4 = static_cast<uint32_t*>(V4);
+  a.S4 = static_cast<uint32_t*>(S4);
+  a.first = first;
+  a.len = len;
+  a.n_rows = n_rows;
+  return pack4(ctx, true, a);
+}
+
+int bkv_unpack4(bkv_ctx* ctx, const void* K4, const void* V4, const void* S4, int32_t n_rows, const int32_t* first,
+                const int32_t* len, void* K, void* V) {
+  if (!ctx) return BKV_EINVAL;
+  bkv::Pack4Args a;
+  a.K = static_cast<uint4*>(K);
+  a.V = static_cast<uint4*>(V);
+  a.K4 = static_cast<uint32_t*>(const_cast<void*>(K4));
+  a.V4 = static_cast<uint32_t*>(const_cast<void*>(V4));
+  a.S4 = static_cast<uint32_t*>(const_cast<void*>(S4));
+  a.first = first;
+  a.len = len;
+  a.n_rows = n_rows;
+  return pack4(ctx, false, a);
+}
+
+int bkv_attend4(bkv_ctx* ctx, const void* q, int32_t n_q, const void* K4, const void* V4, const void* S4,
+                const int32_t* len, double scale, void* o, float* lse_out, float* weights) {
+  if (!ctx) return BKV_EINVAL;
+  const int rc = check_attend_shape(ctx, n_q, 0);
+  if (rc != BKV_OK || n_q == 0) return rc;
+  bkv::Attend4Args a;
+  a.q = static_cast<const __nv_bfloat16*>(q);
+  a.K4 = static_cast<const uint32_t*>(K4);
+  a.V4 = static_cast<const uint32_t*>(V4);
+  a.S4 = static_cast<const uint32_t*>(S4);
+  a.len = len;
+  a.n_q = n_q;
+  a.o = static_cast<__nv_bfloat16*>(o);
+  a.lse = lse_out;
+  a.weights = weights;
+  return attend4(ctx, a, scale);
+}
+
+int bkv_evict4(bkv_ctx* ctx, const void* K4, const void* V4, const void* S4, const float* weights, const int32_t* L,
+               int32_t budget, void* K4_out, void* V4_out, void* S4_out, float* weights_out, int32_t capacity_out,
+               int32_t* kept_idx_out, int32_t* len_out) {
+  if (!ctx) return BKV_EINVAL;
   bkv::EvictArgs a;
-  a.K = static_cast<const __nv_bfloat16*>(K);
-  a.V = static_cast<const __nv_bfloat16*>(V);
+  a.four = true;
+  a.K = K4;
+  a.V = V4;
+  a.S = S4;
   a.weights = weights;
   a.L = L;
   a.budget = budget;
   a.cap_out = capacity_out;
-  a.K_out = static_cast<__nv_bfloat16*>(K_out);
-  a.V_out = static_cast<__nv_bfloat16*>(V_out);
+  a.K_out = K4_out;
+  a.V_out = V4_out;
+  a.S_out = S4_out;
   a.weights_out = weights_out;
   a.kept = kept_idx_out;
   a.len_out = len_out;
-  a.plan = reinterpret_cast<int2*>(ctx->valid);  // scratch of a compress, 16 bytes per instance
-  a.err = ctx->err;
-  ProfScope ps(ctx, BKV_K_EVICT);
-  const cudaError_t e = bkv::launch_evict(s, a, ctx->stream);
-  return e == cudaSuccess ? BKV_OK : cuda_fail(ctx, e, "evict launch");
+  return evict(ctx, a);
+}
+
+int bkv_evict(bkv_ctx* ctx, const void* K, const void* V, const float* weights, const int32_t* L, int32_t budget,
+              void* K_out, void* V_out, float* weights_out, int32_t capacity_out, int32_t* kept_idx_out,
+              int32_t* len_out) {
+  if (!ctx) return BKV_EINVAL;
+  bkv::EvictArgs a;
+  a.K = K;
+  a.V = V;
+  a.weights = weights;
+  a.L = L;
+  a.budget = budget;
+  a.cap_out = capacity_out;
+  a.K_out = K_out;
+  a.V_out = V_out;
+  a.weights_out = weights_out;
+  a.kept = kept_idx_out;
+  a.len_out = len_out;
+  return evict(ctx, a);
 }
 
 }  // extern "C"

@@ -185,13 +185,39 @@ struct AttendArgs {
   unsigned char* ws = nullptr;
   int* err = nullptr;
 };
+// Attention over 4-bit caches (k_attend4.cu)
+struct Attend4Args {
+  const __nv_bfloat16* q = nullptr;
+  const uint32_t *K4 = nullptr, *V4 = nullptr, *S4 = nullptr;  // [batch][n_kv][cap] rows
+  const int* len = nullptr;
+  int n_q = 0;
+  float sc = 0.f;
+  __nv_bfloat16* o = nullptr;
+  float* lse = nullptr;
+  float* weights = nullptr;
+  unsigned char* ws = nullptr;
+  int* err = nullptr;
+};
+
+// ---- caches in 4 bits (k_pack4.cu): rows are d / 8 words, scales 2 d / 32 fp16 pairs
+struct Pack4Args {
+  uint4 *K = nullptr, *V = nullptr;                           // bf16 [n_inst][n_rows][d]
+  uint32_t *K4 = nullptr, *V4 = nullptr, *S4 = nullptr;       // [n_inst][cap] rows
+  const int *first = nullptr, *len = nullptr;                 // [n_inst]; first may be nullptr: 0
+  int n_inst = 0, n_rows = 0, cap = 0;
+  int* err = nullptr;
+};
+cudaError_t launch_pack4(int d, const Pack4Args& a, cudaStream_t st);    // reads K, V
+cudaError_t launch_unpack4(int d, const Pack4Args& a, cudaStream_t st);  // writes K, V
+
 // ---- eviction by accumulated weight (k_evict.cu)
 struct EvictArgs {
-  const __nv_bfloat16 *K = nullptr, *V = nullptr;
+  bool four = false;  // 4-bit caches: K, V and S are those of bkv_pack4; else bf16 rows, no S
+  const void *K = nullptr, *V = nullptr, *S = nullptr;
   const float* weights = nullptr;
   const int* L = nullptr;
   int budget = 0, cap_out = 0;
-  __nv_bfloat16 *K_out = nullptr, *V_out = nullptr;
+  void *K_out = nullptr, *V_out = nullptr, *S_out = nullptr;
   float* weights_out = nullptr;
   int* kept = nullptr;
   int* len_out = nullptr;

@@ -38,7 +38,7 @@ size_t align_up(size_t n) { return (n + 255) / 256 * 256; }
 // 128 rows 60 and 63 us; 144 rows (two blocks, and one) 90 and 64 us, 256 rows 105 and 72 us; 8 caches of 32768 keys:
 // 80 rows 35 and 40, 128 rows 42.5 and 42.5, 144 rows 52 and 43 us.
 AtPlan make_plan(const Shape& s, int I, int m, int R, int n_q, bool causal, int cap, int len_div, int sms,
-                 bool& too_large) {
+                 bool& too_large, bool four = false) {
   AtPlan p{};
   AtGeo& g = p.geo;
   g.I = I;
@@ -50,7 +50,12 @@ AtPlan make_plan(const Shape& s, int I, int m, int R, int n_q, bool causal, int 
   g.cap = cap;
   g.len_div = len_div;
   const int most_rows = 1ll * R * m <= kAtTile ? kAtTile : kMaxRows;
-  if (R <= most_rows) {
+  if (four) {  // blocks of up to 16 rows, as even as they can be
+    g.mb = 1;
+    g.nr = (R + kBlockRows4 - 1) / kBlockRows4;
+    g.rr = (R + g.nr - 1) / g.nr;
+    g.nr = (R + g.rr - 1) / g.rr;
+  } else if (R <= most_rows) {
     const int most = most_rows / R, nb = (m + most - 1) / most;
     g.rr = R;
     g.mb = (m + nb - 1) / nb;
@@ -252,8 +257,10 @@ __global__ void __launch_bounds__(kMergeThreads, 4) merge_kernel(MergeArgs a) {
   if (j0 - tid >= len) return;
 #pragma unroll 1
   for (int r = warp; r < g.R; r += kMergeThreads / 32) {
-    const int2 span = a.own_parts.span[e];  // the rows are one block: item e
-    const Run own = make_run(a.own_parts, span, e, r, D, a.own_ctas, a.err), pre = prefix_run(a, e, r, D);
+    int rb;
+    const int c = g.by_rr.mod(r, rb), item = e * g.nrb + rb;  // one sequence to a block
+    const Run own = make_run(a.own_parts, a.own_parts.span[item], item, c, D, a.own_ctas, a.err),
+              pre = prefix_run(a, e, r, D);
     const float v = pre.n + own.n > 1 || a.has_prefix ? merged_lse2(pre, own, part_ml(pre, own, lane), lane)
                                                       : a.lse2[static_cast<size_t>(e) * g.R + r];
     if (lane == 0) {
@@ -377,6 +384,12 @@ __global__ void __launch_bounds__(kMergeThreads, 3) merge_rows_kernel(MergeArgs 
 
 }  // namespace
 
+size_t attend4_workspace(const Shape& s, int n_q, bool weights) {
+  size_t most = attend4_layout(s, n_q, weights).bytes;
+  for (int n = 1; n < n_q && n <= kMaxRows; ++n) most = std::max(most, attend4_layout(s, n, weights).bytes);
+  return most;
+}
+
 size_t attend_workspace(const Shape& s, int n_q, int groups, bool weights) {
   size_t most = attend_layout(s, n_q, groups, 1, weights).bytes;
   for (int n = 1; n < n_q && n <= kMaxRows; ++n) most = std::max(most, attend_layout(s, n, groups, 1, weights).bytes);
@@ -407,6 +420,32 @@ AtLayout attend_layout(const Shape& s, int n_q, int groups, int pcap, bool weigh
     l.off_wu0 = at;
     at = align_up(at + static_cast<size_t>(weights_items(s) + 1) * sizeof(int));
   }
+  l.bytes = at;
+  return l;
+}
+
+AtLayout attend4_layout(const Shape& s, int n_q, bool weights) {
+  AtLayout l;
+  const int sms = l.sms = device_sms();
+  const int R = s.G * n_q;
+  const size_t rows = static_cast<size_t>(s.batch) * s.n_kv * R;
+  if (R > (weights ? kLogitRows : kRows4)) {
+    l = attend_layout(s, n_q, 0, 0, weights);
+    l.unpacked = true;
+    const size_t cache = align_up(static_cast<size_t>(s.batch) * s.n_kv * s.cap * s.d * 2);
+    l.off_k = l.bytes;
+    l.off_v = l.off_k + cache;
+    l.bytes = l.off_v + cache;
+    return l;
+  }
+  l.four = true;
+  l.own = make_plan(s, s.batch * s.n_kv, 1, R, n_q, true, s.cap, 1, sms, l.too_large, true);
+  size_t at = place_parts(l.own, s.d, sms, 0);
+  l.off_lse2 = at;
+  at = align_up(at + rows * sizeof(float));
+  l.logits = weights;
+  l.off_logits = at;
+  if (l.logits) at = align_up(at + rows * s.cap * sizeof(float));
   l.bytes = at;
   return l;
 }

@@ -20,6 +20,10 @@ namespace bkv {
 constexpr int kAtTile = 128;             // keys per tile
 constexpr uint32_t kAtBox = 128 * 128;   // [128 rows][64 bf16] swizzled box
 constexpr int kMaxRows = 256;            // query rows per row block
+constexpr int kBlockRows4 = 16;          // the same over 4-bit caches
+// Query rows per KV head up to which a 4-bit cache is read code by code, 16 rows at a time; beyond, its rows are
+// unpacked to bf16 first.
+constexpr int kRows4 = 96;
 // Query rows per KV head up to which the logits are kept for the weights, 4 bytes a row and key written and
 // read once more, row by row by the merge; beyond, the weights are recomputed from the keys by two more launches.
 // A call in us, kept and recomputed, by the number of caches and their keys:
@@ -335,6 +339,9 @@ struct AtPlan {
 struct AtLayout {
   AtPlan own, prefix;
   bool has_prefix = false;
+  bool four = false;       // the caches are in 4 bits and the own kernel is that of k_attend4.cu
+  bool unpacked = false;   // they are unpacked into the workspace, and the plan is that of bf16 caches
+  size_t off_k = 0, off_v = 0;  // bf16 [batch][n_kv][cap][d]
   bool logits = false;     // the own kernel stores its logits for the weights
   size_t off_lse2 = 0;     // fp32 [rows]: log2 normalisers
   size_t off_logits = 0;   // fp32 [rows][cap]
@@ -346,9 +353,11 @@ struct AtLayout {
 };
 // The workspace does not depend on pcap.
 AtLayout attend_layout(const Shape& s, int n_q, int groups, int pcap, bool weights);
+AtLayout attend4_layout(const Shape& s, int n_q, bool weights);
 // Bytes that serve every call with at most n_q queries: more queries can need less (beyond kLogitRows rows no
 // logits are kept), but beyond kMaxRows of them the need only grows.
 size_t attend_workspace(const Shape& s, int n_q, int groups, bool weights);
+size_t attend4_workspace(const Shape& s, int n_q, bool weights);
 
 // Tiles of keys that the recomputed weights are made for.
 inline long long weights_items(const Shape& s) {
@@ -360,6 +369,9 @@ inline long long weights_items(const Shape& s) {
 cudaError_t launch_attend(const Shape& s, const AttendArgs& a, const AtLayout& l, cudaStream_t st);
 cudaError_t launch_attend_merge(const Shape& s, const AttendArgs& a, const AtLayout& l, cudaStream_t st);
 cudaError_t launch_attend_weights(const Shape& s, const AttendArgs& a, const AtLayout& l, cudaStream_t st);
+
+// The tiles of 4-bit caches, l.four set; the merge follows as above.
+cudaError_t launch_attend4(const Shape& s, const Attend4Args& a, const AtLayout& l, cudaStream_t st);
 
 // Arguments of the attention kernel.
 struct AtKernelArgs {

@@ -267,13 +267,26 @@ __global__ void __launch_bounds__(THREADS, 2048 / THREADS) evict_select_kernel(S
   }
 }
 
+// What a row consists of: vectors of 16 bytes of K, V and, in a 4-bit cache, of the scales.
+template <int D, bool FOUR>
+struct RowOf {
+  static constexpr int kK = FOUR ? D / 32 : D / 8, kS = FOUR ? D / 64 : 0, kVec = 2 * kK + kS;
+  // a thread's vector: where it lies in row 0 of instance e's rows, and how many vectors on the next row lies
+  template <typename T>
+  static __device__ __forceinline__ T* at(T* K, T* V, T* S, int col, size_t row, int& stride) {
+    const int c = col < kK ? col : col < 2 * kK ? col - kK : col - 2 * kK;
+    stride = FOUR && col >= 2 * kK ? kS : kK;
+    return (col < kK ? K : !FOUR || col < 2 * kK ? V : S) + row * stride + c;
+  }
+};
+
 // Compaction in place: one CTA per instance, the next chunk under way while one is written.
-template <int D, int kThreads>
+template <int D, bool FOUR, int kThreads>
 __global__ void __launch_bounds__(kThreads, 1024 / kThreads) evict_move_in_place_kernel(Shape s, EvictArgs a) {
-  constexpr int kVpr = D * 2 / 16;    // 16-byte vectors per row of one tensor
-  constexpr int kRowVec = 2 * kVpr;   // K row, then V row
+  using Row = RowOf<D, FOUR>;
+  constexpr int kRowVec = Row::kVec;
   constexpr int kPer = 4;             // vectors per thread and chunk, one chunk ahead
-  constexpr int kRowsPerPass = kThreads / kRowVec;
+  constexpr int kRowsPerPass = kThreads / kRowVec;  // a rest of the threads may have no rows
   constexpr int kChunkRows = kRowsPerPass * kPer;
   static_assert(kChunkRows <= kThreads, "one weight per thread and chunk");
   const int e = blockIdx.x, tid = threadIdx.x;
@@ -283,8 +296,10 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) evict_move_in_place
   const int first = plan.y, end = plan.x;
   const int* kept = a.kept + static_cast<size_t>(e) * a.budget;
   const int col = tid % kRowVec, r0 = tid / kRowVec;
-  const int vcol = col < kVpr ? col : col - kVpr;
-  uint4* base = reinterpret_cast<uint4*>((col < kVpr ? a.K_out : a.V_out) + static_cast<size_t>(e) * s.cap * D) + vcol;
+  const int n_rows = r0 < kRowsPerPass ? end : 0;  // rows below it are this thread's to move
+  int stride;
+  uint4* base = Row::at(static_cast<uint4*>(a.K_out), static_cast<uint4*>(a.V_out), static_cast<uint4*>(a.S_out), col,
+                        static_cast<size_t>(e) * s.cap, stride);
   float* weights = a.weights_out + static_cast<size_t>(e) * s.cap;
 
   uint4 cur[kPer], nxt[kPer];
@@ -293,10 +308,10 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) evict_move_in_place
 #pragma unroll
     for (int u = 0; u < kPer; ++u) {
       const int row = i0 + r0 + kRowsPerPass * u;
-      if (row < end) {
+      if (row < n_rows) {
         int j = __ldcg(kept + row);
         if (!in_bounds(j - row, s.cap - row, a.err)) j = row;  // row <= kept[row] < cap
-        R[u] = __ldcg(base + static_cast<size_t>(j) * kVpr);
+        R[u] = __ldcg(base + static_cast<size_t>(j) * stride);
       }
     }
     if (tid < kChunkRows && i0 + tid < end) {
@@ -313,7 +328,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) evict_move_in_place
 #pragma unroll
     for (int u = 0; u < kPer; ++u) {
       const int row = i0 + r0 + kRowsPerPass * u;
-      if (row < end) base[static_cast<size_t>(row) * kVpr] = cur[u];
+      if (row < n_rows) base[static_cast<size_t>(row) * stride] = cur[u];
     }
     if (tid < kChunkRows && i0 + tid < end) weights[i0 + tid] = w_cur;
 #pragma unroll
@@ -326,9 +341,10 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) evict_move_in_place
 
 // Compaction into other buffers: kMoveRows rows of an instance to a block.
 constexpr int kMoveRows = 64, kMoveThreads = 256;
-template <int D>
+template <int D, bool FOUR>
 __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(Shape s, EvictArgs a, int chunks) {
-  constexpr int kVpr = D * 2 / 16, kRowVec = 2 * kVpr, kPer = kMoveRows * kRowVec / kMoveThreads;
+  using Row = RowOf<D, FOUR>;
+  constexpr int kRowVec = Row::kVec, kPass = kMoveThreads / kRowVec, kPer = (kMoveRows + kPass - 1) / kPass;
   __shared__ int rows[kMoveRows];
   const int e = blockIdx.x / chunks, i0 = blockIdx.x % chunks * kMoveRows;
   const int tid = threadIdx.x;
@@ -340,10 +356,12 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(Shape s, Evict
   if (n <= 0) return;
   __syncthreads();
   const int col = tid % kRowVec, r0 = tid / kRowVec;
-  const int vcol = col < kVpr ? col : col - kVpr;
-  const uint4* src = reinterpret_cast<const uint4*>((col < kVpr ? a.K : a.V) + static_cast<size_t>(e) * s.cap * D) + vcol;
-  uint4* dst = reinterpret_cast<uint4*>((col < kVpr ? a.K_out : a.V_out) +
-                                        (static_cast<size_t>(e) * a.cap_out + i0) * D) + vcol;
+  const int n_rows = r0 < kPass ? n : 0;
+  int stride;
+  const uint4* src = Row::at(static_cast<const uint4*>(a.K), static_cast<const uint4*>(a.V),
+                             static_cast<const uint4*>(a.S), col, static_cast<size_t>(e) * s.cap, stride);
+  uint4* dst = Row::at(static_cast<uint4*>(a.K_out), static_cast<uint4*>(a.V_out), static_cast<uint4*>(a.S_out), col,
+                       static_cast<size_t>(e) * a.cap_out + i0, stride);
   const bool mine = tid < n;  // one weight per thread
   float w = 0.f;
   if (mine) {
@@ -354,17 +372,17 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(Shape s, Evict
   uint4 R[kPer];
 #pragma unroll
   for (int u = 0; u < kPer; ++u) {
-    const int r = r0 + u * (kMoveThreads / kRowVec);
-    if (r < n) {
+    const int r = r0 + u * kPass;
+    if (r < n_rows) {
       int j = rows[r];
       if (!in_bounds(j, s.cap, a.err)) j = i0 + r;
-      R[u] = __ldcg(src + static_cast<size_t>(j) * kVpr);
+      R[u] = __ldcg(src + static_cast<size_t>(j) * stride);
     }
   }
 #pragma unroll
   for (int u = 0; u < kPer; ++u) {
-    const int r = r0 + u * (kMoveThreads / kRowVec);
-    if (r < n) dst[static_cast<size_t>(r) * kVpr] = R[u];
+    const int r = r0 + u * kPass;
+    if (r < n_rows) dst[static_cast<size_t>(r) * stride] = R[u];
   }
   if (mine) a.weights_out[static_cast<size_t>(e) * a.cap_out + i0 + tid] = w;
 }
@@ -383,7 +401,7 @@ cudaError_t select(const Shape& s, const EvictArgs& a, cudaStream_t st) {
   return cudaGetLastError();
 }
 
-template <int D>
+template <int D, bool FOUR>
 cudaError_t launch_d(const Shape& s, const EvictArgs& a, cudaStream_t st) {
   const cudaError_t e = s.cap <= 2048    ? select<256>(s, a, st)
                         : s.cap <= 10240 ? select<512>(s, a, st)
@@ -396,19 +414,20 @@ cudaError_t launch_d(const Shape& s, const EvictArgs& a, cudaStream_t st) {
     // 110 us, 384 instances 343 and 318, 1024 instances 762 and 701, 4608 instances 3216 and 3095 us.
     const int sms = device_sms();
     const auto move = [&](auto kernel, int threads) { return launch_after(kernel, s.n_inst, threads, 0, st, s, a); };
-    return s.n_inst <= sms       ? move(evict_move_in_place_kernel<D, 1024>, 1024)
-           : s.n_inst <= 2 * sms ? move(evict_move_in_place_kernel<D, 512>, 512)
-           : s.n_inst <= 4 * sms ? move(evict_move_in_place_kernel<D, 256>, 256)
-                                 : move(evict_move_in_place_kernel<D, 128>, 128);
+    return s.n_inst <= sms       ? move(evict_move_in_place_kernel<D, FOUR, 1024>, 1024)
+           : s.n_inst <= 2 * sms ? move(evict_move_in_place_kernel<D, FOUR, 512>, 512)
+           : s.n_inst <= 4 * sms ? move(evict_move_in_place_kernel<D, FOUR, 256>, 256)
+                                 : move(evict_move_in_place_kernel<D, FOUR, 128>, 128);
   }
   const int kept = a.budget < s.cap ? a.budget : s.cap, chunks = (kept + kMoveRows - 1) / kMoveRows;
-  return launch_after(evict_move_kernel<D>, static_cast<unsigned>(s.n_inst) * chunks, kMoveThreads, 0, st, s, a, chunks);
+  return launch_after(evict_move_kernel<D, FOUR>, static_cast<unsigned>(s.n_inst) * chunks, kMoveThreads, 0, st, s, a, chunks);
 }
 
 }  // namespace
 
 cudaError_t launch_evict(const Shape& s, const EvictArgs& a, cudaStream_t st) {
-  return s.d == 128 ? launch_d<128>(s, a, st) : launch_d<64>(s, a, st);
+  if (a.four) return s.d == 128 ? launch_d<128, true>(s, a, st) : launch_d<64, true>(s, a, st);
+  return s.d == 128 ? launch_d<128, false>(s, a, st) : launch_d<64, false>(s, a, st);
 }
 
 }  // namespace bkv
