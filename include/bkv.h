@@ -317,6 +317,20 @@ int bkv_attend_shared(bkv_ctx* ctx, const void* q, int32_t n_q, const void* Kp, 
                       double scale, void* o, float* lse_out, float* weights);
 
 /*
+ * bkv_attend with a sliding window and first tokens that stay visible (sinks):
+ * query i, whose own row is row p = len - n_q + i, sees the rows j <= p with
+ * j > p - window or j < n_sink, and no others are read (but for what lies in a
+ * block of 128 rows with one that is).  A window of 1 is the own row alone.
+ *   window  >= 1;  n_sink >= 0.
+ * Everything else is as in bkv_attend, and the workspace is the one that
+ * bkv_attend_reserve makes for bkv_attend without weights.  No weights are
+ * accumulated: rows leave a window by their age.  The context's own `window`
+ * (of the scoring and the evictions) plays no part.
+ */
+int bkv_attend_window(bkv_ctx* ctx, const void* q, int32_t n_q, const void* K, const void* V, const int32_t* len,
+                      int32_t window, int32_t n_sink, double scale, void* o, float* lse_out);
+
+/*
  * Makes the workspace of bkv_attend (n_groups = 0) or bkv_attend_shared for
  * calls with n_q queries per head, with or without weights.  The workspace only
  * grows, so a reservation for the largest call serves the smaller ones of the

@@ -82,6 +82,8 @@ def load_library(path: str | None = None, build: bool = True):
             "bkv_attend": (ctypes.c_int, [_P, _P, ctypes.c_int32, _P, _P, _P, ctypes.c_double, _P, _P, _P]),
             "bkv_attend_shared": (ctypes.c_int, [_P, _P, ctypes.c_int32, _P, _P, _P, ctypes.c_int32, ctypes.c_int32,
                                                  _P, _P, _P, ctypes.c_double, _P, _P, _P]),
+            "bkv_attend_window": (ctypes.c_int, [_P, _P, ctypes.c_int32, _P, _P, _P, ctypes.c_int32, ctypes.c_int32,
+                                                 ctypes.c_double, _P, _P]),
             "bkv_attend_reserve": (ctypes.c_int, [_P, ctypes.c_int32, ctypes.c_int32, ctypes.c_int]),
             "bkv_evict": (ctypes.c_int, [_P, _P, _P, _P, _P, ctypes.c_int32, _P, _P, _P, ctypes.c_int32, _P, _P]),
             "bkv_pack4": (ctypes.c_int, [_P, _P, _P, ctypes.c_int32, _P, _P, _P, _P, _P]),
@@ -259,6 +261,16 @@ def bkv_attend_shared(ctx, q: torch.Tensor, n_q: int, Kp: torch.Tensor, Vp: torc
                                   _ptr(K, bf16, "K"), _ptr(V, bf16, "V"), _ptr(length, i32, "length"), float(scale),
                                   _ptr(o, bf16, "o"), _ptr(lse_out, f32, "lse_out"), _ptr(weights, f32, "weights")),
            "bkv_attend_shared", ctx)
+
+
+def bkv_attend_window(ctx, q: torch.Tensor, n_q: int, K: torch.Tensor, V: torch.Tensor, length: torch.Tensor,
+                      window: int, n_sink: int, scale: float, o: torch.Tensor,
+                      lse_out: torch.Tensor | None = None) -> None:
+    bf16 = torch.bfloat16
+    _check(_l().bkv_attend_window(ctx, _ptr(q, bf16, "q"), int(n_q), _ptr(K, bf16, "K"), _ptr(V, bf16, "V"),
+                                  _ptr(length, torch.int32, "length"), int(window), int(n_sink), float(scale),
+                                  _ptr(o, bf16, "o"), _ptr(lse_out, torch.float32, "lse_out")), "bkv_attend_window",
+           ctx)
 
 
 def bkv_evict(ctx, K: torch.Tensor, V: torch.Tensor, weights: torch.Tensor, L: torch.Tensor, budget: int,
@@ -597,6 +609,13 @@ class BeaconKV:
         self._expect(prefix_len, groups, "prefix_len")
         bkv_attend_shared(self.ctx, q, n_q, Kp, Vp, prefix_len, groups, pcap, K, V, length, scale or 0.0, o, lse,
                           weights)
+        return o, lse
+
+    def attend_window(self, q, K, V, *, length, window, n_sink=0, scale=None, o_out=None, lse_out=None):
+        """attend where a query sees the `window` newest rows up to its own and the first `n_sink` rows
+        (bkv_attend_window); the reservation is that of attend.  Returns (o, lse)."""
+        n_q, o, lse = self._attend_args(q, K, V, length, None, o_out, lse_out)
+        bkv_attend_window(self.ctx, q, n_q, K, V, length, window, n_sink, scale or 0.0, o, lse)
         return o, lse
 
     # ------------------------------------------------------------ caches in 4 bits

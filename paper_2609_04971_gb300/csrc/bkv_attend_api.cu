@@ -374,6 +374,26 @@ int bkv_attend_shared(bkv_ctx* ctx, const void* q, int32_t n_q, const void* Kp, 
   return attend(ctx, a, scale);
 }
 
+int bkv_attend_window(bkv_ctx* ctx, const void* q, int32_t n_q, const void* K, const void* V, const int32_t* len,
+                      int32_t window, int32_t n_sink, double scale, void* o, float* lse_out) {
+  if (!ctx) return BKV_EINVAL;
+  const int rc = check_attend_shape(ctx, n_q, 0);
+  if (rc != BKV_OK) return rc;
+  if (window < 1 || n_sink < 0) return fail(ctx, BKV_EINVAL, "window must be >= 1 and n_sink >= 0");
+  if (n_q == 0) return BKV_OK;
+  bkv::AttendArgs a;
+  a.q = static_cast<const __nv_bfloat16*>(q);
+  a.K = static_cast<const __nv_bfloat16*>(K);
+  a.V = static_cast<const __nv_bfloat16*>(V);
+  a.len = len;
+  a.n_q = n_q;
+  a.window = std::min(window, ctx->shape.cap);  // no row sees more than the capacity
+  a.n_sink = std::min(n_sink, ctx->shape.cap);
+  a.o = static_cast<__nv_bfloat16*>(o);
+  a.lse = lse_out;
+  return attend(ctx, a, scale);
+}
+
 int bkv_pack4(bkv_ctx* ctx, const void* K, const void* V, int32_t n_rows, const int32_t* first, const int32_t* len,
               void* K4, void* V4, void* S4) {
   if (!ctx) return BKV_EINVAL;

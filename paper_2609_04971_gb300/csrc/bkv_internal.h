@@ -178,6 +178,7 @@ struct AttendArgs {
   const int* plen = nullptr;  // [groups]
   int n_q = 0;
   int groups = 0, pcap = 0;  // 0 groups: no shared prefix
+  int window = 0, n_sink = 0;  // 0: every row sees all that comes before it
   float sc = 0.f;            // log2(e) * scale
   __nv_bfloat16* o = nullptr;
   float* lse = nullptr;      // [batch][n_kv * G][n_q] or nullptr

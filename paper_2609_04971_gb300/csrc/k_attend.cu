@@ -473,6 +473,17 @@ cudaError_t launch_attend(const Shape& s, const AttendArgs& a, const AtLayout& l
     k.logits = own ? logits : nullptr;
     k.err = a.err;
     k.after_prefix = own && l.has_prefix;
+    if (a.window > 0) {
+      k.geo.window = a.window;
+      k.geo.n_sink = a.n_sink;
+      if (g.mb * g.rr > kAtTile) return launch_attend_rows_window(s.d, p, qmap, kmap, vmap, k, st);
+      AtSinkMaps<true> sink;
+      if (encode_rows_bf16(&sink.k, K, rows, s.d, kSinkRows) != CUDA_SUCCESS ||
+          encode_rows_bf16(&sink.v, V, rows, s.d, kSinkRows) != CUDA_SUCCESS)
+        return cudaErrorInvalidValue;
+      return s.d == 128 ? launch_attend_window_128(p, qmap, kmap, vmap, sink, k, st)
+                        : launch_attend_window_64(p, qmap, kmap, vmap, sink, k, st);
+    }
     if (g.mb * g.rr > kAtTile) return launch_attend_rows(s.d, p, qmap, kmap, vmap, k, st);
     return s.d == 128 ? launch_attend_tiles_128(p, qmap, kmap, vmap, k, st)
                       : launch_attend_tiles_64(p, qmap, kmap, vmap, k, st);

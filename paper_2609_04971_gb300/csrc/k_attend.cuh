@@ -101,6 +101,8 @@ struct AtGeo {
   int cap;        // rows allocated per instance
   const int* len; // own: one per instance; prefix: one per sequence group
   int len_div;    // instance e has length len[e / len_div]
+  // With a window a row of limit n sees the keys j < n with j >= n - window or j < n_sink (bkv_attend_window).
+  int window, n_sink;
   FastDiv by_n_kv, by_m, by_rr, by_mb, by_nr, by_nrb, by_n_q, by_len_div;
 };
 
@@ -143,6 +145,21 @@ __device__ __forceinline__ int at_limit(const AtGeo& g, int len, int r0, int c) 
 
 // Tiles of an item: an item without keys still has one, all masked, that writes its empty rows.
 __device__ __forceinline__ int at_tiles(int limit) { return max(1, (limit + kAtTile - 1) / kAtTile); }
+
+// Where the tiles of an item lie.  Without a window one run from key 0.  With one, `ts` tiles of the first ns keys
+// and then a run from key w0, the first that a row's window reaches; one run from key 0 where the two would meet.
+struct AtRuns {
+  int ts, ns, w0, T;
+};
+template <bool WIN>
+__device__ __forceinline__ AtRuns at_runs(const AtGeo& g, int len, int r0) {
+  const int limit = at_limit_max(g, len, r0);
+  if (!WIN) return {0, 0, 0, at_tiles(limit)};
+  const int lo = at_limit_min(g, len, r0) - g.window, ns = min(g.n_sink, limit);
+  const int ts = (ns + kAtTile - 1) / kAtTile;
+  if (lo <= ts * kAtTile) return {0, ns, 0, at_tiles(limit)};
+  return {ts, ns, lo, ts + at_tiles(limit - lo)};
+}
 
 // Row of q, o and lse (there are fewer than 2^27) that column c of a row block stands for, or -1.
 __device__ __forceinline__ int at_row(const AtGeo& g, int e, AtBlock blk, int c) {
@@ -210,11 +227,12 @@ __device__ __forceinline__ void at_split(int n, Count&& count, Find&& find, int*
 
 // The split of a source's tiles: by instances where all row blocks of one have the same tiles, else by
 // row blocks.
-template <int THREADS>
+template <int THREADS, bool WIN = false>
 __device__ __forceinline__ void at_split_tiles(const AtGeo& g, int* scan, AtShare* out) {
   const bool even = !g.causal || g.n_q == 1;
   auto tiles = [&](int x) {
     const int e = even ? x : g.by_nrb.div(x), len = at_len(g, e);
+    if (WIN) return at_runs<true>(g, len, even ? 0 : at_block(g, x - e * g.nrb).r0).T;
     return at_tiles(even ? len : at_limit_max(g, len, at_block(g, x - e * g.nrb).r0));
   };
   at_split<THREADS>(
@@ -253,14 +271,29 @@ __host__ __device__ inline bool at_split_over(uint32_t u, uint32_t n, uint32_t p
 struct AtSeg {
   int e, rb, t0, t1, T, len, r0, b0;
   int item, u;  // u: number of tile t0 in the run of all tiles
+  int ts, ns, w0;  // with a window
 };
 
+// The first key of tile t of a segment's item.
+template <bool WIN>
+__device__ __forceinline__ int at_key0(const AtSeg& s, int t) {
+  return WIN && t >= s.ts ? s.w0 + (t - s.ts) * kAtTile : t * kAtTile;
+}
+
+// With a window: the first key from `from` on that a row of limit n sees, or -1.  In a run that begins there the row
+// sees none before.
+__device__ __forceinline__ int at_first_seen(const AtGeo& g, int n, int from) {
+  const int j = from < g.n_sink ? from : max(from, n - g.window);
+  return j < n ? j : -1;
+}
+
 // Walks the CTA's segments; every role has its own.
-struct AtWalk {
+template <bool WIN>
+struct AtWalkOf {
   int e, rb, t, left, u;
   int raw, raw_ahead;  // lengths of instances e and e + 1; the latter is under way until it is needed
   __device__ __forceinline__ void look(const AtGeo& g) { raw_ahead = at_raw_len(g, min(e + 1, g.I - 1)); }
-  __device__ __forceinline__ AtWalk(const AtGeo& g, const AtShare& s)
+  __device__ __forceinline__ AtWalkOf(const AtGeo& g, const AtShare& s)
       : e(s.at.e), rb(s.at.k), t(s.at.t), left(s.left), u(s.u), raw(at_raw_len(g, s.at.e)) {
     look(g);
   }
@@ -272,7 +305,11 @@ struct AtWalk {
     s.b0 = blk.b0;
     s.r0 = blk.r0;
     s.len = at_valid_len(g, raw);
-    s.T = at_tiles(at_limit_max(g, s.len, blk.r0));
+    const AtRuns runs = at_runs<WIN>(g, s.len, blk.r0);
+    s.T = runs.T;
+    s.ts = runs.ts;
+    s.ns = runs.ns;
+    s.w0 = runs.w0;
     s.t0 = t;
     s.t1 = min(s.T, t + left);
     s.item = e * g.nrb + rb;
@@ -292,6 +329,8 @@ struct AtWalk {
     return true;
   }
 };
+
+using AtWalk = AtWalkOf<false>;
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   uint32_t r;
@@ -386,10 +425,26 @@ struct AtKernelArgs {
   float* logits;       // [rows][cap] or nullptr
   int* err;
 };
+// With a window, boxes of kSinkRows rows of the keys and values, for the first keys.
+constexpr int kSinkRows = 16;
+template <bool WIN>
+struct AtSinkMaps {
+  CUtensorMap k, v;
+};
+template <>
+struct AtSinkMaps<false> {};
 // Row blocks of up to 128 rows (k_attend_tiles.cuh, one translation unit per head_dim), and of up to
-// 256 (k_attend_rows.cu).
+// 256 (k_attend_rows.cuh); each once without and once with a window.
 cudaError_t launch_attend_rows(int d, const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap,
                                const CUtensorMap& vmap, const AtKernelArgs& a, cudaStream_t st);
+cudaError_t launch_attend_rows_window(int d, const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap,
+                                      const CUtensorMap& vmap, const AtKernelArgs& a, cudaStream_t st);
+cudaError_t launch_attend_window_64(const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap,
+                                    const CUtensorMap& vmap, const AtSinkMaps<true>& sink, const AtKernelArgs& a,
+                                    cudaStream_t st);
+cudaError_t launch_attend_window_128(const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap,
+                                     const CUtensorMap& vmap, const AtSinkMaps<true>& sink, const AtKernelArgs& a,
+                                     cudaStream_t st);
 cudaError_t launch_attend_tiles_64(const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap,
                                    const CUtensorMap& vmap, const AtKernelArgs& a, cudaStream_t st);
 cudaError_t launch_attend_tiles_128(const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap,

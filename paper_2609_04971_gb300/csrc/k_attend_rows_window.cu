@@ -1,0 +1,11 @@
+// The attention kernel for many query rows (k_attend_rows.cuh) with a window.
+#include "k_attend_rows.cuh"
+
+namespace bkv {
+
+cudaError_t launch_attend_rows_window(int d, const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap,
+                                      const CUtensorMap& vmap, const AtKernelArgs& a, cudaStream_t st) {
+  return d == 128 ? launch<128, true>(p, qmap, kmap, vmap, a, st) : launch<64, true>(p, qmap, kmap, vmap, a, st);
+}
+
+}  // namespace bkv

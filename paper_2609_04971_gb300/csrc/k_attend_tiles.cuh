@@ -47,6 +47,8 @@
 // 28 us.  About 4.5 us pass until the first tile is there and 2 us after the last.
 #pragma once
 
+#include <climits>
+
 #include "k_attend.cuh"
 
 namespace bkv {
@@ -133,10 +135,11 @@ __device__ __forceinline__ uint32_t pack_rest(uint32_t p, float lo, float hi) {
   return pack_bf16(lo - __uint_as_float(p << 16), hi - __uint_as_float(p & 0xFFFF0000u));
 }
 
-template <int D, int U>
+template <int D, int U, bool WIN>
 __global__ void __launch_bounds__(kAtThreads, 1)
     attend_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
-                  const __grid_constant__ CUtensorMap vmap, AtKernelArgs a) {
+                  const __grid_constant__ CUtensorMap vmap, const __grid_constant__ AtSinkMaps<WIN> sink,
+                  AtKernelArgs a) {
   using C = AtCfg<D, U>;
   constexpr int N = C::N, NC = C::kNC;
   extern __shared__ unsigned char smem_raw[];
@@ -149,6 +152,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
   __shared__ AtShare share_sh;
   __shared__ __align__(16) float ref_sh[2][N];   // minus the reference of a column, by segment parity
   __shared__ __align__(16) int lim_sh[2][N];
+  __shared__ int first_sh[WIN ? 2 : 1][WIN ? N : 1];  // the first key of the segment that a column sees
   __shared__ int row_sh[2][N];  // row of q, o and lse (below 2^27), or -1
   __shared__ float red_sh[kSmWarps][NC];
   __shared__ float fac_sh[N];
@@ -203,11 +207,11 @@ __global__ void __launch_bounds__(kAtThreads, 1)
   grid_dependents_go();
   if (blockIdx.x == 0) at_check_lengths<kAtThreads>(g, a.err);
   tc_fence_before();
-  at_split_tiles<kAtThreads>(g, scan_sh, &share_sh);
+  at_split_tiles<kAtThreads, WIN>(g, scan_sh, &share_sh);
   tc_fence_after();
   if (tid == 0 && share_sh.left == 0) a.parts.cut[blockIdx.x] = make_int2(-1, -1);
   const uint32_t tmem = tmem_base_sh;
-  AtWalk walk(g, share_sh);
+  AtWalkOf<WIN> walk(g, share_sh);
   const int n_tiles = share_sh.left;  // tiles of this CTA (below 2^31)
 
   // Ring positions.  Tile i of the CTA: K(0); then for each i: K(i + 1), V(i), but V(i) first where
@@ -223,14 +227,14 @@ __global__ void __launch_bounds__(kAtThreads, 1)
         const uint64_t pol_q = l2_policy_evict_last();
         int pos = 0, n_seg = 0;
         bool ok = true;
-        auto load = [&](const CUtensorMap* map, int row) {
+        auto load = [&](const CUtensorMap* map, int row, uint32_t bytes) {
           const int st = pos % C::kStages;
           if (pos >= C::kStages &&
               !at_wait(&empty_bar[st], ((pos / C::kStages) - 1) & 1, abort_flag, a.err, kDevTimeoutProducer)) {
             ok = false;
             return;
           }
-          mbar_arrive_expect_tx(&full_bar[st], C::kTileBytes);
+          mbar_arrive_expect_tx(&full_bar[st], bytes);
           for (int b = 0; b < C::kBoxes; ++b)
             tma_load_2d(kv_smem + st * C::kTileBytes + b * kAtBox, map, &full_bar[st], b * 64, row, pol);
           ++pos;
@@ -252,6 +256,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
         };
         AtSeg s;
         int t = 0, k_row = 0, v_row = 0;
+        bool k_few = false, v_few = false;  // only the first kSinkRows rows of the tile are needed
         s.t1 = 0;
         for (int i = 0; ok && i <= n_tiles; ++i) {  // K(i) and V(i - 1)
           const bool turn = t == s.t1;              // tile i begins a segment
@@ -261,7 +266,8 @@ __global__ void __launch_bounds__(kAtThreads, 1)
               walk.next(g, s);
               t = s.t0;
             }
-            k_row = s.e * g.cap + t * kAtTile;
+            k_row = s.e * g.cap + at_key0<WIN>(s, t);
+            if (WIN) k_few = t < s.ts && s.ns - t * kAtTile <= kSinkRows;
             ++t;
           }
 #pragma unroll 1
@@ -269,9 +275,18 @@ __global__ void __launch_bounds__(kAtThreads, 1)
             const bool is_k = (h == 0) != v_first;
             if (is_k ? i == n_tiles : i == 0) continue;
             if (is_k && turn) load_q(s);
-            if (ok) load(is_k ? &kmap : &vmap, is_k ? k_row : v_row);
+            const CUtensorMap* map = is_k ? &kmap : &vmap;
+            uint32_t bytes = C::kTileBytes;
+            if constexpr (WIN) {
+              if (is_k ? k_few : v_few) {
+                map = is_k ? &sink.k : &sink.v;
+                bytes = C::kBoxes * kSinkRows * 128;
+              }
+            }
+            if (ok) load(map, is_k ? k_row : v_row, bytes);
           }
           v_row = k_row;
+          v_few = k_few;
         }
         if (!ok || *abort_flag) {  // let every copy already issued land before the CTA exits
           for (int p = max(0, n_seg - C::kQBufs); p < n_seg; ++p)
@@ -452,6 +467,10 @@ __global__ void __launch_bounds__(kAtThreads, 1)
         const int c = c0 + wt;
         rows[wt] = c < cols ? at_row(g, s.e, {s.b0, s.r0}, c) : -1;
         lim[wt] = at_limit(g, s.len, s.r0, c);
+        if (WIN) {
+          first_sh[WIN ? seg & 1 : 0][WIN ? c : 0] = at_first_seen(g, lim[wt], at_key0<WIN>(s, s.t0));
+          ref[wt] = 0.f;
+        }
       }
       named_barrier(bar_id, 128);
       float l[NC];
@@ -459,7 +478,13 @@ __global__ void __launch_bounds__(kAtThreads, 1)
       for (int c = 0; c < NC; ++c) l[c] = 0.f;
       for (bool first = true; t < t_end; ++t, first = false) {
         if (have) {
-          const int buf = i & 1, k0 = t * kAtTile, j = k0 + key_lane;
+          const int buf = i & 1, k0 = at_key0<WIN>(s, t), j = k0 + key_lane;
+          // keys past `end` are not this tile's
+          const int end = WIN && t < s.ts ? s.ns : limit_max;
+          // some row does not see all keys of the tile
+          const bool masked = WIN ? k0 + kAtTile > min(limit_min, end) ||
+                                        (k0 <= limit_max - g.window && k0 + kAtTile > g.n_sink)
+                                  : k0 + kAtTile > limit_min;
           wait(&sfull_bar[buf], (i >> 1) & 1);
           tc_fence_after();
           const int pb = i % C::kPBufs;
@@ -482,10 +507,18 @@ __global__ void __launch_bounds__(kAtThreads, 1)
                 y[c + 2] = a1.x;
                 y[c + 3] = a1.y;
               }
-              if (k0 + kAtTile > limit_min) {  // some row does not see all keys of the tile
+              if (masked) {
+                // with a window a row of limit n sees key j where j < n <= j + window, or j < n for the first keys
+                const int most = WIN ? (j >= end ? INT_MIN : j < g.n_sink ? INT_MAX : j + g.window) : 0;
 #pragma unroll
                 for (int c = 0; c < NC; c += 4) {
-                  const int4 m = *reinterpret_cast<const int4*>(lim + c);
+                  int4 m = *reinterpret_cast<const int4*>(lim + c);
+                  if (WIN) {
+                    m.x = m.x <= most ? m.x : INT_MIN;
+                    m.y = m.y <= most ? m.y : INT_MIN;
+                    m.z = m.z <= most ? m.z : INT_MIN;
+                    m.w = m.w <= most ? m.w : INT_MIN;
+                  }
                   y[c] = j < m.x ? y[c] : -INFINITY;
                   y[c + 1] = j < m.y ? y[c + 1] : -INFINITY;
                   y[c + 2] = j < m.z ? y[c + 2] : -INFINITY;
@@ -503,7 +536,16 @@ __global__ void __launch_bounds__(kAtThreads, 1)
                   if (c0 + c < cols) dst[static_cast<size_t>(c) * g.cap] = y[c];
               }
             }
-            if (t == s.t0) {
+            if constexpr (WIN) {
+              // a column's reference is the logit of the first key that it sees; until then it may be anything
+              if (first || masked) {
+                const int* seen = first_sh[seg & 1] + c0;
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
+                  if (j == seen[c]) ref[c] = -fmaxf(y[c] * sc, kRefFloor);
+                named_barrier(bar_id, 128);
+              }
+            } else if (t == s.t0) {
               if (key_lane == 0) {
 #pragma unroll
                 for (int c = 0; c < NC; ++c) ref[c] = k0 < lim[c] ? -fmaxf(y[c] * sc, kRefFloor) : 0.f;
@@ -606,7 +648,7 @@ __global__ void __launch_bounds__(kAtThreads, 1)
           } else if (lane == 0) {
             mbar_arrive(&sfree_bar[buf]);
           }
-          if (grp == 0 && k0 + kAtTile > limit_max && j >= limit_max) {
+          if (grp == 0 && k0 + kAtTile > end && j >= end) {
             // rows of V that no row of the item sees
             const bool last = i + 1 == n_tiles, turn = t + 1 == s.t1;
             const int vpos = 2 * i + (last || (turn && C::kQBufs == 1) ? 1 : 2);
@@ -661,29 +703,30 @@ __global__ void __launch_bounds__(kAtThreads, 1)
   if (a.after_prefix) grid_dependency_wait();  // what follows this kernel needs the prefix's results too
 }
 
-template <int D, int U>
+template <int D, int U, bool WIN>
 cudaError_t launch(const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap, const CUtensorMap& vmap,
-                   const AtKernelArgs& a, cudaStream_t st) {
+                   const AtSinkMaps<WIN>& sink, const AtKernelArgs& a, cudaStream_t st) {
   using C = AtCfg<D, U>;
-  const cudaError_t e = allow_smem<attend_kernel<D, U>>(C::kSmem);
+  const cudaError_t e = allow_smem<attend_kernel<D, U, WIN>>(C::kSmem);
   if (e != cudaSuccess) return e;
-  return launch_after(attend_kernel<D, U>, p.grid, kAtThreads, C::kSmem, st, qmap, kmap, vmap, a);
+  return launch_after(attend_kernel<D, U, WIN>, p.grid, kAtThreads, C::kSmem, st, qmap, kmap, vmap, sink, a);
 }
 
 }  // namespace
 
-template <int D>
+template <int D, bool WIN>
 cudaError_t launch_attend_tiles_d(const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap,
-                                  const CUtensorMap& vmap, const AtKernelArgs& a, cudaStream_t st) {
+                                  const CUtensorMap& vmap, const AtSinkMaps<WIN>& sink, const AtKernelArgs& a,
+                                  cudaStream_t st) {
   switch ((p.geo.mb * p.geo.rr + 15) / 16) {
-    case 1: return launch<D, 1>(p, qmap, kmap, vmap, a, st);
-    case 2: return launch<D, 2>(p, qmap, kmap, vmap, a, st);
-    case 3: return launch<D, 3>(p, qmap, kmap, vmap, a, st);
-    case 4: return launch<D, 4>(p, qmap, kmap, vmap, a, st);
-    case 5: return launch<D, 5>(p, qmap, kmap, vmap, a, st);
-    case 6: return launch<D, 6>(p, qmap, kmap, vmap, a, st);
-    case 7: return launch<D, 7>(p, qmap, kmap, vmap, a, st);
-    default: return launch<D, 8>(p, qmap, kmap, vmap, a, st);
+    case 1: return launch<D, 1>(p, qmap, kmap, vmap, sink, a, st);
+    case 2: return launch<D, 2>(p, qmap, kmap, vmap, sink, a, st);
+    case 3: return launch<D, 3>(p, qmap, kmap, vmap, sink, a, st);
+    case 4: return launch<D, 4>(p, qmap, kmap, vmap, sink, a, st);
+    case 5: return launch<D, 5>(p, qmap, kmap, vmap, sink, a, st);
+    case 6: return launch<D, 6>(p, qmap, kmap, vmap, sink, a, st);
+    case 7: return launch<D, 7>(p, qmap, kmap, vmap, sink, a, st);
+    default: return launch<D, 8>(p, qmap, kmap, vmap, sink, a, st);
   }
 }
 
