@@ -383,11 +383,13 @@ int bkv_unpack4(bkv_ctx* ctx, const void* K4, const void* V4, const void* S4, in
 /*
  * bkv_attend over 4-bit caches: the same formulas, arguments and limits, with
  * K and V the numbers that K4, V4 and S4 stand for.
- * Up to 96 query rows per KV head (G * n_q), 32 with weights, the codes are
- * multiplied as they are: the logits are fp32, and only the products of an
- * attention weight and a step are rounded, to fp16.  More rows read the caches
- * unpacked to bf16 into the workspace, and then all is as in bkv_attend.
- * Queries up to 2^100 in magnitude.
+ * Queries must lie within +-65504, and so must the values that the codes stand for.
+ * The logits are those of the values themselves, in fp32.  Up to 96 query rows
+ * per KV head (G * n_q), 32 with weights, the codes are multiplied as they are,
+ * and the products of an attention weight and a step are rounded to fp16.  More
+ * rows read the caches unpacked into the workspace, K as sums of two fp16
+ * numbers, V rounded to fp16, query elements below 2^-14 to multiples of 2^-24,
+ * and the attention weights are rounded to fp16.
  * BKV_ESTATE when the workspace that bkv_attend4_reserve made is too small.
  */
 int bkv_attend4(bkv_ctx* ctx, const void* q, int32_t n_q, const void* K4, const void* V4, const void* S4,
@@ -395,8 +397,8 @@ int bkv_attend4(bkv_ctx* ctx, const void* q, int32_t n_q, const void* K4, const 
 
 /*
  * bkv_attend_reserve for bkv_attend4, out of the same workspace.  Past the rows
- * that are read code by code it holds one layer's caches in bf16 beside what
- * bkv_attend takes.
+ * that are read code by code it holds the numbers of one layer's caches, 6
+ * head_dim bytes a row, and q beside what bkv_attend takes.
  */
 int bkv_attend4_reserve(bkv_ctx* ctx, int32_t n_q, int weights);
 

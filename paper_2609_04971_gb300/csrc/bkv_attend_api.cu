@@ -235,22 +235,27 @@ int attend4(bkv_ctx* ctx, bkv::Attend4Args& a, double scale) {
   b.ws = a.ws;
   b.err = a.err;
   if (l.unpacked) {
-    bkv::Pack4Args u;
+    bkv::Unpack16Args u;
     u.K = reinterpret_cast<uint4*>(a.ws + l.off_k);
+    u.K_rest = reinterpret_cast<uint4*>(a.ws + l.off_k_rest);
     u.V = reinterpret_cast<uint4*>(a.ws + l.off_v);
-    u.K4 = const_cast<uint32_t*>(a.K4);
-    u.V4 = const_cast<uint32_t*>(a.V4);
-    u.S4 = const_cast<uint32_t*>(a.S4);
+    u.K4 = a.K4;
+    u.V4 = a.V4;
+    u.S4 = a.S4;
     u.len = a.len;
     u.n_inst = s.batch * s.n_kv;
-    u.n_rows = u.cap = s.cap;
-    u.err = a.err;
+    u.cap = s.cap;
+    u.q = reinterpret_cast<const uint4*>(a.q);
+    u.q16 = reinterpret_cast<uint4*>(a.ws + l.off_q);
+    u.q_vecs = rows * s.d / 8;
+    b.q = reinterpret_cast<const __nv_bfloat16*>(u.q16);
     b.K = reinterpret_cast<const __nv_bfloat16*>(u.K);
+    b.K_rest = u.K_rest;
     b.V = reinterpret_cast<const __nv_bfloat16*>(u.V);
     cudaError_t e;
     {
       ProfScope ps(ctx, BKV_K_UNPACK4);
-      e = bkv::launch_unpack4(s.d, u, ctx->stream);
+      e = bkv::launch_unpack16(s.d, u, ctx->stream);
     }
     if (e != cudaSuccess) return cuda_fail(ctx, e, "unpack launch");
     return launch_attend_kernels(ctx, b, l);

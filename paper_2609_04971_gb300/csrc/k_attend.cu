@@ -38,7 +38,7 @@ size_t align_up(size_t n) { return (n + 255) / 256 * 256; }
 // 128 rows 60 and 63 us; 144 rows (two blocks, and one) 90 and 64 us, 256 rows 105 and 72 us; 8 caches of 32768 keys:
 // 80 rows 35 and 40, 128 rows 42.5 and 42.5, 144 rows 52 and 43 us.
 AtPlan make_plan(const Shape& s, int I, int m, int R, int n_q, bool causal, int cap, int len_div, int sms,
-                 bool& too_large, bool four = false) {
+                 bool& too_large, int most4 = 0) {
   AtPlan p{};
   AtGeo& g = p.geo;
   g.I = I;
@@ -50,9 +50,9 @@ AtPlan make_plan(const Shape& s, int I, int m, int R, int n_q, bool causal, int 
   g.cap = cap;
   g.len_div = len_div;
   const int most_rows = 1ll * R * m <= kAtTile ? kAtTile : kMaxRows;
-  if (four) {  // blocks of up to 16 rows, as even as they can be
+  if (most4) {  // blocks of up to that many rows, as even as they can be
     g.mb = 1;
-    g.nr = (R + kBlockRows4 - 1) / kBlockRows4;
+    g.nr = (R + most4 - 1) / most4;
     g.rr = (R + g.nr - 1) / g.nr;
     g.nr = (R + g.rr - 1) / g.rr;
   } else if (R <= most_rows) {
@@ -97,6 +97,14 @@ size_t place_parts(AtPlan& p, int d, int sms, size_t at) {
   at = align_up(at + static_cast<size_t>(p.items) * sizeof(int2));
   p.off_cut = at;
   return align_up(at + static_cast<size_t>(sms) * sizeof(int2));
+}
+
+// What the weights need that are recomputed from the keys.
+size_t place_weights(AtLayout& l, const Shape& s, size_t at) {
+  l.off_wpart = at;
+  at = align_up(at + static_cast<size_t>(2 * l.sms) * kAtTile * sizeof(float));
+  l.off_wu0 = at;
+  return align_up(at + static_cast<size_t>(weights_items(s) + 1) * sizeof(int));
 }
 
 struct MergeArgs {
@@ -414,12 +422,7 @@ AtLayout attend_layout(const Shape& s, int n_q, int groups, int pcap, bool weigh
   l.logits = weights && R <= kLogitRows;
   l.off_logits = at;
   if (l.logits) at = align_up(at + rows * s.cap * sizeof(float));
-  if (weights && !l.logits) {
-    l.off_wpart = at;
-    at = align_up(at + static_cast<size_t>(2 * sms) * kAtTile * sizeof(float));
-    l.off_wu0 = at;
-    at = align_up(at + static_cast<size_t>(weights_items(s) + 1) * sizeof(int));
-  }
+  if (weights && !l.logits) at = place_weights(l, s, at);
   l.bytes = at;
   return l;
 }
@@ -429,17 +432,24 @@ AtLayout attend4_layout(const Shape& s, int n_q, bool weights) {
   const int sms = l.sms = device_sms();
   const int R = s.G * n_q;
   const size_t rows = static_cast<size_t>(s.batch) * s.n_kv * R;
-  if (R > (weights ? kLogitRows : kRows4)) {
-    l = attend_layout(s, n_q, 0, 0, weights);
+  if (R > (weights ? kLogitRows4 : kRows4)) {
     l.unpacked = true;
+    // the rows kernel of k_attend_rows.cuh, whatever the rows
+    l.own = make_plan(s, s.batch * s.n_kv, 1, R, n_q, true, s.cap, 1, sms, l.too_large, R <= kMaxRows ? kMaxRows : 0);
+    size_t at = place_parts(l.own, s.d, sms, 0);
+    l.off_lse2 = at;
+    at = align_up(at + rows * sizeof(float));
+    if (weights) at = place_weights(l, s, at);
     const size_t cache = align_up(static_cast<size_t>(s.batch) * s.n_kv * s.cap * s.d * 2);
-    l.off_k = l.bytes;
-    l.off_v = l.off_k + cache;
-    l.bytes = l.off_v + cache;
+    l.off_k = at;
+    l.off_k_rest = l.off_k + cache;
+    l.off_v = l.off_k_rest + cache;
+    l.off_q = l.off_v + cache;
+    l.bytes = align_up(l.off_q + rows * s.d * 2);
     return l;
   }
   l.four = true;
-  l.own = make_plan(s, s.batch * s.n_kv, 1, R, n_q, true, s.cap, 1, sms, l.too_large, true);
+  l.own = make_plan(s, s.batch * s.n_kv, 1, R, n_q, true, s.cap, 1, sms, l.too_large, kBlockRows4);
   size_t at = place_parts(l.own, s.d, sms, 0);
   l.off_lse2 = at;
   at = align_up(at + rows * sizeof(float));
@@ -473,6 +483,11 @@ cudaError_t launch_attend(const Shape& s, const AttendArgs& a, const AtLayout& l
     k.logits = own ? logits : nullptr;
     k.err = a.err;
     k.after_prefix = own && l.has_prefix;
+    if (a.K_rest) {
+      CUtensorMap restmap;
+      if (encode_rows_bf16(&restmap, a.K_rest, rows, s.d, kAtTile) != CUDA_SUCCESS) return cudaErrorInvalidValue;
+      return launch_attend_rows_split(s.d, p, qmap, kmap, restmap, vmap, k, st);
+    }
     if (a.window > 0) {
       k.geo.window = a.window;
       k.geo.n_sink = a.n_sink;

@@ -22,8 +22,9 @@ constexpr uint32_t kAtBox = 128 * 128;   // [128 rows][64 bf16] swizzled box
 constexpr int kMaxRows = 256;            // query rows per row block
 constexpr int kBlockRows4 = 16;          // the same over 4-bit caches
 // Query rows per KV head up to which a 4-bit cache is read code by code, 16 rows at a time; beyond, its rows are
-// unpacked to bf16 first.
+// unpacked to fp16 first.
 constexpr int kRows4 = 96;
+constexpr int kLogitRows4 = 32;  // the same with weights
 // Query rows per KV head up to which the logits are kept for the weights, 4 bytes a row and key written and
 // read once more, row by row by the merge; beyond, the weights are recomputed from the keys by two more launches.
 // A call in us, kept and recomputed, by the number of caches and their keys:
@@ -338,6 +339,12 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return r;
 }
 
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
 // Where one source's kernel leaves what the merge needs.  Segment `cta + item` is the part of an
 // item that a CTA worked on: both rise along the run of all segments, one of them by at least 1 from
 // each segment to the next, so the numbers differ.
@@ -379,8 +386,8 @@ struct AtLayout {
   AtPlan own, prefix;
   bool has_prefix = false;
   bool four = false;       // the caches are in 4 bits and the own kernel is that of k_attend4.cu
-  bool unpacked = false;   // they are unpacked into the workspace, and the plan is that of bf16 caches
-  size_t off_k = 0, off_v = 0;  // bf16 [batch][n_kv][cap][d]
+  bool unpacked = false;   // they are unpacked into the workspace as fp16 numbers, for the rows kernel
+  size_t off_k = 0, off_k_rest = 0, off_v = 0, off_q = 0;  // fp16 [batch][n_kv][cap][d], and q
   bool logits = false;     // the own kernel stores its logits for the weights
   size_t off_lse2 = 0;     // fp32 [rows]: log2 normalisers
   size_t off_logits = 0;   // fp32 [rows][cap]
@@ -437,6 +444,10 @@ struct AtSinkMaps<false> {};
 // 256 (k_attend_rows.cuh); each once without and once with a window.
 cudaError_t launch_attend_rows(int d, const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap,
                                const CUtensorMap& vmap, const AtKernelArgs& a, cudaStream_t st);
+// Over fp16 numbers, the keys in two terms.
+cudaError_t launch_attend_rows_split(int d, const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap,
+                                     const CUtensorMap& restmap, const CUtensorMap& vmap, const AtKernelArgs& a,
+                                     cudaStream_t st);
 cudaError_t launch_attend_rows_window(int d, const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap,
                                       const CUtensorMap& vmap, const AtKernelArgs& a, cudaStream_t st);
 cudaError_t launch_attend_window_64(const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap,

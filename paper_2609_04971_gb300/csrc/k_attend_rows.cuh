@@ -61,11 +61,23 @@ __device__ __forceinline__ void store_sector(void* dst, const uint32_t* v) {
                : "memory");
 }
 
-template <int D, bool WIN>
+// Of fp16 operands, where the keys are sums of two terms: the map of the second.
+template <bool SPLIT>
+struct RestMap {
+  CUtensorMap k;
+};
+template <>
+struct RestMap<false> {};
+
+template <int D, bool WIN, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, 1)
     rows_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
-                const __grid_constant__ CUtensorMap vmap, AtKernelArgs a) {
+                const __grid_constant__ CUtensorMap vmap, const __grid_constant__ RestMap<SPLIT> rest,
+                AtKernelArgs a) {
   using C = RowsCfg<D>;
+  // stages of a tile's keys; a tile's stages; P of fp16 numbers stays below 2^15
+  constexpr int kK = SPLIT ? 2 : 1, kPer = kK + 1;
+  constexpr float kTop = SPLIT ? 32768.f : kSumAbove;
   extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(8) uint64_t full_bar[C::kStages], empty_bar[C::kStages];
   __shared__ __align__(8) uint64_t qfull_bar, qempty_bar, sfull_bar[2], pfull_bar[2];
@@ -124,7 +136,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   AtWalkOf<WIN> walk(g, share_sh);
   const int n_tiles = share_sh.left;  // key tiles of this CTA
 
-  // Ring of stages: K(0), then for each tile i: V(i), K(i + 1).
+  // Ring of stages: K(0), then for each tile i: V(i), K(i + 1); with SPLIT a K is two.
   if (warp < 4) {
     set_max_regs_dec<kRegsFew>();
     if (warp == 0) {
@@ -173,8 +185,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             ++t;
           }
 #pragma unroll 1
-          for (int h = 0; ok && h < 2; ++h)
-            if (h == 0 ? i > 0 : i < n_tiles) load(h == 0 ? &vmap : &kmap, h == 0 ? v_row : k_row);
+          for (int h = 0; ok && h < kPer; ++h) {
+            const CUtensorMap* map = h == 0 ? &vmap : &kmap;
+            if constexpr (SPLIT) map = h == 2 ? &rest.k : map;
+            if (h == 0 ? i > 0 : i < n_tiles) load(map, h == 0 ? v_row : k_row);
+          }
           if (ok && turn && i < n_tiles) load_q(s);
           v_row = k_row;
         }
@@ -190,24 +205,33 @@ __global__ void __launch_bounds__(kThreads, 1)
       // Products run in the order in which they are issued, so S_w of the next tile may follow O_w of
       // this one at once although it overwrites its P.
       // The whole warp walks along and one lane issues, so that descriptors stay in uniform registers.
-      const uint32_t idesc_s = idesc_bf16_f32(kRows, kAtTile), idesc_o = idesc_bf16_f32(kRows, D) | kIdescMnMajorB;
+      const uint32_t idesc_s = SPLIT ? idesc_f16_f32(kRows, kAtTile) : idesc_bf16_f32(kRows, kAtTile);
+      const uint32_t idesc_o = (SPLIT ? idesc_f16_f32(kRows, D) : idesc_bf16_f32(kRows, D)) | kIdescMnMajorB;
       const uint32_t kv_addr = smem_u32(kv_smem), q_addr = smem_u32(q_smem);
       const uint32_t tm = __shfl_sync(0xffffffffu, tmem, 0);
       bool ok = true;
       auto await = [&](uint64_t* bar, uint32_t parity) {
         if (ok) ok = __all_sync(0xffffffffu, at_wait(bar, parity, abort_flag, a.err, kDevTimeoutMma));
       };
-      auto issue_s = [&](int w, int st, bool done, bool last_of_seg) {
+      auto issue_s = [&](int w, int st, int st2, bool done, bool last_of_seg) {
         if (!ok) return;
         tc_fence_after();
         const uint64_t q = sdesc_kmajor_sw128(q_addr + w * kAtBox), k = sdesc_kmajor_sw128(kv_addr + st * C::kTileBytes);
+        const uint64_t k2 = sdesc_kmajor_sw128(kv_addr + st2 * C::kTileBytes);
         if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk)
             mma_bf16_ss(tm + w * kAtTile, q + (((kk >> 2) * C::kQBox + (kk & 3) * 32) >> 4),
                         k + (((kk >> 2) * kAtBox + (kk & 3) * 32) >> 4), idesc_s, kk > 0);
+          if (SPLIT) {
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk)
+              mma_bf16_ss(tm + w * kAtTile, q + (((kk >> 2) * C::kQBox + (kk & 3) * 32) >> 4),
+                          k2 + (((kk >> 2) * kAtBox + (kk & 3) * 32) >> 4), idesc_s, 1);
+          }
           mma_commit(&sfull_bar[w]);
           if (done) mma_commit(&empty_bar[st]);
+          if (SPLIT && done) mma_commit(&empty_bar[st2]);
           if (done && last_of_seg) mma_commit(&qempty_bar);
         }
         __syncwarp();
@@ -233,8 +257,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       s.t1 = 0;
       for (int i = 0; ok && i <= n_tiles; ++i) {  // for each row tile O(i - 1), then S(i)
         const bool turn = t == s.t1, more = i < n_tiles;
-        const int seg_o = seg, v_pos = 2 * i - 1, k_pos = 2 * i;
-        const int v_st = i > 0 ? v_pos % C::kStages : 0, k_st = k_pos % C::kStages;
+        const int seg_o = seg, v_pos = kPer * i - 1, k_pos = kPer * i, k2_pos = k_pos + kK - 1;
+        const int v_st = i > 0 ? v_pos % C::kStages : 0, k_st = k_pos % C::kStages, k2_st = k2_pos % C::kStages;
         if (more) {
           if (turn) {
             walk.next(g, s);
@@ -255,7 +279,8 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (more) {
             if (w == 0 && turn) await(&qfull_bar, seg & 1);
             if (w == 0) await(&full_bar[k_st], (k_pos / C::kStages) & 1);
-            issue_s(w, k_st, w == 1, last_s);
+            if (SPLIT && w == 0) await(&full_bar[k2_st], (k2_pos / C::kStages) & 1);
+            issue_s(w, k_st, k2_st, w == 1, last_s);
           }
         }
       }
@@ -341,8 +366,8 @@ __global__ void __launch_bounds__(kThreads, 1)
               const float2 e1 = make_float2(ex2_approx(v[x + 2]), ex2_approx(v[x + 3]));
               s0 = add2(s0, e0);
               s1 = add2(s1, e1);
-              p[q * 16 + x / 2] = pack_bf16(e0.x, e0.y);
-              p[q * 16 + x / 2 + 1] = pack_bf16(e1.x, e1.y);
+              p[q * 16 + x / 2] = SPLIT ? pack_f16(e0.x, e0.y) : pack_bf16(e0.x, e0.y);
+              p[q * 16 + x / 2 + 1] = SPLIT ? pack_f16(e1.x, e1.y) : pack_bf16(e1.x, e1.y);
             }
           }
           s0 = add2(s0, s1);
@@ -368,8 +393,8 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll 1
         for (int pass = 0;; ++pass) {
           weigh(!WIN && pass == 0 && t == s.t0);
-          // a weight above 2^32 shows in the sum, so no maximum is kept
-          if (pass > 0 || !__any_sync(0xffffffffu, sum > kSumAbove)) break;
+          // a weight above 2^32 (2^15 of fp16 numbers) shows in the sum, so no maximum is kept
+          if (pass > 0 || !__any_sync(0xffffffffu, sum > kTop)) break;
           // Move the references up to the tile's maxima.  The products of the tiles before are complete:
           // the barrier of this tile's S was waited for, and they were issued before it.
           float up = 0.f;
@@ -404,7 +429,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         tmem_wait_st();
         if (w == 0 && k0 + kAtTile > end && k0 + lane_row >= end) {
           // rows of V that no row of the item sees must not hold what 0 times it is not 0
-          const int v_pos = 2 * i + 1, st = v_pos % C::kStages;
+          const int v_pos = kPer * i + kK, st = v_pos % C::kStages;
           at_wait(&full_bar[st], (v_pos / C::kStages) & 1, abort_flag, a.err, kDevTimeoutEpilogue);
 #pragma unroll
           for (int b = 0; b < C::kBoxes; ++b)
@@ -478,13 +503,13 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (a.after_prefix) grid_dependency_wait();  // what follows this kernel needs the prefix's results too
 }
 
-template <int D, bool WIN>
+template <int D, bool WIN, bool SPLIT>
 cudaError_t launch(const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap, const CUtensorMap& vmap,
-                   const AtKernelArgs& a, cudaStream_t st) {
+                   const RestMap<SPLIT>& rest, const AtKernelArgs& a, cudaStream_t st) {
   using C = RowsCfg<D>;
-  const cudaError_t e = allow_smem<rows_kernel<D, WIN>>(C::kSmem);
+  const cudaError_t e = allow_smem<rows_kernel<D, WIN, SPLIT>>(C::kSmem);
   if (e != cudaSuccess) return e;
-  return launch_after(rows_kernel<D, WIN>, p.grid, kThreads, C::kSmem, st, qmap, kmap, vmap, a);
+  return launch_after(rows_kernel<D, WIN, SPLIT>, p.grid, kThreads, C::kSmem, st, qmap, kmap, vmap, rest, a);
 }
 
 }  // namespace

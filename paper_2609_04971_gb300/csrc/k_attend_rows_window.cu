@@ -5,7 +5,9 @@ namespace bkv {
 
 cudaError_t launch_attend_rows_window(int d, const AtPlan& p, const CUtensorMap& qmap, const CUtensorMap& kmap,
                                       const CUtensorMap& vmap, const AtKernelArgs& a, cudaStream_t st) {
-  return d == 128 ? launch<128, true>(p, qmap, kmap, vmap, a, st) : launch<64, true>(p, qmap, kmap, vmap, a, st);
+  const RestMap<false> none;
+  return d == 128 ? launch<128, true>(p, qmap, kmap, vmap, none, a, st)
+                  : launch<64, true>(p, qmap, kmap, vmap, none, a, st);
 }
 
 }  // namespace bkv

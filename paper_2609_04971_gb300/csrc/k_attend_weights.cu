@@ -143,18 +143,20 @@ struct Desc {
                                                         // prev_ends = 0 where that group needs no help
 };
 
-template <int D>
+// SPLIT: q and K hold fp16 numbers, and the keys are sums of two terms.
+template <int D, bool SPLIT>
 struct WCfg {
   static constexpr int kBoxes = D / 64;
-  static constexpr uint32_t kTileBytes = kBoxes * kBox;
-  static constexpr int kStages = D == 128 ? 4 : 8;
-  static constexpr size_t kSmem = 1024 + (2 + kStages) * static_cast<size_t>(kTileBytes);
+  static constexpr uint32_t kTileBytes = kBoxes * kBox, kKBytes = (SPLIT ? 2 : 1) * kTileBytes;
+  static constexpr int kStages = (D == 128 ? 4 : 8) / (SPLIT ? 2 : 1);
+  static constexpr size_t kSmem = 1024 + 2 * static_cast<size_t>(kKBytes) + kStages * static_cast<size_t>(kTileBytes);
 };
 
-template <int D>
+template <int D, bool SPLIT>
 __global__ void __launch_bounds__(kThreads, 1)
-    weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap, WArgs a) {
-  using C = WCfg<D>;
+    weights_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap,
+                   const __grid_constant__ CUtensorMap restmap, WArgs a) {
+  using C = WCfg<D, SPLIT>;
   extern __shared__ unsigned char smem_raw[];
   __shared__ __align__(8) uint64_t full_bar[C::kStages], empty_bar[C::kStages];
   __shared__ __align__(8) uint64_t kfull_bar[2], kempty_bar[2], sfull_bar[kBufs], meet_bar, drain_bar;
@@ -171,7 +173,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   unsigned char* base = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
   unsigned char* k_smem = base;
-  unsigned char* q_smem = base + 2 * C::kTileBytes;
+  unsigned char* q_smem = base + 2 * C::kKBytes;
   volatile int* abort_flag = &abort_sh;
 
   if (tid == 0) {
@@ -240,10 +242,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (i == 0 || u.k == 0) {  // a new tile of keys
           const int kb = n_k & 1;
           if (n_k >= 2 && !at_wait(&kempty_bar[kb], ((n_k >> 1) - 1) & 1, abort_flag, a.err, kDevTimeoutProducer)) break;
-          mbar_arrive_expect_tx(&kfull_bar[kb], C::kTileBytes);
-          for (int b = 0; b < C::kBoxes; ++b)
-            tma_load_2d(k_smem + kb * C::kTileBytes + b * kBox, &kmap, &kfull_bar[kb], b * 64,
-                        u.e * a.cap + u.t * kAtTile, pol);
+          mbar_arrive_expect_tx(&kfull_bar[kb], C::kKBytes);
+          for (int b = 0; b < C::kBoxes; ++b) {
+            const int row = u.e * a.cap + u.t * kAtTile;
+            unsigned char* dst = k_smem + kb * C::kKBytes + b * kBox;
+            tma_load_2d(dst, &kmap, &kfull_bar[kb], b * 64, row, pol);
+            if (SPLIT) tma_load_2d(dst + C::kTileBytes, &restmap, &kfull_bar[kb], b * 64, row, pol);
+          }
           ++n_k;
         }
         const int st = i % C::kStages;
@@ -287,14 +292,21 @@ __global__ void __launch_bounds__(kThreads, 1)
         // buffer of S, are done.  It stays until those of this unit are.
         const int cols = __shfl_sync(0xffffffffu, desc_sh[x].ends_cols, 0), ends = cols >> 16;
         tc_fence_after();
-        const uint32_t idesc = idesc_bf16_f32(128, ((cols & 0xFFFF) + 15) / 16 * 16);
-        const uint64_t k = sdesc_kmajor_sw128(k_addr + (n_k & 1) * C::kTileBytes);
+        const int n = ((cols & 0xFFFF) + 15) / 16 * 16;
+        const uint32_t idesc = SPLIT ? idesc_f16_f32(128, n) : idesc_bf16_f32(128, n);
+        const uint64_t k = sdesc_kmajor_sw128(k_addr + (n_k & 1) * C::kKBytes);
         const uint64_t q = sdesc_kmajor_sw128(q_addr + st * C::kTileBytes);
         if (elect_one()) {
 #pragma unroll
           for (int kk = 0; kk < D / 16; ++kk)
             mma_bf16_ss(tm + buf * kCols, k + (((kk >> 2) * kBox + (kk & 3) * 32) >> 4),
                         q + (((kk >> 2) * kBox + (kk & 3) * 32) >> 4), idesc, kk > 0);
+          if (SPLIT) {
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk)
+              mma_bf16_ss(tm + buf * kCols, k + ((C::kTileBytes + (kk >> 2) * kBox + (kk & 3) * 32) >> 4),
+                          q + (((kk >> 2) * kBox + (kk & 3) * 32) >> 4), idesc, 1);
+          }
           mma_commit(&empty_bar[st]);
           mma_commit(&sfull_bar[buf]);
           if (ends) mma_commit(&kempty_bar[n_k & 1]);
@@ -485,11 +497,13 @@ __global__ void __launch_bounds__(kAtTile) weights_merge_kernel(WArgs a) {
   a.weights[static_cast<size_t>(e) * a.cap + j] += sum;
 }
 
-template <int D>
-cudaError_t launch(const CUtensorMap& qmap, const CUtensorMap& kmap, const WArgs& a, cudaStream_t st) {
-  const cudaError_t e = allow_smem<weights_kernel<D>>(WCfg<D>::kSmem);
+template <int D, bool SPLIT>
+cudaError_t launch(const CUtensorMap& qmap, const CUtensorMap& kmap, const CUtensorMap& restmap, const WArgs& a,
+                   cudaStream_t st) {
+  constexpr size_t smem = WCfg<D, SPLIT>::kSmem;
+  const cudaError_t e = allow_smem<weights_kernel<D, SPLIT>>(smem);
   if (e != cudaSuccess) return e;
-  const cudaError_t w = launch_after(weights_kernel<D>, a.ctas, kThreads, WCfg<D>::kSmem, st, qmap, kmap, a);
+  const cudaError_t w = launch_after(weights_kernel<D, SPLIT>, a.ctas, kThreads, smem, st, qmap, kmap, restmap, a);
   if (w != cudaSuccess) return w;
   return launch_after(weights_merge_kernel, static_cast<unsigned>(a.I) * a.tiles, kAtTile, 0, st, a);
 }
@@ -521,11 +535,16 @@ cudaError_t launch_attend_weights(const Shape& s, const AttendArgs& a, const AtL
   w.by_n_kv = FastDiv(w.n_kv);
   w.by_n_q = FastDiv(w.n_q);
   w.by_tiles = FastDiv(w.tiles);
-  CUtensorMap qmap, kmap;
+  CUtensorMap qmap, kmap, restmap{};
   if (encode_queries_bf16(&qmap, a.q, s.batch, s.n_kv, w.R, s.d, 1, w.brow) != CUDA_SUCCESS ||
       encode_rows_bf16(&kmap, a.K, static_cast<uint64_t>(w.I) * s.cap, s.d, kAtTile) != CUDA_SUCCESS)
     return cudaErrorInvalidValue;
-  return s.d == 128 ? launch<128>(qmap, kmap, w, st) : launch<64>(qmap, kmap, w, st);
+  if (a.K_rest) {
+    if (encode_rows_bf16(&restmap, a.K_rest, static_cast<uint64_t>(w.I) * s.cap, s.d, kAtTile) != CUDA_SUCCESS)
+      return cudaErrorInvalidValue;
+    return s.d == 128 ? launch<128, true>(qmap, kmap, restmap, w, st) : launch<64, true>(qmap, kmap, restmap, w, st);
+  }
+  return s.d == 128 ? launch<128, false>(qmap, kmap, restmap, w, st) : launch<64, false>(qmap, kmap, restmap, w, st);
 }
 
 }  // namespace bkv

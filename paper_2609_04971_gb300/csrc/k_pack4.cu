@@ -158,6 +158,63 @@ __global__ void __launch_bounds__(kPackThreads) pack4_kernel(Pack4Args a, FastDi
   }
 }
 
+// For the attention of many rows: its operands are fp16 numbers, and a key, of up to 15 significant bits beside low's
+// 11, is a sum of two.
+__device__ __forceinline__ float to_f16_range(float v) { return fminf(fmaxf(v, -kHalfMax), kHalfMax); }
+__device__ __forceinline__ void values16(uint32_t codes, uint32_t scale, uint4& hi, uint4& rest) {
+  const float step = __half2float(__ushort_as_half(static_cast<unsigned short>(scale & 0xFFFFu))),
+              low = __half2float(__ushort_as_half(static_cast<unsigned short>(scale >> 16)));
+  uint32_t h[4], r[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float a = to_f16_range(fmaf(step, static_cast<float>((codes >> (8 * i)) & 15u), low)),
+                b = to_f16_range(fmaf(step, static_cast<float>((codes >> (8 * i + 4)) & 15u), low));
+    h[i] = pack_f16(a, b);
+    const float2 back = __half22float2(*reinterpret_cast<__half2*>(&h[i]));
+    r[i] = pack_f16(a - back.x, b - back.y);
+  }
+  hi = make_uint4(h[0], h[1], h[2], h[3]);
+  rest = make_uint4(r[0], r[1], r[2], r[3]);
+}
+
+template <int D>
+__global__ void __launch_bounds__(kPackThreads) unpack16_kernel(Unpack16Args a, FastDiv by_blocks, int row_blocks) {
+  constexpr int T = D / 8, kRows = kPackThreads / T, kGroups = D / 32;
+  grid_dependency_wait();
+  grid_dependents_go();
+  if (static_cast<int>(blockIdx.x) >= row_blocks) {  // queries
+    const size_t i = static_cast<size_t>(blockIdx.x - row_blocks) * kPackThreads + threadIdx.x;
+    if (i >= a.q_vecs) return;
+    const uint4 v = __ldg(a.q + i);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t h[4];
+#pragma unroll
+    for (int y = 0; y < 4; ++y) h[y] = pack_f16(to_f16_range(bf16_lo(w[y])), to_f16_range(bf16_hi(w[y])));
+    a.q16[i] = make_uint4(h[0], h[1], h[2], h[3]);
+    return;
+  }
+  int e;
+  const int i0 = by_blocks.mod(blockIdx.x, e) * kRows;
+  int len = __ldg(a.len + e);
+  if (len > a.cap) len = 0;  // the attention reports it
+  if (i0 >= len) return;
+  const int i = threadIdx.x % T, r = i0 + threadIdx.x / T, row0 = (threadIdx.x & 31) / T * T;
+  const bool mine = r < len;
+  const int grp = i >> 2, t = i & 3;
+  const size_t row = static_cast<size_t>(e) * a.cap + r;
+  const uint32_t kw = mine ? __ldg(a.K4 + row * T + t * kGroups + grp) : 0u, vw = mine ? __ldg(a.V4 + row * T + i) : 0u;
+  const uint32_t ks = mine ? __ldg(a.S4 + row * (2 * kGroups) + grp) : 0u,
+                 vs = mine ? __ldg(a.S4 + row * (2 * kGroups) + kGroups + grp) : 0u;
+  const uint32_t vc = codes_of_v<D>(vw, i, row0);
+  if (!mine) return;
+  uint4 hi, rest, none;
+  values16(kw, ks, hi, rest);
+  a.K[row * T + i] = hi;
+  a.K_rest[row * T + i] = rest;
+  values16(vc, vs, hi, none);
+  a.V[row * T + i] = hi;
+}
+
 template <bool PACK>
 cudaError_t launch(int d, const Pack4Args& a, cudaStream_t st) {
   const int rows = kPackThreads / (d / 8), blocks = (a.n_rows + rows - 1) / rows;
@@ -167,6 +224,12 @@ cudaError_t launch(int d, const Pack4Args& a, cudaStream_t st) {
 
 }  // namespace
 
+cudaError_t launch_unpack16(int d, const Unpack16Args& a, cudaStream_t st) {
+  const int rows = kPackThreads / (d / 8), blocks = (a.cap + rows - 1) / rows, row_blocks = a.n_inst * blocks;
+  const unsigned q_blocks = static_cast<unsigned>((a.q_vecs + kPackThreads - 1) / kPackThreads);
+  return launch_after(d == 128 ? unpack16_kernel<128> : unpack16_kernel<64>, row_blocks + q_blocks, kPackThreads, 0, st,
+                      a, FastDiv(blocks), row_blocks);
+}
 cudaError_t launch_pack4(int d, const Pack4Args& a, cudaStream_t st) { return launch<true>(d, a, st); }
 cudaError_t launch_unpack4(int d, const Pack4Args& a, cudaStream_t st) { return launch<false>(d, a, st); }
 

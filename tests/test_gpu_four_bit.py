@@ -11,7 +11,11 @@ bkv_attend4 on the codes, with B_j = scale * sum_g (step_jg sum n |q| + |low_jg|
 - o: p step is rounded to fp16 (2^-11), and where it lies below fp16's normal range, whose lower end is 2^-21 of the
   largest step at most, by 2^-32 of the largest step, 15 times that as a code; the result to bf16 (2^-8):
   |o - o64| <= 2^-8 |o| + sum_j p_j ((2^-11 + 2 delta) step_j n_j + 2 delta |low_j|) + len 2^-28 max step.
-More rows are read as bf16: bkv_attend's tolerances, with the caches' rows rounded to bf16.
+More rows read the values as fp16 numbers, with S_j = scale sum |q k_j|:
+- a logit takes twice the head_dim additions (K is a sum of two terms, off by 2^-22 of itself): 2^-15 S, and query elements
+  below 2^-14 are off by 2^-25 at most: scale sum |k| 2^-25;
+- o: the weights (2^-11, below 2^-14 of the first key's 2^-25 of that) and V (2^-11, below 2^-14 2^-25) are rounded to fp16:
+  |o - o64| <= 2^-8 |o| + (2^-10 + 2 delta) sum p |v| + 2^-25 (len max |v| + 1).
 """
 import math
 
@@ -196,7 +200,7 @@ def test_pack_lengths_out_of_range():
 
 
 # ------------------------------------------------------------------------------------------ attention
-def reference4(q, K4, V4, S4, lens, scale=None):
+def reference4(q, K4, V4, S4, lens, scale=None, many=False):
     b, hq, n_q, d = q.shape
     hkv, cap = K4.shape[1:3]
     G = hq // hkv
@@ -216,18 +220,25 @@ def reference4(q, K4, V4, S4, lens, scale=None):
             seen = torch.arange(n, device=DEV)[None] < n - n_q + 1 + i
             qq = q[x, y * G:(y + 1) * G].reshape(G * n_q, d).double()
             z = (qq @ k.T * scale).masked_fill(~seen, -math.inf)
-            B = (qq.abs() @ (k_sn + k_low.abs()).T * scale).masked_fill(~seen, 0).amax(-1)
+            terms = k.abs() if many else k_sn + k_low.abs()
+            err = qq.abs() @ terms.T * scale * 2.0 ** (-15 if many else -16)
+            if many:
+                err = err + k.abs().sum(-1) * scale * 2.0 ** -25
+            err = err.masked_fill(~seen, 0).amax(-1)
             t = torch.logsumexp(z, -1)
             p = torch.exp(z - torch.where(t == -math.inf, 0.0, t)[:, None])
-            delta = (2 * 2.0 ** -16 * B + 2.0 ** -14)[:, None]
+            delta = (2 * err + 2.0 ** -14)[:, None]
             r = slice(y * G, (y + 1) * G)
             oo = p @ v
             o[x, r] = oo.view(G, n_q, d)
-            step = float(S4[x, y, :n, 1, :, 0].max())
-            to[x, r] = (2.0 ** -8 * oo.abs() + (2.0 ** -11 + 2 * delta) * (p @ v_sn) + 2 * delta * (p @ v_low.abs())
-                        + n * 2.0 ** -28 * step).view(G, n_q, d)
+            if many:
+                off = (2.0 ** -10 + 2 * delta) * (p @ v.abs()) + 2.0 ** -25 * (n * v.abs().max() + 1)
+            else:
+                off = ((2.0 ** -11 + 2 * delta) * (p @ v_sn) + 2 * delta * (p @ v_low.abs())
+                       + n * 2.0 ** -28 * float(S4[x, y, :n, 1, :, 0].max()))
+            to[x, r] = (2.0 ** -8 * oo.abs() + off).view(G, n_q, d)
             lse[x, r] = t.view(G, n_q)
-            tl[x, r] = (2.0 ** -16 * B + 2.0 ** -15 + 2.0 ** -22 * t.abs()).view(G, n_q)
+            tl[x, r] = (err + 2.0 ** -15 + 2.0 ** -22 * t.abs()).view(G, n_q)
             w[x, y, :n] = p.sum(0)
             tw[x, y, :n] = (p * delta).sum(0) + (G * n_q + 8) * 2.0 ** -24 * w[x, y, :n]
     return (o, lse, w), (to, tl, tw)
@@ -296,20 +307,36 @@ def test_several_tokens(d, G, n_q):
 
 
 @pytest.mark.parametrize("d", [64, 128])
-@pytest.mark.parametrize("G,n_q,weights", [(4, 9, True), (4, 25, False), (1, 97, True), (8, 40, True), (2, 300, False)])
-def test_many_rows_are_read_as_bf16(d, G, n_q, weights):
-    b, hkv, cap = 2, 2, 450
-    lens = ga._lens(b, hkv, [450, 301, 129, 5])
+@pytest.mark.parametrize("G,n_q,weights", [(4, 9, True), (4, 25, False), (1, 97, True), (8, 40, True), (2, 300, False),
+                                           (5, 130, True)])
+def test_many_rows_are_read_as_fp16(d, G, n_q, weights):
+    b, hkv, cap = 2, 2, 750
+    lens = ga._lens(b, hkv, [750, 301, 129, 5])
     q, cache = case(b, G * hkv, hkv, d, cap, n_q, lens, seed=n_q)
-    K, V = (values64(cache[i], cache[2], i)[0].bfloat16() for i in (0, 1))
-    for x in range(b):
-        for y in range(hkv):
-            K[x, y, int(lens[x, y]):] = 0
-            V[x, y, int(lens[x, y]):] = 0
     bk = ga._bk(b, G * hkv, hkv, d, cap)
     try:
-        ref = ga.reference(q, K, V, lens)
-        run4(bk, q, cache, lens, weights=weights, ref=ref)
+        run4(bk, q, cache, lens, weights=weights, ref=reference4(q, *cache, lens, many=True))
+    finally:
+        bk.close()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_references_move_with_many_rows(d):
+    """Logits that rise by hundreds along a cache, in fp16: the references follow before a weight is too large."""
+    b, hq, hkv, cap, n_q = 2, 4, 2, 900, 150
+    lens = ga._lens(b, hkv, [900, 513, 899, 640])
+    g = torch.Generator(device=DEV).manual_seed(9)
+    ramp = torch.linspace(0.1, 12, cap, device=DEV)[:, None]
+    u = torch.randn(b, hkv, 1, d, generator=g, device=DEV)
+    K = (u * ramp + torch.randn(b, hkv, cap, d, generator=g, device=DEV)).bfloat16()
+    V = torch.randn(b, hkv, cap, d, generator=g, device=DEV).bfloat16()
+    q = (torch.randn(b, hq, n_q, d, generator=g, device=DEV) + 4 * u.repeat_interleave(2, 1)).bfloat16()
+    cache = packed(K, V)
+    poison(cache, lens)
+    bk = ga._bk(b, hq, hkv, d, cap)
+    try:
+        for qq in (q, -q):
+            run4(bk, qq, cache, lens, ref=reference4(qq, *cache, lens, many=True))
     finally:
         bk.close()
 
