@@ -85,25 +85,57 @@ struct Slice4 {
 template <int D, int NB>
 struct Cfg4 {
   static constexpr int kRow = D + 4;  // floats of a joined row, so that a warp's stores meet no bank twice
-  static constexpr size_t kSmem = sizeof(float) * kWarps4 * 8 * NB * kRow;
+  static constexpr size_t kJoin = sizeof(float) * kWarps4 * 8 * NB * kRow;
+  // a slot of a warp's ring: a slice's rows of K, V and scales
+  static constexpr uint32_t kCodes = kSlice * D / 2, kScales = kSlice * D / 4, kSlot = 2 * kCodes + kScales;
+  static constexpr int kDepth = (D == 128 ? 8 : 16) / NB + (NB > 1 ? 2 : 0);
+  static constexpr size_t kSmem = kJoin + static_cast<size_t>(kWarps4) * kDepth * kSlot;
 };
 
 template <int N>
-__device__ __forceinline__ void load_words(uint32_t (&w)[N], const uint32_t* p) {
+__device__ __forceinline__ void load_words(uint32_t (&w)[N], const void* p) {
   if constexpr (N == 4) {
-    const uint4 x = __ldg(reinterpret_cast<const uint4*>(p));
-    w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+    const uint4 x = *reinterpret_cast<const uint4*>(p);
+    w[0] = x.x;
+    w[1] = x.y;
+    w[2] = x.z;
+    w[3] = x.w;
   } else if constexpr (N == 2) {
-    const uint2 x = __ldg(reinterpret_cast<const uint2*>(p));
-    w[0] = x.x; w[1] = x.y;
+    const uint2 x = *reinterpret_cast<const uint2*>(p);
+    w[0] = x.x;
+    w[1] = x.y;
   } else {
-    w[0] = __ldg(p);
+    w[0] = *reinterpret_cast<const uint32_t*>(p);
   }
 }
-template <int N>
-__device__ __forceinline__ void zero_words(uint32_t (&w)[N]) {
-#pragma unroll
-  for (int i = 0; i < N; ++i) w[i] = 0;
+
+// The slices of a warp in the order in which it takes them, ahead of the warp itself.
+struct Ahead4 {
+  AtWalk walk;
+  size_t row;  // of the caches: the present instance's first
+  int j, j_end, len;
+  __device__ __forceinline__ Ahead4(const AtGeo& g, const AtShare& s) : walk(g, s), row(0), j(0), j_end(0), len(0) {}
+  // Moves to a slice there is, if one is left.
+  __device__ __forceinline__ bool find(const AtGeo& g, int warp) {
+    while (j >= j_end) {
+      AtSeg s;
+      if (!walk.next(g, s)) return false;
+      row = static_cast<size_t>(s.e) * g.cap;
+      len = s.len;
+      j = s.t0 * kAtTile + warp * kSlice;
+      j_end = min(s.t1 * kAtTile, at_limit_max(g, s.len, s.r0));
+    }
+    return true;
+  }
+};
+
+// Linear copy of `bytes` (a multiple of 16, both ends 16-byte aligned) into shared memory.
+__device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar, uint64_t policy) {
+  asm volatile(
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(
+          smem_u32(dst)),
+      "l"(src), "r"(bytes), "r"(smem_u32(bar)), "l"(policy)
+      : "memory");
 }
 
 template <int D, int NB>
@@ -111,19 +143,51 @@ __global__ void __launch_bounds__(kThreads4, 1) attend4_kernel(Kernel4Args a) {
   using C = Cfg4<D, NB>;
   constexpr int kG = D / 32, kW = D / 8;  // groups, words of a row
   constexpr int kMt = D / 16;             // tiles of 16 elements of o
-  extern __shared__ __align__(16) float join[];  // [warp][8 NB rows][kRow]
+  extern __shared__ __align__(128) unsigned char smem4[];
+  float* join = reinterpret_cast<float*>(smem4);  // [warp][8 NB rows][kRow]
+  __shared__ __align__(8) uint64_t full_bar[kWarps4][C::kDepth];
   __shared__ float ref_sh[kWarps4][8 * NB], sum_sh[kWarps4][8 * NB];
   __shared__ int scan_sh[kThreads4 / 32];
   __shared__ AtShare share_sh;
 
   const AtGeo& g = a.geo;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, lg = lane >> 2, lt = lane & 3;
+  if (lane == 0) {
+    for (int i = 0; i < C::kDepth; ++i) mbar_init(&full_bar[warp][i], 1);
+    fence_mbar_init();
+  }
   grid_dependency_wait();
   grid_dependents_go();
   if (blockIdx.x == 0) at_check_lengths<kThreads4>(g, a.err);
   at_split_tiles<kThreads4>(g, scan_sh, &share_sh);
   if (tid == 0 && share_sh.left == 0) a.parts.cut[blockIdx.x] = make_int2(-1, -1);
   AtWalk walk(g, share_sh);
+
+  // Every warp has a ring of its own, filled by its first lane: what the warp has read it may overwrite.
+  unsigned char* ring = smem4 + C::kJoin + warp * (C::kDepth * C::kSlot);
+  // with one row block to an instance every key is read once
+  const uint64_t pol = g.nrb == 1 ? l2_policy_evict_first() : l2_policy_evict_last();
+  Ahead4 ahead(g, share_sh);
+  int slot = 0, phase = 0;  // of the slice to come
+  int under_way = 0;        // slices loaded and not yet taken
+  bool ok = true;           // false once a wait expired: nothing is loaded any more
+  auto load_next = [&](int to) {
+    if (!ahead.find(g, warp)) return;
+    if (lane == 0) {
+      const uint32_t n = min(kSlice, ahead.len - ahead.j);
+      const size_t row = ahead.row + ahead.j;
+      unsigned char* dst = ring + to * C::kSlot;
+      uint64_t* bar = &full_bar[warp][to];
+      mbar_arrive_expect_tx(bar, n * (D + D / 4));
+      bulk_load(dst, a.K4 + row * kW, n * (D / 2), bar, pol);
+      bulk_load(dst + 2 * C::kCodes, a.S4 + row * (2 * kG), n * (D / 4), bar, pol);
+      bulk_load(dst + C::kCodes, a.V4 + row * kW, n * (D / 2), bar, pol);
+    }
+    ahead.j += kWarps4 * kSlice;
+    ++under_way;
+  };
+#pragma unroll 1
+  for (int i = 0; i < C::kDepth; ++i) load_next(i);
 
   AtSeg s, next;
   bool more = walk.next(g, next);
@@ -193,26 +257,34 @@ __global__ void __launch_bounds__(kThreads4, 1) attend4_kernel(Kernel4Args a) {
     float grow = 0.f;  // 2^E
 
     const int j_end = min(s.t1 * kAtTile, limit_max);
-    const size_t base = static_cast<size_t>(s.e) * g.cap;
     for (int j0 = s.t0 * kAtTile + warp * kSlice; j0 < j_end; j0 += kWarps4 * kSlice) {
       Slice4<D> x;
+      ok = ok && __all_sync(0xffffffffu, at_wait(&full_bar[warp][slot], phase, nullptr, a.err, kDevTimeoutProducer));
+      if (!ok) break;  // an expired wait: the outputs are invalid, the barriers below are still met
+      const unsigned char* at = ring + slot * C::kSlot;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const int j = j0 + lg + 8 * h;
-        zero_words(x.k[h]);
-        zero_words(x.ks[h]);
-        zero_words(x.vs[h]);
-        if (j < s.len) {
-          load_words(x.k[h], a.K4 + (base + j) * kW + lt * kG);
-          load_words(x.ks[h], a.S4 + (base + j) * (2 * kG));
-          load_words(x.vs[h], a.S4 + (base + j) * (2 * kG) + kG);
-        }
+        const int r = lg + 8 * h;
+        load_words(x.k[h], at + r * (D / 2) + lt * (kG * 4));
+        load_words(x.ks[h], at + 2 * C::kCodes + r * (D / 4));
+        load_words(x.vs[h], at + 2 * C::kCodes + r * (D / 4) + kG * 4);
       }
 #pragma unroll
-      for (int h = 0; h < 4; ++h) {
-        const int j = j0 + 2 * lt + (h & 1) + 8 * (h >> 1);
-        zero_words(x.v[h]);
-        if (j < s.len) load_words(x.v[h], a.V4 + (base + j) * kW + lg * (D / 64));
+      for (int h = 0; h < 4; ++h)
+        load_words(x.v[h], at + C::kCodes + (2 * lt + (h & 1) + 8 * (h >> 1)) * (D / 2) + lg * (D / 16));
+      if (j0 + kSlice > s.len) {  // rows past the length hold anything
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < kG; ++i)
+            if (j0 + lg + 8 * h >= s.len) x.vs[h][i] = 0;
+      }
+      __syncwarp();
+      --under_way;
+      load_next(slot);
+      if (++slot == C::kDepth) {
+        slot = 0;
+        phase ^= 1;
       }
       // ---- logits
       float y[NB][4] = {};
@@ -399,6 +471,15 @@ __global__ void __launch_bounds__(kThreads4, 1) attend4_kernel(Kernel4Args a) {
       }
     }
     __syncthreads();
+  }
+  if (!ok) {  // let every copy already issued land before the CTA exits
+    for (; under_way > 0; --under_way) {
+      at_wait_always(&full_bar[warp][slot], phase, a.err, kDevTimeoutDrain, 1);
+      if (++slot == C::kDepth) {
+        slot = 0;
+        phase ^= 1;
+      }
+    }
   }
 }
 
