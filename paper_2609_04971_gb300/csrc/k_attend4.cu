@@ -30,26 +30,37 @@
 namespace bkv {
 namespace {
 
-constexpr int kWarps4 = 8, kThreads4 = 32 * kWarps4;
-constexpr int kSlice = 16;                 // keys of a warp's step
-constexpr float kAbove4 = 4.f;             // log2 of how far p may exceed 1
-constexpr float kStepTop = 2048.f;         // step 2^E stays at or below it
-constexpr float kCodeUnit = 16777216.f;    // a code n stands as n / 2^24
+constexpr int kSlice = 16, kStep = 2 * kSlice;  // keys of a product, of a warp's step
+constexpr float kAbove4 = 4.f;                  // log2 of how far p may exceed 2^E
+constexpr float kStepTop = 2048.f;              // step 2^E stays at or below it
+constexpr int kMostUp = 11;                     // E stays at or below it
+constexpr float kCodeUnit = 16777216.f;         // a code n stands as n / 2^24
+constexpr float kSumUnit = 64.f;                // sums of queries as fp16 terms are divided by it
 
-// D += A B: A [16 x 16] and B [16 x 8] of fp16, fragments by lane as PTX defines them for m16n8k16.
+// A B + C: A [16 x 16] and B [16 x 8] of fp16, fragments by lane as PTX defines them for m16n8k16.
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                         uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-               : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                              uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 // The transpose of an 8 x 8 matrix of 16-bit numbers, a row to four lanes.
 __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
   uint32_t r;
-  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
   return r;
 }
-__device__ __forceinline__ float2 unpack_f16(uint32_t v) { return __half22float2(*reinterpret_cast<__half2*>(&v)); }
+__device__ __forceinline__ float half_lo(uint32_t v) { return __low2float(*reinterpret_cast<__half2*>(&v)); }
+__device__ __forceinline__ uint32_t max_f16x2(uint32_t a, uint32_t b) {
+  const __half2 m = __hmax2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&m);
+}
 
 // 2^k for any k (0 below the normal range).
 __device__ __forceinline__ float pow2i(int k) {
@@ -73,23 +84,15 @@ struct Kernel4Args {
   int* err;
 };
 
-// What a warp loads of a slice; a thread's lane is 4 g + t.
-template <int D>
-struct Slice4 {
-  static constexpr int kG = D / 32;
-  uint32_t k[2][kG];         // K: words t kG .. of keys g and g + 8, one for each group
-  uint32_t v[4][D / 64];     // V: words g D / 64 .. of keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9
-  uint32_t ks[2][kG], vs[2][kG];  // (step, low) of keys g and g + 8
-};
-
 template <int D, int NB>
 struct Cfg4 {
+  static constexpr int kWarps = NB == 1 ? 12 : 8, kThreads = 32 * kWarps;
   static constexpr int kRow = D + 4;  // floats of a joined row, so that a warp's stores meet no bank twice
-  static constexpr size_t kJoin = sizeof(float) * kWarps4 * 8 * NB * kRow;
-  // a slot of a warp's ring: a slice's rows of K, V and scales
-  static constexpr uint32_t kCodes = kSlice * D / 2, kScales = kSlice * D / 4, kSlot = 2 * kCodes + kScales;
-  static constexpr int kDepth = (D == 128 ? 8 : 16) / NB + (NB > 1 ? 2 : 0);
-  static constexpr size_t kSmem = kJoin + static_cast<size_t>(kWarps4) * kDepth * kSlot;
+  static constexpr size_t kJoin = sizeof(float) * kWarps * 8 * NB * kRow;
+  // a slot of a warp's ring: a step's rows of K, V and scales
+  static constexpr uint32_t kCodes = kStep * D / 2, kScales = kStep * D / 4, kSlot = 2 * kCodes + kScales;
+  static constexpr int kDepth = (D == 128 ? 2 : 4) + (NB > 1);
+  static constexpr size_t kSmem = kJoin + static_cast<size_t>(kWarps) * kDepth * kSlot;
 };
 
 template <int N>
@@ -109,20 +112,21 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[N], const void* p) {
   }
 }
 
-// The slices of a warp in the order in which it takes them, ahead of the warp itself.
+// The steps of a warp in the order in which it takes them, ahead of the warp itself.
+template <int WARPS>
 struct Ahead4 {
   AtWalk walk;
   size_t row;  // of the caches: the present instance's first
   int j, j_end, len;
   __device__ __forceinline__ Ahead4(const AtGeo& g, const AtShare& s) : walk(g, s), row(0), j(0), j_end(0), len(0) {}
-  // Moves to a slice there is, if one is left.
+  // Moves to a step there is, if one is left.
   __device__ __forceinline__ bool find(const AtGeo& g, int warp) {
     while (j >= j_end) {
       AtSeg s;
       if (!walk.next(g, s)) return false;
       row = static_cast<size_t>(s.e) * g.cap;
       len = s.len;
-      j = s.t0 * kAtTile + warp * kSlice;
+      j = s.t0 * kAtTile + warp * kStep;
       j_end = min(s.t1 * kAtTile, at_limit_max(g, s.len, s.r0));
     }
     return true;
@@ -139,15 +143,16 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
 }
 
 template <int D, int NB>
-__global__ void __launch_bounds__(kThreads4, 1) attend4_kernel(Kernel4Args a) {
+__global__ void __launch_bounds__(Cfg4<D, NB>::kThreads, 1) attend4_kernel(Kernel4Args a) {
   using C = Cfg4<D, NB>;
+  constexpr int kWarps = C::kWarps;
   constexpr int kG = D / 32, kW = D / 8;  // groups, words of a row
   constexpr int kMt = D / 16;             // tiles of 16 elements of o
   extern __shared__ __align__(128) unsigned char smem4[];
   float* join = reinterpret_cast<float*>(smem4);  // [warp][8 NB rows][kRow]
-  __shared__ __align__(8) uint64_t full_bar[kWarps4][C::kDepth];
-  __shared__ float ref_sh[kWarps4][8 * NB], sum_sh[kWarps4][8 * NB];
-  __shared__ int scan_sh[kThreads4 / 32];
+  __shared__ __align__(8) uint64_t full_bar[kWarps][C::kDepth];
+  __shared__ float ref_sh[kWarps][8 * NB], sum_sh[kWarps][8 * NB];
+  __shared__ int scan_sh[kWarps];
   __shared__ AtShare share_sh;
 
   const AtGeo& g = a.geo;
@@ -158,8 +163,8 @@ __global__ void __launch_bounds__(kThreads4, 1) attend4_kernel(Kernel4Args a) {
   }
   grid_dependency_wait();
   grid_dependents_go();
-  if (blockIdx.x == 0) at_check_lengths<kThreads4>(g, a.err);
-  at_split_tiles<kThreads4>(g, scan_sh, &share_sh);
+  if (blockIdx.x == 0) at_check_lengths<C::kThreads>(g, a.err);
+  at_split_tiles<C::kThreads>(g, scan_sh, &share_sh);
   if (tid == 0 && share_sh.left == 0) a.parts.cut[blockIdx.x] = make_int2(-1, -1);
   AtWalk walk(g, share_sh);
 
@@ -167,14 +172,14 @@ __global__ void __launch_bounds__(kThreads4, 1) attend4_kernel(Kernel4Args a) {
   unsigned char* ring = smem4 + C::kJoin + warp * (C::kDepth * C::kSlot);
   // with one row block to an instance every key is read once
   const uint64_t pol = g.nrb == 1 ? l2_policy_evict_first() : l2_policy_evict_last();
-  Ahead4 ahead(g, share_sh);
-  int slot = 0, phase = 0;  // of the slice to come
-  int under_way = 0;        // slices loaded and not yet taken
+  Ahead4<kWarps> ahead(g, share_sh);
+  int slot = 0, phase = 0;  // of the step to come
+  int under_way = 0;        // steps loaded and not yet taken
   bool ok = true;           // false once a wait expired: nothing is loaded any more
   auto load_next = [&](int to) {
     if (!ahead.find(g, warp)) return;
     if (lane == 0) {
-      const uint32_t n = min(kSlice, ahead.len - ahead.j);
+      const uint32_t n = min(kStep, ahead.len - ahead.j);
       const size_t row = ahead.row + ahead.j;
       unsigned char* dst = ring + to * C::kSlot;
       uint64_t* bar = &full_bar[warp][to];
@@ -183,7 +188,7 @@ __global__ void __launch_bounds__(kThreads4, 1) attend4_kernel(Kernel4Args a) {
       bulk_load(dst + 2 * C::kCodes, a.S4 + row * (2 * kG), n * (D / 4), bar, pol);
       bulk_load(dst + C::kCodes, a.V4 + row * kW, n * (D / 2), bar, pol);
     }
-    ahead.j += kWarps4 * kSlice;
+    ahead.j += kWarps * kStep;
     ++under_way;
   };
 #pragma unroll 1
@@ -199,19 +204,18 @@ __global__ void __launch_bounds__(kThreads4, 1) attend4_kernel(Kernel4Args a) {
     const int limit_max = at_limit_max(g, s.len, s.r0), limit_min = at_limit_min(g, s.len, s.r0);
     const size_t row0 = static_cast<size_t>(s.e) * g.R + s.r0;  // of q, o and lse
 
-    // ---- the block's queries: right operands, and their sums over groups
-    uint32_t qb[NB][kG][4];
-    float qs[NB][kG][2], unit[NB][2];  // columns 2 t, 2 t + 1
+    // ---- the block's queries: right operands, and their sums over groups as three fp16 terms
+    uint32_t qb[NB][kG][4], qs[NB][2];
+    float unit[NB][2];  // columns 2 t, 2 t + 1: what a logit counts in
     int lim[NB][2];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
       const int c = b * 8 + lg;
-      const bool there = c < cols;
       float x[kG][8], top = 0.f;
 #pragma unroll
       for (int i = 0; i < kG; ++i) {
         uint4 r = make_uint4(0, 0, 0, 0);
-        if (there) r = __ldg(reinterpret_cast<const uint4*>(a.q + (row0 + c) * D + 32 * i + 8 * lt));
+        if (c < cols) r = __ldg(reinterpret_cast<const uint4*>(a.q + (row0 + c) * D + 32 * i + 8 * lt));
         const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
         for (int y = 0; y < 4; ++y) {
@@ -222,9 +226,9 @@ __global__ void __launch_bounds__(kThreads4, 1) attend4_kernel(Kernel4Args a) {
       }
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
       top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      const int ex = max(exponent(top), -115);
+      const int ex = top == 0.f ? 0 : max(exponent(top), -115);
       const float up = pow2i(11 - ex);
-      float sums[kG];
+      float term[kG][3];
 #pragma unroll
       for (int i = 0; i < kG; ++i) {
         float sum = 0.f;
@@ -232,52 +236,251 @@ __global__ void __launch_bounds__(kThreads4, 1) attend4_kernel(Kernel4Args a) {
         for (int y = 0; y < 8; ++y) sum += x[i][y] *= up;
         sum += __shfl_xor_sync(0xffffffffu, sum, 1);
         sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-        sums[i] = sum * (1.f / kCodeUnit);
+        sum *= 1.f / kSumUnit;
+#pragma unroll
+        for (int z = 0; z < 3; ++z) {
+          term[i][z] = __half2float(__float2half_rn(sum));
+          sum -= term[i][z];
+        }
         // codes 2 y and 2 y + 1 of a byte: the second stands 16 times as high
         qb[b][i][0] = pack_f16(x[i][0], x[i][4]);
         qb[b][i][1] = pack_f16(x[i][1] * 0.0625f, x[i][5] * 0.0625f);
         qb[b][i][2] = pack_f16(x[i][2], x[i][6]);
         qb[b][i][3] = pack_f16(x[i][3] * 0.0625f, x[i][7] * 0.0625f);
       }
+      // Products with the keys' lows: k = 2 t, 2 t + 1 are a pair of groups and a term, k = 2 t + 8, 2 t + 9 too.
+      if constexpr (D == 128) {
+        const bool odd = lt & 1;
+        const float h0 = odd ? term[2][0] : term[0][0], h1 = odd ? term[3][0] : term[1][0];
+        const float m0 = odd ? term[2][1] : term[0][1], m1 = odd ? term[3][1] : term[1][1];
+        const float l0 = odd ? term[2][2] : term[0][2], l1 = odd ? term[3][2] : term[1][2];
+        qs[b][0] = lt < 2 ? pack_f16(h0, h1) : pack_f16(m0, m1);
+        qs[b][1] = lt < 2 ? pack_f16(l0, l1) : 0u;
+      } else {
+        qs[b][0] = lt == 0   ? pack_f16(term[0][0], term[1][0])
+                   : lt == 1 ? pack_f16(term[0][1], term[1][1])
+                   : lt == 2 ? pack_f16(term[0][2], term[1][2])
+                             : 0u;
+        qs[b][1] = 0u;
+      }
       // columns 2 t and 2 t + 1 are the rows of lanes 8 t and 8 t + 4
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
-        const int from = 8 * lt + 4 * y;
-#pragma unroll
-        for (int i = 0; i < kG; ++i) qs[b][i][y] = __shfl_sync(0xffffffffu, sums[i], from);
-        unit[b][y] = pow2i(__shfl_sync(0xffffffffu, ex, from) + 13);
+        unit[b][y] = pow2i(__shfl_sync(0xffffffffu, ex, 8 * lt + 4 * y) + 13);
         const int cc = b * 8 + 2 * lt + y;
         lim[b][y] = cc < cols ? at_limit(g, s.len, s.r0, cc) : 0;
       }
     }
 
-    float o[NB][kMt][4] = {}, ol[NB][kG][2] = {}, l[NB][2] = {}, ref[NB][2];
+    // p = 2^(y - ref): ref is the reference of the column less E
+    float o[NB][kMt][4] = {}, low[NB][4] = {}, l[NB][2] = {}, ref[NB][2];
+    int up = -1000;  // E; none yet
 #pragma unroll
-    for (int b = 0; b < NB; ++b) ref[b][0] = ref[b][1] = kRefFloor;
-    float grow = 0.f;  // 2^E
+    for (int b = 0; b < NB; ++b) ref[b][0] = ref[b][1] = 0.f;
 
     const int j_end = min(s.t1 * kAtTile, limit_max);
-    for (int j0 = s.t0 * kAtTile + warp * kSlice; j0 < j_end; j0 += kWarps4 * kSlice) {
-      Slice4<D> x;
+#pragma unroll 1
+    for (int j0 = s.t0 * kAtTile + warp * kStep; j0 < j_end; j0 += kWarps * kStep) {
       ok = ok && __all_sync(0xffffffffu, at_wait(&full_bar[warp][slot], phase, nullptr, a.err, kDevTimeoutProducer));
       if (!ok) break;  // an expired wait: the outputs are invalid, the barriers below are still met
       const unsigned char* at = ring + slot * C::kSlot;
+      const unsigned char* scales = at + 2 * C::kCodes;
+      const bool tail = j0 + kStep > s.len;  // rows past the length hold anything
+      // ---- logits, in the columns' units
+      float y[2][NB][4];
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int r = lg + 8 * h;
-        load_words(x.k[h], at + r * (D / 2) + lt * (kG * 4));
-        load_words(x.ks[h], at + 2 * C::kCodes + r * (D / 4));
-        load_words(x.vs[h], at + 2 * C::kCodes + r * (D / 4) + kG * 4);
+      for (int u = 0; u < 2; ++u) {
+        uint32_t k[2][kG], ks[2][kG];
+        uint32_t lows[2];  // of a pair of groups of keys g and g + 8
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int r = u * kSlice + lg + 8 * h;
+          load_words(k[h], at + r * (D / 2) + lt * (kG * 4));
+          load_words(ks[h], scales + r * (D / 4));
+          uint32_t pair[2];
+          load_words(pair, scales + r * (D / 4) + (D == 128 ? (lt & 1) * 8 : 0));
+          lows[h] = __byte_perm(pair[0], pair[1], 0x7632);
+        }
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          float c[4];
+          mma_f16_first(c, lows[0], lows[1], lows[0], lows[1], qs[b][0], qs[b][1]);
+#pragma unroll
+          for (int z = 0; z < 4; ++z) y[u][b][z] = c[z] * (kSumUnit / kCodeUnit);
+        }
+#pragma unroll
+        for (int i = 0; i < kG; ++i) {
+          uint32_t f[2][4];  // codes (0, 4), (1, 5), (2, 6), (3, 7) of the word
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const uint32_t w = k[h][i], w8 = w >> 8;
+            f[h][0] = w & 0x000F000Fu;
+            f[h][1] = w & 0x00F000F0u;
+            f[h][2] = w8 & 0x000F000Fu;
+            f[h][3] = w8 & 0x00F000F0u;
+          }
+          const float s0 = half_lo(ks[0][i]), s1 = half_lo(ks[1][i]);
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            float c[4];
+            mma_f16_first(c, f[0][0], f[1][0], f[0][1], f[1][1], qb[b][i][0], qb[b][i][1]);
+            mma_f16(c, f[0][2], f[1][2], f[0][3], f[1][3], qb[b][i][2], qb[b][i][3]);
+            y[u][b][0] = fmaf(s0, c[0], y[u][b][0]);
+            y[u][b][1] = fmaf(s0, c[1], y[u][b][1]);
+            y[u][b][2] = fmaf(s1, c[2], y[u][b][2]);
+            y[u][b][3] = fmaf(s1, c[3], y[u][b][3]);
+          }
+        }
+      }
+      if (a.logits) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int z = 0; z < 2; ++z) {
+            const int c = b * 8 + 2 * lt + z;
+            if (c < cols) {
+              float* dst = a.logits + (row0 + c) * g.cap + j0 + lg;
+#pragma unroll
+              for (int r = 0; r < 4; ++r)
+                if (!tail || j0 + lg + 8 * r < s.len) dst[8 * r] = y[r >> 1][b][z + 2 * (r & 1)] * unit[b][z];
+            }
+          }
+      }
+      // the largest step of V
+      auto v_scales = [&](int u, int h, uint32_t(&w)[kG]) {  // (step, low) of keys g and g + 8 of a product
+        const int r = u * kSlice + lg + 8 * h;
+        load_words(w, scales + r * (D / 4) + kG * 4);
+        if (tail && j0 + r >= s.len) {
+#pragma unroll
+          for (int i = 0; i < kG; ++i) w[i] = 0;
+        }
+      };
+      uint32_t top2 = 0;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        uint32_t w[kG];
+        v_scales(x >> 1, x & 1, w);
+#pragma unroll
+        for (int i = 0; i < kG; ++i) top2 = max_f16x2(top2, w[i]);
+      }
+      // ---- to base 2, against the references
+      const float step = half_lo(top2), most = 16.f * pow2i(up);  // p 2^-E may be 2^4
+      float above = -INFINITY;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int z = 0; z < 4; ++z) {
+          const float f = unit[b][z & 1] * a.sc;
+          y[0][b][z] = fmaf(y[0][b][z], f, -ref[b][z & 1]);
+          y[1][b][z] = fmaf(y[1][b][z], f, -ref[b][z & 1]);
+        }
+      if (j0 + kStep > limit_min) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int z = 0; z < 4; ++z)
+              if (j0 + u * kSlice + lg + 8 * (z >> 1) >= lim[b][z & 1]) y[u][b][z] = -INFINITY;
       }
 #pragma unroll
-      for (int h = 0; h < 4; ++h)
-        load_words(x.v[h], at + C::kCodes + (2 * lt + (h & 1) + 8 * (h >> 1)) * (D / 2) + lg * (D / 16));
-      if (j0 + kSlice > s.len) {  // rows past the length hold anything
+      for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int z = 0; z < 4; ++z) above = fmaxf(above, fmaxf(y[0][b][z], y[1][b][z]));
+      if (__any_sync(0xffffffffu, above > kAbove4 + up || step * most > 16.f * kStepTop || up < -999)) {
+        // Move the references to the step's maxima, and the steps' scale.  A column that sees nothing of a warp's
+        // first step sees nothing after it either: it stays at the floor.
+        float top = step;
 #pragma unroll
-          for (int i = 0; i < kG; ++i)
-            if (j0 + lg + 8 * h >= s.len) x.vs[h][i] = 0;
+        for (int m = 1; m < 32; m <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+        const int now = up < -999 || top * most > 16.f * kStepTop ? min(kMostUp, 7 - exponent(top)) : up;
+        const bool begins = up < -999;
+        const float back = begins ? kRefFloor : static_cast<float>(up);
+        up = now;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int z = 0; z < 2; ++z) {
+            float v = fmaxf(fmaxf(y[0][b][z], y[0][b][z + 2]), fmaxf(y[1][b][z], y[1][b][z + 2]));
+#pragma unroll
+            for (int m = 4; m < 32; m <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, m));
+            // relative to ref: the reference was at `back`; it moves up to v, and 2^E moves to `now`
+            const float by = fmaxf(v, back) - static_cast<float>(now);
+            const float fac = begins ? 0.f : ex2_approx(-by);
+            ref[b][z] += by;
+            l[b][z] *= fac;
+            low[b][z] *= fac;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              y[u][b][z] -= by;
+              y[u][b][z + 2] -= by;
+            }
+#pragma unroll
+            for (int m = 0; m < kMt; ++m) {
+              o[b][m][z] *= fac;
+              o[b][m][z + 2] *= fac;
+            }
+          }
+      }
+      // ---- weights and values
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        uint32_t vs[2][kG], lv[2];  // lv: lows of group g of keys 2 t, 2 t + 1 and 2 t + 8, 2 t + 9
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          v_scales(u, h, vs[h]);
+          uint32_t w[2];
+#pragma unroll
+          for (int z = 0; z < 2; ++z) {
+            const int r = u * kSlice + 8 * h + 2 * lt + z;
+            w[z] = *reinterpret_cast<const uint32_t*>(scales + r * (D / 4) + kG * 4 + (lg & (kG - 1)) * 4);
+            if (tail && j0 + r >= s.len) w[z] = 0;
+          }
+          lv[h] = __byte_perm(w[0], w[1], 0x7632);
+        }
+        uint32_t pb[NB][kG][2];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          float p[4];
+#pragma unroll
+          for (int z = 0; z < 4; ++z) p[z] = ex2_approx(y[u][b][z]);
+          l[b][0] += p[0] + p[2];
+          l[b][1] += p[1] + p[3];
+#pragma unroll
+          for (int i = 0; i < kG; ++i) {
+            const float s0 = half_lo(vs[0][i]), s1 = half_lo(vs[1][i]);
+            pb[b][i][0] = transpose8(pack_f16(p[0] * s0, p[1] * s0));
+            pb[b][i][1] = transpose8(pack_f16(p[2] * s1, p[3] * s1));
+          }
+          mma_f16(low[b], lv[0], 0u, lv[1], 0u, transpose8(pack_f16(p[0], p[1])),
+                  transpose8(pack_f16(p[2], p[3])));
+        }
+        uint32_t v[4][D / 64];  // words g D / 64 .. of keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9
+#pragma unroll
+        for (int h = 0; h < 4; ++h)
+          load_words(v[h], at + C::kCodes + (u * kSlice + 2 * lt + (h & 1) + 8 * (h >> 1)) * (D / 2) + lg * (D / 16));
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {  // byte m of the words: codes 2 m and 2 m + 1
+          uint32_t f[D / 64][2];       // [word][keys 2 t.., 2 t + 8..]: that byte of both keys
+#pragma unroll
+          for (int w = 0; w < D / 64; ++w)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              f[w][h] = __byte_perm(v[2 * h][w], v[2 * h + 1][w], m | (m << 4) | ((4 + m) << 8) | ((4 + m) << 12));
+          constexpr uint32_t kLo = 0x000F000Fu, kHi = 0x00F000F0u;
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            if constexpr (D == 128) {  // rows g and g + 8: words 2 g and 2 g + 1, one code of each
+              mma_f16(o[b][2 * m], f[0][0] & kLo, f[1][0] & kLo, f[0][1] & kLo, f[1][1] & kLo, pb[b][m][0],
+                      pb[b][m][1]);
+              mma_f16(o[b][2 * m + 1], f[0][0] & kHi, f[1][0] & kHi, f[0][1] & kHi, f[1][1] & kHi, pb[b][m][0],
+                      pb[b][m][1]);
+            } else {  // rows g and g + 8: both codes of word g
+              mma_f16(o[b][m], f[0][0] & kLo, f[0][0] & kHi, f[0][1] & kLo, f[0][1] & kHi, pb[b][m >> 1][0],
+                      pb[b][m >> 1][1]);
+            }
+          }
+        }
       }
       __syncwarp();
       --under_way;
@@ -286,140 +489,18 @@ __global__ void __launch_bounds__(kThreads4, 1) attend4_kernel(Kernel4Args a) {
         slot = 0;
         phase ^= 1;
       }
-      // ---- logits
-      float y[NB][4] = {};
-#pragma unroll
-      for (int i = 0; i < kG; ++i) {
-        uint32_t f[2][4];  // codes (0, 4), (1, 5), (2, 6), (3, 7) of the word
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t w = x.k[h][i], w8 = w >> 8;
-          f[h][0] = w & 0x000F000Fu;
-          f[h][1] = w & 0x00F000F0u;
-          f[h][2] = w8 & 0x000F000Fu;
-          f[h][3] = w8 & 0x00F000F0u;
-        }
-        const float2 s0 = unpack_f16(x.ks[0][i]), s1 = unpack_f16(x.ks[1][i]);
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          float c[4] = {};
-          mma_f16(c, f[0][0], f[1][0], f[0][1], f[1][1], qb[b][i][0], qb[b][i][1]);
-          mma_f16(c, f[0][2], f[1][2], f[0][3], f[1][3], qb[b][i][2], qb[b][i][3]);
-          y[b][0] = fmaf(s0.x, c[0], fmaf(s0.y, qs[b][i][0], y[b][0]));
-          y[b][1] = fmaf(s0.x, c[1], fmaf(s0.y, qs[b][i][1], y[b][1]));
-          y[b][2] = fmaf(s1.x, c[2], fmaf(s1.y, qs[b][i][0], y[b][2]));
-          y[b][3] = fmaf(s1.x, c[3], fmaf(s1.y, qs[b][i][1], y[b][3]));
-        }
-      }
-      // ---- to base 2, against the references
-      float above = -INFINITY;
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-#pragma unroll
-        for (int z = 0; z < 4; ++z) {
-          y[b][z] *= unit[b][z & 1];
-          const int j = j0 + lg + 8 * (z >> 1), c = b * 8 + 2 * lt + (z & 1);
-          if (a.logits && c < cols && j < s.len) a.logits[(row0 + c) * g.cap + j] = y[b][z];
-          y[b][z] *= a.sc;
-          if (j0 + kSlice > limit_min) y[b][z] = j < lim[b][z & 1] ? y[b][z] : -INFINITY;
-          above = fmaxf(above, y[b][z] - ref[b][z & 1]);
-        }
-      }
-      float2 vs[2][kG];
-      float step = 0.f;
-#pragma unroll
-      for (int h = 0; h < 2; ++h)
-#pragma unroll
-        for (int i = 0; i < kG; ++i) {
-          vs[h][i] = unpack_f16(x.vs[h][i]);
-          step = fmaxf(step, vs[h][i].x);
-        }
-      if (__any_sync(0xffffffffu, above > kAbove4 || step * grow > kStepTop || grow == 0.f)) {
-        // move the references to the slice's maxima, and the steps' scale
-        float fac[NB][2];
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-          for (int z = 0; z < 2; ++z) {
-            float v = fmaxf(y[b][z], y[b][z + 2]);
-#pragma unroll
-            for (int m = 4; m < 32; m <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, m));
-            v = fmaxf(v, ref[b][z]);
-            fac[b][z] = ex2_approx(ref[b][z] - v);
-            ref[b][z] = v;
-            l[b][z] *= fac[b][z];
-#pragma unroll
-            for (int i = 0; i < kG; ++i) ol[b][i][z] *= fac[b][z];
-          }
-#pragma unroll
-        for (int m = 1; m < 32; m <<= 1) step = fmaxf(step, __shfl_xor_sync(0xffffffffu, step, m));
-        float regrow = 1.f;
-        if (step * grow > kStepTop || grow == 0.f) {
-          const float now = pow2i(7 - exponent(step));
-          regrow = grow == 0.f ? 0.f : now / grow;
-          grow = now;
-        }
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-          for (int m = 0; m < kMt; ++m)
-#pragma unroll
-            for (int z = 0; z < 4; ++z) o[b][m][z] *= fac[b][z & 1] * regrow;
-      }
-      // ---- weights
-      uint32_t pb[NB][kG][2];
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        float p[4];
-#pragma unroll
-        for (int z = 0; z < 4; ++z) p[z] = ex2_approx(y[b][z] - ref[b][z & 1]);
-        l[b][0] += p[0] + p[2];
-        l[b][1] += p[1] + p[3];
-#pragma unroll
-        for (int i = 0; i < kG; ++i) {
-          ol[b][i][0] = fmaf(p[0], vs[0][i].y, fmaf(p[2], vs[1][i].y, ol[b][i][0]));
-          ol[b][i][1] = fmaf(p[1], vs[0][i].y, fmaf(p[3], vs[1][i].y, ol[b][i][1]));
-          const float s0 = vs[0][i].x * grow, s1 = vs[1][i].x * grow;
-          pb[b][i][0] = transpose8(pack_f16(p[0] * s0, p[1] * s0));
-          pb[b][i][1] = transpose8(pack_f16(p[2] * s1, p[3] * s1));
-        }
-      }
-      // ---- values
-#pragma unroll
-      for (int m = 0; m < 4; ++m) {  // byte m of the words: codes 2 m and 2 m + 1
-        uint32_t f[D / 64][2];       // [word][keys 2 t.., 2 t + 8..]: that byte of both keys
-#pragma unroll
-        for (int w = 0; w < D / 64; ++w)
-#pragma unroll
-          for (int h = 0; h < 2; ++h)
-            f[w][h] = __byte_perm(x.v[2 * h][w], x.v[2 * h + 1][w], m | (m << 4) | ((4 + m) << 8) | ((4 + m) << 12));
-        constexpr uint32_t kLo = 0x000F000Fu, kHi = 0x00F000F0u;
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          if constexpr (D == 128) {  // rows g and g + 8: words 2 g and 2 g + 1, one code of each
-            mma_f16(o[b][2 * m], f[0][0] & kLo, f[1][0] & kLo, f[0][1] & kLo, f[1][1] & kLo, pb[b][m][0], pb[b][m][1]);
-            mma_f16(o[b][2 * m + 1], f[0][0] & kHi, f[1][0] & kHi, f[0][1] & kHi, f[1][1] & kHi, pb[b][m][0],
-                    pb[b][m][1]);
-          } else {  // rows g and g + 8: both codes of word g
-            mma_f16(o[b][m], f[0][0] & kLo, f[0][0] & kHi, f[0][1] & kLo, f[0][1] & kHi, pb[b][m >> 1][0],
-                    pb[b][m >> 1][1]);
-          }
-        }
-      }
     }
 
     // ---- join the warps
-    const float shrink = grow == 0.f ? 0.f : kCodeUnit / grow;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
 #pragma unroll
       for (int z = 0; z < 2; ++z) {
 #pragma unroll
-        for (int m = 4; m < 32; m <<= 1) {
-          l[b][z] += __shfl_xor_sync(0xffffffffu, l[b][z], m);
+        for (int m = 4; m < 32; m <<= 1) l[b][z] += __shfl_xor_sync(0xffffffffu, l[b][z], m);
+        float lo[kG];  // the lanes of row g hold the sums of group g
 #pragma unroll
-          for (int i = 0; i < kG; ++i) ol[b][i][z] += __shfl_xor_sync(0xffffffffu, ol[b][i][z], m);
-        }
+        for (int i = 0; i < kG; ++i) lo[i] = __shfl_sync(0xffffffffu, low[b][z], 4 * i + lt);
         const int c = b * 8 + 2 * lt + z;
         if (lg == 0) {
           ref_sh[warp][c] = ref[b][z];
@@ -428,14 +509,14 @@ __global__ void __launch_bounds__(kThreads4, 1) attend4_kernel(Kernel4Args a) {
         float* dst = join + (warp * 8 * NB + c) * C::kRow;
 #pragma unroll
         for (int m = 0; m < kMt; ++m) {
-          const float lo = ol[b][m / 2][z];
+          constexpr float f0 = kCodeUnit, f1 = kCodeUnit / 16.f;
           if constexpr (D == 128) {
-            const float f = m & 1 ? shrink * 0.0625f : shrink;
+            const float f = m & 1 ? f1 : f0;
             *reinterpret_cast<float2*>(dst + 16 * m + 2 * lg) =
-                make_float2(fmaf(o[b][m][z], f, lo), fmaf(o[b][m][2 + z], f, lo));
+                make_float2(fmaf(o[b][m][z], f, lo[m / 2]), fmaf(o[b][m][2 + z], f, lo[m / 2]));
           } else {
-            dst[16 * m + lg] = fmaf(o[b][m][z], shrink, lo);
-            dst[16 * m + 8 + lg] = fmaf(o[b][m][2 + z], shrink * 0.0625f, lo);
+            dst[16 * m + lg] = fmaf(o[b][m][z], f0, lo[m / 2]);
+            dst[16 * m + 8 + lg] = fmaf(o[b][m][2 + z], f1, lo[m / 2]);
           }
         }
       }
@@ -443,12 +524,12 @@ __global__ void __launch_bounds__(kThreads4, 1) attend4_kernel(Kernel4Args a) {
     __syncthreads();
     const bool whole = s.t0 == 0 && s.t1 == s.T;
     const size_t part = (static_cast<size_t>(blockIdx.x) + s.item) * a.parts.rows;
-    for (int c = warp; c < cols; c += kWarps4) {
-      float m = kRefFloor, sum = 0.f, f[kWarps4];
+    for (int c = warp; c < cols; c += kWarps) {
+      float m = kRefFloor, sum = 0.f, f[kWarps];
 #pragma unroll
-      for (int w = 0; w < kWarps4; ++w) m = fmaxf(m, ref_sh[w][c]);
+      for (int w = 0; w < kWarps; ++w) m = fmaxf(m, ref_sh[w][c]);
 #pragma unroll
-      for (int w = 0; w < kWarps4; ++w) {
+      for (int w = 0; w < kWarps; ++w) {
         f[w] = ex2_approx(ref_sh[w][c] - m);
         sum = fmaf(sum_sh[w][c], f[w], sum);
       }
@@ -456,7 +537,7 @@ __global__ void __launch_bounds__(kThreads4, 1) attend4_kernel(Kernel4Args a) {
       for (int d = lane; d < D; d += 32) {
         float v = 0.f;
 #pragma unroll
-        for (int w = 0; w < kWarps4; ++w) v = fmaf(join[(w * 8 * NB + c) * C::kRow + d], f[w], v);
+        for (int w = 0; w < kWarps; ++w) v = fmaf(join[(w * 8 * NB + c) * C::kRow + d], f[w], v);
         if (whole) a.o[(row0 + c) * D + d] = __float2bfloat16(v * inv);
         else a.parts.o[(part + c) * D + d] = v;
       }
@@ -488,7 +569,7 @@ cudaError_t launch(const AtPlan& p, const Kernel4Args& k, cudaStream_t st) {
   using C = Cfg4<D, NB>;
   const cudaError_t e = allow_smem<attend4_kernel<D, NB>>(C::kSmem);
   if (e != cudaSuccess) return e;
-  return launch_after(attend4_kernel<D, NB>, p.grid, kThreads4, C::kSmem, st, k);
+  return launch_after(attend4_kernel<D, NB>, p.grid, C::kThreads, C::kSmem, st, k);
 }
 
 }  // namespace
