@@ -57,6 +57,11 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t v) {
   return r;
 }
 __device__ __forceinline__ float half_lo(uint32_t v) { return __low2float(*reinterpret_cast<__half2*>(&v)); }
+// Both numbers of `a` times the lower one of `b`.
+__device__ __forceinline__ uint32_t mul_lo(uint32_t a, uint32_t b) {
+  const __half2 m = __hmul2(*reinterpret_cast<__half2*>(&a), __low2half2(*reinterpret_cast<__half2*>(&b)));
+  return *reinterpret_cast<const uint32_t*>(&m);
+}
 __device__ __forceinline__ uint32_t max_f16x2(uint32_t a, uint32_t b) {
   const __half2 m = __hmax2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b));
   return *reinterpret_cast<const uint32_t*>(&m);
@@ -86,13 +91,29 @@ struct Kernel4Args {
 
 template <int D, int NB>
 struct Cfg4 {
-  static constexpr int kWarps = NB == 1 ? 12 : 8, kThreads = 32 * kWarps;
+  // Warps at work on slices, behind three loading ones and one that joins.  Registers: 128 a thread at launch for
+  // 16 warps (168 for 12), of which the first four give back what the others take.
+  static constexpr int kWarps = NB == 1 ? 12 : 8, kFirst = 4;
+  static constexpr int kThreads = 32 * (kFirst + kWarps);
+  static constexpr int kRegsFew = NB == 1 ? 80 : 88, kRegsMany = NB == 1 ? 144 : 208;
   static constexpr int kRow = D + 4;  // floats of a joined row, so that a warp's stores meet no bank twice
   static constexpr size_t kJoin = sizeof(float) * kWarps * 8 * NB * kRow;
-  // a slot of a warp's ring: a step's rows of K, V and scales
-  static constexpr uint32_t kCodes = kStep * D / 2, kScales = kStep * D / 4, kSlot = 2 * kCodes + kScales;
-  static constexpr int kDepth = (D == 128 ? 2 : 4) + (NB > 1);
-  static constexpr size_t kSmem = kJoin + static_cast<size_t>(kWarps) * kDepth * kSlot;
+  // a slot of the ring: a tile's rows of K, V and scales, kPart steps
+  static constexpr uint32_t kCodes = kAtTile * D / 2, kScales = kAtTile * D / 4, kSlot = 2 * kCodes + kScales;
+  static constexpr int kPart = kAtTile / kStep;
+  static constexpr int kSlots = D == 64 ? 16 : NB == 1 ? 8 : 7;
+  static constexpr size_t kSmem = kJoin + static_cast<size_t>(kSlots) * kSlot;
+  static_assert(kWarps % kPart == 0, "a warp takes the same part of every tile of a segment");
+};
+
+// A row block's right operands, by lane: of every group the queries, then the terms of their sums; what a logit of
+// columns 2 t and 2 t + 1 counts in, and how many keys they see.
+template <int D, int NB>
+struct Queries4 {
+  uint4 qb[NB][D / 32][32];
+  uint2 qs[NB][32];
+  float2 unit[NB][32];
+  int2 lim[NB][32];
 };
 
 template <int N>
@@ -112,27 +133,6 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[N], const void* p) {
   }
 }
 
-// The steps of a warp in the order in which it takes them, ahead of the warp itself.
-template <int WARPS>
-struct Ahead4 {
-  AtWalk walk;
-  size_t row;  // of the caches: the present instance's first
-  int j, j_end, len;
-  __device__ __forceinline__ Ahead4(const AtGeo& g, const AtShare& s) : walk(g, s), row(0), j(0), j_end(0), len(0) {}
-  // Moves to a step there is, if one is left.
-  __device__ __forceinline__ bool find(const AtGeo& g, int warp) {
-    while (j >= j_end) {
-      AtSeg s;
-      if (!walk.next(g, s)) return false;
-      row = static_cast<size_t>(s.e) * g.cap;
-      len = s.len;
-      j = s.t0 * kAtTile + warp * kStep;
-      j_end = min(s.t1 * kAtTile, at_limit_max(g, s.len, s.r0));
-    }
-    return true;
-  }
-};
-
 // Linear copy of `bytes` (a multiple of 16, both ends 16-byte aligned) into shared memory.
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar, uint64_t policy) {
   asm volatile(
@@ -142,323 +142,452 @@ __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t b
       : "memory");
 }
 
+// The right operands of the block of rows [row0, row0 + cols), by one warp.
+template <int D, int NB>
+__device__ __forceinline__ void prepare_queries(Queries4<D, NB>& out, const Kernel4Args& a, size_t row0, int cols,
+                                                const AtSeg& s, int lane) {
+  constexpr int kG = D / 32;
+  const int lg = lane >> 2, lt = lane & 3;
+#pragma unroll 1
+  for (int b = 0; b < NB; ++b) {
+    const int c = b * 8 + lg;
+    const uint4* src = reinterpret_cast<const uint4*>(a.q + (row0 + c) * D + 8 * lt);
+    uint4 r[kG];
+    uint32_t top2 = 0;  // the largest magnitude, as bf16
+#pragma unroll
+    for (int i = 0; i < kG; ++i) {
+      r[i] = c < cols ? __ldg(src + 4 * i) : make_uint4(0, 0, 0, 0);
+      const uint32_t w[4] = {r[i].x, r[i].y, r[i].z, r[i].w};
+#pragma unroll
+      for (int y = 0; y < 4; ++y) top2 = __vmaxu2(top2, w[y] & 0x7FFF7FFFu);
+    }
+    top2 = __vmaxu2(top2, __shfl_xor_sync(0xffffffffu, top2, 1));
+    top2 = __vmaxu2(top2, __shfl_xor_sync(0xffffffffu, top2, 2));
+    const float top = fmaxf(__uint_as_float(top2 << 16), __uint_as_float(top2 & 0x7FFF0000u));
+    const int ex = top == 0.f ? 0 : max(exponent(top), -115);
+    const float up = pow2i(11 - ex);
+    float term[kG][3];
+#pragma unroll
+    for (int i = 0; i < kG; ++i) {
+      const uint32_t w[4] = {r[i].x, r[i].y, r[i].z, r[i].w};
+      float lo[4], hi[4], sum = 0.f;  // elements 2 y and 2 y + 1
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        lo[y] = __uint_as_float(w[y] << 16) * up;
+        hi[y] = __uint_as_float(w[y] & 0xFFFF0000u) * up;
+        sum += lo[y] + hi[y];
+      }
+      sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+      sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+      sum *= 1.f / kSumUnit;
+#pragma unroll
+      for (int z = 0; z < 3; ++z) {
+        term[i][z] = __half2float(__float2half_rn(sum));
+        sum -= term[i][z];
+      }
+      // codes 2 y and 2 y + 1 of a byte: the second stands 16 times as high
+      out.qb[b][i][lane] = make_uint4(pack_f16(lo[0], lo[2]), pack_f16(hi[0] * 0.0625f, hi[2] * 0.0625f),
+                                      pack_f16(lo[1], lo[3]), pack_f16(hi[1] * 0.0625f, hi[3] * 0.0625f));
+    }
+    // Products with the keys' lows: k = 2 t, 2 t + 1 are a pair of groups and a term, k = 2 t + 8, 2 t + 9 too.
+    uint2 qs;
+    if constexpr (D == 128) {
+      const bool odd = lt & 1;
+      const float h0 = odd ? term[2][0] : term[0][0], h1 = odd ? term[3][0] : term[1][0];
+      const float m0 = odd ? term[2][1] : term[0][1], m1 = odd ? term[3][1] : term[1][1];
+      const float l0 = odd ? term[2][2] : term[0][2], l1 = odd ? term[3][2] : term[1][2];
+      qs = make_uint2(lt < 2 ? pack_f16(h0, h1) : pack_f16(m0, m1), lt < 2 ? pack_f16(l0, l1) : 0u);
+    } else {
+      qs = make_uint2(lt == 0   ? pack_f16(term[0][0], term[1][0])
+                      : lt == 1 ? pack_f16(term[0][1], term[1][1])
+                      : lt == 2 ? pack_f16(term[0][2], term[1][2])
+                                : 0u,
+                      0u);
+    }
+    out.qs[b][lane] = qs;
+    // columns 2 t and 2 t + 1 are the rows of lanes 8 t and 8 t + 4
+    float unit[2];
+    int lim[2];
+#pragma unroll
+    for (int y = 0; y < 2; ++y) {
+      unit[y] = pow2i(__shfl_sync(0xffffffffu, ex, 8 * lt + 4 * y) + 13);
+      const int cc = b * 8 + 2 * lt + y;
+      lim[y] = cc < cols ? at_limit(a.geo, s.len, s.r0, cc) : 0;
+    }
+    out.unit[b][lane] = make_float2(unit[0], unit[1]);
+    out.lim[b][lane] = make_int2(lim[0], lim[1]);
+  }
+}
+
+// Steps of a segment: of 32 keys each.
+__device__ __forceinline__ int steps_of(const AtGeo& g, const AtSeg& s) {
+  return max(0, (min(s.t1 * kAtTile, at_limit_max(g, s.len, s.r0)) - s.t0 * kAtTile + kStep - 1) / kStep);
+}
+
 template <int D, int NB>
 __global__ void __launch_bounds__(Cfg4<D, NB>::kThreads, 1) attend4_kernel(Kernel4Args a) {
   using C = Cfg4<D, NB>;
   constexpr int kWarps = C::kWarps;
-  constexpr int kG = D / 32, kW = D / 8;  // groups, words of a row
+  constexpr int kG = D / 32;   // groups of a row
   constexpr int kMt = D / 16;             // tiles of 16 elements of o
   extern __shared__ __align__(128) unsigned char smem4[];
   float* join = reinterpret_cast<float*>(smem4);  // [warp][8 NB rows][kRow]
-  __shared__ __align__(8) uint64_t full_bar[kWarps][C::kDepth];
+  unsigned char* ring = smem4 + C::kJoin;
+  __shared__ __align__(16) Queries4<D, NB> queries_sh[2];
+  __shared__ __align__(8) uint64_t full_bar[C::kSlots], empty_bar[C::kSlots];
+  __shared__ __align__(8) uint64_t qfull_bar[2], qempty_bar[2], jfull_bar, jempty_bar;
   __shared__ float ref_sh[kWarps][8 * NB], sum_sh[kWarps][8 * NB];
-  __shared__ int scan_sh[kWarps];
+  __shared__ int scan_sh[C::kThreads / 32];
   __shared__ AtShare share_sh;
+  __shared__ int abort_sh;
 
   const AtGeo& g = a.geo;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, lg = lane >> 2, lt = lane & 3;
-  if (lane == 0) {
-    for (int i = 0; i < C::kDepth; ++i) mbar_init(&full_bar[warp][i], 1);
-    fence_mbar_init();
+  volatile int* abort_flag = &abort_sh;
+  if (tid < C::kSlots) {
+    mbar_init(&full_bar[tid], 3);
+    mbar_init(&empty_bar[tid], C::kPart);
   }
+  if (tid == 0) {
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&qfull_bar[i], 1);
+      mbar_init(&qempty_bar[i], kWarps);
+    }
+    mbar_init(&jfull_bar, kWarps);
+    mbar_init(&jempty_bar, 1);
+    abort_sh = 0;
+  }
+  fence_mbar_init();
   grid_dependency_wait();
   grid_dependents_go();
   if (blockIdx.x == 0) at_check_lengths<C::kThreads>(g, a.err);
   at_split_tiles<C::kThreads>(g, scan_sh, &share_sh);
   if (tid == 0 && share_sh.left == 0) a.parts.cut[blockIdx.x] = make_int2(-1, -1);
   AtWalk walk(g, share_sh);
-
-  // Every warp has a ring of its own, filled by its first lane: what the warp has read it may overwrite.
-  unsigned char* ring = smem4 + C::kJoin + warp * (C::kDepth * C::kSlot);
-  // with one row block to an instance every key is read once
-  const uint64_t pol = g.nrb == 1 ? l2_policy_evict_first() : l2_policy_evict_last();
-  Ahead4<kWarps> ahead(g, share_sh);
-  int slot = 0, phase = 0;  // of the step to come
-  int under_way = 0;        // steps loaded and not yet taken
-  bool ok = true;           // false once a wait expired: nothing is loaded any more
-  auto load_next = [&](int to) {
-    if (!ahead.find(g, warp)) return;
-    if (lane == 0) {
-      const uint32_t n = min(kStep, ahead.len - ahead.j);
-      const size_t row = ahead.row + ahead.j;
-      unsigned char* dst = ring + to * C::kSlot;
-      uint64_t* bar = &full_bar[warp][to];
-      mbar_arrive_expect_tx(bar, n * (D + D / 4));
-      bulk_load(dst, a.K4 + row * kW, n * (D / 2), bar, pol);
-      bulk_load(dst + 2 * C::kCodes, a.S4 + row * (2 * kG), n * (D / 4), bar, pol);
-      bulk_load(dst + C::kCodes, a.V4 + row * kW, n * (D / 2), bar, pol);
-    }
-    ahead.j += kWarps * kStep;
-    ++under_way;
+  AtSeg s;
+  auto wait = [&](uint64_t* bar, uint32_t parity) {  // after an abort every wait returns at once
+    at_wait(bar, parity, abort_flag, a.err, kDevTimeoutEpilogue);
+    __syncwarp();
   };
+
+  if (warp < C::kFirst) set_max_regs_dec<C::kRegsFew>();
+  if (warp < C::kFirst && warp != 1) {
+    // ---------------------------------------------------------------- loads: K, V and the scales by a warp each
+    // (one warp for all three took 660 clocks for three copies, and a step of 128 caches 49.8 us)
+    if (lane == 0) {
+      // with one row block to an instance every key is read once
+      const uint64_t pol = g.nrb == 1 ? l2_policy_evict_first() : l2_policy_evict_last();
+      const unsigned char* src =
+          reinterpret_cast<const unsigned char*>(warp == 0 ? a.K4 : warp == 2 ? a.V4 : a.S4);
+      const uint32_t row_bytes = warp == 3 ? D / 4 : D / 2;
+      unsigned char* dst = ring + (warp == 0 ? 0 : warp == 2 ? C::kCodes : 2 * C::kCodes);
+      int slot = 0, turn = 0;  // slots are taken in order; turns of the ring so far
+      bool ok = true;
+      while (ok && walk.next(g, s)) {
+        const int steps = steps_of(g, s);
+        const int left = s.len - s.t0 * kAtTile;
+        const unsigned char* at = src + (static_cast<size_t>(s.e) * g.cap + s.t0 * kAtTile) * row_bytes;
 #pragma unroll 1
-  for (int i = 0; i < C::kDepth; ++i) load_next(i);
+        for (int i = 0; i < steps; i += C::kPart) {
+          if (turn > 0 && !at_wait(&empty_bar[slot], (turn - 1) & 1, abort_flag, a.err, kDevTimeoutProducer)) {
+            ok = false;
+            break;
+          }
+          const uint32_t bytes = min(kAtTile, left - i * kStep) * row_bytes;
+          mbar_arrive_expect_tx(&full_bar[slot], bytes);
+          bulk_load(dst + slot * C::kSlot, at, bytes, &full_bar[slot], pol);
+          if (warp == 0)  // parts of the tile that no warp takes
+            for (int x = steps - i; x < C::kPart; ++x) mbar_arrive(&empty_bar[slot]);
+          at += kAtTile * row_bytes;
+          if (++slot == C::kSlots) {
+            slot = 0;
+            ++turn;
+          }
+        }
+      }
+      if (!ok || *abort_flag) {
+        // Let every copy already issued land before the CTA exits.  Where another loading warp gave up earlier a
+        // barrier does not complete, and the wait ends by its limit.
+        for (int i = 0; i < C::kSlots; ++i) {
+          const int fills = turn + (i < slot);
+          if (fills > 0) at_wait_always(&full_bar[i], (fills - 1) & 1, a.err, kDevTimeoutDrain, 1);
+        }
+      }
+    }
+    __syncwarp();
+    return;
+  }
+  if (warp == 1) {
+    // ---------------------------------------------------------------- queries, and the join of the warps' sums
+    AtSeg done;
+    bool have = false;
+    for (int seg = 0;; ++seg) {  // the queries of segment seg, then the sums of the one before
+      const bool more = walk.next(g, s);
+      if (more) {
+        if (seg >= 2) wait(&qempty_bar[seg & 1], ((seg >> 1) - 1) & 1);
+        prepare_queries<D, NB>(queries_sh[seg & 1], a, static_cast<size_t>(s.e) * g.R + s.r0, min(g.rr, g.R - s.r0), s,
+                               lane);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&qfull_bar[seg & 1]);
+      }
+      if (have) {
+        if (lane == 0) at_note(a.parts, done, !more, share_sh.per);
+        wait(&jfull_bar, (seg - 1) & 1);
+        const int cols = min(g.rr, g.R - done.r0);
+        const size_t row0 = static_cast<size_t>(done.e) * g.R + done.r0;
+        int whole = done.t0 == 0 && done.t1 == done.T;
+        const size_t part = (static_cast<size_t>(blockIdx.x) + done.item) * a.parts.rows;
+#pragma unroll 1
+        for (int c = 0; c < cols; ++c) {
+          constexpr int kPer = D / 32;
+          const float ref = lane < kWarps ? ref_sh[lane][c] : kRefFloor, l = lane < kWarps ? sum_sh[lane][c] : 0.f;
+          float m = ref;
+#pragma unroll
+          for (int x = 16; x; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
+          const float f = ex2_approx(ref - m);
+          float sum = l * f;
+#pragma unroll
+          for (int x = 16; x; x >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, x);
+          float v[kPer] = {};
+#pragma unroll
+          for (int w = 0; w < kWarps; ++w) {
+            const float fw = __shfl_sync(0xffffffffu, f, w);
+            uint32_t r[kPer];
+            load_words(r, join + (w * 8 * NB + c) * C::kRow + lane * kPer);
+#pragma unroll
+            for (int y = 0; y < kPer; ++y) v[y] = fmaf(__uint_as_float(r[y]), fw, v[y]);
+          }
+          const float inv = sum != 0.f ? 1.f / sum : 0.f;
+          asm volatile("" : "+r"(whole));  // not two copies of the loop
+          if (whole) {
+            uint32_t* dst = reinterpret_cast<uint32_t*>(a.o + (row0 + c) * D) + lane * (kPer / 2);
+#pragma unroll
+            for (int y = 0; y < kPer; y += 2) dst[y / 2] = pack_bf16(v[y] * inv, v[y + 1] * inv);
+          } else {
+            float* dst = a.parts.o + (part + c) * D + lane * kPer;
+#pragma unroll
+            for (int y = 0; y < kPer; ++y) dst[y] = v[y];
+          }
+          if (lane == 0) {
+            if (whole) {
+              const float y2 = sum != 0.f ? m + log2f(sum) : -INFINITY;
+              a.lse2[row0 + c] = y2;
+              if (a.lse) a.lse[row0 + c] = y2 * 0.69314718055994531f;
+            } else {
+              a.parts.ml[part + c] = make_float2(m, sum);
+            }
+          }
+        }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&jempty_bar);
+      }
+      if (!more) break;
+      done = s;
+      have = true;
+    }
+    return;
+  }
 
-  AtSeg s, next;
-  bool more = walk.next(g, next);
-  while (more) {
-    s = next;
-    more = walk.next(g, next);
-    if (tid == 0) at_note(a.parts, s, !more, share_sh.per);
+  // ------------------------------------------------------------------ products
+  set_max_regs_inc<C::kRegsMany>();
+  const int mine = warp - C::kFirst;
+  int first = mine;  // step of the coming segment that is the warp's first
+  int tiles = 0;     // of the segments before
+  for (int seg = 0; walk.next(g, s); ++seg) {
     const int cols = min(g.rr, g.R - s.r0);       // rows of this block
-    const int limit_max = at_limit_max(g, s.len, s.r0), limit_min = at_limit_min(g, s.len, s.r0);
-    const size_t row0 = static_cast<size_t>(s.e) * g.R + s.r0;  // of q, o and lse
-
-    // ---- the block's queries: right operands, and their sums over groups as three fp16 terms
+    const int limit_min = at_limit_min(g, s.len, s.r0), n_steps = steps_of(g, s), len = s.len;
+    float* logits = a.logits;
+    if (logits) logits += (static_cast<size_t>(s.e) * g.R + s.r0) * g.cap;
     uint32_t qb[NB][kG][4], qs[NB][2];
-    float unit[NB][2];  // columns 2 t, 2 t + 1: what a logit counts in
+    float unit[NB][2];
     int lim[NB][2];
+    wait(&qfull_bar[seg & 1], (seg >> 1) & 1);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      const int c = b * 8 + lg;
-      float x[kG][8], top = 0.f;
+      const Queries4<D, NB>& in = queries_sh[seg & 1];
 #pragma unroll
-      for (int i = 0; i < kG; ++i) {
-        uint4 r = make_uint4(0, 0, 0, 0);
-        if (c < cols) r = __ldg(reinterpret_cast<const uint4*>(a.q + (row0 + c) * D + 32 * i + 8 * lt));
-        const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-        for (int y = 0; y < 4; ++y) {
-          x[i][2 * y] = __uint_as_float(w[y] << 16);
-          x[i][2 * y + 1] = __uint_as_float(w[y] & 0xFFFF0000u);
-          top = fmaxf(top, fmaxf(fabsf(x[i][2 * y]), fabsf(x[i][2 * y + 1])));
-        }
-      }
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-      const int ex = top == 0.f ? 0 : max(exponent(top), -115);
-      const float up = pow2i(11 - ex);
-      float term[kG][3];
-#pragma unroll
-      for (int i = 0; i < kG; ++i) {
-        float sum = 0.f;
-#pragma unroll
-        for (int y = 0; y < 8; ++y) sum += x[i][y] *= up;
-        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-        sum *= 1.f / kSumUnit;
-#pragma unroll
-        for (int z = 0; z < 3; ++z) {
-          term[i][z] = __half2float(__float2half_rn(sum));
-          sum -= term[i][z];
-        }
-        // codes 2 y and 2 y + 1 of a byte: the second stands 16 times as high
-        qb[b][i][0] = pack_f16(x[i][0], x[i][4]);
-        qb[b][i][1] = pack_f16(x[i][1] * 0.0625f, x[i][5] * 0.0625f);
-        qb[b][i][2] = pack_f16(x[i][2], x[i][6]);
-        qb[b][i][3] = pack_f16(x[i][3] * 0.0625f, x[i][7] * 0.0625f);
-      }
-      // Products with the keys' lows: k = 2 t, 2 t + 1 are a pair of groups and a term, k = 2 t + 8, 2 t + 9 too.
-      if constexpr (D == 128) {
-        const bool odd = lt & 1;
-        const float h0 = odd ? term[2][0] : term[0][0], h1 = odd ? term[3][0] : term[1][0];
-        const float m0 = odd ? term[2][1] : term[0][1], m1 = odd ? term[3][1] : term[1][1];
-        const float l0 = odd ? term[2][2] : term[0][2], l1 = odd ? term[3][2] : term[1][2];
-        qs[b][0] = lt < 2 ? pack_f16(h0, h1) : pack_f16(m0, m1);
-        qs[b][1] = lt < 2 ? pack_f16(l0, l1) : 0u;
-      } else {
-        qs[b][0] = lt == 0   ? pack_f16(term[0][0], term[1][0])
-                   : lt == 1 ? pack_f16(term[0][1], term[1][1])
-                   : lt == 2 ? pack_f16(term[0][2], term[1][2])
-                             : 0u;
-        qs[b][1] = 0u;
-      }
-      // columns 2 t and 2 t + 1 are the rows of lanes 8 t and 8 t + 4
-#pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        unit[b][y] = pow2i(__shfl_sync(0xffffffffu, ex, 8 * lt + 4 * y) + 13);
-        const int cc = b * 8 + 2 * lt + y;
-        lim[b][y] = cc < cols ? at_limit(g, s.len, s.r0, cc) : 0;
-      }
+      for (int i = 0; i < kG; ++i) load_words(qb[b][i], &in.qb[b][i][lane]);
+      load_words(qs[b], &in.qs[b][lane]);
+      const float2 u = in.unit[b][lane];
+      const int2 m = in.lim[b][lane];
+      unit[b][0] = u.x;
+      unit[b][1] = u.y;
+      lim[b][0] = m.x;
+      lim[b][1] = m.y;
     }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&qempty_bar[seg & 1]);
 
     // p = 2^(y - ref): ref is the reference of the column less E
     float o[NB][kMt][4] = {}, low[NB][4] = {}, l[NB][2] = {}, ref[NB][2];
-    int up = -1000;  // E; none yet
+    int up = -1000;                         // E; none yet
+    float most = 0.f, most_y = -INFINITY;   // what it allows of a step, and of y - ref
 #pragma unroll
     for (int b = 0; b < NB; ++b) ref[b][0] = ref[b][1] = 0.f;
 
-    const int j_end = min(s.t1 * kAtTile, limit_max);
+    int step_no = first;
+    int slot = (tiles + first / C::kPart) % C::kSlots, phase = (tiles + first / C::kPart) / C::kSlots & 1;
 #pragma unroll 1
-    for (int j0 = s.t0 * kAtTile + warp * kStep; j0 < j_end; j0 += kWarps * kStep) {
-      ok = ok && __all_sync(0xffffffffu, at_wait(&full_bar[warp][slot], phase, nullptr, a.err, kDevTimeoutProducer));
-      if (!ok) break;  // an expired wait: the outputs are invalid, the barriers below are still met
-      const unsigned char* at = ring + slot * C::kSlot;
-      const unsigned char* scales = at + 2 * C::kCodes;
-      const bool tail = j0 + kStep > s.len;  // rows past the length hold anything
-      // ---- logits, in the columns' units
-      float y[2][NB][4];
+    for (; step_no < n_steps; step_no += kWarps) {
+      const int j0 = s.t0 * kAtTile + step_no * kStep;
+      wait(&full_bar[slot], phase);
+      const int row = step_no % C::kPart * kStep;  // of the tile
+      const unsigned char* at = ring + slot * C::kSlot + row * (D / 2);
+      unsigned char* scales = ring + slot * C::kSlot + 2 * C::kCodes + row * (D / 4);
+      const int left = len - j0;
+      if (left < kStep) {  // rows past the length hold anything: their steps and lows become 0
+        if (lane >= left) {
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        uint32_t k[2][kG], ks[2][kG];
-        uint32_t lows[2];  // of a pair of groups of keys g and g + 8
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int r = u * kSlice + lg + 8 * h;
-          load_words(k[h], at + r * (D / 2) + lt * (kG * 4));
-          load_words(ks[h], scales + r * (D / 4));
-          uint32_t pair[2];
-          load_words(pair, scales + r * (D / 4) + (D == 128 ? (lt & 1) * 8 : 0));
-          lows[h] = __byte_perm(pair[0], pair[1], 0x7632);
+          for (int i = 0; i < D / 4; i += 16) *reinterpret_cast<uint4*>(scales + lane * (D / 4) + i) = uint4{};
         }
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          float c[4];
-          mma_f16_first(c, lows[0], lows[1], lows[0], lows[1], qs[b][0], qs[b][1]);
-#pragma unroll
-          for (int z = 0; z < 4; ++z) y[u][b][z] = c[z] * (kSumUnit / kCodeUnit);
-        }
-#pragma unroll
-        for (int i = 0; i < kG; ++i) {
-          uint32_t f[2][4];  // codes (0, 4), (1, 5), (2, 6), (3, 7) of the word
+        fence_async_smem();  // the slot is loaded again
+        __syncwarp();
+      }
+#pragma unroll 1
+      for (int r0 = 0; r0 < kStep; r0 += kSlice) {  // rolled: what a short call waits for is instructions
+        // ---- logits, in the columns' units
+        float y[NB][4];
+        {
+          uint32_t k[2][kG], ks[2][kG], lows[2];  // lows of a pair of groups of keys g and g + 8
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            const uint32_t w = k[h][i], w8 = w >> 8;
-            f[h][0] = w & 0x000F000Fu;
-            f[h][1] = w & 0x00F000F0u;
-            f[h][2] = w8 & 0x000F000Fu;
-            f[h][3] = w8 & 0x00F000F0u;
+            const int r = r0 + lg + 8 * h;
+            load_words(k[h], at + r * (D / 2) + lt * (kG * 4));
+            load_words(ks[h], scales + r * (D / 4));
+            uint32_t pair[2];
+            load_words(pair, scales + r * (D / 4) + (D == 128 ? (lt & 1) * 8 : 0));
+            lows[h] = __byte_perm(pair[0], pair[1], 0x7632);
           }
-          const float s0 = half_lo(ks[0][i]), s1 = half_lo(ks[1][i]);
 #pragma unroll
           for (int b = 0; b < NB; ++b) {
             float c[4];
-            mma_f16_first(c, f[0][0], f[1][0], f[0][1], f[1][1], qb[b][i][0], qb[b][i][1]);
-            mma_f16(c, f[0][2], f[1][2], f[0][3], f[1][3], qb[b][i][2], qb[b][i][3]);
-            y[u][b][0] = fmaf(s0, c[0], y[u][b][0]);
-            y[u][b][1] = fmaf(s0, c[1], y[u][b][1]);
-            y[u][b][2] = fmaf(s1, c[2], y[u][b][2]);
-            y[u][b][3] = fmaf(s1, c[3], y[u][b][3]);
+            mma_f16_first(c, lows[0], lows[1], lows[0], lows[1], qs[b][0], qs[b][1]);
+#pragma unroll
+            for (int z = 0; z < 4; ++z) y[b][z] = c[z] * (kSumUnit / kCodeUnit);
+          }
+#pragma unroll
+          for (int i = 0; i < kG; ++i) {
+            uint32_t f[2][4];  // codes (0, 4), (1, 5), (2, 6), (3, 7) of the word
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t w = k[h][i], w8 = w >> 8;
+              f[h][0] = w & 0x000F000Fu;
+              f[h][1] = w & 0x00F000F0u;
+              f[h][2] = w8 & 0x000F000Fu;
+              f[h][3] = w8 & 0x00F000F0u;
+            }
+            const float s0 = half_lo(ks[0][i]), s1 = half_lo(ks[1][i]);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+              float c[4];
+              mma_f16_first(c, f[0][0], f[1][0], f[0][1], f[1][1], qb[b][i][0], qb[b][i][1]);
+              mma_f16(c, f[0][2], f[1][2], f[0][3], f[1][3], qb[b][i][2], qb[b][i][3]);
+              y[b][0] = fmaf(s0, c[0], y[b][0]);
+              y[b][1] = fmaf(s0, c[1], y[b][1]);
+              y[b][2] = fmaf(s1, c[2], y[b][2]);
+              y[b][3] = fmaf(s1, c[3], y[b][3]);
+            }
           }
         }
-      }
-      if (a.logits) {
+        asm volatile("" : "+l"(logits));  // not two copies of the loop
+        if (logits) {
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int z = 0; z < 4; ++z) {
+              const int c = b * 8 + 2 * lt + (z & 1), r = r0 + lg + 8 * (z >> 1);
+              if (c < cols && r < left) logits[static_cast<size_t>(c) * g.cap + j0 + r] = y[b][z] * unit[b][z & 1];
+            }
+        }
+        uint32_t vs[2][kG];  // (step, low) of V of keys g and g + 8
+#pragma unroll
+        for (int h = 0; h < 2; ++h) load_words(vs[h], scales + (r0 + lg + 8 * h) * (D / 4) + kG * 4);
+        uint32_t lv[2], top2 = 0;  // lows of group g of keys 2 t, 2 t + 1 and 2 t + 8, 2 t + 9; the largest step
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t w[2];
+#pragma unroll
+          for (int z = 0; z < 2; ++z) {
+            w[z] = *reinterpret_cast<const uint32_t*>(scales + (r0 + 8 * h + 2 * lt + z) * (D / 4) + kG * 4 +
+                                                      (lg & (kG - 1)) * 4);
+            top2 = max_f16x2(top2, w[z]);
+          }
+          lv[h] = __byte_perm(w[0], w[1], 0x7632);
+        }
+        // ---- to base 2, against the references
+        const float step = half_lo(top2);
+        float above = -INFINITY;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int z = 0; z < 2; ++z) {
-            const int c = b * 8 + 2 * lt + z;
-            if (c < cols) {
-              float* dst = a.logits + (row0 + c) * g.cap + j0 + lg;
-#pragma unroll
-              for (int r = 0; r < 4; ++r)
-                if (!tail || j0 + lg + 8 * r < s.len) dst[8 * r] = y[r >> 1][b][z + 2 * (r & 1)] * unit[b][z];
-            }
-          }
-      }
-      // the largest step of V
-      auto v_scales = [&](int u, int h, uint32_t(&w)[kG]) {  // (step, low) of keys g and g + 8 of a product
-        const int r = u * kSlice + lg + 8 * h;
-        load_words(w, scales + r * (D / 4) + kG * 4);
-        if (tail && j0 + r >= s.len) {
-#pragma unroll
-          for (int i = 0; i < kG; ++i) w[i] = 0;
-        }
-      };
-      uint32_t top2 = 0;
-#pragma unroll
-      for (int x = 0; x < 4; ++x) {
-        uint32_t w[kG];
-        v_scales(x >> 1, x & 1, w);
-#pragma unroll
-        for (int i = 0; i < kG; ++i) top2 = max_f16x2(top2, w[i]);
-      }
-      // ---- to base 2, against the references
-      const float step = half_lo(top2), most = 16.f * pow2i(up);  // p 2^-E may be 2^4
-      float above = -INFINITY;
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int z = 0; z < 4; ++z) {
-          const float f = unit[b][z & 1] * a.sc;
-          y[0][b][z] = fmaf(y[0][b][z], f, -ref[b][z & 1]);
-          y[1][b][z] = fmaf(y[1][b][z], f, -ref[b][z & 1]);
-        }
-      if (j0 + kStep > limit_min) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
+          for (int z = 0; z < 4; ++z) y[b][z] = fmaf(y[b][z], unit[b][z & 1] * a.sc, -ref[b][z & 1]);
+        if (j0 + r0 + kSlice > limit_min) {
 #pragma unroll
           for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int z = 0; z < 4; ++z)
-              if (j0 + u * kSlice + lg + 8 * (z >> 1) >= lim[b][z & 1]) y[u][b][z] = -INFINITY;
-      }
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int z = 0; z < 4; ++z) above = fmaxf(above, fmaxf(y[0][b][z], y[1][b][z]));
-      if (__any_sync(0xffffffffu, above > kAbove4 + up || step * most > 16.f * kStepTop || up < -999)) {
-        // Move the references to the step's maxima, and the steps' scale.  A column that sees nothing of a warp's
-        // first step sees nothing after it either: it stays at the floor.
-        float top = step;
-#pragma unroll
-        for (int m = 1; m < 32; m <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
-        const int now = up < -999 || top * most > 16.f * kStepTop ? min(kMostUp, 7 - exponent(top)) : up;
-        const bool begins = up < -999;
-        const float back = begins ? kRefFloor : static_cast<float>(up);
-        up = now;
+              if (j0 + r0 + lg + 8 * (z >> 1) >= lim[b][z & 1]) y[b][z] = -INFINITY;
+        }
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int z = 0; z < 2; ++z) {
-            float v = fmaxf(fmaxf(y[0][b][z], y[0][b][z + 2]), fmaxf(y[1][b][z], y[1][b][z + 2]));
+          for (int z = 0; z < 4; ++z) above = fmaxf(above, y[b][z]);
+        if (__any_sync(0xffffffffu, above > most_y || step > most)) {
+          // Move the references to the slice's maxima, and the steps' scale.  A column that sees nothing of a warp's
+          // first slice sees nothing after it either: it stays at the floor.
+          float top = step;
 #pragma unroll
-            for (int m = 4; m < 32; m <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, m));
-            // relative to ref: the reference was at `back`; it moves up to v, and 2^E moves to `now`
-            const float by = fmaxf(v, back) - static_cast<float>(now);
-            const float fac = begins ? 0.f : ex2_approx(-by);
-            ref[b][z] += by;
-            l[b][z] *= fac;
-            low[b][z] *= fac;
+          for (int m = 1; m < 32; m <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
+          const bool begins = up < -999;
+          const int now = begins || top > most ? min(kMostUp, 9 - exponent(top)) : up;
+          const float back = begins ? kRefFloor : static_cast<float>(up);
+          up = now;
+          most = kStepTop * pow2i(-now);
+          most_y = kAbove4 + static_cast<float>(now);
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              y[u][b][z] -= by;
-              y[u][b][z + 2] -= by;
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int z = 0; z < 2; ++z) {
+              float v = fmaxf(y[b][z], y[b][z + 2]);
+#pragma unroll
+              for (int m = 4; m < 32; m <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, m));
+              // relative to ref: the reference was at `back`; it moves up to v, and 2^E moves to `now`
+              const float by = fmaxf(v, back) - static_cast<float>(now);
+              const float fac = begins ? 0.f : ex2_approx(-by);
+              ref[b][z] += by;
+              l[b][z] *= fac;
+              low[b][z] *= fac;
+              y[b][z] -= by;
+              y[b][z + 2] -= by;
+#pragma unroll
+              for (int m = 0; m < kMt; ++m) {
+                o[b][m][z] *= fac;
+                o[b][m][z + 2] *= fac;
+              }
             }
-#pragma unroll
-            for (int m = 0; m < kMt; ++m) {
-              o[b][m][z] *= fac;
-              o[b][m][z + 2] *= fac;
-            }
-          }
-      }
-      // ---- weights and values
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        uint32_t vs[2][kG], lv[2];  // lv: lows of group g of keys 2 t, 2 t + 1 and 2 t + 8, 2 t + 9
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          v_scales(u, h, vs[h]);
-          uint32_t w[2];
-#pragma unroll
-          for (int z = 0; z < 2; ++z) {
-            const int r = u * kSlice + 8 * h + 2 * lt + z;
-            w[z] = *reinterpret_cast<const uint32_t*>(scales + r * (D / 4) + kG * 4 + (lg & (kG - 1)) * 4);
-            if (tail && j0 + r >= s.len) w[z] = 0;
-          }
-          lv[h] = __byte_perm(w[0], w[1], 0x7632);
         }
+        // ---- weights
         uint32_t pb[NB][kG][2];
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
           float p[4];
 #pragma unroll
-          for (int z = 0; z < 4; ++z) p[z] = ex2_approx(y[u][b][z]);
+          for (int z = 0; z < 4; ++z) p[z] = ex2_approx(y[b][z]);
           l[b][0] += p[0] + p[2];
           l[b][1] += p[1] + p[3];
+          const uint32_t p0 = pack_f16(p[0], p[1]), p1 = pack_f16(p[2], p[3]);
 #pragma unroll
           for (int i = 0; i < kG; ++i) {
-            const float s0 = half_lo(vs[0][i]), s1 = half_lo(vs[1][i]);
-            pb[b][i][0] = transpose8(pack_f16(p[0] * s0, p[1] * s0));
-            pb[b][i][1] = transpose8(pack_f16(p[2] * s1, p[3] * s1));
+            pb[b][i][0] = transpose8(mul_lo(p0, vs[0][i]));
+            pb[b][i][1] = transpose8(mul_lo(p1, vs[1][i]));
           }
-          mma_f16(low[b], lv[0], 0u, lv[1], 0u, transpose8(pack_f16(p[0], p[1])),
-                  transpose8(pack_f16(p[2], p[3])));
+          mma_f16(low[b], lv[0], 0u, lv[1], 0u, transpose8(p0), transpose8(p1));
         }
+        // ---- values
         uint32_t v[4][D / 64];  // words g D / 64 .. of keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9
 #pragma unroll
         for (int h = 0; h < 4; ++h)
-          load_words(v[h], at + C::kCodes + (u * kSlice + 2 * lt + (h & 1) + 8 * (h >> 1)) * (D / 2) + lg * (D / 16));
+          load_words(v[h], at + C::kCodes + (r0 + 2 * lt + (h & 1) + 8 * (h >> 1)) * (D / 2) + lg * (D / 16));
 #pragma unroll
         for (int m = 0; m < 4; ++m) {  // byte m of the words: codes 2 m and 2 m + 1
           uint32_t f[D / 64][2];       // [word][keys 2 t.., 2 t + 8..]: that byte of both keys
@@ -483,15 +612,18 @@ __global__ void __launch_bounds__(Cfg4<D, NB>::kThreads, 1) attend4_kernel(Kerne
         }
       }
       __syncwarp();
-      --under_way;
-      load_next(slot);
-      if (++slot == C::kDepth) {
-        slot = 0;
+      if (lane == 0) mbar_arrive(&empty_bar[slot]);
+      slot += kWarps / C::kPart;
+      if (slot >= C::kSlots) {
+        slot -= C::kSlots;
         phase ^= 1;
       }
     }
+    first = step_no - n_steps;
+    tiles += (n_steps + C::kPart - 1) / C::kPart;
 
-    // ---- join the warps
+    // ---- the warp's sums, for the join
+    if (seg >= 1) wait(&jempty_bar, (seg - 1) & 1);
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
 #pragma unroll
@@ -503,10 +635,10 @@ __global__ void __launch_bounds__(Cfg4<D, NB>::kThreads, 1) attend4_kernel(Kerne
         for (int i = 0; i < kG; ++i) lo[i] = __shfl_sync(0xffffffffu, low[b][z], 4 * i + lt);
         const int c = b * 8 + 2 * lt + z;
         if (lg == 0) {
-          ref_sh[warp][c] = ref[b][z];
-          sum_sh[warp][c] = l[b][z];
+          ref_sh[mine][c] = ref[b][z];
+          sum_sh[mine][c] = l[b][z];
         }
-        float* dst = join + (warp * 8 * NB + c) * C::kRow;
+        float* dst = join + (mine * 8 * NB + c) * C::kRow;
 #pragma unroll
         for (int m = 0; m < kMt; ++m) {
           constexpr float f0 = kCodeUnit, f1 = kCodeUnit / 16.f;
@@ -521,46 +653,8 @@ __global__ void __launch_bounds__(Cfg4<D, NB>::kThreads, 1) attend4_kernel(Kerne
         }
       }
     }
-    __syncthreads();
-    const bool whole = s.t0 == 0 && s.t1 == s.T;
-    const size_t part = (static_cast<size_t>(blockIdx.x) + s.item) * a.parts.rows;
-    for (int c = warp; c < cols; c += kWarps) {
-      float m = kRefFloor, sum = 0.f, f[kWarps];
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) m = fmaxf(m, ref_sh[w][c]);
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        f[w] = ex2_approx(ref_sh[w][c] - m);
-        sum = fmaf(sum_sh[w][c], f[w], sum);
-      }
-      const float inv = sum != 0.f ? 1.f / sum : 0.f;
-      for (int d = lane; d < D; d += 32) {
-        float v = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWarps; ++w) v = fmaf(join[(w * 8 * NB + c) * C::kRow + d], f[w], v);
-        if (whole) a.o[(row0 + c) * D + d] = __float2bfloat16(v * inv);
-        else a.parts.o[(part + c) * D + d] = v;
-      }
-      if (lane == 0) {
-        if (whole) {
-          const float y2 = sum != 0.f ? m + log2f(sum) : -INFINITY;
-          a.lse2[row0 + c] = y2;
-          if (a.lse) a.lse[row0 + c] = y2 * 0.69314718055994531f;
-        } else {
-          a.parts.ml[part + c] = make_float2(m, sum);
-        }
-      }
-    }
-    __syncthreads();
-  }
-  if (!ok) {  // let every copy already issued land before the CTA exits
-    for (; under_way > 0; --under_way) {
-      at_wait_always(&full_bar[warp][slot], phase, a.err, kDevTimeoutDrain, 1);
-      if (++slot == C::kDepth) {
-        slot = 0;
-        phase ^= 1;
-      }
-    }
+    __syncwarp();
+    if (lane == 0) mbar_arrive(&jfull_bar);
   }
 }
 
