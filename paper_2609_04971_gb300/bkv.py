@@ -162,6 +162,16 @@ def _expect(t: torch.Tensor | None, n: int, name: str) -> None:
         raise ValueError(f"{name} has {t.numel()} elements; the configured shape needs {n}")
 
 
+def _arg(t: torch.Tensor | None, dtype: torch.dtype, n: int, name: str):
+    """_expect and _ptr in one, for the calls of a decode step: a step's host time is what its small calls take."""
+    if t is None:
+        return None
+    if t.dtype is dtype and t.is_cuda and t.is_contiguous() and t.numel() == n:
+        return t.data_ptr()
+    _expect(t, n, name)
+    return _ptr(t, dtype, name)
+
+
 def _check(rc: int, where: str, ctx=None) -> None:
     if rc != BKV_OK:
         detail = _l().bkv_last_error(ctx).decode() if ctx is not None else ""
@@ -556,18 +566,14 @@ class BeaconKV:
         bkv_attend_reserve(self.ctx, n_q, n_groups, weights)
 
     def _attend_args(self, q, K, V, length, weights, o_out, lse_out):
-        d, rows_kv = self._layer[2], self._layer[4]
-        self._expect(K, rows_kv * d, "K")
-        self._expect(V, rows_kv * d, "V")
-        return self._query_args(q, length, weights, o_out, lse_out)
-
-    def _query_args(self, q, length, weights, o_out, lse_out):
         batch, heads, d, lens, rows_kv = self._layer
         shape = q.shape
         if len(shape) != 4 or shape[0] != batch or shape[1] != heads or shape[3] != d:
             raise ValueError(f"q must be [batch = {batch}, n_q_heads = {heads}, n_q, head_dim = {d}], got "
                              f"{tuple(shape)}")
         expect = self._expect
+        expect(K, rows_kv * d, "K")
+        expect(V, rows_kv * d, "V")
         expect(length, lens, "length")
         expect(weights, rows_kv, "weights")
         if not q.is_cuda:
@@ -611,45 +617,73 @@ class BeaconKV:
                           weights)
         return o, lse
 
+    def _outputs(self, q, o_out, lse_out):
+        """n_q, the pointer of q, and the outputs of an attention call, new where they are not given."""
+        batch, heads, d = self._layer[:3]
+        shape = q.shape
+        if len(shape) != 4 or shape[0] != batch or shape[1] != heads or shape[3] != d:
+            raise ValueError(f"q must be [batch = {batch}, n_q_heads = {heads}, n_q, head_dim = {d}], got "
+                             f"{tuple(shape)}")
+        if q.dtype is not torch.bfloat16 or not q.is_cuda or not q.is_contiguous():
+            _ptr(q, torch.bfloat16, "q")
+        if o_out is None and lse_out is None:
+            o_out, lse_out = self._new(q, shape, torch.bfloat16, shape[:3], torch.float32)
+        elif o_out is None:
+            o_out, _ = self._new(q, shape, torch.bfloat16, 0, torch.float32)
+        elif lse_out is None:
+            lse_out, _ = self._new(q, shape[:3], torch.float32, 0, torch.float32)
+        n = batch * heads * shape[2]
+        return (shape[2], q.data_ptr(), o_out, lse_out, _arg(o_out, torch.bfloat16, n * d, "o_out"),
+                _arg(lse_out, torch.float32, n, "lse_out"))
+
     def attend_window(self, q, K, V, *, length, window, n_sink=0, scale=None, o_out=None, lse_out=None):
         """attend where a query sees the `window` newest rows up to its own and the first `n_sink` rows
         (bkv_attend_window); the reservation is that of attend.  Returns (o, lse)."""
-        n_q, o, lse = self._attend_args(q, K, V, length, None, o_out, lse_out)
-        bkv_attend_window(self.ctx, q, n_q, K, V, length, window, n_sink, scale or 0.0, o, lse)
+        _, _, d, lens, rows = self._layer
+        kp, vp = _arg(K, torch.bfloat16, rows * d, "K"), _arg(V, torch.bfloat16, rows * d, "V")
+        lp = _arg(length, torch.int32, lens, "length")
+        n_q, qp, o, lse, op, ep = self._outputs(q, o_out, lse_out)
+        rc = _lib.bkv_attend_window(self.ctx, qp, n_q, kp, vp, lp, window, n_sink, scale or 0.0, op, ep)
+        if rc:
+            _check(rc, "bkv_attend_window", self.ctx)
         return o, lse
 
     # ------------------------------------------------------------ caches in 4 bits
-    def _cache4_args(self, K4, V4, S4, rows, suffix=""):
-        d = self.cfg.head_dim
-        self._expect(K4, rows * (d // 2), "K4" + suffix)
-        self._expect(V4, rows * (d // 2), "V4" + suffix)
-        self._expect(S4, rows * (d // 8), "S4" + suffix)
+    def _cache4(self, K4, V4, S4, rows, suffix=""):
+        d, u8 = self.cfg.head_dim, torch.uint8
+        return (_arg(K4, u8, rows * (d // 2), "K4" + suffix), _arg(V4, u8, rows * (d // 2), "V4" + suffix),
+                _arg(S4, torch.float16, rows * (d // 8), "S4" + suffix))
 
-    def _rows4(self, K, V, K4, V4, S4, first, length):
-        c = self.cfg
-        if K.dim() != 4 or K.shape[0] != c.batch or K.shape[1] != c.n_kv_heads or K.shape[3] != c.head_dim:
-            raise ValueError(f"K must be [batch = {c.batch}, n_kv_heads = {c.n_kv_heads}, n_rows, head_dim = "
-                             f"{c.head_dim}], got {tuple(K.shape)}")
-        lens, rows_kv = self._layer[3], self._layer[4]
-        self._expect(V, K.numel(), "V")
-        self._cache4_args(K4, V4, S4, rows_kv)
-        self._expect(first, lens, "first")
-        self._expect(length, lens, "length")
-        return K.shape[2]
+    def _rows4(self, K, V, first, length):
+        """Pointers of K, V, first and length, and n_rows."""
+        c, shape = self.cfg, K.shape
+        batch, _, d, lens, _ = self._layer
+        if len(shape) != 4 or shape[0] != batch or shape[1] != c.n_kv_heads or shape[3] != d:
+            raise ValueError(f"K must be [batch = {batch}, n_kv_heads = {c.n_kv_heads}, n_rows, head_dim = {d}], got "
+                             f"{tuple(shape)}")
+        n, bf16, i32 = lens * shape[2] * d, torch.bfloat16, torch.int32
+        return (_arg(K, bf16, n, "K"), _arg(V, bf16, n, "V"), _arg(first, i32, lens, "first"),
+                _arg(length, i32, lens, "length"), shape[2])
 
     def pack4(self, K, V, K4, V4, S4, *, length, first=None):
         """Writes rows of one layer into its 4-bit caches (bkv_pack4): row i of K and V [batch, n_kv_heads, n_rows,
         head_dim] becomes row first + i of its cache, for first + i < length.  K4 and V4 are uint8 [batch,
         n_kv_heads, capacity, head_dim / 2], S4 fp16 [batch, n_kv_heads, capacity, 2, head_dim / 32, 2]; first
         (None: 0) and length int32 [batch, n_kv_heads]."""
-        n = self._rows4(K, V, K4, V4, S4, first, length)
-        bkv_pack4(self.ctx, K, V, n, first, length, K4, V4, S4)
+        kp, vp, fp, lp, n = self._rows4(K, V, first, length)
+        k4, v4, s4 = self._cache4(K4, V4, S4, self._layer[4])
+        rc = _lib.bkv_pack4(self.ctx, kp, vp, n, fp, lp, k4, v4, s4)
+        if rc:
+            _check(rc, "bkv_pack4", self.ctx)
 
     def unpack4(self, K4, V4, S4, K_out, V_out, *, length, first=None):
         """The inverse of pack4 (bkv_unpack4): row first + i of each cache, below its length, to row i of K_out and
         V_out; their other rows keep what they held."""
-        n = self._rows4(K_out, V_out, K4, V4, S4, first, length)
-        bkv_unpack4(self.ctx, K4, V4, S4, n, first, length, K_out, V_out)
+        kp, vp, fp, lp, n = self._rows4(K_out, V_out, first, length)
+        k4, v4, s4 = self._cache4(K4, V4, S4, self._layer[4])
+        rc = _lib.bkv_unpack4(self.ctx, k4, v4, s4, n, fp, lp, kp, vp)
+        if rc:
+            _check(rc, "bkv_unpack4", self.ctx)
 
     def reserve_attend4(self, *, n_q: int = 1, weights: bool = False):
         """Workspace for attend4 with n_q queries per head (bkv_attend4_reserve)."""
@@ -657,9 +691,13 @@ class BeaconKV:
 
     def attend4(self, q, K4, V4, S4, *, length, scale=None, weights=None, o_out=None, lse_out=None):
         """attend over one layer's 4-bit caches (bkv_attend4), which are those of pack4.  Returns (o, lse)."""
-        self._cache4_args(K4, V4, S4, self._layer[4])
-        n_q, o, lse = self._query_args(q, length, weights, o_out, lse_out)
-        bkv_attend4(self.ctx, q, n_q, K4, V4, S4, length, scale or 0.0, o, lse, weights)
+        _, _, _, lens, rows = self._layer
+        k4, v4, s4 = self._cache4(K4, V4, S4, rows)
+        lp, wp = _arg(length, torch.int32, lens, "length"), _arg(weights, torch.float32, rows, "weights")
+        n_q, qp, o, lse, op, ep = self._outputs(q, o_out, lse_out)
+        rc = _lib.bkv_attend4(self.ctx, qp, n_q, k4, v4, s4, lp, scale or 0.0, op, ep, wp)
+        if rc:
+            _check(rc, "bkv_attend4", self.ctx)
         return o, lse
 
     def evict4(self, K4, V4, S4, weights, *, L, budget, K4_out=None, V4_out=None, S4_out=None, weights_out=None,
@@ -671,10 +709,9 @@ class BeaconKV:
             K4_out, V4_out, S4_out, weights_out = K4, V4, S4, weights
         elif given != 4:
             raise ValueError("K4_out, V4_out, S4_out and weights_out come together or not at all")
-        rows = self.n_inst * self.cfg.capacity
         cap_out = weights_out.numel() // self.n_inst
-        self._cache4_args(K4, V4, S4, rows)
-        self._cache4_args(K4_out, V4_out, S4_out, self.n_inst * cap_out, "_out")
+        self._cache4(K4, V4, S4, self.n_inst * self.cfg.capacity)
+        self._cache4(K4_out, V4_out, S4_out, self.n_inst * cap_out, "_out")
         kept_out, len_out = self._evict_args(K4, weights, L, budget, weights_out, kept_out, len_out)
         bkv_evict4(self.ctx, K4, V4, S4, weights, L, budget, K4_out, V4_out, S4_out, weights_out, cap_out, kept_out,
                    len_out)
