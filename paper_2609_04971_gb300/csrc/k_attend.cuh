@@ -275,6 +275,16 @@ struct AtSeg {
   int ts, ns, w0;  // with a window
 };
 
+// With a window: whether no row of [r0, r0 + n) sees a key of tile t, whose first key is k0.
+__device__ __forceinline__ bool at_unseen(const AtGeo& g, const AtSeg& s, int r0, int n, int k0) {
+  const int r1 = min(min(s.r0 + g.rr, g.R), r0 + n) - 1;
+  if (r1 < r0) return true;
+  int h0, h1;
+  const int i0 = g.by_n_q.mod(r0, h0), i1 = g.by_n_q.mod(r1, h1);  // rows of several heads: all queries
+  const int most = s.len - g.n_q + 1 + (h1 > h0 ? g.n_q - 1 : i1), least = s.len - g.n_q + 1 + (h1 > h0 ? 0 : i0);
+  return k0 >= most || (k0 + kAtTile <= least - g.window && k0 >= g.n_sink);
+}
+
 // The first key of tile t of a segment's item.
 template <bool WIN>
 __device__ __forceinline__ int at_key0(const AtSeg& s, int t) {

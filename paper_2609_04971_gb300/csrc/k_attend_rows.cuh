@@ -213,16 +213,21 @@ __global__ void __launch_bounds__(kThreads, 1)
       auto await = [&](uint64_t* bar, uint32_t parity) {
         if (ok) ok = __all_sync(0xffffffffu, at_wait(bar, parity, abort_flag, a.err, kDevTimeoutMma));
       };
-      auto issue_s = [&](int w, int st, int st2, bool done, bool last_of_seg) {
+      // A row tile that sees nothing of a tile of keys has no products with it, and the few first keys of a window only
+      // those of 16 keys; their barriers take part as ever.
+      const uint32_t idesc_few = idesc_bf16_f32(kRows, kSinkRows);
+      auto issue_s = [&](int w, int st, int st2, bool done, bool last_of_seg, bool unseen, bool few) {
         if (!ok) return;
         tc_fence_after();
         const uint64_t q = sdesc_kmajor_sw128(q_addr + w * kAtBox), k = sdesc_kmajor_sw128(kv_addr + st * C::kTileBytes);
         const uint64_t k2 = sdesc_kmajor_sw128(kv_addr + st2 * C::kTileBytes);
         if (elect_one()) {
+          if (!WIN || !unseen) {
 #pragma unroll
-          for (int kk = 0; kk < D / 16; ++kk)
-            mma_bf16_ss(tm + w * kAtTile, q + (((kk >> 2) * C::kQBox + (kk & 3) * 32) >> 4),
-                        k + (((kk >> 2) * kAtBox + (kk & 3) * 32) >> 4), idesc_s, kk > 0);
+            for (int kk = 0; kk < D / 16; ++kk)
+              mma_bf16_ss(tm + w * kAtTile, q + (((kk >> 2) * C::kQBox + (kk & 3) * 32) >> 4),
+                          k + (((kk >> 2) * kAtBox + (kk & 3) * 32) >> 4), WIN && few ? idesc_few : idesc_s, kk > 0);
+          }
           if (SPLIT) {
 #pragma unroll
             for (int kk = 0; kk < D / 16; ++kk)
@@ -236,24 +241,36 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         __syncwarp();
       };
-      auto issue_o = [&](int w, int i, int st, int seg, bool first, bool last_of_seg, bool done) {
+      bool begun[2] = {};  // O of the row tile has a product of this segment
+      auto issue_o = [&](int w, int i, int st, int seg, bool first, bool last_of_seg, bool done, bool unseen, bool few) {
         await(&pfull_bar[w], i & 1);
         if (first && seg >= 1) await(&ofree_bar[w], (seg - 1) & 1);
         if (!ok) return;
         tc_fence_after();
         const uint64_t v = sdesc_mnmajor_sw128(kv_addr + st * C::kTileBytes, kAtBox);
         if (elect_one()) {
+          if constexpr (WIN) {
+            const int steps = unseen ? 0 : few ? kSinkRows / 16 : kAtTile / 16;
+            const bool more = !first && begun[w];
 #pragma unroll
-          for (int kk = 0; kk < kAtTile / 16; ++kk)
-            mma_bf16_ts(tm + C::kO + w * D, tm + w * kAtTile + kk * 8, v + kk * (2048 >> 4), idesc_o, !first || kk > 0);
+            for (int kk = 0; kk < kAtTile / 16; ++kk)
+              if (kk < steps)
+                mma_bf16_ts(tm + C::kO + w * D, tm + w * kAtTile + kk * 8, v + kk * (2048 >> 4), idesc_o, more || kk > 0);
+          } else {
+#pragma unroll
+            for (int kk = 0; kk < kAtTile / 16; ++kk)
+              mma_bf16_ts(tm + C::kO + w * D, tm + w * kAtTile + kk * 8, v + kk * (2048 >> 4), idesc_o, !first || kk > 0);
+          }
           if (last_of_seg) mma_commit(&ofull_bar[w]);
           if (done) mma_commit(&empty_bar[st]);
         }
+        if (WIN) begun[w] = (!first && begun[w]) || !unseen;
         __syncwarp();
       };
       AtSeg s;
       int t = 0, seg = -1;
       bool o_first = false, o_last = false;  // tile i - 1 begins, ends its segment
+      bool unseen[2] = {}, few = false;      // of the present tile
       s.t1 = 0;
       for (int i = 0; ok && i <= n_tiles; ++i) {  // for each row tile O(i - 1), then S(i)
         const bool turn = t == s.t1, more = i < n_tiles;
@@ -268,19 +285,26 @@ __global__ void __launch_bounds__(kThreads, 1)
           ++t;
         }
         const bool first = o_first, last = o_last, last_s = t == s.t1;
+        const bool o_unseen[2] = {unseen[0], unseen[1]}, o_few = few;
         o_first = turn;
         o_last = last_s;
+        if (WIN && more) {
+          const int k0 = at_key0<WIN>(s, t - 1);
+          unseen[0] = at_unseen(g, s, s.r0, kRows, k0);
+          unseen[1] = at_unseen(g, s, s.r0 + kRows, kRows, k0);
+          few = t - 1 < s.ts && s.ns - k0 <= kSinkRows;
+        }
 #pragma unroll
         for (int w = 0; w < 2; ++w) {
           if (i > 0) {
             if (w == 0) await(&full_bar[v_st], (v_pos / C::kStages) & 1);
-            issue_o(w, i - 1, v_st, seg_o, first, last, w == 1);
+            issue_o(w, i - 1, v_st, seg_o, first, last, w == 1, o_unseen[w], o_few);
           }
           if (more) {
             if (w == 0 && turn) await(&qfull_bar, seg & 1);
             if (w == 0) await(&full_bar[k_st], (k_pos / C::kStages) & 1);
             if (SPLIT && w == 0) await(&full_bar[k2_st], (k2_pos / C::kStages) & 1);
-            issue_s(w, k_st, k2_st, w == 1, last_s);
+            issue_s(w, k_st, k2_st, w == 1, last_s, unseen[w], few);
           }
         }
       }
@@ -327,106 +351,124 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int seen = (WIN ? min(lim, end) : lim) - k0, from = lim - g.window - k0, sinks = g.n_sink - k0;
         const bool masked = WIN ? k0 + kAtTile > min(lim_min, end) || (k0 <= lo_max && k0 + kAtTile > g.n_sink)
                                 : k0 + kAtTile > lim_min;
-        auto sees = [&](int x) { return x < seen && (!WIN || x >= from || x < sinks); };
+        // bits of the 32 keys of a quarter that lie below key n of the tile
+        auto below = [](int n, int q) {
+          n -= q * 32;
+          return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u;
+        };
+        auto sees = [&](int q) { return below(seen, q) & (~below(from, q) | below(sinks, q)); };
+        const bool few = WIN && t < s.ts && s.ns - k0 <= kSinkRows;
         wait(&sfull_bar[w], i & 1);
         tc_fence_after();
-        uint32_t p[kAtTile / 2];
-        float sum = 0.f;
-        // a quarter of the tile's logits, as exponents against the reference
-        auto shift = [&](float(&v)[32], int q) {
-          const float2 sc2 = make_float2(sc, sc), ref2 = make_float2(ref, ref);
+        if (WIN && t == s.t0) ref = -INFINITY;
+        const bool skip = WIN && at_unseen(g, s, s.r0 + w * kRows, kRows, k0);
+        if (!skip) {
+          uint32_t p[kAtTile / 2];
+          float sum = 0.f;
+          // a quarter of the tile's logits, as exponents against the reference
+          auto shift = [&](float(&v)[32], int q) {
+            const float2 sc2 = make_float2(sc, sc), ref2 = make_float2(ref, ref);
 #pragma unroll
-          for (int x = 0; x < 32; x += 2) {
-            const float2 y = fma2(make_float2(v[x], v[x + 1]), sc2, ref2);
-            v[x] = y.x;
-            v[x + 1] = y.y;
-          }
-          if (masked) {
-#pragma unroll
-            for (int x = 0; x < 32; ++x) v[x] = sees(q * 32 + x) ? v[x] : -INFINITY;
-          }
-        };
-        // the tile's weights against the present reference, and their sum
-        auto weigh = [&](bool first) {
-          float2 s0 = make_float2(0.f, 0.f), s1 = s0;
-          float y[2][32];
-          tmem_ld32(s_addr, y[0]);
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            float(&v)[32] = y[q & 1];
-            tmem_wait_ld();
-            if (q < 3) tmem_ld32(s_addr + (q + 1) * 32, y[(q + 1) & 1]);
-            // A lane that sees nothing of the segment, or stands for no row but holds one of the next group, has
-            // p = 0 whatever its logits are, so that they cannot ask for a move of the references.
-            if (!WIN && q == 0 && first) ref = seen > 0 ? -fmaxf(v[0] * sc, kRefFloor) : -INFINITY;
-            shift(v, q);
-#pragma unroll
-            for (int x = 0; x < 32; x += 4) {
-              const float2 e0 = make_float2(ex2_approx(v[x]), ex2_approx(v[x + 1]));
-              const float2 e1 = make_float2(ex2_approx(v[x + 2]), ex2_approx(v[x + 3]));
-              s0 = add2(s0, e0);
-              s1 = add2(s1, e1);
-              p[q * 16 + x / 2] = SPLIT ? pack_f16(e0.x, e0.y) : pack_bf16(e0.x, e0.y);
-              p[q * 16 + x / 2 + 1] = SPLIT ? pack_f16(e1.x, e1.y) : pack_bf16(e1.x, e1.y);
+            for (int x = 0; x < 32; x += 2) {
+              const float2 y = fma2(make_float2(v[x], v[x + 1]), sc2, ref2);
+              v[x] = y.x;
+              v[x + 1] = y.y;
             }
-          }
-          s0 = add2(s0, s1);
-          sum = s0.x + s0.y;
-        };
-        if (WIN && (t == s.t0 || masked)) {
-          // A row's reference is the logit of the first key that it sees; before that it has p = 0 throughout.
-          if (t == s.t0) ref = -INFINITY;
-          const int at = first - k0;
-          if (__any_sync(0xffffffffu, at >= 0 && at < kAtTile)) {
+            if (masked) {
+              const uint32_t m = WIN ? sees(q) : 0u;
+#pragma unroll
+              for (int x = 0; x < 32; ++x) v[x] = (WIN ? (m >> x & 1u) != 0 : q * 32 + x < seen) ? v[x] : -INFINITY;
+            }
+          };
+          // the tile's weights against the present reference, and their sum
+          auto weigh = [&](bool first) {
+            float2 s0 = make_float2(0.f, 0.f), s1 = s0;
+            float y[2][32];
+            tmem_ld32(s_addr, y[0]);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              float(&v)[32] = y[q & 1];
+              if (WIN && q > 0 && few) break;
+              tmem_wait_ld();
+              if (q < 3 && !(WIN && few)) tmem_ld32(s_addr + (q + 1) * 32, y[(q + 1) & 1]);
+              // A lane that sees nothing of the segment, or stands for no row but holds one of the next group, has
+              // p = 0 whatever its logits are, so that they cannot ask for a move of the references.
+              if (!WIN && q == 0 && first) ref = seen > 0 ? -fmaxf(v[0] * sc, kRefFloor) : -INFINITY;
+              shift(v, q);
+#pragma unroll
+              for (int x = 0; x < 32; x += 4) {
+                const float2 e0 = make_float2(ex2_approx(v[x]), ex2_approx(v[x + 1]));
+                const float2 e1 = make_float2(ex2_approx(v[x + 2]), ex2_approx(v[x + 3]));
+                s0 = add2(s0, e0);
+                s1 = add2(s1, e1);
+                p[q * 16 + x / 2] = SPLIT ? pack_f16(e0.x, e0.y) : pack_bf16(e0.x, e0.y);
+                p[q * 16 + x / 2 + 1] = SPLIT ? pack_f16(e1.x, e1.y) : pack_bf16(e1.x, e1.y);
+              }
+            }
+            s0 = add2(s0, s1);
+            sum = s0.x + s0.y;
+          };
+          if (WIN && (t == s.t0 || masked)) {
+            // A row's reference is the logit of the first key that it sees; before that it has p = 0 throughout.
+            const int at = first - k0;
+            const bool here = at >= 0 && at < kAtTile;
             float found = 0.f;
+            if (__all_sync(0xffffffffu, at == 0 || !here)) {
+              float v[8];
+              tmem_ld8(s_addr, v);
+              tmem_wait_ld();
+              found = v[0];
+            } else {
+#pragma unroll 1
+              for (int q = 0; q < 4; ++q) {
+                float v[32];
+                tmem_ld32(s_addr + q * 32, v);
+                tmem_wait_ld();
+#pragma unroll
+                for (int x = 0; x < 32; ++x) found = q * 32 + x == at ? v[x] : found;
+              }
+            }
+            if (here) ref = -fmaxf(found * sc, kRefFloor);
+          }
+#pragma unroll 1
+          for (int pass = 0;; ++pass) {
+            weigh(!WIN && pass == 0 && t == s.t0);
+            // a weight above 2^32 (2^15 of fp16 numbers) shows in the sum, so no maximum is kept
+            if (pass > 0 || !__any_sync(0xffffffffu, sum > kTop)) break;
+            // Move the references up to the tile's maxima.  The products of the tiles before are complete:
+            // the barrier of this tile's S was waited for, and they were issued before it.
+            float up = 0.f;
 #pragma unroll 1
             for (int q = 0; q < 4; ++q) {
               float v[32];
               tmem_ld32(s_addr + q * 32, v);
               tmem_wait_ld();
+              shift(v, WIN ? q : 0);
 #pragma unroll
-              for (int x = 0; x < 32; ++x) found = q * 32 + x == at ? v[x] : found;
+              for (int x = 0; x < 32; ++x)
+                up = fmaxf(up, (WIN ? (sees(q) >> x & 1u) != 0 : q * 32 + x < seen) ? v[x] : 0.f);
             }
-            if (at >= 0 && at < kAtTile) ref = -fmaxf(found * sc, kRefFloor);
-          }
-        }
+            const float f = ex2_approx(-up);
+            ref -= up;
+            l *= f;
+            if (t > s.t0) {
 #pragma unroll 1
-        for (int pass = 0;; ++pass) {
-          weigh(!WIN && pass == 0 && t == s.t0);
-          // a weight above 2^32 (2^15 of fp16 numbers) shows in the sum, so no maximum is kept
-          if (pass > 0 || !__any_sync(0xffffffffu, sum > kTop)) break;
-          // Move the references up to the tile's maxima.  The products of the tiles before are complete:
-          // the barrier of this tile's S was waited for, and they were issued before it.
-          float up = 0.f;
-#pragma unroll 1
-          for (int q = 0; q < 4; ++q) {
-            float v[32];
-            tmem_ld32(s_addr + q * 32, v);
-            tmem_wait_ld();
-            shift(v, WIN ? q : 0);
+              for (int x = 0; x < D; x += 8) {
+                float o8[8];
+                tmem_ld8(o_addr + x, o8);
+                tmem_wait_ld();
 #pragma unroll
-            for (int x = 0; x < 32; ++x) up = fmaxf(up, sees(q * 32 + x) ? v[x] : 0.f);
-          }
-          const float f = ex2_approx(-up);
-          ref -= up;
-          l *= f;
-          if (t > s.t0) {
-#pragma unroll 1
-            for (int x = 0; x < D; x += 8) {
-              float o8[8];
-              tmem_ld8(o_addr + x, o8);
-              tmem_wait_ld();
-#pragma unroll
-              for (int z = 0; z < 8; ++z) o8[z] *= f;
-              tmem_st8(o_addr + x, o8);
+                for (int z = 0; z < 8; ++z) o8[z] *= f;
+                tmem_st8(o_addr + x, o8);
+              }
+              tmem_wait_st();
             }
-            tmem_wait_st();
           }
+          l += sum;
+          tmem_st32(s_addr, p);
+          tmem_st32(s_addr + 32, p + 32);
+          tmem_wait_st();
         }
-        l += sum;
-        tmem_st32(s_addr, p);
-        tmem_st32(s_addr + 32, p + 32);
-        tmem_wait_st();
         if (w == 0 && k0 + kAtTile > end && k0 + lane_row >= end) {
           // rows of V that no row of the item sees must not hold what 0 times it is not 0
           const int v_pos = kPer * i + kK, st = v_pos % C::kStages;
@@ -457,6 +499,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
       }
       const float inv = some ? 1.f / l : 0.f;
+      const bool none = WIN && !some;  // O may have no product of this segment
       wait(&ofull_bar[w], seg & 1);
       tc_fence_after();
       float* dst = a.parts.o + (part * a.parts.rows + c) * D;
@@ -465,6 +508,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         float o[32];
         tmem_ld32(o_addr + x, o);
         tmem_wait_ld();
+        if (none) {
+#pragma unroll
+          for (int z = 0; z < 32; ++z) o[z] = 0.f;
+        }
         if (row >= 0) {
           if (final_rows) {
             __nv_bfloat16* out = a.o + static_cast<size_t>(row) * D + x;
