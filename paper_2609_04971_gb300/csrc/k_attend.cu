@@ -289,13 +289,24 @@ __global__ void __launch_bounds__(kMergeThreads, 4) merge_kernel(MergeArgs a) {
     }
   }
 #pragma unroll 1
-  for (int r = kAhead; r < g.R; ++r) {
-    const float lse2 = lse2_sh[r];
-    const int seen = seen_sh[r];
+  for (int r0 = kAhead; r0 < g.R; r0 += kAhead) {  // as many rows' loads under way again
+    float next[kAhead][kKeys];
 #pragma unroll
-    for (int x = 0; x < kKeys; ++x) {
-      const int j = j0 + x * kMergeThreads;
-      if (j < seen) add[x] += ex2_approx(fmaf(__ldcg(y + static_cast<size_t>(r) * g.cap + j), a.sc, -lse2));
+    for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+      for (int x = 0; x < kKeys; ++x) {
+        const int r = r0 + u, j = j0 + x * kMergeThreads;
+        next[u][x] = r < g.R && j < g.cap ? __ldcg(y + static_cast<size_t>(r) * g.cap + j) : 0.f;
+      }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (r0 + u < g.R) {
+        const float lse2 = lse2_sh[r0 + u];
+        const int seen = seen_sh[r0 + u];
+#pragma unroll
+        for (int x = 0; x < kKeys; ++x)
+          if (j0 + x * kMergeThreads < seen) add[x] += ex2_approx(fmaf(next[u][x], a.sc, -lse2));
+      }
     }
   }
 #pragma unroll
