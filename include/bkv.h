@@ -385,9 +385,9 @@ int bkv_unpack4(bkv_ctx* ctx, const void* K4, const void* V4, const void* S4, in
  * K and V the numbers that K4, V4 and S4 stand for.
  * Queries must lie within +-65504, and so must the values that the codes stand for.
  * The logits are those of the values themselves, in fp32.  Up to 96 query rows
- * per KV head (G * n_q), 32 with weights, the codes are multiplied as they are,
- * and the products of an attention weight and a step are rounded to fp16.  More
- * rows read the caches unpacked into the workspace, K as sums of two fp16
+ * per KV head (G * n_q; 80 for head_dim 64, 48 with weights) the codes are
+ * multiplied as they are, the attention weights and their products with the
+ * steps are rounded to fp16.  More rows read the caches unpacked into the workspace, K as sums of two fp16
  * numbers, V rounded to fp16, query elements below 2^-14 to multiples of 2^-24,
  * and the attention weights are rounded to fp16.
  * BKV_ESTATE when the workspace that bkv_attend4_reserve made is too small.

@@ -175,7 +175,8 @@ int pack4(bkv_ctx* ctx, bool pack, bkv::Pack4Args& a) {
   if (a.n_rows < 0) return fail(ctx, BKV_EINVAL, "n_rows must be >= 0");
   a.n_inst = s.batch * s.n_kv;
   a.cap = s.cap;
-  if (1LL * a.n_inst * a.n_rows >= (1LL << 31)) return fail(ctx, BKV_EINVAL, "batch * n_kv_heads * n_rows must be below 2^31");
+  if (1LL * a.n_inst * a.n_rows >= (1LL << 31))
+    return fail(ctx, BKV_EINVAL, "batch * n_kv_heads * n_rows must be below 2^31");
   if (a.n_rows == 0) return BKV_OK;
   if (!a.K || !a.V || !a.K4 || !a.V4 || !a.S4 || !a.len)
     return fail(ctx, BKV_EINVAL, "K, V, K4, V4, S4 and len must be non-NULL");

@@ -244,8 +244,9 @@ __global__ void __launch_bounds__(kMergeThreads, 4) merge_kernel(MergeArgs a) {
     return;
   }
   // ---- weights from the kept logits: one block per instance and run of keys
-  __shared__ float lse2_sh[kLogitRows];
-  __shared__ int seen_sh[kLogitRows];
+  constexpr int kMostRows = kLogitRows > kLogitRows4 ? kLogitRows : kLogitRows4;
+  __shared__ float lse2_sh[kMostRows];
+  __shared__ int seen_sh[kMostRows];
   int e;
   const int j0 = a.by_key_blocks.mod(blockIdx.x - a.row_blocks, e) * kMergeKeys + tid;
   // loads that need no normaliser, under way while it is computed: the first kAhead rows
@@ -443,7 +444,7 @@ AtLayout attend4_layout(const Shape& s, int n_q, bool weights) {
   const int sms = l.sms = device_sms();
   const int R = s.G * n_q;
   const size_t rows = static_cast<size_t>(s.batch) * s.n_kv * R;
-  if (R > (weights ? kLogitRows4 : kRows4)) {
+  if (R > (weights ? kLogitRows4 : kRows4[s.d == 128])) {
     l.unpacked = true;
     // the rows kernel of k_attend_rows.cuh, whatever the rows
     l.own = make_plan(s, s.batch * s.n_kv, 1, R, n_q, true, s.cap, 1, sms, l.too_large, R <= kMaxRows ? kMaxRows : 0);

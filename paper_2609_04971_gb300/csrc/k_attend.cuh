@@ -21,10 +21,19 @@ constexpr int kAtTile = 128;             // keys per tile
 constexpr uint32_t kAtBox = 128 * 128;   // [128 rows][64 bf16] swizzled box
 constexpr int kMaxRows = 256;            // query rows per row block
 constexpr int kBlockRows4 = 16;          // the same over 4-bit caches
-// Query rows per KV head up to which a 4-bit cache is read code by code, 16 rows at a time; beyond, its rows are
-// unpacked to fp16 first.
-constexpr int kRows4 = 96;
-constexpr int kLogitRows4 = 32;  // the same with weights
+// Query rows per KV head up to which a 4-bit cache is read code by code, 16 rows at a time, which takes time by the
+// row; beyond, its rows are unpacked to fp16 first, which does not.  A call in us, by codes and unpacked:
+//   without weights       32 rows     64 rows     80 rows     96 rows     128 rows
+//   128 x 4224          74, 177    122, 178    144, 179    169, 179    212, 181
+//   8 x 32768           48, 101     68, 101     76, 102     89, 103    107, 103
+//   32 x 1024            23, 25      31, 25      33, 27      40, 27      42, 27
+//   128 x 4224, d 64    54, 102     87, 102    101, 103    117, 103    146, 105
+//   with weights          16 rows     32 rows     48 rows     64 rows      96 rows
+//   128 x 4224          66, 225    116, 225    161, 227    208, 228    294, 231
+//   8 x 32768           46, 127     66, 129     91, 129    113, 129    165, 131
+//   32 x 1024            27, 36      36, 32      46, 32      54, 34      72, 35
+constexpr int kRows4[2] = {80, 96};  // head_dim 64, 128
+constexpr int kLogitRows4 = 48;      // the same with weights
 // Query rows per KV head up to which the logits are kept for the weights, 4 bytes a row and key written and
 // read once more, row by row by the merge; beyond, the weights are recomputed from the keys by two more launches.
 // A call in us, kept and recomputed, by the number of caches and their keys:

@@ -10,8 +10,8 @@
 // No element is ever scaled or rounded by itself.  A code in the lowest bits of an fp16 number is the
 // number n 2^-24 (a subnormal, or in bits 4..7 16 n 2^-24: up to 2047 the bits of fp16 count linearly), so one
 // AND makes two operands of a tensor-core product; a shift every second.  The queries, scaled to 2^11 by a
-// power of two of each row, are exact in fp16 down to 2^-24 of the row's largest element; p step is rounded to fp16 once
-// (2^-11 of itself; below some 2^-31 of the largest it becomes 0).
+// power of two of each row, are exact in fp16 down to 2^-24 of the row's largest element; p and p step are rounded to
+// fp16 (2^-11 of themselves each; p below some 2^-35 of the largest becomes 0).
 //
 // Warps, not the tcgen05 unit, hold the operands: m16n8k16 products take the unpacked codes from the registers
 // they are unpacked in, where tcgen05 would need 16-bit copies of every code in shared memory, four times the
@@ -136,8 +136,8 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[N], const void* p) {
 // Linear copy of `bytes` (a multiple of 16, both ends 16-byte aligned) into shared memory.
 __device__ __forceinline__ void bulk_load(void* dst, const void* src, uint32_t bytes, uint64_t* bar, uint64_t policy) {
   asm volatile(
-      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(
-          smem_u32(dst)),
+      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint"
+      " [%0], [%1], %2, [%3], %4;" ::"r"(smem_u32(dst)),
       "l"(src), "r"(bytes), "r"(smem_u32(bar)), "l"(policy)
       : "memory");
 }

@@ -219,7 +219,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       auto issue_s = [&](int w, int st, int st2, bool done, bool last_of_seg, bool unseen, bool few) {
         if (!ok) return;
         tc_fence_after();
-        const uint64_t q = sdesc_kmajor_sw128(q_addr + w * kAtBox), k = sdesc_kmajor_sw128(kv_addr + st * C::kTileBytes);
+        const uint64_t q = sdesc_kmajor_sw128(q_addr + w * kAtBox);
+        const uint64_t k = sdesc_kmajor_sw128(kv_addr + st * C::kTileBytes);
         const uint64_t k2 = sdesc_kmajor_sw128(kv_addr + st2 * C::kTileBytes);
         if (elect_one()) {
           if (!WIN || !unseen) {
@@ -242,24 +243,25 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
       };
       bool begun[2] = {};  // O of the row tile has a product of this segment
-      auto issue_o = [&](int w, int i, int st, int seg, bool first, bool last_of_seg, bool done, bool unseen, bool few) {
+      auto issue_o = [&](int w, int i, int st, int seg, bool first, bool last_of_seg, bool done, bool unseen,
+                         bool few) {
         await(&pfull_bar[w], i & 1);
         if (first && seg >= 1) await(&ofree_bar[w], (seg - 1) & 1);
         if (!ok) return;
         tc_fence_after();
         const uint64_t v = sdesc_mnmajor_sw128(kv_addr + st * C::kTileBytes, kAtBox);
+        const uint32_t o = tm + C::kO + w * D, p = tm + w * kAtTile;
         if (elect_one()) {
           if constexpr (WIN) {
             const int steps = unseen ? 0 : few ? kSinkRows / 16 : kAtTile / 16;
             const bool more = !first && begun[w];
 #pragma unroll
             for (int kk = 0; kk < kAtTile / 16; ++kk)
-              if (kk < steps)
-                mma_bf16_ts(tm + C::kO + w * D, tm + w * kAtTile + kk * 8, v + kk * (2048 >> 4), idesc_o, more || kk > 0);
+              if (kk < steps) mma_bf16_ts(o, p + kk * 8, v + kk * (2048 >> 4), idesc_o, more || kk > 0);
           } else {
 #pragma unroll
             for (int kk = 0; kk < kAtTile / 16; ++kk)
-              mma_bf16_ts(tm + C::kO + w * D, tm + w * kAtTile + kk * 8, v + kk * (2048 >> 4), idesc_o, !first || kk > 0);
+              mma_bf16_ts(o, p + kk * 8, v + kk * (2048 >> 4), idesc_o, !first || kk > 0);
           }
           if (last_of_seg) mma_commit(&ofull_bar[w]);
           if (done) mma_commit(&empty_bar[st]);

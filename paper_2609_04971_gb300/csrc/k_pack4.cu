@@ -245,7 +245,8 @@ __global__ void __launch_bounds__(kPackThreads) unpack16_kernel(Unpack16Args a, 
   const bool mine = r < len;
   const int grp = i >> 2, t = i & 3;
   const size_t row = static_cast<size_t>(e) * a.cap + r;
-  const uint32_t kw = mine ? __ldg(a.K4 + row * T + t * kGroups + grp) : 0u, vw = mine ? __ldg(a.V4 + row * T + v_word<D>(i)) : 0u;
+  const uint32_t kw = mine ? __ldg(a.K4 + row * T + t * kGroups + grp) : 0u,
+                 vw = mine ? __ldg(a.V4 + row * T + v_word<D>(i)) : 0u;
   const uint32_t ks = mine ? __ldg(a.S4 + row * (2 * kGroups) + grp) : 0u,
                  vs = mine ? __ldg(a.S4 + row * (2 * kGroups) + kGroups + grp) : 0u;
   const uint32_t vc = transpose_row<D>(vw, i);

@@ -73,7 +73,7 @@ def test_single_tokens(d, G):
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("G,n_q", [(1, 2), (4, 5), (2, 40), (1, 128), (5, 25)])
 def test_several_tokens(d, G, n_q):
-    """Rows that begin to see keys at different places, windows shorter than the new tokens, caches shorter than them."""
+    """Rows that begin to see keys at different places, windows and caches shorter than the new tokens."""
     b, hkv, cap = 3, 2, 520
     lens = ga._lens(b, hkv, [520, max(1, n_q - 1), n_q, 300, 131, 256])
     q, K, V = ga._inputs(b, G * hkv, hkv, d, cap, n_q, seed=n_q)
