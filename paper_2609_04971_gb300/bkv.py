@@ -626,14 +626,16 @@ class BeaconKV:
                              f"{tuple(shape)}")
         if q.dtype is not torch.bfloat16 or not q.is_cuda or not q.is_contiguous():
             _ptr(q, torch.bfloat16, "q")
+        n_q = shape[2]
         if o_out is None and lse_out is None:
-            o_out, lse_out = self._new(q, shape, torch.bfloat16, shape[:3], torch.float32)
-        elif o_out is None:
+            o, lse = self._new(q, shape, torch.bfloat16, shape[:3], torch.float32)
+            return n_q, q.data_ptr(), o, lse, o.data_ptr(), lse.data_ptr()
+        if o_out is None:
             o_out, _ = self._new(q, shape, torch.bfloat16, 0, torch.float32)
         elif lse_out is None:
             lse_out, _ = self._new(q, shape[:3], torch.float32, 0, torch.float32)
-        n = batch * heads * shape[2]
-        return (shape[2], q.data_ptr(), o_out, lse_out, _arg(o_out, torch.bfloat16, n * d, "o_out"),
+        n = batch * heads * n_q
+        return (n_q, q.data_ptr(), o_out, lse_out, _arg(o_out, torch.bfloat16, n * d, "o_out"),
                 _arg(lse_out, torch.float32, n, "lse_out"))
 
     def attend_window(self, q, K, V, *, length, window, n_sink=0, scale=None, o_out=None, lse_out=None):
@@ -709,25 +711,27 @@ class BeaconKV:
             K4_out, V4_out, S4_out, weights_out = K4, V4, S4, weights
         elif given != 4:
             raise ValueError("K4_out, V4_out, S4_out and weights_out come together or not at all")
-        cap_out = weights_out.numel() // self.n_inst
-        self._cache4(K4, V4, S4, self.n_inst * self.cfg.capacity)
-        self._cache4(K4_out, V4_out, S4_out, self.n_inst * cap_out, "_out")
-        kept_out, len_out = self._evict_args(K4, weights, L, budget, weights_out, kept_out, len_out)
-        bkv_evict4(self.ctx, K4, V4, S4, weights, L, budget, K4_out, V4_out, S4_out, weights_out, cap_out, kept_out,
-                   len_out)
+        n_inst, f32, i32 = self.n_inst, torch.float32, torch.int32
+        cap_out = weights_out.numel() // n_inst
+        rows = n_inst * self.cfg.capacity
+        k4, v4, s4 = self._cache4(K4, V4, S4, rows)
+        ko, vo, so = (k4, v4, s4) if given == 0 else self._cache4(K4_out, V4_out, S4_out, n_inst * cap_out, "_out")
+        wp, wo = _arg(weights, f32, rows, "weights"), _arg(weights_out, f32, n_inst * cap_out, "weights_out")
+        lp = _arg(L, i32, n_inst, "L")
+        kept_out, len_out = self._evict_outputs(K4, budget, kept_out, len_out)
+        rc = _lib.bkv_evict4(self.ctx, k4, v4, s4, wp, lp, budget, ko, vo, so, wo, cap_out,
+                             _arg(kept_out, i32, n_inst * budget, "kept_out"), _arg(len_out, i32, n_inst, "len_out"))
+        if rc:
+            _check(rc, "bkv_evict4", self.ctx)
         return kept_out, len_out
 
-    def _evict_args(self, K, weights, L, budget, weights_out, kept_out, len_out):
-        c, n_inst = self.cfg, self.n_inst
-        self._expect(weights, n_inst * c.capacity, "weights")
-        self._expect(L, n_inst, "L")
-        self._expect(weights_out, weights_out.numel() // n_inst * n_inst, "weights_out")
-        self._expect(kept_out, n_inst * budget, "kept_out")
-        self._expect(len_out, n_inst, "len_out")
+    def _evict_outputs(self, K, budget, kept_out, len_out):
+        """The outputs of an eviction, new where they are not given."""
         if not K.is_cuda:
-            raise TypeError("the caches must be CUDA tensors")
+            raise TypeError("K must be a CUDA tensor")
         if kept_out is None or len_out is None:
-            shape, i32 = (c.n_layers, c.batch, c.n_kv_heads), torch.int32
+            c, i32 = self.cfg, torch.int32
+            shape = (c.n_layers, c.batch, c.n_kv_heads)
             kept, length = self._new(K, shape + (max(0, budget) if kept_out is None else 0,), i32, shape, i32)
             kept_out = kept if kept_out is None else kept_out
             len_out = length if len_out is None else len_out
@@ -753,7 +757,12 @@ class BeaconKV:
         self._expect(V, rows * d, "V")
         self._expect(K_out, rows_out * d, "K_out")
         self._expect(V_out, rows_out * d, "V_out")
-        kept_out, len_out = self._evict_args(K, weights, L, budget, weights_out, kept_out, len_out)
+        self._expect(weights, rows, "weights")
+        self._expect(L, n_inst, "L")
+        self._expect(weights_out, rows_out, "weights_out")
+        self._expect(kept_out, n_inst * budget, "kept_out")
+        self._expect(len_out, n_inst, "len_out")
+        kept_out, len_out = self._evict_outputs(K, budget, kept_out, len_out)
         bkv_evict(self.ctx, K, V, weights, L, budget, K_out, V_out, weights_out, cap_out, kept_out, len_out)
         return kept_out, len_out
 
