@@ -243,8 +243,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
       };
       bool begun[2] = {};  // O of the row tile has a product of this segment
-      auto issue_o = [&](int w, int i, int st, int seg, bool first, bool last_of_seg, bool done, bool unseen,
-                         bool few) {
+      bool early[2] = {};  // its results were announced before the segment's last tile, which it does not see
+      auto issue_o = [&](int w, int i, int st, int seg, bool first, bool last_tile, bool done, bool unseen, bool few,
+                         bool rest_unseen) {
+        const bool last_of_seg = WIN ? (last_tile && !early[w]) || rest_unseen : last_tile;
         await(&pfull_bar[w], i & 1);
         if (first && seg >= 1) await(&ofree_bar[w], (seg - 1) & 1);
         if (!ok) return;
@@ -266,6 +268,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           if (last_of_seg) mma_commit(&ofull_bar[w]);
           if (done) mma_commit(&empty_bar[st]);
         }
+        if (WIN) early[w] = last_of_seg && !last_tile;
         if (WIN) begun[w] = (!first && begun[w]) || !unseen;
         __syncwarp();
       };
@@ -300,7 +303,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         for (int w = 0; w < 2; ++w) {
           if (i > 0) {
             if (w == 0) await(&full_bar[v_st], (v_pos / C::kStages) & 1);
-            issue_o(w, i - 1, v_st, seg_o, first, last, w == 1, o_unseen[w], o_few);
+            issue_o(w, i - 1, v_st, seg_o, first, last, w == 1, o_unseen[w], o_few,
+                    WIN && more && !turn && last_s && unseen[w]);
           }
           if (more) {
             if (w == 0 && turn) await(&qfull_bar, seg & 1);
@@ -329,22 +333,31 @@ __global__ void __launch_bounds__(kThreads, 1)
       at_wait(bar, parity, abort_flag, a.err, kDevTimeoutEpilogue);
       __syncwarp();
     };
+    // What a thread needs to know of a segment: its row of q, o and lse (or -1), the keys that the row and the warp's
+    // rows see, with a window the first of them, and those that any row of the block sees.
+    struct Rows {
+      int row, lim, lim_min, lo_max, first, limit_max;
+    };
+    auto rows_of = [&](const AtSeg& s) {
+      Rows r;
+      r.row = c < cols ? at_row(g, s.e, {s.b0, s.r0}, c) : -1;
+      r.lim = r.row < 0 ? 0 : at_limit(g, s.len, s.r0, c);
+      r.lim_min = __reduce_min_sync(0xffffffffu, r.row < 0 ? 0x7fffffff : r.lim);
+      r.lo_max = WIN ? __reduce_max_sync(0xffffffffu, r.lim) - g.window : 0;
+      r.first = WIN ? at_first_seen(g, r.lim, at_key0<WIN>(s, s.t0)) : 0;
+      r.limit_max = at_limit_max(g, s.len, s.r0);
+      return r;
+    };
     AtSeg s, next;
+    Rows now, then;
     int i = 0;  // tile of the CTA
-    bool more = false;
-    for (int seg = -1;; ++seg) {  // each segment is looked up one ahead
-      const bool have = more;
+    bool have = walk.next(g, next), more = false;
+    if (have) then = rows_of(next);
+    for (int seg = 0; have; ++seg, have = more) {
       s = next;
-      more = walk.next(g, next);
-      if (seg < 0) continue;
-      if (!have) break;
-      const int row = c < cols ? at_row(g, s.e, {s.b0, s.r0}, c) : -1;
-      const int lim = row < 0 ? 0 : at_limit(g, s.len, s.r0, c);
-      const int lim_min = __reduce_min_sync(0xffffffffu, row < 0 ? 0x7fffffff : lim);  // of the warp's rows
-      const int lo_max = WIN ? __reduce_max_sync(0xffffffffu, lim) - g.window : 0;
-      const int first = WIN ? at_first_seen(g, lim, at_key0<WIN>(s, s.t0)) : 0;
-      const int limit_max = at_limit_max(g, s.len, s.r0);
-      if (tid == 128) at_note(a.parts, s, !more, share_sh.per);
+      now = then;
+      const int row = now.row, lim = now.lim, lim_min = now.lim_min, lo_max = now.lo_max, first = now.first;
+      const int limit_max = now.limit_max;
       float ref = 0.f, l = 0.f;  // ref: minus the reference
       for (int t = s.t0; t < s.t1; ++t, ++i) {
         const int k0 = at_key0<WIN>(s, t);
@@ -487,7 +500,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive(&pfull_bar[w]);
       }
-      // ---- the segment's result
+      // ---- the segment's result; the next one is looked up while its last products run
+      more = walk.next(g, next);
+      if (more) then = rows_of(next);
+      if (tid == 128) at_note(a.parts, s, !more, share_sh.per);
       const bool final_rows = a.whole_is_final && s.t0 == 0 && s.t1 == s.T;
       const size_t part = blockIdx.x + s.item;
       const bool some = l != 0.f;  // a NaN stays one
