@@ -19,10 +19,23 @@
 //
 // Persistent, one CTA per SM, the work split into segments as in k_attend.cuh.  A warp takes slices
 // of 16 keys: S [16 keys x 8 rows] per block of 8 query rows, P transposed in registers (movmatrix), and
-// O^T [D x 8 rows] += V^T P.  Each warp has its own reference m of a row's logits (base 2): it moves up
-// when a logit exceeds it by more than 4, and p = 2^(y - m) stays below 2^4.  The steps are scaled by a
-// power of two 2^E, which moves likewise, so that p step 2^E fits fp16.  The warps' sums are joined in shared
-// memory at a segment's end.
+// O^T [D x 8 rows] += V^T P.  The lows' share of a logit is a product too, of a key's lows and the queries' sums as
+// three fp16 terms (33 bits), and so is their share of the output.  Each warp has its own reference m of a row's
+// logits (base 2), which moves up when a logit exceeds it by more than 4, less an exponent E that keeps
+// p step = 2^(y - m + E) step within fp16 and moves when a step is too large for it.
+//
+// Warp roles: three load tiles of 128 keys into a ring, K, V and scales each (linear copies, 20 KB a tile at
+// head_dim 128), one prepares the queries of the next segment as operands and joins the warps' sums of the last one,
+// twelve (eight with two blocks of rows, whose accumulators need the registers) take steps of 32 keys in turn.
+//
+// Bound by HBM on long caches and by start and end on short ones; 293 instructions a slice, half of them on the
+// integer pipe, which unpacks, leave it there.  head_dim 128, cold: 128 caches of 4097..4224 keys, 4 rows 26.3 us,
+// 88 MB; of 16896 keys 69 us, 346 MB, 5.0 TB/s; from 4224 to 16896 keys 6.3 TB/s (0.95 of the measured copy rate), so
+// some 14 us are fixed: 2.7 until the first load leaves (the lengths, the split), 2 until it is there, 2 to 3 after the
+// last step, a segment's queries and join in between.  8 rows cost as much as 4; 16 rows 45 us, 32 rows 70 us: eight
+// warps of long dependent chains.  Blocks of 8 rows: 51 and 80 us; twelve warps for two blocks, their operands read
+// from shared memory each time: 52 and 79 us (head_dim 64, operands in registers: 32 rows 52 us and 55, but 28 rows of
+// 7 sequences with weights 57 us and 53).
 #include <cuda_fp16.h>
 
 #include "k_attend.cuh"

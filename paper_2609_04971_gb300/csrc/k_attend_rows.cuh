@@ -23,11 +23,20 @@
 // Per 256 x 128 tile with head_dim 128 the products take 2048 clocks, as do the shared
 // memory's reads for them and the copies into it (256 KB), and the exponentials, 32 per
 // clock and SM, 1024; the two groups overlap them to some 3400.  A prompt of 4096
-// tokens, 32 heads, cold: 128 us, 1.07 PFLOP/s of the causal pairs (0.57 of the measured
+// tokens, 32 heads, cold: 117 us, 1.17 PFLOP/s of the causal pairs (0.61 of the measured
 // rate of a large product); some 2 us at the end of each of a CTA's four segments are its
 // results' way out, in which the tensor cores wait.  Steps of 64 keys, with S of both halves under way, were slower
 // (a call of this prompt 196 us instead of 152): a product of half the columns takes more than
 // half the time, and there are twice as many hand-overs.  So were two issuing warps.
+//
+// With a window (WIN) tiles and references are as in k_attend_tiles.cuh, a row tile has no products with a tile of
+// which it sees nothing, and a tile of up to 16 first keys only the products of those.  8192 queries of 32 heads,
+// window 1024 and 4 first keys: 180 us, 0.72 PFLOP/s of the pairs seen.  A tile takes 1.85 us, 0.95 of it a group's
+// exponentials and 0.9 its products; three of a row tile's ten are masked in part (1.4 us of exponentials); from one
+// segment of ten tiles to the next 3 to 4 us pass.
+//
+// With SPLIT q, K and V hold fp16 numbers and the keys are K + K_rest, so S takes twice the products; P is fp16, and
+// its reference moves at 2^15.  512 queries of 32 heads over 32768 keys: 257 us, tensor pipe busy 0.67 of the time.
 #pragma once
 
 #include "k_attend.cuh"

@@ -45,6 +45,11 @@
 // of 4097..4224 keys, 4 rows: 48 us, 277 MB, 5.8 TB/s (0.85 of the measured copy rate);
 // 8 caches of 32768 keys: 27 us, 134 MB, 5.0 TB/s; 8 prefixes of 32768 keys, 64 rows:
 // 28 us.  About 4.5 us pass until the first tile is there and 2 us after the last.
+//
+// With a window (WIN, bkv_attend_window) an item's tiles are those of the first keys, then a run that begins at the
+// first key that any row's window reaches (a TMA copy may start at any row), and a column's reference is the logit of
+// the first key that it sees.  Up to 16 first keys are loaded in boxes of 16 rows, not as a whole tile: 128 caches,
+// window 1024 and 4 first keys, cold: 19.5 us, 70 MB, 3.6 TB/s.
 #pragma once
 
 #include <climits>

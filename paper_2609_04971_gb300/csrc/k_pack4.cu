@@ -11,7 +11,8 @@
 // K stores a thread's eight codes as one word.  A row of V stores in one word what the attention's
 // products need of eight of their rows, which eight threads hold: a transpose in three exchanges.
 //
-// Bound by HBM: 4 d bytes of bf16 and 1.25 d bytes of codes and scales a row.
+// Bound by HBM: 4 d bytes of bf16 and 1.25 d bytes of codes and scales a row.  295 thousand rows of head_dim 128,
+// cold: packed in 58.5 us (199 MB, 3.4 TB/s; some 140 instructions to eight elements), read back in 35 us (5.6 TB/s).
 #include <cuda_fp16.h>
 
 #include "bkv_device.cuh"
