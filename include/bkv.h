@@ -9,7 +9,9 @@
  * data-parallel parts of that step for a whole model (all layers, batch rows
  * and KV heads at once), and the attention of a decode loop over the caches
  * that it compacts, with eviction by accumulated attention weight as a second
- * rule (bkv_attend, bkv_attend_shared, bkv_evict):
+ * rule (bkv_attend, bkv_attend_shared, bkv_evict), with a sliding window
+ * (bkv_attend_window) and over caches held in 4 bits (bkv_pack4, bkv_attend4,
+ * bkv_evict4):
  *
  *   beacon maintenance  - FPS seeding from prompt queries (Appendix D.1,
  *                         Algorithm 1) and, per decode query, nearest-beacon
@@ -32,8 +34,8 @@
  * row-major and contiguous, aligned to 16 bytes, unless the description says
  * "host".  bf16 tensors hold IEEE binary32 values truncated to their top 16
  * bits (bfloat16).  The library owns only what bkv_create (beacon state and
- * scratch) and bkv_attend_reserve (workspace) allocate and frees it in
- * bkv_destroy.
+ * scratch), bkv_attend_reserve and bkv_attend4_reserve (workspace) allocate and
+ * frees it in bkv_destroy.
  *
  * Streams.  All work is enqueued on the CUDA stream given to bkv_create (or
  * bkv_set_stream); calls return before it completes.  Outputs are valid once
@@ -480,8 +482,8 @@ int bkv_set_cfps_state(bkv_ctx* ctx, const void* buffers, const int32_t* sizes);
  * Waits for the context's stream, then reads and clears the device error
  * word.  Returns BKV_OK, BKV_ETIMEOUT (a kernel gave up a bounded wait and
  * its outputs are invalid), BKV_EINVAL (a per-instance length of
- * bkv_compress_ragged outside 1..capacity, or of bkv_attend, bkv_attend_shared
- * or bkv_evict outside 0..capacity), BKV_EBOUNDS (a library built with
+ * bkv_compress_ragged outside 1..capacity, of an attention, an eviction, bkv_pack4
+ * or bkv_unpack4 outside 0..capacity, or a `first` past it), BKV_EBOUNDS (a library built with
  * BKV_CHECKED found an index from device data out of range, skipped that
  * access, and the outputs are invalid) or BKV_ECUDA.
  */
@@ -524,10 +526,10 @@ int bkv_selftest_bounds(bkv_ctx* ctx);
 
 /*
  * Allocation-failure hook (test diagnostic).  With nth > 0, the nth device
- * or pinned host allocation that later bkv_create and bkv_attend_reserve calls
- * attempt (counted from this call, across contexts) fails as if memory ran
+ * or pinned host allocation that later bkv_create, bkv_attend_reserve and
+ * bkv_attend4_reserve calls attempt (counted from this call, across contexts) fails as if memory ran
  * out, without allocating: that bkv_create releases what it had allocated,
- * leaves *out NULL and returns BKV_ENOMEM; that bkv_attend_reserve returns
+ * leaves *out NULL and returns BKV_ENOMEM; that reservation returns
  * BKV_ENOMEM and leaves the workspace as it was.  The hook disarms itself after that one
  * failure; nth = 0 disarms it.  Not thread-safe with concurrent bkv_create
  * calls.  Returns BKV_OK, or BKV_EINVAL for nth < 0.

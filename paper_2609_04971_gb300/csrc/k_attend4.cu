@@ -28,7 +28,7 @@
 // head_dim 128), one prepares the queries of the next segment as operands and joins the warps' sums of the last one,
 // twelve (eight with two blocks of rows, whose accumulators need the registers) take steps of 32 keys in turn.
 //
-// Bound by HBM on long caches and by start and end on short ones; 293 instructions a slice, half of them on the
+// Bound by HBM on long caches and by start and end on short ones; 290 instructions a slice, half of them on the
 // integer pipe, which unpacks, leave it there.  head_dim 128, cold: 128 caches of 4097..4224 keys, 4 rows 26.3 us,
 // 88 MB; of 16896 keys 69 us, 346 MB, 5.0 TB/s; from 4224 to 16896 keys 6.3 TB/s (0.95 of the measured copy rate), so
 // some 14 us are fixed: 2.7 until the first load leaves (the lengths, the split), 2 until it is there, 2 to 3 after the
