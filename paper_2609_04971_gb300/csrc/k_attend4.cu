@@ -353,7 +353,9 @@ __global__ void __launch_bounds__(Cfg4<D, NB>::kThreads, 1) attend4_kernel(Kerne
 #pragma unroll 1
         for (int c = 0; c < cols; ++c) {
           constexpr int kPer = D / 32;
-          const float ref = lane < kWarps ? ref_sh[lane][c] : kRefFloor, l = lane < kWarps ? sum_sh[lane][c] : 0.f;
+          const float l = lane < kWarps ? sum_sh[lane][c] : 0.f;
+          // a warp that took no step has no reference either
+          const float ref = l != 0.f ? ref_sh[lane][c] : kRefFloor;
           float m = ref;
 #pragma unroll
           for (int x = 16; x; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));

@@ -389,6 +389,26 @@ def test_references_and_step_scales_move(d):
 
 
 @pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,n_q,level", [(4, 1, -1), (4, 1, 1), (5, 3, -1), (2, 60, -1)])
+def test_logits_far_from_zero(d, G, n_q, level):
+    """All logits hundreds below (or above) 0, in caches so short that most of a block's warps have no keys."""
+    b, hkv, cap = 2, 2, 333
+    lens = ga._lens(b, hkv, [1, 40, 333, 129])
+    g = torch.Generator(device=DEV).manual_seed(4)
+    u = torch.randn(b, hkv, 1, d, generator=g, device=DEV)
+    K = (4 * u + torch.randn(b, hkv, cap, d, generator=g, device=DEV)).bfloat16()
+    q = (level * 8 * u.repeat_interleave(G, 1) + torch.randn(b, G * hkv, n_q, d, generator=g, device=DEV)).bfloat16()
+    cache = packed(K, rows(b, hkv, cap, d, seed=5))
+    poison(cache, lens)
+    bk = ga._bk(b, G * hkv, hkv, d, cap)
+    try:
+        many = G * n_q > 96
+        run4(bk, q, cache, lens, weights=not many, ref=reference4(q, *cache, lens, many=many))
+    finally:
+        bk.close()
+
+
+@pytest.mark.parametrize("d", [64, 128])
 def test_extreme_queries_and_constant_rows(d):
     """Queries of every magnitude (with a scale to match), zero queries, rows of one value, all-zero caches."""
     b, hq, hkv, cap = 4, 8, 2, 150
