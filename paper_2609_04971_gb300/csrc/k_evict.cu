@@ -1,15 +1,15 @@
 // Eviction by accumulated attention weight: selection of the kept rows and
 // compaction of K, V and the weights.
 //
-// Selection, one CTA per instance.  Each warp owns a contiguous run of rows, 32 at
-// a time across its lanes; the keys stay in shared memory (in registers the passes
-// would have to be unrolled, and a short kernel pays for every instruction that it
-// fetches).  A three-pass radix select (digits of 12, 10 and 10 bits from the top, one shared histogram) finds the
-// key T of the last row that is kept by weight and how many rows equal to T are needed.
-// A 12-bit first digit splits an octave into 8 bins: weights that span a few octaves,
+// Selection, one CTA per instance.  Each warp owns a contiguous run of rows, four to a lane.  A radix select finds the
+// key T of the last row that is kept by weight and how many rows equal to T are needed: one pass over the
+// weights counts their first digits, a second one marks the rows that these decide, four bits to four rows, and lists
+// those that share the first digit of T.  The list is short, so that it alone is searched for the other digits and
+// corrects the marks; weights of which more share a digit than the list holds are read in three more
+// passes.  A first digit of 12 bits splits an octave into 8 bins: weights that span a few octaves,
 // as softmax sums do, then spread over enough bins that the histogram's atomics seldom
-// meet.  Kept rows are numbered in index order by ballots inside each warp and one scan
-// of the warps' totals; rows equal to T are taken in index order.
+// meet.  The marked rows are numbered in index order by scans inside each warp and one scan of the warps' totals;
+// rows equal to T are taken in index order.  Bound by instruction issue (2.5 a clock on each SM that has a block).
 //
 // Compaction, a launch of its own.  Row i receives row kept[i] >= i.  Into other
 // buffers the rows are independent and move in small blocks spread over all SMs.  In
@@ -20,10 +20,10 @@
 //
 // Bound by HBM: the kept rows are read and written once (8 d bytes a row), the
 // weights read (4 bytes a cached row) and written.  head_dim 128, cold: 1024 instances of
-// 4224 rows to 4096, selection 35.5 us, rows 604 us, 4.3 GB at 7.1 TB/s (1.05 of the measured copy
-// rate), in place 701 us for the whole call; 320 instances of 1..32768 rows to 2048, 47.5 and
-// 95.5 us (the selection there is one CTA of 1024 threads to an SM, in 2.1 waves).  4-bit caches (1.25 d bytes a row,
-// moved in vectors of K, V and scales): the same selections, rows 203 us (1.34 GB, 6.6 TB/s) and 45 us.
+// 4224 rows to 4096, selection 32 us, rows 607 us, 4.3 GB at 7.1 TB/s (1.05 of the measured copy
+// rate), in place 701 us for the whole call; 320 instances of 1..32768 rows to 2048, 30.5 and
+// 99 us.  4-bit caches (1.25 d bytes a row, moved in vectors of K, V and scales): the same selections, rows 207 us
+// (1.34 GB, 6.5 TB/s) and 51 us.
 #include "bkv_device.cuh"
 #include "bkv_internal.h"
 #include "k_launch.cuh"
@@ -64,60 +64,71 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* wsum, uint3
   return before + incl - v;
 }
 
-// The rows of one warp: row0 + 32 i + lane for i < n, and their keys in shared memory.
+// The rows of one warp, four to a lane: row0 + 128 i + c for i < n and c < 4, in order over the lanes.  each(f) calls
+// f(first row, keys) for them, every lane together; candidates are the rows of [c_lo, c_hi).  The weights are read again
+// in every pass: the first one leaves them in L1 and L2, and without a copy in shared memory a block of 1024 threads
+// has a second one beside it.
 struct WarpRows {
-  uint32_t* key;
-  int row0, n, lane, L;
-  __device__ __forceinline__ void init(const float* w) {
-    constexpr int kBatch = 8;  // loads under way
+  const float* w;
+  int row0, n, L, c_lo, c_hi;
+  bool aligned;  // to 16 bytes, and an instance's rows a multiple of four
+  __device__ __forceinline__ float4 load(int j) const {
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (aligned) {
+      if (j < L) v = __ldg(reinterpret_cast<const float4*>(w + j));
+    } else {
+      if (j < L) v.x = __ldg(w + j);
+      if (j + 1 < L) v.y = __ldg(w + j + 1);
+      if (j + 2 < L) v.z = __ldg(w + j + 2);
+      if (j + 3 < L) v.w = __ldg(w + j + 3);
+    }
+    return v;
+  }
+  template <typename F>
+  __device__ __forceinline__ void each(F&& f) const {
+    float4 next = load(row0);
 #pragma unroll 1
-    for (int i0 = 0; i0 < n; i0 += kBatch) {
-      float v[kBatch];
-#pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const int j = row0 + (i0 + u) * 32 + lane;
-        v[u] = j < L ? w[j] : 0.f;
-      }
-#pragma unroll
-      for (int u = 0; u < kBatch; ++u) {
-        const int j = row0 + (i0 + u) * 32 + lane;
-        if (i0 + u < n && j < L) key[j] = weight_key(v[u]);
-      }
-    }
-    __syncwarp();
-  }
-  // inner(row, key) for 32 rows that are all candidates, [c_lo, c_hi); edge(row, key) for the others, also
-  // where a row is not below L (every lane takes part).
-  template <typename F, typename G>
-  __device__ __forceinline__ void each(int c_lo, int c_hi, F&& inner, G&& edge) const {
-#pragma unroll 2
     for (int i = 0; i < n; ++i) {
-      const int j = row0 + i * 32;
-      if (j >= c_lo && j + 32 <= c_hi) inner(j + lane, key[j + lane]);
-      else edge(j + lane, j + lane < L ? key[j + lane] : 0u);
+      const int j = row0 + i * 128;
+      const float4 v = next;
+      if (i + 1 < n) next = load(j + 128);
+      const uint32_t key[4] = {weight_key(v.x), weight_key(v.y), weight_key(v.z), weight_key(v.w)};
+      f(j, key);
     }
   }
+  // One bit to a row of j .. j + 3: which are below `end`, and which are candidates.
+  static __device__ __forceinline__ uint32_t below(int j, int end) { return 15u >> min(max(j + 4 - end, 0), 4); }
+  __device__ __forceinline__ uint32_t candidates(int j) const { return below(j, c_hi) & ~below(j, c_lo); }
 };
 
-// One digit of the radix select: among the candidates [c_lo, c_hi) that match `prefix` under `mask`,
-// finds the digit that holds the k-th largest (k >= 1, at most the number of matches) and what is left
-// of k inside it.  Called by the whole block; the result is the same in every thread.
-template <int THREADS, int BITS>
-__device__ __forceinline__ void select_digit(const WarpRows& rows, int c_lo, int c_hi, int shift, uint32_t& prefix,
-                                             uint32_t& mask, uint32_t& k, uint32_t* hist, uint32_t* wsum,
-                                             uint32_t* found) {
+// Set bits of the lower lanes' words, and of all lanes'.
+__device__ __forceinline__ uint32_t before_lane(uint32_t bits, uint32_t& all) {
+  const uint32_t own = __popc(bits);
+  uint32_t incl = own;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const uint32_t n = __shfl_up_sync(0xffffffffu, incl, o);
+    if (static_cast<int>(threadIdx.x & 31) >= o) incl += n;
+  }
+  all = __shfl_sync(0xffffffffu, incl, 31);
+  return incl - own;
+}
+
+// One digit of the radix select: count(add) calls add(key) for the keys that it may lie in, of which those that match
+// `prefix` under `mask` are counted; finds the digit that holds the k-th largest of them (k >= 1, at most
+// their number), what is left of k inside it, and how many keys share it.  Called by the whole block; the
+// results are the same in every thread.
+template <int THREADS, int BITS, typename F>
+__device__ __forceinline__ void select_digit(F&& count, int shift, uint32_t& prefix, uint32_t& mask, uint32_t& k,
+                                             uint32_t& shared, uint32_t* hist, uint32_t* wsum, uint32_t* found) {
   constexpr int kBins = 1 << BITS;
   constexpr int kPer = kBins / THREADS >= 4 ? kBins / THREADS : 4;  // bins per thread, from the top
   const int tid = threadIdx.x;
-  for (int i = tid; i < kBins; i += THREADS) hist[i] = 0;
+  for (int i = 4 * tid; i < kBins; i += 4 * THREADS) *reinterpret_cast<uint4*>(hist + i) = make_uint4(0, 0, 0, 0);
   __syncthreads();
-  auto count = [&](uint32_t key) {
+  count([&](uint32_t key) {
     if ((key & mask) == prefix) atomicAdd(&hist[(key >> shift) & (kBins - 1)], 1u);
-  };
-  rows.each(c_lo, c_hi, [&](int, uint32_t key) { count(key); },
-            [&](int j, uint32_t key) {
-              if (j >= c_lo && j < c_hi) count(key);
-            });
+  });
   __syncthreads();
   uint32_t loc[kPer], sum = 0;
 #pragma unroll
@@ -138,6 +149,7 @@ __device__ __forceinline__ void select_digit(const WarpRows& rows, int c_lo, int
       if (above < k && k <= above + loc[i]) {
         found[0] = static_cast<uint32_t>(kBins - 1 - (tid * kPer + i));
         found[1] = k - above;
+        found[2] = loc[i];
       }
       above += loc[i];
     }
@@ -146,17 +158,27 @@ __device__ __forceinline__ void select_digit(const WarpRows& rows, int c_lo, int
   prefix |= found[0] << shift;
   mask |= static_cast<uint32_t>(kBins - 1) << shift;
   k = found[1];
+  shared = found[2];
   __syncthreads();
 }
+
+// Rows of an instance that a block has room for: 8 runs of 128 rows to a warp.
+template <int THREADS>
+constexpr int kMostRows = 32 * THREADS;
 
 // Selection: kept, len_out, into other buffers the zeros of weights_out, and in `plan` the number of kept
 // rows (-1 for a length out of range) and the first of them that has to move.
 template <int THREADS>
 __global__ void __launch_bounds__(THREADS, 2048 / THREADS) evict_select_kernel(Shape s, EvictArgs a) {
-  extern __shared__ uint32_t keys[];  // [cap]
-  constexpr int kWarps = THREADS / 32;
+  constexpr int kWarps = THREADS / 32, kList = 5 * THREADS / 2;
+  constexpr int kLow = 20;  // bits of a key below its first digit
+  constexpr uint32_t kLowMask = (1u << kLow) - 1u;
+  constexpr uint32_t kRanked = 128;  // keys that are compared with one another
   __shared__ __align__(16) uint32_t hist[kEvBins];
-  __shared__ uint32_t wsum[kWarps], found[2];
+  __shared__ uint32_t list[kList];  // keys with the first digit of T, without it
+  __shared__ uint16_t list_row[kList];
+  __shared__ __align__(4) uint8_t kinds[kMostRows<THREADS> / 4];  // of rows 4 i .. 4 i + 3: bits kept, bits equal to T
+  __shared__ uint32_t wsum[kWarps], found[3], n_list;
   __shared__ uint32_t w_tie[kWarps], w_keep[kWarps];
   __shared__ int first_sh;
   const int e = blockIdx.x;
@@ -174,93 +196,184 @@ __global__ void __launch_bounds__(THREADS, 2048 / THREADS) evict_select_kernel(S
     }
     return;
   }
-  const bool in_place = a.K_out == a.K;
-  const float* w_in = a.weights + static_cast<size_t>(e) * s.cap;
-  float* w_out = a.weights_out + static_cast<size_t>(e) * a.cap_out;
   const int n_keep = min(L, a.budget);
-
-  WarpRows rows;
-  rows.key = keys;
-  rows.L = L;
-  rows.n = (L + kWarps * 32 - 1) / (kWarps * 32);
-  rows.row0 = warp * rows.n * 32;
-  rows.lane = lane;
-  rows.init(w_in);
-  if (tid == 0) first_sh = n_keep;
-  uint32_t T = 0, ties = 0;
-  const int c_lo = s.n_prefix, c_hi = L - s.W;
-  const bool all = L <= a.budget;
-  const int k_sel = a.budget - s.n_prefix - s.W;
-  if (!all && k_sel > 0) {
-    uint32_t prefix = 0, mask = 0, k = static_cast<uint32_t>(k_sel);
-    select_digit<THREADS, 12>(rows, c_lo, c_hi, 20, prefix, mask, k, hist, wsum, found);
-    select_digit<THREADS, 10>(rows, c_lo, c_hi, 10, prefix, mask, k, hist, wsum, found);
-    select_digit<THREADS, 10>(rows, c_lo, c_hi, 0, prefix, mask, k, hist, wsum, found);
-    T = prefix;
-    ties = k;
+  if (tid == 0) {
+    first_sh = n_keep;
+    n_list = 0;
   }
-  // 0: not kept, 1: kept, 2: kept if it is among the first `ties` rows equal to T
-  auto kind = [&](int j, uint32_t key) -> int {
-    if (j >= L) return 0;
-    if (all || j < c_lo || j >= c_hi) return 1;
-    if (k_sel <= 0) return 0;
-    return key > T ? 1 : (key == T ? 2 : 0);
-  };
-  uint32_t n_tie = 0, n_sure = 0;
-  const int in_lo = all || k_sel <= 0 ? L : c_lo;  // no inner rows where nothing is selected by weight
-  rows.each(in_lo, c_hi,
-            [&](int, uint32_t key) {
-              n_tie += key == T;
-              n_sure += key > T;
-            },
-            [&](int j, uint32_t key) {
-              const int c = kind(j, key);
-              n_tie += c == 2;
-              n_sure += c == 1;
-            });
-  n_tie = __reduce_add_sync(0xffffffffu, n_tie);
-  n_sure = __reduce_add_sync(0xffffffffu, n_sure);
-  if (lane == 0) {
-    w_tie[warp] = n_tie;
-    w_keep[warp] = n_sure;
-  }
-  __syncthreads();
-  uint32_t tie_at = 0, at = 0;
+  if (L <= a.budget) {
+    for (int j = tid; j < L; j += THREADS) kept_e[j] = j;
+  } else {
+    WarpRows rows;
+    rows.w = a.weights + static_cast<size_t>(e) * s.cap;
+    rows.n = (L + kWarps * 128 - 1) / (kWarps * 128);
+    rows.row0 = warp * rows.n * 128 + lane * 4;
+    rows.L = L;
+    rows.aligned = (reinterpret_cast<uintptr_t>(a.weights) & 15) == 0 && (s.cap & 3) == 0;
+    rows.c_lo = s.n_prefix;
+    rows.c_hi = L - s.W;
+    // Of the candidates those above T are kept, and the first `ties` of those equal to it.
+    uint32_t T = 0xFFFFFFFFu, ties = 0, in_list = 0;
+    uint32_t top = T, low = T;  // keys above top are kept, those from low to top depend on the digits to come
+    const int k_sel = a.budget - s.n_prefix - s.W;
+    const auto count_rows = [&](auto&& add) {
+      rows.each([&](int j, const uint32_t (&key)[4]) {
+        const uint32_t candidates = rows.candidates(j);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (candidates >> c & 1) add(key[c]);
+      });
+    };
+    uint32_t prefix = 0, mask = 0, k = static_cast<uint32_t>(k_sel), shared;
+    if (k_sel > 0) {
+      static_assert(kLow == 20, "digits of 12, 10 and 10 bits");
+      select_digit<THREADS, 12>(count_rows, kLow, prefix, mask, k, shared, hist, wsum, found);
+      if (shared <= kList) {
+        in_list = shared;
+        low = prefix;
+        top = prefix | kLowMask;
+      } else {
 #pragma unroll 1
-  for (int v = 0; v < warp; ++v) {
-    const uint32_t t = w_tie[v];
-    at += w_keep[v] + min(t, ties > tie_at ? ties - tie_at : 0u);
-    tie_at += t;
-  }
-  const uint32_t below = (1u << lane) - 1u;
-  bool moves = false;  // a row of this warp that has to move was seen
-  auto put = [&](int j, bool sure, bool tie) {
-    bool keep = sure;
-    if (n_tie) {
-      const uint32_t tie_mask = __ballot_sync(0xffffffffu, tie);
-      keep = sure || (tie && tie_at + __popc(tie_mask & below) < ties);
-      tie_at += __popc(tie_mask);
-    }
-    const uint32_t keep_mask = __ballot_sync(0xffffffffu, keep);
-    const int pos = static_cast<int>(at + __popc(keep_mask & below));
-    if (keep && in_bounds(pos, n_keep, a.err)) kept_e[pos] = j;
-    if (!moves) {  // rows before the first one that moves stand where they belong
-      const uint32_t m = __ballot_sync(0xffffffffu, keep && pos != j);
-      if (m) {
-        moves = true;
-        if (lane == __ffs(m) - 1) atomicMin(&first_sh, pos);
+        for (int shift = 10; shift >= 0; shift -= 10)
+          select_digit<THREADS, 10>(count_rows, shift, prefix, mask, k, shared, hist, wsum, found);
+        low = top = T = prefix;
+        ties = k;
       }
     }
-    at += __popc(keep_mask);
-  };
-  rows.each(in_lo, c_hi, [&](int j, uint32_t key) { put(j, key > T, key == T); },
-            [&](int j, uint32_t key) {
-              const int c = kind(j, key);
-              put(j, c == 1, c == 2);
-            });
+    uint32_t n_tie = 0, n_sure = 0;
+    rows.each([&](int j, const uint32_t (&key)[4]) {
+      uint32_t above = 0, from = 0;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        above |= static_cast<uint32_t>(key[c] > top) << c;
+        from |= static_cast<uint32_t>(key[c] >= low) << c;
+      }
+      const uint32_t candidates = rows.candidates(j), open = from & ~above & candidates;
+      const uint32_t sure = (above & candidates) | (WarpRows::below(j, L) & ~candidates);
+      n_sure += __popc(sure);
+      kinds[j >> 2] = static_cast<uint8_t>(sure | (in_list ? 0u : open << 4));
+      if (open) {
+        n_tie += __popc(open);
+        if (in_list) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            if (open >> c & 1) {
+              const uint32_t at = atomicAdd(&n_list, 1u);
+              if (at < kList) {
+                list[at] = key[c] & kLowMask;
+                list_row[at] = static_cast<uint16_t>(j + c);
+              }
+            }
+          }
+        }
+      }
+    });
+    n_tie = __reduce_add_sync(0xffffffffu, n_tie);
+    n_sure = __reduce_add_sync(0xffffffffu, n_sure);
+    if (lane == 0) {
+      w_tie[warp] = in_list ? 0 : n_tie;
+      w_keep[warp] = n_sure;
+    }
+    __syncthreads();
+    if (in_list) {
+      const uint32_t digit = prefix;
+      if (in_list <= kRanked) {
+        for (uint32_t i = tid; i < in_list; i += THREADS) {
+          const uint32_t mine = list[i];
+          uint32_t above = 0, equal = 0;
+#pragma unroll 4
+          for (uint32_t u = 0; u < in_list; ++u) {
+            above += list[u] > mine;
+            equal += list[u] == mine;
+          }
+          if (above < k && k <= above + equal) {
+            found[0] = mine;
+            found[1] = k - above;
+          }
+        }
+        __syncthreads();
+        T = digit | found[0];
+        ties = found[1];
+      } else {
+        const auto count_list = [&](auto&& add) {
+          for (uint32_t i = tid; i < in_list; i += THREADS) add(digit | list[i]);
+        };
+#pragma unroll 1
+        for (int shift = 10; shift >= 0; shift -= 10)
+          select_digit<THREADS, 10>(count_list, shift, prefix, mask, k, shared, hist, wsum, found);
+        T = prefix;
+        ties = k;
+      }
+      const uint32_t run = static_cast<uint32_t>(rows.n) * 128u;
+      for (uint32_t i = tid; i < in_list; i += THREADS) {
+        const uint32_t key = digit | list[i], row = list_row[i] % kMostRows<THREADS>;
+        if (key >= T) {
+          const uint32_t bit = (row >> 2 & 3u) * 8u + (row & 3u) + (key > T ? 0u : 4u);
+          atomicOr(reinterpret_cast<uint32_t*>(kinds) + (row >> 4), 1u << bit);
+          atomicAdd((key > T ? w_keep : w_tie) + min(row / run, kWarps - 1u), 1u);
+        }
+      }
+      __syncthreads();
+    }
+    // this warp's first place among the kept rows, and the ties before it
+    const uint32_t t = lane < kWarps ? w_tie[lane] : 0u;
+    uint32_t tie_at = t, at = 0;
+#pragma unroll
+    for (int o = 1; o < kWarps; o <<= 1) {
+      const uint32_t n = __shfl_up_sync(0xffffffffu, tie_at, o);
+      if (lane >= o) tie_at += n;
+    }
+    tie_at -= t;
+    const uint32_t kept_w = lane < kWarps ? w_keep[lane] + min(t, ties > tie_at ? ties - tie_at : 0u) : 0u;
+    at = __reduce_add_sync(0xffffffffu, lane < warp ? kept_w : 0u);
+    tie_at = __shfl_sync(0xffffffffu, tie_at, warp);
+    n_tie = __shfl_sync(0xffffffffu, t, warp);
+
+    bool moves = false;  // a row of this warp that has to move was seen
+#pragma unroll 1
+    for (int i = 0; i < rows.n; ++i) {
+      const int j = rows.row0 + i * 128;
+      const uint32_t kind = kinds[j >> 2], tie = kind >> 4;
+      uint32_t keep = kind & 15u;
+      if (n_tie && __any_sync(0xffffffffu, tie)) {
+        uint32_t all;
+        uint32_t t_at = tie_at + before_lane(tie, all);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (tie >> c & 1) keep |= static_cast<uint32_t>(t_at++ < ties) << c;
+        tie_at += all;
+      }
+      uint32_t all;
+      const int pos = static_cast<int>(at + before_lane(keep, all));
+      if (keep && in_bounds(pos + __popc(keep), n_keep + 1, a.err)) {
+        int to = pos;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (keep >> c & 1) kept_e[to++] = j + c;
+      }
+      if (!moves) {  // rows before the first one that moves stand where they belong
+        int first = n_keep, to = pos;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          if (keep >> c & 1) {
+            if (to != j + c) first = min(first, to);
+            ++to;
+          }
+        }
+        const uint32_t m = __ballot_sync(0xffffffffu, first < n_keep);
+        if (m) {
+          moves = true;
+          if (lane == __ffs(m) - 1) atomicMin(&first_sh, first);
+        }
+      }
+      at += all;
+    }
+  }
   for (int i = n_keep + tid; i < a.budget; i += THREADS) kept_e[i] = -1;
-  if (!in_place)
+  if (a.K_out != a.K) {
+    float* w_out = a.weights_out + static_cast<size_t>(e) * a.cap_out;
     for (int i = n_keep + tid; i < a.cap_out; i += THREADS) w_out[i] = 0.f;
+  }
   __syncthreads();
   if (tid == 0) {
     if (a.len_out) a.len_out[e] = n_keep;
@@ -388,17 +501,14 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(Shape s, Evict
   if (mine) a.weights_out[static_cast<size_t>(e) * a.cap_out + i0 + tid] = w;
 }
 
-// More threads for more rows.  A call with 256, 512 and 1024 threads, 4.3 M rows in all: instances of 1088 rows
-// 51, 63 and 94 us; of 2048 rows 45, 46 and 60; of 4224 rows 47, 45 and 52; of 10240 rows 50, 44 and 45 us;
-// 2.1 M rows, instances of 16384 rows 58, 46 and 41 us, of 32768 rows 86, 62 and 50 us.
+// More threads for more rows.  A call with 256, 512 and 1024 threads, 4-bit caches of head_dim 64, half or more of the
+// rows evicted, 4.5 M rows in all: instances of 1088 rows 146, 156 and 212 us; of 2048 rows 125, 130 and 157; of 4224
+// rows 122, 123 and 138 (16 instances 21, 18 and 18); of 10240 rows 82 us with 512 and 87 with 1024; 128 instances of
+// 16384 rows 43 and 40 us.
 template <int THREADS>
 cudaError_t select(const Shape& s, const EvictArgs& a, cudaStream_t st) {
-  const size_t smem = sizeof(uint32_t) * s.cap;
-  if (smem > 30 * 1024) {  // with the static 17 KB past the 48 KB that need no opt-in
-    const cudaError_t e = allow_smem<evict_select_kernel<THREADS>>(sizeof(uint32_t) * kMaxCapacity);
-    if (e != cudaSuccess) return e;
-  }
-  evict_select_kernel<THREADS><<<s.n_inst, THREADS, smem, st>>>(s, a);
+  if (s.cap > kMostRows<THREADS>) return cudaErrorInvalidValue;
+  evict_select_kernel<THREADS><<<s.n_inst, THREADS, 0, st>>>(s, a);
   return cudaGetLastError();
 }
 
