@@ -5,7 +5,7 @@
 // key T of the last row that is kept by weight and how many rows equal to T are needed: one pass over the
 // weights counts their first digits, a second one marks the rows that these decide, four bits to four rows, and lists
 // those that share the first digit of T.  The list is short, so that it alone is searched for the other digits and
-// corrects the marks; weights of which more share a digit than the list holds are read in three more
+// corrects the marks; weights of which more share a digit than the list holds are read in two more
 // passes.  A first digit of 12 bits splits an octave into 8 bins: weights that span a few octaves,
 // as softmax sums do, then spread over enough bins that the histogram's atomics seldom
 // meet.  The marked rows are numbered in index order by scans inside each warp and one scan of the warps' totals;
@@ -23,7 +23,7 @@
 // 4224 rows to 4096, selection 32 us, rows 607 us, 4.3 GB at 7.1 TB/s (1.05 of the measured copy
 // rate), in place 701 us for the whole call; 320 instances of 1..32768 rows to 2048, 30.5 and
 // 99 us.  4-bit caches (1.25 d bytes a row, moved in vectors of K, V and scales): the same selections, rows 207 us
-// (1.34 GB, 6.5 TB/s) and 51 us.
+// (1.34 GB, 6.5 TB/s) and 41.5 us.
 #include "bkv_device.cuh"
 #include "bkv_internal.h"
 #include "k_launch.cuh"
@@ -65,9 +65,9 @@ __device__ __forceinline__ uint32_t block_scan(uint32_t v, uint32_t* wsum, uint3
 }
 
 // The rows of one warp, four to a lane: row0 + 128 i + c for i < n and c < 4, in order over the lanes.  each(f) calls
-// f(first row, keys) for them, every lane together; candidates are the rows of [c_lo, c_hi).  The weights are read again
-// in every pass: the first one leaves them in L1 and L2, and without a copy in shared memory a block of 1024 threads
-// has a second one beside it.
+// f(first row, keys) for them, every lane together; candidates are the rows of [c_lo, c_hi).  The weights are read
+// again in every pass: the first one leaves them in L1 and L2, and without a copy in shared memory a block of 1024
+// threads has a second one beside it.
 struct WarpRows {
   const float* w;
   int row0, n, L, c_lo, c_hi;
@@ -394,6 +394,18 @@ struct RowOf {
   }
 };
 
+// 16 bytes of a row, from L2, which fetches 64 bytes with them and not the 128 of its default: a row of a 4-bit cache has
+// pieces of 64 and 32 bytes, and what lies beside them may not be kept.  320 instances of 1..32768 rows to 2048,
+// 4-bit caches of head_dim 128: 140 MB read and 41.5 us, with the default 228 MB and 51 us.
+__device__ __forceinline__ uint4 load_piece(const uint4* p) {
+  uint4 v;
+  asm volatile("ld.global.cg.L2::64B.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p)
+               : "memory");
+  return v;
+}
+
 // Compaction in place: one CTA per instance, the next chunk under way while one is written.
 template <int D, bool FOUR, int kThreads>
 __global__ void __launch_bounds__(kThreads, 1024 / kThreads) evict_move_in_place_kernel(Shape s, EvictArgs a) {
@@ -425,7 +437,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) evict_move_in_place
       if (row < n_rows) {
         int j = __ldcg(kept + row);
         if (!in_bounds(j - row, s.cap - row, a.err)) j = row;  // row <= kept[row] < cap
-        R[u] = __ldcg(base + static_cast<size_t>(j) * stride);
+        R[u] = load_piece(base + static_cast<size_t>(j) * stride);
       }
     }
     if (tid < kChunkRows && i0 + tid < end) {
@@ -490,7 +502,7 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(Shape s, Evict
     if (r < n_rows) {
       int j = rows[r];
       if (!in_bounds(j, s.cap, a.err)) j = i0 + r;
-      R[u] = __ldcg(src + static_cast<size_t>(j) * stride);
+      R[u] = load_piece(src + static_cast<size_t>(j) * stride);
     }
   }
 #pragma unroll
