@@ -472,10 +472,31 @@ AtLayout attend4_layout(const Shape& s, int n_q, bool weights) {
   return l;
 }
 
+namespace {
+
+// With a window: whether every item is one CTA's, which writes its rows' results, with no merge after it.  An even
+// split shares the tiles among all SMs, and then costs a second launch that joins the parts.  Where `lost` counts the
+// tiles by which an item is longer than an even share, a call over long caches, head_dim 128, even and whole: lost 1.6
+// (128 items, window 1024) 4 rows 26.7 and 22.5 us; 2.6 (96 items, window 512) 8 rows 22.5 and 16.4, 128 rows 41.0 and
+// 32.8 us; 2.8 (8 items, window 128) 4 rows 14.4 and 12.3; 3.2 (32 items, window 128) 64 rows 19.5 and 20.4, 128 rows
+// 22.5 and 27.6; 9.5 (8 items, window 1024) 8 rows 16.4 and 18.4 us.  Sequences much shorter than the window would make
+// an even share smaller than what is known here, so windows of many tiles are split as well.
+constexpr int kWholeTiles = 12, kWholeLost = 3;
+bool whole_items(const AttendArgs& a, const AtLayout& l) {
+  const AtPlan& p = l.own;
+  if (a.window <= 0 || p.items > l.sms) return false;
+  const int span = std::min(p.geo.n_q, p.geo.rr);  // queries of a row block
+  const int tiles = (std::min(a.n_sink, p.geo.cap) + kAtTile - 1) / kAtTile + (a.window + span + kAtTile - 2) / kAtTile;
+  return tiles <= kWholeTiles && tiles * (l.sms - p.items) <= kWholeLost * l.sms;
+}
+
+}  // namespace
+
 cudaError_t launch_attend(const Shape& s, const AttendArgs& a, const AtLayout& l, cudaStream_t st) {
   float* lse2 = reinterpret_cast<float*>(a.ws + l.off_lse2);
   float* logits = l.logits ? reinterpret_cast<float*>(a.ws + l.off_logits) : nullptr;
-  auto tiles = [&](const AtPlan& p, const __nv_bfloat16* K, const __nv_bfloat16* V, const int* len, bool own) {
+  const bool whole = whole_items(a, l);
+  auto tiles = [&](AtPlan p, const __nv_bfloat16* K, const __nv_bfloat16* V, const int* len, bool own) {
     CUtensorMap qmap, kmap, vmap;
     const AtGeo& g = p.geo;
     const uint64_t rows = static_cast<uint64_t>(g.I) * g.cap;
@@ -501,6 +522,8 @@ cudaError_t launch_attend(const Shape& s, const AttendArgs& a, const AtLayout& l
       return launch_attend_rows_split(s.d, p, qmap, kmap, restmap, vmap, k, st);
     }
     if (a.window > 0) {
+      if (whole) p.grid = static_cast<int>(p.items);
+      k.geo.whole = whole;
       k.geo.window = a.window;
       k.geo.n_sink = a.n_sink;
       if (g.mb * g.rr > kAtTile) return launch_attend_rows_window(s.d, p, qmap, kmap, vmap, k, st);
@@ -522,6 +545,7 @@ cudaError_t launch_attend(const Shape& s, const AttendArgs& a, const AtLayout& l
 }
 
 cudaError_t launch_attend_merge(const Shape& s, const AttendArgs& a, const AtLayout& l, cudaStream_t st) {
+  if (whole_items(a, l)) return cudaSuccess;  // nothing to join
   MergeArgs m{};
   m.own = l.own.geo;
   m.own.len = a.len;

@@ -113,6 +113,7 @@ struct AtGeo {
   int len_div;    // instance e has length len[e / len_div]
   // With a window a row of limit n sees the keys j < n with j >= n - window or j < n_sink (bkv_attend_window).
   int window, n_sink;
+  int whole;  // with a window: CTA b takes item b and nothing else
   FastDiv by_n_kv, by_m, by_rr, by_mb, by_nr, by_nrb, by_n_q, by_len_div;
 };
 
@@ -236,9 +237,16 @@ __device__ __forceinline__ void at_split(int n, Count&& count, Find&& find, int*
 }
 
 // The split of a source's tiles: by instances where all row blocks of one have the same tiles, else by
-// row blocks.
+// row blocks; or an item to a CTA.
 template <int THREADS, bool WIN = false>
 __device__ __forceinline__ void at_split_tiles(const AtGeo& g, int* scan, AtShare* out) {
+  if (WIN && g.whole) {
+    int e;
+    const int rb = g.by_nrb.mod(blockIdx.x, e), n = at_runs<WIN>(g, at_len(g, e), at_block(g, rb).r0).T;
+    if (threadIdx.x == 0) *out = {{e, rb, 0}, n, 0, n};
+    __syncthreads();
+    return;
+  }
   const bool even = !g.causal || g.n_q == 1;
   auto tiles = [&](int x) {
     const int e = even ? x : g.by_nrb.div(x), len = at_len(g, e);
