@@ -21,7 +21,7 @@
 // Bound by HBM: the kept rows are read and written once (8 d bytes a row), the
 // weights read (4 bytes a cached row) and written.  head_dim 128, cold: 1024 instances of
 // 4224 rows to 4096, selection 32 us, rows 607 us, 4.3 GB at 7.1 TB/s (1.05 of the measured copy
-// rate), in place 701 us for the whole call; 320 instances of 1..32768 rows to 2048, 30.5 and
+// rate), in place 684 us for the whole call; 320 instances of 1..32768 rows to 2048, 30.5 and
 // 99 us.  4-bit caches (1.25 d bytes a row, moved in vectors of K, V and scales): the same selections, rows 207 us
 // (1.34 GB, 6.5 TB/s) and 41.5 us.
 #include "bkv_device.cuh"
@@ -394,8 +394,8 @@ struct RowOf {
   }
 };
 
-// 16 bytes of a row, from L2, which fetches 64 bytes with them and not the 128 of its default: a row of a 4-bit cache has
-// pieces of 64 and 32 bytes, and what lies beside them may not be kept.  320 instances of 1..32768 rows to 2048,
+// 16 bytes of a row, from L2, which fetches 64 bytes with them and not the 128 of its default: a row of a 4-bit cache
+// has pieces of 64 and 32 bytes, and what lies beside them may not be kept.  320 instances of 1..32768 rows to 2048,
 // 4-bit caches of head_dim 128: 140 MB read and 41.5 us, with the default 228 MB and 51 us.
 __device__ __forceinline__ uint4 load_piece(const uint4* p) {
   uint4 v;
@@ -534,7 +534,8 @@ cudaError_t launch_d(const Shape& s, const EvictArgs& a, cudaStream_t st) {
     // An instance's rows move in order, so its block has as many threads as still let the blocks of all
     // instances be on the SMs at once, 1024 threads of 64 registers on each.  A call with blocks of 512 threads,
     // and of this rule's: 16 instances, 32768 rows to 2048, 73 and 60 us; 4224 rows to 4096, 128 instances 138 and
-    // 110 us, 384 instances 343 and 318, 1024 instances 762 and 701, 4608 instances 3216 and 3095 us.
+    // 110 us, 384 instances 343 and 318, 1024 instances 762 and 701, 4608 instances 3216 and 3095 us (with a slower
+    // selection; now 59, 108, 313, 684 and 2977 us).
     const int sms = device_sms();
     const auto move = [&](auto kernel, int threads) { return launch_after(kernel, s.n_inst, threads, 0, st, s, a); };
     return s.n_inst <= sms       ? move(evict_move_in_place_kernel<D, FOUR, 1024>, 1024)
