@@ -26,7 +26,8 @@
 //
 // Warp roles: three load tiles of 128 keys into a ring, K, V and scales each (linear copies, 20 KB a tile at
 // head_dim 128), one prepares the queries of the next segment as operands and joins the warps' sums of the last one,
-// twelve (eight with two blocks of rows, whose accumulators need the registers) take steps of 32 keys in turn.
+// twelve (eight with two blocks of rows, whose accumulators need the registers) take steps of 32 keys in turn
+// (k_ring4.cuh: what a step waits for).
 //
 // Bound by HBM on long caches and by start and end on short ones; 290 instructions a slice, half of them on the
 // integer pipe, which unpacks, leave it there.  head_dim 128, cold: 128 caches of 4097..4224 keys, 4 rows 26.3 us,
@@ -39,6 +40,7 @@
 #include <cuda_fp16.h>
 
 #include "k_attend.cuh"
+#include "k_ring4.cuh"
 
 namespace bkv {
 namespace {
@@ -106,17 +108,17 @@ template <int D, int NB>
 struct Cfg4 {
   // Warps at work on slices, behind three loading ones and one that joins.  Registers: 128 a thread at launch for
   // 16 warps (168 for 12), of which the first four give back what the others take.
-  static constexpr int kWarps = NB == 1 ? 12 : 8, kFirst = 4;
+  using Ring = Ring4<D, NB>;
+  static constexpr int kWarps = Ring::kWarps, kFirst = 4;
   static constexpr int kThreads = 32 * (kFirst + kWarps);
   static constexpr int kRegsFew = NB == 1 ? 80 : 88, kRegsMany = NB == 1 ? 144 : 208;
   static constexpr int kRow = D + 4;  // floats of a joined row, so that a warp's stores meet no bank twice
   static constexpr size_t kJoin = sizeof(float) * kWarps * 8 * NB * kRow;
   // a slot of the ring: a tile's rows of K, V and scales, kPart steps
   static constexpr uint32_t kCodes = kAtTile * D / 2, kScales = kAtTile * D / 4, kSlot = 2 * kCodes + kScales;
-  static constexpr int kPart = kAtTile / kStep;
-  static constexpr int kSlots = D == 64 ? 16 : NB == 1 ? 8 : 7;
+  static constexpr int kPart = Ring::kPart, kSlots = Ring::kSlots;
+  static_assert(kPart == kAtTile / kStep, "a tile's steps");
   static constexpr size_t kSmem = kJoin + static_cast<size_t>(kSlots) * kSlot;
-  static_assert(kWarps % kPart == 0, "a warp takes the same part of every tile of a segment");
 };
 
 // A row block's right operands, by lane: of every group the queries, then the terms of their sums; what a logit of
@@ -406,8 +408,7 @@ __global__ void __launch_bounds__(Cfg4<D, NB>::kThreads, 1) attend4_kernel(Kerne
   // ------------------------------------------------------------------ products
   set_max_regs_inc<C::kRegsMany>();
   const int mine = warp - C::kFirst;
-  int first = mine;  // step of the coming segment that is the warp's first
-  int tiles = 0;     // of the segments before
+  RingWalk<typename C::Ring> ring_at(mine);
   for (int seg = 0; walk.next(g, s); ++seg) {
     const int cols = min(g.rr, g.R - s.r0);       // rows of this block
     const int limit_min = at_limit_min(g, s.len, s.r0), n_steps = steps_of(g, s), len = s.len;
@@ -440,13 +441,17 @@ __global__ void __launch_bounds__(Cfg4<D, NB>::kThreads, 1) attend4_kernel(Kerne
 #pragma unroll
     for (int b = 0; b < NB; ++b) ref[b][0] = ref[b][1] = 0.f;
 
-    int step_no = first;
-    int slot = (tiles + first / C::kPart) % C::kSlots, phase = (tiles + first / C::kPart) / C::kSlots & 1;
+    ring_at.begin();
 #pragma unroll 1
-    for (; step_no < n_steps; step_no += kWarps) {
-      const int j0 = s.t0 * kAtTile + step_no * kStep;
-      wait(&full_bar[slot], phase);
-      const int row = step_no % C::kPart * kStep;  // of the tile
+    for (; ring_at.step < n_steps; ring_at.next()) {
+      const int j0 = s.t0 * kAtTile + ring_at.step * kStep, slot = ring_at.slot;
+      if (!ring_at.there([&](int i, int parity) { return mbar_try_wait(&empty_bar[i], parity); },
+                         [&](int i, int parity) { return mbar_try_wait(&full_bar[i], parity); }))
+        ring_at.await(
+            [&](int i, int parity) { at_wait(&empty_bar[i], parity, abort_flag, a.err, kDevTimeoutEpilogue); },
+            [&](int i, int parity) { at_wait(&full_bar[i], parity, abort_flag, a.err, kDevTimeoutEpilogue); });
+      __syncwarp();
+      const int row = ring_at.step % C::kPart * kStep;  // of the tile
       const unsigned char* at = ring + slot * C::kSlot + row * (D / 2);
       unsigned char* scales = ring + slot * C::kSlot + 2 * C::kCodes + row * (D / 4);
       const int left = len - j0;
@@ -628,14 +633,8 @@ __global__ void __launch_bounds__(Cfg4<D, NB>::kThreads, 1) attend4_kernel(Kerne
       }
       __syncwarp();
       if (lane == 0) mbar_arrive(&empty_bar[slot]);
-      slot += kWarps / C::kPart;
-      if (slot >= C::kSlots) {
-        slot -= C::kSlots;
-        phase ^= 1;
-      }
     }
-    first = step_no - n_steps;
-    tiles += (n_steps + C::kPart - 1) / C::kPart;
+    ring_at.end(n_steps);
 
     // ---- the warp's sums, for the join
     if (seg >= 1) wait(&jempty_bar, (seg - 1) & 1);
