@@ -351,8 +351,10 @@ int bkv_attend_reserve(bkv_ctx* ctx, int32_t n_q, int32_t n_groups, int weights)
  *   low = fp16(min x), step = fp16((max x - low) / 15), both limited to 65504,
  *   codes n = (x - low) / step rounded to the nearest of 0 .. 15 (0 for step 0),
  * ties of each rounding to even, and stands for low + step * n.  An element must
- * be finite; beyond +-65504 it counts as that.  One row takes 1.25 d bytes of K
- * and V together instead of 4 d:
+ * be finite.  The limits are those of low and step, not of the elements: one of 1e5 in
+ * a group from 0 on stands for about 1e5, larger ones for at most low + 15 * 65504.
+ * Where all elements lie within +-65504, so do the numbers that they stand for.  One row
+ * takes 1.25 d bytes of K and V together instead of 4 d:
  *   K4, V4   uint8 [batch][n_kv_heads][capacity][head_dim / 2], words of 32 bits
  *            with eight codes each, the first in the lowest four bits.  Word
  *            t d/32 + g of a row of K4 (t < 4) holds elements 32 g + 8 t ..
@@ -385,7 +387,9 @@ int bkv_unpack4(bkv_ctx* ctx, const void* K4, const void* V4, const void* S4, in
 /*
  * bkv_attend over 4-bit caches: the same formulas, arguments and limits, with
  * K and V the numbers that K4, V4 and S4 stand for.
- * Queries must lie within +-65504, and so must the values that the codes stand for.
+ * Queries must lie within +-65504, and so must the numbers that the codes stand for
+ * (those of rows packed from elements within it do): past it a number counts as it is
+ * or as 65504, by the rows of the call.
  * The logits are those of the values themselves, in fp32.  Up to 96 query rows
  * per KV head (G * n_q; 80 for head_dim 64, 48 with weights) the codes are
  * multiplied as they are, the attention weights and their products with the
