@@ -249,9 +249,12 @@ int attend4(bkv_ctx* ctx, bkv::Attend4Args& a, double scale) {
     u.q = reinterpret_cast<const uint4*>(a.q);
     u.q16 = reinterpret_cast<uint4*>(a.ws + l.off_q);
     u.q_vecs = rows * s.d / 8;
+    u.sc = a.sc;
+    u.row_sc = reinterpret_cast<float*>(a.ws + l.off_row_sc);
     b.q = reinterpret_cast<const __nv_bfloat16*>(u.q16);
     b.K = reinterpret_cast<const __nv_bfloat16*>(u.K);
     b.K_rest = u.K_rest;
+    b.row_sc = u.row_sc;
     b.V = reinterpret_cast<const __nv_bfloat16*>(u.V);
     cudaError_t e;
     {

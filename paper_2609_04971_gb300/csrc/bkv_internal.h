@@ -173,7 +173,10 @@ cudaError_t launch_keep_all(const Shape& s, int L, int budget, int* kept, cudaSt
 struct AttendArgs {
   const __nv_bfloat16* q = nullptr;              // [batch][n_kv * G][n_q][d]
   const __nv_bfloat16 *K = nullptr, *V = nullptr;    // [batch][n_kv][cap][d]
-  const void* K_rest = nullptr;  // where given, q, K and V hold fp16 numbers and the keys are K + K_rest
+  // where given, q, K and V hold fp16 numbers, the keys are K + K_rest, and a query row's own factor of its logits
+  // (to base 2) stands for sc
+  const void* K_rest = nullptr;
+  const float* row_sc = nullptr;
   const __nv_bfloat16 *Kp = nullptr, *Vp = nullptr;  // [groups][n_kv][pcap][d]
   const int* len = nullptr;   // [batch][n_kv]
   const int* plen = nullptr;  // [groups]
@@ -209,7 +212,8 @@ struct Pack4Args {
   int n_inst = 0, n_rows = 0, cap = 0;
   int* err = nullptr;
 };
-// Rows below len as fp16 numbers of the attention: V = V, K = K + K_rest to 2^-22; and q as fp16.
+// Rows below len as fp16 numbers of the attention: V = V, K = K + K_rest to 2^-22; and the rows of q, each times a
+// power of two that row_sc takes back.
 struct Unpack16Args {
   const uint32_t *K4 = nullptr, *V4 = nullptr, *S4 = nullptr;  // [n_inst][cap] rows
   const int* len = nullptr;
@@ -218,6 +222,8 @@ struct Unpack16Args {
   const uint4* q = nullptr;  // q_vecs vectors of bf16
   uint4* q16 = nullptr;
   size_t q_vecs = 0;
+  float sc = 0.f;           // log2(e) * scale
+  float* row_sc = nullptr;  // [rows of q]
 };
 cudaError_t launch_unpack16(int d, const Unpack16Args& a, cudaStream_t st);
 cudaError_t launch_pack4(int d, const Pack4Args& a, cudaStream_t st);    // reads K, V

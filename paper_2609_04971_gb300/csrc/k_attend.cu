@@ -457,7 +457,8 @@ AtLayout attend4_layout(const Shape& s, int n_q, bool weights) {
     l.off_k_rest = l.off_k + cache;
     l.off_v = l.off_k_rest + cache;
     l.off_q = l.off_v + cache;
-    l.bytes = align_up(l.off_q + rows * s.d * 2);
+    l.off_row_sc = align_up(l.off_q + rows * s.d * 2);
+    l.bytes = align_up(l.off_row_sc + rows * sizeof(float));
     return l;
   }
   l.four = true;
@@ -517,6 +518,7 @@ cudaError_t launch_attend(const Shape& s, const AttendArgs& a, const AtLayout& l
     k.err = a.err;
     k.after_prefix = own && l.has_prefix;
     if (a.K_rest) {
+      k.row_sc = a.row_sc;
       CUtensorMap restmap;
       if (encode_rows_bf16(&restmap, a.K_rest, rows, s.d, kAtTile) != CUDA_SUCCESS) return cudaErrorInvalidValue;
       return launch_attend_rows_split(s.d, p, qmap, kmap, restmap, vmap, k, st);

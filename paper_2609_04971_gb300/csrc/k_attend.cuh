@@ -372,6 +372,11 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   return r;
 }
 
+// 2^k for any k (0 below the normal range).
+__device__ __forceinline__ float pow2i(int k) {
+  return k < -126 ? 0.f : __uint_as_float(static_cast<uint32_t>(min(k, 127) + 127) << 23);
+}
+
 // Where one source's kernel leaves what the merge needs.  Segment `cta + item` is the part of an
 // item that a CTA worked on: both rise along the run of all segments, one of them by at least 1 from
 // each segment to the next, so the numbers differ.
@@ -415,6 +420,7 @@ struct AtLayout {
   bool four = false;       // the caches are in 4 bits and the own kernel is that of k_attend4.cu
   bool unpacked = false;   // they are unpacked into the workspace as fp16 numbers, for the rows kernel
   size_t off_k = 0, off_k_rest = 0, off_v = 0, off_q = 0;  // fp16 [batch][n_kv][cap][d], and q
+  size_t off_row_sc = 0;   // fp32 [rows]
   bool logits = false;     // the own kernel stores its logits for the weights
   size_t off_lse2 = 0;     // fp32 [rows]: log2 normalisers
   size_t off_logits = 0;   // fp32 [rows][cap]
@@ -453,6 +459,7 @@ struct AtKernelArgs {
   int whole_is_final;  // an item that one CTA finished writes o and lse itself (no other source)
   int after_prefix;    // launched to overlap the prefix's kernel, which its own work does not need
   float sc;
+  const float* row_sc;  // of fp16 operands: [rows], instead of sc
   __nv_bfloat16* o;
   float* lse;
   float* lse2;

@@ -82,10 +82,6 @@ __device__ __forceinline__ uint32_t max_f16x2(uint32_t a, uint32_t b) {
   return *reinterpret_cast<const uint32_t*>(&m);
 }
 
-// 2^k for any k (0 below the normal range).
-__device__ __forceinline__ float pow2i(int k) {
-  return k < -126 ? 0.f : __uint_as_float(static_cast<uint32_t>(min(k, 127) + 127) << 23);
-}
 // The exponent of a finite x >= 0 (of the smallest normal number below that).
 __device__ __forceinline__ int exponent(float x) {
   return max(1, static_cast<int>(__float_as_uint(x) >> 23)) - 127;

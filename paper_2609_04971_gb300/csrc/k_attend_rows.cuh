@@ -35,8 +35,8 @@
 // exponentials and 0.9 its products; three of a row tile's ten are masked in part (1.4 us of exponentials); from one
 // segment of ten tiles to the next 3 to 4 us pass.
 //
-// With SPLIT q, K and V hold fp16 numbers and the keys are K + K_rest, so S takes twice the products; P is fp16, and
-// its reference moves at 2^15.  512 queries of 32 heads over 32768 keys: 257 us, tensor pipe busy 0.67 of the time.
+// With SPLIT q, K and V hold fp16 numbers, the keys are K + K_rest, so S takes twice the products, and a row's logits
+// have a factor of their own; P is fp16, and its reference moves at 2^15.  512 queries of 32 heads over 32768 keys: 257 us, tensor pipe busy 0.67 of the time.
 #pragma once
 
 #include "k_attend.cuh"
@@ -336,7 +336,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t lane_addr = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t s_addr = tmem + w * kAtTile + lane_addr, o_addr = tmem + C::kO + w * D + lane_addr;
     const int c = w * kRows + lane_row, cols = g.mb * g.rr;  // row of the block
-    const float sc = a.sc;
     const bool wide = (reinterpret_cast<uintptr_t>(a.o) & 31) == 0;  // the caller's o is aligned to 16 bytes at least
     auto wait = [&](uint64_t* bar, uint32_t parity) {  // after an abort every wait returns at once
       at_wait(bar, parity, abort_flag, a.err, kDevTimeoutEpilogue);
@@ -346,6 +345,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // rows see, with a window the first of them, and those that any row of the block sees.
     struct Rows {
       int row, lim, lim_min, lo_max, first, limit_max;
+      float sc;  // of its logits, to base 2
     };
     auto rows_of = [&](const AtSeg& s) {
       Rows r;
@@ -355,6 +355,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       r.lo_max = WIN ? __reduce_max_sync(0xffffffffu, r.lim) - g.window : 0;
       r.first = WIN ? at_first_seen(g, r.lim, at_key0<WIN>(s, s.t0)) : 0;
       r.limit_max = at_limit_max(g, s.len, s.r0);
+      r.sc = SPLIT && r.row >= 0 ? __ldg(a.row_sc + r.row) : a.sc;
       return r;
     };
     AtSeg s, next;
@@ -367,6 +368,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       now = then;
       const int row = now.row, lim = now.lim, lim_min = now.lim_min, lo_max = now.lo_max, first = now.first;
       const int limit_max = now.limit_max;
+      const float sc = SPLIT ? now.sc : a.sc;
       float ref = 0.f, l = 0.f;  // ref: minus the reference
       for (int t = s.t0; t < s.t1; ++t, ++i) {
         const int k0 = at_key0<WIN>(s, t);

@@ -45,6 +45,7 @@ struct WArgs {
   int hp, brow;     // heads per block (1: blocks within a head); rows of a Q box
   const int* len;
   float sc;
+  const float* row_sc;  // of fp16 operands: a row's own factor instead of sc
   const float* lse2;
   float* weights;
   float* parts;     // [2 grid][128]
@@ -143,7 +144,7 @@ struct Desc {
                                                         // prev_ends = 0 where that group needs no help
 };
 
-// SPLIT: q and K hold fp16 numbers, and the keys are sums of two terms.
+// SPLIT: q and K hold fp16 numbers, the keys are sums of two terms, and a row's logits have a factor of their own.
 template <int D, bool SPLIT>
 struct WCfg {
   static constexpr int kBoxes = D / 64;
@@ -165,6 +166,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __shared__ int scan_sh[kThreads / 32];
   __shared__ AtShare share_sh;
   __shared__ __align__(16) float lse_sh[kDescs][kCols];
+  __shared__ __align__(16) float sc_sh[SPLIT ? kDescs : 1][SPLIT ? kCols : 4];
   __shared__ __align__(16) int lim_sh[kDescs][kCols];
   __shared__ Desc desc_sh[kDescs];
   __shared__ __align__(8) uint64_t dfull_bar[kDescs], dempty_bar[kDescs];
@@ -331,21 +333,24 @@ __global__ void __launch_bounds__(kThreads, 1)
       int began = 0;               // unit of the CTA at which the item began
       Desc d;
       d.e = d.j0 = d.len = d.ends = d.part = 0;
-      float lse[kCols / 32], lse_next[kCols / 32];
-      auto fetch = [&](const Unit& v, float(&out)[kCols / 32]) {
+      constexpr int kPerLane = kCols / 32;
+      float lse[kPerLane], lse_next[kPerLane], sc[SPLIT ? kPerLane : 1], sc_next[SPLIT ? kPerLane : 1];
+      auto fetch = [&](const Unit& v, float(&out)[kPerLane], float(&row_sc)[SPLIT ? kPerLane : 1]) {
 #pragma unroll
-        for (int y = 0; y < kCols / 32; ++y) {
+        for (int y = 0; y < kPerLane; ++y) {
           const int c = y * 32 + lane;
-          out[y] = c < v.cols ? a.lse2[static_cast<size_t>(v.e) * a.R + v.r0 + c] : 0.f;
+          const size_t row = static_cast<size_t>(v.e) * a.R + v.r0 + c;
+          out[y] = c < v.cols ? a.lse2[row] : 0.f;
+          if constexpr (SPLIT) row_sc[y] = c < v.cols ? __ldg(a.row_sc + row) : 1.f;
         }
       };
-      fetch(u, lse);
+      fetch(u, lse, sc);
       for (int i = 0; i < n_units; ++i) {
         const int x = i % kDescs;
         Unit v = u;
         if (i + 1 < n_units) {  // the next unit's normalisers are under way while this one is described
           v.next(a);
-          fetch(v, lse_next);
+          fetch(v, lse_next, sc_next);
         }
         if (from_start && u.k == 0 && lane == 0) a.u0[static_cast<size_t>(u.e) * a.tiles + u.t] = share.u + i;
         if (i >= kDescs &&
@@ -357,6 +362,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int c = y * 32 + lane;
           // a row that sees nothing has -inf, and its columns are masked: any finite number will do
           lse_sh[x][c] = lse[y] == -INFINITY ? 0.f : -lse[y];
+          if constexpr (SPLIT) sc_sh[x][c] = sc[y];
           // columns without a row see nothing
           lim_sh[x][c] = c < u.cols ? u.len - a.n_q + 1 + (a.hp > 1 ? a.by_n_q.mod(c) : u.i0 + c) : 0;
         }
@@ -376,7 +382,10 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         u = v;
 #pragma unroll
-        for (int y = 0; y < kCols / 32; ++y) lse[y] = lse_next[y];
+        for (int y = 0; y < kPerLane; ++y) {
+          lse[y] = lse_next[y];
+          if constexpr (SPLIT) sc[y] = sc_next[y];
+        }
       }
     }
   } else if (warp >= 4) {
@@ -433,9 +442,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       float2 s0 = make_float2(0.f, 0.f), s1 = s0;
       auto add4 = [&](const float* y, int c) {
         const float4 l = *reinterpret_cast<const float4*>(&lse_sh[x][c]);  // minus the normalisers
-        const float2 sc2 = make_float2(sc, sc);
-        const float2 a0 = fma2(make_float2(y[0], y[1]), sc2, make_float2(l.x, l.y));
-        const float2 a1 = fma2(make_float2(y[2], y[3]), sc2, make_float2(l.z, l.w));
+        float2 f0 = make_float2(sc, sc), f1 = f0;
+        if constexpr (SPLIT) {
+          const float4 f = *reinterpret_cast<const float4*>(&sc_sh[x][c]);
+          f0 = make_float2(f.x, f.y);
+          f1 = make_float2(f.z, f.w);
+        }
+        const float2 a0 = fma2(make_float2(y[0], y[1]), f0, make_float2(l.x, l.y));
+        const float2 a1 = fma2(make_float2(y[2], y[3]), f1, make_float2(l.z, l.w));
         s0 = add2(s0, make_float2(ex2_approx(a0.x), ex2_approx(a0.y)));
         s1 = add2(s1, make_float2(ex2_approx(a1.x), ex2_approx(a1.y)));
       };
@@ -525,6 +539,7 @@ cudaError_t launch_attend_weights(const Shape& s, const AttendArgs& a, const AtL
   w.brow = w.hp > 1 ? w.hp * a.n_q : (a.n_q < kCols ? a.n_q : kCols);
   w.len = a.len;
   w.sc = a.sc;
+  w.row_sc = a.row_sc;
   w.lse2 = reinterpret_cast<const float*>(a.ws + l.off_lse2);
   w.weights = a.weights;
   w.parts = reinterpret_cast<float*>(a.ws + l.off_wpart);

@@ -15,6 +15,8 @@
 // cold: packed in 58.5 us (199 MB, 3.4 TB/s; some 140 instructions to eight elements), read back in 35 us (5.6 TB/s).
 #include <cuda_fp16.h>
 
+#include <cfloat>
+
 #include "bkv_device.cuh"
 #include "bkv_internal.h"
 #include "k_attend.cuh"
@@ -204,6 +206,7 @@ __global__ void __launch_bounds__(kPackThreads) pack4_kernel(Pack4Args a, FastDi
 
 // For the attention of many rows: its operands are fp16 numbers, and a key, of up to 15 significant bits beside low's
 // 11, is a sum of two.
+constexpr int kQueryTop = 14, kLeastQuery = -112;  // exponents of a scaled row's largest element, of the least one's
 __device__ __forceinline__ float to_f16_range(float v) { return fminf(fmaxf(v, -kHalfMax), kHalfMax); }
 __device__ __forceinline__ void values16(uint32_t codes, uint32_t scale, uint4& hi, uint4& rest) {
   const float step = __half2float(__ushort_as_half(static_cast<unsigned short>(scale & 0xFFFFu))),
@@ -226,15 +229,28 @@ __global__ void __launch_bounds__(kPackThreads) unpack16_kernel(Unpack16Args a, 
   constexpr int T = D / 8, kRows = kPackThreads / T, kGroups = D / 32;
   grid_dependency_wait();
   grid_dependents_go();
-  if (static_cast<int>(blockIdx.x) >= row_blocks) {  // queries
+  if (static_cast<int>(blockIdx.x) >= row_blocks) {
+    // Queries: T threads to a row, which is scaled by a power of two that brings its largest element to
+    // 2^14 .. 2^15.  Elements down to 2^-31 of that are exact, smaller ones off by 2^-39 of it at most.
     const size_t i = static_cast<size_t>(blockIdx.x - row_blocks) * kPackThreads + threadIdx.x;
-    if (i >= a.q_vecs) return;
-    const uint4 v = __ldg(a.q + i);
+    const bool mine = i < a.q_vecs;  // a row's threads all or none
+    const uint4 v = mine ? __ldg(a.q + i) : make_uint4(0, 0, 0, 0);
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t top2 = 0;  // the largest magnitude, as bf16
+#pragma unroll
+    for (int y = 0; y < 4; ++y) top2 = __vmaxu2(top2, w[y] & 0x7FFF7FFFu);
+#pragma unroll
+    for (int x = 1; x < T; x <<= 1) top2 = __vmaxu2(top2, __shfl_xor_sync(0xffffffffu, top2, x));
+    if (!mine) return;
+    const int top = static_cast<int>(max(top2 & 0xFFFFu, top2 >> 16));
+    const int ex = top == 0 ? 0 : max((top >> 7) - 127, kLeastQuery);
+    const float up = pow2i(kQueryTop - ex);
     uint32_t h[4];
 #pragma unroll
-    for (int y = 0; y < 4; ++y) h[y] = pack_f16(to_f16_range(bf16_lo(w[y])), to_f16_range(bf16_hi(w[y])));
+    for (int y = 0; y < 4; ++y) h[y] = pack_f16(bf16_lo(w[y]) * up, bf16_hi(w[y]) * up);
     a.q16[i] = make_uint4(h[0], h[1], h[2], h[3]);
+    // positive and finite, whatever the scale: a factor of 0 would make a hidden key's -inf a NaN
+    if (i % T == 0) a.row_sc[i / T] = fminf(fmaxf(a.sc * pow2i(ex - kQueryTop), FLT_MIN), FLT_MAX);
     return;
   }
   int e;
