@@ -11,7 +11,7 @@
 // number n 2^-24 (a subnormal, or in bits 4..7 16 n 2^-24: up to 2047 the bits of fp16 count linearly), so one
 // AND makes two operands of a tensor-core product; a shift every second.  The queries, scaled to 2^11 by a
 // power of two of each row, are exact in fp16 down to 2^-24 of the row's largest element; p and p step are rounded to
-// fp16 (2^-11 of themselves each; p below some 2^-35 of the largest becomes 0).
+// fp16 (2^-11 of themselves each).
 //
 // Warps, not the tcgen05 unit, hold the operands: m16n8k16 products take the unpacked codes from the registers
 // they are unpacked in, where tcgen05 would need 16-bit copies of every code in shared memory, four times the
@@ -21,8 +21,11 @@
 // of 16 keys: S [16 keys x 8 rows] per block of 8 query rows, P transposed in registers (movmatrix), and
 // O^T [D x 8 rows] += V^T P.  The lows' share of a logit is a product too, of a key's lows and the queries' sums as
 // three fp16 terms (33 bits), and so is their share of the output.  Each warp has its own reference m of a row's
-// logits (base 2), which moves up when a logit exceeds it by more than 4, less an exponent E that keeps
-// p step = 2^(y - m + E) step within fp16 and moves when a step is too large for it.
+// logits (base 2), which moves up when a logit exceeds it by more than 4.  p stands as 2^(y - m + 11), which fp16 holds
+// down to 2^-36 of p = 1.  Where all steps of a slice's values lie in 2^-11 .. 1, as those of values of ordinary size
+// do, or are 0, p step is a product of fp16 numbers, which loses what is below 2^-25 of p = 1 for the smallest of them.
+// Other steps are multiplied in fp32, and the sums of a group of elements then have a power of two of their own that
+// follows the slice's largest p step: neither large steps whose p is small nor small steps take digits from the rest.
 //
 // Warp roles: three load tiles of 128 keys into a ring, K, V and scales each (linear copies, 20 KB a tile at
 // head_dim 128), one prepares the queries of the next segment as operands and joins the warps' sums of the last one,
@@ -39,6 +42,8 @@
 // 7 sequences with weights 57 us and 53).
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "k_attend.cuh"
 #include "k_ring4.cuh"
 
@@ -46,9 +51,11 @@ namespace bkv {
 namespace {
 
 constexpr int kSlice = 16, kStep = 2 * kSlice;  // keys of a product, of a warp's step
-constexpr float kAbove4 = 4.f;                  // log2 of how far p may exceed 2^E
-constexpr float kStepTop = 2048.f;              // step 2^E stays at or below it
-constexpr int kMostUp = 11;                     // E stays at or below it
+constexpr float kAbove4 = 4.f;                  // log2 of how far p may exceed 1
+constexpr float kUp = 11.f;                     // p stands as p 2^kUp, at most 2^15
+constexpr uint32_t kLeastStep = 0x1000, kMostStep = 0x3C00;  // 2^-11 and 1 as fp16: p step is an fp16 product
+constexpr int kProductTop = 14, kProductLow = 8;  // exponents that the largest scaled p step of a slice may have
+constexpr int kLeastScale = -26;                // p step below 2^-51 is nothing beside steps of at least 2^-24
 constexpr float kCodeUnit = 16777216.f;         // a code n stands as n / 2^24
 constexpr float kSumUnit = 64.f;                // sums of queries as fp16 terms are divided by it
 
@@ -77,10 +84,8 @@ __device__ __forceinline__ uint32_t mul_lo(uint32_t a, uint32_t b) {
   const __half2 m = __hmul2(*reinterpret_cast<__half2*>(&a), __low2half2(*reinterpret_cast<__half2*>(&b)));
   return *reinterpret_cast<const uint32_t*>(&m);
 }
-__device__ __forceinline__ uint32_t max_f16x2(uint32_t a, uint32_t b) {
-  const __half2 m = __hmax2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b));
-  return *reinterpret_cast<const uint32_t*>(&m);
-}
+// The groups' exponents, a byte each.
+__device__ __forceinline__ int scale_of(int exps, int i) { return static_cast<int8_t>(exps >> (8 * i)); }
 
 // The exponent of a finite x >= 0 (of the smallest normal number below that).
 __device__ __forceinline__ int exponent(float x) {
@@ -430,10 +435,23 @@ __global__ void __launch_bounds__(Cfg4<D, NB>::kThreads, 1) attend4_kernel(Kerne
     __syncwarp();
     if (lane == 0) mbar_arrive(&qempty_bar[seg & 1]);
 
-    // p = 2^(y - ref): ref is the reference of the column less E
+    // p = 2^(y - ref): ref is the reference of the column less kUp
     float o[NB][kMt][4] = {}, low[NB][4] = {}, l[NB][2] = {}, ref[NB][2];
-    int up = -1000;                         // E; none yet
-    float most = 0.f, most_y = -INFINITY;   // what it allows of a step, and of y - ref
+    int exps = 0;              // o of group i is times 2^-scale_of(i)
+    float most_y = -INFINITY;  // what y - ref may be; no reference yet
+    auto rescale = [&](int now) {
+#pragma unroll
+      for (int i = 0; i < kG; ++i) {
+        const float f = pow2i(scale_of(exps, i) - scale_of(now, i));
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int m = i * (kMt / kG); m < (i + 1) * (kMt / kG); ++m)
+#pragma unroll
+            for (int z = 0; z < 4; ++z) o[b][m][z] *= f;
+      }
+      exps = now;
+    };
 #pragma unroll
     for (int b = 0; b < NB; ++b) ref[b][0] = ref[b][1] = 0.f;
 
@@ -518,7 +536,8 @@ __global__ void __launch_bounds__(Cfg4<D, NB>::kThreads, 1) attend4_kernel(Kerne
         uint32_t vs[2][kG];  // (step, low) of V of keys g and g + 8
 #pragma unroll
         for (int h = 0; h < 2; ++h) load_words(vs[h], scales + (r0 + lg + 8 * h) * (D / 4) + kG * 4);
-        uint32_t lv[2], top2 = 0;  // lows of group g of keys 2 t, 2 t + 1 and 2 t + 8, 2 t + 9; the largest step
+        // lows of group g of keys 2 t, 2 t + 1 and 2 t + 8, 2 t + 9; their largest step and their smallest one but 0
+        uint32_t lv[2], most = 0, least = 0xFFFFFFFFu;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           uint32_t w[2];
@@ -526,12 +545,13 @@ __global__ void __launch_bounds__(Cfg4<D, NB>::kThreads, 1) attend4_kernel(Kerne
           for (int z = 0; z < 2; ++z) {
             w[z] = *reinterpret_cast<const uint32_t*>(scales + (r0 + 8 * h + 2 * lt + z) * (D / 4) + kG * 4 +
                                                       (lg & (kG - 1)) * 4);
-            top2 = max_f16x2(top2, w[z]);
+            most = max(most, w[z] << 16);
+            least = min(least, (w[z] << 16) - 0x10000u);
           }
           lv[h] = __byte_perm(w[0], w[1], 0x7632);
         }
         // ---- to base 2, against the references
-        const float step = half_lo(top2);
+        const bool wide = most > kMostStep << 16 || least < (kLeastStep - 1) << 16;
         float above = -INFINITY;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
@@ -548,18 +568,13 @@ __global__ void __launch_bounds__(Cfg4<D, NB>::kThreads, 1) attend4_kernel(Kerne
         for (int b = 0; b < NB; ++b)
 #pragma unroll
           for (int z = 0; z < 4; ++z) above = fmaxf(above, y[b][z]);
-        if (__any_sync(0xffffffffu, above > most_y || step > most)) {
-          // Move the references to the slice's maxima, and the steps' scale.  A column that sees nothing of a warp's
-          // first slice sees nothing after it either: it stays at the floor.
-          float top = step;
-#pragma unroll
-          for (int m = 1; m < 32; m <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, m));
-          const bool begins = up < -999;
-          const int now = begins || top > most ? min(kMostUp, 9 - exponent(top)) : up;
-          const float back = begins ? kRefFloor : static_cast<float>(up);
-          up = now;
-          most = kStepTop * pow2i(-now);
-          most_y = kAbove4 + static_cast<float>(now);
+        const bool any_wide = __any_sync(0xffffffffu, wide);
+        if (__any_sync(0xffffffffu, above > most_y)) {
+          // Move the references to the slice's maxima.  A column that sees nothing of the slice of a warp's first
+          // reference sees nothing after it either: it stays at the floor.
+          const bool begins = most_y == -INFINITY;
+          const float back = begins ? kRefFloor : kUp;
+          most_y = kAbove4 + kUp;
 #pragma unroll
           for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -567,8 +582,8 @@ __global__ void __launch_bounds__(Cfg4<D, NB>::kThreads, 1) attend4_kernel(Kerne
               float v = fmaxf(y[b][z], y[b][z + 2]);
 #pragma unroll
               for (int m = 4; m < 32; m <<= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, m));
-              // relative to ref: the reference was at `back`; it moves up to v, and 2^E moves to `now`
-              const float by = fmaxf(v, back) - static_cast<float>(now);
+              // relative to ref: the reference was at `back`; it moves up to v
+              const float by = fmaxf(v, back) - kUp;
               const float fac = begins ? 0.f : ex2_approx(-by);
               ref[b][z] += by;
               l[b][z] *= fac;
@@ -584,20 +599,53 @@ __global__ void __launch_bounds__(Cfg4<D, NB>::kThreads, 1) attend4_kernel(Kerne
         }
         // ---- weights
         uint32_t pb[NB][kG][2];
+        auto weigh = [&](auto ordinary) {  // p, its sums, and p step; one piece of code to a case
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          float p[4];
+          for (int b = 0; b < NB; ++b) {
+            float(&p)[4] = y[b];
 #pragma unroll
-          for (int z = 0; z < 4; ++z) p[z] = ex2_approx(y[b][z]);
-          l[b][0] += p[0] + p[2];
-          l[b][1] += p[1] + p[3];
-          const uint32_t p0 = pack_f16(p[0], p[1]), p1 = pack_f16(p[2], p[3]);
+            for (int z = 0; z < 4; ++z) p[z] = ex2_approx(p[z]);
+            l[b][0] += p[0] + p[2];
+            l[b][1] += p[1] + p[3];
+            const uint32_t p0 = pack_f16(p[0], p[1]), p1 = pack_f16(p[2], p[3]);
+            if constexpr (ordinary.value) {
+#pragma unroll
+              for (int i = 0; i < kG; ++i) {
+                pb[b][i][0] = transpose8(mul_lo(p0, vs[0][i]));
+                pb[b][i][1] = transpose8(mul_lo(p1, vs[1][i]));
+              }
+            }
+            mma_f16(low[b], lv[0], 0u, lv[1], 0u, transpose8(p0), transpose8(p1));
+          }
+        };
+        if (!any_wide && exps == 0) {
+          weigh(std::true_type{});
+        } else {
+          weigh(std::false_type{});
+          int now = 0;
 #pragma unroll
           for (int i = 0; i < kG; ++i) {
-            pb[b][i][0] = transpose8(mul_lo(p0, vs[0][i]));
-            pb[b][i][1] = transpose8(mul_lo(p1, vs[1][i]));
+            const float s0 = half_lo(vs[0][i]), s1 = half_lo(vs[1][i]);
+            float m = 0.f;  // a NaN is its column's own matter, and columns without a row are nobody's
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+              for (int z = 0; z < 2; ++z)
+                if (b * 8 + 2 * lt + z < cols) m = fmaxf(m, fmaxf(y[b][z] * s0, y[b][z + 2] * s1));
+            const uint32_t top = __reduce_max_sync(0xffffffffu, __float_as_uint(m));
+            int scale = any_wide ? scale_of(exps, i) : 0;
+            const int ex = exponent(__uint_as_float(top));
+            if (any_wide && top != 0 && (ex - scale > kProductTop || ex - scale < kProductLow))
+              scale = max(kLeastScale, ex - kProductTop);
+            now |= (scale & 255) << (8 * i);
+            const float f0 = s0 * pow2i(-scale), f1 = s1 * pow2i(-scale);
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+              pb[b][i][0] = transpose8(pack_f16(y[b][0] * f0, y[b][1] * f0));
+              pb[b][i][1] = transpose8(pack_f16(y[b][2] * f1, y[b][3] * f1));
+            }
           }
-          mma_f16(low[b], lv[0], 0u, lv[1], 0u, transpose8(p0), transpose8(p1));
+          if (now != exps) rescale(now);
         }
         // ---- values
         uint32_t v[4][D / 64];  // words g D / 64 .. of keys 2 t, 2 t + 1, 2 t + 8, 2 t + 9
@@ -632,6 +680,7 @@ __global__ void __launch_bounds__(Cfg4<D, NB>::kThreads, 1) attend4_kernel(Kerne
     }
     ring_at.end(n_steps);
 
+    if (exps != 0) rescale(0);
     // ---- the warp's sums, for the join
     if (seg >= 1) wait(&jempty_bar, (seg - 1) & 1);
 #pragma unroll

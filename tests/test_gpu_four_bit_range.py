@@ -76,3 +76,67 @@ def test_queries_of_every_magnitude_in_calls_of_many_rows(d, G, n_q, weights):
             ga.check(lse[:, ::2], l64[:, ::2], tl[:, ::2], "lse")
     finally:
         bk.close()
+
+
+def weighted(b, hkv, cap, d, far, V, seed=0):
+    """Caches whose keys have weights by design with queries of ones and the scale ln 2 / d: of every 16 keys 2^0 for one,
+    2^-60 for one, 2^far for the others (rows of one value, exact in fp16); V holds what the test gives it."""
+    y = torch.full((b, hkv, cap), float(far), device=DEV)
+    y[:, :, 3::16] = -60.0
+    y[:, :, 5::16] = 0.0
+    return fb.packed(y[..., None].expand(b, hkv, cap, d).bfloat16(), V.bfloat16())
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("G,n_q", [(4, 1), (3, 4)])
+@pytest.mark.parametrize("what", ["a large row", "large rows", "a large group", "small values", "both"])
+def test_values_of_many_small_weights(d, G, n_q, what):
+    """Keys with zeros as values have all the weight, of the others each 2^-22 of one of these: what they add up to is the
+    output.  Large rows of no weight, a large group of elements and values near fp16's smallest do not take their digits.
+    |o - o64| is as in tests/test_gpu_four_bit.py but for what fp16 rounds below its normal range: p stands as p 2^11
+    against a reference of the row's largest at most, off by 2^-36 of that, of a low; a product of it and a step of
+    2^-11 to 1 by as much, or any by 2^-33 of the largest such product, each times a code of 15 at most."""
+    b, hkv, cap = 1, 2, 20011
+    lens = ga._lens(b, hkv, [cap, 19000])
+    g = torch.Generator(device=DEV).manual_seed(d + G)
+    V = torch.rand(b, hkv, cap, d, generator=g, device=DEV) + 0.5
+    if what == "a large row":
+        V[:, :, 3] = 60000 * torch.sign(torch.randn(d, generator=g, device=DEV))
+    if what in ("large rows", "both"):
+        V[:, :, 3::16] *= 40000.0 * torch.sign(torch.randn(d, generator=g, device=DEV))
+    if what in ("a large group", "both"):
+        V[..., :32] = (V[..., :32] - 0.9) * 50000
+    if what == "small values":
+        V *= 2.0 ** -16
+    if what == "both":
+        V[..., 32:] *= 2.0 ** -12
+    V[:, :, 5::16] = 0
+    cache = weighted(b, hkv, cap, d, -22, V)
+    fb.poison(cache, lens)
+    scale = math.log(2.0) / d
+    q = torch.ones(b, G * hkv, n_q, d, device=DEV).bfloat16()
+    bk = ga._bk(b, G * hkv, hkv, d, cap)
+    try:
+        _, lse, _ = fb.run4(bk, q, cache, lens, scale=scale)
+        o, _ = bk.attend4(q, *cache, length=lens, scale=scale)
+        bk.sync()
+        (o64, l64, _), _ = fb.reference4(q, *cache, lens, scale)
+        for y in range(hkv):
+            n = int(lens[0, y])
+            _, k_sn, k_low = fb.values64(cache[0][0, y, :n], cache[2][0, y, :n], 0)
+            v, sn, low = fb.values64(cache[1][0, y, :n], cache[2][0, y, :n], 1)
+            step = cache[2][0, y, :n, 1, :, 0].double().repeat_interleave(32, -1)
+            ordinary = ((step >= 2.0 ** -11) & (step <= 1)).any(0)
+            for i in range(n_q):
+                m = n - n_q + 1 + i
+                z = k_low[:m, 0] * d * scale
+                p = torch.exp(z - torch.logsumexp(z, 0))
+                delta = 2 * 2.0 ** -16 * float(k_low[:m, 0].abs().max()) * math.log(2.0) + 2.0 ** -14
+                off = ((2.0 ** -10 + 2 * delta) * (p @ sn[:m]) + (2.0 ** -11 + 2 * delta) * (p @ low[:m].abs())
+                       + 2.0 ** -36 * p.max() * (15 * m * ordinary + low[:m].abs().sum(0))
+                       + 15 * m * 2.0 ** -33 * (p[:, None] * step[:m]).amax(0))
+                want = p @ v[:m]
+                for h in range(y * G, (y + 1) * G):
+                    ga.check(o[0, h, i], want, 2.0 ** -8 * want.abs() + off, f"o of {what}")
+    finally:
+        bk.close()
