@@ -140,3 +140,19 @@ def test_values_of_many_small_weights(d, G, n_q, what):
                     ga.check(o[0, h, i], want, 2.0 ** -8 * want.abs() + off, f"o of {what}")
     finally:
         bk.close()
+
+
+@pytest.mark.parametrize("d,G,n_q,weights,many", [
+    (128, 3, 16, True, False), (128, 7, 7, True, True), (64, 16, 3, True, False), (64, 7, 7, True, True),
+    (128, 8, 12, False, False), (128, 1, 97, False, True), (64, 5, 16, False, False), (64, 1, 81, False, True)])
+def test_rows_on_both_sides_of_a_border(d, G, n_q, weights, many):
+    """48 and 49 rows with weights, 96 and 97 without (80 and 81 of head_dim 64): the last that are read code by code, and
+    the first that are read unpacked."""
+    b, hkv, cap = 2, 2, 500
+    lens = ga._lens(b, hkv, [500, 257, 128, 33])
+    q, cache = fb.case(b, G * hkv, hkv, d, cap, n_q, lens, seed=n_q)
+    bk = ga._bk(b, G * hkv, hkv, d, cap)
+    try:
+        fb.run4(bk, q, cache, lens, weights=weights, ref=fb.reference4(q, *cache, lens, many=many))
+    finally:
+        bk.close()
