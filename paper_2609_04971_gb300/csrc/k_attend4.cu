@@ -477,6 +477,17 @@ __global__ void __launch_bounds__(Cfg4<D, NB>::kThreads, 1) attend4_kernel(Kerne
         fence_async_smem();  // the slot is loaded again
         __syncwarp();
       }
+      bool any_wide;  // a step of the values, lane's row by lane, that is none of the ordinary ones
+      {
+        uint32_t w[kG], most = 0, least = 0xFFFFFFFFu;
+        load_words(w, scales + lane * (D / 4) + kG * 4);
+#pragma unroll
+        for (int i = 0; i < kG; ++i) {
+          most = max(most, w[i] << 16);
+          least = min(least, (w[i] << 16) - 0x10000u);  // 0 is the largest
+        }
+        any_wide = __any_sync(0xffffffffu, most > kMostStep << 16 || least < (kLeastStep - 1) << 16);
+      }
 #pragma unroll 1
       for (int r0 = 0; r0 < kStep; r0 += kSlice) {  // rolled: what a short call waits for is instructions
         // ---- logits, in the columns' units
@@ -536,22 +547,17 @@ __global__ void __launch_bounds__(Cfg4<D, NB>::kThreads, 1) attend4_kernel(Kerne
         uint32_t vs[2][kG];  // (step, low) of V of keys g and g + 8
 #pragma unroll
         for (int h = 0; h < 2; ++h) load_words(vs[h], scales + (r0 + lg + 8 * h) * (D / 4) + kG * 4);
-        // lows of group g of keys 2 t, 2 t + 1 and 2 t + 8, 2 t + 9; their largest step and their smallest one but 0
-        uint32_t lv[2], most = 0, least = 0xFFFFFFFFu;
+        uint32_t lv[2];  // lows of group g of keys 2 t, 2 t + 1 and 2 t + 8, 2 t + 9
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           uint32_t w[2];
 #pragma unroll
-          for (int z = 0; z < 2; ++z) {
+          for (int z = 0; z < 2; ++z)
             w[z] = *reinterpret_cast<const uint32_t*>(scales + (r0 + 8 * h + 2 * lt + z) * (D / 4) + kG * 4 +
                                                       (lg & (kG - 1)) * 4);
-            most = max(most, w[z] << 16);
-            least = min(least, (w[z] << 16) - 0x10000u);
-          }
           lv[h] = __byte_perm(w[0], w[1], 0x7632);
         }
         // ---- to base 2, against the references
-        const bool wide = most > kMostStep << 16 || least < (kLeastStep - 1) << 16;
         float above = -INFINITY;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
@@ -568,7 +574,6 @@ __global__ void __launch_bounds__(Cfg4<D, NB>::kThreads, 1) attend4_kernel(Kerne
         for (int b = 0; b < NB; ++b)
 #pragma unroll
           for (int z = 0; z < 4; ++z) above = fmaxf(above, y[b][z]);
-        const bool any_wide = __any_sync(0xffffffffu, wide);
         if (__any_sync(0xffffffffu, above > most_y)) {
           // Move the references to the slice's maxima.  A column that sees nothing of the slice of a warp's first
           // reference sees nothing after it either: it stays at the floor.
