@@ -322,7 +322,8 @@ int bkv_attend_shared(bkv_ctx* ctx, const void* q, int32_t n_q, const void* Kp, 
  * bkv_attend with a sliding window and first tokens that stay visible (sinks):
  * query i, whose own row is row p = len - n_q + i, sees the rows j <= p with
  * j > p - window or j < n_sink, and no others are read (but for what lies in a
- * block of 128 rows with one that is).  A window of 1 is the own row alone.
+ * block of 128 rows with one that is; it may hold anything where no query sees it).
+ * A window of 1 is the own row alone.
  *   window  >= 1;  n_sink >= 0.
  * Everything else is as in bkv_attend, and the workspace is the one that
  * bkv_attend_reserve makes for bkv_attend without weights.  No weights are

@@ -344,7 +344,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // What a thread needs to know of a segment: its row of q, o and lse (or -1), the keys that the row and the warp's
     // rows see, with a window the first of them, and those that any row of the block sees.
     struct Rows {
-      int row, lim, lim_min, lo_max, first, limit_max;
+      int row, lim, lim_min, lo_max, lo_min, first, limit_max;
       float sc;  // of its logits, to base 2
     };
     auto rows_of = [&](const AtSeg& s) {
@@ -353,6 +353,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       r.lim = r.row < 0 ? 0 : at_limit(g, s.len, s.r0, c);
       r.lim_min = __reduce_min_sync(0xffffffffu, r.row < 0 ? 0x7fffffff : r.lim);
       r.lo_max = WIN ? __reduce_max_sync(0xffffffffu, r.lim) - g.window : 0;
+      r.lo_min = WIN ? at_limit_min(g, s.len, s.r0) - g.window : 0;  // of any row of the block
       r.first = WIN ? at_first_seen(g, r.lim, at_key0<WIN>(s, s.t0)) : 0;
       r.limit_max = at_limit_max(g, s.len, s.r0);
       r.sc = SPLIT && r.row >= 0 ? __ldg(a.row_sc + r.row) : a.sc;
@@ -495,8 +496,10 @@ __global__ void __launch_bounds__(kThreads, 1)
           tmem_st32(s_addr + 32, p + 32);
           tmem_wait_st();
         }
-        if (w == 0 && k0 + kAtTile > end && k0 + lane_row >= end) {
-          // rows of V that no row of the item sees must not hold what 0 times it is not 0
+        // Rows of V that no row of the item sees must not hold what 0 times it is not 0: those past the last key, with a
+        // window also those between the first keys and it.
+        const int j = k0 + lane_row;
+        if (w == 0 && (WIN ? j >= end || (j >= g.n_sink && j < now.lo_min) : j >= end)) {
           const int v_pos = kPer * i + kK, st = v_pos % C::kStages;
           at_wait(&full_bar[st], (v_pos / C::kStages) & 1, abort_flag, a.err, kDevTimeoutEpilogue);
 #pragma unroll

@@ -653,8 +653,9 @@ __global__ void __launch_bounds__(kAtThreads, 1)
           } else if (lane == 0) {
             mbar_arrive(&sfree_bar[buf]);
           }
-          if (grp == 0 && k0 + kAtTile > end && j >= end) {
-            // rows of V that no row of the item sees
+          // rows of V that no row of the item sees: past the last key, with a window also between the first ones and it
+          const bool dead = WIN ? j >= end || (j >= g.n_sink && j < limit_min - g.window) : j >= end;
+          if (grp == 0 && (WIN ? masked : k0 + kAtTile > end) && dead) {
             const bool last = i + 1 == n_tiles, turn = t + 1 == s.t1;
             const int vpos = 2 * i + (last || (turn && C::kQBufs == 1) ? 1 : 2);
             const int st = vpos % C::kStages;
