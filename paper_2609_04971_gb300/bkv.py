@@ -692,7 +692,8 @@ class BeaconKV:
         bkv_attend4_reserve(self.ctx, n_q, weights)
 
     def attend4(self, q, K4, V4, S4, *, length, scale=None, weights=None, o_out=None, lse_out=None):
-        """attend over one layer's 4-bit caches (bkv_attend4), which are those of pack4.  Returns (o, lse)."""
+        """attend over one layer's 4-bit caches, which are those of pack4 (bkv_attend4: made for up to some 16 query
+        rows per KV head; with more, attend over bf16 caches is faster).  Returns (o, lse)."""
         _, _, _, lens, rows = self._layer
         k4, v4, s4 = self._cache4(K4, V4, S4, rows)
         lp, wp = _arg(length, torch.int32, lens, "length"), _arg(weights, torch.float32, rows, "weights")

@@ -24,14 +24,15 @@ constexpr int kBlockRows4 = 16;          // the same over 4-bit caches
 // Query rows per KV head up to which a 4-bit cache is read code by code, 16 rows at a time, which takes time by the
 // row; beyond, its rows are unpacked to fp16 first, which does not.  A call in us, by codes and unpacked:
 //   without weights       32 rows     64 rows     80 rows     96 rows     128 rows
-//   128 x 4224          74, 177    122, 178    144, 179    169, 179    212, 181
-//   8 x 32768           48, 101     68, 101     76, 102     89, 103    107, 103
-//   32 x 1024            23, 25      31, 25      33, 27      40, 27      42, 27
-//   128 x 4224, d 64    54, 102     87, 102    101, 103    117, 103    146, 105
+//   128 x 4224          81, 176    131, 177    156, 177    182, 178    230, 181
+//   8 x 32768           51, 100     73, 101     83, 101     95, 101    117, 102
+//   32 x 1024            25, 25      31, 26      36, 25      43, 27      44, 27
+//   128 x 4224, d 64    60, 102     93, 102    110, 102    128, 102    160, 103
 //   with weights          16 rows     32 rows     48 rows     64 rows      96 rows
-//   128 x 4224          66, 225    116, 225    161, 227    208, 228    294, 231
-//   8 x 32768           46, 127     66, 129     91, 129    113, 129    165, 131
-//   32 x 1024            27, 36      36, 32      46, 32      54, 34      72, 35
+//   128 x 4224          66, 225    116, 226    160, 225    204, 227    290, 230
+//   8 x 32768           47, 128     66, 130     91, 128    113, 129    163, 131
+//   32 x 1024            27, 37      36, 32      48, 32      55, 33      72, 37
+// From 16 to 24 rows on bkv_attend over bf16 caches of the same keys is faster than either.
 constexpr int kRows4[2] = {80, 96};  // head_dim 64, 128
 constexpr int kLogitRows4 = 48;      // the same with weights
 // Query rows per KV head up to which the logits are kept for the weights, 4 bytes a row and key written and

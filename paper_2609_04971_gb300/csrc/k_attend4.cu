@@ -32,14 +32,16 @@
 // twelve (eight with two blocks of rows, whose accumulators need the registers) take steps of 32 keys in turn
 // (k_ring4.cuh: what a step waits for).
 //
-// Bound by HBM on long caches and by start and end on short ones; 290 instructions a slice, half of them on the
-// integer pipe, which unpacks, leave it there.  head_dim 128, cold: 128 caches of 4097..4224 keys, 4 rows 26.3 us,
-// 88 MB; of 16896 keys 69 us, 346 MB, 5.0 TB/s; from 4224 to 16896 keys 6.3 TB/s (0.95 of the measured copy rate), so
-// some 14 us are fixed: 2.7 until the first load leaves (the lengths, the split), 2 until it is there, 2 to 3 after the
-// last step, a segment's queries and join in between.  8 rows cost as much as 4; 16 rows 45 us, 32 rows 70 us: eight
-// warps of long dependent chains.  Blocks of 8 rows: 51 and 80 us; twelve warps for two blocks, their operands read
-// from shared memory each time: 52 and 79 us (head_dim 64, operands in registers: 32 rows 52 us and 55, but 28 rows of
-// 7 sequences with weights 57 us and 53).
+// Bound by HBM on long caches and by start and end on short ones; 310 instructions a slice, half of them on the
+// integer pipe, which unpacks, leave it there.  head_dim 128, cold: 128 caches of 4097..4224 keys, 4 rows 27.1 us,
+// 88 MB; of 16896 keys 72 us, 346 MB, 4.8 TB/s; from 4224 to 16896 keys 6.0 TB/s (0.90 of the measured copy rate), so
+// some 14 us do not depend on the bytes: 2.7 until the first load leaves (the lengths, the split), 2 until it is there,
+// 2 to 3 after the last step; what makes up the rest was not measured.  8 rows cost 3 us more than 4; 16 rows 49 us,
+// 32 rows 76 us: eight warps of long dependent chains.  When these took 45 and 70 us, blocks of 8 rows took 51 and
+// 80, twelve warps for two blocks, their operands read from shared memory each time, 52 and 79 (head_dim 64, operands in
+// registers: 32 rows 52 us instead of 55, but 28 rows of 7 sequences with weights 57 instead of 53).  Of that, 0.4 us of
+// a step of 128 caches are the wait for the slot's last tile, and 0.4 the look at the steps of V; where these are none of
+// the ordinary ones, a call over 128 caches of 4224 keys with weights takes 42 us instead of 36.
 #include <cuda_fp16.h>
 
 #include <type_traits>

@@ -144,7 +144,8 @@ __device__ __forceinline__ uint4 values(uint32_t codes, uint32_t scale) {
   return make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
 }
 
-// kBatch rows to a thread, their loads under way together: with one, a prompt's rows took 90 us to pack instead of 4.
+// kBatch rows to a thread, their loads under way together: 295 thousand rows of head_dim 128, with one row to a thread,
+// 71 us to pack and 43 us to read back; with four 61 and 36 us (launches timed by events).
 template <int D, bool PACK>
 __global__ void __launch_bounds__(kPackThreads) pack4_kernel(Pack4Args a, FastDiv by_blocks) {
   constexpr int T = D / 8, kRows = kPackThreads / T;  // threads per row, rows of a pass
