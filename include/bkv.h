@@ -394,7 +394,9 @@ int bkv_unpack4(bkv_ctx* ctx, const void* K4, const void* V4, const void* S4, in
  * The logits are those of the values themselves, in fp32.  Up to 96 query rows
  * per KV head (G * n_q; 80 for head_dim 64, 48 with weights) the codes are
  * multiplied as they are, the attention weights and their products with the
- * steps are rounded to fp16, to within 2^-36 of the row's largest weight at least.
+ * steps are rounded to fp16, small ones to within 2^-36 of the row's largest weight
+ * (where a step of V near by lies outside 2^-11 .. 1, products to within 2^-33 of the
+ * largest one of the rows read together, with 16 keys and 32 elements).
  * More rows read the caches unpacked into the workspace, K as sums of two fp16
  * numbers, V rounded to fp16, query elements below 2^-31 of their row's largest to
  * within 2^-39 of that, and the attention weights are rounded to fp16, small ones to

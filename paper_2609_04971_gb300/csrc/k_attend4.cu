@@ -39,9 +39,9 @@
 // 2 to 3 after the last step; what makes up the rest was not measured.  8 rows cost 3 us more than 4; 16 rows 49 us,
 // 32 rows 76 us: eight warps of long dependent chains.  When these took 45 and 70 us, blocks of 8 rows took 51 and
 // 80, twelve warps for two blocks, their operands read from shared memory each time, 52 and 79 (head_dim 64, operands in
-// registers: 32 rows 52 us instead of 55, but 28 rows of 7 sequences with weights 57 instead of 53).  Of that, 0.4 us of
-// a step of 128 caches are the wait for the slot's last tile, and 0.4 the look at the steps of V; where these are none of
-// the ordinary ones, a call over 128 caches of 4224 keys with weights takes 42 us instead of 36.
+// registers: 32 rows 52 us instead of 55, but 28 rows of 7 sequences with weights 57 instead of 53).  A decode step over
+// 128 caches spends 0.4 us on the waits for a slot's last tile and 0.4 on the look at the steps of V; where these are
+// not the ordinary ones, a call over 128 caches of 4224 keys with weights takes 42 us instead of 36.
 #include <cuda_fp16.h>
 
 #include <type_traits>
