@@ -3,8 +3,8 @@
 // Tiles of kPart steps fill the slots in order, over all segments of a CTA, and a warp takes every kWarps-th step of
 // that run (a segment's last tile may have fewer steps; a warp's steps go on from one segment to the next as if
 // nobody knew of segments).  So a warp uses some tiles of a slot and never sees the others.  A parity wait tells a
-// phase only from its neighbours: one for fill k of a slot's full barrier passes where k fills have landed less one,
-// too.  Before it a warp therefore waits for the slot's empty barrier: fill k - 1 was used up, as the loads themselves
+// phase only from its neighbours: one for fill k of a slot (k fills came before it) also passes where only k - 1 fills
+// have landed.  Before it a warp therefore waits for the slot's empty barrier: fill k - 1 was used up, as the loads themselves
 // wait before fill k.  That wait has one meaning, as
 //   - no more than k fills were used up: the warp's own arrival for fill k is outstanding;
 //   - no fewer than k - 1 were: between two steps of a warp lie kWarps - 1 others, of at most four tiles, so the warp's
@@ -31,7 +31,7 @@ struct Ring4 {
 template <typename R>
 struct RingWalk {
   static_assert(R::kWarps % R::kPart == 0, "a warp takes the same part of every tile of a segment");
-  // Of two steps of a warp that are neighbours, the second's tile is at most 1 + (kWarps - 1 + kPart - 1) / kPart tiles on.
+  // Of two neighbouring steps of a warp the second's tile is at most 1 + (kWarps - 1 + kPart - 1) / kPart tiles on.
   static_assert(R::kSlots >= 2 + (R::kWarps - 1 + R::kPart - 1) / R::kPart, "see above");
   int step;       // of the present segment, the warp's next one
   int tiles = 0;  // of the segments before
